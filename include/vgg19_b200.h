@@ -340,6 +340,57 @@ int vgg19_conv_wgrad_static(const void *x, const void *dz, int32_t batch, int32_
                             int32_t cin, int32_t cout, int32_t dtype, float *dw, float *db,
                             size_t *needed_bytes, void *stream);
 
+/* Log probabilities of rows of logits: what a classifier answers with beyond
+ * its softmax (section 7.1), and what a loss other than the mean cross-entropy
+ * of vgg19_backward is built from.  No handle; any number of classes.  For a
+ * row z with lse = log sum_j exp(z_j), log p_j = z_j - lse:
+ *   logprob[r][i]     log p of class ids[r][i]
+ *   lse[r]            the log-sum-exp
+ *   entropy[r]        -sum_j p_j log p_j
+ *   top_id[r][k], top_logprob[r][k]   the top_k most probable classes, the
+ *                     largest first, the lower index first among equal logits
+ * logits: device, VGG19_FP32 or VGG19_BF16, `rows` rows of `classes` values, row
+ * r at logits + r * ld elements (ld >= classes; any alignment of the element
+ * type).  ids: device int32 [rows][n_ids], n_ids in [0,
+ * VGG19_LOGPROBS_MAX_IDS] (ids and logprob may be NULL for 0).  lse and entropy
+ * may be NULL.  top_k in [0, VGG19_LOGPROBS_MAX_TOP]; it may exceed the number of
+ * classes.  All results are fp32 (top_id int32) and dense; sums are held in fp32.
+ * rows == 0 does nothing.
+ *
+ * An id VGG19_NO_CLASS asks for nothing (a padded row): its logprob is 0.  Any
+ * other id outside [0, classes) is never used as an index: its logprob is NaN
+ * and vgg19_ops_status reports VGG19_ERR_ARG.  A logit of -inf excludes its class:
+ * probability 0, never among the top.  Places of the top list that no class is
+ * left for hold VGG19_NO_CLASS and -inf.  A row whose every logit is -inf has lse
+ * and logprobs -inf and entropy 0.  A row that holds a NaN or +inf gives NaN (and
+ * VGG19_NO_CLASS). */
+#define VGG19_NO_CLASS (-1)
+#define VGG19_LOGPROBS_MAX_TOP 32
+#define VGG19_LOGPROBS_MAX_IDS 256
+int vgg19_logprobs(const void *logits, int32_t dtype, int64_t rows, int32_t classes, int64_t ld, const int32_t *ids,
+                   int32_t n_ids, int32_t top_k, float *logprob, float *lse, float *entropy, int32_t *top_id,
+                   float *top_logprob, void *stream);
+
+/* Gradient with respect to the logits of sum_r (sum_i d_logprob[r][i] *
+ * logprob[r][i] + d_entropy[r] * entropy[r]), from the lse and entropy that
+ * vgg19_logprobs gave:
+ *   d z_j = sum_i g_i [j = ids_i] - p_j (sum_i g_i + w (log p_j + H)).
+ * d_logits: device, the type of logits, row stride d_ld; overwritten.  It may be
+ * logits itself with d_ld == ld.  d_logprob: fp32 [rows][n_ids].  d_entropy: fp32
+ * [rows] or NULL (entropy may then be NULL).  Ids that name no class, VGG19_NO_CLASS
+ * or others, contribute nothing (others are reported as above); a class named
+ * twice gets both shares.  To differentiate the top list, pass its top_id as
+ * ids.  A row whose every logit is -inf has gradient 0. */
+int vgg19_logprobs_backward(const void *logits, int32_t dtype, int64_t rows, int32_t classes, int64_t ld,
+                            const int32_t *ids, int32_t n_ids, const float *lse, const float *entropy,
+                            const float *d_logprob, const float *d_entropy, void *d_logits, int64_t d_ld,
+                            void *stream);
+
+/* Wait for the stream and report, and clear, what the operators without a handle
+ * (vgg19_logprobs and those below it) have recorded on the current device:
+ * VGG19_ERR_ARG for an id outside the classes. */
+int vgg19_ops_status(void *stream);
+
 /* Wait for the stream and report any device-side error recorded so far:
  * VGG19_ERR_DEVICE_TIMEOUT when a bounded wait inside a kernel ran out,
  * VGG19_ERR_ARG when a label outside [0,1000) reached the loss (the label is

@@ -44,6 +44,18 @@ class Net:
         binding.vgg19_forward(self.handle, images, B, logits, probs, stream)
         return logits
 
+    def classify(self, images, top_k=5, stream=None):
+        """The top_k classes of every image, most probable first: (ids int32, log probabilities fp32), [batch][top_k]."""
+        torch = self._torch
+        stream = stream or torch.cuda.current_stream(self.device)
+        B = images.shape[0]
+        with torch.cuda.device(self.device), torch.cuda.stream(stream):
+            logits = self.forward(images, stream=stream)
+            ids = torch.empty(B, top_k, dtype=torch.int32, device=self.device)
+            logprob = torch.empty(B, top_k, dtype=torch.float32, device=self.device)
+            binding.vgg19_logprobs(logits, top_id=ids, top_logprob=logprob, stream=stream)
+        return ids, logprob
+
     def backward(self, images, labels, grads=None, loss=None, logits=None, stream=None):
         torch = self._torch
         B = images.shape[0]

@@ -26,7 +26,10 @@ EXPORTS = (
     "vgg19_set_dense_grads_event", "vgg19_io_bytes", "vgg19_forward_host", "vgg19_forward_host_async", "vgg19_backward_host",
     "vgg19_conv_layer_forward", "vgg19_conv_layer_forward_ex", "vgg19_first_block_forward", "vgg19_conv_layer_backward", "vgg19_conv_layer_backward_ex", "vgg19_dense_layer_forward", "vgg19_dense_layer_backward", "vgg19_saved_tensor", "vgg19_conv_wgrad_static", "vgg19_sync_status", "vgg19_selftest_wait_timeout", "vgg19_launch_count",
     "vgg19_describe", "vgg19_last_error",
+    "vgg19_logprobs", "vgg19_logprobs_backward", "vgg19_ops_status",
 )
+VGG19_NO_CLASS = -1
+VGG19_LOGPROBS_MAX_TOP, VGG19_LOGPROBS_MAX_IDS = 32, 256
 
 
 class vgg19_config(ctypes.Structure):
@@ -57,7 +60,7 @@ def load():
         raise RuntimeError(f"{path} is missing: build it with `python -c 'import __graft_entry__ as g; g.build()'` "
                            "(there is no CPU fallback)")
     L = ctypes.CDLL(path)
-    vp, i32, u64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_size_t
+    vp, i32, i64, u64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t
     cfgp = ctypes.POINTER(vgg19_config)
     sig = {
         "vgg19_create": ([cfgp, u64, ctypes.POINTER(vp)], ctypes.c_int),
@@ -93,6 +96,9 @@ def load():
         "vgg19_launch_count": ([vp, i32, ctypes.POINTER(i32)], ctypes.c_int),
         "vgg19_describe": ([vp, ctypes.c_char_p, sz], ctypes.c_int),
         "vgg19_last_error": ([vp], ctypes.c_char_p),
+        "vgg19_logprobs": ([vp, i32, i64, i32, i64, vp, i32, i32, vp, vp, vp, vp, vp, vp], ctypes.c_int),
+        "vgg19_logprobs_backward": ([vp, i32, i64, i32, i64, vp, i32, vp, vp, vp, vp, vp, i64, vp], ctypes.c_int),
+        "vgg19_ops_status": ([vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
@@ -297,3 +303,98 @@ def vgg19_describe(net):
 
 def vgg19_last_error(net=None):
     return load().vgg19_last_error(net).decode()
+
+
+# ---- operators without a handle -------------------------------------------------------------------------------
+# They take torch CUDA tensors and read sizes, strides and types from them; a tensor that does not fit is refused here,
+# before its address reaches the library.  They run on the tensors' device, whichever is current.  stream as above:
+# None is the legacy default stream.
+
+def _refuse(code, text):
+    raise Vgg19Error(code, text)
+
+
+def _tensor(t, name, dtype, shape, device):
+    """Address of a dense tensor of that type and shape on `device` (of any device where it is None)."""
+    if t.dtype != dtype:
+        _refuse(VGG19_ERR_ARG, f"{name} is {t.dtype}, not {dtype}")
+    if tuple(t.shape) != shape:
+        _refuse(VGG19_ERR_SHAPE, f"{name} is {tuple(t.shape)}, not {shape}")
+    if not t.is_contiguous():
+        _refuse(VGG19_ERR_ARG, f"{name} is not contiguous")
+    if t.device != device:
+        _refuse(VGG19_ERR_ARG, f"{name} is on {t.device}, not on {device}")
+    return t.data_ptr()
+
+
+def _rows_of(t, name):
+    """(storage type, rows, columns, row stride, device) of a 2-d tensor whose rows are dense."""
+    import torch
+    dtype = {torch.float32: VGG19_FP32, torch.bfloat16: VGG19_BF16}.get(t.dtype)
+    if dtype is None:
+        _refuse(VGG19_ERR_ARG, f"{name} is {t.dtype}, neither float32 nor bfloat16")
+    if t.dim() != 2:
+        _refuse(VGG19_ERR_SHAPE, f"{name} has {t.dim()} dimensions, not 2")
+    if not t.is_cuda:
+        _refuse(VGG19_ERR_ARG, f"{name} is on {t.device}, not on a CUDA device")
+    rows, cols = t.shape
+    ld = t.stride(0) if rows > 1 else cols
+    if (cols > 1 and t.stride(1) != 1) or ld < cols:
+        _refuse(VGG19_ERR_ARG, f"{name}: strides {t.stride()}; a row has to be dense and rows must not overlap")
+    return dtype, rows, cols, ld, t.device
+
+
+def _call(device, name, *args):
+    """The entry point, on the tensors' device."""
+    import torch
+    fn = getattr(load(), name)
+    if device.index == torch.cuda.current_device():
+        return _check(None, fn(*args))
+    with torch.cuda.device(device):
+        return _check(None, fn(*args))
+
+
+def vgg19_logprobs(logits, ids=None, logprob=None, lse=None, entropy=None, top_id=None, top_logprob=None, stream=None):
+    """logits [rows][classes] (a row stride is allowed), ids and logprob [rows][n_ids], lse and entropy [rows], top_id and
+    top_logprob [rows][top_k]; what is None is left out."""
+    import torch
+    dtype, rows, classes, ld, dev = _rows_of(logits, "logits")
+    n_ids = 0 if ids is None else ids.shape[-1]
+    top_k = 0 if top_id is None else top_id.shape[-1]
+    if (ids is None) != (logprob is None) or (top_id is None) != (top_logprob is None):
+        _refuse(VGG19_ERR_ARG, "ids goes with logprob, and top_id with top_logprob")
+    f32, i32 = torch.float32, torch.int32
+    return _call(dev, "vgg19_logprobs", logits.data_ptr(), dtype, rows, classes, ld,
+                 None if ids is None else _tensor(ids, "ids", i32, (rows, n_ids), dev), n_ids, top_k,
+                 None if logprob is None else _tensor(logprob, "logprob", f32, (rows, n_ids), dev),
+                 None if lse is None else _tensor(lse, "lse", f32, (rows,), dev),
+                 None if entropy is None else _tensor(entropy, "entropy", f32, (rows,), dev),
+                 None if top_id is None else _tensor(top_id, "top_id", i32, (rows, top_k), dev),
+                 None if top_logprob is None else _tensor(top_logprob, "top_logprob", f32, (rows, top_k), dev),
+                 _stream(stream))
+
+
+def vgg19_logprobs_backward(logits, ids, lse, entropy, d_logprob, d_entropy, d_logits, stream=None):
+    """The gradient at the logits; ids and d_logprob may be None together, and so may d_entropy (entropy then too).
+    d_logits may be logits."""
+    import torch
+    dtype, rows, classes, ld, dev = _rows_of(logits, "logits")
+    d_dtype, d_rows, d_classes, d_ld, d_dev = _rows_of(d_logits, "d_logits")
+    if (d_dtype, d_rows, d_classes, d_dev) != (dtype, rows, classes, dev):
+        _refuse(VGG19_ERR_SHAPE, "d_logits differs from logits in type, shape or device")
+    n_ids = 0 if ids is None else ids.shape[-1]
+    if (ids is None) != (d_logprob is None):
+        _refuse(VGG19_ERR_ARG, "ids goes with d_logprob")
+    f32 = torch.float32
+    return _call(dev, "vgg19_logprobs_backward", logits.data_ptr(), dtype, rows, classes, ld,
+                 None if ids is None else _tensor(ids, "ids", torch.int32, (rows, n_ids), dev), n_ids,
+                 _tensor(lse, "lse", f32, (rows,), dev),
+                 None if entropy is None else _tensor(entropy, "entropy", f32, (rows,), dev),
+                 None if d_logprob is None else _tensor(d_logprob, "d_logprob", f32, (rows, n_ids), dev),
+                 None if d_entropy is None else _tensor(d_entropy, "d_entropy", f32, (rows,), dev),
+                 d_logits.data_ptr(), d_ld, _stream(stream))
+
+
+def vgg19_ops_status(stream=None):
+    """Waits for the stream; raises what the operators without a handle recorded on the current device."""
+    return _check(None, load().vgg19_ops_status(_stream(stream)))

@@ -31,6 +31,12 @@ enum DeviceError : int {
   kDevSplitRange = 65,      // fp32 configuration on tensor cores: an activation beyond fp16's range
 };
 
+// Sets the text vgg19_last_error(NULL) gives and returns `code`: for entry points without a handle.
+int note_error(int code, const char* fmt, ...);
+
+// Reads and clears the device-side error word of the operators without a handle (logprobs.cu).
+cudaError_t logprobs_take_error(int* code);
+
 // ---- CUDA-core kernels (simt_kernels.cu) ---------------------------------
 // T is the storage type of activations and weights (float or bf16); every
 // sum is accumulated in fp32.

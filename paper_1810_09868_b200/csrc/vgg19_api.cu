@@ -19,6 +19,17 @@
 
 using namespace vgg;
 
+static int handle_free_error(int code, const char *text);
+
+int vgg::note_error(int code, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return handle_free_error(code, buf);
+}
+
 namespace {
 
 constexpr int kConvLayers = 16, kFcLayers = 3, kLayers = 19, kClasses = 1000;
@@ -39,7 +50,8 @@ struct FcLayer {
   size_t w_off, b_off;
 };
 
-std::string g_create_error;
+// Text of the last failed call that has no handle, of this thread.
+thread_local std::string g_create_error;
 
 size_t align_up(size_t v, size_t a = 256) { return (v + a - 1) / a * a; }
 
@@ -95,7 +107,8 @@ int fail(vgg19 *n, int code, const char *fmt, ...) {
   va_start(ap, fmt);
   vsnprintf(buf, sizeof buf, fmt, ap);
   va_end(ap);
-  if (n) n->err = buf; else g_create_error = buf;
+  // (an entry point lets no exception out: without memory for the text there is none)
+  try { if (n) n->err = buf; else g_create_error = buf; } catch (...) {}
   return code;
 }
 
@@ -737,7 +750,18 @@ int create_common(const vgg19_config *cfg, vgg19 **out) {
 
 }  // namespace
 
+static int handle_free_error(int code, const char *text) { return fail(nullptr, code, "%s", text); }
+
 extern "C" {
+
+int vgg19_ops_status(void *stream) {
+  cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
+  int code = 0;
+  if (e == cudaSuccess) e = logprobs_take_error(&code);
+  if (e != cudaSuccess) return fail(nullptr, VGG19_ERR_CUDA, "reading the device status failed: %s", cudaGetErrorString(e));
+  if (code) return fail(nullptr, VGG19_ERR_ARG, "an id outside the row's classes (its log probability is NaN)");
+  return VGG19_OK;
+}
 
 int vgg19_create_from_params(const vgg19_config *cfg, const float *host_params, vgg19_t **out) {
   if (!host_params) return fail(nullptr, VGG19_ERR_ARG, "null host_params");
