@@ -63,8 +63,14 @@ enum {
    * operand (an absolute 3e-8 for activations below 0.25).  Activations must stay within fp16's range (65504): one beyond it makes vgg19_sync_status
    * return VGG19_ERR_RANGE.  Backward and training passes keep the CUDA-core kernels.  The paper runs its
    * fp32 network (section 7.2) on CPU and GPU back ends and has no counterpart of this. */
-  VGG19_FLAG_SPLIT_F16 = 16
+  VGG19_FLAG_SPLIT_F16 = 16,
+  /* forward-only passes (vgg19_forward*, vgg19_dense_layer_forward) run the dense layers on 4-bit copies of their
+   * weights, packed by vgg19_q4_pack in groups of VGG19_DENSE_Q4_GROUP and rebuilt with every other copy when the
+   * parameters change: at 224x224 they are 86 % of the parameters, and for a few images reading them is most of
+   * what those layers cost.  Backward and training passes keep the full weights.  Not with VGG19_FLAG_SPLIT_F16. */
+  VGG19_FLAG_DENSE_Q4 = 32
 };
+#define VGG19_DENSE_Q4_GROUP 64
 
 typedef enum {
   VGG19_MODE_FORWARD = 0,  /* vgg19_forward */
@@ -385,6 +391,37 @@ int vgg19_logprobs_backward(const void *logits, int32_t dtype, int64_t rows, int
                             const int32_t *ids, int32_t n_ids, const float *lse, const float *entropy,
                             const float *d_logprob, const float *d_entropy, void *d_logits, int64_t d_ld,
                             void *stream);
+
+/* Dense layers over 4-bit weights, for the few rows of an answer: a dense layer
+ * (section 7.1, dense(W, x, b) = W*x .+ b) whose weights are small integers times
+ * a scale per group of `group` (32, 64 or 128) consecutive weights of a row:
+ *   W[o][k] = scale[o][k / group] * (code[o][k] - 8),  code in 0..15.
+ *
+ * Layout.  Rows come in tiles of 16 and weights in blocks of 128, both padded:
+ * codes is [tiles][blocks][16 rows][64 bytes], where the code of weight k = 32 u +
+ * 8 t + j of a block (u, t in 0..3, j in 0..7) is nibble j (the low one of a byte
+ * first) of the little-endian 32-bit word 4 t + u; scales is bf16
+ * [tiles][blocks][16 rows][128 / group].  In the padding codes are arbitrary and
+ * scales finite (vgg19_q4_pack writes 8 and 0).  Both are 16-byte aligned; the byte counts are
+ * vgg19_q4_code_bytes and vgg19_q4_scale_bytes (0 for sizes that are refused). */
+size_t vgg19_q4_code_bytes(int32_t out, int32_t in);
+size_t vgg19_q4_scale_bytes(int32_t out, int32_t in, int32_t group);
+
+/* Codes and scales of w: device [out][in] with row stride ld, VGG19_FP32 or
+ * VGG19_BF16.  scale = bf16(largest magnitude of the group / 7), code = 8 + the
+ * nearest integer (ties to even) to w / scale within -8..7; all codes 8 where the scale is
+ * 0.  A group that holds a NaN or an infinity gets an infinite scale, which makes its row's results NaN. */
+int vgg19_q4_pack(const void *w, int32_t dtype, int32_t out, int32_t in, int64_t ld, int32_t group, void *codes,
+                  void *scales, void *stream);
+
+/* y = W x + bias, then ReLU if `relu`: x device [rows][in] with row stride ldx, in
+ * `dtype` (VGG19_FP32 or VGG19_BF16); y (or NULL): [rows][out] in that type;
+ * y_f32 (or NULL): the same values as fp32; at least one.  bias: fp32 [out] or NULL.  The products are exact and
+ * summed in fp32 (fp32 activations are taken in full, as three bf16 terms).  Made for up to 16 rows, which read the
+ * weights once; more rows are taken 16 at a time.  rows == 0 does nothing. */
+int vgg19_q4_linear(const void *x, int32_t dtype, int64_t rows, int32_t in, int64_t ldx, const void *codes,
+                    const void *scales, int32_t out, int32_t group, const float *bias, int32_t relu, void *y,
+                    float *y_f32, void *stream);
 
 /* Wait for the stream and report, and clear, what the operators without a handle
  * (vgg19_logprobs and those below it) have recorded on the current device:

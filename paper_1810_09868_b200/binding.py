@@ -16,7 +16,8 @@ VGG19_ERR_ARG, VGG19_ERR_SHAPE, VGG19_ERR_WORKSPACE = -1, -2, -3
 VGG19_ERR_CUDA, VGG19_ERR_DEVICE_TIMEOUT, VGG19_ERR_UNSUPPORTED_ARCH, VGG19_ERR_RANGE = -4, -5, -6, -7
 VGG19_FP32, VGG19_BF16 = 0, 1
 VGG19_FLAG_NO_GRAPH, VGG19_FLAG_NO_TENSOR_CORES, VGG19_FLAG_NO_CTA_PAIRS, VGG19_FLAG_FIRST_FUSION = 1, 2, 4, 8
-VGG19_FLAG_SPLIT_F16 = 16
+VGG19_FLAG_SPLIT_F16, VGG19_FLAG_DENSE_Q4 = 16, 32
+VGG19_DENSE_Q4_GROUP = 64
 VGG19_MODE_FORWARD, VGG19_MODE_BACKWARD, VGG19_MODE_TRAIN = 0, 1, 2
 
 EXPORTS = (
@@ -27,6 +28,7 @@ EXPORTS = (
     "vgg19_conv_layer_forward", "vgg19_conv_layer_forward_ex", "vgg19_first_block_forward", "vgg19_conv_layer_backward", "vgg19_conv_layer_backward_ex", "vgg19_dense_layer_forward", "vgg19_dense_layer_backward", "vgg19_saved_tensor", "vgg19_conv_wgrad_static", "vgg19_sync_status", "vgg19_selftest_wait_timeout", "vgg19_launch_count",
     "vgg19_describe", "vgg19_last_error",
     "vgg19_logprobs", "vgg19_logprobs_backward", "vgg19_ops_status",
+    "vgg19_q4_code_bytes", "vgg19_q4_scale_bytes", "vgg19_q4_pack", "vgg19_q4_linear",
 )
 VGG19_NO_CLASS = -1
 VGG19_LOGPROBS_MAX_TOP, VGG19_LOGPROBS_MAX_IDS = 32, 256
@@ -99,6 +101,10 @@ def load():
         "vgg19_logprobs": ([vp, i32, i64, i32, i64, vp, i32, i32, vp, vp, vp, vp, vp, vp], ctypes.c_int),
         "vgg19_logprobs_backward": ([vp, i32, i64, i32, i64, vp, i32, vp, vp, vp, vp, vp, i64, vp], ctypes.c_int),
         "vgg19_ops_status": ([vp], ctypes.c_int),
+        "vgg19_q4_code_bytes": ([i32, i32], sz),
+        "vgg19_q4_scale_bytes": ([i32, i32, i32], sz),
+        "vgg19_q4_pack": ([vp, i32, i32, i32, i64, i32, vp, vp, vp], ctypes.c_int),
+        "vgg19_q4_linear": ([vp, i32, i64, i32, i64, vp, vp, i32, i32, vp, i32, vp, vp, vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
@@ -393,6 +399,40 @@ def vgg19_logprobs_backward(logits, ids, lse, entropy, d_logprob, d_entropy, d_l
                  None if d_logprob is None else _tensor(d_logprob, "d_logprob", f32, (rows, n_ids), dev),
                  None if d_entropy is None else _tensor(d_entropy, "d_entropy", f32, (rows,), dev),
                  d_logits.data_ptr(), d_ld, _stream(stream))
+
+
+def vgg19_q4_code_bytes(out, in_):
+    return load().vgg19_q4_code_bytes(out, in_)
+
+
+def vgg19_q4_scale_bytes(out, in_, group):
+    return load().vgg19_q4_scale_bytes(out, in_, group)
+
+
+def _q4_buffers(codes, scales, out, in_, group, dev):
+    for t, name, need in ((codes, "codes", vgg19_q4_code_bytes(out, in_)), (scales, "scales", vgg19_q4_scale_bytes(out, in_, group))):
+        if t.device != dev or not t.is_contiguous():
+            _refuse(VGG19_ERR_ARG, f"{name} is on {t.device}, or not contiguous")
+        if t.numel() * t.element_size() < need:
+            _refuse(VGG19_ERR_SHAPE, f"{name} holds {t.numel() * t.element_size()} bytes, {out} x {in_} in groups of {group} take {need}")
+
+
+def vgg19_q4_pack(w, group, codes, scales, stream=None):
+    """w [out][in] (a row stride is allowed) into codes and scales, of vgg19_q4_code_bytes and vgg19_q4_scale_bytes."""
+    dtype, out, in_, ld, dev = _rows_of(w, "w")
+    _q4_buffers(codes, scales, out, in_, group, dev)
+    return _call(dev, "vgg19_q4_pack", w.data_ptr(), dtype, out, in_, ld, group, codes.data_ptr(), scales.data_ptr(), _stream(stream))
+
+
+def vgg19_q4_linear(x, codes, scales, out, group, bias=None, relu=False, y=None, y_f32=None, stream=None):
+    """x [rows][in] (a row stride is allowed); y [rows][out] in x's type and / or y_f32 in fp32."""
+    import torch
+    dtype, rows, in_, ldx, dev = _rows_of(x, "x")
+    _q4_buffers(codes, scales, out, in_, group, dev)
+    return _call(dev, "vgg19_q4_linear", x.data_ptr(), dtype, rows, in_, ldx, codes.data_ptr(), scales.data_ptr(), out, group,
+                 None if bias is None else _tensor(bias, "bias", torch.float32, (out,), dev), int(relu),
+                 None if y is None else _tensor(y, "y", x.dtype, (rows, out), dev),
+                 None if y_f32 is None else _tensor(y_f32, "y_f32", torch.float32, (rows, out), dev), _stream(stream))
 
 
 def vgg19_ops_status(stream=None):

@@ -37,6 +37,15 @@ int note_error(int code, const char* fmt, ...);
 // Reads and clears the device-side error word of the operators without a handle (logprobs.cu).
 cudaError_t logprobs_take_error(int* code);
 
+// Dense layers over 4-bit weights (q4_dense.cu; layout and formulas in the public header).  T: type of w, x and y.
+size_t q4_code_bytes(int out, int in);
+size_t q4_scale_bytes(int out, int in, int group);
+template <typename T>
+cudaError_t q4_pack(const T* w, long ld, int out, int in, int group, void* codes, void* scales, cudaStream_t st);
+template <typename T>
+cudaError_t q4_linear(const T* x, long ldx, long rows, int in, const void* codes, const void* scales, int out, int group,
+                      const float* bias, bool relu, T* y, float* y_f32, cudaStream_t st);
+
 // ---- CUDA-core kernels (simt_kernels.cu) ---------------------------------
 // T is the storage type of activations and weights (float or bf16); every
 // sum is accumulated in fp32.

@@ -1,0 +1,432 @@
+// Dense layers over 4-bit weights with group scales, for a few rows at a time:
+//   y[b][o] = act(sum_g s[o][g] * sum_{k in g} x[b][k] * (code[o][k] - 8) + bias[o]).
+//
+// For few rows the layer is bound by reading its weights, and 4 bits are a quarter of the bf16 copy's bytes.  What
+// stands against that rate is unpacking: 64 codes per lane and KB.  So the products run on the tensor cores
+// (mma.sync m16n8k16, bf16 operands, fp32 sums): a code becomes an exact bf16 value in 1.4 instructions, 16 rows of
+// weights meet up to 8 rows of x per instruction, and the scale is applied once per group, in fp32, to the sum over
+// the group (exact products, so nothing but the sums is rounded).  tcgen05 would need the codes unpacked into shared
+// memory first, a round trip that costs more than the products.  fp32 activations travel as three bf16 terms that
+// add up to them exactly, three products per product.
+//
+// Layout (made by q4_pack, documented in the header): blocks of 16 rows x 128 weights, 1 KB each, in which lane
+// (g, t) of a warp finds with two 16-byte loads what its fragments need: row g (and g + 8), and in each of the four
+// 32-weight groups the eight weights 8 t .. 8 t + 7.  All 16 weights of one instruction's K then lie in one group.
+//
+// A block of four warps owns 16 output rows over a share of K; the shares of a cluster join in its first block
+// through distributed shared memory, in a fixed order: one launch, no scratch.
+#include <cooperative_groups.h>
+#include <cuda_runtime.h>
+
+#include "../../include/vgg19_b200.h"
+#include "common.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace vgg {
+namespace {
+
+constexpr int kWarps = 4, kThreads = kWarps * 32, kUnroll = 4;
+constexpr int kTileRows = 16, kBlockK = 128, kBlockBytes = kTileRows * kBlockK / 2;
+constexpr int kMaxRows = 16;                 // rows of x per launch
+constexpr int kStageBytes = 48 << 10;        // of x in shared memory at a time
+constexpr int kMaxKSplit = 8;
+
+// Two codes, four nibbles apart, become a pair of bf16 values (code - 8) / 16: 0x4100 | code is 8 + code / 16.  (Sixteenths,
+// so that no product is larger than its activation; the factor comes back with the last sum.)
+__device__ __forceinline__ uint32_t codes_to_bf16x2(uint32_t w) {
+  uint32_t v;
+  asm("lop3.b32 %0, %1, 0x000f000f, 0x41004100, 0xea;" : "=r"(v) : "r"(w));  // (w & mask) | magic
+  const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), __nv_bfloat162(__float2bfloat16_rn(8.5f), __float2bfloat16_rn(8.5f)));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+struct Q4Args {
+  const void* x;
+  const uint4* codes;
+  const uint16_t* scales;
+  const float* bias;
+  void* y;
+  float* y_f32;
+  long ldx;
+  int in, out, rows, blocks, ksplit, stage_blocks, relu;
+};
+
+// The terms of eight consecutive activations, each a 16-byte row of bf16 in the order 0 4 1 5 2 6 3 7 (the order in
+// which codes_to_bf16x2 yields them).  fp32: truncated to 8 bits three times, the rest exact each time.
+template <typename T> struct Terms;
+template <> struct Terms<bf16> {
+  static constexpr int N = 1;
+  __device__ static void split(const bf16* v, uint32_t (&out)[1][4]) {
+    const uint16_t* h = reinterpret_cast<const uint16_t*>(v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[0][i] = (uint32_t)h[i] | (uint32_t)h[i + 4] << 16;
+  }
+};
+template <> struct Terms<float> {
+  static constexpr int N = 3;
+  __device__ static void split(const float* v, uint32_t (&out)[3][4]) {
+    uint32_t t[3][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t b = __float_as_uint(v[i]);
+      const bool finite = (b & 0x7f800000u) != 0x7f800000u;
+      const bool nan = (b & 0x7fffffffu) > 0x7f800000u;
+      t[0][i] = nan ? 0x7fc0u : b >> 16;
+      const float r1 = finite ? v[i] - __uint_as_float(b & 0xffff0000u) : 0.f;
+      const uint32_t b1 = __float_as_uint(r1);
+      t[1][i] = b1 >> 16;
+      t[2][i] = __float_as_uint(r1 - __uint_as_float(b1 & 0xffff0000u)) >> 16;
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out[k][i] = t[k][i] | t[k][i + 4] << 16;
+  }
+};
+
+// NT: tiles of eight rows of x.  GROUP: 32, 64 or 128 weights a scale.
+template <typename T, int GROUP, int NT>
+__global__ void __launch_bounds__(kThreads) q4_linear_kernel(const Q4Args a) {
+  constexpr int TERMS = Terms<T>::N, PER = kBlockK / GROUP, USTEP = GROUP / 32;
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ float part[kWarps][NT * 8][kTileRows];
+  __shared__ float cluster_part[kMaxKSplit][NT * 8][kTileRows];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int ks = a.ksplit, rank = ks > 1 ? (int)cluster.block_rank() : 0;
+  if (ks > 1) cluster.barrier_arrive();  // waited for before the first write into the first block's shared memory
+  const int tile = blockIdx.x / ks;
+  const int b0 = (int)((long)a.blocks * rank / ks), b1 = (int)((long)a.blocks * (rank + 1) / ks);
+  const uint4* codes = a.codes + (long)tile * a.blocks * (kBlockBytes / 16);
+  const uint16_t* scales = a.scales + (long)tile * a.blocks * kTileRows * PER;
+  const int stride = a.stage_blocks * kBlockK * 2 + 64;  // bytes of a staged row: rows 64 bytes apart modulo 128
+  const long term_bytes = (long)a.rows * stride;
+
+  float acc[NT][4] = {};
+  int xrow[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) xrow[n] = min(n * 8 + g, a.rows - 1) * stride;  // columns past the last row are not used
+
+  for (int c0 = b0; c0 < b1; c0 += a.stage_blocks) {
+    const int c1 = min(c0 + a.stage_blocks, b1);
+    for (int base = c0; base < c1; base += kWarps * kUnroll) {
+      uint4 w[kUnroll][2];
+      uint32_t s[kUnroll][2][2];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const int b = base + u * kWarps + warp;
+        if (b < c1) {
+          const uint4* p = codes + (long)b * (kBlockBytes / 16) + lane;
+          w[u][0] = __ldcs(p);
+          w[u][1] = __ldcs(p + 32);
+          const uint16_t* q = scales + ((long)b * kTileRows + g) * PER;
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            if (PER == 4) {
+              const uint2 v = *reinterpret_cast<const uint2*>(q + r * 8 * PER);
+              s[u][r][0] = v.x; s[u][r][1] = v.y;
+            } else if (PER == 2) {
+              s[u][r][0] = *reinterpret_cast<const uint32_t*>(q + r * 8 * PER);
+            } else {
+              s[u][r][0] = q[r * 8 * PER];
+            }
+          }
+        }
+      }
+      if (base == c0) {
+        // stage this part of x while the first weights are on their way
+        if (c0 != b0) __syncthreads();
+        const int n8 = (c1 - c0) * (kBlockK / 8);
+        for (int i = tid; i < n8 * a.rows; i += kThreads) {
+          const int row = i / n8, k8 = i - row * n8;
+          const long k = (long)c0 * kBlockK + k8 * 8;
+          const T* src = static_cast<const T*>(a.x) + row * a.ldx + k;
+          T v[8];
+          if (k + 8 <= a.in && (reinterpret_cast<uintptr_t>(src) & 15) == 0) {
+#pragma unroll
+            for (int j = 0; j < (int)(8 * sizeof(T) / 16); ++j)
+              reinterpret_cast<uint4*>(v)[j] = __ldg(reinterpret_cast<const uint4*>(src) + j);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = k + j < a.in ? src[j] : from_f32<T>(0.f);
+          }
+          uint32_t o[TERMS][4];
+          Terms<T>::split(v, o);
+#pragma unroll
+          for (int q = 0; q < TERMS; ++q)
+            *reinterpret_cast<uint4*>(smem + q * term_bytes + (long)row * stride + k8 * 16) = make_uint4(o[q][0], o[q][1], o[q][2], o[q][3]);
+        }
+        __syncthreads();
+      }
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const int b = base + u * kWarps + warp;
+        if (b >= c1) break;
+        const unsigned char* xb = smem + (b - c0) * (kBlockK * 2) + t * 16;
+        const uint32_t lo[4] = {w[u][0].x, w[u][0].y, w[u][0].z, w[u][0].w};
+        const uint32_t hi[4] = {w[u][1].x, w[u][1].y, w[u][1].z, w[u][1].w};
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+          float d[NT][4] = {};
+#pragma unroll
+          for (int q = 0; q < USTEP; ++q) {
+            const int v = p * USTEP + q;
+            uint32_t al[4], ah[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              al[i] = codes_to_bf16x2(lo[v] >> (4 * i));
+              ah[i] = codes_to_bf16x2(hi[v] >> (4 * i));
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int m = TERMS - 1; m >= 0; --m) {  // the small terms first
+                const uint4 xv = *reinterpret_cast<const uint4*>(xb + m * term_bytes + xrow[n] + v * 64);
+                mma(d[n], al[0], ah[0], al[1], ah[1], xv.x, xv.y);
+                mma(d[n], al[2], ah[2], al[3], ah[3], xv.z, xv.w);
+              }
+          }
+          const uint32_t s0 = PER == 1 ? s[u][0][0] << 16 : (p & 1) ? s[u][0][p >> 1] & 0xffff0000u : s[u][0][p >> 1] << 16;
+          const uint32_t s1 = PER == 1 ? s[u][1][0] << 16 : (p & 1) ? s[u][1][p >> 1] & 0xffff0000u : s[u][1][p >> 1] << 16;
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            acc[n][0] = fmaf(d[n][0], __uint_as_float(s0), acc[n][0]);
+            acc[n][1] = fmaf(d[n][1], __uint_as_float(s0), acc[n][1]);
+            acc[n][2] = fmaf(d[n][2], __uint_as_float(s1), acc[n][2]);
+            acc[n][3] = fmaf(d[n][3], __uint_as_float(s1), acc[n][3]);
+          }
+        }
+      }
+    }
+  }
+
+  // accumulator: rows g, g + 8 of the tile by columns 2 t, 2 t + 1 of the rows of x
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    part[warp][n * 8 + 2 * t][g] = acc[n][0];
+    part[warp][n * 8 + 2 * t + 1][g] = acc[n][1];
+    part[warp][n * 8 + 2 * t][g + 8] = acc[n][2];
+    part[warp][n * 8 + 2 * t + 1][g + 8] = acc[n][3];
+  }
+  __syncthreads();
+  if (ks > 1) cluster.barrier_wait();
+  for (int i = tid; i < NT * 8 * kTileRows; i += kThreads) {
+    const int n = i / kTileRows, o = i % kTileRows;
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) v += part[k][n][o];
+    if (ks > 1) cluster.map_shared_rank(&cluster_part[0][0][0], 0)[(rank * NT * 8 + n) * kTileRows + o] = v;
+    else part[0][n][o] = v;  // (each element is read and written by one thread)
+  }
+  if (ks > 1) {
+    cluster.sync();
+    if (rank != 0) return;
+  } else {
+    __syncthreads();
+  }
+  for (int i = tid; i < a.rows * kTileRows; i += kThreads) {
+    const int n = i / kTileRows, o = i % kTileRows, col = tile * kTileRows + o;
+    if (col >= a.out) continue;
+    float v = 0.f;
+    if (ks > 1)
+      for (int k = 0; k < ks; ++k) v += cluster_part[k][n][o];
+    else
+      v = part[0][n][o];
+    v *= 16.f;
+    if (a.bias) v += a.bias[col];
+    if (a.relu) v = v < 0.f ? 0.f : v;  // a NaN stays
+    if (a.y) static_cast<T*>(a.y)[(long)n * a.out + col] = from_f32<T>(v);
+    if (a.y_f32) a.y_f32[(long)n * a.out + col] = v;
+  }
+}
+
+// One warp per row and block of 128 weights, four consecutive weights per lane.
+template <typename T>
+__global__ void __launch_bounds__(256) q4_pack_kernel(const T* w, long ld, int out, int in, int blocks, int group, uint8_t* codes, bf16* scales) {
+  const long item = (long)blockIdx.x * 8 + threadIdx.x / 32;
+  const int lane = threadIdx.x & 31;
+  const long total = (long)((out + kTileRows - 1) / kTileRows) * kTileRows * blocks;
+  if (item >= total) return;
+  const int b = (int)(item % blocks);
+  const long row = item / blocks;
+  const int k = b * kBlockK + lane * 4;
+  float v[4] = {};
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (row < out && k + j < in) v[j] = to_f32(w[row * ld + k + j]);
+  float m = 0.f;
+  bool nan = false;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) { m = fmaxf(m, fabsf(v[j])); nan |= v[j] != v[j]; }
+  if (nan) m = INFINITY;  // a group with a NaN or an infinity gets an infinite scale: its row's results become NaN
+  for (int o = 1; o < group / 4; o *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const bf16 sb = __float2bfloat16_rn(m / 7.f);
+  const float s = __bfloat162float(sb);
+  uint32_t c = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float q = s > 0.f && s < INFINITY ? rintf(v[j] / s) : 0.f;
+    q = fminf(fmaxf(q, -8.f), 7.f);
+    c |= (uint32_t)((int)q + 8) << (4 * j);
+  }
+  const int u = lane / 8, t = lane % 8 / 2;
+  const long block = (row / kTileRows) * blocks + b;
+  uint8_t* dst = codes + block * kBlockBytes + (row % kTileRows) * 64 + (4 * t + u) * 4 + (lane & 1) * 2;
+  *reinterpret_cast<uint16_t*>(dst) = (uint16_t)c;
+  if (lane % (group / 4) == 0) scales[(block * kTileRows + row % kTileRows) * (kBlockK / group) + lane / (group / 4)] = sb;
+}
+
+template <typename T, int GROUP, int NT> cudaError_t launch(Q4Args a, cudaStream_t st) {
+  const int tiles = (a.out + kTileRows - 1) / kTileRows;
+  // K is shared by as many blocks as give every SM four, while each warp still has a block of weights
+  a.ksplit = 1;
+  while (a.ksplit < kMaxKSplit && tiles * a.ksplit < 4 * 148 && a.blocks >= 2 * a.ksplit * kWarps) a.ksplit *= 2;
+  const int share = (a.blocks + a.ksplit - 1) / a.ksplit;
+  int stage = kStageBytes / (a.rows * Terms<T>::N * kBlockK * 2);
+  if (stage > share) stage = share;
+  else if (stage > kWarps * kUnroll) stage -= stage % (kWarps * kUnroll);
+  if (stage < 1) stage = 1;
+  a.stage_blocks = stage;
+  const size_t smem = (size_t)a.rows * Terms<T>::N * (stage * kBlockK * 2 + 64);
+  static_assert(kMaxRows * 3 * (kBlockK * 2 + 64) <= kStageBytes, "one block of x fits");
+  auto kernel = q4_linear_kernel<T, GROUP, NT>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kStageBytes + kMaxRows * 3 * 64);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(tiles * a.ksplit));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = (unsigned)a.ksplit;
+  at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+template <typename T, int GROUP> cudaError_t launch_group(const Q4Args& a, cudaStream_t st) {
+  return a.rows > 8 ? launch<T, GROUP, 2>(a, st) : launch<T, GROUP, 1>(a, st);
+}
+
+template <typename T> cudaError_t launch_type(const Q4Args& a, int group, cudaStream_t st) {
+  return group == 32 ? launch_group<T, 32>(a, st) : group == 64 ? launch_group<T, 64>(a, st) : launch_group<T, 128>(a, st);
+}
+
+int shape_checks(int32_t out, int32_t in, int32_t group) {
+  if (out < 1 || in < 1 || out > (1 << 24) || in > (1 << 24))
+    return note_error(VGG19_ERR_SHAPE, "%d x %d weights: both sizes in [1, 2^24]", out, in);
+  if (group != 32 && group != 64 && group != 128) return note_error(VGG19_ERR_ARG, "group %d is none of 32, 64, 128", group);
+  return VGG19_OK;
+}
+
+}  // namespace
+
+size_t q4_code_bytes(int out, int in) {
+  return (size_t)((out + kTileRows - 1) / kTileRows) * ((in + kBlockK - 1) / kBlockK) * kBlockBytes;
+}
+size_t q4_scale_bytes(int out, int in, int group) {
+  return (size_t)((out + kTileRows - 1) / kTileRows) * ((in + kBlockK - 1) / kBlockK) * kTileRows * (kBlockK / group) * 2;
+}
+
+template <typename T>
+cudaError_t q4_pack(const T* w, long ld, int out, int in, int group, void* codes, void* scales, cudaStream_t st) {
+  const int blocks = (in + kBlockK - 1) / kBlockK;
+  const long items = (long)((out + kTileRows - 1) / kTileRows) * kTileRows * blocks;
+  q4_pack_kernel<T><<<(unsigned)((items + 7) / 8), 256, 0, st>>>(w, ld, out, in, blocks, group, static_cast<uint8_t*>(codes),
+                                                                static_cast<bf16*>(scales));
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t q4_linear(const T* x, long ldx, long rows, int in, const void* codes, const void* scales, int out, int group,
+                      const float* bias, bool relu, T* y, float* y_f32, cudaStream_t st) {
+  for (long r = 0; r < rows; r += kMaxRows) {
+    Q4Args a{};
+    a.x = x + r * ldx;
+    a.codes = static_cast<const uint4*>(codes);
+    a.scales = static_cast<const uint16_t*>(scales);
+    a.bias = bias;
+    a.y = y ? y + r * out : nullptr;
+    a.y_f32 = y_f32 ? y_f32 + r * out : nullptr;
+    a.ldx = ldx; a.in = in; a.out = out; a.relu = relu;
+    a.rows = (int)(rows - r < kMaxRows ? rows - r : kMaxRows);
+    a.blocks = (in + kBlockK - 1) / kBlockK;
+    const cudaError_t e = launch_type<T>(a, group, st);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+#define INSTANTIATE(T)                                                                                                    \
+  template cudaError_t q4_pack<T>(const T*, long, int, int, int, void*, void*, cudaStream_t);                             \
+  template cudaError_t q4_linear<T>(const T*, long, long, int, const void*, const void*, int, int, const float*, bool, T*, \
+                                    float*, cudaStream_t);
+INSTANTIATE(float)
+INSTANTIATE(bf16)
+
+}  // namespace vgg
+
+extern "C" {
+
+size_t vgg19_q4_code_bytes(int32_t out, int32_t in) {
+  return vgg::shape_checks(out, in, 32) == VGG19_OK ? vgg::q4_code_bytes(out, in) : 0;
+}
+size_t vgg19_q4_scale_bytes(int32_t out, int32_t in, int32_t group) {
+  return vgg::shape_checks(out, in, group) == VGG19_OK ? vgg::q4_scale_bytes(out, in, group) : 0;
+}
+
+int vgg19_q4_pack(const void* w, int32_t dtype, int32_t out, int32_t in, int64_t ld, int32_t group, void* codes,
+                  void* scales, void* stream) {
+  using namespace vgg;
+  const int rc = shape_checks(out, in, group);
+  if (rc != VGG19_OK) return rc;
+  if (dtype != VGG19_FP32 && dtype != VGG19_BF16)
+    return note_error(VGG19_ERR_ARG, "dtype %d is neither VGG19_FP32 nor VGG19_BF16", dtype);
+  if (!w || !codes || !scales) return note_error(VGG19_ERR_ARG, "weights, codes and scales must not be null");
+  if (ld < in) return note_error(VGG19_ERR_SHAPE, "row stride %lld below %d", (long long)ld, in);
+  if (reinterpret_cast<uintptr_t>(w) % (dtype == VGG19_FP32 ? 4 : 2) || reinterpret_cast<uintptr_t>(codes) % 16 ||
+      reinterpret_cast<uintptr_t>(scales) % 16)
+    return note_error(VGG19_ERR_ARG, "weights are aligned to their type, codes and scales to 16 bytes");
+  if (((long)((out + kTileRows - 1) / kTileRows) * kTileRows * ((in + kBlockK - 1) / kBlockK) + 7) / 8 > 0x7fffffffL)
+    return note_error(VGG19_ERR_SHAPE, "%d x %d weights are too many for one call", out, in);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = dtype == VGG19_BF16 ? q4_pack(static_cast<const bf16*>(w), ld, out, in, group, codes, scales, st)
+                                            : q4_pack(static_cast<const float*>(w), ld, out, in, group, codes, scales, st);
+  return e == cudaSuccess ? VGG19_OK : note_error(VGG19_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+}
+
+int vgg19_q4_linear(const void* x, int32_t dtype, int64_t rows, int32_t in, int64_t ldx, const void* codes,
+                    const void* scales, int32_t out, int32_t group, const float* bias, int32_t relu, void* y,
+                    float* y_f32, void* stream) {
+  using namespace vgg;
+  const int rc = shape_checks(out, in, group);
+  if (rc != VGG19_OK) return rc;
+  if (dtype != VGG19_FP32 && dtype != VGG19_BF16)
+    return note_error(VGG19_ERR_ARG, "dtype %d is neither VGG19_FP32 nor VGG19_BF16", dtype);
+  if (rows < 0 || rows > (1 << 20)) return note_error(VGG19_ERR_SHAPE, "%lld rows outside [0, 2^20]", (long long)rows);
+  if (ldx < in) return note_error(VGG19_ERR_SHAPE, "row stride %lld below %d", (long long)ldx, in);
+  if (rows == 0) return VGG19_OK;
+  if (!x || !codes || !scales || (!y && !y_f32))
+    return note_error(VGG19_ERR_ARG, "x, codes, scales and one of the outputs must not be null");
+  const uintptr_t elt = dtype == VGG19_FP32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(x) % elt || reinterpret_cast<uintptr_t>(y) % elt || reinterpret_cast<uintptr_t>(y_f32) % 4 ||
+      reinterpret_cast<uintptr_t>(bias) % 4 || reinterpret_cast<uintptr_t>(codes) % 16 || reinterpret_cast<uintptr_t>(scales) % 16)
+    return note_error(VGG19_ERR_ARG, "x, bias and outputs are aligned to their types, codes and scales to 16 bytes");
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const cudaError_t e =
+      dtype == VGG19_BF16
+          ? q4_linear(static_cast<const bf16*>(x), ldx, rows, in, codes, scales, out, group, bias, relu != 0, static_cast<bf16*>(y), y_f32, st)
+          : q4_linear(static_cast<const float*>(x), ldx, rows, in, codes, scales, out, group, bias, relu != 0, static_cast<float*>(y), y_f32, st);
+  return e == cudaSuccess ? VGG19_OK : note_error(VGG19_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+}
+
+}  // extern "C"

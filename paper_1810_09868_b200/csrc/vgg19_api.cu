@@ -78,6 +78,8 @@ struct vgg19 {
   bf16 *tap_bwd = nullptr;   // tap-major rotated filters [9][Cin][Cout] of the same layers
   bf16 *w8 = nullptr;        // first-layer filter padded to [64][10][8] (bf16 tensor-core path)
   half16 *split_w = nullptr; // fp32 configuration on tensor cores: rows [hi | lo | hi] (fp16 terms) of every weight matrix, at 3 * w_off
+  char *q4 = nullptr;        // VGG19_FLAG_DENSE_Q4: codes and scales of the dense layers
+  size_t q4_codes[kFcLayers] = {}, q4_scales[kFcLayers] = {};  // byte offsets in it
   int *dev_error = nullptr;
   void *ws = nullptr;
   size_t ws_bytes = 0;
@@ -250,6 +252,7 @@ struct Pass {
   // fp32 configuration, forward only: activations travel as [hi | lo] fp16 terms (the same bytes as fp32) and
   // layers 2..16 and the dense layers run on tensor cores with three fp16 products per product
   bool split = false;
+  bool q4 = false;  // dense layers on their 4-bit copies (forward only)
   // Training step on one GPU: the learning rate (device scalar).  Where a filter-gradient kernel can
   // apply the update itself (the dense layers' GEMM: 86 % of the parameters at 224x224) the gradient is
   // never stored; `folded` tells the caller which parameter ranges are already updated.
@@ -387,6 +390,12 @@ struct Pass {
       ok(tc_dense_forward_split((const half16 *)x, n->split_w + 3 * f.w_off, n->params + f.b_off, o, fbuf(p.partial), B,
                                 f.In, f.Out, f.relu, n->dev_error, st), 2);
       if (!out_f) ok(split_rows(o, (half16 *)out_t, B, f.Out, n->dev_error, st), 1);
+      return;
+    }
+    if (q4) {
+      const int i = (int)(&f - n->fc);
+      ok(q4_linear<T>(x, f.In, B, f.In, n->q4 + n->q4_codes[i], n->q4 + n->q4_scales[i], f.Out, VGG19_DENSE_Q4_GROUP,
+                      n->params + f.b_off, f.relu, out_t, out_f, st), (B + 15) / 16);
       return;
     }
     if (tc_dense_ok(B, f))
@@ -527,6 +536,7 @@ int enqueue(vgg19 *n, int mode, const PassArgs &a, cudaStream_t st, int *launche
   if (mode == VGG19_MODE_FORWARD) {
     pass.keep_activations = false;
     pass.split = n->use_split;
+    pass.q4 = n->q4 != nullptr;
     pass.forward(a);
   } else if (mode == VGG19_MODE_BACKWARD) {
     pass.forward_tail_split = false;
@@ -558,7 +568,7 @@ int enqueue(vgg19 *n, int mode, const PassArgs &a, cudaStream_t st, int *launche
       }
       int rc = refresh_filter_copies(n, st);
       if (rc != VGG19_OK) return rc;
-      pass.launches += n->use_tc ? 2 : 0;
+      pass.launches += (n->use_tc ? 2 : 0) + (n->q4 ? kFcLayers : 0);
     }
   }
   if (launches) *launches = pass.launches;
@@ -626,6 +636,12 @@ void drop_graphs(vgg19 *n) {
 // gradients, tap-major filters, the padded first-layer filter), rebuilt from the fp32 master on `st`.
 int refresh_filter_copies(vgg19 *n, cudaStream_t st) {
   const bool h = n->cfg.dtype == VGG19_BF16;
+  if (n->q4)
+    for (int i = 0; i < kFcLayers; ++i) {
+      const FcLayer &f = n->fc[i];
+      CUDA_TRY(n, q4_pack<float>(n->params + f.w_off, f.In, f.Out, f.In, VGG19_DENSE_Q4_GROUP, n->q4 + n->q4_codes[i],
+                                 n->q4 + n->q4_scales[i], st));
+    }
   if (n->split_w) {
     for (int l = 1; l < kConvLayers; ++l) {
       const ConvLayer &c = n->conv[l];
@@ -691,6 +707,8 @@ int create_common(const vgg19_config *cfg, vgg19 **out) {
   if (cfg->batch_max < 1) return fail(nullptr, VGG19_ERR_ARG, "batch_max %d < 1", cfg->batch_max);
   if ((cfg->flags & VGG19_FLAG_SPLIT_F16) && cfg->dtype != VGG19_FP32)
     return fail(nullptr, VGG19_ERR_ARG, "VGG19_FLAG_SPLIT_F16 applies to the fp32 configuration only");
+  if ((cfg->flags & VGG19_FLAG_SPLIT_F16) && (cfg->flags & VGG19_FLAG_DENSE_Q4))
+    return fail(nullptr, VGG19_ERR_ARG, "VGG19_FLAG_DENSE_Q4 does not go with VGG19_FLAG_SPLIT_F16");
   int dev = 0;
   cudaDeviceProp prop;
   CUDA_TRY(nullptr, cudaGetDevice(&dev));
@@ -737,6 +755,14 @@ int create_common(const vgg19_config *cfg, vgg19 **out) {
   if (e == cudaSuccess && n->use_tc) e = cudaMalloc(&n->tap_fwd, n->n_dgrad * sizeof(bf16));
   if (e == cudaSuccess && n->use_tc) e = cudaMalloc(&n->tap_bwd, n->n_dgrad * sizeof(bf16));
   if (e == cudaSuccess && n->use_split) e = cudaMalloc(&n->split_w, 3 * n->n_params * sizeof(half16));
+  if (e == cudaSuccess && (cfg->flags & VGG19_FLAG_DENSE_Q4)) {
+    size_t bytes = 0;
+    for (int i = 0; i < kFcLayers; ++i) {
+      n->q4_codes[i] = bytes; bytes += align_up(q4_code_bytes(n->fc[i].Out, n->fc[i].In));
+      n->q4_scales[i] = bytes; bytes += align_up(q4_scale_bytes(n->fc[i].Out, n->fc[i].In, VGG19_DENSE_Q4_GROUP));
+    }
+    e = cudaMalloc(&n->q4, bytes);
+  }
   if (e == cudaSuccess) e = cudaMalloc(&n->dev_error, 256);
   if (e == cudaSuccess) e = cudaMemset(n->dev_error, 0, 256);
   if (e != cudaSuccess) {
@@ -794,6 +820,7 @@ void vgg19_destroy(vgg19_t *n) {
   if (n->dgrad_w) cudaFree(n->dgrad_w);
   if (n->w8) cudaFree(n->w8);
   if (n->split_w) cudaFree(n->split_w);
+  if (n->q4) cudaFree(n->q4);
   if (n->tap_fwd) cudaFree(n->tap_fwd);
   if (n->tap_bwd) cudaFree(n->tap_bwd);
   if (n->dev_error) cudaFree(n->dev_error);
@@ -1159,10 +1186,12 @@ int vgg19_dense_layer_forward(vgg19_t *n, int32_t layer, const void *x, int32_t 
   cudaError_t e;
   if (n->cfg.dtype == VGG19_BF16) {
     Pass<bf16> ps{n, p, st};
+    ps.q4 = n->q4 != nullptr;
     ps.dense_forward(n->fc[layer - 1], (const bf16 *)x, batch, (bf16 *)y, y_f32);
     e = ps.err;
   } else {
     Pass<float> ps{n, p, st};
+    ps.q4 = n->q4 != nullptr;
     ps.dense_forward(n->fc[layer - 1], (const float *)x, batch, (float *)y, y_f32);
     e = ps.err;
   }
@@ -1285,7 +1314,8 @@ int vgg19_describe(const vgg19_t *n, char *out, size_t cap) {
   for (int i = 0; i < kFcLayers; ++i) {
     const FcLayer &f = n->fc[i];
     snprintf(line, sizeof line, "dense%d %5d->%-4d +bias%s%s\n", i + 1, f.In, f.Out, f.relu ? " +relu" : "",
-             n->use_split ? "  fwd=tcgen05:gemm-split-fp16 (forward-only passes; else simt)" : "");
+             n->use_split ? "  fwd=tcgen05:gemm-split-fp16 (forward-only passes; else simt)"
+             : n->q4 ? "  fwd=4-bit weights (forward-only passes)" : "");
     s += line;
   }
   s += "softmax 1000\n";

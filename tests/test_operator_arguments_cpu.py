@@ -59,3 +59,38 @@ def test_the_binding_refuses_host_tensors_and_wrong_types(p):
     with pytest.raises(p.Vgg19Error) as e:
         p.vgg19_logprobs(torch.zeros(5))
     assert e.value.code == p.VGG19_ERR_SHAPE
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(x=None), "ARG"), (dict(dtype=5), "ARG"), (dict(rows=-1), "SHAPE"), (dict(rows=(1 << 20) + 1), "SHAPE"), (dict(in_=0), "SHAPE"),
+    (dict(in_=(1 << 24) + 1), "SHAPE"), (dict(out=0), "SHAPE"), (dict(ldx=99), "SHAPE"), (dict(group=16), "ARG"), (dict(codes=None), "ARG"),
+    (dict(scales=None), "ARG"), (dict(codes=SOME + 8), "ARG"), (dict(scales=SOME + 2), "ARG"), (dict(y=None, y_f32=None), "ARG"),
+    (dict(x=SOME + 1), "ARG"), (dict(bias=SOME + 2), "ARG"), (dict(y_f32=SOME + 2), "ARG")])
+def test_q4_linear_refuses(p, over, code):
+    a = dict(x=SOME, dtype=1, rows=2, in_=100, ldx=100, codes=SOME, scales=SOME, out=10, group=32, bias=SOME, relu=0, y=SOME,
+             y_f32=SOME, stream=None)
+    a.update(over)
+    assert p.binding.load().vgg19_q4_linear(*a.values()) == getattr(p, "VGG19_ERR_" + code)
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(w=None), "ARG"), (dict(dtype=-1), "ARG"), (dict(out=0), "SHAPE"), (dict(in_=0), "SHAPE"), (dict(ld=99), "SHAPE"),
+    (dict(group=100), "ARG"), (dict(codes=None), "ARG"), (dict(scales=None), "ARG"), (dict(w=SOME + 1), "ARG"),
+    (dict(out=1 << 24, in_=1 << 24, ld=1 << 24), "SHAPE")])
+def test_q4_pack_refuses(p, over, code):
+    a = dict(w=SOME, dtype=0, out=10, in_=100, ld=100, group=32, codes=SOME, scales=SOME, stream=None)
+    a.update(over)
+    assert p.binding.load().vgg19_q4_pack(*a.values()) == getattr(p, "VGG19_ERR_" + code)
+
+
+def test_q4_sizes(p):
+    assert p.vgg19_q4_code_bytes(1, 1) == 1024 and p.vgg19_q4_code_bytes(17, 129) == 4 * 1024
+    assert p.vgg19_q4_scale_bytes(1, 1, 128) == 32 and p.vgg19_q4_scale_bytes(17, 129, 32) == 4 * 128
+    assert p.vgg19_q4_code_bytes(0, 5) == 0 and p.vgg19_q4_scale_bytes(5, 5, 48) == 0
+
+
+def test_q4_configuration(p):
+    import ctypes
+    out = ctypes.c_void_p()
+    cfg = p.binding.vgg19_config(32, 32, 1, p.VGG19_FP32, p.VGG19_FLAG_SPLIT_F16 | p.VGG19_FLAG_DENSE_Q4)
+    assert p.binding.load().vgg19_create(ctypes.byref(cfg), 0, ctypes.byref(out)) == p.VGG19_ERR_ARG
