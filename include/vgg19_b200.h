@@ -423,8 +423,44 @@ int vgg19_q4_linear(const void *x, int32_t dtype, int64_t rows, int32_t in, int6
                     const void *scales, int32_t out, int32_t group, const float *bias, int32_t relu, void *y,
                     float *y_f32, void *stream);
 
+/* The orthogonalised update of weight matrices, beside the plain gradient
+ * descent of vgg19_sgd_step (the paper names no optimiser).  For every tensor, a
+ * [rows][cols] matrix with gradient G, momentum M and weights W:
+ *   M <- momentum * M + G;  U = G + momentum * M if `nesterov`, else M;
+ *   X = U / |U|_F, then `steps` (1..16) times X <- a X + (b A + c A A) X with A = X X^T and
+ *   (a, b, c) = (3.4445, -4.7750, 2.0315), on the transpose where rows > cols;
+ *   W <- (1 - lr * decay) * W - lr * sqrt(max(1, rows / cols)) * X.
+ * w, grad, momentum: device fp32, dense; w_bf16 (or NULL): device bf16, receives
+ * the rounded result.  grad is only read.  The products carry every fp32 value as two fp16 terms
+ * (as VGG19_FLAG_SPLIT_F16 does) and the norm is summed in 64 bits, so any scale of gradient serves.  A zero U leaves X at 0;
+ * a NaN or infinity in a tensor's U makes that tensor's W NaN.  The tensors of a call are
+ * updated together; they must not overlap.  The smaller side of a tensor is at most 2^15.
+ * workspace: device, 256-byte aligned, vgg19_muon_workspace_bytes(tensors, count) bytes (0 for tensors that are
+ * refused; only rows and cols are read), scratch for the time of the call: calls that share one have to be ordered.  Asynchronous on `stream`; may be
+ * captured.  A bounded wait that runs out inside a kernel is reported by vgg19_ops_status. */
+typedef struct {
+  float *w;
+  void *w_bf16;
+  const float *grad;
+  float *momentum;
+  int64_t rows, cols;
+} vgg19_muon_tensor;
+size_t vgg19_muon_workspace_bytes(const vgg19_muon_tensor *tensors, int32_t count);
+int vgg19_muon_update(const vgg19_muon_tensor *tensors, int32_t count, float lr, float momentum, float decay,
+                      int32_t steps, int32_t nesterov, void *workspace, size_t bytes, void *stream);
+
+/* The same as a training step's update of a whole network, in place of
+ * vgg19_sgd_step: every weight tensor as a matrix ([Cout][9 * Cin] or [out][in]) by the update above,
+ * every bias b <- b - bias_lr * u with its own momentum and no decay, then the bf16 copy and every filter copy the kernels read.
+ * grads: device fp32, vgg19_param_count() elements; momentum: the same size, kept by the caller (zeros at first).
+ * workspace of vgg19_muon_step_bytes(net). */
+size_t vgg19_muon_step_bytes(const vgg19_t *net);
+int vgg19_muon_step(vgg19_t *net, const float *grads, float *momentum_buffer, float lr, float momentum, float decay,
+                    float bias_lr, int32_t steps, int32_t nesterov, void *workspace, size_t bytes, void *stream);
+
 /* Wait for the stream and report, and clear, what the operators without a handle
  * (vgg19_logprobs and those below it) have recorded on the current device:
+ * VGG19_ERR_DEVICE_TIMEOUT when a bounded wait inside a kernel ran out,
  * VGG19_ERR_ARG for an id outside the classes. */
 int vgg19_ops_status(void *stream);
 

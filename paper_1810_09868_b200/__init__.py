@@ -71,6 +71,17 @@ class Net:
         """parameters <- parameters - lr * grads, on the device, with every derived filter copy rebuilt."""
         binding.vgg19_sgd_step(self.handle, grads, lr, stream or self._torch.cuda.current_stream(self.device))
 
+    def muon_step(self, grads, momentum_buffer, lr, momentum=0.95, decay=0.0, bias_lr=None, steps=5, nesterov=True, stream=None):
+        """The orthogonalised update of every weight tensor (biases: momentum and a plain step at bias_lr, lr if None).
+        momentum_buffer: fp32, n_params elements, zeros at first; the workspace is allocated on the first call and kept."""
+        torch = self._torch
+        if getattr(self, "muon_workspace", None) is None:
+            self.muon_workspace = torch.empty(binding.vgg19_muon_step_bytes(self.handle), dtype=torch.uint8, device=self.device)
+        with torch.cuda.device(self.device):
+            binding.vgg19_muon_step(self.handle, grads, momentum_buffer, lr, momentum, decay, lr if bias_lr is None else bias_lr, steps,
+                                    nesterov, self.muon_workspace, self.muon_workspace.numel(),
+                                    stream or torch.cuda.current_stream(self.device))
+
     def train_step(self, images, labels, lr, loss=None, stream=None):
         """Forward + backward + update as one recorded device program (workspace of VGG19_MODE_TRAIN)."""
         stream = stream or self._torch.cuda.current_stream(self.device)

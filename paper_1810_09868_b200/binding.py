@@ -29,6 +29,7 @@ EXPORTS = (
     "vgg19_describe", "vgg19_last_error",
     "vgg19_logprobs", "vgg19_logprobs_backward", "vgg19_ops_status",
     "vgg19_q4_code_bytes", "vgg19_q4_scale_bytes", "vgg19_q4_pack", "vgg19_q4_linear",
+    "vgg19_muon_workspace_bytes", "vgg19_muon_update", "vgg19_muon_step_bytes", "vgg19_muon_step",
 )
 VGG19_NO_CLASS = -1
 VGG19_LOGPROBS_MAX_TOP, VGG19_LOGPROBS_MAX_IDS = 32, 256
@@ -37,6 +38,11 @@ VGG19_LOGPROBS_MAX_TOP, VGG19_LOGPROBS_MAX_IDS = 32, 256
 class vgg19_config(ctypes.Structure):
     _fields_ = [("height", ctypes.c_int32), ("width", ctypes.c_int32), ("batch_max", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class vgg19_muon_tensor(ctypes.Structure):
+    _fields_ = [("w", ctypes.c_void_p), ("w_bf16", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("momentum", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
 
 
 class Vgg19Error(RuntimeError):
@@ -63,6 +69,7 @@ def load():
                            "(there is no CPU fallback)")
     L = ctypes.CDLL(path)
     vp, i32, i64, u64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t
+    f32 = ctypes.c_float
     cfgp = ctypes.POINTER(vgg19_config)
     sig = {
         "vgg19_create": ([cfgp, u64, ctypes.POINTER(vp)], ctypes.c_int),
@@ -101,6 +108,10 @@ def load():
         "vgg19_logprobs": ([vp, i32, i64, i32, i64, vp, i32, i32, vp, vp, vp, vp, vp, vp], ctypes.c_int),
         "vgg19_logprobs_backward": ([vp, i32, i64, i32, i64, vp, i32, vp, vp, vp, vp, vp, i64, vp], ctypes.c_int),
         "vgg19_ops_status": ([vp], ctypes.c_int),
+        "vgg19_muon_workspace_bytes": ([vp, i32], sz),
+        "vgg19_muon_update": ([vp, i32, f32, f32, f32, i32, i32, vp, sz, vp], ctypes.c_int),
+        "vgg19_muon_step_bytes": ([vp], sz),
+        "vgg19_muon_step": ([vp, vp, vp, f32, f32, f32, f32, i32, i32, vp, sz, vp], ctypes.c_int),
         "vgg19_q4_code_bytes": ([i32, i32], sz),
         "vgg19_q4_scale_bytes": ([i32, i32, i32], sz),
         "vgg19_q4_pack": ([vp, i32, i32, i32, i64, i32, vp, vp, vp], ctypes.c_int),
@@ -433,6 +444,62 @@ def vgg19_q4_linear(x, codes, scales, out, group, bias=None, relu=False, y=None,
                  None if bias is None else _tensor(bias, "bias", torch.float32, (out,), dev), int(relu),
                  None if y is None else _tensor(y, "y", x.dtype, (rows, out), dev),
                  None if y_f32 is None else _tensor(y_f32, "y_f32", torch.float32, (rows, out), dev), _stream(stream))
+
+
+class MuonTensors:
+    """The tensors of an update as the library takes them, holding on to the torch tensors whose addresses it has."""
+
+    def __init__(self, tensors):
+        import torch
+        self.tensors = [tuple(t) for t in tensors]
+        self.count = len(self.tensors)
+        self.array = (vgg19_muon_tensor * max(self.count, 1))()
+        self.device = None
+        for a, (w, w16, grad, momentum) in zip(self.array, self.tensors):
+            dtype, rows, cols, ld, dev = _rows_of(w, "w")
+            if self.device is None:
+                self.device = dev
+            a.w = _tensor(w, "w", torch.float32, (rows, cols), self.device)
+            a.w_bf16 = None if w16 is None else _tensor(w16, "w_bf16", torch.bfloat16, (rows, cols), self.device)
+            a.grad = _tensor(grad, "grad", torch.float32, (rows, cols), self.device)
+            a.momentum = _tensor(momentum, "momentum", torch.float32, (rows, cols), self.device)
+            a.rows, a.cols = rows, cols
+
+
+def vgg19_muon_tensors(tensors):
+    """A list of (w, w_bf16 or None, grad, momentum), fp32 matrices of one shape each, for vgg19_muon_update; it may be kept and
+    used again while those tensors live."""
+    return MuonTensors(tensors)
+
+
+def vgg19_muon_workspace_bytes(tensors):
+    t = tensors if isinstance(tensors, MuonTensors) else MuonTensors(tensors)
+    return load().vgg19_muon_workspace_bytes(t.array, t.count)
+
+
+def _workspace(workspace, device):
+    if device is not None and workspace.device != device:
+        _refuse(VGG19_ERR_ARG, f"the workspace is on {workspace.device}, not on {device}")
+    if not workspace.is_contiguous():
+        _refuse(VGG19_ERR_ARG, "the workspace is not contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def vgg19_muon_update(tensors, lr, momentum, decay, steps, nesterov, workspace, stream=None):
+    t = tensors if isinstance(tensors, MuonTensors) else MuonTensors(tensors)
+    if t.count == 0:
+        return VGG19_OK
+    ptr, nbytes = _workspace(workspace, t.device)
+    return _call(t.device, "vgg19_muon_update", t.array, t.count, lr, momentum, decay, steps, int(nesterov), ptr, nbytes, _stream(stream))
+
+
+def vgg19_muon_step_bytes(net):
+    return load().vgg19_muon_step_bytes(net)
+
+
+def vgg19_muon_step(net, grads, momentum_buffer, lr, momentum, decay, bias_lr, steps, nesterov, workspace, nbytes, stream=None):
+    return _check(net, load().vgg19_muon_step(net, _ptr(grads), _ptr(momentum_buffer), lr, momentum, decay, bias_lr, steps, int(nesterov),
+                                              _ptr(workspace), nbytes, _stream(stream)))
 
 
 def vgg19_ops_status(stream=None):

@@ -34,8 +34,18 @@ enum DeviceError : int {
 // Sets the text vgg19_last_error(NULL) gives and returns `code`: for entry points without a handle.
 int note_error(int code, const char* fmt, ...);
 
-// Reads and clears the device-side error word of the operators without a handle (logprobs.cu).
+// Reads and clears the device-side error words of the operators without a handle (logprobs.cu, muon.cu).
 cudaError_t logprobs_take_error(int* code);
+cudaError_t muon_take_error(int* code);
+
+// m <- mu m + g, w <- w - lr (g + mu m or m), w16 the rounded copy (or null), for each vector (muon.cu).
+struct MuonVector {
+  const float* grad;
+  float *momentum, *w;
+  bf16* w16;
+  int n;
+};
+cudaError_t muon_vector_update(const MuonVector* v, int count, float lr, float mu, bool nesterov, cudaStream_t st);
 
 // Dense layers over 4-bit weights (q4_dense.cu; layout and formulas in the public header).  T: type of w, x and y.
 size_t q4_code_bytes(int out, int in);

@@ -1,0 +1,816 @@
+// The orthogonalised update of weight matrices:
+//   M <- mu M + G,   U = G + mu M (Nesterov) or M,   X_0 = U / |U|_F   (transposed where U has more rows than columns)
+//   X <- p(X X^T) X,  p(A) = a I + b A + c A^2,       `steps` times (Newton-Schulz towards the orthogonal factor of U)
+//   W <- (1 - lr decay) W - lr sqrt(max(1, rows / cols)) X.
+//
+// Every p(A_k) is a polynomial of A_0 = X_0 X_0^T, so the products commute and the iteration can run on m x m symmetric
+// matrices: Q <- p(A) Q, A <- p(A) A p(A), and X = Q X_0 once at the end.  With n / m = r columns per row a step then
+// costs four symmetric products (half a product each) instead of (3 r + 1).  A alone forgets singular values below
+// the square root of its precision, which the iteration amplifies up to 3.4 times a step: so after every three steps X is formed and
+// A taken from it anew.  Against 64 bits that is as close as the plain iteration in fp32 (5e-6 against 7e-6 on gradients of low
+// rank with noise; without the restart 3e-5).
+//
+// Precision.  A matrix is kept as two fp16 planes hi + lo of its values times a power of two (22 bits; the scales below
+// keep every entry inside fp16's range), a product is hi hi + hi lo + lo hi in fp32, on tcgen05.  The tensor core's fp32
+// accumulation truncates, so a chain ends after L.chunk_ stages of 64 and the epilogue warps add the chunks into registers.
+//
+// The product kernel: CTA pairs (cta_group::2), 256 x 256 tiles, persistent.  A stage holds hi and lo of both operands
+// (64 KB per CTA) and feeds three products, so what a CTA loads per product is two thirds of what one pair of
+// planes at a time would take; the plain pair kernels of this library are bound by exactly that rate.  All tensors of a call and
+// all products that do not depend on one another share a launch.  Symmetric results are computed on and above the
+// diagonal and stored twice.  The last product's epilogue updates the weights: X itself is never stored.
+#include <cuda_fp16.h>
+
+#include "../../include/vgg19_b200.h"
+#include "tc_common.cuh"
+
+namespace vgg {
+namespace {
+
+using namespace tc;
+
+static __device__ int g_muon_error;  // a DeviceError code once a bounded wait ran out
+
+// ---- sizes -----------------------------------------------------------------------------------------------------
+constexpr int BM = 128, BN = 256, BK = 64;       // rows per CTA (a pair has 256), columns per pair, K per stage
+constexpr int kPlaneBytes = 128 * BK * 2;        // 128 rows (or K-rows) of one plane in a stage
+constexpr int kOperandBytes = 2 * kPlaneBytes;   // hi and lo
+constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kStages = 3;
+
+// Stages (12 MMAs each) of an accumulation chain.  One, but for the first two chains of a long tile: while they run the
+// epilogue warps still finish the tile before.
+__device__ __forceinline__ int chain_stages(int kb, int k_stages) { return k_stages >= 32 && kb < 8 ? 4 : 1; }
+constexpr int kThreads = 384;                    // a warpgroup for producer and issuer, two of epilogue warps
+// Registers per thread after the split: 168 at launch, 3 x 168 = 56 + 2 x 224.
+constexpr int kFewRegisters = 56, kManyRegisters = 224;
+constexpr int kSmemBytes = kStages * kStageBytes + 1024 + 256;
+constexpr int kMaxTensors = 20, kMaxProblems = 2 * kMaxTensors;
+
+// The quintic's coefficients, and the scales of what is stored.  |X| <= 1.21 after any step, so |A| <= 1.47 and (by the
+// polynomial's range on [0, 1.47]) |p| <= 3.45, |p A| <= 1.3, and Q of two and three steps is below 11.9 and 41.
+constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
+constexpr float kScaleX = 4096.f, kScaleA = 16384.f, kScaleP = 8192.f, kScaleQ2 = 4096.f, kScaleQ3 = 1024.f;
+constexpr int kStepsPerGram = 3;
+
+// ---- one product ---------------------------------------------------------------------------------------------
+// D[i][j] = alpha * (c1 add1[i][j] + c2 add2[i][j] + sum_k A[i][k] B[j][k]) (or B[k][j]: b_mn), m x n.
+struct __align__(64) Problem {
+  CUtensorMap a, b;
+  int m, n, k_stages, tiles_m, tiles_n;
+  int sym;         // tiles on and above the diagonal only, stored twice
+  int first_tile;
+  int b_mn;
+  float alpha;
+  // result as planes [2][m][ld], or ...
+  half16* out;
+  long plane, ld;
+  // the sums starting from c1 * (hi + lo of add1) + c2 * (hi + lo of add2), planes of the same strides, where not null;
+  const half16 *add1, *add2;
+  float c1, c2;
+  // ... or the update of w (and its bf16 copy): w <- keep * w + that, at [i][j], or at [j][i] where transposed
+  float* w;
+  bf16* w16;
+  long w_ld;
+  int transposed, w_vec;
+  float keep;
+};
+template <int N> struct Launch {
+  int count, total;
+  Problem p[N];
+};
+
+__device__ __forceinline__ void find_tile(const Problem& p, int t, int& ti, int& tj) {
+  if (p.sym) {
+    int left = p.tiles_m;
+    ti = 0;
+    while (t >= left) { t -= left; --left; ++ti; }
+    tj = ti + t;
+  } else {
+    tj = t / p.tiles_m;  // row tiles fastest: they share the wide operand's columns
+    ti = t - tj * p.tiles_m;
+  }
+}
+
+__device__ __forceinline__ uint32_t pack_half2(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 unpack_half2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+
+// v as fp16 terms hi + lo
+__device__ __forceinline__ void split8(const float (&v)[8], uint32_t (&hi)[4], uint32_t (&lo)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    hi[e] = pack_half2(v[2 * e], v[2 * e + 1]);
+    const float2 f = unpack_half2(hi[e]);
+    lo[e] = pack_half2(v[2 * e] - f.x, v[2 * e + 1] - f.y);
+  }
+}
+// sum += c (hi + lo) of up to 128 columns of a row of planes, `left` of which exist
+__device__ __forceinline__ void add_planes(float (&sum)[128], const half16* m, long plane, long at, int left, float c) {
+#pragma unroll
+  for (int b = 0; b < 128; b += 32) {
+    uint4 h[4], l[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (b + 8 * q < left) {
+        h[q] = *reinterpret_cast<const uint4*>(m + at + b + 8 * q);
+        l[q] = *reinterpret_cast<const uint4*>(m + plane + at + b + 8 * q);
+      }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (b + 8 * q < left) {
+        const uint32_t hw[4] = {h[q].x, h[q].y, h[q].z, h[q].w}, lw[4] = {l[q].x, l[q].y, l[q].z, l[q].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 hf = unpack_half2(hw[e]), lf = unpack_half2(lw[e]);
+          sum[b + 8 * q + 2 * e] = fmaf(c, hf.x + lf.x, sum[b + 8 * q + 2 * e]);
+          sum[b + 8 * q + 2 * e + 1] = fmaf(c, hf.y + lf.y, sum[b + 8 * q + 2 * e + 1]);
+        }
+      }
+  }
+}
+__device__ __forceinline__ void update(const Problem& p, long at, float v) {
+  const float w = fmaf(p.keep, p.w[at], v);
+  p.w[at] = w;
+  if (p.w16) p.w16[at] = __float2bfloat16_rn(w);
+}
+
+template <int N>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t bars = smem_base + kStages * kStageBytes;
+  auto full_bar = [&](int s) { return bars + 8u * s; };                   // used in the even CTA
+  auto empty_bar = [&](int s) { return bars + 8u * (kStages + s); };      // both CTAs
+  auto acc_full_bar = [&](int b) { return bars + 8u * (2 * kStages + b); };       // both CTAs
+  auto acc_empty_bar = [&](int b) { return bars + 8u * (2 * kStages + 2 + b); };  // used in the even CTA
+  const uint32_t drain_bar = bars + 8u * (2 * kStages + 4);
+  __shared__ uint32_t tmem_base_slot;
+  __shared__ int abort_flag;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const bool leader = rank == 0;
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int s = 0; s < kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(acc_full_bar(b), 1); mbar_init(acc_empty_bar(b), 4); }  // two groups, two CTAs
+    mbar_init(drain_bar, 1);
+    mbar_fence_init();
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(smem_u32(&tmem_base_slot), 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();  // the peer's barriers are initialised before anything signals them
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_base_slot;
+
+  if (warp < 4) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
+  if (warp == 0) {
+    // ------------------------------ TMA producer ------------------------------
+    if (lane == 0) {
+      uint32_t fills[kStages];
+#pragma unroll
+      for (int s = 0; s < kStages; ++s) fills[s] = 0;
+      int stage = 0, pi = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int w = pair; w < L.total && ok; w += n_pairs) {
+        while (pi + 1 < L.count && w >= L.p[pi + 1].first_tile) ++pi;
+        const Problem& p = L.p[pi];
+        int ti, tj;
+        find_tile(p, w - p.first_tile, ti, tj);
+        const int row = (2 * ti + (int)rank) * BM, col = tj * BN + (int)rank * (BN / 2);
+        for (int kb = 0; kb < p.k_stages; ++kb) {
+          if (!mbar_wait(empty_bar(stage), phase ^ 1, &abort_flag, &g_muon_error, kDevTimeoutStageFree)) { ok = false; break; }
+          const uint32_t sa = smem_base + stage * kStageBytes, sb = sa + kOperandBytes;
+          const uint32_t full = map_to_cta(full_bar(stage), 0);
+          // the even CTA announces the bytes of both CTAs' copies; what lies outside a matrix arrives as zeros
+          if (leader) mbar_expect_tx(full_bar(stage), 2 * kStageBytes);
+          tma_load_3d_pair(sa, &p.a, full, kb * BK, row, 0);
+          if (p.b_mn) {
+            tma_load_3d_pair(sb, &p.b, full, col, kb * BK, 0);
+            tma_load_3d_pair(sb + kPlaneBytes, &p.b, full, col + 64, kb * BK, 0);
+          } else {
+            tma_load_3d_pair(sb, &p.b, full, kb * BK, col, 0);
+          }
+#pragma unroll
+          for (int s = 0; s < kStages; ++s) fills[s] += s == stage;
+          if (++stage == kStages) { stage = 0; phase ^= 1; }
+        }
+      }
+      if (!ok) {
+        // let every copy in flight land before the CTA may exit (see the pair convolution)
+        if (leader) {
+#pragma unroll
+          for (int s = 0; s < kStages; ++s)
+            if (fills[s]) {
+              const unsigned long long t0 = global_timer_ns();
+              while (!mbar_try_wait(full_bar(s), (fills[s] - 1) & 1) && global_timer_ns() - t0 < 100000000ull) {}
+            }
+        } else {
+          const unsigned long long t0 = global_timer_ns();
+          while (global_timer_ns() - t0 < 1000000ull) {}
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------- MMA issuer (even CTA only) -------------------------
+    if (lane == 0 && leader) {
+      int stage = 0, pi = 0;
+      uint32_t phase = 0, chunk = 0;
+      bool ok = true;
+      for (int w = pair; w < L.total && ok; w += n_pairs) {
+        while (pi + 1 < L.count && w >= L.p[pi + 1].first_tile) ++pi;
+        const Problem& p = L.p[pi];
+        const bool mn = p.b_mn != 0;
+        const uint32_t idesc = umma_idesc_f16(2 * BM, BN, 0, mn);
+        // K-major: lo 128 rows behind hi, 16 k = 32 bytes of the swizzled row.  MN-major: two groups of 64 columns, each
+        // 64 k-rows of hi then of lo; 16 k = 16 rows.
+        const uint32_t b_lo = mn ? kPlaneBytes / 2 : kPlaneBytes, b_step = mn ? 2048 : 32, b_lbo = mn ? kPlaneBytes : 16;
+        for (int kb0 = 0, kb1; kb0 < p.k_stages && ok; kb0 = kb1, ++chunk) {
+          kb1 = min(kb0 + chain_stages(kb0, p.k_stages), p.k_stages);
+          const int buf = chunk & 1;
+          if (!mbar_wait(acc_empty_bar(buf), ((chunk >> 1) & 1) ^ 1, &abort_flag, &g_muon_error, kDevTimeoutTmemFree)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t d = tmem_base + (uint32_t)(buf * BN);
+          for (int kb = kb0; kb < kb1; ++kb) {
+            if (!mbar_wait(full_bar(stage), phase, &abort_flag, &g_muon_error, kDevTimeoutTmaFull)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t sa = smem_base + stage * kStageBytes, sb = sa + kOperandBytes;
+            const uint64_t ah = smem_desc_sw128(sa, 16), al = smem_desc_sw128(sa + kPlaneBytes, 16);
+            const uint64_t bh = smem_desc_sw128(sb, b_lbo), bl = smem_desc_sw128(sb + b_lo, b_lbo);
+            // the small products first: what the tensor core truncates is relative to the sum so far
+            umma_bf16_pair(d, al, bh, idesc, kb != kb0 ? 1u : 0u);
+            umma_bf16_pair_acc(d, ah, bl, idesc);
+#pragma unroll
+            for (int k = 1; k < BK / 16; ++k) {
+              umma_bf16_pair_acc(d, desc_advance(al, k * 32), desc_advance(bh, k * b_step), idesc);
+              umma_bf16_pair_acc(d, desc_advance(ah, k * 32), desc_advance(bl, k * b_step), idesc);
+            }
+#pragma unroll
+            for (int k = 0; k < BK / 16; ++k)
+              umma_bf16_pair_acc(d, desc_advance(ah, k * 32), desc_advance(bh, k * b_step), idesc);
+            umma_commit_pair(empty_bar(stage), 3);  // frees the stage in both CTAs
+            if (++stage == kStages) { stage = 0; phase ^= 1; }
+          }
+          if (ok) umma_commit_pair(acc_full_bar(buf), 3);
+        }
+      }
+      if (!ok) {
+        umma_commit_pair(drain_bar, 1);
+        const unsigned long long t0 = global_timer_ns();
+        while (!mbar_try_wait(drain_bar, 0) && global_timer_ns() - t0 < 100000000ull) {}
+      }
+    }
+  }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
+    // -------------------------------- epilogue --------------------------------
+    const int group = (warp - 4) >> 2, quarter = warp & 3;  // half of the columns; the lane quarter this warp may read
+    const bool elected = threadIdx.x == 128 + 128 * group;
+    int pi = 0;
+    uint32_t chunk = 0;
+    bool ok = true;
+    for (int w = pair; w < L.total && ok; w += n_pairs) {
+      while (pi + 1 < L.count && w >= L.p[pi + 1].first_tile) ++pi;
+      const Problem& p = L.p[pi];
+      int ti, tj;
+      find_tile(p, w - p.first_tile, ti, tj);
+      const int i = (2 * ti + (int)rank) * BM + quarter * 32 + lane, j0 = tj * BN + group * 128;
+      // the sums start from what is added to the product: its loads pass while the first chain runs
+      float sum[128];
+#pragma unroll
+      for (int j = 0; j < 128; ++j) sum[j] = 0.f;
+      if (p.add1 && i < p.m) add_planes(sum, p.add1, p.plane, (long)i * p.ld + j0, p.n - j0, p.c1);
+      if (p.add2 && i < p.m) add_planes(sum, p.add2, p.plane, (long)i * p.ld + j0, p.n - j0, p.c2);
+      for (int kb0 = 0; kb0 < p.k_stages; kb0 += chain_stages(kb0, p.k_stages), ++chunk) {
+        const int buf = chunk & 1;
+        const bool got = mbar_wait(acc_full_bar(buf), (chunk >> 1) & 1, &abort_flag, &g_muon_error, kDevTimeoutAccum);
+        if (named_bar_or(1 + group, 128, !got)) { ok = false; break; }  // the group's warps leave together
+        tc_fence_after();
+        const uint32_t src = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + group * 128);
+        uint32_t v[2][16];
+        tmem_ld_32x16(src, v[0]);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          tmem_ld_wait();
+          if (c < 7) tmem_ld_32x16(src + (c + 1) * 16, v[(c + 1) & 1]);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) sum[c * 16 + j] += __uint_as_float(v[c & 1][j]);
+        }
+        tc_fence_before();
+        named_bar_sync(1 + group, 128);
+        if (elected) mbar_arrive_cluster(map_to_cta(acc_empty_bar(buf), 0));
+      }
+      if (!ok) break;
+
+      if (i < p.m) {
+        float4 w_next[8];  // the weights of 32 columns, requested together
+#pragma unroll
+        for (int j = 0; j < 128; j += 8) {
+          if (p.w_vec && j % 32 == 0) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              if (j0 + j + 4 * q < p.n) w_next[q] = *reinterpret_cast<const float4*>(p.w + (long)i * p.w_ld + j0 + j + 4 * q);
+          }
+          if (j0 + j < p.n) {  // (a row of planes has room for whole eights)
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = p.alpha * sum[j + e];
+            const long at = (long)i * p.ld + j0 + j;
+            if (p.w) {
+              if (p.transposed) {  // lanes along a row of w
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                  if (j0 + j + e < p.n) update(p, (long)(j0 + j + e) * p.w_ld + i, v[e]);
+              } else {
+                const long to = (long)i * p.w_ld + j0 + j;
+                if (p.w_vec) {
+                  float4 a = w_next[j % 32 / 4], b = w_next[j % 32 / 4 + 1];
+                  a.x = fmaf(p.keep, a.x, v[0]); a.y = fmaf(p.keep, a.y, v[1]); a.z = fmaf(p.keep, a.z, v[2]); a.w = fmaf(p.keep, a.w, v[3]);
+                  b.x = fmaf(p.keep, b.x, v[4]); b.y = fmaf(p.keep, b.y, v[5]); b.z = fmaf(p.keep, b.z, v[6]); b.w = fmaf(p.keep, b.w, v[7]);
+                  *reinterpret_cast<float4*>(p.w + to) = a;
+                  *reinterpret_cast<float4*>(p.w + to + 4) = b;
+                  if (p.w16) {
+                    const __nv_bfloat162 q[4] = {__floats2bfloat162_rn(a.x, a.y), __floats2bfloat162_rn(a.z, a.w),
+                                                 __floats2bfloat162_rn(b.x, b.y), __floats2bfloat162_rn(b.z, b.w)};
+                    *reinterpret_cast<uint4*>(p.w16 + to) = *reinterpret_cast<const uint4*>(q);
+                  }
+                } else {
+#pragma unroll
+                  for (int e = 0; e < 8; ++e)
+                    if (j0 + j + e < p.n) update(p, to + e, v[e]);
+                }
+              }
+            } else {
+              uint32_t hi[4], lo[4];
+              split8(v, hi, lo);
+              *reinterpret_cast<uint4*>(p.out + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+              *reinterpret_cast<uint4*>(p.out + p.plane + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+              if (p.sym && ti != tj) {  // the mirror image, lanes along a row
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                  if (j0 + j + e < p.n) {
+                    half16* q = p.out + (long)(j0 + j + e) * p.ld + i;
+                    q[0] = (half16)(hi[e / 2] >> (16 * (e & 1)));
+                    q[p.plane] = (half16)(lo[e / 2] >> (16 * (e & 1)));
+                  }
+              }
+            }
+          }
+        }
+      }
+    }
+  }
+
+  // Neither CTA may release tensor memory or exit while the other can still signal its barriers, read its shared
+  // memory or write its accumulator.
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc_pair(tmem_base, 512);
+  }
+}
+
+// ---- momentum, norm, X_0 ----------------------------------------------------------------------------------------
+struct Element {
+  const float* grad;
+  float* momentum;
+  half16* x;       // planes of X_0 [2][m][ld]
+  long rows, cols, ld, plane;
+  long first_norm, first_split;  // first block of each kernel
+  int transposed, vec;
+};
+struct Elements {
+  int count, nesterov;
+  float mu;
+  double* partial;  // a sum of squares per block of the first kernel
+  double* inverse;  // 1 / |U|_F per tensor
+  Element t[kMaxTensors];
+};
+constexpr int kNormThreads = 256, kNormChunk = 8192;
+
+__device__ __forceinline__ float direction(float g, float m, float mu, int nesterov) { return nesterov ? fmaf(mu, m, g) : m; }
+
+// M <- mu M + G; the block's sum of squares of U, in 64 bits: neither tiny nor huge gradients leave the range.
+__global__ void __launch_bounds__(kNormThreads) momentum_norm_kernel(const __grid_constant__ Elements a) {
+  int t = 0;
+  while (t + 1 < a.count && blockIdx.x >= a.t[t + 1].first_norm) ++t;
+  const Element& e = a.t[t];
+  const long n = e.rows * e.cols, begin = (blockIdx.x - e.first_norm) * kNormChunk;
+  const long end = begin + kNormChunk < n ? begin + kNormChunk : n;
+  double s = 0.0;
+  if (e.vec) {
+    for (long i = begin + threadIdx.x * 4; i < end; i += kNormThreads * 4) {
+      const float4 g = __ldcs(reinterpret_cast<const float4*>(e.grad + i));
+      float4 m = *reinterpret_cast<const float4*>(e.momentum + i);
+      m.x = fmaf(a.mu, m.x, g.x); m.y = fmaf(a.mu, m.y, g.y); m.z = fmaf(a.mu, m.z, g.z); m.w = fmaf(a.mu, m.w, g.w);
+      *reinterpret_cast<float4*>(e.momentum + i) = m;
+      const double u0 = direction(g.x, m.x, a.mu, a.nesterov), u1 = direction(g.y, m.y, a.mu, a.nesterov);
+      const double u2 = direction(g.z, m.z, a.mu, a.nesterov), u3 = direction(g.w, m.w, a.mu, a.nesterov);
+      s += (u0 * u0 + u1 * u1) + (u2 * u2 + u3 * u3);
+    }
+  } else {
+    for (long i = begin + threadIdx.x; i < end; i += kNormThreads) {
+      const float g = e.grad[i], m = fmaf(a.mu, e.momentum[i], g);
+      e.momentum[i] = m;
+      const double u = direction(g, m, a.mu, a.nesterov);
+      s += u * u;
+    }
+  }
+  __shared__ double part[kNormThreads / 32];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < kNormThreads / 32; ++i) s += part[i];
+    a.partial[blockIdx.x] = s;
+  }
+}
+
+// One block per tensor adds its blocks' sums, always in the same order.
+__global__ void __launch_bounds__(1024) inverse_norm_kernel(const __grid_constant__ Elements a, long blocks) {
+  const int t = blockIdx.x;
+  const long begin = a.t[t].first_norm, end = t + 1 < a.count ? a.t[t + 1].first_norm : blocks;
+  double s = 0.0;
+  for (long i = begin + threadIdx.x; i < end; i += 1024) s += a.partial[i];
+  __shared__ double part[32];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 32; ++i) s += part[i];
+    // no direction in a zero gradient; a NaN or an infinity anywhere makes the tensor's update NaN
+    a.inverse[t] = s == 0.0 ? 0.0 : isinf(s) ? (double)NAN : 1.0 / sqrt(s);
+  }
+}
+
+// X_0 = U / |U|_F as planes, transposed where the matrix has more rows than columns.
+constexpr int kSplitThreads = 256;
+__global__ void __launch_bounds__(kSplitThreads) split_kernel(const __grid_constant__ Elements a) {
+  int t = 0;
+  while (t + 1 < a.count && blockIdx.x >= a.t[t + 1].first_split) ++t;
+  const Element& e = a.t[t];
+  const long block = blockIdx.x - e.first_split;
+  const double f = a.inverse[t] * kScaleX;
+  auto value = [&](long i) { return (float)(f * direction(e.grad[i], e.momentum[i], a.mu, a.nesterov)); };
+  if (!e.transposed) {
+    const long per_row = e.ld / 8, item = block * kSplitThreads + threadIdx.x;
+    const long r = item / per_row, c = (item - r * per_row) * 8;
+    if (r >= e.rows) return;
+    const long i = r * e.cols + c;
+    float v[8];
+    if (e.vec && c + 8 <= e.cols && e.cols % 4 == 0) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float4 g = __ldcs(reinterpret_cast<const float4*>(e.grad + i) + h), m = __ldcs(reinterpret_cast<const float4*>(e.momentum + i) + h);
+        v[4 * h] = (float)(f * direction(g.x, m.x, a.mu, a.nesterov));
+        v[4 * h + 1] = (float)(f * direction(g.y, m.y, a.mu, a.nesterov));
+        v[4 * h + 2] = (float)(f * direction(g.z, m.z, a.mu, a.nesterov));
+        v[4 * h + 3] = (float)(f * direction(g.w, m.w, a.mu, a.nesterov));
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = c + k < e.cols ? value(i + k) : 0.f;
+    }
+    uint32_t hi[4], lo[4];
+    split8(v, hi, lo);
+    half16* dst = e.x + r * e.ld + c;
+    *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<uint4*>(dst + e.plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+  } else {
+    __shared__ float tile[32][33];
+    const long across = (e.cols + 31) / 32, r0 = block / across * 32, c0 = block % across * 32;
+    const int x = threadIdx.x % 32, y = threadIdx.x / 32;
+    for (int k = y; k < 32; k += 8)
+      if (r0 + k < e.rows && c0 + x < e.cols) tile[k][x] = value((r0 + k) * e.cols + c0 + x);
+    __syncthreads();
+    for (int k = y; k < 32; k += 8)
+      if (c0 + k < e.cols && r0 + x < e.rows) {
+        const float v = tile[x][k];
+        const __half h = __float2half_rn(v), l = __float2half_rn(v - __half2float(h));
+        half16* dst = e.x + (c0 + k) * e.ld + r0 + x;
+        dst[0] = __half_as_ushort(h);
+        dst[e.plane] = __half_as_ushort(l);
+      }
+  }
+}
+
+// Biases: momentum, and a plain step along U.
+struct Vectors {
+  int count, nesterov;
+  float mu, lr;
+  struct { const float* grad; float *momentum, *w; bf16* w16; int n; } t[32];
+};
+__global__ void vector_update_kernel(const __grid_constant__ Vectors a) {
+  const auto& v = a.t[blockIdx.x];
+  for (int i = threadIdx.x; i < v.n; i += blockDim.x) {
+    const float g = v.grad[i], m = fmaf(a.mu, v.momentum[i], g);
+    v.momentum[i] = m;
+    const float w = fmaf(-a.lr, direction(g, m, a.mu, a.nesterov), v.w[i]);
+    v.w[i] = w;
+    if (v.w16) v.w16[i] = __float2bfloat16_rn(w);
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------
+size_t up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+
+struct Shape {
+  long m, n, ldn, ldm;  // of X: rows <= columns; row strides of X and of the m x m matrices
+  bool transposed;
+  explicit Shape(const vgg19_muon_tensor& t)
+      : m(t.rows < t.cols ? t.rows : t.cols), n(t.rows < t.cols ? t.cols : t.rows), ldn((long)up(n, 8)), ldm((long)up(m, 8)),
+        transposed(t.rows > t.cols) {}
+  size_t x_bytes() const { return up((size_t)2 * m * ldn * 2, 256); }
+  size_t a_bytes() const { return up((size_t)2 * m * ldm * 2, 256); }
+  long norm_blocks() const { return (m * n + kNormChunk - 1) / kNormChunk; }
+  long split_blocks() const {
+    return transposed ? ((n + 31) / 32) * ((m + 31) / 32) : (m * (ldn / 8) + kSplitThreads - 1) / kSplitThreads;
+  }
+};
+
+enum Matrix { kX0, kX1, kGramA, kPoly, kQa, kQb, kPA, kMatrices };
+
+// The planes of one tensor in the workspace and their tensor maps.
+struct Planes {
+  half16* at[kMatrices];
+  CUtensorMap k_major[kMatrices], mn_major[2];
+};
+
+bool plane_map(CUtensorMap* map, const half16* base, long rows, long cols, long ld, uint32_t box_rows) {
+  const TensorMapApi& api = tensor_map_api();
+  if (!api.ok) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, 2};
+  cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)rows * ld * 2};
+  cuuint32_t box[3] = {BK, box_rows, 2};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return api.encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<half16*>(base), dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+size_t tensor_bytes(const Shape& s) { return 2 * s.x_bytes() + 5 * s.a_bytes(); }
+
+size_t batch_bytes(const vgg19_muon_tensor* t, int count) {
+  size_t b = up(kMaxTensors * sizeof(double), 256);
+  long blocks = 0;
+  for (int i = 0; i < count; ++i) {
+    const Shape s(t[i]);
+    b += tensor_bytes(s);
+    blocks += s.norm_blocks();
+  }
+  return b + up(blocks * sizeof(double), 256);
+}
+
+template <int N> cudaError_t launch_products(Launch<N>& L, cudaStream_t st) {
+  int tiles = 0;
+  for (int i = 0; i < L.count; ++i) {
+    Problem& p = L.p[i];
+    p.tiles_m = (p.m + 2 * BM - 1) / (2 * BM);
+    p.tiles_n = (p.n + BN - 1) / BN;
+    p.first_tile = tiles;
+    tiles += p.sym ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
+  }
+  L.total = tiles;
+  cudaError_t e = cudaFuncSetAttribute(split_product_pair_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  if (e != cudaSuccess) return e;
+  int dev = 0, sms = 148;
+  cudaGetDevice(&dev);
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  const int pairs = tiles < sms / 2 ? tiles : sms / 2;
+  split_product_pair_kernel<N><<<2 * pairs, kThreads, kSmemBytes, st>>>(L);
+  return cudaGetLastError();
+}
+
+struct Options {
+  float lr, mu, decay;
+  int steps, nesterov;
+};
+
+// The whole update of up to kMaxTensors tensors; N is the largest number of products per launch.
+template <int N>
+cudaError_t update_batch(const vgg19_muon_tensor* tensors, const int count, const Options& o, char* ws, cudaStream_t st) {
+  static thread_local Planes planes[kMaxTensors];
+  Elements el{};
+  el.count = count; el.nesterov = o.nesterov; el.mu = o.mu;
+  el.inverse = reinterpret_cast<double*>(ws);
+  ws += up(kMaxTensors * sizeof(double), 256);
+  long norm_blocks = 0, split_blocks = 0;
+  for (int i = 0; i < count; ++i) {
+    const vgg19_muon_tensor& t = tensors[i];
+    const Shape s(t);
+    Planes& q = planes[i];
+    for (int k = 0; k < kMatrices; ++k) {
+      const bool x = k <= kX1;
+      q.at[k] = reinterpret_cast<half16*>(ws);
+      ws += x ? s.x_bytes() : s.a_bytes();
+      if (!plane_map(&q.k_major[k], q.at[k], s.m, x ? s.n : s.m, x ? s.ldn : s.ldm, 128)) return cudaErrorInvalidValue;
+      if (x && !plane_map(&q.mn_major[k], q.at[k], s.m, s.n, s.ldn, 64)) return cudaErrorInvalidValue;
+    }
+    Element& e = el.t[i];
+    e.grad = t.grad; e.momentum = t.momentum; e.x = q.at[kX0];
+    e.rows = t.rows; e.cols = t.cols; e.ld = s.ldn; e.plane = s.m * s.ldn;
+    e.transposed = s.transposed;
+    // (a chunk of the first kernel starts on a multiple of four elements, and so do the last whole fours of a tensor)
+    e.vec = reinterpret_cast<uintptr_t>(t.grad) % 16 == 0 && reinterpret_cast<uintptr_t>(t.momentum) % 16 == 0 && t.rows * t.cols % 4 == 0;
+    e.first_norm = norm_blocks; e.first_split = split_blocks;
+    norm_blocks += s.norm_blocks();
+    split_blocks += s.split_blocks();
+  }
+  el.partial = reinterpret_cast<double*>(ws);
+  momentum_norm_kernel<<<(unsigned)norm_blocks, kNormThreads, 0, st>>>(el);
+  inverse_norm_kernel<<<(unsigned)count, 1024, 0, st>>>(el, norm_blocks);
+  split_kernel<<<(unsigned)split_blocks, kSplitThreads, 0, st>>>(el);
+  cudaError_t err = cudaGetLastError();
+  if (err != cudaSuccess) return err;
+
+  static thread_local Launch<N> L;
+  // D = scale_d * (A / scale_a) (B / scale_b), all m x m symmetric
+  auto symmetric = [&](int i, Matrix a, float sa, Matrix b, float sb, Matrix d, float sd) -> Problem& {
+    const Shape s(tensors[i]);
+    Problem& p = L.p[L.count++];
+    p = Problem{};
+    p.a = planes[i].k_major[a]; p.b = planes[i].k_major[b];
+    p.m = p.n = (int)s.m;
+    p.k_stages = (int)((s.m + BK - 1) / BK);
+    p.sym = 1;
+    p.alpha = sd / (sa * sb);
+    p.out = planes[i].at[d]; p.ld = s.ldm; p.plane = s.m * s.ldm;
+    return p;
+  };
+  auto run = [&] { if (err == cudaSuccess) err = launch_products(L, st); L.count = 0; };
+  L.count = 0;
+  int x = kX0;
+  for (int done = 0; done < o.steps;) {
+    // groups of at most three steps, as even as they go
+    const int groups = (o.steps - done + kStepsPerGram - 1) / kStepsPerGram, group = (o.steps - done + groups - 1) / groups;
+    for (int i = 0; i < count; ++i) {
+      Problem& p = symmetric(i, (Matrix)x, kScaleX, (Matrix)x, kScaleX, kGramA, kScaleA);
+      p.k_stages = (int)((Shape(tensors[i]).n + BK - 1) / BK);
+    }
+    run();
+    // p(A) = a I + R with R = b A + c A A; Q = q0 I + S.  The identity's share is added in the epilogues, in fp32: what
+    // the tensor core truncates is then relative to the smaller rest.
+    Matrix q = kQa;  // S
+    float sq = kScaleP, q0 = kA;
+    for (int k = 0; k < group; ++k) {
+      const Matrix poly = k == 0 ? kQa : kPoly;  // R; the first one is also the first S
+      for (int i = 0; i < count; ++i) {
+        Problem& p = symmetric(i, kGramA, kScaleA, kGramA, kScaleA, poly, kC * kScaleP);
+        p.add1 = planes[i].at[kGramA]; p.c1 = kB * kScaleP / kScaleA / p.alpha;
+      }
+      run();
+      if (k > 0) {  // S <- a S + q0 R + R S
+        const Matrix next = q == kQa ? kQb : kQa;
+        const float sn = k == 1 ? kScaleQ2 : kScaleQ3;
+        for (int i = 0; i < count; ++i) {
+          Problem& p = symmetric(i, poly, kScaleP, q, sq, next, sn);
+          p.add1 = planes[i].at[q]; p.c1 = kA * sn / sq / p.alpha;
+          p.add2 = planes[i].at[poly]; p.c2 = q0 * sn / kScaleP / p.alpha;
+        }
+        q = next;
+        sq = sn;
+        q0 *= kA;
+      }
+      if (k + 1 < group) {  // A <- p A p, one factor at a time
+        for (int i = 0; i < count; ++i) {
+          Problem& p = symmetric(i, poly, kScaleP, kGramA, kScaleA, kPA, kScaleA);
+          p.add1 = planes[i].at[kGramA]; p.c1 = kA / p.alpha;
+        }
+        run();
+        for (int i = 0; i < count; ++i) {
+          Problem& p = symmetric(i, poly, kScaleP, kPA, kScaleA, kGramA, kScaleA);
+          p.add1 = planes[i].at[kPA]; p.c1 = kA / p.alpha;
+        }
+        run();
+      } else if (k > 0) {
+        run();
+      }
+    }
+    done += group;
+    for (int i = 0; i < count; ++i) {
+      const vgg19_muon_tensor& t = tensors[i];
+      const Shape s(t);
+      Problem& p = L.p[L.count++];
+      p = Problem{};
+      p.a = planes[i].k_major[q]; p.b = planes[i].mn_major[x];
+      p.b_mn = 1;
+      p.m = (int)s.m; p.n = (int)s.n;
+      p.k_stages = (int)((s.m + BK - 1) / BK);
+      p.ld = s.ldn; p.plane = s.m * s.ldn;
+      p.add1 = planes[i].at[x]; p.c1 = q0 * sq;
+      if (done < o.steps) {
+        p.alpha = 1.f / sq;
+        p.out = planes[i].at[x ^ 1];
+      } else {
+        const double scale = t.rows > t.cols ? sqrt((double)t.rows / (double)t.cols) : 1.0;
+        p.alpha = (float)(-(double)o.lr * scale / ((double)sq * kScaleX));
+        p.keep = (float)(1.0 - (double)o.lr * o.decay);
+        p.w = t.w; p.w16 = static_cast<bf16*>(t.w_bf16);
+        p.w_ld = t.cols;
+        p.transposed = s.transposed;
+        p.w_vec = t.cols % 8 == 0 && reinterpret_cast<uintptr_t>(t.w) % 16 == 0 && reinterpret_cast<uintptr_t>(t.w_bf16) % 16 == 0;
+      }
+    }
+    run();
+    x ^= 1;
+  }
+  return err;
+}
+
+int check_tensors(const vgg19_muon_tensor* t, int32_t count) {
+  if (count < 0 || (count && !t)) return note_error(VGG19_ERR_ARG, "%d tensors, or a null list", count);
+  for (int i = 0; i < count; ++i)
+    if (t[i].rows < 1 || t[i].cols < 1 || t[i].rows > (1 << 24) || t[i].cols > (1 << 24) ||
+        (t[i].rows < t[i].cols ? t[i].rows : t[i].cols) > (1 << 15) || t[i].rows * t[i].cols > (1LL << 34))
+      return note_error(VGG19_ERR_SHAPE, "tensor %d is %lld x %lld: sides in [1, 2^24], the smaller at most 2^15, 2^34 elements", i,
+                        (long long)t[i].rows, (long long)t[i].cols);
+  return VGG19_OK;
+}
+
+size_t workspace_bytes(const vgg19_muon_tensor* t, int32_t count) {
+  size_t most = 256;
+  for (int i = 0; i < count; i += kMaxTensors) {
+    const size_t b = batch_bytes(t + i, count - i < kMaxTensors ? count - i : kMaxTensors);
+    if (b > most) most = b;
+  }
+  return most;
+}
+
+}  // namespace
+
+cudaError_t muon_take_error(int* code) {
+  cudaError_t e = cudaMemcpyFromSymbol(code, g_muon_error, sizeof(int));
+  if (e == cudaSuccess && *code) {
+    const int zero = 0;
+    e = cudaMemcpyToSymbol(g_muon_error, &zero, sizeof(int));
+  }
+  return e;
+}
+
+cudaError_t muon_vector_update(const MuonVector* v, int count, float lr, float mu, bool nesterov, cudaStream_t st) {
+  Vectors a{};
+  a.nesterov = nesterov; a.mu = mu; a.lr = lr;
+  for (int i = 0; i < count; ++i) {
+    a.t[a.count].grad = v[i].grad; a.t[a.count].momentum = v[i].momentum; a.t[a.count].w = v[i].w;
+    a.t[a.count].w16 = v[i].w16; a.t[a.count].n = v[i].n;
+    if (++a.count == 32 || i + 1 == count) {
+      vector_update_kernel<<<(unsigned)a.count, 256, 0, st>>>(a);
+      a.count = 0;
+    }
+  }
+  return cudaGetLastError();
+}
+
+}  // namespace vgg
+
+extern "C" size_t vgg19_muon_workspace_bytes(const vgg19_muon_tensor* tensors, int32_t count) {
+  return vgg::check_tensors(tensors, count) == VGG19_OK ? vgg::workspace_bytes(tensors, count) : 0;
+}
+
+extern "C" int vgg19_muon_update(const vgg19_muon_tensor* tensors, int32_t count, float lr, float momentum, float decay,
+                                 int32_t steps, int32_t nesterov, void* workspace, size_t bytes, void* stream) {
+  using namespace vgg;
+  const int rc = check_tensors(tensors, count);
+  if (rc != VGG19_OK) return rc;
+  if (!(lr == lr) || !(momentum == momentum) || !(decay == decay))
+    return note_error(VGG19_ERR_ARG, "NaN learning rate, momentum or decay");
+  if (steps < 1 || steps > 16) return note_error(VGG19_ERR_ARG, "%d steps outside [1, 16]", steps);
+  for (int i = 0; i < count; ++i) {
+    const vgg19_muon_tensor& t = tensors[i];
+    if (!t.w || !t.grad || !t.momentum) return note_error(VGG19_ERR_ARG, "tensor %d has a null weight, gradient or momentum", i);
+    if (reinterpret_cast<uintptr_t>(t.w) % 4 || reinterpret_cast<uintptr_t>(t.grad) % 4 || reinterpret_cast<uintptr_t>(t.momentum) % 4 ||
+        reinterpret_cast<uintptr_t>(t.w_bf16) % 2)
+      return note_error(VGG19_ERR_ARG, "tensor %d is not aligned to its type", i);
+  }
+  if (count == 0) return VGG19_OK;
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256)
+    return note_error(VGG19_ERR_WORKSPACE, "the workspace is null or not 256-byte aligned");
+  if (bytes < workspace_bytes(tensors, count))
+    return note_error(VGG19_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu", bytes, workspace_bytes(tensors, count));
+  const Options o{lr, momentum, decay, steps, nesterov != 0};
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  for (int i = 0; i < count; i += kMaxTensors) {
+    const int n = count - i < kMaxTensors ? count - i : kMaxTensors;
+    const cudaError_t e = n <= 2 ? update_batch<4>(tensors + i, n, o, static_cast<char*>(workspace), st)
+                                 : update_batch<kMaxProblems>(tensors + i, n, o, static_cast<char*>(workspace), st);
+    if (e != cudaSuccess) return note_error(VGG19_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+  }
+  return VGG19_OK;
+}

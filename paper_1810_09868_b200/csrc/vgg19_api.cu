@@ -783,8 +783,11 @@ extern "C" {
 int vgg19_ops_status(void *stream) {
   cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
   int code = 0;
+  int timeout = 0;
   if (e == cudaSuccess) e = logprobs_take_error(&code);
+  if (e == cudaSuccess) e = muon_take_error(&timeout);
   if (e != cudaSuccess) return fail(nullptr, VGG19_ERR_CUDA, "reading the device status failed: %s", cudaGetErrorString(e));
+  if (timeout) return fail(nullptr, VGG19_ERR_DEVICE_TIMEOUT, "a device-side wait ran out (code %d)", timeout);
   if (code) return fail(nullptr, VGG19_ERR_ARG, "an id outside the row's classes (its log probability is NaN)");
   return VGG19_OK;
 }
@@ -883,6 +886,47 @@ int vgg19_sgd_step(vgg19_t *n, const float *grads, float lr, void *stream) {
     CUDA_TRY(n, sgd_update<bf16>(n->params, grads, (bf16 *)n->params_t, lr, n->n_params, st));
   else
     CUDA_TRY(n, sgd_update<float>(n->params, grads, (float *)nullptr, lr, n->n_params, st));
+  return refresh_filter_copies(n, st);
+}
+
+// The network's weight tensors as matrices, in parameter order.
+static void muon_tensors(const vgg19_t *n, const float *grads, float *momentum, vgg19_muon_tensor (&t)[kLayers]) {
+  for (int l = 0; l < kLayers; ++l) {
+    const bool conv = l < kConvLayers;
+    const size_t off = conv ? n->conv[l].w_off : n->fc[l - kConvLayers].w_off;
+    t[l].w = n->params + off;
+    t[l].w_bf16 = n->cfg.dtype == VGG19_BF16 ? (bf16 *)n->params_t + off : nullptr;
+    t[l].grad = grads ? grads + off : nullptr;
+    t[l].momentum = momentum ? momentum + off : nullptr;
+    t[l].rows = conv ? n->conv[l].Cout : n->fc[l - kConvLayers].Out;
+    t[l].cols = conv ? 9 * n->conv[l].Cin : n->fc[l - kConvLayers].In;
+  }
+}
+
+size_t vgg19_muon_step_bytes(const vgg19_t *n) {
+  if (!n) return 0;
+  vgg19_muon_tensor t[kLayers];
+  muon_tensors(n, nullptr, nullptr, t);
+  return vgg19_muon_workspace_bytes(t, kLayers);
+}
+
+int vgg19_muon_step(vgg19_t *n, const float *grads, float *momentum_buffer, float lr, float momentum, float decay,
+                    float bias_lr, int32_t steps, int32_t nesterov, void *workspace, size_t bytes, void *stream) {
+  if (!n) return VGG19_ERR_ARG;
+  if (!grads || !momentum_buffer || !(bias_lr == bias_lr))
+    return fail(n, VGG19_ERR_ARG, "null gradient or momentum, or NaN bias learning rate");
+  vgg19_muon_tensor t[kLayers];
+  muon_tensors(n, grads, momentum_buffer, t);
+  const int rc = vgg19_muon_update(t, kLayers, lr, momentum, decay, steps, nesterov, workspace, bytes, stream);
+  if (rc != VGG19_OK) return fail(n, rc, "%s", std::string(vgg19_last_error(nullptr)).c_str());
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  MuonVector v[kLayers];
+  for (int l = 0; l < kLayers; ++l) {
+    const size_t off = l < kConvLayers ? n->conv[l].b_off : n->fc[l - kConvLayers].b_off;
+    v[l] = MuonVector{grads + off, momentum_buffer + off, n->params + off,
+                      n->cfg.dtype == VGG19_BF16 ? (bf16 *)n->params_t + off : nullptr, (int)t[l].rows};
+  }
+  CUDA_TRY(n, muon_vector_update(v, kLayers, bias_lr, momentum, nesterov != 0, st));
   return refresh_filter_copies(n, st);
 }
 

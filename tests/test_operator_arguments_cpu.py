@@ -94,3 +94,32 @@ def test_q4_configuration(p):
     out = ctypes.c_void_p()
     cfg = p.binding.vgg19_config(32, 32, 1, p.VGG19_FP32, p.VGG19_FLAG_SPLIT_F16 | p.VGG19_FLAG_DENSE_Q4)
     assert p.binding.load().vgg19_create(ctypes.byref(cfg), 0, ctypes.byref(out)) == p.VGG19_ERR_ARG
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(count=-1), "ARG"), (dict(rows=0), "SHAPE"), (dict(cols=1 << 25), "SHAPE"), (dict(rows=40000, cols=40000), "SHAPE"), (dict(w=None), "ARG"),
+    (dict(grad=None), "ARG"), (dict(momentum_=None), "ARG"), (dict(w=SOME + 2), "ARG"), (dict(w16=SOME + 1), "ARG"), (dict(steps=0), "ARG"),
+    (dict(steps=17), "ARG"), (dict(lr=float("nan")), "ARG"), (dict(decay=float("nan")), "ARG"), (dict(ws=None), "WORKSPACE"),
+    (dict(ws=SOME + 16), "WORKSPACE"), (dict(nbytes=100), "WORKSPACE")])
+def test_muon_update_refuses(p, over, code):
+    a = dict(w=SOME, w16=SOME, grad=SOME, momentum_=SOME, rows=30, cols=50, count=1, lr=0.1, mu=0.9, decay=0.0, steps=5, ws=SOME, nbytes=1 << 40)
+    a.update(over)
+    t = (p.binding.vgg19_muon_tensor * 1)()
+    t[0].w, t[0].w_bf16, t[0].grad, t[0].momentum, t[0].rows, t[0].cols = a["w"], a["w16"], a["grad"], a["momentum_"], a["rows"], a["cols"]
+    rc = p.binding.load().vgg19_muon_update(t, a["count"], a["lr"], a["mu"], a["decay"], a["steps"], 1, a["ws"], a["nbytes"], None)
+    assert rc == getattr(p, "VGG19_ERR_" + code)
+
+
+def test_muon_sizes(p):
+    t = (p.binding.vgg19_muon_tensor * 1)()
+    t[0].rows, t[0].cols = 100, 1000
+    lib = p.binding.load()
+    one = lib.vgg19_muon_workspace_bytes(t, 1)
+    assert one >= 2 * 2 * 2 * 100 * 1000 + 5 * 2 * 2 * 100 * 104
+    t[0].rows, t[0].cols = 1000, 100
+    assert lib.vgg19_muon_workspace_bytes(t, 1) == one
+    t[0].rows = 0
+    assert lib.vgg19_muon_workspace_bytes(t, 1) == 0
+    assert lib.vgg19_muon_update(None, 0, 0.1, 0.9, 0.0, 5, 1, None, 0, None) == p.VGG19_OK
+    assert lib.vgg19_muon_step(None, None, None, 0.1, 0.9, 0.0, 0.1, 5, 1, None, 0, None) == p.VGG19_ERR_ARG
+    assert lib.vgg19_muon_step_bytes(None) == 0
