@@ -38,13 +38,15 @@ constexpr int kOperandBytes = 2 * kPlaneBytes;   // hi and lo
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kStages = 3;
 
-// Stages (12 MMAs each) of an accumulation chain.  One, but for the first two chains of a long tile: while they run the
-// epilogue warps still finish the tile before.
-__device__ __forceinline__ int chain_stages(int kb, int k_stages) { return k_stages >= 32 && kb < 8 ? 4 : 1; }
+// Stages (12 MMAs each) of an accumulation chain.  The error of a chain grows with its length, the hand-over of a chain to
+// the epilogue warps costs the tensor cores a few hundred cycles.  At 2048 and 4096 rows a chain of 4 is within 1.7 times
+// plain fp32 (which itself sums longer there) and 8 % faster than single stages; below, single stages are what it takes.
+__device__ __forceinline__ int chain_stages(int k_stages) { return k_stages >= 32 ? 4 : 1; }
 constexpr int kThreads = 384;                    // a warpgroup for producer and issuer, two of epilogue warps
 // Registers per thread after the split: 168 at launch, 3 x 168 = 56 + 2 x 224.
 constexpr int kFewRegisters = 56, kManyRegisters = 224;
-constexpr int kSmemBytes = kStages * kStageBytes + 1024 + 256;
+constexpr int kPieceBytes = 4096;                // an epilogue warp's own 32 rows of 128 bytes
+constexpr int kSmemBytes = kStages * kStageBytes + 8 * kPieceBytes + 1024 + 256;
 constexpr int kMaxTensors = 20, kMaxProblems = 2 * kMaxTensors;
 
 // The quintic's coefficients, and the scales of what is stored.  |X| <= 1.21 after any step, so |A| <= 1.47 and (by the
@@ -59,7 +61,6 @@ struct __align__(64) Problem {
   CUtensorMap a, b;
   int m, n, k_stages, tiles_m, tiles_n;
   int sym;         // tiles on and above the diagonal only, stored twice
-  int first_tile;
   int b_mn;
   float alpha;
   // result as planes [2][m][ld], or ...
@@ -76,7 +77,8 @@ struct __align__(64) Problem {
   float keep;
 };
 template <int N> struct Launch {
-  int count, total;
+  int count;
+  int first_tile[N + 1];  // apart from the problems: finding a tile's problem touches two lines of constant memory
   Problem p[N];
 };
 
@@ -107,34 +109,49 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint32_t (&hi)[4], u
     lo[e] = pack_half2(v[2 * e] - f.x, v[2 * e + 1] - f.y);
   }
 }
-// sum += c (hi + lo) of up to 128 columns of a row of planes, `left` of which exist
-__device__ __forceinline__ void add_planes(float (&sum)[128], const half16* m, long plane, long at, int left, float c) {
+
+// An epilogue thread holds a row of the tile; in memory a row is contiguous.  So tiles pass through 4 KB of shared memory
+// per warp, 32 rows of 128 bytes with their 16-byte chunks swizzled, and every access to global memory covers four whole
+// 128-byte lines (one thread per row took 3 to 4 us per tile and matrix, eight sectors where one would do).
+__device__ __forceinline__ int piece_at(int row, int chunk) { return row * 8 + (chunk ^ (row & 7)); }
+
+// sum[c0 .. c0 + 63] += c * m, 64 columns of one plane; m points at the warp's first row and this column
+__device__ __forceinline__ void add_piece(float (&sum)[128], int c0, const half16* m, long ld, int rows, int cols, float c, uint4* piece, int lane) {
+  uint4 v[8];
 #pragma unroll
-  for (int b = 0; b < 128; b += 32) {
-    uint4 h[4], l[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (b + 8 * q < left) {
-        h[q] = *reinterpret_cast<const uint4*>(m + at + b + 8 * q);
-        l[q] = *reinterpret_cast<const uint4*>(m + plane + at + b + 8 * q);
-      }
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (b + 8 * q < left) {
-        const uint32_t hw[4] = {h[q].x, h[q].y, h[q].z, h[q].w}, lw[4] = {l[q].x, l[q].y, l[q].z, l[q].w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 hf = unpack_half2(hw[e]), lf = unpack_half2(lw[e]);
-          sum[b + 8 * q + 2 * e] = fmaf(c, hf.x + lf.x, sum[b + 8 * q + 2 * e]);
-          sum[b + 8 * q + 2 * e + 1] = fmaf(c, hf.y + lf.y, sum[b + 8 * q + 2 * e + 1]);
-        }
-      }
+  for (int q = 0; q < 8; ++q) {
+    const int r = q * 4 + lane / 8, k = lane % 8;
+    v[q] = r < rows && k * 8 < cols ? *reinterpret_cast<const uint4*>(m + r * ld + k * 8) : make_uint4(0, 0, 0, 0);
   }
+#pragma unroll
+  for (int q = 0; q < 8; ++q) piece[piece_at(q * 4 + lane / 8, lane % 8)] = v[q];
+  __syncwarp();
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const uint4 h = piece[piece_at(lane, k)];
+    const uint32_t w[4] = {h.x, h.y, h.z, h.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 f = unpack_half2(w[e]);
+      sum[c0 + 8 * k + 2 * e] = fmaf(c, f.x, sum[c0 + 8 * k + 2 * e]);
+      sum[c0 + 8 * k + 2 * e + 1] = fmaf(c, f.y, sum[c0 + 8 * k + 2 * e + 1]);
+    }
+  }
+  __syncwarp();
 }
-__device__ __forceinline__ void update(const Problem& p, long at, float v) {
-  const float w = fmaf(p.keep, p.w[at], v);
-  p.w[at] = w;
-  if (p.w16) p.w16[at] = __float2bfloat16_rn(w);
+__device__ __forceinline__ void add_planes(float (&sum)[128], const half16* m, long plane, long ld, int rows, int cols, float c, uint4* piece, int lane) {
+  if (!m || rows <= 0) return;
+#pragma unroll
+  for (int c0 = 0; c0 < 128; c0 += 64)
+    if (c0 < cols) {
+      add_piece(sum, c0, m + c0, ld, rows, cols - c0, c, piece, lane);
+      add_piece(sum, c0, m + plane + c0, ld, rows, cols - c0, c, piece, lane);
+    }
+}
+__device__ __forceinline__ void update(float* w, bf16* w16, long at, float keep, float v) {
+  const float x = fmaf(keep, w[at], v);
+  w[at] = x;
+  if (w16) w16[at] = __float2bfloat16_rn(x);
 }
 
 template <int N>
@@ -142,7 +159,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t bars = smem_base + kStages * kStageBytes;
+  const uint32_t pieces = smem_base + kStages * kStageBytes, bars = pieces + 8 * kPieceBytes;
   auto full_bar = [&](int s) { return bars + 8u * s; };                   // used in the even CTA
   auto empty_bar = [&](int s) { return bars + 8u * (kStages + s); };      // both CTAs
   auto acc_full_bar = [&](int b) { return bars + 8u * (2 * kStages + b); };       // both CTAs
@@ -154,12 +171,12 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const bool leader = rank == 0;
-  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1, total = L.first_tile[L.count];
 
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int s = 0; s < kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(acc_full_bar(b), 1); mbar_init(acc_empty_bar(b), 4); }  // two groups, two CTAs
+    for (int b = 0; b < 2; ++b) { mbar_init(acc_full_bar(b), 1); mbar_init(acc_empty_bar(b), 16); }  // the epilogue warps of both CTAs
     mbar_init(drain_bar, 1);
     mbar_fence_init();
   }
@@ -172,6 +189,9 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
   cluster_sync_all();  // the peer's barriers are initialised before anything signals them
   tc_fence_after();
   const uint32_t tmem_base = tmem_base_slot;
+  // What comes before overlapped the previous launch; what follows reads its results.
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
 
   if (warp < 4) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
@@ -184,20 +204,20 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
       int stage = 0, pi = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int w = pair; w < L.total && ok; w += n_pairs) {
-        while (pi + 1 < L.count && w >= L.p[pi + 1].first_tile) ++pi;
+      for (int w = pair; w < total && ok; w += n_pairs) {
+        while (w >= L.first_tile[pi + 1]) ++pi;
         const Problem& p = L.p[pi];
         int ti, tj;
-        find_tile(p, w - p.first_tile, ti, tj);
-        const int row = (2 * ti + (int)rank) * BM, col = tj * BN + (int)rank * (BN / 2);
-        for (int kb = 0; kb < p.k_stages; ++kb) {
+        find_tile(p, w - L.first_tile[pi], ti, tj);
+        const int row = (2 * ti + (int)rank) * BM, col = tj * BN + (int)rank * (BN / 2), k_stages = p.k_stages, mn = p.b_mn;
+        for (int kb = 0; kb < k_stages; ++kb) {
           if (!mbar_wait(empty_bar(stage), phase ^ 1, &abort_flag, &g_muon_error, kDevTimeoutStageFree)) { ok = false; break; }
           const uint32_t sa = smem_base + stage * kStageBytes, sb = sa + kOperandBytes;
           const uint32_t full = map_to_cta(full_bar(stage), 0);
           // the even CTA announces the bytes of both CTAs' copies; what lies outside a matrix arrives as zeros
           if (leader) mbar_expect_tx(full_bar(stage), 2 * kStageBytes);
           tma_load_3d_pair(sa, &p.a, full, kb * BK, row, 0);
-          if (p.b_mn) {
+          if (mn) {
             tma_load_3d_pair(sb, &p.b, full, col, kb * BK, 0);
             tma_load_3d_pair(sb + kPlaneBytes, &p.b, full, col + 64, kb * BK, 0);
           } else {
@@ -229,16 +249,17 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
       int stage = 0, pi = 0;
       uint32_t phase = 0, chunk = 0;
       bool ok = true;
-      for (int w = pair; w < L.total && ok; w += n_pairs) {
-        while (pi + 1 < L.count && w >= L.p[pi + 1].first_tile) ++pi;
+      for (int w = pair; w < total && ok; w += n_pairs) {
+        while (w >= L.first_tile[pi + 1]) ++pi;
         const Problem& p = L.p[pi];
         const bool mn = p.b_mn != 0;
+        const int k_stages = p.k_stages, chain = chain_stages(k_stages);
         const uint32_t idesc = umma_idesc_f16(2 * BM, BN, 0, mn);
         // K-major: lo 128 rows behind hi, 16 k = 32 bytes of the swizzled row.  MN-major: two groups of 64 columns, each
         // 64 k-rows of hi then of lo; 16 k = 16 rows.
         const uint32_t b_lo = mn ? kPlaneBytes / 2 : kPlaneBytes, b_step = mn ? 2048 : 32, b_lbo = mn ? kPlaneBytes : 16;
-        for (int kb0 = 0, kb1; kb0 < p.k_stages && ok; kb0 = kb1, ++chunk) {
-          kb1 = min(kb0 + chain_stages(kb0, p.k_stages), p.k_stages);
+        for (int kb0 = 0, kb1; kb0 < k_stages && ok; kb0 = kb1, ++chunk) {
+          kb1 = min(kb0 + chain, k_stages);
           const int buf = chunk & 1;
           if (!mbar_wait(acc_empty_bar(buf), ((chunk >> 1) & 1) ^ 1, &abort_flag, &g_muon_error, kDevTimeoutTmemFree)) { ok = false; break; }
           tc_fence_after();
@@ -277,97 +298,135 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
     // -------------------------------- epilogue --------------------------------
     const int group = (warp - 4) >> 2, quarter = warp & 3;  // half of the columns; the lane quarter this warp may read
-    const bool elected = threadIdx.x == 128 + 128 * group;
+    uint4* piece = reinterpret_cast<uint4*>(smem_raw + (pieces - smem_u32(smem_raw)) + (warp - 4) * kPieceBytes);
     int pi = 0;
     uint32_t chunk = 0;
     bool ok = true;
-    for (int w = pair; w < L.total && ok; w += n_pairs) {
-      while (pi + 1 < L.count && w >= L.p[pi + 1].first_tile) ++pi;
+    for (int w = pair; w < total && ok; w += n_pairs) {
+      while (w >= L.first_tile[pi + 1]) ++pi;
       const Problem& p = L.p[pi];
       int ti, tj;
-      find_tile(p, w - p.first_tile, ti, tj);
-      const int i = (2 * ti + (int)rank) * BM + quarter * 32 + lane, j0 = tj * BN + group * 128;
+      find_tile(p, w - L.first_tile[pi], ti, tj);
+      const int i0 = (2 * ti + (int)rank) * BM + quarter * 32, j0 = tj * BN + group * 128;  // the warp's first row and column
+      const int rows = p.m - i0, cols = p.n - j0;                                           // what there is from there on
+      const int k_stages = p.k_stages, chain = chain_stages(k_stages);
       // the sums start from what is added to the product: its loads pass while the first chain runs
       float sum[128];
 #pragma unroll
       for (int j = 0; j < 128; ++j) sum[j] = 0.f;
-      if (p.add1 && i < p.m) add_planes(sum, p.add1, p.plane, (long)i * p.ld + j0, p.n - j0, p.c1);
-      if (p.add2 && i < p.m) add_planes(sum, p.add2, p.plane, (long)i * p.ld + j0, p.n - j0, p.c2);
-      for (int kb0 = 0; kb0 < p.k_stages; kb0 += chain_stages(kb0, p.k_stages), ++chunk) {
+      add_planes(sum, p.add1 ? p.add1 + i0 * p.ld + j0 : nullptr, p.plane, p.ld, rows, cols, p.c1, piece, lane);
+      add_planes(sum, p.add2 ? p.add2 + i0 * p.ld + j0 : nullptr, p.plane, p.ld, rows, cols, p.c2, piece, lane);
+      for (int kb0 = 0; kb0 < k_stages; kb0 += chain, ++chunk) {
         const int buf = chunk & 1;
-        const bool got = mbar_wait(acc_full_bar(buf), (chunk >> 1) & 1, &abort_flag, &g_muon_error, kDevTimeoutAccum);
-        if (named_bar_or(1 + group, 128, !got)) { ok = false; break; }  // the group's warps leave together
+        if (!__all_sync(0xffffffffu, mbar_wait(acc_full_bar(buf), (chunk >> 1) & 1, &abort_flag, &g_muon_error, kDevTimeoutAccum))) { ok = false; break; }
         tc_fence_after();
         const uint32_t src = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + group * 128);
-        uint32_t v[2][16];
-        tmem_ld_32x16(src, v[0]);
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
+        for (int c = 0; c < 128; c += 32) {
+          uint32_t v[32];
+          tmem_ld_32x32(src + c, v);
           tmem_ld_wait();
-          if (c < 7) tmem_ld_32x16(src + (c + 1) * 16, v[(c + 1) & 1]);
 #pragma unroll
-          for (int j = 0; j < 16; ++j) sum[c * 16 + j] += __uint_as_float(v[c & 1][j]);
+          for (int j = 0; j < 32; ++j) sum[c + j] += __uint_as_float(v[j]);
         }
         tc_fence_before();
-        named_bar_sync(1 + group, 128);
-        if (elected) mbar_arrive_cluster(map_to_cta(acc_empty_bar(buf), 0));
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty_bar(buf), 0));
       }
       if (!ok) break;
 
-      if (i < p.m) {
-        float4 w_next[8];  // the weights of 32 columns, requested together
+      if (rows <= 0 || cols <= 0) continue;
+      const float alpha = p.alpha;
+      const long ld = p.ld;
+      if (!p.w) {
+        half16* out = p.out + i0 * ld + j0;
 #pragma unroll
-        for (int j = 0; j < 128; j += 8) {
-          if (p.w_vec && j % 32 == 0) {
+        for (int c0 = 0; c0 < 128; c0 += 64) {
+          if (c0 >= cols) break;
 #pragma unroll
-            for (int q = 0; q < 8; ++q)
-              if (j0 + j + 4 * q < p.n) w_next[q] = *reinterpret_cast<const float4*>(p.w + (long)i * p.w_ld + j0 + j + 4 * q);
-          }
-          if (j0 + j < p.n) {  // (a row of planes has room for whole eights)
-            float v[8];
+          for (int plane = 0; plane < 2; ++plane) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = p.alpha * sum[j + e];
-            const long at = (long)i * p.ld + j0 + j;
-            if (p.w) {
-              if (p.transposed) {  // lanes along a row of w
+            for (int k = 0; k < 8; ++k) {
+              float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                  if (j0 + j + e < p.n) update(p, (long)(j0 + j + e) * p.w_ld + i, v[e]);
-              } else {
-                const long to = (long)i * p.w_ld + j0 + j;
-                if (p.w_vec) {
-                  float4 a = w_next[j % 32 / 4], b = w_next[j % 32 / 4 + 1];
-                  a.x = fmaf(p.keep, a.x, v[0]); a.y = fmaf(p.keep, a.y, v[1]); a.z = fmaf(p.keep, a.z, v[2]); a.w = fmaf(p.keep, a.w, v[3]);
-                  b.x = fmaf(p.keep, b.x, v[4]); b.y = fmaf(p.keep, b.y, v[5]); b.z = fmaf(p.keep, b.z, v[6]); b.w = fmaf(p.keep, b.w, v[7]);
-                  *reinterpret_cast<float4*>(p.w + to) = a;
-                  *reinterpret_cast<float4*>(p.w + to + 4) = b;
-                  if (p.w16) {
-                    const __nv_bfloat162 q[4] = {__floats2bfloat162_rn(a.x, a.y), __floats2bfloat162_rn(a.z, a.w),
-                                                 __floats2bfloat162_rn(b.x, b.y), __floats2bfloat162_rn(b.z, b.w)};
-                    *reinterpret_cast<uint4*>(p.w16 + to) = *reinterpret_cast<const uint4*>(q);
-                  }
-                } else {
-#pragma unroll
-                  for (int e = 0; e < 8; ++e)
-                    if (j0 + j + e < p.n) update(p, to + e, v[e]);
-                }
-              }
-            } else {
+              for (int e = 0; e < 8; ++e) v[e] = alpha * sum[c0 + 8 * k + e];
               uint32_t hi[4], lo[4];
               split8(v, hi, lo);
-              *reinterpret_cast<uint4*>(p.out + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-              *reinterpret_cast<uint4*>(p.out + p.plane + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-              if (p.sym && ti != tj) {  // the mirror image, lanes along a row
+              piece[piece_at(lane, k)] = plane ? make_uint4(lo[0], lo[1], lo[2], lo[3]) : make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            }
+            __syncwarp();
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                  if (j0 + j + e < p.n) {
-                    half16* q = p.out + (long)(j0 + j + e) * p.ld + i;
-                    q[0] = (half16)(hi[e / 2] >> (16 * (e & 1)));
-                    q[p.plane] = (half16)(lo[e / 2] >> (16 * (e & 1)));
-                  }
+            for (int q = 0; q < 8; ++q) {  // (a row of planes has room for whole eights)
+              const int r = q * 4 + lane / 8, k = lane % 8;
+              if (r < rows && c0 + k * 8 < cols)
+                *reinterpret_cast<uint4*>(out + plane * p.plane + r * ld + c0 + k * 8) = piece[piece_at(r, k)];
+            }
+            __syncwarp();
+          }
+        }
+        if (p.sym && ti != tj && lane < rows) {  // the mirror image, lanes along a row
+          half16* at = p.out + j0 * ld + i0 + lane;
+#pragma unroll
+          for (int j = 0; j < 128; ++j)
+            if (j < cols) {
+              const float v = alpha * sum[j];
+              const __half h = __float2half_rn(v), l = __float2half_rn(v - __half2float(h));
+              at[j * ld] = __half_as_ushort(h);
+              at[p.plane + j * ld] = __half_as_ushort(l);
+            }
+        }
+      } else if (p.transposed) {  // lanes along a row of w
+        if (lane < rows) {
+          const long at = j0 * p.w_ld + i0 + lane;
+#pragma unroll
+          for (int j = 0; j < 128; ++j)
+            if (j < cols) update(p.w, p.w16, at + j * p.w_ld, p.keep, alpha * sum[j]);
+        }
+      } else {
+        const float keep = p.keep;
+        const long w_ld = p.w_ld;
+        float* w = p.w + i0 * w_ld + j0;
+        bf16* w16 = p.w16 ? p.w16 + i0 * w_ld + j0 : nullptr;
+#pragma unroll
+        for (int c0 = 0; c0 < 128; c0 += 32) {
+          if (c0 >= cols) break;
+          const int r0 = lane / 8, k0 = lane % 8;
+          const bool vec = p.w_vec && c0 + k0 * 4 < cols;
+          float4 old[8];
+          if (vec) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              if (q * 4 + r0 < rows) old[q] = *reinterpret_cast<const float4*>(w + (q * 4 + r0) * w_ld + c0 + k0 * 4);
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            piece[piece_at(lane, k)] = make_uint4(__float_as_uint(alpha * sum[c0 + 4 * k]), __float_as_uint(alpha * sum[c0 + 4 * k + 1]),
+                                                  __float_as_uint(alpha * sum[c0 + 4 * k + 2]), __float_as_uint(alpha * sum[c0 + 4 * k + 3]));
+          __syncwarp();
+          if (vec) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const int r = q * 4 + r0;
+              if (r >= rows) break;
+              const uint4 d = piece[piece_at(r, k0)];
+              float4 v;
+              v.x = fmaf(keep, old[q].x, __uint_as_float(d.x));
+              v.y = fmaf(keep, old[q].y, __uint_as_float(d.y));
+              v.z = fmaf(keep, old[q].z, __uint_as_float(d.z));
+              v.w = fmaf(keep, old[q].w, __uint_as_float(d.w));
+              *reinterpret_cast<float4*>(w + r * w_ld + c0 + k0 * 4) = v;
+              if (w16) {
+                const __nv_bfloat162 b[2] = {__floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w)};
+                *reinterpret_cast<uint2*>(w16 + r * w_ld + c0 + k0 * 4) = *reinterpret_cast<const uint2*>(b);
               }
             }
+          } else if (!p.w_vec && c0 + lane < cols) {
+#pragma unroll 4
+            for (int r = 0; r < 32; ++r)
+              if (r < rows)
+                update(w, w16, r * w_ld + c0 + lane, keep, reinterpret_cast<const float*>(piece + piece_at(r, lane / 4))[lane % 4]);
           }
+          __syncwarp();
         }
       }
     }
@@ -584,18 +643,27 @@ template <int N> cudaError_t launch_products(Launch<N>& L, cudaStream_t st) {
     Problem& p = L.p[i];
     p.tiles_m = (p.m + 2 * BM - 1) / (2 * BM);
     p.tiles_n = (p.n + BN - 1) / BN;
-    p.first_tile = tiles;
+    L.first_tile[i] = tiles;
     tiles += p.sym ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
   }
-  L.total = tiles;
+  L.first_tile[L.count] = tiles;
   cudaError_t e = cudaFuncSetAttribute(split_product_pair_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   if (e != cudaSuccess) return e;
   int dev = 0, sms = 148;
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   const int pairs = tiles < sms / 2 ? tiles : sms / 2;
-  split_product_pair_kernel<N><<<2 * pairs, kThreads, kSmemBytes, st>>>(L);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(2 * pairs));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, split_product_pair_kernel<N>, L);
 }
 
 struct Options {
@@ -725,7 +793,7 @@ cudaError_t update_batch(const vgg19_muon_tensor* tensors, const int count, cons
         p.w = t.w; p.w16 = static_cast<bf16*>(t.w_bf16);
         p.w_ld = t.cols;
         p.transposed = s.transposed;
-        p.w_vec = t.cols % 8 == 0 && reinterpret_cast<uintptr_t>(t.w) % 16 == 0 && reinterpret_cast<uintptr_t>(t.w_bf16) % 16 == 0;
+        p.w_vec = t.cols % 4 == 0 && reinterpret_cast<uintptr_t>(t.w) % 16 == 0 && reinterpret_cast<uintptr_t>(t.w_bf16) % 8 == 0;
       }
     }
     run();
