@@ -54,6 +54,10 @@ constexpr int kMaxTensors = 20, kMaxProblems = 2 * kMaxTensors;
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kScaleX = 4096.f, kScaleA = 16384.f, kScaleP = 8192.f, kScaleQ2 = 4096.f, kScaleQ3 = 1024.f;
 constexpr int kStepsPerGram = 3;
+// R = b A + c A A from A: the product's factor and the addend's, as Problem has them; the scale of S after step k.
+__host__ __device__ constexpr float poly_alpha() { return kC * kScaleP / (kScaleA * kScaleA); }
+__host__ __device__ constexpr float poly_c1() { return kB * kScaleP / kScaleA / poly_alpha(); }
+__host__ __device__ constexpr float rest_scale(int k) { return k == 0 ? kScaleP : k == 1 ? kScaleQ2 : kScaleQ3; }
 
 // ---- one product ---------------------------------------------------------------------------------------------
 // D[i][j] = alpha * (c1 add1[i][j] + c2 add2[i][j] + sum_k A[i][k] B[j][k]) (or B[k][j]: b_mn), m x n.
@@ -444,6 +448,170 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
   }
 }
 
+// ---- all steps of small matrices in one block --------------------------------------------------------------------
+// Where every matrix of a call has at most 128 rows, a launch per product is nearly all latency (11 us for 2 us of work).
+// Then one block per tensor keeps A, R and S in shared memory, 64 KB each as K-major operand tiles, and takes the steps
+// between two Gram matrices in one launch.  The products, their chains and the order of every addition are the product
+// kernel's: the results are the same, bit for bit.
+constexpr int kSmall = 128, kSmallThreads = 256, kSmallBytes = 4 * kPlaneBytes;  // a matrix: [64 columns][hi, lo][128 rows][128 bytes]
+constexpr int kSmallSmem = 3 * kSmallBytes + 1024 + 64;
+struct SmallTensor {
+  CUtensorMap gram, rest;  // A, and where S goes
+  int k_stages, pad[15];
+};
+struct SmallLaunch {
+  int group, pad[15];
+  SmallTensor t[kMaxTensors];
+};
+
+__global__ void __launch_bounds__(kSmallThreads, 1) small_steps_kernel(const __grid_constant__ SmallLaunch L) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t A = base, R = base + kSmallBytes, S = R + kSmallBytes, load_bar = S + kSmallBytes, done_bar = load_bar + 8;
+  __shared__ uint32_t tmem_base_slot;
+  __shared__ int abort_flag;
+  const SmallTensor& t = L.t[blockIdx.x];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, k_stages = t.k_stages;
+  if (tid == 0) {
+    abort_flag = 0;
+    mbar_init(load_bar, 1);
+    mbar_init(done_bar, 1);
+    mbar_fence_init();
+  }
+  if (warp == 0) {
+    tmem_alloc(smem_u32(&tmem_base_slot), 256);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_base_slot;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  if (tid == 0) {
+    mbar_expect_tx(load_bar, k_stages * kOperandBytes);
+    for (int kb = 0; kb < k_stages; ++kb) tma_load_3d(A + kb * kOperandBytes, &t.gram, load_bar, kb * BK, 0, 0);
+  }
+  bool ok = __syncthreads_and(mbar_wait(load_bar, 0, &abort_flag, &g_muon_error, kDevTimeoutTmaFull));
+  tc_fence_after();
+
+  // thread: row `row` and 64 columns of every result
+  const int row = (warp & 3) * 32 + lane, group = warp >> 2;
+  uint8_t* generic = smem_raw + (base - smem_u32(smem_raw)) + group * kOperandBytes + row * 128;
+  auto at = [&](uint32_t m, int plane, int chunk) { return reinterpret_cast<uint4*>(generic + (m - base) + plane * kPlaneBytes + ((chunk ^ (row & 7)) << 4)); };
+  uint32_t phase = 0;
+  // D = alpha * (c1 add1 + c2 add2 + x y)
+  auto product = [&](uint32_t x, uint32_t y, uint32_t d, float alpha, uint32_t add1, float c1, uint32_t add2, float c2) {
+    if (!ok) return;
+    if (tid == 0) {
+      constexpr uint32_t idesc = umma_idesc_f16(128, 128, 0, 0);
+      for (int kb = 0; kb < k_stages; ++kb) {
+        const uint32_t sx = x + kb * kOperandBytes, sy = y + kb * kOperandBytes, acc = tmem_base + kb * 128;
+        const uint64_t xh = smem_desc_sw128(sx, 16), xl = smem_desc_sw128(sx + kPlaneBytes, 16);
+        const uint64_t yh = smem_desc_sw128(sy, 16), yl = smem_desc_sw128(sy + kPlaneBytes, 16);
+        umma_bf16(acc, xl, yh, idesc, 0u);
+        umma_bf16_acc(acc, xh, yl, idesc);
+#pragma unroll
+        for (int k = 1; k < BK / 16; ++k) {
+          umma_bf16_acc(acc, desc_advance(xl, k * 32), desc_advance(yh, k * 32), idesc);
+          umma_bf16_acc(acc, desc_advance(xh, k * 32), desc_advance(yl, k * 32), idesc);
+        }
+#pragma unroll
+        for (int k = 0; k < BK / 16; ++k) umma_bf16_acc(acc, desc_advance(xh, k * 32), desc_advance(yh, k * 32), idesc);
+      }
+      umma_commit(done_bar);
+    }
+    float sum[64];
+#pragma unroll
+    for (int j = 0; j < 64; ++j) sum[j] = 0.f;
+    if (group < k_stages) {
+      auto add = [&](uint32_t m, float c) {
+#pragma unroll
+        for (int plane = 0; plane < 2; ++plane)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const uint4 h = *at(m, plane, k);
+            const uint32_t w[4] = {h.x, h.y, h.z, h.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 f = unpack_half2(w[e]);
+              sum[8 * k + 2 * e] = fmaf(c, f.x, sum[8 * k + 2 * e]);
+              sum[8 * k + 2 * e + 1] = fmaf(c, f.y, sum[8 * k + 2 * e + 1]);
+            }
+          }
+      };
+      add(add1, c1);
+      if (add2) add(add2, c2);
+    }
+    ok = __syncthreads_and(mbar_wait(done_bar, phase, &abort_flag, &g_muon_error, kDevTimeoutAccum));
+    phase ^= 1;
+    if (!ok) return;
+    tc_fence_after();
+    if (group < k_stages) {
+      for (int kb = 0; kb < k_stages; ++kb) {
+#pragma unroll
+        for (int c = 0; c < 64; c += 16) {
+          uint32_t v[16];
+          tmem_ld_32x16(tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(kb * 128 + group * 64 + c), v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 16; ++j) sum[c + j] += __uint_as_float(v[j]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = alpha * sum[8 * k + e];
+        uint32_t hi[4], lo[4];
+        split8(v, hi, lo);
+        *at(d, 0, k) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *at(d, 1, k) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      }
+    }
+    tc_fence_before();
+    fence_async_smem();  // the tensor core and the copy engine read what was written here
+    __syncthreads();
+    tc_fence_after();
+  };
+
+  float q0 = kA, sq = kScaleP;
+  for (int k = 0; k < L.group; ++k) {
+    const uint32_t poly = k == 0 ? S : R;
+    product(A, A, poly, poly_alpha(), A, poly_c1(), 0, 0.f);
+    if (k > 0) {
+      const float sn = rest_scale(k);
+      const float alpha = sn / (kScaleP * sq);
+      product(R, S, S, alpha, S, kA * sn / sq / alpha, R, q0 * sn / kScaleP / alpha);
+      q0 *= kA;
+      sq = sn;
+    }
+    if (k + 1 < L.group)
+      for (int twice = 0; twice < 2; ++twice) product(poly, A, A, 1.f / kScaleP, A, kA / (1.f / kScaleP), 0, 0.f);
+  }
+  if (tid == 0 && ok) {
+    for (int kb = 0; kb < k_stages; ++kb)
+      asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(&t.rest),
+                   "r"(S + kb * kOperandBytes), "r"(kb * BK), "r"(0), "r"(0) : "memory");
+    tma_store_commit();
+    tma_store_wait_all();
+  }
+  if (tid == 0 && !ok) {
+    // gave up: copies and products in flight get a while to end before shared and tensor memory go away
+    const unsigned long long t0 = global_timer_ns();
+    while (!mbar_try_wait(load_bar, 0) && global_timer_ns() - t0 < 100000000ull) {}
+    while (!mbar_try_wait(done_bar, phase ^ 1) && global_timer_ns() - t0 < 100000000ull) {}
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem_base, 256);
+  }
+}
+
 // ---- momentum, norm, X_0 ----------------------------------------------------------------------------------------
 struct Element {
   const float* grad;
@@ -666,6 +834,22 @@ template <int N> cudaError_t launch_products(Launch<N>& L, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, split_product_pair_kernel<N>, L);
 }
 
+cudaError_t launch_small(const SmallLaunch& L, int count, cudaStream_t st) {
+  cudaError_t e = cudaFuncSetAttribute(small_steps_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)count);
+  cfg.blockDim = dim3(kSmallThreads);
+  cfg.dynamicSmemBytes = kSmallSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, small_steps_kernel, L);
+}
+
 struct Options {
   float lr, mu, decay;
   int steps, nesterov;
@@ -723,6 +907,8 @@ cudaError_t update_batch(const vgg19_muon_tensor* tensors, const int count, cons
     return p;
   };
   auto run = [&] { if (err == cudaSuccess) err = launch_products(L, st); L.count = 0; };
+  bool small = true;
+  for (int i = 0; i < count; ++i) small = small && Shape(tensors[i]).m <= kSmall;
   L.count = 0;
   int x = kX0;
   for (int done = 0; done < o.steps;) {
@@ -737,16 +923,29 @@ cudaError_t update_batch(const vgg19_muon_tensor* tensors, const int count, cons
     // the tensor core truncates is then relative to the smaller rest.
     Matrix q = kQa;  // S
     float sq = kScaleP, q0 = kA;
-    for (int k = 0; k < group; ++k) {
+    if (small) {
+      static thread_local SmallLaunch sl;
+      sl.group = group;
+      for (int i = 0; i < count; ++i) {
+        sl.t[i].gram = planes[i].k_major[kGramA];
+        sl.t[i].rest = planes[i].k_major[kQa];
+        sl.t[i].k_stages = (int)((Shape(tensors[i]).m + BK - 1) / BK);
+      }
+      if (err == cudaSuccess) err = launch_small(sl, count, st);
+      sq = rest_scale(group - 1);
+      for (int k = 1; k < group; ++k) q0 *= kA;
+    }
+    for (int k = small ? group : 0; k < group; ++k) {
       const Matrix poly = k == 0 ? kQa : kPoly;  // R; the first one is also the first S
       for (int i = 0; i < count; ++i) {
         Problem& p = symmetric(i, kGramA, kScaleA, kGramA, kScaleA, poly, kC * kScaleP);
-        p.add1 = planes[i].at[kGramA]; p.c1 = kB * kScaleP / kScaleA / p.alpha;
+        p.alpha = poly_alpha();
+        p.add1 = planes[i].at[kGramA]; p.c1 = poly_c1();
       }
       run();
       if (k > 0) {  // S <- a S + q0 R + R S
         const Matrix next = q == kQa ? kQb : kQa;
-        const float sn = k == 1 ? kScaleQ2 : kScaleQ3;
+        const float sn = rest_scale(k);
         for (int i = 0; i < count; ++i) {
           Problem& p = symmetric(i, poly, kScaleP, q, sq, next, sn);
           p.add1 = planes[i].at[q]; p.c1 = kA * sn / sq / p.alpha;
