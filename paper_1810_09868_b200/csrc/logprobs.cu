@@ -4,10 +4,15 @@
 //   d(sum_i g_i log p[id_i] + w H) / dz_j = sum_i g_i [j = id_i] - p_j (sum_i g_i + w (log p_j + H)).
 //
 // Both directions are bound by reading the logits (and writing the gradient) once.  The forward kernel makes one
-// pass: every warp keeps a reference `ref` (a value near the largest it has seen), S = sum exp(z - ref) and
-// U = sum exp(z - ref) (z - ref), in fp32, and at the end H = log S - U / S, lse = ref + log S.  The top
-// alternatives ride on the same pass: a warp holds its best `top_k` as 64-bit keys (value, then lower index), sorted
-// over its lanes, and looks closer only at vectors whose maximum reaches the smallest of them.
+// pass: every thread keeps a reference `ref` (a value near the largest it has seen), S = sum exp(z - ref) and
+// U = sum exp(z - ref) (z - ref), in fp32, and at the end H = log S - U / S, lse = ref + log S.  Issue slots are what it
+// has to save (bf16 at the memory's rate leaves 11 instructions a logit): exponents and sums go two at a time
+// (f32x2), the reference is looked at once per 16 logits.
+//
+// The top alternatives cost that pass one maximum per thread.  A value that at least top_k of the threads' maxima
+// reach (found by bisection) is reached by top_k logits; only the threads whose maximum reaches it, about top_k, read
+// their logits again and sort those that do, as 64-bit keys (value, then lower index).  Keeping a sorted list during
+// the pass instead took twice the time for the best 8 of 50021.
 //
 // A row belongs to one block, or, where there are fewer rows than the GPU has room for, to a cluster of up to
 // eight blocks that join through distributed shared memory: one launch, no scratch, and an order of summation that
@@ -26,8 +31,8 @@ namespace {
 static __device__ int g_logprobs_error;  // kDevBadLabel once an id outside [0, classes) was met
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// A warp's reference moves only when a value exceeds it by this much (natural units): exp(z - ref) then stays below
-// e^4, and the moves, each a branch of the whole warp, stay rare after the first vectors.
+// A reference moves only when a value exceeds it by this much (natural units): exp(z - ref) then stays below e^4, and
+// the moves stay rare after the first vectors.
 constexpr float kRefMargin = 4.f;
 constexpr float kFloor = -200.f;  // exp2 of anything lower is 0 in fp32; keeps 0 * (-inf) out of U
 constexpr int kMaxTop = VGG19_LOGPROBS_MAX_TOP, kMaxIds = VGG19_LOGPROBS_MAX_IDS;
@@ -43,16 +48,40 @@ __device__ __forceinline__ float fast_exp2(float x) {
   return r;
 }
 
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float a, float b) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
 // values ordered as unsigned integers; -0 counts as 0
-__device__ __forceinline__ unsigned long long make_key(float v, unsigned index) {
+__device__ __forceinline__ unsigned ordered(float v) {
   const int b = __float_as_int(v + 0.f);
-  const unsigned o = b < 0 ? ~(unsigned)b : (unsigned)b | 0x80000000u;
-  return ((unsigned long long)o << 32) | (0xffffffffu - index);
+  return b < 0 ? ~(unsigned)b : (unsigned)b | 0x80000000u;
 }
-__device__ __forceinline__ float key_value(unsigned long long k) {
-  const unsigned o = (unsigned)(k >> 32);
-  return __int_as_float((int)(o & 0x80000000u ? o & 0x7fffffffu : ~o));
+__device__ __forceinline__ float value_of(unsigned o) { return __int_as_float((int)(o & 0x80000000u ? o & 0x7fffffffu : ~o)); }
+constexpr unsigned kLowest = 0x00800000u;  // ordered(lowest finite value)
+__device__ __forceinline__ unsigned long long make_key(float v, unsigned index) {
+  return ((unsigned long long)ordered(v) << 32) | (0xffffffffu - index);
 }
+__device__ __forceinline__ float key_value(unsigned long long k) { return value_of((unsigned)(k >> 32)); }
 __device__ __forceinline__ unsigned key_index(unsigned long long k) { return 0xffffffffu - (unsigned)k; }
 
 // 16 bytes of logits as floats
@@ -104,99 +133,70 @@ template <typename T> struct RowSplit {
 struct Sums {  // of a set of logits: reference, sum of exp, sum of exp times its exponent in base 2
   float ref, S, U;
 };
-// b folded into a; either may be empty (ref = -inf, S = 0, or NaN when a NaN was met)
-__device__ __forceinline__ Sums join(Sums a, Sums b) {
-  const float m = fmaxf(a.ref, b.ref);
-  const float da = a.ref == m ? 0.f : (a.ref - m) * kLog2e, db = b.ref == m ? 0.f : (b.ref - m) * kLog2e;
-  const float fa = fast_exp2(da), fb = fast_exp2(db);
-  Sums r;
-  r.ref = m;
-  r.S = a.S * fa + b.S * fb;
-  // an empty or vanished part (factor 0) would bring -inf * 0
-  r.U = (fa > 0.f ? (a.U + da * a.S) * fa : a.U * 0.f) + (fb > 0.f ? (b.U + db * b.S) * fb : b.U * 0.f);
-  return r;
-}
+// A thread's sums over the logits it has seen, and the largest of them.
+struct Scan {
+  float ref = -INFINITY, r = 0.f, top = -INFINITY;  // r: ref, but 0 while that is -inf, when every exponent is -inf anyway
+  f32x2 S = 0, U = 0;                               // (the bits of two zeros)
 
-// A warp's state over the logits it has seen.
-struct WarpScan {
-  float ref, S, U;         // ref is the same in all lanes, S and U are a lane's share
-  unsigned long long key;  // lane i: the i-th best so far, 0 for none
-  float thr;               // a logit below this cannot enter the best top_k
-  int top_k;
-
-  __device__ WarpScan(int k) : ref(-INFINITY), S(0.f), U(0.f), key(0), thr(k > 0 ? -3.402823466e38f : INFINITY), top_k(k) {}
-
-  __device__ __forceinline__ void insert(unsigned long long c) {
-    const unsigned long long up = __shfl_up_sync(0xffffffffu, key, 1);
-    const int lane = threadIdx.x & 31;
-    if (c > key) key = lane > 0 && c > up ? up : c;
-  }
-
-  // the vector's N logits; index(e) is the class of element e of this lane
-  template <int N, typename Index> __device__ __forceinline__ void add(const float (&x)[N], Index index) {
+  template <int N> __device__ __forceinline__ void add(const float (&x)[N]) {
     float mx = x[0];
 #pragma unroll
     for (int e = 1; e < N; ++e) mx = fmaxf(mx, x[e]);
-    if (__any_sync(0xffffffffu, mx > ref + kRefMargin || mx >= thr)) slow(x, mx, index);
-    const float r = ref == -INFINITY ? 0.f : ref;  // nothing but -inf so far: every exponent is -inf
-    float s0 = 0.f, s1 = 0.f, u0 = 0.f, u1 = 0.f;
+    top = fmaxf(top, mx);
+    if (mx > ref + kRefMargin) {
+      if (ref != -INFINITY) {
+        const float d = (ref - mx) * kLog2e, f = fast_exp2(d);
+        const f32x2 dd = pack2(d, d), ff = pack2(f, f);
+        U = f > 0.f ? mul2(fma2(dd, S, U), ff) : mul2(U, ff);
+        S = mul2(S, ff);
+      }
+      ref = r = mx;
+    }
+    const f32x2 minus = pack2(-r, -r), log2e = pack2(kLog2e, kLog2e);
 #pragma unroll
     for (int e = 0; e < N; e += 2) {
-      const float t0 = max_nan((x[e] - r) * kLog2e, kFloor);
-      const float e0 = fast_exp2(t0);
-      s0 += e0; u0 = fmaf(e0, t0, u0);
-      if (e + 1 < N) {
-        const float t1 = max_nan((x[e + 1] - r) * kLog2e, kFloor);
-        const float e1 = fast_exp2(t1);
-        s1 += e1; u1 = fmaf(e1, t1, u1);
-      }
+      float a, b;
+      unpack2(mul2(add2(pack2(x[e], e + 1 < N ? x[e + 1] : -INFINITY), minus), log2e), a, b);
+      a = max_nan(a, kFloor);
+      b = max_nan(b, kFloor);
+      const f32x2 p = pack2(fast_exp2(a), fast_exp2(b));
+      S = add2(S, p);
+      U = fma2(p, pack2(a, b), U);
     }
-    S += s0 + s1;
-    U += u0 + u1;
   }
+};
 
-  template <int N, typename Index> __device__ __forceinline__ void slow(const float (&x)[N], float mx, Index index) {
-    const unsigned full = 0xffffffffu;
-    float wm = mx;
+// The sums of a warp's lanes (lanes without any have ref = -inf, S = U = 0), in every lane.
+__device__ __forceinline__ Sums lanes_join(Sums a) {
+  float m = a.ref;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) wm = fmaxf(wm, __shfl_xor_sync(full, wm, o));
-    if (wm > ref + kRefMargin) {
-      if (ref != -INFINITY) {
-        const float d = (ref - wm) * kLog2e, f = fast_exp2(d);
-        U = f > 0.f ? (U + d * S) * f : 0.f * U;
-        S *= f;
-      }
-      ref = wm;
-    }
-    if (top_k == 0 || !__any_sync(full, mx >= thr)) return;
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float d = a.ref == m ? 0.f : (a.ref - m) * kLog2e, f = fast_exp2(d);
+  float S = a.S * f, U = f > 0.f ? (a.U + d * a.S) * f : a.U * 0.f;  // a vanished part would bring -inf * 0
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    S += __shfl_xor_sync(0xffffffffu, S, o);
+    U += __shfl_xor_sync(0xffffffffu, U, o);
+  }
+  return Sums{m, S, U};
+}
+
+// A warp's best keys, sorted over its lanes, largest first; 0 for none.
+struct Best {
+  unsigned long long key = 0;
+  // the elements of the lanes' x that are at least thr
+  template <int N, typename Index> __device__ __forceinline__ void add(const float (&x)[N], float thr, Index index) {
     const int lane = threadIdx.x & 31;
-    if (__shfl_sync(full, key, top_k - 1) == 0) {
-      // not full yet: the top_k-th largest of the lanes' maxima is a bound that top_k logits reach
-      int rank = 0;
-      for (int j = 0; j < 32; ++j) {
-        const float v = __shfl_sync(full, mx, j);
-        rank += v > mx || (v == mx && j < lane);
-      }
-      const unsigned at = __ballot_sync(full, rank == top_k - 1);
-      const float bound = at ? __shfl_sync(full, mx, __ffs(at) - 1) : -INFINITY;  // (a NaN lane takes no rank)
-      if (bound > thr) thr = bound;
-    }
-#pragma unroll 1
-    for (int e = 0; e < N; ++e) {
-      float v = x[0];
 #pragma unroll
-      for (int k = 1; k < N; ++k)
-        if (k == e) v = x[k];
-      unsigned hits = __ballot_sync(full, v >= thr);
+    for (int e = 0; e < N; ++e) {
+      unsigned hits = __ballot_sync(0xffffffffu, x[e] >= thr);
       if (!hits) continue;
-      const unsigned long long mine = v >= thr ? make_key(v, index(e)) : 0;
+      const unsigned long long mine = make_key(x[e], index(e));
       while (hits) {
-        const int src = __ffs(hits) - 1;
+        const unsigned long long c = __shfl_sync(0xffffffffu, mine, __ffs(hits) - 1), up = __shfl_up_sync(0xffffffffu, key, 1);
         hits &= hits - 1;
-        insert(__shfl_sync(full, mine, src));
+        if (c > key) key = lane > 0 && c > up ? up : c;
       }
-      const unsigned long long last = __shfl_sync(full, key, top_k - 1);
-      if (last) thr = fmaxf(thr, key_value(last));
     }
   }
 };
@@ -231,11 +231,14 @@ constexpr int kMaxCluster = 8;
 
 template <typename T, int NT, int UNROLL>
 __global__ void __launch_bounds__(NT) logprobs_kernel(const FwdArgs a) {
-  constexpr int V = Vec<T>::N, W = NT / 32;
+  constexpr int V = Vec<T>::N, W = NT / 32, GROUP = 16 / V;  // vectors a look at the reference
+  static_assert(UNROLL % GROUP == 0 && W <= 32 && kMaxCluster <= 32, "whole groups; a warp joins all parts");
   __shared__ Sums part[W];
-  __shared__ unsigned long long keys[W * kMaxTop];
+  __shared__ unsigned low[W], high[W];
+  __shared__ unsigned long long keys[W * kMaxTop], best[kMaxTop];
+  __shared__ int n_keys;
   __shared__ Sums cpart[kMaxCluster];                             // of the cluster's blocks, in its first
-  __shared__ unsigned long long ckeys[kMaxCluster * kMaxTop], best[kMaxTop];
+  __shared__ unsigned long long ckeys[kMaxCluster * kMaxTop];
   cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   if (C > 1) cluster.barrier_arrive();  // waited for before the first write into the first block's shared memory
@@ -245,67 +248,114 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(const FwdArgs a) {
   const RowSplit<T> sp(z, a.classes);
   const uint4* body = reinterpret_cast<const uint4*>(z + sp.head);
   const int v0 = (int)((long)sp.nvec * rank / C), v1 = (int)((long)sp.nvec * (rank + 1) / C);
+  if (tid == 0) n_keys = 0;
 
-  WarpScan w(a.top_k);
+  // thread t has the vectors v0 + t, v0 + t + NT, ...
+  Scan w;
   const uint4 none = make_uint4(Vec<T>::kMinusInf, Vec<T>::kMinusInf, Vec<T>::kMinusInf, Vec<T>::kMinusInf);
-  for (int base = v0 + warp * 32; base < v1; base += NT * UNROLL) {  // (a warp leaves the loop as one)
+  for (int base = v0 + tid; base < v1; base += NT * UNROLL) {
     uint4 r[UNROLL];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-      const int v = base + u * NT + lane;
-      r[u] = v < v1 ? __ldcs(body + v) : none;
-    }
+    for (int u = 0; u < UNROLL; ++u) r[u] = base + u * NT < v1 ? __ldg(body + base + u * NT) : none;
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-      float x[V];
-      Vec<T>::unpack(r[u], x);
-      const int first = sp.head + (base + u * NT + lane) * V;
-      w.add(x, [first](int e) { return (unsigned)(first + e); });
+    for (int u = 0; u < UNROLL; u += GROUP) {
+      float x[16];
+#pragma unroll
+      for (int g = 0; g < GROUP; ++g) Vec<T>::unpack(r[u + g], x + g * V);
+      w.add(x);
     }
   }
+  const float top = w.top;
+  // the logits before and behind the vectors: one a lane of the first warp
+  int at = -1;
+  float edge[1] = {-INFINITY};
   if (rank == 0 && warp == 0 && sp.head + sp.tail > 0) {
     const int t = lane - 8;  // lanes 0..7 the head, 8..15 the tail
-    const int at = lane < sp.head ? lane : t >= 0 && t < sp.tail ? sp.head + sp.nvec * V + t : -1;
-    float x[1] = {at >= 0 ? to_f32(z[at]) : -INFINITY};
-    w.add(x, [at](int) { return (unsigned)at; });
+    at = lane < sp.head ? lane : t >= 0 && t < sp.tail ? sp.head + sp.nvec * V + t : -1;
+    if (at >= 0) edge[0] = to_f32(z[at]);
+    w.add(edge);
+  }
+  {
+    Sums s{w.ref, 0.f, 0.f};
+    float b;
+    unpack2(w.S, s.S, b); s.S += b;
+    unpack2(w.U, s.U, b); s.U += b;
+    s = lanes_join(s);
+    if (lane == 0) part[warp] = s;
   }
 
-  const float S = lane_sum(w.S), U = lane_sum(w.U);
-  if (lane == 0) part[warp] = Sums{w.ref, S, U};
-  if (lane < a.top_k) keys[warp * a.top_k + lane] = w.key;
-  if (tid < a.top_k) best[tid] = 0;
-  __syncthreads();
-  Sums all = part[0];
-  for (int i = 1; i < W; ++i) all = join(all, part[i]);
   if (a.top_k) {
-    rank_keys(keys, W * a.top_k, a.top_k, best);
+    // a bound that at least top_k of the threads' maxima reach, and few more
+    const unsigned mine = ordered(top);
+    const unsigned mn = __reduce_min_sync(0xffffffffu, mine), mx = __reduce_max_sync(0xffffffffu, mine);
+    if (lane == 0) { low[warp] = mn; high[warp] = mx; }
+    const int finite = __syncthreads_count(mine >= kLowest);
+    unsigned lo = kLowest;
+    if (finite > a.top_k) {
+      unsigned hi = 0, least = 0xffffffffu;
+      for (int i = 0; i < W; ++i) { hi = max(hi, high[i]); least = min(least, low[i]); }
+      if (least > lo) lo = least;
+      // invariant: top_k maxima reach lo; fewer reach hi + 1
+      while (lo < hi) {
+        const unsigned mid = lo + (hi - lo + 1) / 2;
+        const int n = __syncthreads_count(mine >= mid);
+        if (n >= a.top_k) lo = mid; else hi = mid - 1;
+        if (n >= a.top_k && n <= a.top_k + a.top_k / 4) break;
+      }
+    }
+    const float thr = value_of(lo);
+    Best b;
+    unsigned hot = __ballot_sync(0xffffffffu, mine >= lo);
+    while (hot) {  // the lanes share the vectors of each thread whose maximum reaches the bound
+      const int t = warp * 32 + __ffs(hot) - 1;
+      hot &= hot - 1;
+      for (int v = v0 + t; v < v1; v += 32 * NT) {
+        const int u = v + lane * NT;
+        float x[V];
+        Vec<T>::unpack(u < v1 ? __ldg(body + u) : none, x);
+        const int first = sp.head + u * V;
+        b.add(x, thr, [first](int e) { return (unsigned)(first + e); });
+      }
+    }
+    if (rank == 0 && warp == 0) b.add(edge, thr, [at](int) { return (unsigned)at; });
+    const bool have = lane < a.top_k && b.key != 0;
+    const unsigned m = __ballot_sync(0xffffffffu, have);
+    int to = 0;
+    if (lane == 0 && m) to = atomicAdd(&n_keys, __popc(m));  // (their order does not matter)
+    to = __shfl_sync(0xffffffffu, to, 0);
+    if (have) keys[to + lane] = b.key;
+    if (tid < a.top_k) best[tid] = 0;
     __syncthreads();
+    rank_keys(keys, n_keys, a.top_k, best);
   }
+  __syncthreads();
+  if (warp != 0 && C == 1) return;
+  Sums all = lanes_join(lane < W ? part[lane] : Sums{-INFINITY, 0.f, 0.f});
   if (C > 1) {
     cluster.barrier_wait();
     if (tid == 0) cluster.map_shared_rank(cpart, 0)[rank] = all;
     if (tid < a.top_k) cluster.map_shared_rank(ckeys, 0)[rank * a.top_k + tid] = best[tid];
     cluster.sync();
     if (rank != 0) return;
-    all = cpart[0];
-    for (int i = 1; i < C; ++i) all = join(all, cpart[i]);
+    all = lanes_join(lane < C ? cpart[lane] : Sums{-INFINITY, 0.f, 0.f});
     if (a.top_k) {
       if (tid < a.top_k) best[tid] = 0;
       __syncthreads();
       rank_keys(ckeys, C * a.top_k, a.top_k, best);
       __syncthreads();
     }
+    if (warp != 0) return;
   }
 
   // (z - ref) - log S, not z - lse: lse is rounded to its own magnitude
   const bool bad = !(all.S == all.S) || all.ref == INFINITY, empty = !bad && all.ref == -INFINITY;
   const float nan = __int_as_float(0x7fc00000);
   const float logS = logf(all.S);
-  if (tid == 0) {
+  if (lane == 0) {
     if (a.lse) a.lse[row] = bad ? nan : empty ? -INFINITY : all.ref + logS;
     if (a.entropy) a.entropy[row] = bad ? nan : empty ? 0.f : fmaxf(logS - kLn2 * (all.U / all.S), 0.f);
   }
-  for (int i = tid; i < a.n_ids; i += NT) {
+  for (int i = lane; i < a.n_ids; i += 32) {
     const int id = a.ids[row * a.n_ids + i];
     float v = 0.f;
     if (id != VGG19_NO_CLASS) {
@@ -318,10 +368,10 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(const FwdArgs a) {
     }
     a.logprob[row * a.n_ids + i] = v;
   }
-  if (tid < a.top_k) {
-    const unsigned long long k = bad ? 0 : best[tid];
-    a.top_id[row * a.top_k + tid] = k ? (int32_t)key_index(k) : VGG19_NO_CLASS;
-    a.top_logprob[row * a.top_k + tid] = bad ? nan : k ? (key_value(k) - all.ref) - logS : -INFINITY;
+  if (lane < a.top_k) {
+    const unsigned long long k = bad ? 0 : best[lane];
+    a.top_id[row * a.top_k + lane] = k ? (int32_t)key_index(k) : VGG19_NO_CLASS;
+    a.top_logprob[row * a.top_k + lane] = bad ? nan : k ? (key_value(k) - all.ref) - logS : -INFINITY;
   }
 }
 
@@ -334,18 +384,14 @@ struct BwdArgs {
   int classes, n_ids, chunks;
 };
 
-// One block takes `chunk` vectors of one row.  The ids that fall into its chunk (usually none or one) are listed in
-// shared memory first, in their order, so that a class named twice gets both shares in the same order every time and
-// every element is rounded and written once; d_logits may be logits.
-constexpr int kBwdThreads = 256, kBwdUnroll = 8;
+// One block takes `chunk` vectors of one row.  Every warp finds the ids that fall into the chunk (usually none or one) by
+// itself, lane by lane, and hands them round with shuffles, in their order: a class named twice gets both shares in the
+// same order every time, every element is rounded and written once, no warp waits for another, and d_logits may be logits.
+constexpr int kBwdThreads = 256, kBwdUnroll = 4;
 
 template <typename T>
 __global__ void __launch_bounds__(kBwdThreads) logprobs_backward_kernel(const BwdArgs a) {
-  constexpr int V = Vec<T>::N;
-  __shared__ int hit_at[kMaxIds];
-  __shared__ float hit_g[kMaxIds];
-  __shared__ float s_sum;
-  __shared__ int s_hits;
+  constexpr int V = Vec<T>::N, IDS = kMaxIds / 32;
   const long row = blockIdx.x / a.chunks;
   const int chunk = (int)(blockIdx.x - row * a.chunks), tid = threadIdx.x, lane = tid & 31;
   const T* z = static_cast<const T*>(a.logits) + row * a.ld;
@@ -363,65 +409,98 @@ __global__ void __launch_bounds__(kBwdThreads) logprobs_backward_kernel(const Bw
   }
   // the elements this block writes: its vectors, and in the first block the head and the tail
   const int lo = sp.head + min(v0, sp.nvec) * V, hi = sp.head + min(v0 + kBwdThreads * kBwdUnroll, sp.nvec) * V;
-  if (tid < 32) {
-    float sum = 0.f;
-    int hits = 0;
-    for (int i = 0; i < a.n_ids; i += 32) {
-      const int id = i + lane < a.n_ids ? a.ids[row * a.n_ids + i + lane] : VGG19_NO_CLASS;
-      const bool in = (unsigned)id < (unsigned)a.classes;
-      if (!in && id != VGG19_NO_CLASS) atomicCAS(&g_logprobs_error, 0, (int)kDevBadLabel);
-      const float g = in ? a.d_logprob[row * a.n_ids + i + lane] : 0.f;
-      sum += lane_sum(g);
-      const bool mine = in && ((id >= lo && id < hi) || (chunk == 0 && (id < sp.head || id >= sp.head + sp.nvec * V)));
-      const unsigned m = __ballot_sync(0xffffffffu, mine);
-      if (mine) {
-        const int at = hits + __popc(m & ((1u << lane) - 1));
-        hit_at[at] = id;
-        hit_g[at] = g;
-      }
-      hits += __popc(m);
-    }
-    if (lane == 0) { s_sum = sum; s_hits = hits; }
-  }
-  __syncthreads();
-  const float lse = a.lse[row], w = a.d_entropy ? a.d_entropy[row] : 0.f;
-  const float c = s_sum + (a.d_entropy ? w * a.entropy[row] : 0.f);
-  const int hits = s_hits;
-  const bool empty = lse == -INFINITY;  // a row with no class left has no gradient
-  auto grad = [&](float x) {
-    const float lp = max_nan(x - lse, kFloor);
-    return -fast_exp2(lp * kLog2e) * fmaf(w, lp, c);
+  auto load_id = [&](int i, float& g, bool& mine) {
+    const int id = i + lane < a.n_ids ? a.ids[row * a.n_ids + i + lane] : VGG19_NO_CLASS;
+    const bool in = (unsigned)id < (unsigned)a.classes;
+    if (!in && id != VGG19_NO_CLASS) atomicCAS(&g_logprobs_error, 0, (int)kDevBadLabel);
+    g = in ? a.d_logprob[row * a.n_ids + i + lane] : 0.f;
+    mine = in && ((id >= lo && id < hi) || (chunk == 0 && (id < sp.head || id >= sp.head + sp.nvec * V)));
+    return id;
   };
+  // the first 32 ids stay in registers; which further ones are this block's, as a mask per 32
+  float g0, sum;
+  bool mine0;
+  const int id0 = load_id(0, g0, mine0);
+  const unsigned hits0 = __ballot_sync(0xffffffffu, mine0);
+  sum = lane_sum(g0);
+  unsigned more[IDS] = {};
+  bool any_more = false;
+  if (a.n_ids > 32) {
+#pragma unroll
+    for (int k = 1; k < IDS; ++k)
+      if (k * 32 < a.n_ids) {
+        float g;
+        bool mine;
+        load_id(k * 32, g, mine);
+        more[k] = __ballot_sync(0xffffffffu, mine);
+        any_more |= more[k] != 0;
+        sum += lane_sum(g);
+      }
+  }
+  const float lse = a.lse[row], w = a.d_entropy ? a.d_entropy[row] : 0.f;
+  const float c = sum + (a.d_entropy ? w * a.entropy[row] : 0.f);
+  const bool empty = lse == -INFINITY;  // a row with no class left has no gradient
+  // f(id, g) for this block's ids, in order, called by whole warps
+  auto each_hit = [&](auto f) {
+    for (unsigned m = hits0; m; m &= m - 1) {
+      const int l = __ffs(m) - 1;
+      f(__shfl_sync(0xffffffffu, id0, l), __shfl_sync(0xffffffffu, g0, l));
+    }
+    if (any_more) {
+#pragma unroll
+      for (int k = 1; k < IDS; ++k)
+        for (unsigned m = more[k]; m; m &= m - 1) {
+          const long at = row * a.n_ids + k * 32 + __ffs(m) - 1;
+          f(a.ids[at], a.d_logprob[at]);
+        }
+    }
+  };
+  const f32x2 minus = pack2(-lse, -lse), log2e = pack2(kLog2e, kLog2e), w2 = pack2(-w, -w), c2 = pack2(-c, -c);
 #pragma unroll
   for (int u = 0; u < kBwdUnroll; ++u) {
     const int v = v0 + u * kBwdThreads + tid;
-    if (v >= sp.nvec) break;
-    float x[V];
-    Vec<T>::unpack(r[u], x);
+    if (v - lane >= sp.nvec) break;  // whole warps
+    float x[V] = {};
+    if (v < sp.nvec) Vec<T>::unpack(r[u], x);
     const int first = sp.head + v * V;
 #pragma unroll
-    for (int e = 0; e < V; ++e) x[e] = empty ? 0.f : grad(x[e]);
-    for (int h = 0; h < hits; ++h) {
-      const int d = hit_at[h] - first;
-      if ((unsigned)d < (unsigned)V && !empty) {
-        const float g = hit_g[h];
+    for (int e = 0; e < V; e += 2) {
+      float p, q;
+      unpack2(add2(pack2(x[e], x[e + 1]), minus), p, q);
+      const f32x2 lp = pack2(max_nan(p, kFloor), max_nan(q, kFloor));
+      unpack2(mul2(lp, log2e), p, q);
+      unpack2(mul2(pack2(fast_exp2(p), fast_exp2(q)), fma2(w2, lp, c2)), x[e], x[e + 1]);
+    }
+    if (empty) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) x[e] += e == d ? g : 0.f;
+      for (int e = 0; e < V; ++e) x[e] = 0.f;
+    } else {
+      each_hit([&](int id, float g) {
+        const int d = id - first;
+        if ((unsigned)d < (unsigned)V) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) x[e] += e == d ? g : 0.f;
+        }
+      });
+    }
+    if (v < sp.nvec) {
+      if (same) {
+        __stcs(reinterpret_cast<uint4*>(dz + first), Vec<T>::pack(x));
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) dz[first + e] = from_f32<T>(x[e]);
       }
     }
-    if (same) {
-      __stcs(reinterpret_cast<uint4*>(dz + first), Vec<T>::pack(x));
-    } else {
-#pragma unroll
-      for (int e = 0; e < V; ++e) dz[first + e] = from_f32<T>(x[e]);
-    }
   }
-  if (chunk == 0 && tid < sp.head + sp.tail) {
-    const int at = tid < sp.head ? tid : sp.nvec * V + tid;
-    float d = empty ? 0.f : grad(to_f32(z[at]));
-    for (int h = 0; h < hits; ++h)
-      if (hit_at[h] == at && !empty) d += hit_g[h];
-    dz[at] = from_f32<T>(d);
+  if (chunk == 0 && tid < 32 && sp.head + sp.tail > 0) {  // (at most 14 of them)
+    const int at = lane < sp.head ? lane : lane < sp.head + sp.tail ? sp.nvec * V + lane : -1;
+    float d = 0.f;
+    if (at >= 0 && !empty) {
+      const float lp = max_nan(to_f32(z[at]) - lse, kFloor);
+      d = fast_exp2(lp * kLog2e) * fmaf(-w, lp, -c);
+    }
+    each_hit([&](int id, float g) { d += id == at && !empty ? g : 0.f; });
+    if (at >= 0) dz[at] = from_f32<T>(d);
   }
 }
 
@@ -448,7 +527,7 @@ template <typename T, int NT, int UNROLL> cudaError_t launch_forward(const FwdAr
 
 template <typename T> cudaError_t forward(const FwdArgs& a, long rows, cudaStream_t st) {
   const int C = cluster_size(rows, a.classes), per = a.classes / C;
-  if (per <= 2048) return launch_forward<T, 128, 2>(a, rows, C, st);
+  if (per <= 2048) return launch_forward<T, 128, 4>(a, rows, C, st);
   return launch_forward<T, 256, 4>(a, rows, C, st);
 }
 
