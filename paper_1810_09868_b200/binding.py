@@ -331,85 +331,97 @@ def _refuse(code, text):
     raise Vgg19Error(code, text)
 
 
-def _tensor(t, name, dtype, shape, device):
-    """Address of a dense tensor of that type and shape on `device` (of any device where it is None)."""
+_types = None  # (storage types of the library, float32, bfloat16, int32, current_device), once torch is there
+
+
+def _torch():
+    global _types
+    if _types is None:
+        import torch
+        _types = ({torch.float32: VGG19_FP32, torch.bfloat16: VGG19_BF16}, torch.float32, torch.bfloat16, torch.int32,
+                  torch.cuda.current_device)
+    return _types
+
+
+def _tensor(t, name, dtype, shape, dev):
+    """Address of a dense tensor of that type and shape on CUDA device `dev`; None stays None."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype != dtype:
         _refuse(VGG19_ERR_ARG, f"{name} is {t.dtype}, not {dtype}")
     if tuple(t.shape) != shape:
         _refuse(VGG19_ERR_SHAPE, f"{name} is {tuple(t.shape)}, not {shape}")
     if not t.is_contiguous():
         _refuse(VGG19_ERR_ARG, f"{name} is not contiguous")
-    if t.device != device:
-        _refuse(VGG19_ERR_ARG, f"{name} is on {t.device}, not on {device}")
-    return t.data_ptr()
+    _refuse(VGG19_ERR_ARG, f"{name} is on {t.device}, not on cuda:{dev}")
 
 
 def _rows_of(t, name):
-    """(storage type, rows, columns, row stride, device) of a 2-d tensor whose rows are dense."""
-    import torch
-    dtype = {torch.float32: VGG19_FP32, torch.bfloat16: VGG19_BF16}.get(t.dtype)
+    """(storage type, rows, columns, row stride, CUDA device index) of a 2-d tensor whose rows are dense."""
+    dtype = _torch()[0].get(t.dtype)
     if dtype is None:
         _refuse(VGG19_ERR_ARG, f"{name} is {t.dtype}, neither float32 nor bfloat16")
     if t.dim() != 2:
         _refuse(VGG19_ERR_SHAPE, f"{name} has {t.dim()} dimensions, not 2")
-    if not t.is_cuda:
+    dev = t.get_device()
+    if dev < 0:
         _refuse(VGG19_ERR_ARG, f"{name} is on {t.device}, not on a CUDA device")
     rows, cols = t.shape
+    if t.is_contiguous():
+        return dtype, rows, cols, cols, dev
     ld = t.stride(0) if rows > 1 else cols
     if (cols > 1 and t.stride(1) != 1) or ld < cols:
         _refuse(VGG19_ERR_ARG, f"{name}: strides {t.stride()}; a row has to be dense and rows must not overlap")
-    return dtype, rows, cols, ld, t.device
+    return dtype, rows, cols, ld, dev
 
 
-def _call(device, name, *args):
-    """The entry point, on the tensors' device."""
-    import torch
-    fn = getattr(load(), name)
-    if device.index == torch.cuda.current_device():
-        return _check(None, fn(*args))
-    with torch.cuda.device(device):
-        return _check(None, fn(*args))
+def _call(dev, fn, *args):
+    """fn(*args) on the tensors' device."""
+    if dev == _types[4]():
+        rc = fn(*args)
+    else:
+        import torch
+        with torch.cuda.device(dev):
+            rc = fn(*args)
+    return rc if rc == VGG19_OK else _check(None, rc)
 
 
 def vgg19_logprobs(logits, ids=None, logprob=None, lse=None, entropy=None, top_id=None, top_logprob=None, stream=None):
     """logits [rows][classes] (a row stride is allowed), ids and logprob [rows][n_ids], lse and entropy [rows], top_id and
     top_logprob [rows][top_k]; what is None is left out."""
-    import torch
     dtype, rows, classes, ld, dev = _rows_of(logits, "logits")
-    n_ids = 0 if ids is None else ids.shape[-1]
-    top_k = 0 if top_id is None else top_id.shape[-1]
+    _, f32, _, i32, _ = _types
     if (ids is None) != (logprob is None) or (top_id is None) != (top_logprob is None):
         _refuse(VGG19_ERR_ARG, "ids goes with logprob, and top_id with top_logprob")
-    f32, i32 = torch.float32, torch.int32
-    return _call(dev, "vgg19_logprobs", logits.data_ptr(), dtype, rows, classes, ld,
-                 None if ids is None else _tensor(ids, "ids", i32, (rows, n_ids), dev), n_ids, top_k,
-                 None if logprob is None else _tensor(logprob, "logprob", f32, (rows, n_ids), dev),
-                 None if lse is None else _tensor(lse, "lse", f32, (rows,), dev),
-                 None if entropy is None else _tensor(entropy, "entropy", f32, (rows,), dev),
-                 None if top_id is None else _tensor(top_id, "top_id", i32, (rows, top_k), dev),
-                 None if top_logprob is None else _tensor(top_logprob, "top_logprob", f32, (rows, top_k), dev),
-                 _stream(stream))
+    n_ids = 0 if ids is None else ids.shape[-1]
+    top_k = 0 if top_id is None else top_id.shape[-1]
+    given, top, each = (rows, n_ids), (rows, top_k), (rows,)
+    return _call(dev, (_lib or load()).vgg19_logprobs, logits.data_ptr(), dtype, rows, classes, ld, _tensor(ids, "ids", i32, given, dev),
+                 n_ids, top_k, _tensor(logprob, "logprob", f32, given, dev), _tensor(lse, "lse", f32, each, dev),
+                 _tensor(entropy, "entropy", f32, each, dev), _tensor(top_id, "top_id", i32, top, dev),
+                 _tensor(top_logprob, "top_logprob", f32, top, dev), _stream(stream))
 
 
 def vgg19_logprobs_backward(logits, ids, lse, entropy, d_logprob, d_entropy, d_logits, stream=None):
     """The gradient at the logits; ids and d_logprob may be None together, and so may d_entropy (entropy then too).
     d_logits may be logits."""
-    import torch
     dtype, rows, classes, ld, dev = _rows_of(logits, "logits")
     d_dtype, d_rows, d_classes, d_ld, d_dev = _rows_of(d_logits, "d_logits")
     if (d_dtype, d_rows, d_classes, d_dev) != (dtype, rows, classes, dev):
         _refuse(VGG19_ERR_SHAPE, "d_logits differs from logits in type, shape or device")
-    n_ids = 0 if ids is None else ids.shape[-1]
+    _, f32, _, i32, _ = _types
     if (ids is None) != (d_logprob is None):
         _refuse(VGG19_ERR_ARG, "ids goes with d_logprob")
-    f32 = torch.float32
-    return _call(dev, "vgg19_logprobs_backward", logits.data_ptr(), dtype, rows, classes, ld,
-                 None if ids is None else _tensor(ids, "ids", torch.int32, (rows, n_ids), dev), n_ids,
-                 _tensor(lse, "lse", f32, (rows,), dev),
-                 None if entropy is None else _tensor(entropy, "entropy", f32, (rows,), dev),
-                 None if d_logprob is None else _tensor(d_logprob, "d_logprob", f32, (rows, n_ids), dev),
-                 None if d_entropy is None else _tensor(d_entropy, "d_entropy", f32, (rows,), dev),
-                 d_logits.data_ptr(), d_ld, _stream(stream))
+    if lse is None:
+        _refuse(VGG19_ERR_ARG, "lse is needed")
+    n_ids = 0 if ids is None else ids.shape[-1]
+    given, each = (rows, n_ids), (rows,)
+    return _call(dev, (_lib or load()).vgg19_logprobs_backward, logits.data_ptr(), dtype, rows, classes, ld,
+                 _tensor(ids, "ids", i32, given, dev), n_ids, _tensor(lse, "lse", f32, each, dev),
+                 _tensor(entropy, "entropy", f32, each, dev), _tensor(d_logprob, "d_logprob", f32, given, dev),
+                 _tensor(d_entropy, "d_entropy", f32, each, dev), d_logits.data_ptr(), d_ld, _stream(stream))
 
 
 def vgg19_q4_code_bytes(out, in_):
@@ -421,36 +433,38 @@ def vgg19_q4_scale_bytes(out, in_, group):
 
 
 def _q4_buffers(codes, scales, out, in_, group, dev):
-    for t, name, need in ((codes, "codes", vgg19_q4_code_bytes(out, in_)), (scales, "scales", vgg19_q4_scale_bytes(out, in_, group))):
-        if t.device != dev or not t.is_contiguous():
+    lib = _lib or load()
+    for t, name, need in ((codes, "codes", lib.vgg19_q4_code_bytes(out, in_)), (scales, "scales", lib.vgg19_q4_scale_bytes(out, in_, group))):
+        if t.get_device() != dev or not t.is_contiguous():
             _refuse(VGG19_ERR_ARG, f"{name} is on {t.device}, or not contiguous")
         if t.numel() * t.element_size() < need:
             _refuse(VGG19_ERR_SHAPE, f"{name} holds {t.numel() * t.element_size()} bytes, {out} x {in_} in groups of {group} take {need}")
+    return lib
 
 
 def vgg19_q4_pack(w, group, codes, scales, stream=None):
     """w [out][in] (a row stride is allowed) into codes and scales, of vgg19_q4_code_bytes and vgg19_q4_scale_bytes."""
     dtype, out, in_, ld, dev = _rows_of(w, "w")
-    _q4_buffers(codes, scales, out, in_, group, dev)
-    return _call(dev, "vgg19_q4_pack", w.data_ptr(), dtype, out, in_, ld, group, codes.data_ptr(), scales.data_ptr(), _stream(stream))
+    lib = _q4_buffers(codes, scales, out, in_, group, dev)
+    return _call(dev, lib.vgg19_q4_pack, w.data_ptr(), dtype, out, in_, ld, group, codes.data_ptr(), scales.data_ptr(), _stream(stream))
 
 
 def vgg19_q4_linear(x, codes, scales, out, group, bias=None, relu=False, y=None, y_f32=None, stream=None):
     """x [rows][in] (a row stride is allowed); y [rows][out] in x's type and / or y_f32 in fp32."""
-    import torch
     dtype, rows, in_, ldx, dev = _rows_of(x, "x")
-    _q4_buffers(codes, scales, out, in_, group, dev)
-    return _call(dev, "vgg19_q4_linear", x.data_ptr(), dtype, rows, in_, ldx, codes.data_ptr(), scales.data_ptr(), out, group,
-                 None if bias is None else _tensor(bias, "bias", torch.float32, (out,), dev), int(relu),
-                 None if y is None else _tensor(y, "y", x.dtype, (rows, out), dev),
-                 None if y_f32 is None else _tensor(y_f32, "y_f32", torch.float32, (rows, out), dev), _stream(stream))
+    f32 = _types[1]
+    lib = _q4_buffers(codes, scales, out, in_, group, dev)
+    shape = (rows, out)
+    return _call(dev, lib.vgg19_q4_linear, x.data_ptr(), dtype, rows, in_, ldx, codes.data_ptr(), scales.data_ptr(), out, group,
+                 _tensor(bias, "bias", f32, (out,), dev), 1 if relu else 0, _tensor(y, "y", x.dtype, shape, dev),
+                 _tensor(y_f32, "y_f32", f32, shape, dev), _stream(stream))
 
 
 class MuonTensors:
     """The tensors of an update as the library takes them, holding on to the torch tensors whose addresses it has."""
 
     def __init__(self, tensors):
-        import torch
+        _, f32, b16, _, _ = _torch()
         self.tensors = [tuple(t) for t in tensors]
         self.count = len(self.tensors)
         self.array = (vgg19_muon_tensor * max(self.count, 1))()
@@ -459,10 +473,10 @@ class MuonTensors:
             dtype, rows, cols, ld, dev = _rows_of(w, "w")
             if self.device is None:
                 self.device = dev
-            a.w = _tensor(w, "w", torch.float32, (rows, cols), self.device)
-            a.w_bf16 = None if w16 is None else _tensor(w16, "w_bf16", torch.bfloat16, (rows, cols), self.device)
-            a.grad = _tensor(grad, "grad", torch.float32, (rows, cols), self.device)
-            a.momentum = _tensor(momentum, "momentum", torch.float32, (rows, cols), self.device)
+            a.w = _tensor(w, "w", f32, (rows, cols), self.device)
+            a.w_bf16 = _tensor(w16, "w_bf16", b16, (rows, cols), self.device)
+            a.grad = _tensor(grad, "grad", f32, (rows, cols), self.device)
+            a.momentum = _tensor(momentum, "momentum", f32, (rows, cols), self.device)
             a.rows, a.cols = rows, cols
 
 
@@ -478,8 +492,8 @@ def vgg19_muon_workspace_bytes(tensors):
 
 
 def _workspace(workspace, device):
-    if device is not None and workspace.device != device:
-        _refuse(VGG19_ERR_ARG, f"the workspace is on {workspace.device}, not on {device}")
+    if workspace.get_device() != device:
+        _refuse(VGG19_ERR_ARG, f"the workspace is on {workspace.device}, not on cuda:{device}")
     if not workspace.is_contiguous():
         _refuse(VGG19_ERR_ARG, "the workspace is not contiguous")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
@@ -490,7 +504,7 @@ def vgg19_muon_update(tensors, lr, momentum, decay, steps, nesterov, workspace, 
     if t.count == 0:
         return VGG19_OK
     ptr, nbytes = _workspace(workspace, t.device)
-    return _call(t.device, "vgg19_muon_update", t.array, t.count, lr, momentum, decay, steps, int(nesterov), ptr, nbytes, _stream(stream))
+    return _call(t.device, load().vgg19_muon_update, t.array, t.count, lr, momentum, decay, steps, int(nesterov), ptr, nbytes, _stream(stream))
 
 
 def vgg19_muon_step_bytes(net):

@@ -389,7 +389,7 @@ struct BwdArgs {
 // same order every time, every element is rounded and written once, no warp waits for another, and d_logits may be logits.
 constexpr int kBwdThreads = 256, kBwdUnroll = 4;
 
-template <typename T>
+template <typename T, bool MANY>  // MANY: more than 32 ids
 __global__ void __launch_bounds__(kBwdThreads) logprobs_backward_kernel(const BwdArgs a) {
   constexpr int V = Vec<T>::N, IDS = kMaxIds / 32;
   const long row = blockIdx.x / a.chunks;
@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(kBwdThreads) logprobs_backward_kernel(const Bw
   sum = lane_sum(g0);
   unsigned more[IDS] = {};
   bool any_more = false;
-  if (a.n_ids > 32) {
+  if (MANY) {
 #pragma unroll
     for (int k = 1; k < IDS; ++k)
       if (k * 32 < a.n_ids) {
@@ -446,7 +446,7 @@ __global__ void __launch_bounds__(kBwdThreads) logprobs_backward_kernel(const Bw
       const int l = __ffs(m) - 1;
       f(__shfl_sync(0xffffffffu, id0, l), __shfl_sync(0xffffffffu, g0, l));
     }
-    if (any_more) {
+    if (MANY && any_more) {
 #pragma unroll
       for (int k = 1; k < IDS; ++k)
         for (unsigned m = more[k]; m; m &= m - 1) {
@@ -532,7 +532,9 @@ template <typename T> cudaError_t forward(const FwdArgs& a, long rows, cudaStrea
 }
 
 template <typename T> cudaError_t backward(const BwdArgs& a, long rows, cudaStream_t st) {
-  logprobs_backward_kernel<T><<<(unsigned)(rows * a.chunks), kBwdThreads, 0, st>>>(a);
+  const unsigned blocks = (unsigned)(rows * a.chunks);
+  if (a.n_ids > 32) logprobs_backward_kernel<T, true><<<blocks, kBwdThreads, 0, st>>>(a);
+  else logprobs_backward_kernel<T, false><<<blocks, kBwdThreads, 0, st>>>(a);
   return cudaGetLastError();
 }
 
