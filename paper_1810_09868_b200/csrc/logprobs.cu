@@ -512,6 +512,10 @@ int cluster_size(long rows, int classes) {
 }
 
 template <typename T, int NT, int UNROLL> cudaError_t launch_forward(const FwdArgs& a, long rows, int C, cudaStream_t st) {
+  if (C == 1) {
+    logprobs_kernel<T, NT, UNROLL><<<(unsigned)rows, NT, 0, st>>>(a);
+    return cudaGetLastError();
+  }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(rows * C));
   cfg.blockDim = dim3(NT);

@@ -13,7 +13,9 @@
 // (g, t) of a warp finds with two 16-byte loads what its fragments need: row g (and g + 8), and in each of the four
 // 32-weight groups the eight weights 8 t .. 8 t + 7.  All 16 weights of one instruction's K then lie in one group.
 //
-// A block of four warps owns 16 output rows over a share of K; the shares of a cluster join in its first block
+// A block owns RW tiles of 16 output rows over a share of K, a warp one tile over all of that share or half of it.  The
+// block stages its share of x in shared memory (the larger x is, the more tiles share the staging), each warp keeps the
+// next blocks of weights on their way while it multiplies, and the shares of a cluster join
 // through distributed shared memory, in a fixed order: one launch, no scratch.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
@@ -26,10 +28,9 @@ namespace cg = cooperative_groups;
 namespace vgg {
 namespace {
 
-constexpr int kWarps = 4, kThreads = kWarps * 32, kUnroll = 4;
 constexpr int kTileRows = 16, kBlockK = 128, kBlockBytes = kTileRows * kBlockK / 2;
 constexpr int kMaxRows = 16;                 // rows of x per launch
-constexpr int kStageBytes = 48 << 10;        // of x in shared memory at a time
+constexpr int kStageBytes = 24 << 10;        // of x in shared memory at a time (with the static part below 48 KB)
 constexpr int kMaxKSplit = 8;
 
 // Two codes, four nibbles apart, become a pair of bf16 values (code - 8) / 16: 0x4100 | code is 8 + code / 16.  (Sixteenths,
@@ -91,160 +92,156 @@ template <> struct Terms<float> {
   }
 };
 
-// NT: tiles of eight rows of x.  GROUP: 32, 64 or 128 weights a scale.
-template <typename T, int GROUP, int NT>
-__global__ void __launch_bounds__(kThreads) q4_linear_kernel(const Q4Args a) {
-  constexpr int TERMS = Terms<T>::N, PER = kBlockK / GROUP, USTEP = GROUP / 32;
+// What a lane needs of one block of 16 x 128 weights: rows g and g + 8.
+template <int PER> struct Block {
+  uint4 lo, hi;
+  uint32_t s_lo[PER > 2 ? 2 : 1], s_hi[PER > 2 ? 2 : 1];
+  __device__ __forceinline__ void load(const uint4* codes, const uint16_t* scales, int b, int lane) {
+    const uint4* p = codes + (long)b * (kBlockBytes / 16) + lane;
+    lo = __ldcs(p);
+    hi = __ldcs(p + 32);
+    const uint16_t* q = scales + ((long)b * kTileRows + lane / 4) * PER;
+    if constexpr (PER == 4) {
+      const uint2 u = *reinterpret_cast<const uint2*>(q), v = *reinterpret_cast<const uint2*>(q + 8 * PER);
+      s_lo[0] = u.x; s_lo[1] = u.y; s_hi[0] = v.x; s_hi[1] = v.y;
+    } else if constexpr (PER == 2) {
+      s_lo[0] = *reinterpret_cast<const uint32_t*>(q);
+      s_hi[0] = *reinterpret_cast<const uint32_t*>(q + 8 * PER);
+    } else {
+      s_lo[0] = q[0];
+      s_hi[0] = q[8];
+    }
+  }
+  __device__ static __forceinline__ float scale(const uint32_t* s, int p) {
+    return __uint_as_float(PER > 1 && (p & 1) ? s[p >> 1] & 0xffff0000u : s[p >> 1] << 16);
+  }
+};
+
+// NT: tiles of eight rows of x.  GROUP: 32, 64 or 128 weights a scale.  RW x KW warps: row tiles, parts of the K share.
+template <typename T, int GROUP, int NT, int RW, int KW>
+__global__ void __launch_bounds__(32 * RW * KW) q4_linear_kernel(const Q4Args a) {
+  constexpr int TERMS = Terms<T>::N, PER = kBlockK / GROUP, USTEP = GROUP / 32, kThreads = 32 * RW * KW;
+  constexpr int UN = 2;  // blocks multiplied together, while as many more are on their way
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ float part[kWarps][NT * 8][kTileRows];
-  __shared__ float cluster_part[kMaxKSplit][NT * 8][kTileRows];
+  __shared__ float part[KW][RW][NT * 8][kTileRows];
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int rw = warp % RW, kw = warp / RW;
   const int ks = a.ksplit, rank = ks > 1 ? (int)cluster.block_rank() : 0;
-  if (ks > 1) cluster.barrier_arrive();  // waited for before the first write into the first block's shared memory
-  const int tile = blockIdx.x / ks;
+  const int first_tile = blockIdx.x / ks * RW, tile = min(first_tile + rw, (a.out - 1) / kTileRows);  // (a tile too many repeats the last)
   const int b0 = (int)((long)a.blocks * rank / ks), b1 = (int)((long)a.blocks * (rank + 1) / ks);
   const uint4* codes = a.codes + (long)tile * a.blocks * (kBlockBytes / 16);
   const uint16_t* scales = a.scales + (long)tile * a.blocks * kTileRows * PER;
   const int stride = a.stage_blocks * kBlockK * 2 + 64;  // bytes of a staged row: rows 64 bytes apart modulo 128
-  const long term_bytes = (long)a.rows * stride;
+  const int term_bytes = a.rows * stride;
 
   float acc[NT][4] = {};
   int xrow[NT];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) xrow[n] = min(n * 8 + g, a.rows - 1) * stride;  // columns past the last row are not used
+  for (int n = 0; n < NT; ++n) xrow[n] = min(n * 8 + g, a.rows - 1) * stride + t * 16;  // columns past the last row are not used
+
+  auto multiply = [&](const Block<PER>& w, const unsigned char* xb) {
+    const uint32_t lo[4] = {w.lo.x, w.lo.y, w.lo.z, w.lo.w}, hi[4] = {w.hi.x, w.hi.y, w.hi.z, w.hi.w};
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      float d[NT][4] = {};
+#pragma unroll
+      for (int q = 0; q < USTEP; ++q) {
+        const int v = p * USTEP + q;
+        uint32_t al[4], ah[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          al[i] = codes_to_bf16x2(lo[v] >> (4 * i));
+          ah[i] = codes_to_bf16x2(hi[v] >> (4 * i));
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int m = TERMS - 1; m >= 0; --m) {  // the small terms first
+            const uint4 xv = *reinterpret_cast<const uint4*>(xb + m * term_bytes + xrow[n] + v * 64);
+            mma(d[n], al[0], ah[0], al[1], ah[1], xv.x, xv.y);
+            mma(d[n], al[2], ah[2], al[3], ah[3], xv.z, xv.w);
+          }
+      }
+      const float s0 = Block<PER>::scale(w.s_lo, p), s1 = Block<PER>::scale(w.s_hi, p);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        acc[n][0] = fmaf(d[n][0], s0, acc[n][0]);
+        acc[n][1] = fmaf(d[n][1], s0, acc[n][1]);
+        acc[n][2] = fmaf(d[n][2], s1, acc[n][2]);
+        acc[n][3] = fmaf(d[n][3], s1, acc[n][3]);
+      }
+    }
+  };
 
   for (int c0 = b0; c0 < b1; c0 += a.stage_blocks) {
     const int c1 = min(c0 + a.stage_blocks, b1);
-    for (int base = c0; base < c1; base += kWarps * kUnroll) {
-      uint4 w[kUnroll][2];
-      uint32_t s[kUnroll][2][2];
+    const int w0 = c0 + (c1 - c0) * kw / KW, w1 = c0 + (c1 - c0) * (kw + 1) / KW;  // this warp's blocks
+    Block<PER> now[UN], next[UN];
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const int b = base + u * kWarps + warp;
-        if (b < c1) {
-          const uint4* p = codes + (long)b * (kBlockBytes / 16) + lane;
-          w[u][0] = __ldcs(p);
-          w[u][1] = __ldcs(p + 32);
-          const uint16_t* q = scales + ((long)b * kTileRows + g) * PER;
+    for (int u = 0; u < UN; ++u)
+      if (w0 + u < w1) now[u].load(codes, scales, w0 + u, lane);
+    // stage this part of x while the first weights are on their way
+    if (c0 != b0) __syncthreads();
+    const int n8 = (c1 - c0) * (kBlockK / 8);
+    for (int i = tid; i < n8 * a.rows; i += kThreads) {
+      const int row = a.rows == 1 ? 0 : i / n8, k8 = i - row * n8, k = c0 * kBlockK + k8 * 8;
+      const T* src = static_cast<const T*>(a.x) + row * a.ldx + k;
+      T v[8];
+      if (k + 8 <= a.in && (reinterpret_cast<uintptr_t>(src) & 15) == 0) {
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            if (PER == 4) {
-              const uint2 v = *reinterpret_cast<const uint2*>(q + r * 8 * PER);
-              s[u][r][0] = v.x; s[u][r][1] = v.y;
-            } else if (PER == 2) {
-              s[u][r][0] = *reinterpret_cast<const uint32_t*>(q + r * 8 * PER);
-            } else {
-              s[u][r][0] = q[r * 8 * PER];
-            }
-          }
-        }
+        for (int j = 0; j < (int)(8 * sizeof(T) / 16); ++j)
+          reinterpret_cast<uint4*>(v)[j] = __ldg(reinterpret_cast<const uint4*>(src) + j);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = k + j < a.in ? src[j] : from_f32<T>(0.f);
       }
-      if (base == c0) {
-        // stage this part of x while the first weights are on their way
-        if (c0 != b0) __syncthreads();
-        const int n8 = (c1 - c0) * (kBlockK / 8);
-        for (int i = tid; i < n8 * a.rows; i += kThreads) {
-          const int row = i / n8, k8 = i - row * n8;
-          const long k = (long)c0 * kBlockK + k8 * 8;
-          const T* src = static_cast<const T*>(a.x) + row * a.ldx + k;
-          T v[8];
-          if (k + 8 <= a.in && (reinterpret_cast<uintptr_t>(src) & 15) == 0) {
+      uint32_t o[TERMS][4];
+      Terms<T>::split(v, o);
 #pragma unroll
-            for (int j = 0; j < (int)(8 * sizeof(T) / 16); ++j)
-              reinterpret_cast<uint4*>(v)[j] = __ldg(reinterpret_cast<const uint4*>(src) + j);
-          } else {
+      for (int q = 0; q < TERMS; ++q)
+        *reinterpret_cast<uint4*>(smem + q * term_bytes + row * stride + k8 * 16) = make_uint4(o[q][0], o[q][1], o[q][2], o[q][3]);
+    }
+    __syncthreads();
+    for (int b = w0; b < w1; b += UN) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = k + j < a.in ? src[j] : from_f32<T>(0.f);
-          }
-          uint32_t o[TERMS][4];
-          Terms<T>::split(v, o);
+      for (int u = 0; u < UN; ++u)
+        if (b + UN + u < w1) next[u].load(codes, scales, b + UN + u, lane);
 #pragma unroll
-          for (int q = 0; q < TERMS; ++q)
-            *reinterpret_cast<uint4*>(smem + q * term_bytes + (long)row * stride + k8 * 16) = make_uint4(o[q][0], o[q][1], o[q][2], o[q][3]);
-        }
-        __syncthreads();
-      }
+      for (int u = 0; u < UN; ++u)
+        if (b + u < w1) multiply(now[u], smem + (b + u - c0) * (kBlockK * 2));
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const int b = base + u * kWarps + warp;
-        if (b >= c1) break;
-        const unsigned char* xb = smem + (b - c0) * (kBlockK * 2) + t * 16;
-        const uint32_t lo[4] = {w[u][0].x, w[u][0].y, w[u][0].z, w[u][0].w};
-        const uint32_t hi[4] = {w[u][1].x, w[u][1].y, w[u][1].z, w[u][1].w};
-#pragma unroll
-        for (int p = 0; p < PER; ++p) {
-          float d[NT][4] = {};
-#pragma unroll
-          for (int q = 0; q < USTEP; ++q) {
-            const int v = p * USTEP + q;
-            uint32_t al[4], ah[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              al[i] = codes_to_bf16x2(lo[v] >> (4 * i));
-              ah[i] = codes_to_bf16x2(hi[v] >> (4 * i));
-            }
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int m = TERMS - 1; m >= 0; --m) {  // the small terms first
-                const uint4 xv = *reinterpret_cast<const uint4*>(xb + m * term_bytes + xrow[n] + v * 64);
-                mma(d[n], al[0], ah[0], al[1], ah[1], xv.x, xv.y);
-                mma(d[n], al[2], ah[2], al[3], ah[3], xv.z, xv.w);
-              }
-          }
-          const uint32_t s0 = PER == 1 ? s[u][0][0] << 16 : (p & 1) ? s[u][0][p >> 1] & 0xffff0000u : s[u][0][p >> 1] << 16;
-          const uint32_t s1 = PER == 1 ? s[u][1][0] << 16 : (p & 1) ? s[u][1][p >> 1] & 0xffff0000u : s[u][1][p >> 1] << 16;
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            acc[n][0] = fmaf(d[n][0], __uint_as_float(s0), acc[n][0]);
-            acc[n][1] = fmaf(d[n][1], __uint_as_float(s0), acc[n][1]);
-            acc[n][2] = fmaf(d[n][2], __uint_as_float(s1), acc[n][2]);
-            acc[n][3] = fmaf(d[n][3], __uint_as_float(s1), acc[n][3]);
-          }
-        }
-      }
+      for (int u = 0; u < UN; ++u) now[u] = next[u];
     }
   }
 
   // accumulator: rows g, g + 8 of the tile by columns 2 t, 2 t + 1 of the rows of x
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    part[warp][n * 8 + 2 * t][g] = acc[n][0];
-    part[warp][n * 8 + 2 * t + 1][g] = acc[n][1];
-    part[warp][n * 8 + 2 * t][g + 8] = acc[n][2];
-    part[warp][n * 8 + 2 * t + 1][g + 8] = acc[n][3];
+    part[kw][rw][n * 8 + 2 * t][g] = acc[n][0];
+    part[kw][rw][n * 8 + 2 * t + 1][g] = acc[n][1];
+    part[kw][rw][n * 8 + 2 * t][g + 8] = acc[n][2];
+    part[kw][rw][n * 8 + 2 * t + 1][g + 8] = acc[n][3];
   }
-  __syncthreads();
-  if (ks > 1) cluster.barrier_wait();
-  for (int i = tid; i < NT * 8 * kTileRows; i += kThreads) {
-    const int n = i / kTileRows, o = i % kTileRows;
-    float v = 0.f;
-#pragma unroll
-    for (int k = 0; k < kWarps; ++k) v += part[k][n][o];
-    if (ks > 1) cluster.map_shared_rank(&cluster_part[0][0][0], 0)[(rank * NT * 8 + n) * kTileRows + o] = v;
-    else part[0][n][o] = v;  // (each element is read and written by one thread)
-  }
-  if (ks > 1) {
-    cluster.sync();
-    if (rank != 0) return;
-  } else {
-    __syncthreads();
-  }
-  for (int i = tid; i < a.rows * kTileRows; i += kThreads) {
-    const int n = i / kTileRows, o = i % kTileRows, col = tile * kTileRows + o;
+  if (ks > 1) cluster.sync(); else __syncthreads();
+  // every block of the cluster finishes its share of the results, reading the others' parts in their order
+  for (int i = rank * kThreads + tid; i < RW * a.rows * kTileRows; i += ks * kThreads) {
+    const int o = i % kTileRows, r = i / kTileRows % RW, n = i / kTileRows / RW;  // a row of x at a time
+    const int col = (first_tile + r) * kTileRows + o;
     if (col >= a.out) continue;
     float v = 0.f;
-    if (ks > 1)
-      for (int k = 0; k < ks; ++k) v += cluster_part[k][n][o];
-    else
-      v = part[0][n][o];
+    for (int c = 0; c < ks; ++c) {
+      const float* p = ks > 1 ? cluster.map_shared_rank(&part[0][r][n][o], c) : &part[0][r][n][o];
+#pragma unroll
+      for (int k = 0; k < KW; ++k) v += p[k * (RW * NT * 8 * kTileRows)];
+    }
     v *= 16.f;
     if (a.bias) v += a.bias[col];
     if (a.relu) v = v < 0.f ? 0.f : v;  // a NaN stays
     if (a.y) static_cast<T*>(a.y)[(long)n * a.out + col] = from_f32<T>(v);
     if (a.y_f32) a.y_f32[(long)n * a.out + col] = v;
   }
+  if (ks > 1) cluster.sync();  // no block's shared memory goes away while another reads it
 }
 
 // One warp per row and block of 128 weights, four consecutive weights per lane.
@@ -283,25 +280,34 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const T* w, long ld, int o
   if (lane % (group / 4) == 0) scales[(block * kTileRows + row % kTileRows) * (kBlockK / group) + lane / (group / 4)] = sb;
 }
 
-template <typename T, int GROUP, int NT> cudaError_t launch(Q4Args a, cudaStream_t st) {
-  const int tiles = (a.out + kTileRows - 1) / kTileRows;
-  // K is shared by as many blocks as give every SM four, while each warp still has a block of weights
-  a.ksplit = 1;
-  while (a.ksplit < kMaxKSplit && tiles * a.ksplit < 4 * 148 && a.blocks >= 2 * a.ksplit * kWarps) a.ksplit *= 2;
+template <typename T, int GROUP, int NT, int RW, int KW> cudaError_t launch(Q4Args a, cudaStream_t st) {
+  const int groups = ((a.out + kTileRows - 1) / kTileRows + RW - 1) / RW;
+  // How many blocks share K: the least (rounds of blocks over the SMs) x (weights per warp + 2, what a block costs beside
+  // them), among those that give an SM twelve warps where any does.
+  int best = 1;
+  long least = 0;
+  for (int ks = 1; ks <= kMaxKSplit && ks * KW <= a.blocks; ++ks) {
+    const long n = (long)groups * ks, per = (a.blocks + ks * KW - 1) / (ks * KW);
+    const bool full = n * RW * KW >= 12 * 148;
+    const long cost = (n + 147) / 148 * (per + 2) + (full ? 0 : (1L << 40) - n);
+    if (ks == 1 || cost < least) { best = ks; least = cost; }
+  }
+  a.ksplit = best;
   const int share = (a.blocks + a.ksplit - 1) / a.ksplit;
   int stage = kStageBytes / (a.rows * Terms<T>::N * kBlockK * 2);
   if (stage > share) stage = share;
-  else if (stage > kWarps * kUnroll) stage -= stage % (kWarps * kUnroll);
-  if (stage < 1) stage = 1;
-  a.stage_blocks = stage;
-  const size_t smem = (size_t)a.rows * Terms<T>::N * (stage * kBlockK * 2 + 64);
-  static_assert(kMaxRows * 3 * (kBlockK * 2 + 64) <= kStageBytes, "one block of x fits");
-  auto kernel = q4_linear_kernel<T, GROUP, NT>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kStageBytes + kMaxRows * 3 * 64);
-  if (e != cudaSuccess) return e;
+  a.stage_blocks = stage < 1 ? 1 : stage;
+  static_assert(kMaxRows * 3 * kBlockK * 2 <= kStageBytes, "one block of x fits");
+  static_assert(kStageBytes + kMaxRows * 3 * 64 + KW * RW * NT * 8 * kTileRows * 4 <= 48 << 10, "fits without asking for more");
+  const size_t smem = (size_t)a.rows * Terms<T>::N * (a.stage_blocks * kBlockK * 2 + 64);
+  auto kernel = q4_linear_kernel<T, GROUP, NT, RW, KW>;
+  if (a.ksplit == 1) {
+    kernel<<<(unsigned)groups, 32 * RW * KW, smem, st>>>(a);
+    return cudaGetLastError();
+  }
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(tiles * a.ksplit));
-  cfg.blockDim = dim3(kThreads);
+  cfg.gridDim = dim3((unsigned)(groups * a.ksplit));
+  cfg.blockDim = dim3(32 * RW * KW);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at{};
@@ -314,7 +320,9 @@ template <typename T, int GROUP, int NT> cudaError_t launch(Q4Args a, cudaStream
 }
 
 template <typename T, int GROUP> cudaError_t launch_group(const Q4Args& a, cudaStream_t st) {
-  return a.rows > 8 ? launch<T, GROUP, 2>(a, st) : launch<T, GROUP, 1>(a, st);
+  if (a.rows > 8) return launch<T, GROUP, 2, 8, 1>(a, st);
+  if (a.rows * Terms<T>::N > 2) return launch<T, GROUP, 1, 8, 1>(a, st);
+  return launch<T, GROUP, 1, 2, 2>(a, st);
 }
 
 template <typename T> cudaError_t launch_type(const Q4Args& a, int group, cudaStream_t st) {
