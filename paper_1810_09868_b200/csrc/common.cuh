@@ -34,8 +34,9 @@ enum DeviceError : int {
 // Sets the text vgg19_last_error(NULL) gives and returns `code`: for entry points without a handle.
 int note_error(int code, const char* fmt, ...);
 
-// Reads and clears the device-side error words of the operators without a handle (logprobs.cu, muon.cu).
+// Reads and clears the device-side error words of the operators without a handle (logprobs.cu, q4_dense.cu, muon.cu).
 cudaError_t logprobs_take_error(int* code);
+cudaError_t q4_take_error(int* code);
 cudaError_t muon_take_error(int* code);
 
 // m <- mu m + g, w <- w - lr (g + mu m or m), w16 the rounded copy (or null), for each vector (muon.cu).

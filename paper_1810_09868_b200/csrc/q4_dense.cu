@@ -13,20 +13,24 @@
 // (g, t) of a warp finds with two 16-byte loads what its fragments need: row g (and g + 8), and in each of the four
 // 32-weight groups the eight weights 8 t .. 8 t + 7.  All 16 weights of one instruction's K then lie in one group.
 //
-// A block owns RW tiles of 16 output rows over a share of K, a warp one tile over all of that share or half of it.  The
-// block stages its share of x in shared memory (the larger x is, the more tiles share the staging), each warp keeps the
-// next blocks of weights on their way while it multiplies, and the shares of a cluster join
-// through distributed shared memory, in a fixed order: one launch, no scratch.
+// A block owns RW tiles of 16 output rows over a share of K, one a warp or one for two warps that take turns.  Every warp has its own ring of bulk copies
+// (eight blocks on their way, no registers held, no other warp waited for), so that all of a block's first weights are
+// requested before anything else happens; the block's share of x is staged in shared memory meanwhile, once for all
+// its rows.  The shares of a cluster join through distributed shared memory, in a fixed order: one launch, no scratch.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
 #include "../../include/vgg19_b200.h"
-#include "common.cuh"
+#include "tc_common.cuh"
 
 namespace cg = cooperative_groups;
 
 namespace vgg {
 namespace {
+
+using namespace tc;
+
+static __device__ int g_q4_error;  // a DeviceError code once a bounded wait ran out
 
 constexpr int kTileRows = 16, kBlockK = 128, kBlockBytes = kTileRows * kBlockK / 2;
 constexpr int kMaxRows = 16;                 // rows of x per launch
@@ -35,11 +39,11 @@ constexpr int kMaxKSplit = 8;
 
 // Two codes, four nibbles apart, become a pair of bf16 values (code - 8) / 16: 0x4100 | code is 8 + code / 16.  (Sixteenths,
 // so that no product is larger than its activation; the factor comes back with the last sum.)
-__device__ __forceinline__ uint32_t codes_to_bf16x2(uint32_t w) {
+__device__ __forceinline__ uint32_t codes_to_bf16x2(uint32_t w, uint32_t mask, uint32_t magic, uint32_t offset) {
   uint32_t v;
-  asm("lop3.b32 %0, %1, 0x000f000f, 0x41004100, 0xea;" : "=r"(v) : "r"(w));  // (w & mask) | magic
-  const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), __nv_bfloat162(__float2bfloat16_rn(8.5f), __float2bfloat16_rn(8.5f)));
-  return *reinterpret_cast<const uint32_t*>(&r);
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(v) : "r"(w), "r"(mask), "r"(magic));  // (w & mask) | magic
+  asm("sub.bf16x2 %0, %0, %1;" : "+r"(v) : "r"(offset));
+  return v;
 }
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -92,67 +96,77 @@ template <> struct Terms<float> {
   }
 };
 
-// What a lane needs of one block of 16 x 128 weights: rows g and g + 8.
-template <int PER> struct Block {
-  uint4 lo, hi;
-  uint32_t s_lo[PER > 2 ? 2 : 1], s_hi[PER > 2 ? 2 : 1];
-  __device__ __forceinline__ void load(const uint4* codes, const uint16_t* scales, int b, int lane) {
-    const uint4* p = codes + (long)b * (kBlockBytes / 16) + lane;
-    lo = __ldcs(p);
-    hi = __ldcs(p + 32);
-    const uint16_t* q = scales + ((long)b * kTileRows + lane / 4) * PER;
-    if constexpr (PER == 4) {
-      const uint2 u = *reinterpret_cast<const uint2*>(q), v = *reinterpret_cast<const uint2*>(q + 8 * PER);
-      s_lo[0] = u.x; s_lo[1] = u.y; s_hi[0] = v.x; s_hi[1] = v.y;
-    } else if constexpr (PER == 2) {
-      s_lo[0] = *reinterpret_cast<const uint32_t*>(q);
-      s_hi[0] = *reinterpret_cast<const uint32_t*>(q + 8 * PER);
-    } else {
-      s_lo[0] = q[0];
-      s_hi[0] = q[8];
-    }
-  }
-  __device__ static __forceinline__ float scale(const uint32_t* s, int p) {
-    return __uint_as_float(PER > 1 && (p & 1) ? s[p >> 1] & 0xffff0000u : s[p >> 1] << 16);
-  }
-};
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
 
-// NT: tiles of eight rows of x.  GROUP: 32, 64 or 128 weights a scale.  RW x KW warps: row tiles, parts of the K share.
+constexpr int kSlotBlocks = 2, kRing = 4;  // blocks a copy, copies on their way
+template <int PER> __host__ __device__ constexpr int slot_bytes() { return kSlotBlocks * (kBlockBytes + kTileRows * PER * 2); }
+
+template <int WARPS> constexpr int kPerSm = 24 / WARPS;  // resident blocks that registers are kept for
+
+// NT: tiles of eight rows of x.  GROUP: 32, 64 or 128 weights a scale.  RW x KW warps: row tiles, warps to a tile.
 template <typename T, int GROUP, int NT, int RW, int KW>
-__global__ void __launch_bounds__(32 * RW * KW) q4_linear_kernel(const Q4Args a) {
-  constexpr int TERMS = Terms<T>::N, PER = kBlockK / GROUP, USTEP = GROUP / 32, kThreads = 32 * RW * KW;
-  constexpr int UN = 2;  // blocks multiplied together, while as many more are on their way
-  extern __shared__ __align__(16) unsigned char smem[];
+__global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 : kPerSm<RW * KW>) q4_linear_kernel(const Q4Args a) {
+  constexpr int TERMS = Terms<T>::N, PER = kBlockK / GROUP, USTEP = GROUP / 32, kThreads = 32 * RW * KW, STEP = KW * kSlotBlocks;
+  extern __shared__ __align__(128) unsigned char smem[];  // the rings, then x
   __shared__ float part[KW][RW][NT * 8][kTileRows];
+  __shared__ __align__(8) unsigned long long bars[RW * KW][kRing];
+  __shared__ int abort_flag;
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-  const int rw = warp % RW, kw = warp / RW;
   const int ks = a.ksplit, rank = ks > 1 ? (int)cluster.block_rank() : 0;
-  const int first_tile = blockIdx.x / ks * RW, tile = min(first_tile + rw, (a.out - 1) / kTileRows);  // (a tile too many repeats the last)
+  const int first_tile = blockIdx.x / ks * RW, tile = min(first_tile + warp % RW, (a.out - 1) / kTileRows);  // (a tile too many repeats the last)
   const int b0 = (int)((long)a.blocks * rank / ks), b1 = (int)((long)a.blocks * (rank + 1) / ks);
-  const uint4* codes = a.codes + (long)tile * a.blocks * (kBlockBytes / 16);
-  const uint16_t* scales = a.scales + (long)tile * a.blocks * kTileRows * PER;
+  const unsigned char* codes = reinterpret_cast<const unsigned char*>(a.codes) + (long)tile * a.blocks * kBlockBytes;
+  const unsigned char* scales = reinterpret_cast<const unsigned char*>(a.scales) + (long)tile * a.blocks * (kTileRows * PER * 2);
+  const unsigned char* ring = smem + warp * kRing * slot_bytes<PER>();
+  const uint32_t ring_u32 = smem_u32(ring), bar_u32 = smem_u32(&bars[warp][0]);
+  unsigned char* staged = smem + RW * KW * kRing * slot_bytes<PER>();
   const int stride = a.stage_blocks * kBlockK * 2 + 64;  // bytes of a staged row: rows 64 bytes apart modulo 128
   const int term_bytes = a.rows * stride;
+
+  const int first = b0 + warp / RW * kSlotBlocks;  // this warp's blocks: two, then the next two STEP further
+  auto request = [&](int slot, int b) {  // lane 0: the blocks b, b + 1 of this warp's tile
+    const int n = min(kSlotBlocks, b1 - b);
+    const uint32_t bar = bar_u32 + 8 * slot, dst = ring_u32 + slot * slot_bytes<PER>();
+    mbar_expect_tx(bar, n * (kBlockBytes + kTileRows * PER * 2));
+    bulk_copy(dst, codes + (long)b * kBlockBytes, n * kBlockBytes, bar);
+    bulk_copy(dst + kSlotBlocks * kBlockBytes, scales + (long)b * (kTileRows * PER * 2), n * (kTileRows * PER * 2), bar);
+  };
+  if (lane == 0) {
+    for (int s = 0; s < kRing; ++s) mbar_init(bar_u32 + 8 * s, 1);
+    mbar_fence_init();
+    for (int s = 0; s < kRing; ++s)
+      if (first + s * STEP < b1) request(s, first + s * STEP);
+  }
+  if (tid == 0) abort_flag = 0;
 
   float acc[NT][4] = {};
   int xrow[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) xrow[n] = min(n * 8 + g, a.rows - 1) * stride + t * 16;  // columns past the last row are not used
 
-  auto multiply = [&](const Block<PER>& w, const unsigned char* xb) {
-    const uint32_t lo[4] = {w.lo.x, w.lo.y, w.lo.z, w.lo.w}, hi[4] = {w.hi.x, w.hi.y, w.hi.z, w.hi.w};
+  // in registers, where an instruction can take all three
+  uint32_t mask = 0x000f000fu, magic = 0x41004100u, offset = 0x41084108u;
+  asm volatile("" : "+r"(mask), "+r"(magic), "+r"(offset));
+  // one block of weights in the ring by the staged x of the same K
+  auto multiply = [&](const unsigned char* wb, const unsigned char* sb, const unsigned char* xb) {
+    const uint4 l4 = *reinterpret_cast<const uint4*>(wb + lane * 16), h4 = *reinterpret_cast<const uint4*>(wb + 512 + lane * 16);
+    const uint32_t lo[4] = {l4.x, l4.y, l4.z, l4.w}, hi[4] = {h4.x, h4.y, h4.z, h4.w};
+    const uint16_t *sl = reinterpret_cast<const uint16_t*>(sb) + g * PER, *sh = sl + 8 * PER;
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
-      float d[NT][4] = {};
+      float d[NT][4] = {}, e[NT][4] = {};  // (two chains of products)
 #pragma unroll
       for (int q = 0; q < USTEP; ++q) {
         const int v = p * USTEP + q;
         uint32_t al[4], ah[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          al[i] = codes_to_bf16x2(lo[v] >> (4 * i));
-          ah[i] = codes_to_bf16x2(hi[v] >> (4 * i));
+          al[i] = codes_to_bf16x2(lo[v] >> (4 * i), mask, magic, offset);
+          ah[i] = codes_to_bf16x2(hi[v] >> (4 * i), mask, magic, offset);
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -160,28 +174,25 @@ __global__ void __launch_bounds__(32 * RW * KW) q4_linear_kernel(const Q4Args a)
           for (int m = TERMS - 1; m >= 0; --m) {  // the small terms first
             const uint4 xv = *reinterpret_cast<const uint4*>(xb + m * term_bytes + xrow[n] + v * 64);
             mma(d[n], al[0], ah[0], al[1], ah[1], xv.x, xv.y);
-            mma(d[n], al[2], ah[2], al[3], ah[3], xv.z, xv.w);
+            mma(e[n], al[2], ah[2], al[3], ah[3], xv.z, xv.w);
           }
       }
-      const float s0 = Block<PER>::scale(w.s_lo, p), s1 = Block<PER>::scale(w.s_hi, p);
+      const float s0 = __uint_as_float((uint32_t)sl[p] << 16), s1 = __uint_as_float((uint32_t)sh[p] << 16);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        acc[n][0] = fmaf(d[n][0], s0, acc[n][0]);
-        acc[n][1] = fmaf(d[n][1], s0, acc[n][1]);
-        acc[n][2] = fmaf(d[n][2], s1, acc[n][2]);
-        acc[n][3] = fmaf(d[n][3], s1, acc[n][3]);
+        acc[n][0] = fmaf(d[n][0] + e[n][0], s0, acc[n][0]);
+        acc[n][1] = fmaf(d[n][1] + e[n][1], s0, acc[n][1]);
+        acc[n][2] = fmaf(d[n][2] + e[n][2], s1, acc[n][2]);
+        acc[n][3] = fmaf(d[n][3] + e[n][3], s1, acc[n][3]);
       }
     }
   };
 
+  int slot = 0;
+  uint32_t phase = 0;
+  bool ok = true;  // of this warp; one that gave up still meets the others
   for (int c0 = b0; c0 < b1; c0 += a.stage_blocks) {
     const int c1 = min(c0 + a.stage_blocks, b1);
-    const int w0 = c0 + (c1 - c0) * kw / KW, w1 = c0 + (c1 - c0) * (kw + 1) / KW;  // this warp's blocks
-    Block<PER> now[UN], next[UN];
-#pragma unroll
-    for (int u = 0; u < UN; ++u)
-      if (w0 + u < w1) now[u].load(codes, scales, w0 + u, lane);
-    // stage this part of x while the first weights are on their way
     if (c0 != b0) __syncthreads();
     const int n8 = (c1 - c0) * (kBlockK / 8);
     for (int i = tid; i < n8 * a.rows; i += kThreads) {
@@ -200,28 +211,39 @@ __global__ void __launch_bounds__(32 * RW * KW) q4_linear_kernel(const Q4Args a)
       Terms<T>::split(v, o);
 #pragma unroll
       for (int q = 0; q < TERMS; ++q)
-        *reinterpret_cast<uint4*>(smem + q * term_bytes + row * stride + k8 * 16) = make_uint4(o[q][0], o[q][1], o[q][2], o[q][3]);
+        *reinterpret_cast<uint4*>(staged + q * term_bytes + row * stride + k8 * 16) = make_uint4(o[q][0], o[q][1], o[q][2], o[q][3]);
     }
     __syncthreads();
-    for (int b = w0; b < w1; b += UN) {
-#pragma unroll
-      for (int u = 0; u < UN; ++u)
-        if (b + UN + u < w1) next[u].load(codes, scales, b + UN + u, lane);
-#pragma unroll
-      for (int u = 0; u < UN; ++u)
-        if (b + u < w1) multiply(now[u], smem + (b + u - c0) * (kBlockK * 2));
-#pragma unroll
-      for (int u = 0; u < UN; ++u) now[u] = next[u];
+    for (int b = c0 + warp / RW * kSlotBlocks; b < c1; b += STEP) {  // (a part of x is a multiple of STEP, but for the last)
+      if (!ok) break;
+      ok = __all_sync(0xffffffffu, mbar_wait(bar_u32 + 8 * slot, phase, &abort_flag, &g_q4_error, kDevTimeoutTmaFull));
+      if (!ok) {  // let what is on its way land before shared memory goes away
+        if (lane == 0) {
+          const unsigned long long t0 = global_timer_ns();
+          for (int i = 0; i < kRing && b + i * STEP < b1; ++i) {
+            while (!mbar_try_wait(bar_u32 + 8 * slot, phase) && global_timer_ns() - t0 < 100000000ull) {}
+            if (++slot == kRing) { slot = 0; phase ^= 1; }
+          }
+        }
+        break;
+      }
+      const unsigned char* w = ring + slot * slot_bytes<PER>();
+      const unsigned char *sc = w + kSlotBlocks * kBlockBytes, *xb = staged + (b - c0) * (kBlockK * 2);
+      multiply(w, sc, xb);
+      if (b + 1 < c1) multiply(w + kBlockBytes, sc + kTileRows * PER * 2, xb + kBlockK * 2);
+      __syncwarp();
+      if (lane == 0 && b + kRing * STEP < b1) request(slot, b + kRing * STEP);
+      if (++slot == kRing) { slot = 0; phase ^= 1; }
     }
   }
 
   // accumulator: rows g, g + 8 of the tile by columns 2 t, 2 t + 1 of the rows of x
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    part[kw][rw][n * 8 + 2 * t][g] = acc[n][0];
-    part[kw][rw][n * 8 + 2 * t + 1][g] = acc[n][1];
-    part[kw][rw][n * 8 + 2 * t][g + 8] = acc[n][2];
-    part[kw][rw][n * 8 + 2 * t + 1][g + 8] = acc[n][3];
+    part[warp / RW][warp % RW][n * 8 + 2 * t][g] = acc[n][0];
+    part[warp / RW][warp % RW][n * 8 + 2 * t + 1][g] = acc[n][1];
+    part[warp / RW][warp % RW][n * 8 + 2 * t][g + 8] = acc[n][2];
+    part[warp / RW][warp % RW][n * 8 + 2 * t + 1][g + 8] = acc[n][3];
   }
   if (ks > 1) cluster.sync(); else __syncthreads();
   // every block of the cluster finishes its share of the results, reading the others' parts in their order
@@ -231,9 +253,8 @@ __global__ void __launch_bounds__(32 * RW * KW) q4_linear_kernel(const Q4Args a)
     if (col >= a.out) continue;
     float v = 0.f;
     for (int c = 0; c < ks; ++c) {
-      const float* p = ks > 1 ? cluster.map_shared_rank(&part[0][r][n][o], c) : &part[0][r][n][o];
 #pragma unroll
-      for (int k = 0; k < KW; ++k) v += p[k * (RW * NT * 8 * kTileRows)];
+      for (int k = 0; k < KW; ++k) v += ks > 1 ? *cluster.map_shared_rank(&part[k][r][n][o], c) : part[k][r][n][o];
     }
     v *= 16.f;
     if (a.bias) v += a.bias[col];
@@ -281,26 +302,36 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const T* w, long ld, int o
 }
 
 template <typename T, int GROUP, int NT, int RW, int KW> cudaError_t launch(Q4Args a, cudaStream_t st) {
-  const int groups = ((a.out + kTileRows - 1) / kTileRows + RW - 1) / RW;
-  // How many blocks share K: the least (rounds of blocks over the SMs) x (weights per warp + 2, what a block costs beside
-  // them), among those that give an SM twelve warps where any does.
+  constexpr int PER = kBlockK / GROUP, kRings = RW * KW * kRing * slot_bytes<PER>(), kStatic = RW * KW * NT * 8 * kTileRows * 4 + 512;
+  constexpr int STEP = KW * kSlotBlocks;
+  static_assert((KW == 1 ? kMaxRows * 3 : 2) * STEP * kBlockK * 2 <= kStageBytes, "a step's part of x fits");
+  const int groups = ((a.out + kTileRows - 1) / kTileRows + RW - 1) / RW, block_bytes = a.rows * Terms<T>::N * kBlockK * 2;
+  auto stage_for = [&](int share) {  // blocks of x staged at a time: whole steps
+    const int most = kStageBytes / block_bytes / STEP * STEP;
+    const int want = (share + STEP - 1) / STEP * STEP;
+    return want < most ? want : most;
+  };
+  auto smem_for = [&](int stage) { return kRings + a.rows * Terms<T>::N * (stage * kBlockK * 2 + 64); };
+  // How many blocks share K.  A block of weights keeps a warp about twenty times as long as it keeps the SM's issue slots,
+  // so an SM wants that many warps, and more only bring start-ups (three blocks' worth): the least estimated time wins.
   int best = 1;
   long least = 0;
-  for (int ks = 1; ks <= kMaxKSplit && ks * KW <= a.blocks; ++ks) {
-    const long n = (long)groups * ks, per = (a.blocks + ks * KW - 1) / (ks * KW);
-    const bool full = n * RW * KW >= 12 * 148;
-    const long cost = (n + 147) / 148 * (per + 2) + (full ? 0 : (1L << 40) - n);
+  for (int ks = 1; ks <= kMaxKSplit && ks <= a.blocks; ++ks) {
+    const long n = (long)groups * ks, share = (a.blocks + ks - 1) / ks, per = (share + KW - 1) / KW;
+    long resident = (220 << 10) / (smem_for(stage_for((int)share)) + kStatic + 1024);
+    if (resident > 24 / (RW * KW)) resident = 24 / (RW * KW);
+    const long each = (n + 147) / 148, rounds = (each + resident - 1) / resident, warps = (each < resident ? each : resident) * RW * KW;
+    const long cost = rounds * (per + 3) * (warps > 20 ? warps : 20);
     if (ks == 1 || cost < least) { best = ks; least = cost; }
   }
   a.ksplit = best;
-  const int share = (a.blocks + a.ksplit - 1) / a.ksplit;
-  int stage = kStageBytes / (a.rows * Terms<T>::N * kBlockK * 2);
-  if (stage > share) stage = share;
-  a.stage_blocks = stage < 1 ? 1 : stage;
-  static_assert(kMaxRows * 3 * kBlockK * 2 <= kStageBytes, "one block of x fits");
-  static_assert(kStageBytes + kMaxRows * 3 * 64 + KW * RW * NT * 8 * kTileRows * 4 <= 48 << 10, "fits without asking for more");
-  const size_t smem = (size_t)a.rows * Terms<T>::N * (a.stage_blocks * kBlockK * 2 + 64);
+  a.stage_blocks = stage_for((a.blocks + best - 1) / best);
+  const size_t smem = smem_for(a.stage_blocks);
   auto kernel = q4_linear_kernel<T, GROUP, NT, RW, KW>;
+  if (smem + kStatic > (48 << 10)) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRings + kStageBytes + kMaxRows * 3 * 64);
+    if (e != cudaSuccess) return e;
+  }
   if (a.ksplit == 1) {
     kernel<<<(unsigned)groups, 32 * RW * KW, smem, st>>>(a);
     return cudaGetLastError();
@@ -322,7 +353,7 @@ template <typename T, int GROUP, int NT, int RW, int KW> cudaError_t launch(Q4Ar
 template <typename T, int GROUP> cudaError_t launch_group(const Q4Args& a, cudaStream_t st) {
   if (a.rows > 8) return launch<T, GROUP, 2, 8, 1>(a, st);
   if (a.rows * Terms<T>::N > 2) return launch<T, GROUP, 1, 8, 1>(a, st);
-  return launch<T, GROUP, 1, 2, 2>(a, st);
+  return launch<T, GROUP, 1, 4, 2>(a, st);
 }
 
 template <typename T> cudaError_t launch_type(const Q4Args& a, int group, cudaStream_t st) {
@@ -372,6 +403,15 @@ cudaError_t q4_linear(const T* x, long ldx, long rows, int in, const void* codes
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
+}
+
+cudaError_t q4_take_error(int* code) {
+  cudaError_t e = cudaMemcpyFromSymbol(code, g_q4_error, sizeof(int));
+  if (e == cudaSuccess && *code) {
+    const int zero = 0;
+    e = cudaMemcpyToSymbol(g_q4_error, &zero, sizeof(int));
+  }
+  return e;
 }
 
 #define INSTANTIATE(T)                                                                                                    \
