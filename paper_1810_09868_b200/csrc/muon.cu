@@ -43,8 +43,8 @@ constexpr int kStages = 3;
 // plain fp32 (which itself sums longer there) and 8 % faster than single stages; below, single stages are what it takes.
 __device__ __forceinline__ int chain_stages(int k_stages) { return k_stages >= 32 ? 4 : 1; }
 constexpr int kThreads = 384;                    // a warpgroup for producer and issuer, two of epilogue warps
-// Registers per thread after the split: 168 at launch, 3 x 168 = 56 + 2 x 224.
-constexpr int kFewRegisters = 56, kManyRegisters = 224;
+// Registers per thread after the split: 168 at launch, 3 x 168 = 40 + 2 x 232.
+constexpr int kFewRegisters = 40, kManyRegisters = 232;
 constexpr int kPieceBytes = 4096;                // an epilogue warp's own 32 rows of 128 bytes
 constexpr int kSmemBytes = kStages * kStageBytes + 8 * kPieceBytes + 1024 + 256;
 constexpr int kMaxTensors = 20, kMaxProblems = 2 * kMaxTensors;
@@ -65,6 +65,7 @@ struct __align__(64) Problem {
   CUtensorMap a, b;
   int m, n, k_stages, tiles_m, tiles_n;
   int sym;         // tiles on and above the diagonal only, stored twice
+  int splits, per_split;  // K is cut into that many parts, of that many stages
   int b_mn;
   float alpha;
   // result as planes [2][m][ld], or ...
@@ -73,6 +74,8 @@ struct __align__(64) Problem {
   // the sums starting from c1 * (hi + lo of add1) + c2 * (hi + lo of add2), planes of the same strides, where not null;
   const half16 *add1, *add2;
   float c1, c2;
+  // ... or, with K cut, the bare sums in fp32, [splits][m][ld], for gram_finish_kernel;
+  float* partial;
   // ... or the update of w (and its bf16 copy): w <- keep * w + that, at [i][j], or at [j][i] where transposed
   float* w;
   bf16* w16;
@@ -86,16 +89,23 @@ template <int N> struct Launch {
   Problem p[N];
 };
 
-__device__ __forceinline__ void find_tile(const Problem& p, int t, int& ti, int& tj) {
+struct Tile {
+  int i, j, split, k0, k1;  // in tiles; the part of K and its stages
+};
+__device__ __forceinline__ Tile find_tile(const Problem& p, int t) {
+  Tile r{};
+  if (p.splits > 1) { r.split = t % p.splits; t /= p.splits; }
   if (p.sym) {
     int left = p.tiles_m;
-    ti = 0;
-    while (t >= left) { t -= left; --left; ++ti; }
-    tj = ti + t;
+    while (t >= left) { t -= left; --left; ++r.i; }
+    r.j = r.i + t;
   } else {
-    tj = t / p.tiles_m;  // row tiles fastest: they share the wide operand's columns
-    ti = t - tj * p.tiles_m;
+    r.j = t / p.tiles_m;  // row tiles fastest: they share the wide operand's columns
+    r.i = t - r.j * p.tiles_m;
   }
+  r.k0 = r.split * p.per_split;
+  r.k1 = min(r.k0 + p.per_split, p.k_stages);
+  return r;
 }
 
 __device__ __forceinline__ uint32_t pack_half2(float a, float b) {
@@ -119,46 +129,59 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint32_t (&hi)[4], u
 // 128-byte lines (one thread per row took 3 to 4 us per tile and matrix, eight sectors where one would do).
 __device__ __forceinline__ int piece_at(int row, int chunk) { return row * 8 + (chunk ^ (row & 7)); }
 
-// sum[c0 .. c0 + 63] += c * m, 64 columns of one plane; m points at the warp's first row and this column
-__device__ __forceinline__ void add_piece(float (&sum)[128], int c0, const half16* m, long ld, int rows, int cols, float c, uint4* piece, int lane) {
-  uint4 v[8];
+// sum (+)= c (hi + lo) of 128 columns of planes; m points at the warp's first row and column.  What this costs is the latency
+// of its requests: while the sums are still to be set (FIRST) there are registers for both planes of 64 columns at once.
+template <bool FIRST>
+__device__ __forceinline__ void add_planes(float (&sum)[128], const half16* m, long plane, int ld, int rows, int cols, float c, uint4* piece, int lane) {
+  const int r0 = lane / 8, k0 = lane % 8;
+  m += (long)r0 * ld + k0 * 8;
+  auto request = [&](uint4 (&v)[8], int h, int c0) {
+    const half16* at = m + h * plane + c0;
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    const int r = q * 4 + lane / 8, k = lane % 8;
-    v[q] = r < rows && k * 8 < cols ? *reinterpret_cast<const uint4*>(m + r * ld + k * 8) : make_uint4(0, 0, 0, 0);
-  }
+    for (int q = 0; q < 8; ++q, at += 4 * ld)
+      v[q] = q * 4 + r0 < rows && c0 + k0 * 8 < cols ? *reinterpret_cast<const uint4*>(at) : make_uint4(0, 0, 0, 0);
+  };
+  auto add = [&](const uint4 (&v)[8], int h, int c0) {
 #pragma unroll
-  for (int q = 0; q < 8; ++q) piece[piece_at(q * 4 + lane / 8, lane % 8)] = v[q];
-  __syncwarp();
+    for (int q = 0; q < 8; ++q) piece[piece_at(q * 4 + r0, k0)] = v[q];
+    __syncwarp();
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const uint4 h = piece[piece_at(lane, k)];
-    const uint32_t w[4] = {h.x, h.y, h.z, h.w};
+    for (int k = 0; k < 8; ++k) {
+      const uint4 x = piece[piece_at(lane, k)];
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float2 f = unpack_half2(w[e]);
-      sum[c0 + 8 * k + 2 * e] = fmaf(c, f.x, sum[c0 + 8 * k + 2 * e]);
-      sum[c0 + 8 * k + 2 * e + 1] = fmaf(c, f.y, sum[c0 + 8 * k + 2 * e + 1]);
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = unpack_half2(w[e]);
+        float &s0 = sum[c0 + 8 * k + 2 * e], &s1 = sum[c0 + 8 * k + 2 * e + 1];
+        s0 = fmaf(c, f.x, FIRST && h == 0 ? 0.f : s0);
+        s1 = fmaf(c, f.y, FIRST && h == 0 ? 0.f : s1);
+      }
+    }
+    __syncwarp();
+  };
+#pragma unroll
+  for (int c0 = 0; c0 < 128; c0 += 64) {
+    uint4 hi[8];
+    request(hi, 0, c0);
+    if (FIRST) {
+      uint4 lo[8];
+      request(lo, 1, c0);
+      add(hi, 0, c0);
+      add(lo, 1, c0);
+    } else {
+      add(hi, 0, c0);
+      request(hi, 1, c0);
+      add(hi, 1, c0);
     }
   }
-  __syncwarp();
 }
-__device__ __forceinline__ void add_planes(float (&sum)[128], const half16* m, long plane, long ld, int rows, int cols, float c, uint4* piece, int lane) {
-  if (!m || rows <= 0) return;
-#pragma unroll
-  for (int c0 = 0; c0 < 128; c0 += 64)
-    if (c0 < cols) {
-      add_piece(sum, c0, m + c0, ld, rows, cols - c0, c, piece, lane);
-      add_piece(sum, c0, m + plane + c0, ld, rows, cols - c0, c, piece, lane);
-    }
-}
-__device__ __forceinline__ void update(float* w, bf16* w16, long at, float keep, float v) {
-  const float x = fmaf(keep, w[at], v);
-  w[at] = x;
-  if (w16) w16[at] = __float2bfloat16_rn(x);
+__device__ __forceinline__ void put(float* w, bf16* w16, long at, float v) {
+  w[at] = v;
+  if (w16) w16[at] = __float2bfloat16_rn(v);
 }
 
-template <int N>
+// FINAL: every problem updates its w; else none does.
+template <int N, bool FINAL>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
   extern __shared__ uint8_t smem_raw[];
@@ -211,10 +234,9 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
       for (int w = pair; w < total && ok; w += n_pairs) {
         while (w >= L.first_tile[pi + 1]) ++pi;
         const Problem& p = L.p[pi];
-        int ti, tj;
-        find_tile(p, w - L.first_tile[pi], ti, tj);
-        const int row = (2 * ti + (int)rank) * BM, col = tj * BN + (int)rank * (BN / 2), k_stages = p.k_stages, mn = p.b_mn;
-        for (int kb = 0; kb < k_stages; ++kb) {
+        const Tile tile = find_tile(p, w - L.first_tile[pi]);
+        const int row = (2 * tile.i + (int)rank) * BM, col = tile.j * BN + (int)rank * (BN / 2), mn = p.b_mn;
+        for (int kb = tile.k0; kb < tile.k1; ++kb) {
           if (!mbar_wait(empty_bar(stage), phase ^ 1, &abort_flag, &g_muon_error, kDevTimeoutStageFree)) { ok = false; break; }
           const uint32_t sa = smem_base + stage * kStageBytes, sb = sa + kOperandBytes;
           const uint32_t full = map_to_cta(full_bar(stage), 0);
@@ -257,7 +279,8 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
         while (w >= L.first_tile[pi + 1]) ++pi;
         const Problem& p = L.p[pi];
         const bool mn = p.b_mn != 0;
-        const int k_stages = p.k_stages, chain = chain_stages(k_stages);
+        const Tile tile = find_tile(p, w - L.first_tile[pi]);
+        const int k_stages = tile.k1 - tile.k0, chain = chain_stages(k_stages);
         const uint32_t idesc = umma_idesc_f16(2 * BM, BN, 0, mn);
         // K-major: lo 128 rows behind hi, 16 k = 32 bytes of the swizzled row.  MN-major: two groups of 64 columns, each
         // 64 k-rows of hi then of lo; 16 k = 16 rows.
@@ -309,17 +332,19 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
     for (int w = pair; w < total && ok; w += n_pairs) {
       while (w >= L.first_tile[pi + 1]) ++pi;
       const Problem& p = L.p[pi];
-      int ti, tj;
-      find_tile(p, w - L.first_tile[pi], ti, tj);
-      const int i0 = (2 * ti + (int)rank) * BM + quarter * 32, j0 = tj * BN + group * 128;  // the warp's first row and column
+      const Tile tile = find_tile(p, w - L.first_tile[pi]);
+      const int i0 = (2 * tile.i + (int)rank) * BM + quarter * 32, j0 = tile.j * BN + group * 128;  // the warp's first row and column
       const int rows = p.m - i0, cols = p.n - j0;                                           // what there is from there on
-      const int k_stages = p.k_stages, chain = chain_stages(k_stages);
+      const int k_stages = tile.k1 - tile.k0, chain = chain_stages(k_stages);
       // the sums start from what is added to the product: its loads pass while the first chain runs
       float sum[128];
+      if (p.add1 && rows > 0 && cols > 0) {
+        add_planes<true>(sum, p.add1 + i0 * p.ld + j0, p.plane, (int)p.ld, rows, cols, p.c1, piece, lane);
+        if (!FINAL && p.add2) add_planes<false>(sum, p.add2 + i0 * p.ld + j0, p.plane, (int)p.ld, rows, cols, p.c2, piece, lane);
+      } else {
 #pragma unroll
-      for (int j = 0; j < 128; ++j) sum[j] = 0.f;
-      add_planes(sum, p.add1 ? p.add1 + i0 * p.ld + j0 : nullptr, p.plane, p.ld, rows, cols, p.c1, piece, lane);
-      add_planes(sum, p.add2 ? p.add2 + i0 * p.ld + j0 : nullptr, p.plane, p.ld, rows, cols, p.c2, piece, lane);
+        for (int j = 0; j < 128; ++j) sum[j] = 0.f;
+      }
       for (int kb0 = 0; kb0 < k_stages; kb0 += chain, ++chunk) {
         const int buf = chunk & 1;
         if (!__all_sync(0xffffffffu, mbar_wait(acc_full_bar(buf), (chunk >> 1) & 1, &abort_flag, &g_muon_error, kDevTimeoutAccum))) { ok = false; break; }
@@ -342,49 +367,72 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
       if (rows <= 0 || cols <= 0) continue;
       const float alpha = p.alpha;
       const long ld = p.ld;
-      if (!p.w) {
+      const int r0 = lane / 8, k0 = lane % 8;  // what this lane moves between memory and a piece: rows r0, r0 + 4, ..., chunk k0
+      if (!FINAL && p.partial) {
+        float* out = p.partial + ((long)tile.split * p.m + i0) * ld + j0;
+#pragma unroll
+        for (int c0 = 0; c0 < 128; c0 += 32) {
+          if (c0 >= cols) break;
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            piece[piece_at(lane, k)] = make_uint4(__float_as_uint(sum[c0 + 4 * k]), __float_as_uint(sum[c0 + 4 * k + 1]),
+                                                  __float_as_uint(sum[c0 + 4 * k + 2]), __float_as_uint(sum[c0 + 4 * k + 3]));
+          __syncwarp();
+#pragma unroll
+          for (int q = 0; q < 8; ++q)  // (a row has room for whole eights)
+            if (q * 4 + r0 < rows && c0 + k0 * 4 < cols)
+              *reinterpret_cast<uint4*>(out + (q * 4 + r0) * ld + c0 + k0 * 4) = piece[piece_at(q * 4 + r0, k0)];
+          __syncwarp();
+        }
+      } else if (!FINAL) {
         half16* out = p.out + i0 * ld + j0;
 #pragma unroll
         for (int c0 = 0; c0 < 128; c0 += 64) {
           if (c0 >= cols) break;
+          uint32_t hi[8][4], lo[8][4];
 #pragma unroll
-          for (int plane = 0; plane < 2; ++plane) {
+          for (int k = 0; k < 8; ++k) {
+            float v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              float v[8];
+            for (int e = 0; e < 8; ++e) v[e] = alpha * sum[c0 + 8 * k + e];
+            split8(v, hi[k], lo[k]);
+          }
+          if (p.sym && tile.i != tile.j && lane < rows) {  // the mirror image, lanes along a row
+            half16* at = p.out + (j0 + c0) * ld + i0 + lane;
 #pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] = alpha * sum[c0 + 8 * k + e];
-              uint32_t hi[4], lo[4];
-              split8(v, hi, lo);
-              piece[piece_at(lane, k)] = plane ? make_uint4(lo[0], lo[1], lo[2], lo[3]) : make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            }
+            for (int j = 0; j < 64; ++j)
+              if (c0 + j < cols) {
+                at[j * ld] = (half16)(hi[j / 8][j % 8 / 2] >> (16 * (j & 1)));
+                at[p.plane + j * ld] = (half16)(lo[j / 8][j % 8 / 2] >> (16 * (j & 1)));
+              }
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              piece[piece_at(lane, k)] = h ? make_uint4(lo[k][0], lo[k][1], lo[k][2], lo[k][3]) : make_uint4(hi[k][0], hi[k][1], hi[k][2], hi[k][3]);
             __syncwarp();
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {  // (a row of planes has room for whole eights)
-              const int r = q * 4 + lane / 8, k = lane % 8;
-              if (r < rows && c0 + k * 8 < cols)
-                *reinterpret_cast<uint4*>(out + plane * p.plane + r * ld + c0 + k * 8) = piece[piece_at(r, k)];
-            }
+            for (int q = 0; q < 8; ++q)
+              if (q * 4 + r0 < rows && c0 + k0 * 8 < cols)
+                *reinterpret_cast<uint4*>(out + h * p.plane + (q * 4 + r0) * ld + c0 + k0 * 8) = piece[piece_at(q * 4 + r0, k0)];
             __syncwarp();
           }
         }
-        if (p.sym && ti != tj && lane < rows) {  // the mirror image, lanes along a row
-          half16* at = p.out + j0 * ld + i0 + lane;
-#pragma unroll
-          for (int j = 0; j < 128; ++j)
-            if (j < cols) {
-              const float v = alpha * sum[j];
-              const __half h = __float2half_rn(v), l = __float2half_rn(v - __half2float(h));
-              at[j * ld] = __half_as_ushort(h);
-              at[p.plane + j * ld] = __half_as_ushort(l);
-            }
-        }
       } else if (p.transposed) {  // lanes along a row of w
         if (lane < rows) {
-          const long at = j0 * p.w_ld + i0 + lane;
+          const long at = j0 * p.w_ld + i0 + lane, w_ld = p.w_ld;
+          const float keep = p.keep;
 #pragma unroll
-          for (int j = 0; j < 128; ++j)
-            if (j < cols) update(p.w, p.w16, at + j * p.w_ld, p.keep, alpha * sum[j]);
+          for (int c0 = 0; c0 < 128; c0 += 16) {
+            float old[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (c0 + j < cols) old[j] = p.w[at + (c0 + j) * w_ld];
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (c0 + j < cols) put(p.w, p.w16, at + (c0 + j) * w_ld, fmaf(keep, old[j], alpha * sum[c0 + j]));
+          }
         }
       } else {
         const float keep = p.keep;
@@ -394,43 +442,51 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
 #pragma unroll
         for (int c0 = 0; c0 < 128; c0 += 32) {
           if (c0 >= cols) break;
-          const int r0 = lane / 8, k0 = lane % 8;
-          const bool vec = p.w_vec && c0 + k0 * 4 < cols;
-          float4 old[8];
-          if (vec) {
+          {
+            float4 old[8];
+            if (p.w_vec) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q)
-              if (q * 4 + r0 < rows) old[q] = *reinterpret_cast<const float4*>(w + (q * 4 + r0) * w_ld + c0 + k0 * 4);
-          }
+              for (int q = 0; q < 8; ++q)
+                if (q * 4 + r0 < rows && c0 + k0 * 4 < cols) old[q] = *reinterpret_cast<const float4*>(w + (q * 4 + r0) * w_ld + c0 + k0 * 4);
+            }
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-            piece[piece_at(lane, k)] = make_uint4(__float_as_uint(alpha * sum[c0 + 4 * k]), __float_as_uint(alpha * sum[c0 + 4 * k + 1]),
-                                                  __float_as_uint(alpha * sum[c0 + 4 * k + 2]), __float_as_uint(alpha * sum[c0 + 4 * k + 3]));
-          __syncwarp();
-          if (vec) {
+            for (int k = 0; k < 8; ++k)
+              piece[piece_at(lane, k)] = make_uint4(__float_as_uint(alpha * sum[c0 + 4 * k]), __float_as_uint(alpha * sum[c0 + 4 * k + 1]),
+                                                    __float_as_uint(alpha * sum[c0 + 4 * k + 2]), __float_as_uint(alpha * sum[c0 + 4 * k + 3]));
+            __syncwarp();
+            if (p.w_vec) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-              const int r = q * 4 + r0;
-              if (r >= rows) break;
-              const uint4 d = piece[piece_at(r, k0)];
-              float4 v;
-              v.x = fmaf(keep, old[q].x, __uint_as_float(d.x));
-              v.y = fmaf(keep, old[q].y, __uint_as_float(d.y));
-              v.z = fmaf(keep, old[q].z, __uint_as_float(d.z));
-              v.w = fmaf(keep, old[q].w, __uint_as_float(d.w));
-              *reinterpret_cast<float4*>(w + r * w_ld + c0 + k0 * 4) = v;
-              if (w16) {
-                const __nv_bfloat162 b[2] = {__floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w)};
-                *reinterpret_cast<uint2*>(w16 + r * w_ld + c0 + k0 * 4) = *reinterpret_cast<const uint2*>(b);
+              for (int q = 0; q < 8; ++q) {
+                const int r = q * 4 + r0;
+                if (r >= rows || c0 + k0 * 4 >= cols) break;
+                const uint4 d = piece[piece_at(r, k0)];
+                float4 v;
+                v.x = fmaf(keep, old[q].x, __uint_as_float(d.x));
+                v.y = fmaf(keep, old[q].y, __uint_as_float(d.y));
+                v.z = fmaf(keep, old[q].z, __uint_as_float(d.z));
+                v.w = fmaf(keep, old[q].w, __uint_as_float(d.w));
+                *reinterpret_cast<float4*>(w + r * w_ld + c0 + k0 * 4) = v;
+                if (w16) {
+                  const __nv_bfloat162 b[2] = {__floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w)};
+                  *reinterpret_cast<uint2*>(w16 + r * w_ld + c0 + k0 * 4) = *reinterpret_cast<const uint2*>(b);
+                }
+              }
+            } else if (c0 + lane < cols) {
+#pragma unroll 1
+              for (int q = 0; q < 32; q += 8) {
+                float one[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                  if (q + r < rows) one[r] = w[(q + r) * w_ld + c0 + lane];
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                  if (q + r < rows)
+                    put(w, w16, (q + r) * w_ld + c0 + lane,
+                        fmaf(keep, one[r], reinterpret_cast<const float*>(piece + piece_at(q + r, lane / 4))[lane % 4]));
               }
             }
-          } else if (!p.w_vec && c0 + lane < cols) {
-#pragma unroll 4
-            for (int r = 0; r < 32; ++r)
-              if (r < rows)
-                update(w, w16, r * w_ld + c0 + lane, keep, reinterpret_cast<const float*>(piece + piece_at(r, lane / 4))[lane % 4]);
+            __syncwarp();
           }
-          __syncwarp();
         }
       }
     }
@@ -445,6 +501,52 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
     __syncwarp();
     tc_fence_after();
     tmem_dealloc_pair(tmem_base, 512);
+  }
+}
+
+// ---- a Gram matrix from the parts of its sums -----------------------------------------------------------------
+// 32 x 32 elements on and above the diagonal per block: the parts added in their order, split, stored, and stored mirrored.
+struct GramFinish {
+  int count;
+  float alpha;
+  struct {
+    const float* partial;
+    half16* out;
+    long plane, ld;
+    int m, splits, first_block;
+  } t[kMaxTensors];
+};
+__global__ void __launch_bounds__(256) gram_finish_kernel(const __grid_constant__ GramFinish a) {
+  int k = 0;
+  while (k + 1 < a.count && (int)blockIdx.x >= a.t[k + 1].first_block) ++k;
+  const auto& t = a.t[k];
+  int left = (t.m + 31) / 32, bi = 0, bj = blockIdx.x - t.first_block;
+  while (bj >= left) { bj -= left; --left; ++bi; }
+  bj += bi;
+  __shared__ float tile[32][33];
+  const int x = threadIdx.x % 32, y = threadIdx.x / 32;
+  const long ld = t.ld, part = (long)t.m * ld;
+  auto store = [&](int i, int j, float v) {
+    const __half h = __float2half_rn(v), l = __float2half_rn(v - __half2float(h));
+    t.out[i * ld + j] = __half_as_ushort(h);
+    t.out[t.plane + i * ld + j] = __half_as_ushort(l);
+  };
+#pragma unroll
+  for (int r = y; r < 32; r += 8) {
+    const int i = bi * 32 + r, j = bj * 32 + x;
+    if (i >= t.m || j >= t.m) continue;
+    float s = 0.f;
+    for (int p = 0; p < t.splits; ++p) s += t.partial[p * part + i * ld + j];
+    s *= a.alpha;
+    tile[r][x] = s;
+    store(i, j, s);
+  }
+  if (bi == bj) return;
+  __syncthreads();
+#pragma unroll
+  for (int r = y; r < 32; r += 8) {
+    const int i = bj * 32 + r, j = bi * 32 + x;
+    if (i < t.m && j < t.m) store(i, j, tile[x][r]);
   }
 }
 
@@ -766,6 +868,14 @@ struct Shape {
         transposed(t.rows > t.cols) {}
   size_t x_bytes() const { return up((size_t)2 * m * ldn * 2, 256); }
   size_t a_bytes() const { return up((size_t)2 * m * ldm * 2, 256); }
+  // A Gram matrix of at most 1024 rows has few tiles and may have a long K, which is then cut into parts of about 16 stages
+  // (one 512 x 4608 filter's takes 85 us uncut).  By the tensor alone, so that no result depends on what else is updated.
+  int gram_stages() const { return (int)((n + BK - 1) / BK); }
+  int gram_splits() const {
+    const int parts = (gram_stages() + 15) / 16;
+    return m > 1024 || parts < 2 ? 1 : parts < 8 ? parts : 8;
+  }
+  size_t partial_bytes() const { return gram_splits() > 1 ? up((size_t)gram_splits() * m * ldm * 4, 256) : 0; }
   long norm_blocks() const { return (m * n + kNormChunk - 1) / kNormChunk; }
   long split_blocks() const {
     return transposed ? ((n + 31) / 32) * ((m + 31) / 32) : (m * (ldn / 8) + kSplitThreads - 1) / kSplitThreads;
@@ -777,6 +887,7 @@ enum Matrix { kX0, kX1, kGramA, kPoly, kQa, kQb, kPA, kMatrices };
 // The planes of one tensor in the workspace and their tensor maps.
 struct Planes {
   half16* at[kMatrices];
+  float* partial;
   CUtensorMap k_major[kMatrices], mn_major[2];
 };
 
@@ -792,7 +903,7 @@ bool plane_map(CUtensorMap* map, const half16* base, long rows, long cols, long 
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-size_t tensor_bytes(const Shape& s) { return 2 * s.x_bytes() + 5 * s.a_bytes(); }
+size_t tensor_bytes(const Shape& s) { return 2 * s.x_bytes() + 5 * s.a_bytes() + s.partial_bytes(); }
 
 size_t batch_bytes(const vgg19_muon_tensor* t, int count) {
   size_t b = up(kMaxTensors * sizeof(double), 256);
@@ -805,17 +916,18 @@ size_t batch_bytes(const vgg19_muon_tensor* t, int count) {
   return b + up(blocks * sizeof(double), 256);
 }
 
-template <int N> cudaError_t launch_products(Launch<N>& L, cudaStream_t st) {
+template <bool FINAL, int N> cudaError_t launch_products(Launch<N>& L, cudaStream_t st) {
   int tiles = 0;
   for (int i = 0; i < L.count; ++i) {
     Problem& p = L.p[i];
     p.tiles_m = (p.m + 2 * BM - 1) / (2 * BM);
     p.tiles_n = (p.n + BN - 1) / BN;
+    if (p.splits < 1) { p.splits = 1; p.per_split = p.k_stages; }
     L.first_tile[i] = tiles;
-    tiles += p.sym ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
+    tiles += p.splits * (p.sym ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n);
   }
   L.first_tile[L.count] = tiles;
-  cudaError_t e = cudaFuncSetAttribute(split_product_pair_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  cudaError_t e = cudaFuncSetAttribute(split_product_pair_kernel<N, FINAL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   if (e != cudaSuccess) return e;
   int dev = 0, sms = 148;
   cudaGetDevice(&dev);
@@ -831,7 +943,7 @@ template <int N> cudaError_t launch_products(Launch<N>& L, cudaStream_t st) {
   at.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, split_product_pair_kernel<N>, L);
+  return cudaLaunchKernelEx(&cfg, split_product_pair_kernel<N, FINAL>, L);
 }
 
 cudaError_t launch_small(const SmallLaunch& L, int count, cudaStream_t st) {
@@ -875,6 +987,8 @@ cudaError_t update_batch(const vgg19_muon_tensor* tensors, const int count, cons
       if (!plane_map(&q.k_major[k], q.at[k], s.m, x ? s.n : s.m, x ? s.ldn : s.ldm, 128)) return cudaErrorInvalidValue;
       if (x && !plane_map(&q.mn_major[k], q.at[k], s.m, s.n, s.ldn, 64)) return cudaErrorInvalidValue;
     }
+    q.partial = reinterpret_cast<float*>(ws);
+    ws += s.partial_bytes();
     Element& e = el.t[i];
     e.grad = t.grad; e.momentum = t.momentum; e.x = q.at[kX0];
     e.rows = t.rows; e.cols = t.cols; e.ld = s.ldn; e.plane = s.m * s.ldn;
@@ -901,12 +1015,12 @@ cudaError_t update_batch(const vgg19_muon_tensor* tensors, const int count, cons
     p.a = planes[i].k_major[a]; p.b = planes[i].k_major[b];
     p.m = p.n = (int)s.m;
     p.k_stages = (int)((s.m + BK - 1) / BK);
-    p.sym = 1;
+    p.sym = s.m > 512;  // (up to 2 x 2 tiles, a tile more costs less than storing one twice)
     p.alpha = sd / (sa * sb);
     p.out = planes[i].at[d]; p.ld = s.ldm; p.plane = s.m * s.ldm;
     return p;
   };
-  auto run = [&] { if (err == cudaSuccess) err = launch_products(L, st); L.count = 0; };
+  auto run = [&] { if (err == cudaSuccess) err = L.p[0].w ? launch_products<true>(L, st) : launch_products<false>(L, st); L.count = 0; };
   bool small = true;
   for (int i = 0; i < count; ++i) small = small && Shape(tensors[i]).m <= kSmall;
   L.count = 0;
@@ -914,11 +1028,30 @@ cudaError_t update_batch(const vgg19_muon_tensor* tensors, const int count, cons
   for (int done = 0; done < o.steps;) {
     // groups of at most three steps, as even as they go
     const int groups = (o.steps - done + kStepsPerGram - 1) / kStepsPerGram, group = (o.steps - done + groups - 1) / groups;
+    GramFinish finish{};
+    int finish_blocks = 0;
     for (int i = 0; i < count; ++i) {
       Problem& p = symmetric(i, (Matrix)x, kScaleX, (Matrix)x, kScaleX, kGramA, kScaleA);
-      p.k_stages = (int)((Shape(tensors[i]).n + BK - 1) / BK);
+      const Shape s(tensors[i]);
+      p.k_stages = s.gram_stages();
+      if (s.gram_splits() > 1) {
+        p.splits = s.gram_splits();
+        p.per_split = (p.k_stages + p.splits - 1) / p.splits;
+        p.partial = planes[i].partial;
+        auto& t = finish.t[finish.count++];
+        t.partial = p.partial; t.out = p.out; t.plane = p.plane; t.ld = p.ld;
+        t.m = p.m; t.splits = p.splits; t.first_block = finish_blocks;
+        finish.alpha = p.alpha;
+        p.sym = 1;
+        const int b = (p.m + 31) / 32;
+        finish_blocks += b * (b + 1) / 2;
+      }
     }
     run();
+    if (finish.count && err == cudaSuccess) {
+      gram_finish_kernel<<<(unsigned)finish_blocks, 256, 0, st>>>(finish);
+      err = cudaGetLastError();
+    }
     // p(A) = a I + R with R = b A + c A A; Q = q0 I + S.  The identity's share is added in the epilogues, in fp32: what
     // the tensor core truncates is then relative to the smaller rest.
     Matrix q = kQa;  // S
