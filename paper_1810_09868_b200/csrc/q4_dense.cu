@@ -14,9 +14,8 @@
 // 32-weight groups the eight weights 8 t .. 8 t + 7.  All 16 weights of one instruction's K then lie in one group.
 //
 // A block owns RW tiles of 16 output rows over a share of K, one a warp or one for two warps that take turns.  Every warp has its own ring of bulk copies
-// (eight blocks on their way, no registers held, no other warp waited for), so that all of a block's first weights are
-// requested before anything else happens; the block's share of x is staged in shared memory meanwhile, once for all
-// its rows.  The shares of a cluster join through distributed shared memory, in a fixed order: one launch, no scratch.
+// (eight blocks on their way, no registers held, no other warp waited for); the block's share of x is staged in
+// shared memory meanwhile, once for all its rows.  The shares of a cluster join through distributed shared memory, in a fixed order: one launch, no scratch.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
@@ -34,7 +33,7 @@ static __device__ int g_q4_error;  // a DeviceError code once a bounded wait ran
 
 constexpr int kTileRows = 16, kBlockK = 128, kBlockBytes = kTileRows * kBlockK / 2;
 constexpr int kMaxRows = 16;                 // rows of x per launch
-constexpr int kStageBytes = 24 << 10;        // of x in shared memory at a time (with the static part below 48 KB)
+constexpr int kStageBytes = 48 << 10;        // of x in shared memory at a time (with the static part below 48 KB)
 constexpr int kMaxKSplit = 8;
 
 // Two codes, four nibbles apart, become a pair of bf16 values (code - 8) / 16: 0x4100 | code is 8 + code / 16.  (Sixteenths,
@@ -101,7 +100,14 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
-constexpr int kSlotBlocks = 2, kRing = 4;  // blocks a copy, copies on their way
+// (volatile: stays where it is in the order of requests)
+__device__ __forceinline__ uint4 load_now(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+
+constexpr int kSlotBlocks = 4, kRing = 2;  // blocks a copy, copies on their way
 template <int PER> __host__ __device__ constexpr int slot_bytes() { return kSlotBlocks * (kBlockBytes + kTileRows * PER * 2); }
 
 template <int WARPS> constexpr int kPerSm = 24 / WARPS;  // resident blocks that registers are kept for
@@ -112,6 +118,7 @@ __global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 
   constexpr int TERMS = Terms<T>::N, PER = kBlockK / GROUP, USTEP = GROUP / 32, kThreads = 32 * RW * KW, STEP = KW * kSlotBlocks;
   extern __shared__ __align__(128) unsigned char smem[];  // the rings, then x
   __shared__ float part[KW][RW][NT * 8][kTileRows];
+  __shared__ float inbox[RW * NT * 8 * kTileRows + kMaxKSplit];
   __shared__ __align__(8) unsigned long long bars[RW * KW][kRing];
   __shared__ int abort_flag;
   cg::cluster_group cluster = cg::this_cluster();
@@ -127,20 +134,15 @@ __global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 
   const int stride = a.stage_blocks * kBlockK * 2 + 64;  // bytes of a staged row: rows 64 bytes apart modulo 128
   const int term_bytes = a.rows * stride;
 
-  const int first = b0 + warp / RW * kSlotBlocks;  // this warp's blocks: two, then the next two STEP further
-  auto request = [&](int slot, int b) {  // lane 0: the blocks b, b + 1 of this warp's tile
+  const int first = b0 + warp / RW * kSlotBlocks;  // this warp's blocks: a slot's, then those STEP further
+  auto request = [&](int slot, int b) {  // lane 0: a slot's blocks of this warp's tile, from b
     const int n = min(kSlotBlocks, b1 - b);
     const uint32_t bar = bar_u32 + 8 * slot, dst = ring_u32 + slot * slot_bytes<PER>();
     mbar_expect_tx(bar, n * (kBlockBytes + kTileRows * PER * 2));
     bulk_copy(dst, codes + (long)b * kBlockBytes, n * kBlockBytes, bar);
     bulk_copy(dst + kSlotBlocks * kBlockBytes, scales + (long)b * (kTileRows * PER * 2), n * (kTileRows * PER * 2), bar);
   };
-  if (lane == 0) {
-    for (int s = 0; s < kRing; ++s) mbar_init(bar_u32 + 8 * s, 1);
-    mbar_fence_init();
-    for (int s = 0; s < kRing; ++s)
-      if (first + s * STEP < b1) request(s, first + s * STEP);
-  }
+  if (ks > 1) cluster.barrier_arrive();  // waited for before the first write into another block's shared memory
   if (tid == 0) abort_flag = 0;
 
   float acc[NT][4] = {};
@@ -194,24 +196,45 @@ __global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 
   for (int c0 = b0; c0 < b1; c0 += a.stage_blocks) {
     const int c1 = min(c0 + a.stage_blocks, b1);
     if (c0 != b0) __syncthreads();
-    const int n8 = (c1 - c0) * (kBlockK / 8);
-    for (int i = tid; i < n8 * a.rows; i += kThreads) {
-      const int row = a.rows == 1 ? 0 : i / n8, k8 = i - row * n8, k = c0 * kBlockK + k8 * 8;
-      const T* src = static_cast<const T*>(a.x) + row * a.ldx + k;
-      T v[8];
-      if (k + 8 <= a.in && (reinterpret_cast<uintptr_t>(src) & 15) == 0) {
+    const int items = (c1 - c0) * (kBlockK / 8) * a.rows, n8 = (c1 - c0) * (kBlockK / 8);
+    constexpr int BATCH = TERMS == 1 ? 4 : 2;  // rounds of requests before the first is used
+    for (int i0 = tid; i0 < items || (c0 == b0 && i0 == tid); i0 += BATCH * kThreads) {
+      T v[BATCH][8];
 #pragma unroll
-        for (int j = 0; j < (int)(8 * sizeof(T) / 16); ++j)
-          reinterpret_cast<uint4*>(v)[j] = __ldg(reinterpret_cast<const uint4*>(src) + j);
-      } else {
+      for (int u = 0; u < BATCH; ++u) {
+        const int i = i0 + u * kThreads;
+        if (i < items) {
+          const int row = a.rows == 1 ? 0 : i / n8, k = c0 * kBlockK + (i - row * n8) * 8;
+          const T* src = static_cast<const T*>(a.x) + row * a.ldx + k;
+          if (k + 8 <= a.in && (reinterpret_cast<uintptr_t>(src) & 15) == 0) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = k + j < a.in ? src[j] : from_f32<T>(0.f);
+            for (int j = 0; j < (int)(8 * sizeof(T) / 16); ++j) reinterpret_cast<uint4*>(v[u])[j] = load_now(reinterpret_cast<const uint4*>(src) + j);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[u][j] = k + j < a.in ? src[j] : from_f32<T>(0.f);
+          }
+        }
       }
-      uint32_t o[TERMS][4];
-      Terms<T>::split(v, o);
+      // The weights are asked for behind the first of x, not before: x is little and everything waits for it (asked for
+      // after them it came 2.5 us later).
+      if (c0 == b0 && i0 == tid && lane == 0) {
+        for (int s = 0; s < kRing; ++s) mbar_init(bar_u32 + 8 * s, 1);
+        mbar_fence_init();
+        for (int s = 0; s < kRing; ++s)
+          if (first + s * STEP < b1) request(s, first + s * STEP);
+      }
 #pragma unroll
-      for (int q = 0; q < TERMS; ++q)
-        *reinterpret_cast<uint4*>(staged + q * term_bytes + row * stride + k8 * 16) = make_uint4(o[q][0], o[q][1], o[q][2], o[q][3]);
+      for (int u = 0; u < BATCH; ++u) {
+        const int i = i0 + u * kThreads;
+        if (i < items) {
+          const int row = a.rows == 1 ? 0 : i / n8, k8 = i - row * n8;
+          uint32_t o[TERMS][4];
+          Terms<T>::split(v[u], o);
+#pragma unroll
+          for (int q = 0; q < TERMS; ++q)
+            *reinterpret_cast<uint4*>(staged + q * term_bytes + row * stride + k8 * 16) = make_uint4(o[q][0], o[q][1], o[q][2], o[q][3]);
+        }
+      }
     }
     __syncthreads();
     for (int b = c0 + warp / RW * kSlotBlocks; b < c1; b += STEP) {  // (a part of x is a multiple of STEP, but for the last)
@@ -229,8 +252,9 @@ __global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 
       }
       const unsigned char* w = ring + slot * slot_bytes<PER>();
       const unsigned char *sc = w + kSlotBlocks * kBlockBytes, *xb = staged + (b - c0) * (kBlockK * 2);
-      multiply(w, sc, xb);
-      if (b + 1 < c1) multiply(w + kBlockBytes, sc + kTileRows * PER * 2, xb + kBlockK * 2);
+#pragma unroll
+      for (int u = 0; u < kSlotBlocks; ++u)
+        if (b + u < c1) multiply(w + u * kBlockBytes, sc + u * (kTileRows * PER * 2), xb + u * (kBlockK * 2));
       __syncwarp();
       if (lane == 0 && b + kRing * STEP < b1) request(slot, b + kRing * STEP);
       if (++slot == kRing) { slot = 0; phase ^= 1; }
@@ -245,24 +269,36 @@ __global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 
     part[warp / RW][warp % RW][n * 8 + 2 * t][g + 8] = acc[n][2];
     part[warp / RW][warp % RW][n * 8 + 2 * t + 1][g + 8] = acc[n][3];
   }
-  if (ks > 1) cluster.sync(); else __syncthreads();
-  // every block of the cluster finishes its share of the results, reading the others' parts in their order
-  for (int i = rank * kThreads + tid; i < RW * a.rows * kTileRows; i += ks * kThreads) {
-    const int o = i % kTileRows, r = i / kTileRows % RW, n = i / kTileRows / RW;  // a row of x at a time
-    const int col = (first_tile + r) * kTileRows + o;
+  __syncthreads();
+  // Results, a row of x at a time.  Every block of the cluster finishes a share of them: it gets the others' parts by their
+  // writing them into its shared memory, so that one meeting of the cluster is enough.
+  const int results = RW * a.rows * kTileRows, per = (results + ks - 1) / ks;
+  auto sum_of = [&](int i) {
+    const int o = i % kTileRows, r = i / kTileRows % RW, n = i / kTileRows / RW;
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < KW; ++k) v += part[k][r][n][o];
+    return v;
+  };
+  if (ks > 1) {
+    cluster.barrier_wait();  // every block has started
+    for (int i = tid; i < results; i += kThreads) cluster.map_shared_rank(inbox, i / per)[rank * per + i % per] = sum_of(i);
+    cluster.sync();
+  }
+  for (int i = rank * per + tid; i < min(results, (rank + 1) * per); i += kThreads) {
+    const int o = i % kTileRows, r = i / kTileRows % RW, n = i / kTileRows / RW, col = (first_tile + r) * kTileRows + o;
     if (col >= a.out) continue;
     float v = 0.f;
-    for (int c = 0; c < ks; ++c) {
-#pragma unroll
-      for (int k = 0; k < KW; ++k) v += ks > 1 ? *cluster.map_shared_rank(&part[k][r][n][o], c) : part[k][r][n][o];
-    }
+    if (ks > 1)
+      for (int c = 0; c < ks; ++c) v += inbox[c * per + i - rank * per];
+    else
+      v = sum_of(i);
     v *= 16.f;
     if (a.bias) v += a.bias[col];
     if (a.relu) v = v < 0.f ? 0.f : v;  // a NaN stays
     if (a.y) static_cast<T*>(a.y)[(long)n * a.out + col] = from_f32<T>(v);
     if (a.y_f32) a.y_f32[(long)n * a.out + col] = v;
   }
-  if (ks > 1) cluster.sync();  // no block's shared memory goes away while another reads it
 }
 
 // One warp per row and block of 128 weights, four consecutive weights per lane.
@@ -302,7 +338,7 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const T* w, long ld, int o
 }
 
 template <typename T, int GROUP, int NT, int RW, int KW> cudaError_t launch(Q4Args a, cudaStream_t st) {
-  constexpr int PER = kBlockK / GROUP, kRings = RW * KW * kRing * slot_bytes<PER>(), kStatic = RW * KW * NT * 8 * kTileRows * 4 + 512;
+  constexpr int PER = kBlockK / GROUP, kRings = RW * KW * kRing * slot_bytes<PER>(), kStatic = RW * (KW + 1) * NT * 8 * kTileRows * 4 + 512;
   constexpr int STEP = KW * kSlotBlocks;
   static_assert((KW == 1 ? kMaxRows * 3 : 2) * STEP * kBlockK * 2 <= kStageBytes, "a step's part of x fits");
   const int groups = ((a.out + kTileRows - 1) / kTileRows + RW - 1) / RW, block_bytes = a.rows * Terms<T>::N * kBlockK * 2;
