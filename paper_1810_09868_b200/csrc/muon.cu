@@ -41,7 +41,8 @@ constexpr int kStages = 3;
 // Stages (12 MMAs each) of an accumulation chain.  The error of a chain grows with its length, the hand-over of a chain to
 // the epilogue warps costs the tensor cores a few hundred cycles.  At 2048 and 4096 rows a chain of 4 is within 1.7 times
 // plain fp32 (which itself sums longer there) and 8 % faster than single stages; below, single stages are what it takes.
-__device__ __forceinline__ int chain_stages(int k_stages) { return k_stages >= 32 ? 4 : 1; }
+// The last product, whose epilogue is the longest and whose error nothing amplifies, takes two.
+template <bool FINAL> __device__ __forceinline__ int chain_stages(int k_stages) { return k_stages >= 32 ? 4 : FINAL ? 2 : 1; }
 constexpr int kThreads = 384;                    // a warpgroup for producer and issuer, two of epilogue warps
 // Registers per thread after the split: 168 at launch, 3 x 168 = 40 + 2 x 232.
 constexpr int kFewRegisters = 40, kManyRegisters = 232;
@@ -280,7 +281,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
         const Problem& p = L.p[pi];
         const bool mn = p.b_mn != 0;
         const Tile tile = find_tile(p, w - L.first_tile[pi]);
-        const int k_stages = tile.k1 - tile.k0, chain = chain_stages(k_stages);
+        const int k_stages = tile.k1 - tile.k0, chain = chain_stages<FINAL>(k_stages);
         const uint32_t idesc = umma_idesc_f16(2 * BM, BN, 0, mn);
         // K-major: lo 128 rows behind hi, 16 k = 32 bytes of the swizzled row.  MN-major: two groups of 64 columns, each
         // 64 k-rows of hi then of lo; 16 k = 16 rows.
@@ -335,9 +336,15 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
       const Tile tile = find_tile(p, w - L.first_tile[pi]);
       const int i0 = (2 * tile.i + (int)rank) * BM + quarter * 32, j0 = tile.j * BN + group * 128;  // the warp's first row and column
       const int rows = p.m - i0, cols = p.n - j0;                                           // what there is from there on
-      const int k_stages = tile.k1 - tile.k0, chain = chain_stages(k_stages);
+      const int k_stages = tile.k1 - tile.k0, chain = chain_stages<FINAL>(k_stages);
       // the sums start from what is added to the product: its loads pass while the first chain runs
       float sum[128];
+      if (FINAL && p.w_vec && lane < rows) {  // the weights of this lane's row come from far: have them nearer by the time they are updated
+        const char* w = reinterpret_cast<const char*>(p.w + (i0 + lane) * p.w_ld + j0);
+#pragma unroll
+        for (int c = 0; c < 128; c += 32)
+          if (c < cols) asm volatile("prefetch.global.L2 [%0];" ::"l"(w + c * 4));
+      }
       if (p.add1 && rows > 0 && cols > 0) {
         add_planes<true>(sum, p.add1 + i0 * p.ld + j0, p.plane, (int)p.ld, rows, cols, p.c1, piece, lane);
         if (!FINAL && p.add2) add_planes<false>(sum, p.add2 + i0 * p.ld + j0, p.plane, (int)p.ld, rows, cols, p.c2, piece, lane);
@@ -517,6 +524,8 @@ struct GramFinish {
   } t[kMaxTensors];
 };
 __global__ void __launch_bounds__(256) gram_finish_kernel(const __grid_constant__ GramFinish a) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   int k = 0;
   while (k + 1 < a.count && (int)blockIdx.x >= a.t[k + 1].first_block) ++k;
   const auto& t = a.t[k];
@@ -916,6 +925,21 @@ size_t batch_bytes(const vgg19_muon_tensor* t, int count) {
   return b + up(blocks * sizeof(double), 256);
 }
 
+// A launch whose set-up overlaps the one before it in the stream (the kernel waits for that one itself).
+template <typename P> cudaError_t launch_behind(void (*kernel)(P), unsigned blocks, int threads, int smem, const P& params, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, params);
+}
+
 template <bool FINAL, int N> cudaError_t launch_products(Launch<N>& L, cudaStream_t st) {
   int tiles = 0;
   for (int i = 0; i < L.count; ++i) {
@@ -933,33 +957,13 @@ template <bool FINAL, int N> cudaError_t launch_products(Launch<N>& L, cudaStrea
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   const int pairs = tiles < sms / 2 ? tiles : sms / 2;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(2 * pairs));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kSmemBytes;
-  cfg.stream = st;
-  cudaLaunchAttribute at{};
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, split_product_pair_kernel<N, FINAL>, L);
+  return launch_behind(split_product_pair_kernel<N, FINAL>, (unsigned)(2 * pairs), kThreads, kSmemBytes, L, st);
 }
 
 cudaError_t launch_small(const SmallLaunch& L, int count, cudaStream_t st) {
   cudaError_t e = cudaFuncSetAttribute(small_steps_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)count);
-  cfg.blockDim = dim3(kSmallThreads);
-  cfg.dynamicSmemBytes = kSmallSmem;
-  cfg.stream = st;
-  cudaLaunchAttribute at{};
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, small_steps_kernel, L);
+  return launch_behind(small_steps_kernel, (unsigned)count, kSmallThreads, kSmallSmem, L, st);
 }
 
 struct Options {
@@ -1049,8 +1053,7 @@ cudaError_t update_batch(const vgg19_muon_tensor* tensors, const int count, cons
     }
     run();
     if (finish.count && err == cudaSuccess) {
-      gram_finish_kernel<<<(unsigned)finish_blocks, 256, 0, st>>>(finish);
-      err = cudaGetLastError();
+      err = launch_behind(gram_finish_kernel, (unsigned)finish_blocks, 256, 0, finish, st);
     }
     // p(A) = a I + R with R = b A + c A A; Q = q0 I + S.  The identity's share is added in the epilogues, in fp32: what
     // the tensor core truncates is then relative to the smaller rest.
@@ -1076,31 +1079,39 @@ cudaError_t update_batch(const vgg19_muon_tensor* tensors, const int count, cons
         p.add1 = planes[i].at[kGramA]; p.c1 = poly_c1();
       }
       run();
-      if (k > 0) {  // S <- a S + q0 R + R S
-        const Matrix next = q == kQa ? kQb : kQa;
-        const float sn = rest_scale(k);
-        for (int i = 0; i < count; ++i) {
+      // S <- a S + q0 R + R S, for the tensors of one parity: between them the two launches that follow have room for it
+      const Matrix next = q == kQa ? kQb : kQa;
+      const float sn = rest_scale(k);
+      auto rest = [&](int parity) {
+        if (k == 0) return;
+        for (int i = parity; i < count; i += 2) {
           Problem& p = symmetric(i, poly, kScaleP, q, sq, next, sn);
           p.add1 = planes[i].at[q]; p.c1 = kA * sn / sq / p.alpha;
           p.add2 = planes[i].at[poly]; p.c2 = q0 * sn / kScaleP / p.alpha;
         }
-        q = next;
-        sq = sn;
-        q0 *= kA;
-      }
+      };
       if (k + 1 < group) {  // A <- p A p, one factor at a time
         for (int i = 0; i < count; ++i) {
           Problem& p = symmetric(i, poly, kScaleP, kGramA, kScaleA, kPA, kScaleA);
           p.add1 = planes[i].at[kGramA]; p.c1 = kA / p.alpha;
         }
+        rest(0);
         run();
         for (int i = 0; i < count; ++i) {
           Problem& p = symmetric(i, poly, kScaleP, kPA, kScaleA, kGramA, kScaleA);
           p.add1 = planes[i].at[kPA]; p.c1 = kA / p.alpha;
         }
+        rest(1);
         run();
       } else if (k > 0) {
+        rest(0);
+        rest(1);
         run();
+      }
+      if (k > 0) {
+        q = next;
+        sq = sn;
+        q0 *= kA;
       }
     }
     done += group;
