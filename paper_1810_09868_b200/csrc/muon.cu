@@ -540,22 +540,31 @@ __global__ void __launch_bounds__(256) gram_finish_kernel(const __grid_constant_
     t.out[i * ld + j] = __half_as_ushort(h);
     t.out[t.plane + i * ld + j] = __half_as_ushort(l);
   };
+  const int j = bj * 32 + x;
+  float v[4][8];  // everything this thread adds, requested at once
 #pragma unroll
-  for (int r = y; r < 32; r += 8) {
-    const int i = bi * 32 + r, j = bj * 32 + x;
-    if (i >= t.m || j >= t.m) continue;
-    float s = 0.f;
-    for (int p = 0; p < t.splits; ++p) s += t.partial[p * part + i * ld + j];
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      const int i = bi * 32 + y + 8 * r;
+      v[r][p] = p < t.splits && i < t.m && j < t.m ? t.partial[p * part + i * ld + j] : 0.f;
+    }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int i = bi * 32 + y + 8 * r;
+    float s = v[r][0];
+#pragma unroll
+    for (int p = 1; p < 8; ++p) s += v[r][p];
     s *= a.alpha;
-    tile[r][x] = s;
-    store(i, j, s);
+    tile[y + 8 * r][x] = s;
+    if (i < t.m && j < t.m) store(i, j, s);
   }
   if (bi == bj) return;
   __syncthreads();
 #pragma unroll
   for (int r = y; r < 32; r += 8) {
-    const int i = bj * 32 + r, j = bi * 32 + x;
-    if (i < t.m && j < t.m) store(i, j, tile[x][r]);
+    const int i = bj * 32 + r, c = bi * 32 + x;
+    if (i < t.m && c < t.m) store(i, c, tile[x][r]);
   }
 }
 
