@@ -467,8 +467,9 @@ int vgg19_ops_status(void *stream);
 /* Wait for the stream and report any device-side error recorded so far:
  * VGG19_ERR_DEVICE_TIMEOUT when a bounded wait inside a kernel ran out,
  * VGG19_ERR_ARG when a label outside [0,1000) reached the loss (the label is
- * never used as an index; that pass's loss is NaN).  The record is cleared,
- * and the handle stays usable. */
+ * never used as an index; that pass's loss is NaN).  Waits inside the 4-bit
+ * dense layers and vgg19_muon_step are reported here too, if the handle has
+ * run them.  The record is cleared, and the handle stays usable. */
 int vgg19_sync_status(vgg19_t *net, void *stream);
 
 /* Diagnostic for the error path above.  Every wait inside the kernels (on a

@@ -75,6 +75,9 @@ class Net:
         """The orthogonalised update of every weight tensor (biases: momentum and a plain step at bias_lr, lr if None).
         momentum_buffer: fp32, n_params elements, zeros at first; the workspace is allocated on the first call and kept."""
         torch = self._torch
+        for name, t in (("grads", grads), ("momentum_buffer", momentum_buffer)):
+            if t.dtype != torch.float32 or t.device != self.workspace.device or not t.is_contiguous() or t.numel() != self.n_params:
+                raise binding.Vgg19Error(binding.VGG19_ERR_ARG, f"{name}: {self.n_params} dense float32 values on {self.device} are needed")
         if getattr(self, "muon_workspace", None) is None:
             self.muon_workspace = torch.empty(binding.vgg19_muon_step_bytes(self.handle), dtype=torch.uint8, device=self.device)
         with torch.cuda.device(self.device):

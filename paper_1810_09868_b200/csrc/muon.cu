@@ -4,21 +4,30 @@
 //   W <- (1 - lr decay) W - lr sqrt(max(1, rows / cols)) X.
 //
 // Every p(A_k) is a polynomial of A_0 = X_0 X_0^T, so the products commute and the iteration can run on m x m symmetric
-// matrices: Q <- p(A) Q, A <- p(A) A p(A), and X = Q X_0 once at the end.  With n / m = r columns per row a step then
-// costs four symmetric products (half a product each) instead of (3 r + 1).  A alone forgets singular values below
-// the square root of its precision, which the iteration amplifies up to 3.4 times a step: so after every three steps X is formed and
-// A taken from it anew.  Against 64 bits that is as close as the plain iteration in fp32 (5e-6 against 7e-6 on gradients of low
-// rank with noise; without the restart 3e-5).
+// matrices: Q <- p(A) Q, A <- p(A) A p(A), and X = Q X_0 once at the end.  With r = n / m columns per row a step then
+// costs four symmetric products (half a product each) instead of 3 r + 1.  A alone forgets singular values below the square
+// root of its precision, which the iteration amplifies up to 3.4 times a step: so after every three steps X is formed and
+// A taken from it anew (five steps: 6 r + 14 such halves against 15 r + 5).  Measured against 64 bits on gradients of low rank with noise:
+// 4e-6 to 6e-6 relative, plain fp32 products 1.1e-5 to 3.9e-5; without the restart 3e-5 to 1.8e-4.
 //
 // Precision.  A matrix is kept as two fp16 planes hi + lo of its values times a power of two (22 bits; the scales below
 // keep every entry inside fp16's range), a product is hi hi + hi lo + lo hi in fp32, on tcgen05.  The tensor core's fp32
-// accumulation truncates, so a chain ends after L.chunk_ stages of 64 and the epilogue warps add the chunks into registers.
+// accumulation truncates (about half a unit of the sum so far per instruction), so a chain ends after one to four stages
+// of 64 and the epilogue warps add the chains in registers.
+//
+// Identities stay out of the products: with p(A) = a I + R and Q = q0 I + S the epilogues add a and q0 times their matrix in
+// fp32, and what the tensor core truncates is relative to the smaller rest (9e-6 -> 5e-6).
 //
 // The product kernel: CTA pairs (cta_group::2), 256 x 256 tiles, persistent.  A stage holds hi and lo of both operands
 // (64 KB per CTA) and feeds three products, so what a CTA loads per product is two thirds of what one pair of
 // planes at a time would take; the plain pair kernels of this library are bound by exactly that rate.  All tensors of a call and
 // all products that do not depend on one another share a launch.  Symmetric results are computed on and above the
 // diagonal and stored twice.  The last product's epilogue updates the weights: X itself is never stored.
+//
+// Measured (B200, five steps): the dense layers of a 224 x 224 network (4096 x 25088, 4096 x 4096, 1000 x 4096) in 12.8 ms, of which
+// 0.43 ms momentum, norm and X_0 at 6.9 TB/s; 14.7 TFLOP of fp16 products at 1.19 PFLOP/s, 0.86 of the measured sustained rate
+// under the power cap that bounds them.  The sixteen filters in 0.68 ms: launches of 15 to 25 us, each a chain of latencies (3 us
+// from one launch to the next, 5 us for the addends beside the stages on an SM's 64 bytes a cycle from L2, 0.8 us a stage, 4 us of stores).
 #include <cuda_fp16.h>
 
 #include "../../include/vgg19_b200.h"

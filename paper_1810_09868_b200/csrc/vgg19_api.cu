@@ -80,6 +80,7 @@ struct vgg19 {
   half16 *split_w = nullptr; // fp32 configuration on tensor cores: rows [hi | lo | hi] (fp16 terms) of every weight matrix, at 3 * w_off
   char *q4 = nullptr;        // VGG19_FLAG_DENSE_Q4: codes and scales of the dense layers
   size_t q4_codes[kFcLayers] = {}, q4_scales[kFcLayers] = {};  // byte offsets in it
+  bool muon_used = false;    // vgg19_muon_step has run: vgg19_sync_status looks at its kernels' error word too
   int *dev_error = nullptr;
   void *ws = nullptr;
   size_t ws_bytes = 0;
@@ -919,7 +920,12 @@ int vgg19_muon_step(vgg19_t *n, const float *grads, float *momentum_buffer, floa
   vgg19_muon_tensor t[kLayers];
   muon_tensors(n, grads, momentum_buffer, t);
   const int rc = vgg19_muon_update(t, kLayers, lr, momentum, decay, steps, nesterov, workspace, bytes, stream);
-  if (rc != VGG19_OK) return fail(n, rc, "%s", std::string(vgg19_last_error(nullptr)).c_str());
+  if (rc != VGG19_OK) {
+    char text[512];
+    snprintf(text, sizeof text, "%s", vgg19_last_error(nullptr));
+    return fail(n, rc, "%s", text);
+  }
+  n->muon_used = true;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   MuonVector v[kLayers];
   for (int l = 0; l < kLayers; ++l) {
@@ -1306,6 +1312,10 @@ int vgg19_sync_status(vgg19_t *n, void *stream) {
       return fail(n, VGG19_ERR_RANGE, "an activation beyond fp16's range (65504) met the split-fp16 path");
     return fail(n, VGG19_ERR_DEVICE_TIMEOUT, "a device-side wait ran out (code %d)", code);
   }
+  // the operators without a handle that this network's calls have run
+  if (n->q4) CUDA_TRY(n, q4_take_error(&code));
+  if (!code && n->muon_used) CUDA_TRY(n, muon_take_error(&code));
+  if (code) return fail(n, VGG19_ERR_DEVICE_TIMEOUT, "a device-side wait ran out (code %d)", code);
   return VGG19_OK;
 }
 

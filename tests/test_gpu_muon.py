@@ -104,8 +104,9 @@ def test_update(p, rows, cols):
 
 
 @pytest.mark.parametrize("steps", [1, 2, 3, 4, 5, 6, 7, 10])
-def test_steps(p, steps):
-    t = tensors(70, 200, seed=steps)
+@pytest.mark.parametrize("rows,cols", [(70, 200), (200, 330), (530, 300)])
+def test_steps(p, rows, cols, steps):
+    t = tensors(rows, cols, seed=steps)
     before = copies(t)
     run(p, [t], steps=steps)
     check(t, before, 0.02, 0.95, 0.01, steps, True)
@@ -271,4 +272,6 @@ def test_network_step(p, dtype_name):
     b, _ = again.backward(images, labels)
     assert torch.equal(a, b)
     assert torch.equal(net.forward(images), again.forward(images))
+    with pytest.raises(p.Vgg19Error):
+        net.muon_step(grads, momentum[:-1], 0.02)
     net.close(), again.close()
