@@ -41,11 +41,16 @@ using namespace tc;
 static __device__ int g_muon_error;  // a DeviceError code once a bounded wait ran out
 
 // ---- sizes -----------------------------------------------------------------------------------------------------
-constexpr int BM = 128, BN = 256, BK = 64;       // rows per CTA (a pair has 256), columns per pair, K per stage
+constexpr int BM = 128, BK = 64;                 // rows per CTA (a pair has 256), K per stage
 constexpr int kPlaneBytes = 128 * BK * 2;        // 128 rows (or K-rows) of one plane in a stage
 constexpr int kOperandBytes = 2 * kPlaneBytes;   // hi and lo
-constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kStages = 3;
+// Columns per pair: 256, or 128 where that still leaves pairs idle: then a tile's loads, products, addends and stores are
+// what a launch takes, and half of each is 10 us where a whole is 16.
+template <int BN> constexpr int kOtherBytes = BN * BK * 2;  // hi and lo of a CTA's half of the columns
+template <int BN> constexpr int kStageBytes = kOperandBytes + kOtherBytes<BN>;
+template <int BN> constexpr int kStages = BN == 256 ? 3 : 4;
+constexpr int kRingBytes = 3 * kStageBytes<256>;
+static_assert(kRingBytes == 4 * kStageBytes<128>, "the same shared memory");
 
 // Stages (12 MMAs each) of an accumulation chain.  The error of a chain grows with its length, the hand-over of a chain to
 // the epilogue warps costs the tensor cores a few hundred cycles.  At 2048 and 4096 rows a chain of 4 is within 1.7 times
@@ -56,7 +61,7 @@ constexpr int kThreads = 384;                    // a warpgroup for producer and
 // Registers per thread after the split: 168 at launch, 3 x 168 = 40 + 2 x 232.
 constexpr int kFewRegisters = 40, kManyRegisters = 232;
 constexpr int kPieceBytes = 4096;                // an epilogue warp's own 32 rows of 128 bytes
-constexpr int kSmemBytes = kStages * kStageBytes + 8 * kPieceBytes + 1024 + 256;
+constexpr int kSmemBytes = kRingBytes + 8 * kPieceBytes + 1024 + 256;
 constexpr int kMaxTensors = 20, kMaxProblems = 2 * kMaxTensors;
 
 // The quintic's coefficients, and the scales of what is stored.  |X| <= 1.21 after any step, so |A| <= 1.47 and (by the
@@ -69,12 +74,20 @@ __host__ __device__ constexpr float poly_alpha() { return kC * kScaleP / (kScale
 __host__ __device__ constexpr float poly_c1() { return kB * kScaleP / kScaleA / poly_alpha(); }
 __host__ __device__ constexpr float rest_scale(int k) { return k == 0 ? kScaleP : k == 1 ? kScaleQ2 : kScaleQ3; }
 
+// What a kernel did before this overlapped the launch before it in the stream; what follows reads that one's results.  (Its
+// own successor may be set up from here on.)
+__device__ __forceinline__ void behind_previous() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // ---- one product ---------------------------------------------------------------------------------------------
 // D[i][j] = alpha * (c1 add1[i][j] + c2 add2[i][j] + sum_k A[i][k] B[j][k]) (or B[k][j]: b_mn), m x n.
 struct __align__(64) Problem {
   CUtensorMap a, b;
   int m, n, k_stages, tiles_m, tiles_n;
-  int sym;         // tiles on and above the diagonal only, stored twice
+  int sym;         // tiles on and above the diagonal only, stored twice (or mirrored by gram_finish_kernel)
+  int square;      // for the host: 1 always so, 2 so with square tiles, else all tiles
   int splits, per_split;  // K is cut into that many parts, of that many stages
   int b_mn;
   float alpha;
@@ -139,10 +152,10 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint32_t (&hi)[4], u
 // 128-byte lines (one thread per row took 3 to 4 us per tile and matrix, eight sectors where one would do).
 __device__ __forceinline__ int piece_at(int row, int chunk) { return row * 8 + (chunk ^ (row & 7)); }
 
-// sum (+)= c (hi + lo) of 128 columns of planes; m points at the warp's first row and column.  What this costs is the latency
+// sum (+)= c (hi + lo) of CW columns of planes; m points at the warp's first row and column.  What this costs is the latency
 // of its requests: while the sums are still to be set (FIRST) there are registers for both planes of 64 columns at once.
-template <bool FIRST>
-__device__ __forceinline__ void add_planes(float (&sum)[128], const half16* m, long plane, int ld, int rows, int cols, float c, uint4* piece, int lane) {
+template <bool FIRST, int CW>
+__device__ __forceinline__ void add_planes(float (&sum)[CW], const half16* m, long plane, int ld, int rows, int cols, float c, uint4* piece, int lane) {
   const int r0 = lane / 8, k0 = lane % 8;
   m += (long)r0 * ld + k0 * 8;
   auto request = [&](uint4 (&v)[8], int h, int c0) {
@@ -170,7 +183,7 @@ __device__ __forceinline__ void add_planes(float (&sum)[128], const half16* m, l
     __syncwarp();
   };
 #pragma unroll
-  for (int c0 = 0; c0 < 128; c0 += 64) {
+  for (int c0 = 0; c0 < CW; c0 += 64) {
     uint4 hi[8];
     request(hi, 0, c0);
     if (FIRST) {
@@ -191,17 +204,18 @@ __device__ __forceinline__ void put(float* w, bf16* w16, long at, float v) {
 }
 
 // FINAL: every problem updates its w; else none does.
-template <int N, bool FINAL>
+template <int N, bool FINAL, int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
+  constexpr int STAGES = kStages<BN>, STAGE_BYTES = kStageBytes<BN>, CW = BN / 2;  // CW: columns of an epilogue group, a thread's sums
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t pieces = smem_base + kStages * kStageBytes, bars = pieces + 8 * kPieceBytes;
+  const uint32_t pieces = smem_base + kRingBytes, bars = pieces + 8 * kPieceBytes;
   auto full_bar = [&](int s) { return bars + 8u * s; };                   // used in the even CTA
-  auto empty_bar = [&](int s) { return bars + 8u * (kStages + s); };      // both CTAs
-  auto acc_full_bar = [&](int b) { return bars + 8u * (2 * kStages + b); };       // both CTAs
-  auto acc_empty_bar = [&](int b) { return bars + 8u * (2 * kStages + 2 + b); };  // used in the even CTA
-  const uint32_t drain_bar = bars + 8u * (2 * kStages + 4);
+  auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };      // both CTAs
+  auto acc_full_bar = [&](int b) { return bars + 8u * (2 * STAGES + b); };       // both CTAs
+  auto acc_empty_bar = [&](int b) { return bars + 8u * (2 * STAGES + 2 + b); };  // used in the even CTA
+  const uint32_t drain_bar = bars + 8u * (2 * STAGES + 4);
   __shared__ uint32_t tmem_base_slot;
   __shared__ int abort_flag;
 
@@ -212,13 +226,13 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
 
   if (threadIdx.x == 0) {
     abort_flag = 0;
-    for (int s = 0; s < kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(acc_full_bar(b), 1); mbar_init(acc_empty_bar(b), 16); }  // the epilogue warps of both CTAs
     mbar_init(drain_bar, 1);
     mbar_fence_init();
   }
   if (warp == 1) {
-    tmem_alloc_pair(smem_u32(&tmem_base_slot), 512);
+    tmem_alloc_pair(smem_u32(&tmem_base_slot), 2 * BN);
     tmem_relinquish_pair();
   }
   tc_fence_before();
@@ -226,18 +240,16 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
   cluster_sync_all();  // the peer's barriers are initialised before anything signals them
   tc_fence_after();
   const uint32_t tmem_base = tmem_base_slot;
-  // What comes before overlapped the previous launch; what follows reads its results.
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  behind_previous();
 
   if (warp < 4) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
   if (warp == 0) {
     // ------------------------------ TMA producer ------------------------------
     if (lane == 0) {
-      uint32_t fills[kStages];
+      uint32_t fills[STAGES];
 #pragma unroll
-      for (int s = 0; s < kStages; ++s) fills[s] = 0;
+      for (int s = 0; s < STAGES; ++s) fills[s] = 0;
       int stage = 0, pi = 0;
       uint32_t phase = 0;
       bool ok = true;
@@ -248,27 +260,27 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
         const int row = (2 * tile.i + (int)rank) * BM, col = tile.j * BN + (int)rank * (BN / 2), mn = p.b_mn;
         for (int kb = tile.k0; kb < tile.k1; ++kb) {
           if (!mbar_wait(empty_bar(stage), phase ^ 1, &abort_flag, &g_muon_error, kDevTimeoutStageFree)) { ok = false; break; }
-          const uint32_t sa = smem_base + stage * kStageBytes, sb = sa + kOperandBytes;
+          const uint32_t sa = smem_base + stage * STAGE_BYTES, sb = sa + kOperandBytes;
           const uint32_t full = map_to_cta(full_bar(stage), 0);
           // the even CTA announces the bytes of both CTAs' copies; what lies outside a matrix arrives as zeros
-          if (leader) mbar_expect_tx(full_bar(stage), 2 * kStageBytes);
+          if (leader) mbar_expect_tx(full_bar(stage), 2 * STAGE_BYTES);
           tma_load_3d_pair(sa, &p.a, full, kb * BK, row, 0);
           if (mn) {
             tma_load_3d_pair(sb, &p.b, full, col, kb * BK, 0);
-            tma_load_3d_pair(sb + kPlaneBytes, &p.b, full, col + 64, kb * BK, 0);
+            if (BN == 256) tma_load_3d_pair(sb + kPlaneBytes, &p.b, full, col + 64, kb * BK, 0);
           } else {
             tma_load_3d_pair(sb, &p.b, full, kb * BK, col, 0);
           }
 #pragma unroll
-          for (int s = 0; s < kStages; ++s) fills[s] += s == stage;
-          if (++stage == kStages) { stage = 0; phase ^= 1; }
+          for (int s = 0; s < STAGES; ++s) fills[s] += s == stage;
+          if (++stage == STAGES) { stage = 0; phase ^= 1; }
         }
       }
       if (!ok) {
         // let every copy in flight land before the CTA may exit (see the pair convolution)
         if (leader) {
 #pragma unroll
-          for (int s = 0; s < kStages; ++s)
+          for (int s = 0; s < STAGES; ++s)
             if (fills[s]) {
               const unsigned long long t0 = global_timer_ns();
               while (!mbar_try_wait(full_bar(s), (fills[s] - 1) & 1) && global_timer_ns() - t0 < 100000000ull) {}
@@ -292,9 +304,9 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
         const Tile tile = find_tile(p, w - L.first_tile[pi]);
         const int k_stages = tile.k1 - tile.k0, chain = chain_stages<FINAL>(k_stages);
         const uint32_t idesc = umma_idesc_f16(2 * BM, BN, 0, mn);
-        // K-major: lo 128 rows behind hi, 16 k = 32 bytes of the swizzled row.  MN-major: two groups of 64 columns, each
+        // K-major: lo behind all rows of hi, 16 k = 32 bytes of the swizzled row.  MN-major: two groups of 64 columns, each
         // 64 k-rows of hi then of lo; 16 k = 16 rows.
-        const uint32_t b_lo = mn ? kPlaneBytes / 2 : kPlaneBytes, b_step = mn ? 2048 : 32, b_lbo = mn ? kPlaneBytes : 16;
+        const uint32_t b_lo = mn ? kPlaneBytes / 2 : kOtherBytes<BN> / 2, b_step = mn ? 2048 : 32, b_lbo = mn ? kPlaneBytes : 16;
         for (int kb0 = 0, kb1; kb0 < k_stages && ok; kb0 = kb1, ++chunk) {
           kb1 = min(kb0 + chain, k_stages);
           const int buf = chunk & 1;
@@ -304,7 +316,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
           for (int kb = kb0; kb < kb1; ++kb) {
             if (!mbar_wait(full_bar(stage), phase, &abort_flag, &g_muon_error, kDevTimeoutTmaFull)) { ok = false; break; }
             tc_fence_after();
-            const uint32_t sa = smem_base + stage * kStageBytes, sb = sa + kOperandBytes;
+            const uint32_t sa = smem_base + stage * STAGE_BYTES, sb = sa + kOperandBytes;
             const uint64_t ah = smem_desc_sw128(sa, 16), al = smem_desc_sw128(sa + kPlaneBytes, 16);
             const uint64_t bh = smem_desc_sw128(sb, b_lbo), bl = smem_desc_sw128(sb + b_lo, b_lbo);
             // the small products first: what the tensor core truncates is relative to the sum so far
@@ -319,7 +331,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
             for (int k = 0; k < BK / 16; ++k)
               umma_bf16_pair_acc(d, desc_advance(ah, k * 32), desc_advance(bh, k * b_step), idesc);
             umma_commit_pair(empty_bar(stage), 3);  // frees the stage in both CTAs
-            if (++stage == kStages) { stage = 0; phase ^= 1; }
+            if (++stage == STAGES) { stage = 0; phase ^= 1; }
           }
           if (ok) umma_commit_pair(acc_full_bar(buf), 3);
         }
@@ -343,31 +355,31 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
       while (w >= L.first_tile[pi + 1]) ++pi;
       const Problem& p = L.p[pi];
       const Tile tile = find_tile(p, w - L.first_tile[pi]);
-      const int i0 = (2 * tile.i + (int)rank) * BM + quarter * 32, j0 = tile.j * BN + group * 128;  // the warp's first row and column
+      const int i0 = (2 * tile.i + (int)rank) * BM + quarter * 32, j0 = tile.j * BN + group * CW;  // the warp's first row and column
       const int rows = p.m - i0, cols = p.n - j0;                                           // what there is from there on
       const int k_stages = tile.k1 - tile.k0, chain = chain_stages<FINAL>(k_stages);
       // the sums start from what is added to the product: its loads pass while the first chain runs
-      float sum[128];
+      float sum[CW];
       if (FINAL && p.w_vec && lane < rows) {  // the weights of this lane's row come from far: have them nearer by the time they are updated
         const char* w = reinterpret_cast<const char*>(p.w + (i0 + lane) * p.w_ld + j0);
 #pragma unroll
-        for (int c = 0; c < 128; c += 32)
+        for (int c = 0; c < CW; c += 32)
           if (c < cols) asm volatile("prefetch.global.L2 [%0];" ::"l"(w + c * 4));
       }
       if (p.add1 && rows > 0 && cols > 0) {
-        add_planes<true>(sum, p.add1 + i0 * p.ld + j0, p.plane, (int)p.ld, rows, cols, p.c1, piece, lane);
-        if (!FINAL && p.add2) add_planes<false>(sum, p.add2 + i0 * p.ld + j0, p.plane, (int)p.ld, rows, cols, p.c2, piece, lane);
+        add_planes<true, CW>(sum, p.add1 + i0 * p.ld + j0, p.plane, (int)p.ld, rows, cols, p.c1, piece, lane);
+        if (!FINAL && p.add2) add_planes<false, CW>(sum, p.add2 + i0 * p.ld + j0, p.plane, (int)p.ld, rows, cols, p.c2, piece, lane);
       } else {
 #pragma unroll
-        for (int j = 0; j < 128; ++j) sum[j] = 0.f;
+        for (int j = 0; j < CW; ++j) sum[j] = 0.f;
       }
       for (int kb0 = 0; kb0 < k_stages; kb0 += chain, ++chunk) {
         const int buf = chunk & 1;
         if (!__all_sync(0xffffffffu, mbar_wait(acc_full_bar(buf), (chunk >> 1) & 1, &abort_flag, &g_muon_error, kDevTimeoutAccum))) { ok = false; break; }
         tc_fence_after();
-        const uint32_t src = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + group * 128);
+        const uint32_t src = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + group * CW);
 #pragma unroll
-        for (int c = 0; c < 128; c += 32) {
+        for (int c = 0; c < CW; c += 32) {
           uint32_t v[32];
           tmem_ld_32x32(src + c, v);
           tmem_ld_wait();
@@ -387,7 +399,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
       if (!FINAL && p.partial) {
         float* out = p.partial + ((long)tile.split * p.m + i0) * ld + j0;
 #pragma unroll
-        for (int c0 = 0; c0 < 128; c0 += 32) {
+        for (int c0 = 0; c0 < CW; c0 += 32) {
           if (c0 >= cols) break;
 #pragma unroll
           for (int k = 0; k < 8; ++k)
@@ -403,7 +415,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
       } else if (!FINAL) {
         half16* out = p.out + i0 * ld + j0;
 #pragma unroll
-        for (int c0 = 0; c0 < 128; c0 += 64) {
+        for (int c0 = 0; c0 < CW; c0 += 64) {
           if (c0 >= cols) break;
           uint32_t hi[8][4], lo[8][4];
 #pragma unroll
@@ -440,7 +452,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
           const long at = j0 * p.w_ld + i0 + lane, w_ld = p.w_ld;
           const float keep = p.keep;
 #pragma unroll
-          for (int c0 = 0; c0 < 128; c0 += 16) {
+          for (int c0 = 0; c0 < CW; c0 += 16) {
             float old[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j)
@@ -456,7 +468,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
         float* w = p.w + i0 * w_ld + j0;
         bf16* w16 = p.w16 ? p.w16 + i0 * w_ld + j0 : nullptr;
 #pragma unroll
-        for (int c0 = 0; c0 < 128; c0 += 32) {
+        for (int c0 = 0; c0 < CW; c0 += 32) {
           if (c0 >= cols) break;
           {
             float4 old[8];
@@ -516,7 +528,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
-    tmem_dealloc_pair(tmem_base, 512);
+    tmem_dealloc_pair(tmem_base, 2 * BN);
   }
 }
 
@@ -533,8 +545,7 @@ struct GramFinish {
   } t[kMaxTensors];
 };
 __global__ void __launch_bounds__(256) gram_finish_kernel(const __grid_constant__ GramFinish a) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  behind_previous();
   int k = 0;
   while (k + 1 < a.count && (int)blockIdx.x >= a.t[k + 1].first_block) ++k;
   const auto& t = a.t[k];
@@ -615,8 +626,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_steps_kernel(const __g
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = tmem_base_slot;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  behind_previous();
 
   if (tid == 0) {
     mbar_expect_tx(load_bar, k_stages * kOperandBytes);
@@ -753,6 +763,7 @@ struct Element {
 struct Elements {
   int count, nesterov;
   float mu;
+  long norm_blocks;
   double* partial;  // a sum of squares per block of the first kernel
   double* inverse;  // 1 / |U|_F per tensor
   Element t[kMaxTensors];
@@ -763,6 +774,7 @@ __device__ __forceinline__ float direction(float g, float m, float mu, int neste
 
 // M <- mu M + G; the block's sum of squares of U, in 64 bits: neither tiny nor huge gradients leave the range.
 __global__ void __launch_bounds__(kNormThreads) momentum_norm_kernel(const __grid_constant__ Elements a) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   int t = 0;
   while (t + 1 < a.count && blockIdx.x >= a.t[t + 1].first_norm) ++t;
   const Element& e = a.t[t];
@@ -799,9 +811,10 @@ __global__ void __launch_bounds__(kNormThreads) momentum_norm_kernel(const __gri
 }
 
 // One block per tensor adds its blocks' sums, always in the same order.
-__global__ void __launch_bounds__(1024) inverse_norm_kernel(const __grid_constant__ Elements a, long blocks) {
+__global__ void __launch_bounds__(1024) inverse_norm_kernel(const __grid_constant__ Elements a) {
+  behind_previous();
   const int t = blockIdx.x;
-  const long begin = a.t[t].first_norm, end = t + 1 < a.count ? a.t[t + 1].first_norm : blocks;
+  const long begin = a.t[t].first_norm, end = t + 1 < a.count ? a.t[t + 1].first_norm : a.norm_blocks;
   double s = 0.0;
   for (long i = begin + threadIdx.x; i < end; i += 1024) s += a.partial[i];
   __shared__ double part[32];
@@ -819,6 +832,7 @@ __global__ void __launch_bounds__(1024) inverse_norm_kernel(const __grid_constan
 // X_0 = U / |U|_F as planes, transposed where the matrix has more rows than columns.
 constexpr int kSplitThreads = 256;
 __global__ void __launch_bounds__(kSplitThreads) split_kernel(const __grid_constant__ Elements a) {
+  behind_previous();
   int t = 0;
   while (t + 1 < a.count && blockIdx.x >= a.t[t + 1].first_split) ++t;
   const Element& e = a.t[t];
@@ -915,7 +929,7 @@ enum Matrix { kX0, kX1, kGramA, kPoly, kQa, kQb, kPA, kMatrices };
 struct Planes {
   half16* at[kMatrices];
   float* partial;
-  CUtensorMap k_major[kMatrices], mn_major[2];
+  CUtensorMap k_major[kMatrices], box64[kMatrices];  // boxes of 128 and of 64 rows
 };
 
 bool plane_map(CUtensorMap* map, const half16* base, long rows, long cols, long ld, uint32_t box_rows) {
@@ -958,24 +972,44 @@ template <typename P> cudaError_t launch_behind(void (*kernel)(P), unsigned bloc
   return cudaLaunchKernelEx(&cfg, kernel, params);
 }
 
-template <bool FINAL, int N> cudaError_t launch_products(Launch<N>& L, cudaStream_t st) {
+// The launch's tiles of 256 x bn; -1 where a problem takes square tiles only (a triangle of them).
+template <int N> int count_tiles(Launch<N>& L, int bn) {
   int tiles = 0;
   for (int i = 0; i < L.count; ++i) {
     Problem& p = L.p[i];
-    p.tiles_m = (p.m + 2 * BM - 1) / (2 * BM);
-    p.tiles_n = (p.n + BN - 1) / BN;
     if (p.splits < 1) { p.splits = 1; p.per_split = p.k_stages; }
+    p.tiles_m = (p.m + 2 * BM - 1) / (2 * BM);
+    p.tiles_n = (p.n + bn - 1) / bn;
+    p.sym = p.square == 1 || (p.square == 2 && bn == 2 * BM);
+    if (p.sym && bn != 2 * BM) return -1;
     L.first_tile[i] = tiles;
     tiles += p.splits * (p.sym ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n);
   }
   L.first_tile[L.count] = tiles;
-  cudaError_t e = cudaFuncSetAttribute(split_product_pair_kernel<N, FINAL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  return tiles;
+}
+
+template <bool FINAL, int BN, int N> cudaError_t launch_tiles(const Launch<N>& L, int pairs, cudaStream_t st) {
+  const cudaError_t e = cudaFuncSetAttribute(split_product_pair_kernel<N, FINAL, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   if (e != cudaSuccess) return e;
+  const int tiles = L.first_tile[L.count];
+  return launch_behind(split_product_pair_kernel<N, FINAL, BN>, (unsigned)(2 * (tiles < pairs ? tiles : pairs)), kThreads, kSmemBytes, L, st);
+}
+
+// narrow[i]: the map of problem i's second operand in boxes of 64 rows, or null where p.b is that (or it is read by columns).
+template <bool FINAL, int N> cudaError_t launch_products(Launch<N>& L, const CUtensorMap* const* narrow, cudaStream_t st) {
   int dev = 0, sms = 148;
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  const int pairs = tiles < sms / 2 ? tiles : sms / 2;
-  return launch_behind(split_product_pair_kernel<N, FINAL>, (unsigned)(2 * pairs), kThreads, kSmemBytes, L, st);
+  const int pairs = sms / 2, half = count_tiles(L, 128), whole = count_tiles(L, 256);
+  // a round of halves takes about 5/8 of a round of whole tiles.  (The sums are the same, bit for bit.)
+  if (half > 0 && 5 * ((half + pairs - 1) / pairs) < 8 * ((whole + pairs - 1) / pairs)) {
+    count_tiles(L, 128);
+    for (int i = 0; i < L.count; ++i)
+      if (narrow[i]) L.p[i].b = *narrow[i];
+    return launch_tiles<FINAL, 128>(L, pairs, st);
+  }
+  return launch_tiles<FINAL, 256>(L, pairs, st);
 }
 
 cudaError_t launch_small(const SmallLaunch& L, int count, cudaStream_t st) {
@@ -1007,7 +1041,7 @@ cudaError_t update_batch(const vgg19_muon_tensor* tensors, const int count, cons
       q.at[k] = reinterpret_cast<half16*>(ws);
       ws += x ? s.x_bytes() : s.a_bytes();
       if (!plane_map(&q.k_major[k], q.at[k], s.m, x ? s.n : s.m, x ? s.ldn : s.ldm, 128)) return cudaErrorInvalidValue;
-      if (x && !plane_map(&q.mn_major[k], q.at[k], s.m, s.n, s.ldn, 64)) return cudaErrorInvalidValue;
+      if (!plane_map(&q.box64[k], q.at[k], s.m, x ? s.n : s.m, x ? s.ldn : s.ldm, 64)) return cudaErrorInvalidValue;
     }
     q.partial = reinterpret_cast<float*>(ws);
     ws += s.partial_bytes();
@@ -1021,28 +1055,34 @@ cudaError_t update_batch(const vgg19_muon_tensor* tensors, const int count, cons
     norm_blocks += s.norm_blocks();
     split_blocks += s.split_blocks();
   }
+  el.norm_blocks = norm_blocks;
   el.partial = reinterpret_cast<double*>(ws);
   momentum_norm_kernel<<<(unsigned)norm_blocks, kNormThreads, 0, st>>>(el);
-  inverse_norm_kernel<<<(unsigned)count, 1024, 0, st>>>(el, norm_blocks);
-  split_kernel<<<(unsigned)split_blocks, kSplitThreads, 0, st>>>(el);
   cudaError_t err = cudaGetLastError();
+  if (err == cudaSuccess) err = launch_behind(inverse_norm_kernel, (unsigned)count, 1024, 0, el, st);
+  if (err == cudaSuccess) err = launch_behind(split_kernel, (unsigned)split_blocks, kSplitThreads, 0, el, st);
   if (err != cudaSuccess) return err;
 
   static thread_local Launch<N> L;
+  const CUtensorMap* narrow[N];
   // D = scale_d * (A / scale_a) (B / scale_b), all m x m symmetric
   auto symmetric = [&](int i, Matrix a, float sa, Matrix b, float sb, Matrix d, float sd) -> Problem& {
     const Shape s(tensors[i]);
     Problem& p = L.p[L.count++];
     p = Problem{};
     p.a = planes[i].k_major[a]; p.b = planes[i].k_major[b];
+    narrow[L.count - 1] = &planes[i].box64[b];
     p.m = p.n = (int)s.m;
     p.k_stages = (int)((s.m + BK - 1) / BK);
-    p.sym = s.m > 512;  // (up to 2 x 2 tiles, a tile more costs less than storing one twice)
+    p.square = s.m > 1024;  // (where all tiles are taken, halves of them can fill idle pairs, and none is stored twice)
     p.alpha = sd / (sa * sb);
     p.out = planes[i].at[d]; p.ld = s.ldm; p.plane = s.m * s.ldm;
     return p;
   };
-  auto run = [&] { if (err == cudaSuccess) err = L.p[0].w ? launch_products<true>(L, st) : launch_products<false>(L, st); L.count = 0; };
+  auto run = [&] {
+    if (err == cudaSuccess) err = L.p[0].w ? launch_products<true>(L, narrow, st) : launch_products<false>(L, narrow, st);
+    L.count = 0;
+  };
   bool small = true;
   for (int i = 0; i < count; ++i) small = small && Shape(tensors[i]).m <= kSmall;
   L.count = 0;
@@ -1064,7 +1104,7 @@ cudaError_t update_batch(const vgg19_muon_tensor* tensors, const int count, cons
         t.partial = p.partial; t.out = p.out; t.plane = p.plane; t.ld = p.ld;
         t.m = p.m; t.splits = p.splits; t.first_block = finish_blocks;
         finish.alpha = p.alpha;
-        p.sym = 1;
+        if (!p.square) p.square = 2;
         const int b = (p.m + 31) / 32;
         finish_blocks += b * (b + 1) / 2;
       }
@@ -1136,9 +1176,10 @@ cudaError_t update_batch(const vgg19_muon_tensor* tensors, const int count, cons
     for (int i = 0; i < count; ++i) {
       const vgg19_muon_tensor& t = tensors[i];
       const Shape s(t);
+      narrow[L.count] = nullptr;
       Problem& p = L.p[L.count++];
       p = Problem{};
-      p.a = planes[i].k_major[q]; p.b = planes[i].mn_major[x];
+      p.a = planes[i].k_major[q]; p.b = planes[i].box64[x];
       p.b_mn = 1;
       p.m = (int)s.m; p.n = (int)s.n;
       p.k_stages = (int)((s.m + BK - 1) / BK);
