@@ -26,7 +26,7 @@
 //
 // Measured (B200, five steps): the dense layers of a 224 x 224 network (4096 x 25088, 4096 x 4096, 1000 x 4096) in 12.8 ms, of which
 // 0.43 ms momentum, norm and X_0 at 6.9 TB/s; 14.7 TFLOP of fp16 products at 1.19 PFLOP/s, 0.86 of the measured sustained rate
-// under the power cap that bounds them.  The sixteen filters in 0.68 ms: launches of 15 to 25 us, each a chain of latencies (3 us
+// under the power cap that bounds them.  The sixteen filters in 0.66 ms: launches of 15 to 25 us, each a chain of latencies (3 us
 // from one launch to the next, 5 us for the addends beside the stages on an SM's 64 bytes a cycle from L2, 0.8 us a stage, 4 us of stores).
 #include <cuda_fp16.h>
 
@@ -989,6 +989,24 @@ template <int N> int count_tiles(Launch<N>& L, int bn) {
   return tiles;
 }
 
+// The longest that a pair is busy with 256 x bn tiles: with each its stages, and about seven more for what comes before and
+// after them; a half takes about 5/8 of a whole.  (The sums are the same, bit for bit.)  Measured: the sixteen filters
+// 674 -> 657 us against counting tiles alone, with the largest tensors first in both.
+template <int N> long busiest(Launch<N>& L, int bn, int pairs) {
+  constexpr int kMost = 128;
+  const int tiles = count_tiles(L, bn);
+  if (tiles < 0 || pairs > kMost || (bn == 128 && tiles > 16 * pairs)) return 1L << 60;
+  if (tiles > 16 * pairs) return 0;
+  long load[kMost] = {}, most = 0;
+  for (int i = 0; i < L.count; ++i)
+    for (int t = L.first_tile[i]; t < L.first_tile[i + 1]; ++t) {
+      long& l = load[t % pairs];
+      l += (7 + L.p[i].per_split) * (bn == 128 ? 5 : 8);
+      if (l > most) most = l;
+    }
+  return most;
+}
+
 template <bool FINAL, int BN, int N> cudaError_t launch_tiles(const Launch<N>& L, int pairs, cudaStream_t st) {
   const cudaError_t e = cudaFuncSetAttribute(split_product_pair_kernel<N, FINAL, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   if (e != cudaSuccess) return e;
@@ -1001,14 +1019,14 @@ template <bool FINAL, int N> cudaError_t launch_products(Launch<N>& L, const CUt
   int dev = 0, sms = 148;
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  const int pairs = sms / 2, half = count_tiles(L, 128), whole = count_tiles(L, 256);
-  // a round of halves takes about 5/8 of a round of whole tiles.  (The sums are the same, bit for bit.)
-  if (half > 0 && 5 * ((half + pairs - 1) / pairs) < 8 * ((whole + pairs - 1) / pairs)) {
+  const int pairs = sms / 2;
+  if (busiest(L, 128, pairs) < busiest(L, 256, pairs)) {
     count_tiles(L, 128);
     for (int i = 0; i < L.count; ++i)
       if (narrow[i]) L.p[i].b = *narrow[i];
     return launch_tiles<FINAL, 128>(L, pairs, st);
   }
+  count_tiles(L, 256);
   return launch_tiles<FINAL, 256>(L, pairs, st);
 }
 
@@ -1025,7 +1043,14 @@ struct Options {
 
 // The whole update of up to kMaxTensors tensors; N is the largest number of products per launch.
 template <int N>
-cudaError_t update_batch(const vgg19_muon_tensor* tensors, const int count, const Options& o, char* ws, cudaStream_t st) {
+cudaError_t update_batch(const vgg19_muon_tensor* given, const int count, const Options& o, char* ws, cudaStream_t st) {
+  // the largest first: their tiles are the longest, and what is left over at the end of a launch should be short
+  vgg19_muon_tensor tensors[kMaxTensors];
+  for (int i = 0; i < count; ++i) {
+    int at = i;
+    for (; at > 0 && Shape(tensors[at - 1]).m < Shape(given[i]).m; --at) tensors[at] = tensors[at - 1];
+    tensors[at] = given[i];
+  }
   static thread_local Planes planes[kMaxTensors];
   Elements el{};
   el.count = count; el.nesterov = o.nesterov; el.mu = o.mu;
