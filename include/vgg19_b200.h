@@ -382,7 +382,7 @@ int vgg19_logprobs(const void *logits, int32_t dtype, int64_t rows, int32_t clas
  * vgg19_logprobs gave:
  *   d z_j = sum_i g_i [j = ids_i] - p_j (sum_i g_i + w (log p_j + H)).
  * d_logits: device, the type of logits, row stride d_ld; overwritten.  It may be
- * logits itself with d_ld == ld.  d_logprob: fp32 [rows][n_ids].  d_entropy: fp32
+ * logits itself with d_ld == ld; any other overlap is refused.  d_logprob: fp32 [rows][n_ids].  d_entropy: fp32
  * [rows] or NULL (entropy may then be NULL).  Ids that name no class, VGG19_NO_CLASS
  * or others, contribute nothing (others are reported as above); a class named
  * twice gets both shares.  To differentiate the top list, pass its top_id as
@@ -416,7 +416,7 @@ int vgg19_q4_pack(const void *w, int32_t dtype, int32_t out, int32_t in, int64_t
 
 /* y = W x + bias, then ReLU if `relu`: x device [rows][in] with row stride ldx, in
  * `dtype` (VGG19_FP32 or VGG19_BF16); y (or NULL): [rows][out] in that type;
- * y_f32 (or NULL): the same values as fp32; at least one.  bias: fp32 [out] or NULL.  The products are exact and
+ * y_f32 (or NULL): the same values as fp32; at least one, overlapping neither x nor each other.  bias: fp32 [out] or NULL.  The products are exact and
  * summed in fp32 (fp32 activations are taken in full, as three bf16 terms).  Made for up to 16 rows, which read the
  * weights once; more rows are taken 16 at a time.  rows == 0 does nothing. */
 int vgg19_q4_linear(const void *x, int32_t dtype, int64_t rows, int32_t in, int64_t ldx, const void *codes,
@@ -434,7 +434,7 @@ int vgg19_q4_linear(const void *x, int32_t dtype, int64_t rows, int32_t in, int6
  * the rounded result.  grad is only read.  The products carry every fp32 value as two fp16 terms
  * (as VGG19_FLAG_SPLIT_F16 does) and the norm is summed in 64 bits, so any scale of gradient serves.  A zero U leaves X at 0;
  * a NaN or infinity in a tensor's U makes that tensor's W NaN.  The tensors of a call are
- * updated together; they must not overlap.  The smaller side of a tensor is at most 2^15.
+ * updated together; they must not overlap one another or the workspace (only a grad may be given twice).  The smaller side of a tensor is at most 2^15.
  * workspace: device, 256-byte aligned, vgg19_muon_workspace_bytes(tensors, count) bytes (0 for tensors that are
  * refused; only rows and cols are read), scratch for the time of the call: calls that share one have to be ordered.  Asynchronous on `stream`; may be
  * captured.  A bounded wait that runs out inside a kernel is reported by vgg19_ops_status. */

@@ -327,6 +327,9 @@ def vgg19_last_error(net=None):
 # before its address reaches the library.  They run on the tensors' device, whichever is current.  stream as above:
 # None is the legacy default stream.
 
+_MOST = (1 << 31) - 1
+
+
 def _refuse(code, text):
     raise Vgg19Error(code, text)
 
@@ -358,6 +361,10 @@ def _tensor(t, name, dtype, shape, dev):
     _refuse(VGG19_ERR_ARG, f"{name} is on {t.device}, not on cuda:{dev}")
 
 
+def _last(t):
+    return t.shape[-1] if t.dim() else 0  # (what has no dimension is refused for its shape)
+
+
 def _rows_of(t, name):
     """(storage type, rows, columns, row stride, CUDA device index) of a 2-d tensor whose rows are dense."""
     dtype = _torch()[0].get(t.dtype)
@@ -365,10 +372,12 @@ def _rows_of(t, name):
         _refuse(VGG19_ERR_ARG, f"{name} is {t.dtype}, neither float32 nor bfloat16")
     if t.dim() != 2:
         _refuse(VGG19_ERR_SHAPE, f"{name} has {t.dim()} dimensions, not 2")
+    rows, cols = t.shape
+    if cols > _MOST:  # (a C int: beyond it the library would be told another size)
+        _refuse(VGG19_ERR_SHAPE, f"{name} has {cols} columns, at most {_MOST} are possible")
     dev = t.get_device()
     if dev < 0:
         _refuse(VGG19_ERR_ARG, f"{name} is on {t.device}, not on a CUDA device")
-    rows, cols = t.shape
     if t.is_contiguous():
         return dtype, rows, cols, cols, dev
     ld = t.stride(0) if rows > 1 else cols
@@ -395,8 +404,8 @@ def vgg19_logprobs(logits, ids=None, logprob=None, lse=None, entropy=None, top_i
     _, f32, _, i32, _ = _types
     if (ids is None) != (logprob is None) or (top_id is None) != (top_logprob is None):
         _refuse(VGG19_ERR_ARG, "ids goes with logprob, and top_id with top_logprob")
-    n_ids = 0 if ids is None else ids.shape[-1]
-    top_k = 0 if top_id is None else top_id.shape[-1]
+    n_ids = 0 if ids is None else _last(ids)
+    top_k = 0 if top_id is None else _last(top_id)
     given, top, each = (rows, n_ids), (rows, top_k), (rows,)
     return _call(dev, (_lib or load()).vgg19_logprobs, logits.data_ptr(), dtype, rows, classes, ld, _tensor(ids, "ids", i32, given, dev),
                  n_ids, top_k, _tensor(logprob, "logprob", f32, given, dev), _tensor(lse, "lse", f32, each, dev),
@@ -416,7 +425,7 @@ def vgg19_logprobs_backward(logits, ids, lse, entropy, d_logprob, d_entropy, d_l
         _refuse(VGG19_ERR_ARG, "ids goes with d_logprob")
     if lse is None:
         _refuse(VGG19_ERR_ARG, "lse is needed")
-    n_ids = 0 if ids is None else ids.shape[-1]
+    n_ids = 0 if ids is None else _last(ids)
     given, each = (rows, n_ids), (rows,)
     return _call(dev, (_lib or load()).vgg19_logprobs_backward, logits.data_ptr(), dtype, rows, classes, ld,
                  _tensor(ids, "ids", i32, given, dev), n_ids, _tensor(lse, "lse", f32, each, dev),
@@ -434,6 +443,8 @@ def vgg19_q4_scale_bytes(out, in_, group):
 
 def _q4_buffers(codes, scales, out, in_, group, dev):
     lib = _lib or load()
+    if not 0 < out <= _MOST or group not in (32, 64, 128):
+        _refuse(VGG19_ERR_SHAPE if group in (32, 64, 128) else VGG19_ERR_ARG, f"{out} rows in groups of {group}")
     for t, name, need in ((codes, "codes", lib.vgg19_q4_code_bytes(out, in_)), (scales, "scales", lib.vgg19_q4_scale_bytes(out, in_, group))):
         if t.get_device() != dev or not t.is_contiguous():
             _refuse(VGG19_ERR_ARG, f"{name} is on {t.device}, or not contiguous")

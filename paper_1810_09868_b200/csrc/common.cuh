@@ -34,6 +34,19 @@ enum DeviceError : int {
 // Sets the text vgg19_last_error(NULL) gives and returns `code`: for entry points without a handle.
 int note_error(int code, const char* fmt, ...);
 
+// Whether `n` rows of `bytes` each, `pitch` bytes apart, meet m rows of other_bytes, other_pitch apart (pitches at least the rows).
+// Rows of one pitch may lie between one another; otherwise what counts is the range, save that a single row may lie between.
+inline bool rows_meet(const void* a, long n, long bytes, long pitch, const void* b, long m, long other_bytes, long other_pitch) {
+  if (!a || !b || n < 1 || m < 1) return false;
+  if (m == 1) other_pitch = pitch;
+  if (n == 1) pitch = other_pitch;
+  const long x = (long)reinterpret_cast<uintptr_t>(a), y = (long)reinterpret_cast<uintptr_t>(b);
+  if (x + (n - 1) * pitch + bytes <= y || y + (m - 1) * other_pitch + other_bytes <= x) return false;
+  if (pitch != other_pitch || pitch < 1) return true;
+  const long d = ((y - x) % pitch + pitch) % pitch;  // where b's rows start between a's
+  return d < bytes || d + other_bytes > pitch;
+}
+
 // Reads and clears the device-side error words of the operators without a handle (logprobs.cu, q4_dense.cu, muon.cu).
 cudaError_t logprobs_take_error(int* code);
 cudaError_t q4_take_error(int* code);

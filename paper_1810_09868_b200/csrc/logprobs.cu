@@ -556,6 +556,8 @@ int common_checks(const void* logits, int32_t dtype, int64_t rows, int32_t class
     return note_error(VGG19_ERR_ARG, "logits are not aligned to their type");
   return VGG19_OK;
 }
+// whether all of these (null among them) are addresses of 32-bit values
+template <typename... P> bool words(P... p) { return ((reinterpret_cast<uintptr_t>(p) % 4 == 0) && ...); }
 
 }  // namespace
 
@@ -580,6 +582,7 @@ extern "C" int vgg19_logprobs(const void* logits, int32_t dtype, int64_t rows, i
   if (rows == 0) return VGG19_OK;
   if ((n_ids && !logprob) || (top_k && (!top_id || !top_logprob)))
     return note_error(VGG19_ERR_ARG, "null output for %d ids or the top %d", n_ids, top_k);
+  if (!words(ids, logprob, lse, entropy, top_id, top_logprob)) return note_error(VGG19_ERR_ARG, "ids or an output is not aligned to 4 bytes");
   const FwdArgs a{logits, ids, logprob, lse, entropy, top_logprob, top_id, (long)ld, classes, n_ids, top_k};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e = dtype == VGG19_BF16 ? forward<bf16>(a, rows, st) : forward<float>(a, rows, st);
@@ -599,6 +602,10 @@ extern "C" int vgg19_logprobs_backward(const void* logits, int32_t dtype, int64_
     return note_error(VGG19_ERR_ARG, "null lse or d_logits, ids without d_logprob, or d_entropy without entropy");
   if (reinterpret_cast<uintptr_t>(d_logits) % (dtype == VGG19_FP32 ? 4 : 2))
     return note_error(VGG19_ERR_ARG, "d_logits is not aligned to its type");
+  if (!words(ids, lse, entropy, d_logprob, d_entropy)) return note_error(VGG19_ERR_ARG, "ids or an fp32 input is not aligned to 4 bytes");
+  const long elt = dtype == VGG19_FP32 ? 4 : 2;
+  if (!(d_logits == logits && (d_ld == ld || rows == 1)) && rows_meet(logits, rows, classes * elt, ld * elt, d_logits, rows, classes * elt, d_ld * elt))
+    return note_error(VGG19_ERR_ARG, "d_logits overlaps logits without being the same rows");
   const int per = kBwdThreads * kBwdUnroll * (dtype == VGG19_BF16 ? 8 : 4);
   const int64_t chunks = (classes + per - 1) / per;
   if (rows * chunks > 0x7fffffffLL) return note_error(VGG19_ERR_SHAPE, "%lld rows of %d classes are too many", (long long)rows, classes);

@@ -30,6 +30,9 @@
 // from one launch to the next, 5 us for the addends beside the stages on an SM's 64 bytes a cycle from L2, 0.8 us a stage, 4 us of stores).
 #include <cuda_fp16.h>
 
+#include <algorithm>
+#include <vector>
+
 #include "../../include/vgg19_b200.h"
 #include "tc_common.cuh"
 
@@ -1239,6 +1242,42 @@ int check_tensors(const vgg19_muon_tensor* t, int32_t count) {
   return VGG19_OK;
 }
 
+// Blocks read and write in no order, so what is written may overlap nothing: neither another tensor (or the same one
+// twice), nor the workspace.  Gradients are only read.
+int check_overlaps(const vgg19_muon_tensor* t, int32_t count, const void* workspace, size_t bytes) {
+  struct Range {
+    uintptr_t begin, end;
+    bool written;
+  };
+  try {
+    std::vector<Range> r;
+    r.reserve(4 * (size_t)count + 1);
+    auto add = [&r](const void* p, size_t n, bool written) {
+      const uintptr_t b = reinterpret_cast<uintptr_t>(p);
+      if (p) r.push_back(Range{b, b + n, written});
+    };
+    add(workspace, bytes, true);
+    for (int i = 0; i < count; ++i) {
+      const size_t n = (size_t)(t[i].rows * t[i].cols);
+      add(t[i].w, 4 * n, true);
+      add(t[i].w_bf16, 2 * n, true);
+      add(t[i].momentum, 4 * n, true);
+      add(t[i].grad, 4 * n, false);
+    }
+    std::sort(r.begin(), r.end(), [](const Range& a, const Range& b) { return a.begin < b.begin; });
+    uintptr_t end = 0, written_end = 0;  // of what began before
+    for (const Range& x : r) {
+      if (x.begin < written_end || (x.written && x.begin < end))
+        return note_error(VGG19_ERR_ARG, "a weight, its copy, a momentum or the workspace overlaps another tensor of the call");
+      if (x.end > end) end = x.end;
+      if (x.written && x.end > written_end) written_end = x.end;
+    }
+  } catch (...) {
+    return note_error(VGG19_ERR_ARG, "no host memory for the list of %d tensors", count);
+  }
+  return VGG19_OK;
+}
+
 size_t workspace_bytes(const vgg19_muon_tensor* t, int32_t count) {
   size_t most = 256;
   for (int i = 0; i < count; i += kMaxTensors) {
@@ -1299,6 +1338,8 @@ extern "C" int vgg19_muon_update(const vgg19_muon_tensor* tensors, int32_t count
     return note_error(VGG19_ERR_WORKSPACE, "the workspace is null or not 256-byte aligned");
   if (bytes < workspace_bytes(tensors, count))
     return note_error(VGG19_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu", bytes, workspace_bytes(tensors, count));
+  const int apart = check_overlaps(tensors, count, workspace, workspace_bytes(tensors, count));
+  if (apart != VGG19_OK) return apart;
   const Options o{lr, momentum, decay, steps, nesterov != 0};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   for (int i = 0; i < count; i += kMaxTensors) {

@@ -505,6 +505,10 @@ int vgg19_q4_linear(const void* x, int32_t dtype, int64_t rows, int32_t in, int6
   if (reinterpret_cast<uintptr_t>(x) % elt || reinterpret_cast<uintptr_t>(y) % elt || reinterpret_cast<uintptr_t>(y_f32) % 4 ||
       reinterpret_cast<uintptr_t>(bias) % 4 || reinterpret_cast<uintptr_t>(codes) % 16 || reinterpret_cast<uintptr_t>(scales) % 16)
     return note_error(VGG19_ERR_ARG, "x, bias and outputs are aligned to their types, codes and scales to 16 bytes");
+  const long x_bytes = (long)elt * in, x_pitch = (long)elt * ldx, y_bytes = (long)elt * out * rows, f_bytes = 4L * out * rows;
+  if (rows_meet(x, rows, x_bytes, x_pitch, y, 1, y_bytes, 0) || rows_meet(x, rows, x_bytes, x_pitch, y_f32, 1, f_bytes, 0) ||
+      rows_meet(y, 1, y_bytes, 0, y_f32, 1, f_bytes, 0))
+    return note_error(VGG19_ERR_ARG, "an output overlaps x or the other output");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e =
       dtype == VGG19_BF16

@@ -783,11 +783,11 @@ extern "C" {
 
 int vgg19_ops_status(void *stream) {
   cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
-  int code = 0;
-  int timeout = 0;
+  int code = 0, timeout = 0, later = 0;
   if (e == cudaSuccess) e = logprobs_take_error(&code);
   if (e == cudaSuccess) e = q4_take_error(&timeout);
-  if (e == cudaSuccess && !timeout) e = muon_take_error(&timeout);
+  if (e == cudaSuccess) e = muon_take_error(&later);
+  if (!timeout) timeout = later;
   if (e != cudaSuccess) return fail(nullptr, VGG19_ERR_CUDA, "reading the device status failed: %s", cudaGetErrorString(e));
   if (timeout) return fail(nullptr, VGG19_ERR_DEVICE_TIMEOUT, "a device-side wait ran out (code %d)", timeout);
   if (code) return fail(nullptr, VGG19_ERR_ARG, "an id outside the row's classes (its log probability is NaN)");

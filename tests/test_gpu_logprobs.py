@@ -391,3 +391,22 @@ def test_the_network_names_its_best_classes(p):
     assert np.array_equal(ids.cpu().numpy(), want["top_id"].numpy())
     assert close(lp, want["top_logprob"], (1000 / 128 + 48 + 3 * want["top_logprob"].abs()) * U)
     net.close()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_gradient_beside_the_logits(p, dtype):
+    """Logits and their gradient as the two halves of the same rows: nothing overlaps."""
+    n = 1003
+    src, ids = make(9, n, dtype, seed=4)
+    both = torch.full((9, 2 * n + 1), float("nan"), dtype=src.dtype, device=DEV)
+    z, beside = both[:, 1:n + 1], both[:, n + 1:]
+    z.copy_(src)
+    g, w = upstream(9, 3)
+    o = call(p, z, ids, 1)
+    d = torch.empty(9, n, dtype=z.dtype, device=DEV)
+    p.vgg19_logprobs_backward(z, ids, o["lse"], o["entropy"], g, w, d, torch.cuda.current_stream())
+    p.vgg19_logprobs_backward(z, ids, o["lse"], o["entropy"], g, w, beside, torch.cuda.current_stream())
+    assert torch.equal(beside, d) and torch.equal(z, src) and torch.isnan(both[:, 0]).all()
+    with pytest.raises(p.Vgg19Error) as e:
+        p.vgg19_logprobs_backward(z, ids, o["lse"], o["entropy"], g, w, both[:, :n], torch.cuda.current_stream())
+    assert e.value.code == p.VGG19_ERR_ARG

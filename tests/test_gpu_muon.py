@@ -275,3 +275,58 @@ def test_network_step(p, dtype_name):
     with pytest.raises(p.Vgg19Error):
         net.muon_step(grads, momentum[:-1], 0.02)
     net.close(), again.close()
+
+
+def test_elements_beyond_32_bits(p):
+    """130 x 2^24: the last row's end is beyond 2^31 elements.  Columns without gradient take no part, so the first and the last
+    thousand are those of the matrix that has only them, and what lies between decays."""
+    rows, cols, k = 130, 1 << 24, 1000
+    small = tensors(rows, 2 * k, seed=4)
+    before = copies(small)
+    wide = (torch.ones(rows, cols, device=DEV), torch.ones(rows, cols, device=DEV, dtype=torch.bfloat16), torch.zeros(rows, cols, device=DEV),
+            torch.zeros(rows, cols, device=DEV))
+    for a, b in zip(wide, small):
+        a[:, :k], a[:, -k:] = b[:, :k], b[:, k:]
+    run(p, [wide], lr=0.02, decay=0.01)
+    got = tuple(torch.cat([a[:, :k], a[:, -k:]], 1) for a in wide)
+    check(got, before, 0.02, 0.95, 0.01, 5, True)
+    decayed = torch.tensor(1 - 0.02 * 0.01, device=DEV)
+    for c0 in range(k, cols - k, 1 << 20):
+        between = wide[0][:, c0:min(c0 + (1 << 20), cols - k)]
+        assert (between - decayed).abs().max() <= 2 * U
+    assert not wide[3][:, k:-k].any()
+
+
+def test_one_gradient_for_two_matrices(p):
+    t = tensors(90, 200, seed=6)
+    other = copies(t)[:2] + (t[2], copies(t)[3])
+    before = copies(t)
+    run(p, [t, other])
+    check(t, before, 0.02, 0.95, 0.01, 5, True)
+    assert torch.equal(t[0], other[0]) and torch.equal(t[3], other[3])
+    for bad in ([t, t], [t, other[:3] + (t[3],)], [(t[0], None, t[0], t[3])]):
+        with pytest.raises(p.Vgg19Error) as e:
+            run(p, bad)
+        assert e.value.code == p.VGG19_ERR_ARG
+
+
+def test_two_recorded_graphs_share_a_workspace(p):
+    """Replayed in turn on one stream, as the documentation asks."""
+    ts = [tensors(150, 400, seed=8), tensors(300, 64, seed=9)]
+    want = [copies(t) for t in ts]
+    tables = [p.vgg19_muon_tensors([t]) for t in ts]
+    ws = torch.empty(max(p.vgg19_muon_workspace_bytes(t) for t in tables), dtype=torch.uint8, device=DEV)
+    st = torch.cuda.Stream()
+    graphs = []
+    for table in tables:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            p.vgg19_muon_update(table, 0.02, 0.95, 0.01, 5, True, ws, stream=st)
+        graphs.append(graph)
+    for _ in range(3):
+        for graph, w in zip(graphs, want):
+            graph.replay()
+            run(p, [w])
+    torch.cuda.synchronize()
+    for t, w in zip(ts, want):
+        assert torch.equal(t[0], w[0]) and torch.equal(t[3], w[3])

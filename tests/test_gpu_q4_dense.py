@@ -314,3 +314,21 @@ def test_dense_layer_entry_point(p):
     want, size = x.double().cpu() @ w.T + b, x.double().cpu().abs() @ w.abs().T + b.abs()
     assert within(y, want, size, k)
     net.close()
+
+
+def test_codes_beyond_32_bits(p):
+    """The last rows' codes start more than 2^32 bytes after the first."""
+    out, in_, group, rows = 65600, 1 << 17, 128, 2
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    codes = torch.randint(0, 256, (p.vgg19_q4_code_bytes(out, in_),), generator=gen, dtype=torch.uint8, device=DEV)
+    assert codes.numel() > 1 << 32
+    scales = (torch.rand(p.vgg19_q4_scale_bytes(out, in_, group) // 2, generator=gen, device=DEV) * 0.01).to(torch.bfloat16)
+    x = inputs(rows, in_, "bf16", seed=2)
+    y = torch.full((rows, out), float("nan"), dtype=torch.float32, device=DEV)
+    p.vgg19_q4_linear(x, codes, scales, out, group, None, False, None, y, torch.cuda.current_stream())
+    for first in (0, out // 2 // 16 * 16, out - 32):
+        c = codes.view(out // 16, -1)[first // 16:first // 16 + 2].reshape(-1)
+        s = scales.view(out // 16, -1)[first // 16:first // 16 + 2].reshape(-1)
+        want, size = reference(x, c, s, 32, group, None, False)
+        assert within(y[:, first:first + 32], want, size, in_)
+    assert not torch.isnan(y).any()

@@ -123,3 +123,64 @@ def test_muon_sizes(p):
     assert lib.vgg19_muon_update(None, 0, 0.1, 0.9, 0.0, 5, 1, None, 0, None) == p.VGG19_OK
     assert lib.vgg19_muon_step(None, None, None, 0.1, 0.9, 0.0, 0.1, 5, 1, None, 0, None) == p.VGG19_ERR_ARG
     assert lib.vgg19_muon_step_bytes(None) == 0
+
+
+@pytest.mark.parametrize("where", ["ids", "logprob", "lse", "entropy", "top_id", "top_logprob"])
+def test_logprobs_refuses_unaligned_words(p, where):
+    assert p.binding.load().vgg19_logprobs(*logprobs_args(**{where: SOME + 2})) == p.VGG19_ERR_ARG
+
+
+def backward_args(**over):
+    a = dict(logits=SOME, dtype=0, rows=3, classes=10, ld=24, ids=SOME, n_ids=1, lse=SOME, entropy=SOME, d_logprob=SOME,
+             d_entropy=SOME, d_logits=SOME, d_ld=24, stream=None)
+    a.update(over)
+    return a.values()
+
+
+@pytest.mark.parametrize("where", ["ids", "lse", "entropy", "d_logprob", "d_entropy"])
+def test_logprobs_backward_refuses_unaligned_words(p, where):
+    assert p.binding.load().vgg19_logprobs_backward(*backward_args(**{where: SOME + 2})) == p.VGG19_ERR_ARG
+
+
+# Gradients over other logits than their own: shifted within the row, rows of another stride, one row further.
+@pytest.mark.parametrize("over", [
+    dict(d_logits=SOME + 4), dict(d_logits=SOME - 4), dict(d_ld=25), dict(d_ld=10), dict(d_logits=SOME + 4 * 24), dict(d_logits=SOME + 4 * 9),
+    dict(d_logits=SOME + 4 * 15), dict(rows=1, d_logits=SOME + 4 * 9), dict(d_logits=SOME + 4 * 57, d_ld=30)])
+def test_logprobs_backward_refuses_overlaps(p, over):
+    assert p.binding.load().vgg19_logprobs_backward(*backward_args(**over)) == p.VGG19_ERR_ARG
+    assert "overlap" in p.vgg19_last_error()
+
+
+@pytest.mark.parametrize("over", [
+    dict(y=SOME), dict(y=SOME + 2 * 99), dict(y=SOME - 2 * 19), dict(y_f32=SOME + 2 * 200), dict(y=SOME + 2 * 101), dict(y=SOME + 4 * 1000, y_f32=SOME + 4 * 1000),
+    dict(rows=1, y=SOME + 2 * 99)])
+def test_q4_linear_refuses_overlaps(p, over):
+    a = dict(x=SOME, dtype=1, rows=2, in_=100, ldx=116, codes=SOME, scales=SOME, out=10, group=32, bias=SOME, relu=0, y=None,
+             y_f32=None, stream=None)
+    a.update(over)
+    assert p.binding.load().vgg19_q4_linear(*a.values()) == p.VGG19_ERR_ARG
+    assert "overlap" in p.vgg19_last_error()
+
+
+# 30 x 50 matrices: 6000 bytes of fp32, 3000 of bf16; places are multiples of 8000 but for what each case changes.
+@pytest.mark.parametrize("change", [
+    {(0, "w"): 5}, {(0, "w_bf16"): 0.5}, {(1, "grad"): 0}, {(0, "grad"): 3}, {(1, "momentum"): 3}, {(1, "w_bf16"): 1}, {(1, "grad"): 5.9 / 8}, {(0, "w"): 9},
+    {(0, "momentum"): 7.7}])
+def test_muon_update_refuses_overlaps(p, change):
+    t = (p.binding.vgg19_muon_tensor * 2)()
+    for i in range(2):
+        t[i].rows, t[i].cols = 30, 50
+        for k, name in enumerate(("w", "w_bf16", "grad", "momentum")):
+            setattr(t[i], name, SOME + int(8000 * change.get((i, name), 4 * i + k)))
+    lib = p.binding.load()
+    ws = SOME + 9 * 8000 // 256 * 256
+    rc = lib.vgg19_muon_update(t, 2, 0.1, 0.9, 0.0, 5, 1, ws if (0, "w") in change else 1 << 30, 1 << 40, None)
+    assert rc == p.VGG19_ERR_ARG and "overlap" in p.vgg19_last_error()
+
+
+def test_the_binding_refuses_sizes_beyond_an_int(p):
+    wide = torch.empty(1, (1 << 32) + 5, device="meta")
+    for call in (lambda: p.vgg19_logprobs(wide), lambda: p.vgg19_q4_pack(wide, 64, None, None), lambda: p.vgg19_muon_tensors([(wide, None, wide, wide)])):
+        with pytest.raises(p.Vgg19Error) as e:
+            call()
+        assert e.value.code == p.VGG19_ERR_SHAPE
