@@ -44,12 +44,17 @@ class Net:
         binding.vgg19_forward(self.handle, images, B, logits, probs, stream)
         return logits
 
+    def _allocating_for(self, stream):
+        """What is allocated meanwhile belongs to `stream`: a torch stream, or its address."""
+        torch = self._torch
+        return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self.device) if isinstance(stream, int) else stream)
+
     def classify(self, images, top_k=5, stream=None):
         """The top_k classes of every image, most probable first: (ids int32, log probabilities fp32), [batch][top_k]."""
         torch = self._torch
         stream = stream or torch.cuda.current_stream(self.device)
         B = images.shape[0]
-        with torch.cuda.device(self.device), torch.cuda.stream(stream):
+        with torch.cuda.device(self.device), self._allocating_for(stream):
             logits = self.forward(images, stream=stream)
             ids = torch.empty(B, top_k, dtype=torch.int32, device=self.device)
             logprob = torch.empty(B, top_k, dtype=torch.float32, device=self.device)
@@ -78,12 +83,12 @@ class Net:
         for name, t in (("grads", grads), ("momentum_buffer", momentum_buffer)):
             if t.dtype != torch.float32 or t.device != self.workspace.device or not t.is_contiguous() or t.numel() != self.n_params:
                 raise binding.Vgg19Error(binding.VGG19_ERR_ARG, f"{name}: {self.n_params} dense float32 values on {self.device} are needed")
-        if getattr(self, "muon_workspace", None) is None:
-            self.muon_workspace = torch.empty(binding.vgg19_muon_step_bytes(self.handle), dtype=torch.uint8, device=self.device)
-        with torch.cuda.device(self.device):
+        stream = stream or torch.cuda.current_stream(self.device)
+        with torch.cuda.device(self.device), self._allocating_for(stream):  # (memory that this stream may write to)
+            if getattr(self, "muon_workspace", None) is None:
+                self.muon_workspace = torch.empty(binding.vgg19_muon_step_bytes(self.handle), dtype=torch.uint8, device=self.device)
             binding.vgg19_muon_step(self.handle, grads, momentum_buffer, lr, momentum, decay, lr if bias_lr is None else bias_lr, steps,
-                                    nesterov, self.muon_workspace, self.muon_workspace.numel(),
-                                    stream or torch.cuda.current_stream(self.device))
+                                    nesterov, self.muon_workspace, self.muon_workspace.numel(), stream)
 
     def train_step(self, images, labels, lr, loss=None, stream=None):
         """Forward + backward + update as one recorded device program (workspace of VGG19_MODE_TRAIN)."""

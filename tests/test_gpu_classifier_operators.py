@@ -157,3 +157,19 @@ def test_two_streams_at_once(p):
     for a, b in zip(alone, both):
         for k in ("lse", "ent", "tid", "tlp", "codes", "scales", "y", "w", "m"):
             assert torch.equal(a[k], b[k]), k
+
+
+def test_a_network_on_a_stream_given_by_its_address(p):
+    net = p.Net(32, 32, 2, p.VGG19_BF16, seed=1, mode=p.VGG19_MODE_BACKWARD)
+    images = torch.rand(2, 32, 32, 3, device=DEV).to(torch.bfloat16)
+    grads, momentum = torch.full((net.n_params,), 1e-3, device=DEV), torch.zeros(net.n_params, device=DEV)
+    before = net.classify(images)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    ids, logprob = net.classify(images, stream=st.cuda_stream)
+    st.synchronize()
+    assert torch.equal(ids, before[0]) and torch.equal(logprob, before[1])
+    net.muon_step(grads, momentum, 0.01, stream=st.cuda_stream)
+    st.synchronize()
+    assert not torch.equal(net.classify(images)[1], logprob)
+    net.close()
