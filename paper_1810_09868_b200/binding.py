@@ -325,7 +325,28 @@ def vgg19_last_error(net=None):
 # ---- operators without a handle -------------------------------------------------------------------------------
 # They take torch CUDA tensors and read sizes, strides and types from them; a tensor that does not fit is refused here,
 # before its address reaches the library.  They run on the tensors' device, whichever is current.  stream as above:
-# None is the legacy default stream.
+# None is the legacy default stream.  The ones a program calls once per answer go through _tensor_calls first
+# (csrc/tensor_calls.cpp), which makes the same checks in a tenth of the time and answers None where one of them fails.
+
+_tensor_calls = None
+
+
+def _calls():
+    global _tensor_calls
+    if _tensor_calls is None:
+        load()
+        import torch  # noqa: F401  (its libraries come first)
+        try:
+            from . import _tensor_calls as module
+        except ImportError as e:
+            raise RuntimeError("_tensor_calls is missing or of another torch: build it with `python -c 'import __graft_entry__ as g; g.build()'`") from e
+        _tensor_calls = module
+    return _tensor_calls
+
+
+def _answered(rc):
+    return rc if rc == VGG19_OK else _check(None, rc)
+
 
 _MOST = (1 << 31) - 1
 
@@ -400,6 +421,9 @@ def _call(dev, fn, *args):
 def vgg19_logprobs(logits, ids=None, logprob=None, lse=None, entropy=None, top_id=None, top_logprob=None, stream=None):
     """logits [rows][classes] (a row stride is allowed), ids and logprob [rows][n_ids], lse and entropy [rows], top_id and
     top_logprob [rows][top_k]; what is None is left out."""
+    rc = (_tensor_calls or _calls()).logprobs(logits, ids, logprob, lse, entropy, top_id, top_logprob, stream)
+    if rc is not None:
+        return _answered(rc)
     dtype, rows, classes, ld, dev = _rows_of(logits, "logits")
     _, f32, _, i32, _ = _types
     if (ids is None) != (logprob is None) or (top_id is None) != (top_logprob is None):
@@ -416,6 +440,9 @@ def vgg19_logprobs(logits, ids=None, logprob=None, lse=None, entropy=None, top_i
 def vgg19_logprobs_backward(logits, ids, lse, entropy, d_logprob, d_entropy, d_logits, stream=None):
     """The gradient at the logits; ids and d_logprob may be None together, and so may d_entropy (entropy then too).
     d_logits may be logits."""
+    rc = (_tensor_calls or _calls()).logprobs_backward(logits, ids, lse, entropy, d_logprob, d_entropy, d_logits, stream)
+    if rc is not None:
+        return _answered(rc)
     dtype, rows, classes, ld, dev = _rows_of(logits, "logits")
     d_dtype, d_rows, d_classes, d_ld, d_dev = _rows_of(d_logits, "d_logits")
     if (d_dtype, d_rows, d_classes, d_dev) != (dtype, rows, classes, dev):
@@ -462,6 +489,9 @@ def vgg19_q4_pack(w, group, codes, scales, stream=None):
 
 def vgg19_q4_linear(x, codes, scales, out, group, bias=None, relu=False, y=None, y_f32=None, stream=None):
     """x [rows][in] (a row stride is allowed); y [rows][out] in x's type and / or y_f32 in fp32."""
+    rc = (_tensor_calls or _calls()).q4_linear(x, codes, scales, out, group, bias, relu, y, y_f32, stream)
+    if rc is not None:
+        return _answered(rc)
     dtype, rows, in_, ldx, dev = _rows_of(x, "x")
     f32 = _types[1]
     lib = _q4_buffers(codes, scales, out, in_, group, dev)

@@ -9,6 +9,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libvgg19_b200.so")
+CALLS, CALLS_SOURCE = os.path.join(PKG, "_tensor_calls.so"), os.path.join(CSRC, "tensor_calls.cpp")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared", "--threads", "0"]
@@ -32,4 +33,25 @@ def build(force: bool = False, verbose: bool = False) -> str:
         nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
         cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB] + sources()
         subprocess.run(cmd, check=True)
+    build_calls(force)
     return LIB
+
+
+def build_calls(force: bool = False) -> str:
+    """Compile csrc/tensor_calls.cpp, which reads torch tensors, against the installed torch's headers."""
+    deps = (CALLS_SOURCE, os.path.join(ROOT, "include", "vgg19_b200.h"))
+    if force or not os.path.exists(CALLS) or any(os.path.getmtime(d) > os.path.getmtime(CALLS) for d in deps):
+        import sysconfig
+
+        import torch
+        where = os.path.dirname(torch.__file__)
+        cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+        include = (os.path.join(where, "include"), os.path.join(where, "include", "torch", "csrc", "api", "include"),
+                   os.path.join(cuda, "include"), sysconfig.get_paths()["include"])
+        cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+        for i in include:
+            cmd += ["-isystem", i]
+        cmd += ["-o", CALLS, CALLS_SOURCE, "-L" + os.path.join(where, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda",
+                "-L" + PKG, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"]
+        subprocess.run(cmd, check=True)
+    return CALLS

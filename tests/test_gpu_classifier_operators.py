@@ -173,3 +173,37 @@ def test_a_network_on_a_stream_given_by_its_address(p):
     st.synchronize()
     assert not torch.equal(net.classify(images)[1], logprob)
     net.close()
+
+
+class _Unanswered:
+    """Stands for the compiled calls, answering none of them."""
+
+    def __getattr__(self, name):
+        return lambda *a: None
+
+
+def test_the_binding_without_its_compiled_calls_gives_the_same(p, monkeypatch):
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    z = torch.randn(5, 700, generator=gen, device=DEV)[:, :603]
+    ids = torch.randint(0, 603, (5, 2), generator=gen, device=DEV, dtype=torch.int32)
+    codes = torch.randint(0, 256, (p.vgg19_q4_code_bytes(33, 603),), generator=gen, dtype=torch.uint8, device=DEV)
+    scales = torch.rand(p.vgg19_q4_scale_bytes(33, 603, 64) // 2, generator=gen, device=DEV).to(torch.bfloat16)
+    g, w, bias = torch.randn(5, 2, generator=gen, device=DEV), torch.randn(5, generator=gen, device=DEV), torch.randn(33, generator=gen, device=DEV)
+
+    def all_calls(stream):
+        o = dict(logprob=torch.empty(5, 2, device=DEV), lse=torch.empty(5, device=DEV), entropy=torch.empty(5, device=DEV),
+                 top_id=torch.empty(5, 4, dtype=torch.int32, device=DEV), top_logprob=torch.empty(5, 4, device=DEV))
+        d, y, yf = torch.empty(5, 603, device=DEV), torch.empty(5, 33, device=DEV), torch.empty(5, 33, device=DEV)
+        assert p.vgg19_logprobs(z, ids, stream=stream, **o) == p.VGG19_OK
+        assert p.vgg19_logprobs_backward(z, ids, o["lse"], o["entropy"], g, w, d, stream) == p.VGG19_OK
+        assert p.vgg19_q4_linear(z, codes, scales, 33, 64, bias, True, y, yf, stream) == p.VGG19_OK
+        torch.cuda.synchronize()
+        return [*o.values(), d, y, yf]
+
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    want = [all_calls(s) for s in (torch.cuda.current_stream(), st, st.cuda_stream, None)]
+    monkeypatch.setattr(p.binding, "_tensor_calls", _Unanswered())
+    for other in want[1:] + [all_calls(st), all_calls(st.cuda_stream), all_calls(None)]:
+        for a, b in zip(want[0], other):
+            assert torch.equal(a, b)
