@@ -14,9 +14,9 @@
 // their logits again and sort those that do, as 64-bit keys (value, then lower index).  Keeping a sorted list during
 // the pass instead took twice the time for the best 8 of 50021.
 //
-// A row belongs to one block, or, where there are fewer rows than the GPU has room for, to a cluster of up to
-// eight blocks that join through distributed shared memory: one launch, no scratch, and an order of summation that
-// depends on the sizes alone.
+// A short row (up to 1024 classes) belongs to one warp, a longer one to one block, or, where there are fewer rows than the
+// GPU has room for, to a cluster of up to eight blocks that join through distributed shared memory: one launch, no
+// scratch, and an order of summation that depends on the sizes alone.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
@@ -504,6 +504,130 @@ __global__ void __launch_bounds__(kBwdThreads) logprobs_backward_kernel(const Bw
   }
 }
 
+// ---- short rows ------------------------------------------------------------------------------------------------
+// A warp per row, its logits in registers (element e of a lane is class lane + 32 e): no thread waits for another warp, and
+// no pass is repeated for the top list, which is taken one class after another from the lanes' best.
+// Measured against the blocks above (B200): 2048 rows of 250, bf16, the best 32: 9.4 against 60 us, none: 2.5 against 6.3, gradient 2.8
+// against 5.6; one row of 1000, fp32, the best 5: 3.6 against 4.2, the best 32: 10 against 6.4; 100 rows' gradient at 1000: 3.4
+// against 2.0, 2048 rows': 4.0 against 5.6.
+constexpr int kShortWarps = 4;
+bool short_forward_wins(int classes, int top_k) { return classes <= 512 || (classes <= 1024 && top_k <= 8); }
+bool short_backward_wins(int classes, long rows) { return classes <= 256 || (classes <= 1024 && rows >= 512); }
+
+template <typename T, int P>
+__global__ void __launch_bounds__(32 * kShortWarps) short_rows_kernel(const FwdArgs a, long rows) {
+  const int lane = threadIdx.x & 31, n = a.classes;
+  const long row = (long)blockIdx.x * kShortWarps + threadIdx.x / 32;
+  if (row >= rows) return;
+  const T* z = static_cast<const T*>(a.logits) + row * a.ld;
+  float x[P];
+#pragma unroll
+  for (int e = 0; e < P; ++e) x[e] = lane + 32 * e < n ? to_f32(z[lane + 32 * e]) : -INFINITY;
+  float ref = x[0];
+#pragma unroll
+  for (int e = 1; e < P; ++e) ref = fmaxf(ref, x[e]);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, o));  // (passes over NaN: S will be one)
+  const float r = ref == -INFINITY ? 0.f : ref;
+  float S = 0.f, U = 0.f;
+#pragma unroll
+  for (int e = 0; e < P; ++e) {
+    const float d = max_nan((x[e] - r) * kLog2e, kFloor), p = fast_exp2(d);
+    S += p;
+    U = fmaf(p, d, U);
+  }
+  S = lane_sum(S);
+  U = lane_sum(U);
+  const bool bad = !(S == S) || ref == INFINITY, empty = !bad && ref == -INFINITY;
+  const float nan = __int_as_float(0x7fc00000), logS = logf(S);
+  if (lane == 0) {
+    if (a.lse) a.lse[row] = bad ? nan : empty ? -INFINITY : ref + logS;
+    if (a.entropy) a.entropy[row] = bad ? nan : empty ? 0.f : fmaxf(logS - kLn2 * (U / S), 0.f);
+  }
+  for (int i = lane; i < a.n_ids; i += 32) {
+    const int id = a.ids[row * a.n_ids + i];
+    float v = 0.f;
+    if (id != VGG19_NO_CLASS) {
+      if ((unsigned)id < (unsigned)n) {
+        v = bad ? nan : empty ? -INFINITY : (to_f32(z[id]) - ref) - logS;
+      } else {  // never used as an index
+        v = nan;
+        atomicCAS(&g_logprobs_error, 0, (int)kDevBadLabel);
+      }
+    }
+    a.logprob[row * a.n_ids + i] = v;
+  }
+  if (!a.top_k) return;
+  unsigned left[P], mine = 0;  // what the lane has not given yet, and the largest of it (the first among equals)
+  int at = 0;
+#pragma unroll
+  for (int e = 0; e < P; ++e) left[e] = ordered(x[e]);
+  auto look = [&] {
+    mine = left[0];
+    at = 0;
+#pragma unroll
+    for (int e = 1; e < P; ++e)
+      if (left[e] > mine) { mine = left[e]; at = e; }
+  };
+  look();
+  unsigned value = 0;
+  int id = VGG19_NO_CLASS;  // of place `lane` in the list
+  for (int k = 0; k < a.top_k && !bad; ++k) {
+    const unsigned most = __reduce_max_sync(0xffffffffu, mine);
+    if (most < kLowest) break;  // excluded classes only
+    const unsigned index = mine == most ? lane + 32 * at : 0xffffffffu, first = __reduce_min_sync(0xffffffffu, index);
+    if (lane == k) { value = most; id = (int)first; }
+    if (index == first) {
+#pragma unroll
+      for (int e = 0; e < P; ++e)
+        if (e == at) left[e] = 0;
+      look();
+    }
+  }
+  if (lane < a.top_k) {
+    a.top_id[row * a.top_k + lane] = id;
+    a.top_logprob[row * a.top_k + lane] = bad ? nan : id != VGG19_NO_CLASS ? (value_of(value) - ref) - logS : -INFINITY;
+  }
+}
+
+template <typename T, int P>
+__global__ void __launch_bounds__(32 * kShortWarps) short_rows_backward_kernel(const BwdArgs a, long rows) {
+  const int lane = threadIdx.x & 31, n = a.classes;
+  const long row = (long)blockIdx.x * kShortWarps + threadIdx.x / 32;
+  if (row >= rows) return;
+  const T* z = static_cast<const T*>(a.logits) + row * a.ld;
+  T* dz = static_cast<T*>(a.d_logits) + row * a.d_ld;
+  float x[P], given[P];
+#pragma unroll
+  for (int e = 0; e < P; ++e) {
+    x[e] = lane + 32 * e < n ? to_f32(z[lane + 32 * e]) : 0.f;
+    given[e] = 0.f;
+  }
+  float sum = 0.f;
+  for (int i = 0; i < a.n_ids; i += 32) {  // in their order
+    const int id = i + lane < a.n_ids ? a.ids[row * a.n_ids + i + lane] : VGG19_NO_CLASS;
+    const bool in = (unsigned)id < (unsigned)n;
+    if (!in && id != VGG19_NO_CLASS) atomicCAS(&g_logprobs_error, 0, (int)kDevBadLabel);
+    const float g = in ? a.d_logprob[row * a.n_ids + i + lane] : 0.f;
+    sum += lane_sum(g);
+    for (unsigned m = __ballot_sync(0xffffffffu, in); m; m &= m - 1) {
+      const int l = __ffs(m) - 1, d = __shfl_sync(0xffffffffu, id, l) - lane;
+      const float v = __shfl_sync(0xffffffffu, g, l);
+#pragma unroll
+      for (int e = 0; e < P; ++e) given[e] += d == 32 * e ? v : 0.f;
+    }
+  }
+  const float lse = a.lse[row], w = a.d_entropy ? a.d_entropy[row] : 0.f;
+  const float c = sum + (a.d_entropy ? w * a.entropy[row] : 0.f);
+  const bool empty = lse == -INFINITY;  // a row with no class left has no gradient
+#pragma unroll
+  for (int e = 0; e < P; ++e)
+    if (lane + 32 * e < n) {
+      const float lp = max_nan(x[e] - lse, kFloor);
+      dz[lane + 32 * e] = from_f32<T>(empty ? 0.f : fmaf(fast_exp2(lp * kLog2e), fmaf(-w, lp, -c), given[e]));
+    }
+}
+
 // How many blocks share a row: enough to give every SM two blocks while each still has a few thousand classes.
 int cluster_size(long rows, int classes) {
   int c = 1;
@@ -529,13 +653,34 @@ template <typename T, int NT, int UNROLL> cudaError_t launch_forward(const FwdAr
   return cudaLaunchKernelEx(&cfg, logprobs_kernel<T, NT, UNROLL>, a);
 }
 
+template <typename T, int P> cudaError_t short_forward(const FwdArgs& a, long rows, cudaStream_t st) {
+  short_rows_kernel<T, P><<<(unsigned)((rows + kShortWarps - 1) / kShortWarps), 32 * kShortWarps, 0, st>>>(a, rows);
+  return cudaGetLastError();
+}
+template <typename T, int P> cudaError_t short_backward(const BwdArgs& a, long rows, cudaStream_t st) {
+  short_rows_backward_kernel<T, P><<<(unsigned)((rows + kShortWarps - 1) / kShortWarps), 32 * kShortWarps, 0, st>>>(a, rows);
+  return cudaGetLastError();
+}
+
 template <typename T> cudaError_t forward(const FwdArgs& a, long rows, cudaStream_t st) {
+  if (short_forward_wins(a.classes, a.top_k)) {
+    if (a.classes <= 64) return short_forward<T, 2>(a, rows, st);
+    if (a.classes <= 256) return short_forward<T, 8>(a, rows, st);
+    if (a.classes <= 512) return short_forward<T, 16>(a, rows, st);
+    return short_forward<T, 32>(a, rows, st);
+  }
   const int C = cluster_size(rows, a.classes), per = a.classes / C;
   if (per <= 2048) return launch_forward<T, 128, 4>(a, rows, C, st);
   return launch_forward<T, 256, 4>(a, rows, C, st);
 }
 
 template <typename T> cudaError_t backward(const BwdArgs& a, long rows, cudaStream_t st) {
+  if (short_backward_wins(a.classes, rows)) {
+    if (a.classes <= 64) return short_backward<T, 2>(a, rows, st);
+    if (a.classes <= 256) return short_backward<T, 8>(a, rows, st);
+    if (a.classes <= 512) return short_backward<T, 16>(a, rows, st);
+    return short_backward<T, 32>(a, rows, st);
+  }
   const unsigned blocks = (unsigned)(rows * a.chunks);
   if (a.n_ids > 32) logprobs_backward_kernel<T, true><<<blocks, kBwdThreads, 0, st>>>(a);
   else logprobs_backward_kernel<T, false><<<blocks, kBwdThreads, 0, st>>>(a);

@@ -410,3 +410,81 @@ def test_gradient_beside_the_logits(p, dtype):
     with pytest.raises(p.Vgg19Error) as e:
         p.vgg19_logprobs_backward(z, ids, o["lse"], o["entropy"], g, w, both[:, :n], torch.cuda.current_stream())
     assert e.value.code == p.VGG19_ERR_ARG
+
+
+# Rows that belong to one warp (see the kernels): a lane adds n / 32 terms, five joins follow; n / 32 + 5 <= n / 128 + 32 up to 1024.
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,n,top", [(1, 1, 1), (601, 3, 2), (5, 32, 32), (130, 33, 7), (2, 64, 32), (600, 65, 32), (3, 255, 9), (40, 256, 32),
+                                        (2, 257, 32), (700, 512, 32), (6, 513, 8), (6, 513, 9), (513, 1000, 3), (7, 1023, 0), (600, 1024, 8), (3, 1024, 32),
+                                        (2, 1025, 8)])
+def test_short_rows(p, rows, n, top, dtype):
+    z, ids = make(rows, n, dtype, seed=rows + n, ld=n + rows % 3, offset=n % 5)
+    if rows > 2:
+        z[1] = -math.inf                                   # nothing left
+        z[2, : n // 2] = torch.finfo(z.dtype).min
+        z[rows - 1, ::3] = z[rows - 1, 0].clone()          # ties
+        ids[0, 1] = p.VGG19_NO_CLASS
+    want, logp = reference(z, ids, top)
+    o = call(p, z, ids, top)
+    check(o, want, n)
+    g, w = upstream(rows, 3)
+    d = torch.empty(rows, n, dtype=z.dtype, device=DEV)
+    lse, h = want["lse"].float().to(DEV), want["entropy"].float().to(DEV)
+    p.vgg19_logprobs_backward(z, ids, lse, h, g, w, d, torch.cuda.current_stream())
+    check_gradient(d, z, ids, logp, want["entropy"], want["lse"], g, w)
+    p.vgg19_logprobs_backward(z, ids, lse, h, g, w, z, torch.cuda.current_stream())  # in place
+    assert torch.equal(z, d)
+
+
+@pytest.mark.parametrize("n", [20, 300, 800])
+@pytest.mark.parametrize("n_ids", [33, 256])
+def test_short_rows_many_ids(p, n, n_ids):
+    rows = 512
+    z, _ = make(rows, n, "fp32", seed=n)
+    gen = torch.Generator(device=DEV).manual_seed(n_ids)
+    ids = torch.randint(0, n, (rows, n_ids), generator=gen, device=DEV, dtype=torch.int32)
+    ids[:, 5] = ids[:, 40 % n_ids]
+    want, logp = reference(z, ids, 1)
+    check(call(p, z, ids, 1), want, n)
+    g, w = upstream(rows, n_ids)
+    d, again = torch.empty_like(z), torch.empty_like(z)
+    lse, h = want["lse"].float().to(DEV), want["entropy"].float().to(DEV)
+    p.vgg19_logprobs_backward(z, ids, lse, h, g, w, d, torch.cuda.current_stream())
+    ids64, g64, w64 = ids.long().cpu(), g.double().cpu(), w.double().cpu()[:, None]
+    pr, h64 = logp.exp(), want["entropy"][:, None]
+    given, shares = torch.zeros_like(logp).scatter_add_(1, ids64, g64), torch.zeros_like(logp).scatter_add_(1, ids64, g64.abs())
+    exact = given - pr * (g64.sum(1, keepdim=True) + w64 * (logp + h64))
+    size = pr * (g64.abs().sum(1, keepdim=True) + w64.abs() * (logp.abs() + h64))
+    # as above: the sum over n_ids shares is n_ids more roundings of their total size
+    slack = n_ids * U * (g64.abs().sum(1, keepdim=True) * pr + shares)
+    assert close(d, exact, slack + U * size * (3 * logp.abs() + 2 * want["lse"].abs()[:, None] + 32) + 4 * U * given.abs())
+    p.vgg19_logprobs_backward(z, ids, lse, h, g, w, again, torch.cuda.current_stream())
+    assert torch.equal(d, again)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,at", [(7, 6), (64, 40), (250, 249), (500, 3), (1000, 500)])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_short_rows_with_a_nan_or_infinity(p, n, at, value, dtype):
+    z, ids = make(6, n, dtype)
+    clean = call(p, z, ids, 4)
+    z[3, at] = value
+    o = call(p, z, ids, 4)
+    for k in ("lse", "entropy", "top_logprob", "logprob"):
+        assert torch.isnan(o[k][3]).all()
+        assert torch.equal(o[k][:3], clean[k][:3]) and torch.equal(o[k][4:], clean[k][4:])
+    assert (o["top_id"][3] == p.VGG19_NO_CLASS).all()
+    bad = ids.clone()
+    bad[0, 0], bad[4, 2] = n, -2
+    o = call(p, z, bad, 4)
+    assert torch.isnan(o["logprob"][0, 0]) and torch.isnan(o["logprob"][4, 2]) and torch.equal(o["logprob"][1:3], clean["logprob"][1:3])
+    with pytest.raises(p.Vgg19Error) as e:
+        p.vgg19_ops_status(torch.cuda.current_stream())
+    assert e.value.code == p.VGG19_ERR_ARG
+    g, w = upstream(6, 3)
+    d = torch.empty_like(z)
+    p.vgg19_logprobs_backward(z, bad, o["lse"], o["entropy"], g, w, d, torch.cuda.current_stream())
+    assert torch.isnan(d[3]).all() and not torch.isnan(d[:3]).any() and not torch.isnan(d[4:]).any()
+    with pytest.raises(p.Vgg19Error):
+        p.vgg19_ops_status(torch.cuda.current_stream())
