@@ -13,9 +13,15 @@
 // (g, t) of a warp finds with two 16-byte loads what its fragments need: row g (and g + 8), and in each of the four
 // 32-weight groups the eight weights 8 t .. 8 t + 7.  All 16 weights of one instruction's K then lie in one group.
 //
-// A block owns RW tiles of 16 output rows over a share of K, one a warp or one for two warps that take turns.  Every warp has its own ring of bulk copies
-// (eight blocks on their way, no registers held, no other warp waited for); the block's share of x is staged in
-// shared memory meanwhile, once for all its rows.  The shares of a cluster join through distributed shared memory, in a fixed order: one launch, no scratch.
+// A block owns RW tiles of 16 output rows over a share of K, one a warp or one for two warps that take turns.  Every warp
+// has its own ring of bulk copies (four or eight blocks on their way, no registers held, no other warp waited for); the
+// block's share of x is staged in shared memory meanwhile, once for all its rows.  The shares of a cluster join through
+// distributed shared memory, in a fixed order: one launch, no scratch.
+//
+// Measured (B200, device time): 25088 -> 4096 in groups of 128, one row, bf16: 18.6 us, 2.8 TB/s, bound by unpacking (76
+// integer instructions a KB on a pipe of half rate); sixteen rows, groups of 64: 32 us; 4096 -> 4096, sixteen rows, groups of
+// 32: 8.2 us, 2.4 of them until x is staged, 2.3 products, 2.2 joining; 6344 -> 11710, ten rows of fp32: 36 us, where the
+// tensor cores (three terms, two tiles of rows: 48 products a KB at 8 cycles) are busy a third of the time.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
@@ -33,7 +39,6 @@ static __device__ int g_q4_error;  // a DeviceError code once a bounded wait ran
 
 constexpr int kTileRows = 16, kBlockK = 128, kBlockBytes = kTileRows * kBlockK / 2;
 constexpr int kMaxRows = 16;                 // rows of x per launch
-constexpr int kStageBytes = 48 << 10;        // of x in shared memory at a time (with the static part below 48 KB)
 constexpr int kMaxKSplit = 8;
 
 // Two codes, four nibbles apart, become a pair of bf16 values (code - 8) / 16: 0x4100 | code is 8 + code / 16.  (Sixteenths,
@@ -107,15 +112,15 @@ __device__ __forceinline__ uint4 load_now(const uint4* p) {
   return v;
 }
 
-constexpr int kSlotBlocks = 4, kRing = 2;  // blocks a copy, copies on their way
-template <int PER> __host__ __device__ constexpr int slot_bytes() { return kSlotBlocks * (kBlockBytes + kTileRows * PER * 2); }
+constexpr int kRing = 2;  // copies on their way
+template <int PER, int SLOT> __host__ __device__ constexpr int slot_bytes() { return SLOT * (kBlockBytes + kTileRows * PER * 2); }
 
 template <int WARPS> constexpr int kPerSm = 24 / WARPS;  // resident blocks that registers are kept for
 
-// NT: tiles of eight rows of x.  GROUP: 32, 64 or 128 weights a scale.  RW x KW warps: row tiles, warps to a tile.
-template <typename T, int GROUP, int NT, int RW, int KW>
+// NT: tiles of eight rows of x.  GROUP: 32, 64 or 128 weights a scale.  RW x KW warps: row tiles, warps to a tile.  SLOT: blocks a copy.
+template <typename T, int GROUP, int NT, int RW, int KW, int SLOT>
 __global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 : kPerSm<RW * KW>) q4_linear_kernel(const Q4Args a) {
-  constexpr int TERMS = Terms<T>::N, PER = kBlockK / GROUP, USTEP = GROUP / 32, kThreads = 32 * RW * KW, STEP = KW * kSlotBlocks;
+  constexpr int TERMS = Terms<T>::N, PER = kBlockK / GROUP, USTEP = GROUP / 32, kThreads = 32 * RW * KW, STEP = KW * SLOT;
   extern __shared__ __align__(128) unsigned char smem[];  // the rings, then x
   __shared__ float part[KW][RW][NT * 8][kTileRows];
   __shared__ float inbox[RW * NT * 8 * kTileRows + kMaxKSplit];
@@ -128,19 +133,19 @@ __global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 
   const int b0 = (int)((long)a.blocks * rank / ks), b1 = (int)((long)a.blocks * (rank + 1) / ks);
   const unsigned char* codes = reinterpret_cast<const unsigned char*>(a.codes) + (long)tile * a.blocks * kBlockBytes;
   const unsigned char* scales = reinterpret_cast<const unsigned char*>(a.scales) + (long)tile * a.blocks * (kTileRows * PER * 2);
-  const unsigned char* ring = smem + warp * kRing * slot_bytes<PER>();
+  const unsigned char* ring = smem + warp * kRing * slot_bytes<PER, SLOT>();
   const uint32_t ring_u32 = smem_u32(ring), bar_u32 = smem_u32(&bars[warp][0]);
-  unsigned char* staged = smem + RW * KW * kRing * slot_bytes<PER>();
+  unsigned char* staged = smem + RW * KW * kRing * slot_bytes<PER, SLOT>();
   const int stride = a.stage_blocks * kBlockK * 2 + 64;  // bytes of a staged row: rows 64 bytes apart modulo 128
   const int term_bytes = a.rows * stride;
 
-  const int first = b0 + warp / RW * kSlotBlocks;  // this warp's blocks: a slot's, then those STEP further
+  const int first = b0 + warp / RW * SLOT;  // this warp's blocks: a slot's, then those STEP further
   auto request = [&](int slot, int b) {  // lane 0: a slot's blocks of this warp's tile, from b
-    const int n = min(kSlotBlocks, b1 - b);
-    const uint32_t bar = bar_u32 + 8 * slot, dst = ring_u32 + slot * slot_bytes<PER>();
+    const int n = min(SLOT, b1 - b);
+    const uint32_t bar = bar_u32 + 8 * slot, dst = ring_u32 + slot * slot_bytes<PER, SLOT>();
     mbar_expect_tx(bar, n * (kBlockBytes + kTileRows * PER * 2));
     bulk_copy(dst, codes + (long)b * kBlockBytes, n * kBlockBytes, bar);
-    bulk_copy(dst + kSlotBlocks * kBlockBytes, scales + (long)b * (kTileRows * PER * 2), n * (kTileRows * PER * 2), bar);
+    bulk_copy(dst + SLOT * kBlockBytes, scales + (long)b * (kTileRows * PER * 2), n * (kTileRows * PER * 2), bar);
   };
   if (ks > 1) cluster.barrier_arrive();  // waited for before the first write into another block's shared memory
   if (tid == 0) abort_flag = 0;
@@ -237,7 +242,7 @@ __global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 
       }
     }
     __syncthreads();
-    for (int b = c0 + warp / RW * kSlotBlocks; b < c1; b += STEP) {  // (a part of x is a multiple of STEP, but for the last)
+    for (int b = c0 + warp / RW * SLOT; b < c1; b += STEP) {  // (a part of x is a multiple of STEP, but for the last)
       if (!ok) break;
       ok = __all_sync(0xffffffffu, mbar_wait(bar_u32 + 8 * slot, phase, &abort_flag, &g_q4_error, kDevTimeoutTmaFull));
       if (!ok) {  // let what is on its way land before shared memory goes away
@@ -250,10 +255,10 @@ __global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 
         }
         break;
       }
-      const unsigned char* w = ring + slot * slot_bytes<PER>();
-      const unsigned char *sc = w + kSlotBlocks * kBlockBytes, *xb = staged + (b - c0) * (kBlockK * 2);
+      const unsigned char* w = ring + slot * slot_bytes<PER, SLOT>();
+      const unsigned char *sc = w + SLOT * kBlockBytes, *xb = staged + (b - c0) * (kBlockK * 2);
 #pragma unroll
-      for (int u = 0; u < kSlotBlocks; ++u)
+      for (int u = 0; u < SLOT; ++u)
         if (b + u < c1) multiply(w + u * kBlockBytes, sc + u * (kTileRows * PER * 2), xb + u * (kBlockK * 2));
       __syncwarp();
       if (lane == 0 && b + kRing * STEP < b1) request(slot, b + kRing * STEP);
@@ -337,59 +342,81 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const T* w, long ld, int o
   if (lane % (group / 4) == 0) scales[(block * kTileRows + row % kTileRows) * (kBlockK / group) + lane / (group / 4)] = sb;
 }
 
-template <typename T, int GROUP, int NT, int RW, int KW> cudaError_t launch(Q4Args a, cudaStream_t st) {
-  constexpr int PER = kBlockK / GROUP, kRings = RW * KW * kRing * slot_bytes<PER>(), kStatic = RW * (KW + 1) * NT * 8 * kTileRows * 4 + 512;
-  constexpr int STEP = KW * kSlotBlocks;
-  static_assert((KW == 1 ? kMaxRows * 3 : 2) * STEP * kBlockK * 2 <= kStageBytes, "a step's part of x fits");
-  const int groups = ((a.out + kTileRows - 1) / kTileRows + RW - 1) / RW, block_bytes = a.rows * Terms<T>::N * kBlockK * 2;
-  auto stage_for = [&](int share) {  // blocks of x staged at a time: whole steps
-    const int most = kStageBytes / block_bytes / STEP * STEP;
-    const int want = (share + STEP - 1) / STEP * STEP;
-    return want < most ? want : most;
-  };
-  auto smem_for = [&](int stage) { return kRings + a.rows * Terms<T>::N * (stage * kBlockK * 2 + 64); };
+// A launch's shape, and an estimate of its time.
+struct Plan {
+  int ksplit, stage_blocks;
+  size_t smem;
+  double cost;
+};
+
+template <typename T, int GROUP, int NT, int RW, int KW, int SLOT> struct Shape {
+  static constexpr int PER = kBlockK / GROUP, kRings = RW * KW * kRing * slot_bytes<PER, SLOT>(), STEP = KW * SLOT;
+  static constexpr int kStatic = RW * (KW + 1) * NT * 8 * kTileRows * 4 + 512, kStage = SLOT == 4 ? 48 << 10 : 40 << 10;  // of x in shared memory at a time
+  static_assert((KW == 1 ? kMaxRows * 3 : 2) * STEP * kBlockK * 2 <= kStage, "a step's part of x fits");
+
   // How many blocks share K.  A block of weights keeps a warp about twenty times as long as it keeps the SM's issue slots,
   // so an SM wants that many warps, and more only bring start-ups (three blocks' worth): the least estimated time wins.
-  int best = 1;
-  long least = 0;
-  for (int ks = 1; ks <= kMaxKSplit && ks <= a.blocks; ++ks) {
-    const long n = (long)groups * ks, share = (a.blocks + ks - 1) / ks, per = (share + KW - 1) / KW;
-    long resident = (220 << 10) / (smem_for(stage_for((int)share)) + kStatic + 1024);
-    if (resident > 24 / (RW * KW)) resident = 24 / (RW * KW);
-    const long each = (n + 147) / 148, rounds = (each + resident - 1) / resident, warps = (each < resident ? each : resident) * RW * KW;
-    const long cost = rounds * (per + 3) * (warps > 20 ? warps : 20);
-    if (ks == 1 || cost < least) { best = ks; least = cost; }
+  static Plan plan(const Q4Args& a) {
+    const int groups = ((a.out + kTileRows - 1) / kTileRows + RW - 1) / RW, block_bytes = a.rows * Terms<T>::N * kBlockK * 2;
+    Plan best{};
+    for (int ks = 1; ks <= kMaxKSplit && ks <= a.blocks; ++ks) {
+      const int share = (a.blocks + ks - 1) / ks, most = kStage / block_bytes / STEP * STEP, want = (share + STEP - 1) / STEP * STEP;
+      const int stage = want < most ? want : most;
+      const size_t smem = kRings + a.rows * Terms<T>::N * (stage * kBlockK * 2 + 64);
+      const long n = (long)groups * ks, per = (share + KW - 1) / KW;
+      long resident = (220 << 10) / (smem + kStatic + 1024);
+      if (resident > 24 / (RW * KW)) resident = 24 / (RW * KW);
+      const long sms = ks > 2 ? 141 : 148, each = (n + sms - 1) / sms;  // (a cluster stays within a part of the GPU, and some of a part's SMs stay empty)
+      const long rounds = (each + resident - 1) / resident, warps = (each < resident ? each : resident) * RW * KW;
+      const double cost = rounds * (per + 3) * (warps > 20 ? warps : 20) * (SLOT == 4 ? 1.0 : 1.1);
+      if (best.ksplit == 0 || cost < best.cost) best = Plan{ks, stage, smem, cost};
+    }
+    return best;
   }
-  a.ksplit = best;
-  a.stage_blocks = stage_for((a.blocks + best - 1) / best);
-  const size_t smem = smem_for(a.stage_blocks);
-  auto kernel = q4_linear_kernel<T, GROUP, NT, RW, KW>;
-  if (smem + kStatic > (48 << 10)) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRings + kStageBytes + kMaxRows * 3 * 64);
-    if (e != cudaSuccess) return e;
+
+  static cudaError_t launch(Q4Args a, const Plan& p, cudaStream_t st) {
+    const int groups = ((a.out + kTileRows - 1) / kTileRows + RW - 1) / RW;
+    a.ksplit = p.ksplit;
+    a.stage_blocks = p.stage_blocks;
+    auto kernel = q4_linear_kernel<T, GROUP, NT, RW, KW, SLOT>;
+    if (p.smem + kStatic > (48 << 10)) {
+      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRings + kStage + kMaxRows * 3 * 64);
+      if (e != cudaSuccess) return e;
+    }
+    if (a.ksplit == 1) {
+      kernel<<<(unsigned)groups, 32 * RW * KW, p.smem, st>>>(a);
+      return cudaGetLastError();
+    }
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(groups * a.ksplit));
+    cfg.blockDim = dim3(32 * RW * KW);
+    cfg.dynamicSmemBytes = p.smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = (unsigned)a.ksplit;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
   }
-  if (a.ksplit == 1) {
-    kernel<<<(unsigned)groups, 32 * RW * KW, smem, st>>>(a);
-    return cudaGetLastError();
-  }
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(groups * a.ksplit));
-  cfg.blockDim = dim3(32 * RW * KW);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute at{};
-  at.id = cudaLaunchAttributeClusterDimension;
-  at.val.clusterDim.x = (unsigned)a.ksplit;
-  at.val.clusterDim.y = at.val.clusterDim.z = 1;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, a);
+};
+
+// Copies of four blocks, whose products fill one another's gaps, or of two, a tenth slower, which leave shared memory for a
+// second block per SM where x takes much of it: 4096 -> 4096 at sixteen rows takes 8.2 against 8.4 us, 6344 -> 11710 at
+// ten rows of fp32 69 against 36.
+template <typename T, int GROUP, int NT, int RW> cudaError_t launch_rows(const Q4Args& a, cudaStream_t st) {
+  using Long = Shape<T, GROUP, NT, RW, 1, 4>;
+  using Short = Shape<T, GROUP, NT, RW, 1, 2>;
+  const Plan l = Long::plan(a), s = Short::plan(a);
+  return l.cost <= s.cost ? Long::launch(a, l, st) : Short::launch(a, s, st);
 }
 
 template <typename T, int GROUP> cudaError_t launch_group(const Q4Args& a, cudaStream_t st) {
-  if (a.rows > 8) return launch<T, GROUP, 2, 8, 1>(a, st);
-  if (a.rows * Terms<T>::N > 2) return launch<T, GROUP, 1, 8, 1>(a, st);
-  return launch<T, GROUP, 1, 4, 2>(a, st);
+  if (a.rows > 8) return launch_rows<T, GROUP, 2, 8>(a, st);
+  if (a.rows * Terms<T>::N > 2) return launch_rows<T, GROUP, 1, 8>(a, st);
+  using One = Shape<T, GROUP, 1, 4, 2, 4>;
+  return One::launch(a, One::plan(a), st);
 }
 
 template <typename T> cudaError_t launch_type(const Q4Args& a, int group, cudaStream_t st) {

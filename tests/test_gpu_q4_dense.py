@@ -332,3 +332,20 @@ def test_codes_beyond_32_bits(p):
         want, size = reference(x, c, s, 32, group, None, False)
         assert within(y[:, first:first + 32], want, size, in_)
     assert not torch.isnan(y).any()
+
+
+# Sizes at which x takes much of a block's shared memory, and few rows of weights over a long K.
+@pytest.mark.parametrize("rows,out,in_,group,dtype", [(10, 2700, 6344, 64, "fp32"), (16, 2500, 3001, 32, "bf16"), (12, 7067, 1299, 128, "bf16"), (16, 4700, 2050, 128, "fp32"),
+                                                      (15, 117, 9279, 32, "fp32"), (2, 3097, 4050, 64, "bf16"), (7, 1500, 4100, 32, "fp32")])
+def test_larger_sizes_for_several_rows(p, rows, out, in_, group, dtype):
+    codes, scales = buffers(p, out, in_, group)
+    st = torch.cuda.current_stream()
+    p.vgg19_q4_pack(weights(out, in_, seed=3), group, codes, scales, st)
+    x = inputs(rows, in_, dtype, seed=rows, ld=in_ + in_ % 3)
+    yf = torch.full((rows, out), float("nan"), dtype=torch.float32, device=DEV)
+    p.vgg19_q4_linear(x, codes, scales, out, group, None, False, None, yf, st)
+    want, size = reference(x, codes, scales, out, group, None, False)
+    assert within(yf, want, size, in_)
+    again = torch.empty_like(yf)
+    p.vgg19_q4_linear(x, codes, scales, out, group, None, False, None, again, st)
+    assert torch.equal(again, yf)
