@@ -17,6 +17,10 @@
 // A short row (up to 1024 classes) belongs to one warp, a longer one to one block, or, where there are fewer rows than the
 // GPU has room for, to a cluster of up to eight blocks that join through distributed shared memory: one launch, no
 // scratch, and an order of summation that depends on the sizes alone.
+//
+// Measured (B200, device time): 2048 rows of 50021 fp32 with the best 8 in 80 us, 5.1 TB/s (0.80 of a copy's rate; without a
+// top list 66 us, 0.97); 4096 rows of 32003 bf16 forward in 54 us and the gradient in 83 us (4.9 and 6.3 TB/s); one row of
+// 131072 bf16 with the best 20 in 8.2 us, of 1000 fp32 with the best 5 in 3.4 us, all latency.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
@@ -306,13 +310,33 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(const FwdArgs a) {
     const float thr = value_of(lo);
     Best b;
     unsigned hot = __ballot_sync(0xffffffffu, mine >= lo);
-    while (hot) {  // the lanes share the vectors of each thread whose maximum reaches the bound
-      const int t = warp * 32 + __ffs(hot) - 1;
-      hot &= hot - 1;
-      for (int v = v0 + t; v < v1; v += 32 * NT) {
-        const int u = v + lane * NT;
+    // The lanes share the vectors of each thread whose maximum reaches the bound, one thread after another, or, where a thread
+    // has few, several at once: `share` lanes to a thread's.  (700 rows of 1467, the best 31: 13.5 -> 9.5 us; with many vectors
+    // a thread the first loop is the faster one, 61 against 67 us for 2048 rows of 50021.)
+    const int each = (v1 - v0 + NT - 1) / NT;
+    if (each > 16) {
+      while (hot) {
+        const int t = warp * 32 + __ffs(hot) - 1;
+        hot &= hot - 1;
+        for (int v = v0 + t; v < v1; v += 32 * NT) {
+          const int u = v + lane * NT;
+          float x[V];
+          Vec<T>::unpack(u < v1 ? __ldg(body + u) : none, x);
+          const int first = sp.head + u * V;
+          b.add(x, thr, [first](int e) { return (unsigned)(first + e); });
+        }
+      }
+    } else {
+      const int share = each > 8 ? 16 : each > 4 ? 8 : 4;
+      while (hot) {
+        unsigned m = hot;  // without the threads of the lanes before these
+        for (int j = 0; j < 32 / share; ++j) {
+          if (j < lane / share) m &= m - 1;
+          hot &= hot - 1;
+        }
+        const int k = lane % share, u = v0 + warp * 32 + __ffs(m) - 1 + k * NT;  // (m may be 0)
         float x[V];
-        Vec<T>::unpack(u < v1 ? __ldg(body + u) : none, x);
+        Vec<T>::unpack(m && k < each && u < v1 ? __ldg(body + u) : none, x);
         const int first = sp.head + u * V;
         b.add(x, thr, [first](int e) { return (unsigned)(first + e); });
       }
