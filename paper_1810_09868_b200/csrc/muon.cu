@@ -89,7 +89,7 @@ __device__ __forceinline__ void behind_previous() {
 struct __align__(64) Problem {
   CUtensorMap a, b;
   int m, n, k_stages, tiles_m, tiles_n;
-  int sym;         // tiles on and above the diagonal only, stored twice (or mirrored by gram_finish_kernel)
+  int sym;         // tiles on and above the diagonal only; what lies above it is stored twice (or mirrored by gram_finish_kernel)
   int square;      // for the host: 1 always so, 2 so with square tiles, else all tiles
   int splits, per_split;  // K is cut into that many parts, of that many stages
   int b_mn;
@@ -118,13 +118,16 @@ template <int N> struct Launch {
 struct Tile {
   int i, j, split, k0, k1;  // in tiles; the part of K and its stages
 };
-__device__ __forceinline__ Tile find_tile(const Problem& p, int t) {
+// Of a symmetric result, the tiles that reach the diagonal or lie above it: in row i of tiles those from column (256 / BN) i on.
+// (Halves there too: 1500 x 1500 689 -> 541 us.)
+template <int BN> __device__ __forceinline__ Tile find_tile(const Problem& p, int t) {
+  constexpr int WIDE = 2 * BM / BN;  // tiles of columns to a tile of rows
   Tile r{};
   if (p.splits > 1) { r.split = t % p.splits; t /= p.splits; }
   if (p.sym) {
-    int left = p.tiles_m;
-    while (t >= left) { t -= left; --left; ++r.i; }
-    r.j = r.i + t;
+    int left = p.tiles_n;
+    while (t >= left) { t -= left; left -= WIDE; ++r.i; }
+    r.j = WIDE * r.i + t;
   } else {
     r.j = t / p.tiles_m;  // row tiles fastest: they share the wide operand's columns
     r.i = t - r.j * p.tiles_m;
@@ -259,7 +262,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
       for (int w = pair; w < total && ok; w += n_pairs) {
         while (w >= L.first_tile[pi + 1]) ++pi;
         const Problem& p = L.p[pi];
-        const Tile tile = find_tile(p, w - L.first_tile[pi]);
+        const Tile tile = find_tile<BN>(p, w - L.first_tile[pi]);
         const int row = (2 * tile.i + (int)rank) * BM, col = tile.j * BN + (int)rank * (BN / 2), mn = p.b_mn;
         for (int kb = tile.k0; kb < tile.k1; ++kb) {
           if (!mbar_wait(empty_bar(stage), phase ^ 1, &abort_flag, &g_muon_error, kDevTimeoutStageFree)) { ok = false; break; }
@@ -304,7 +307,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
         while (w >= L.first_tile[pi + 1]) ++pi;
         const Problem& p = L.p[pi];
         const bool mn = p.b_mn != 0;
-        const Tile tile = find_tile(p, w - L.first_tile[pi]);
+        const Tile tile = find_tile<BN>(p, w - L.first_tile[pi]);
         const int k_stages = tile.k1 - tile.k0, chain = chain_stages<FINAL>(k_stages);
         const uint32_t idesc = umma_idesc_f16(2 * BM, BN, 0, mn);
         // K-major: lo behind all rows of hi, 16 k = 32 bytes of the swizzled row.  MN-major: two groups of 64 columns, each
@@ -357,7 +360,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
     for (int w = pair; w < total && ok; w += n_pairs) {
       while (w >= L.first_tile[pi + 1]) ++pi;
       const Problem& p = L.p[pi];
-      const Tile tile = find_tile(p, w - L.first_tile[pi]);
+      const Tile tile = find_tile<BN>(p, w - L.first_tile[pi]);
       const int i0 = (2 * tile.i + (int)rank) * BM + quarter * 32, j0 = tile.j * BN + group * CW;  // the warp's first row and column
       const int rows = p.m - i0, cols = p.n - j0;                                           // what there is from there on
       const int k_stages = tile.k1 - tile.k0, chain = chain_stages<FINAL>(k_stages);
@@ -428,7 +431,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
             for (int e = 0; e < 8; ++e) v[e] = alpha * sum[c0 + 8 * k + e];
             split8(v, hi[k], lo[k]);
           }
-          if (p.sym && tile.i != tile.j && lane < rows) {  // the mirror image, lanes along a row
+          if (p.sym && tile.j / (2 * BM / BN) != tile.i && lane < rows) {  // the mirror image, lanes along a row
             half16* at = p.out + (j0 + c0) * ld + i0 + lane;
 #pragma unroll
             for (int j = 0; j < 64; ++j)
@@ -913,11 +916,13 @@ struct Shape {
   size_t x_bytes() const { return up((size_t)2 * m * ldn * 2, 256); }
   size_t a_bytes() const { return up((size_t)2 * m * ldm * 2, 256); }
   // A Gram matrix of at most 1024 rows has few tiles and may have a long K, which is then cut into parts of about 16 stages
-  // (one 512 x 4608 filter's takes 85 us uncut).  By the tensor alone, so that no result depends on what else is updated.
+  // (one 512 x 4608 filter's takes 85 us uncut); a larger one into as many as leave every pair of SMs a tile.  By the
+  // tensor alone, so that no result depends on what else is updated.
   int gram_stages() const { return (int)((n + BK - 1) / BK); }
   int gram_splits() const {
-    const int parts = (gram_stages() + 15) / 16;
-    return m > 1024 || parts < 2 ? 1 : parts < 8 ? parts : 8;
+    const long i = (m + 2 * BM - 1) / (2 * BM), j = (m + BM - 1) / BM, halves = i * j - i * (i - 1);  // tiles of 128 columns from the diagonal on
+    const long most = m <= 1024 ? 8 : 74 / halves, parts = (gram_stages() + 15) / 16;
+    return (int)(most < 2 || parts < 2 ? 1 : parts < most ? parts : most);
   }
   size_t partial_bytes() const { return gram_splits() > 1 ? up((size_t)gram_splits() * m * ldm * 4, 256) : 0; }
   long norm_blocks() const { return (m * n + kNormChunk - 1) / kNormChunk; }
@@ -975,18 +980,18 @@ template <typename P> cudaError_t launch_behind(void (*kernel)(P), unsigned bloc
   return cudaLaunchKernelEx(&cfg, kernel, params);
 }
 
-// The launch's tiles of 256 x bn; -1 where a problem takes square tiles only (a triangle of them).
+// The launch's tiles of 256 x bn.
 template <int N> int count_tiles(Launch<N>& L, int bn) {
   int tiles = 0;
+  const int wide = 2 * BM / bn;
   for (int i = 0; i < L.count; ++i) {
     Problem& p = L.p[i];
     if (p.splits < 1) { p.splits = 1; p.per_split = p.k_stages; }
     p.tiles_m = (p.m + 2 * BM - 1) / (2 * BM);
     p.tiles_n = (p.n + bn - 1) / bn;
     p.sym = p.square == 1 || (p.square == 2 && bn == 2 * BM);
-    if (p.sym && bn != 2 * BM) return -1;
     L.first_tile[i] = tiles;
-    tiles += p.splits * (p.sym ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n);
+    tiles += p.splits * (p.tiles_m * p.tiles_n - (p.sym ? wide * (p.tiles_m * (p.tiles_m - 1) / 2) : 0));
   }
   L.first_tile[L.count] = tiles;
   return tiles;
@@ -998,7 +1003,7 @@ template <int N> int count_tiles(Launch<N>& L, int bn) {
 template <int N> long busiest(Launch<N>& L, int bn, int pairs) {
   constexpr int kMost = 128;
   const int tiles = count_tiles(L, bn);
-  if (tiles < 0 || pairs > kMost || (bn == 128 && tiles > 16 * pairs)) return 1L << 60;
+  if (pairs > kMost || (bn == 128 && tiles > 16 * pairs)) return 1L << 60;
   if (tiles > 16 * pairs) return 0;
   long load[kMost] = {}, most = 0;
   for (int i = 0; i < L.count; ++i)

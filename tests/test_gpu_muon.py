@@ -330,3 +330,22 @@ def test_two_recorded_graphs_share_a_workspace(p):
     torch.cuda.synchronize()
     for t, w in zip(ts, want):
         assert torch.equal(t[0], w[0]) and torch.equal(t[3], w[3])
+
+
+@pytest.mark.parametrize("rows,cols", [(1025, 1025), (1100, 1300), (1290, 3000), (2048, 2048), (1700, 1410)])
+def test_symmetric_products_of_many_tiles(p, rows, cols):
+    t = tensors(rows, cols, seed=rows)
+    before = copies(t)
+    run(p, [t])
+    check(t, before, 0.02, 0.95, 0.01, 5, True)
+
+
+def test_many_tiles_alone_and_together(p):
+    """Alone the tiles are halves, together whole ones: the same, bit for bit."""
+    ts = [tensors(1100 + 90 * i, 1500, seed=i) for i in range(5)]
+    before = [copies(t) for t in ts]
+    run(p, ts)
+    for k in (0, 3):
+        alone = copies(before[k])
+        run(p, [alone], fill=0)
+        assert torch.equal(alone[0], ts[k][0])
