@@ -207,3 +207,45 @@ def test_the_binding_without_its_compiled_calls_gives_the_same(p, monkeypatch):
     for other in want[1:] + [all_calls(st), all_calls(st.cuda_stream), all_calls(None)]:
         for a, b in zip(want[0], other):
             assert torch.equal(a, b)
+
+
+def test_two_host_threads(p):
+    """Each with its own stream, buffers and refusals; what they get is what one alone gets."""
+    import threading
+
+    def job(seed, stream, out):
+        gen = torch.Generator(device=DEV).manual_seed(seed)
+        rows, n = 40 + seed, 900 + 300 * seed
+        with torch.cuda.stream(stream):
+            z = torch.randn(rows, n, generator=gen, device=DEV)
+            lse, top = torch.empty(rows, device=DEV), (torch.empty(rows, 6, dtype=torch.int32, device=DEV), torch.empty(rows, 6, device=DEV))
+            codes = torch.randint(0, 256, (p.vgg19_q4_code_bytes(100 * seed, n),), generator=gen, dtype=torch.uint8, device=DEV)
+            scales = torch.rand(p.vgg19_q4_scale_bytes(100 * seed, n, 64) // 2, generator=gen, device=DEV).to(torch.bfloat16)
+            y = torch.empty(rows, 100 * seed, device=DEV)
+            w, g, m = (torch.randn(70 * seed, 210, generator=gen, device=DEV) for _ in range(3))
+            table = p.vgg19_muon_tensors([(w, None, g, m)])
+            ws = torch.empty(p.vgg19_muon_workspace_bytes(table), dtype=torch.uint8, device=DEV)
+            for _ in range(20):
+                p.vgg19_logprobs(z, lse=lse, top_id=top[0], top_logprob=top[1], stream=stream)
+                p.vgg19_q4_linear(z, codes, scales, 100 * seed, 64, y=y, stream=stream)
+                p.vgg19_muon_update(table, 0.01, 0.9, 0.0, 5, True, ws, stream=stream)
+                try:
+                    p.vgg19_q4_linear(z, codes, scales, 100 * seed, 64, y=z, stream=stream)
+                except p.Vgg19Error as e:
+                    out.append(str(e))
+            stream.synchronize()
+        out += [lse, *top, y, w, m]
+
+    alone, together = [[], []], [[], []]
+    for i in range(2):
+        job(i + 1, torch.cuda.Stream(), alone[i])
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=job, args=(i + 1, torch.cuda.Stream(), together[i])) for i in range(2)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    torch.cuda.synchronize()
+    for a, b in zip(alone, together):
+        assert len(a) == len(b) == 26 and a[:20] == b[:20]
+        for x, y in zip(a[20:], b[20:]):
+            assert torch.equal(x, y)
+    p.vgg19_ops_status(torch.cuda.current_stream())
