@@ -188,14 +188,19 @@ __device__ __forceinline__ Sums lanes_join(Sums a) {
 // A warp's best keys, sorted over its lanes, largest first; 0 for none.
 struct Best {
   unsigned long long key = 0;
-  // the elements of the lanes' x that are at least thr
-  template <int N, typename Index> __device__ __forceinline__ void add(const float (&x)[N], float thr, Index index) {
+  // The elements of the lanes' x that are at least thr.  Where there are many, as in a row of equals, they have to be better than
+  // the last place wanted first (512 rows of 50021 equals, the best 5: 738 us without that, 70 with it).
+  template <int N, typename Index> __device__ __forceinline__ void add(const float (&x)[N], float thr, int top_k, Index index) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       unsigned hits = __ballot_sync(0xffffffffu, x[e] >= thr);
       if (!hits) continue;
       const unsigned long long mine = make_key(x[e], index(e));
+      if (__popc(hits) > 4) {  // (of the whole warp)
+        const unsigned long long last = __shfl_sync(0xffffffffu, key, top_k - 1);
+        hits = __ballot_sync(0xffffffffu, x[e] >= thr && mine > last);
+      }
       while (hits) {
         const unsigned long long c = __shfl_sync(0xffffffffu, mine, __ffs(hits) - 1), up = __shfl_up_sync(0xffffffffu, key, 1);
         hits &= hits - 1;
@@ -323,7 +328,7 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(const FwdArgs a) {
           float x[V];
           Vec<T>::unpack(u < v1 ? __ldg(body + u) : none, x);
           const int first = sp.head + u * V;
-          b.add(x, thr, [first](int e) { return (unsigned)(first + e); });
+          b.add(x, thr, a.top_k, [first](int e) { return (unsigned)(first + e); });
         }
       }
     } else {
@@ -338,10 +343,10 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(const FwdArgs a) {
         float x[V];
         Vec<T>::unpack(m && k < each && u < v1 ? __ldg(body + u) : none, x);
         const int first = sp.head + u * V;
-        b.add(x, thr, [first](int e) { return (unsigned)(first + e); });
+        b.add(x, thr, a.top_k, [first](int e) { return (unsigned)(first + e); });
       }
     }
-    if (rank == 0 && warp == 0) b.add(edge, thr, [at](int) { return (unsigned)at; });
+    if (rank == 0 && warp == 0) b.add(edge, thr, a.top_k, [at](int) { return (unsigned)at; });
     const bool have = lane < a.top_k && b.key != 0;
     const unsigned m = __ballot_sync(0xffffffffu, have);
     int to = 0;

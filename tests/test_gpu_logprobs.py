@@ -488,3 +488,17 @@ def test_short_rows_with_a_nan_or_infinity(p, n, at, value, dtype):
     assert torch.isnan(d[3]).all() and not torch.isnan(d[:3]).any() and not torch.isnan(d[4:]).any()
     with pytest.raises(p.Vgg19Error):
         p.vgg19_ops_status(torch.cuda.current_stream())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,n,top", [(3, 2000, 1), (2, 9001, 32), (1, 131072, 20), (300, 50021, 3)])
+def test_rows_of_equals(p, rows, n, top, dtype):
+    """What a classifier answers before it has learnt anything; and a few classes that stand out of equals, below and above."""
+    z = torch.zeros(rows, n, dtype=TYPES[dtype], device=DEV)
+    if rows > 1:
+        z[1, 5::7] = -1.0
+        z[1, n - 3:] = 2.0
+        z[rows - 1] = torch.linspace(-4, 4, n, device=DEV).to(TYPES[dtype])  # bf16: runs of equals
+    ids = torch.zeros(rows, 1, dtype=torch.int32, device=DEV)
+    want, _ = reference(z, ids, top)
+    check(call(p, z, ids, top), want, n)
