@@ -482,6 +482,20 @@ int vgg19_sync_status(vgg19_t *net, void *stream);
  * VGG19_ERR_DEVICE_TIMEOUT, and passes enqueued afterwards run normally. */
 int vgg19_selftest_wait_timeout(vgg19_t *net, void *stream);
 
+/* The same for the operators that wait for copies or products inside their
+ * kernels: a call of the operator over zeros in which one block asks for none of
+ * its copies, with a limit of about a millisecond.  The kernels' own way out of such a
+ * wait runs (what is in flight ends, the blocks of a cluster meet, tensor memory is
+ * freed) and the next vgg19_ops_status reports VGG19_ERR_DEVICE_TIMEOUT.
+ * workspace: device, 256-byte aligned, VGG19_SELFTEST_BYTES, overwritten. */
+#define VGG19_SELFTEST_BYTES 1048576
+enum {
+  VGG19_SELFTEST_DENSE_Q4 = 0,    /* vgg19_q4_linear */
+  VGG19_SELFTEST_UPDATE = 1,      /* vgg19_muon_update, its products */
+  VGG19_SELFTEST_UPDATE_STEPS = 2 /* vgg19_muon_update, the steps of small matrices */
+};
+int vgg19_selftest_operator_timeout(int32_t which, void *workspace, size_t bytes, void *stream);
+
 /* Number of kernel launches (graph nodes) one forward / backward call makes. */
 int vgg19_launch_count(const vgg19_t *net, int32_t mode, int32_t *n_kernels);
 

@@ -29,10 +29,12 @@ EXPORTS = (
     "vgg19_describe", "vgg19_last_error",
     "vgg19_logprobs", "vgg19_logprobs_backward", "vgg19_ops_status",
     "vgg19_q4_code_bytes", "vgg19_q4_scale_bytes", "vgg19_q4_pack", "vgg19_q4_linear",
-    "vgg19_muon_workspace_bytes", "vgg19_muon_update", "vgg19_muon_step_bytes", "vgg19_muon_step",
+    "vgg19_selftest_operator_timeout", "vgg19_muon_workspace_bytes", "vgg19_muon_update", "vgg19_muon_step_bytes", "vgg19_muon_step",
 )
 VGG19_NO_CLASS = -1
 VGG19_LOGPROBS_MAX_TOP, VGG19_LOGPROBS_MAX_IDS = 32, 256
+VGG19_SELFTEST_DENSE_Q4, VGG19_SELFTEST_UPDATE, VGG19_SELFTEST_UPDATE_STEPS = 0, 1, 2
+VGG19_SELFTEST_BYTES = 1048576
 
 
 class vgg19_config(ctypes.Structure):
@@ -108,6 +110,7 @@ def load():
         "vgg19_logprobs": ([vp, i32, i64, i32, i64, vp, i32, i32, vp, vp, vp, vp, vp, vp], ctypes.c_int),
         "vgg19_logprobs_backward": ([vp, i32, i64, i32, i64, vp, i32, vp, vp, vp, vp, vp, i64, vp], ctypes.c_int),
         "vgg19_ops_status": ([vp], ctypes.c_int),
+        "vgg19_selftest_operator_timeout": ([i32, vp, sz, vp], ctypes.c_int),
         "vgg19_muon_workspace_bytes": ([vp, i32], sz),
         "vgg19_muon_update": ([vp, i32, f32, f32, f32, i32, i32, vp, sz, vp], ctypes.c_int),
         "vgg19_muon_step_bytes": ([vp], sz),
@@ -555,6 +558,13 @@ def vgg19_muon_step_bytes(net):
 def vgg19_muon_step(net, grads, momentum_buffer, lr, momentum, decay, bias_lr, steps, nesterov, workspace, nbytes, stream=None):
     return _check(net, load().vgg19_muon_step(net, _ptr(grads), _ptr(momentum_buffer), lr, momentum, decay, bias_lr, steps, int(nesterov),
                                               _ptr(workspace), nbytes, _stream(stream)))
+
+
+def vgg19_selftest_operator_timeout(which, workspace, stream=None):
+    """workspace: a CUDA tensor of at least VGG19_SELFTEST_BYTES."""
+    dev = workspace.get_device()
+    _torch()
+    return _call(dev, load().vgg19_selftest_operator_timeout, which, *_workspace(workspace, dev), _stream(stream))
 
 
 def vgg19_ops_status(stream=None):

@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "../../include/vgg19_b200.h"
+
 namespace vgg {
 
 typedef __nv_bfloat16 bf16;
@@ -31,6 +33,18 @@ enum DeviceError : int {
   kDevSplitRange = 65,      // fp32 configuration on tensor cores: an activation beyond fp16's range
 };
 
+// A wait gives up after this long (far above any tile's duration, profiler
+// replays included), records a DeviceError code and lets the CTA drain.
+constexpr long long kWaitLimitCycles = 4000ll * 1000ll * 1000ll;  // about two seconds of SM clock
+
+// How the waits of an operator's kernels end when what they wait for does not come.  Starved, the first block (or pair) of a launch asks
+// for none of its copies, so that its waits are certain to run out: for the self-test alone.
+enum Starve : int { kStarveNone = 0, kStarveProducts = 1, kStarveSmallSteps = 2, kStarveDense = 3 };
+struct Waits {
+  long long limit_cycles = kWaitLimitCycles;
+  int starve = kStarveNone;
+};
+
 // Sets the text vgg19_last_error(NULL) gives and returns `code`: for entry points without a handle.
 int note_error(int code, const char* fmt, ...);
 
@@ -52,6 +66,10 @@ cudaError_t logprobs_take_error(int* code);
 cudaError_t q4_take_error(int* code);
 cudaError_t muon_take_error(int* code);
 
+// vgg19_muon_update with the waits of its kernels (muon.cu).
+int muon_update(const vgg19_muon_tensor* tensors, int32_t count, float lr, float momentum, float decay, int32_t steps, int32_t nesterov,
+                void* workspace, size_t bytes, const Waits& waits, void* stream);
+
 // m <- mu m + g, w <- w - lr (g + mu m or m), w16 the rounded copy (or null), for each vector (muon.cu).
 struct MuonVector {
   const float* grad;
@@ -68,7 +86,7 @@ template <typename T>
 cudaError_t q4_pack(const T* w, long ld, int out, int in, int group, void* codes, void* scales, cudaStream_t st);
 template <typename T>
 cudaError_t q4_linear(const T* x, long ldx, long rows, int in, const void* codes, const void* scales, int out, int group,
-                      const float* bias, bool relu, T* y, float* y_f32, cudaStream_t st);
+                      const float* bias, bool relu, T* y, float* y_f32, const Waits& waits, cudaStream_t st);
 
 // ---- CUDA-core kernels (simt_kernels.cu) ---------------------------------
 // T is the storage type of activations and weights (float or bf16); every

@@ -110,6 +110,7 @@ struct __align__(64) Problem {
   float keep;
 };
 template <int N> struct Launch {
+  Waits waits;
   int count;
   int first_tile[N + 1];  // apart from the problems: finding a tile's problem touches two lines of constant memory
   Problem p[N];
@@ -258,14 +259,14 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
       for (int s = 0; s < STAGES; ++s) fills[s] = 0;
       int stage = 0, pi = 0;
       uint32_t phase = 0;
-      bool ok = true;
+      bool ok = !(L.waits.starve == kStarveProducts && pair == 0);
       for (int w = pair; w < total && ok; w += n_pairs) {
         while (w >= L.first_tile[pi + 1]) ++pi;
         const Problem& p = L.p[pi];
         const Tile tile = find_tile<BN>(p, w - L.first_tile[pi]);
         const int row = (2 * tile.i + (int)rank) * BM, col = tile.j * BN + (int)rank * (BN / 2), mn = p.b_mn;
         for (int kb = tile.k0; kb < tile.k1; ++kb) {
-          if (!mbar_wait(empty_bar(stage), phase ^ 1, &abort_flag, &g_muon_error, kDevTimeoutStageFree)) { ok = false; break; }
+          if (!mbar_wait(empty_bar(stage), phase ^ 1, &abort_flag, &g_muon_error, kDevTimeoutStageFree, L.waits.limit_cycles)) { ok = false; break; }
           const uint32_t sa = smem_base + stage * STAGE_BYTES, sb = sa + kOperandBytes;
           const uint32_t full = map_to_cta(full_bar(stage), 0);
           // the even CTA announces the bytes of both CTAs' copies; what lies outside a matrix arrives as zeros
@@ -316,11 +317,11 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
         for (int kb0 = 0, kb1; kb0 < k_stages && ok; kb0 = kb1, ++chunk) {
           kb1 = min(kb0 + chain, k_stages);
           const int buf = chunk & 1;
-          if (!mbar_wait(acc_empty_bar(buf), ((chunk >> 1) & 1) ^ 1, &abort_flag, &g_muon_error, kDevTimeoutTmemFree)) { ok = false; break; }
+          if (!mbar_wait(acc_empty_bar(buf), ((chunk >> 1) & 1) ^ 1, &abort_flag, &g_muon_error, kDevTimeoutTmemFree, L.waits.limit_cycles)) { ok = false; break; }
           tc_fence_after();
           const uint32_t d = tmem_base + (uint32_t)(buf * BN);
           for (int kb = kb0; kb < kb1; ++kb) {
-            if (!mbar_wait(full_bar(stage), phase, &abort_flag, &g_muon_error, kDevTimeoutTmaFull)) { ok = false; break; }
+            if (!mbar_wait(full_bar(stage), phase, &abort_flag, &g_muon_error, kDevTimeoutTmaFull, L.waits.limit_cycles)) { ok = false; break; }
             tc_fence_after();
             const uint32_t sa = smem_base + stage * STAGE_BYTES, sb = sa + kOperandBytes;
             const uint64_t ah = smem_desc_sw128(sa, 16), al = smem_desc_sw128(sa + kPlaneBytes, 16);
@@ -381,7 +382,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
       }
       for (int kb0 = 0; kb0 < k_stages; kb0 += chain, ++chunk) {
         const int buf = chunk & 1;
-        if (!__all_sync(0xffffffffu, mbar_wait(acc_full_bar(buf), (chunk >> 1) & 1, &abort_flag, &g_muon_error, kDevTimeoutAccum))) { ok = false; break; }
+        if (!__all_sync(0xffffffffu, mbar_wait(acc_full_bar(buf), (chunk >> 1) & 1, &abort_flag, &g_muon_error, kDevTimeoutAccum, L.waits.limit_cycles))) { ok = false; break; }
         tc_fence_after();
         const uint32_t src = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + group * CW);
 #pragma unroll
@@ -606,7 +607,8 @@ struct SmallTensor {
   int k_stages, pad[15];
 };
 struct SmallLaunch {
-  int group, pad[15];
+  Waits waits;
+  int group, pad[11];
   SmallTensor t[kMaxTensors];
 };
 
@@ -634,11 +636,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_steps_kernel(const __g
   const uint32_t tmem_base = tmem_base_slot;
   behind_previous();
 
-  if (tid == 0) {
+  if (tid == 0 && !(L.waits.starve == kStarveSmallSteps && blockIdx.x == 0)) {
     mbar_expect_tx(load_bar, k_stages * kOperandBytes);
     for (int kb = 0; kb < k_stages; ++kb) tma_load_3d(A + kb * kOperandBytes, &t.gram, load_bar, kb * BK, 0, 0);
   }
-  bool ok = __syncthreads_and(mbar_wait(load_bar, 0, &abort_flag, &g_muon_error, kDevTimeoutTmaFull));
+  bool ok = __syncthreads_and(mbar_wait(load_bar, 0, &abort_flag, &g_muon_error, kDevTimeoutTmaFull, L.waits.limit_cycles));
   tc_fence_after();
 
   // thread: row `row` and 64 columns of every result
@@ -689,7 +691,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_steps_kernel(const __g
       add(add1, c1);
       if (add2) add(add2, c2);
     }
-    ok = __syncthreads_and(mbar_wait(done_bar, phase, &abort_flag, &g_muon_error, kDevTimeoutAccum));
+    ok = __syncthreads_and(mbar_wait(done_bar, phase, &abort_flag, &g_muon_error, kDevTimeoutAccum, L.waits.limit_cycles));
     phase ^= 1;
     if (!ok) return;
     tc_fence_after();
@@ -1047,6 +1049,7 @@ cudaError_t launch_small(const SmallLaunch& L, int count, cudaStream_t st) {
 struct Options {
   float lr, mu, decay;
   int steps, nesterov;
+  Waits waits;
 };
 
 // The whole update of up to kMaxTensors tensors; N is the largest number of products per launch.
@@ -1119,6 +1122,7 @@ cudaError_t update_batch(const vgg19_muon_tensor* given, const int count, const 
   bool small = true;
   for (int i = 0; i < count; ++i) small = small && Shape(tensors[i]).m <= kSmall;
   L.count = 0;
+  L.waits = o.waits;
   int x = kX0;
   for (int done = 0; done < o.steps;) {
     // groups of at most three steps, as even as they go
@@ -1152,6 +1156,7 @@ cudaError_t update_batch(const vgg19_muon_tensor* given, const int count, const 
     float sq = kScaleP, q0 = kA;
     if (small) {
       static thread_local SmallLaunch sl;
+      sl.waits = o.waits;
       sl.group = group;
       for (int i = 0; i < count; ++i) {
         sl.t[i].gram = planes[i].k_major[kGramA];
@@ -1323,9 +1328,8 @@ extern "C" size_t vgg19_muon_workspace_bytes(const vgg19_muon_tensor* tensors, i
   return vgg::check_tensors(tensors, count) == VGG19_OK ? vgg::workspace_bytes(tensors, count) : 0;
 }
 
-extern "C" int vgg19_muon_update(const vgg19_muon_tensor* tensors, int32_t count, float lr, float momentum, float decay,
-                                 int32_t steps, int32_t nesterov, void* workspace, size_t bytes, void* stream) {
-  using namespace vgg;
+int vgg::muon_update(const vgg19_muon_tensor* tensors, int32_t count, float lr, float momentum, float decay, int32_t steps, int32_t nesterov,
+                     void* workspace, size_t bytes, const Waits& waits, void* stream) {
   const int rc = check_tensors(tensors, count);
   if (rc != VGG19_OK) return rc;
   if (!(lr == lr) || !(momentum == momentum) || !(decay == decay))
@@ -1345,7 +1349,7 @@ extern "C" int vgg19_muon_update(const vgg19_muon_tensor* tensors, int32_t count
     return note_error(VGG19_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu", bytes, workspace_bytes(tensors, count));
   const int apart = check_overlaps(tensors, count, workspace, workspace_bytes(tensors, count));
   if (apart != VGG19_OK) return apart;
-  const Options o{lr, momentum, decay, steps, nesterov != 0};
+  const Options o{lr, momentum, decay, steps, nesterov != 0, waits};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   for (int i = 0; i < count; i += kMaxTensors) {
     const int n = count - i < kMaxTensors ? count - i : kMaxTensors;
@@ -1354,4 +1358,9 @@ extern "C" int vgg19_muon_update(const vgg19_muon_tensor* tensors, int32_t count
     if (e != cudaSuccess) return note_error(VGG19_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(e));
   }
   return VGG19_OK;
+}
+
+extern "C" int vgg19_muon_update(const vgg19_muon_tensor* tensors, int32_t count, float lr, float momentum, float decay,
+                                 int32_t steps, int32_t nesterov, void* workspace, size_t bytes, void* stream) {
+  return vgg::muon_update(tensors, count, lr, momentum, decay, steps, nesterov, workspace, bytes, vgg::Waits{}, stream);
 }

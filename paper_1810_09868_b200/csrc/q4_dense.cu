@@ -65,6 +65,7 @@ struct Q4Args {
   float* y_f32;
   long ldx;
   int in, out, rows, blocks, ksplit, stage_blocks, relu;
+  Waits waits;
 };
 
 // The terms of eight consecutive activations, each a 16-byte row of bf16 in the order 0 4 1 5 2 6 3 7 (the order in
@@ -149,6 +150,7 @@ __global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 
   };
   if (ks > 1) cluster.barrier_arrive();  // waited for before the first write into another block's shared memory
   if (tid == 0) abort_flag = 0;
+  const bool starved = a.waits.starve == kStarveDense && blockIdx.x == 0;
 
   float acc[NT][4] = {};
   int xrow[NT];
@@ -226,7 +228,7 @@ __global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 
         for (int s = 0; s < kRing; ++s) mbar_init(bar_u32 + 8 * s, 1);
         mbar_fence_init();
         for (int s = 0; s < kRing; ++s)
-          if (first + s * STEP < b1) request(s, first + s * STEP);
+          if (first + s * STEP < b1 && !starved) request(s, first + s * STEP);
       }
 #pragma unroll
       for (int u = 0; u < BATCH; ++u) {
@@ -244,7 +246,7 @@ __global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 
     __syncthreads();
     for (int b = c0 + warp / RW * SLOT; b < c1; b += STEP) {  // (a part of x is a multiple of STEP, but for the last)
       if (!ok) break;
-      ok = __all_sync(0xffffffffu, mbar_wait(bar_u32 + 8 * slot, phase, &abort_flag, &g_q4_error, kDevTimeoutTmaFull));
+      ok = __all_sync(0xffffffffu, mbar_wait(bar_u32 + 8 * slot, phase, &abort_flag, &g_q4_error, kDevTimeoutTmaFull, a.waits.limit_cycles));
       if (!ok) {  // let what is on its way land before shared memory goes away
         if (lane == 0) {
           const unsigned long long t0 = global_timer_ns();
@@ -450,7 +452,7 @@ cudaError_t q4_pack(const T* w, long ld, int out, int in, int group, void* codes
 
 template <typename T>
 cudaError_t q4_linear(const T* x, long ldx, long rows, int in, const void* codes, const void* scales, int out, int group,
-                      const float* bias, bool relu, T* y, float* y_f32, cudaStream_t st) {
+                      const float* bias, bool relu, T* y, float* y_f32, const Waits& waits, cudaStream_t st) {
   for (long r = 0; r < rows; r += kMaxRows) {
     Q4Args a{};
     a.x = x + r * ldx;
@@ -462,6 +464,7 @@ cudaError_t q4_linear(const T* x, long ldx, long rows, int in, const void* codes
     a.ldx = ldx; a.in = in; a.out = out; a.relu = relu;
     a.rows = (int)(rows - r < kMaxRows ? rows - r : kMaxRows);
     a.blocks = (in + kBlockK - 1) / kBlockK;
+    a.waits = waits;
     const cudaError_t e = launch_type<T>(a, group, st);
     if (e != cudaSuccess) return e;
   }
@@ -480,7 +483,7 @@ cudaError_t q4_take_error(int* code) {
 #define INSTANTIATE(T)                                                                                                    \
   template cudaError_t q4_pack<T>(const T*, long, int, int, int, void*, void*, cudaStream_t);                             \
   template cudaError_t q4_linear<T>(const T*, long, long, int, const void*, const void*, int, int, const float*, bool, T*, \
-                                    float*, cudaStream_t);
+                                    float*, const Waits&, cudaStream_t);
 INSTANTIATE(float)
 INSTANTIATE(bf16)
 
@@ -539,8 +542,8 @@ int vgg19_q4_linear(const void* x, int32_t dtype, int64_t rows, int32_t in, int6
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e =
       dtype == VGG19_BF16
-          ? q4_linear(static_cast<const bf16*>(x), ldx, rows, in, codes, scales, out, group, bias, relu != 0, static_cast<bf16*>(y), y_f32, st)
-          : q4_linear(static_cast<const float*>(x), ldx, rows, in, codes, scales, out, group, bias, relu != 0, static_cast<float*>(y), y_f32, st);
+          ? q4_linear(static_cast<const bf16*>(x), ldx, rows, in, codes, scales, out, group, bias, relu != 0, static_cast<bf16*>(y), y_f32, Waits{}, st)
+          : q4_linear(static_cast<const float*>(x), ldx, rows, in, codes, scales, out, group, bias, relu != 0, static_cast<float*>(y), y_f32, Waits{}, st);
   return e == cudaSuccess ? VGG19_OK : note_error(VGG19_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(e));
 }
 

@@ -13,10 +13,6 @@
 namespace vgg {
 namespace tc {
 
-// A wait gives up after this long (far above any tile's duration, profiler
-// replays included), records a DeviceError code and lets the CTA drain.
-constexpr long long kWaitLimitCycles = 4000ll * 1000ll * 1000ll;  // about two seconds of SM clock
-
 __device__ __forceinline__ uint32_t smem_u32(const void* p) {
   return static_cast<uint32_t>(__cvta_generic_to_shared(p));
 }

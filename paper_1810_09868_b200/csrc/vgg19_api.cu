@@ -396,7 +396,7 @@ struct Pass {
     if (q4) {
       const int i = (int)(&f - n->fc);
       ok(q4_linear<T>(x, f.In, B, f.In, n->q4 + n->q4_codes[i], n->q4 + n->q4_scales[i], f.Out, VGG19_DENSE_Q4_GROUP,
-                      n->params + f.b_off, f.relu, out_t, out_f, st), (B + 15) / 16);
+                      n->params + f.b_off, f.relu, out_t, out_f, Waits{}, st), (B + 15) / 16);
       return;
     }
     if (tc_dense_ok(B, f))
@@ -1324,6 +1324,37 @@ int vgg19_selftest_wait_timeout(vgg19_t *n, void *stream) {
   // a millisecond or two of SM clock: long enough to be a real wait, short enough for a test
   CUDA_TRY(n, tc_wait_selftest(n->dev_error, 2000000ll, static_cast<cudaStream_t>(stream)));
   return VGG19_OK;
+}
+
+int vgg19_selftest_operator_timeout(int32_t which, void *workspace, size_t bytes, void *stream) {
+  if (which < VGG19_SELFTEST_DENSE_Q4 || which > VGG19_SELFTEST_UPDATE_STEPS)
+    return fail(nullptr, VGG19_ERR_ARG, "there is no operator's self-test %d", which);
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || bytes < VGG19_SELFTEST_BYTES)
+    return fail(nullptr, VGG19_ERR_WORKSPACE, "the self-test takes %d bytes, 256-byte aligned", VGG19_SELFTEST_BYTES);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  CUDA_TRY(nullptr, cudaMemsetAsync(workspace, 0, VGG19_SELFTEST_BYTES, st));
+  char *at = static_cast<char *>(workspace);
+  auto take = [&at](size_t size) { char *p = at; at += align_up(size); return p; };
+  Waits waits;
+  waits.limit_cycles = 2000000;  // a millisecond or two
+  if (which == VGG19_SELFTEST_DENSE_Q4) {
+    // three rows, so that every warp has a row tile of its own, over a K that a cluster of blocks shares
+    constexpr int rows = 3, in = 1024, out = 128, group = VGG19_DENSE_Q4_GROUP;
+    waits.starve = kStarveDense;
+    void *codes = take(q4_code_bytes(out, in)), *scales = take(q4_scale_bytes(out, in, group));
+    const bf16 *x = reinterpret_cast<bf16 *>(take(rows * in * 2));
+    float *y = reinterpret_cast<float *>(take(rows * out * 4));
+    CUDA_TRY(nullptr, q4_linear<bf16>(x, in, rows, in, codes, scales, out, group, nullptr, false, nullptr, y, waits, st));
+    return VGG19_OK;
+  }
+  waits.starve = which == VGG19_SELFTEST_UPDATE ? kStarveProducts : kStarveSmallSteps;
+  constexpr int rows = 96, cols = 160;
+  vgg19_muon_tensor t{};
+  t.rows = rows; t.cols = cols;
+  t.w = reinterpret_cast<float *>(take(rows * cols * 4));
+  t.grad = reinterpret_cast<float *>(take(rows * cols * 4));
+  t.momentum = reinterpret_cast<float *>(take(rows * cols * 4));
+  return muon_update(&t, 1, 0.1f, 0.9f, 0.f, 1, 0, at, VGG19_SELFTEST_BYTES - (at - static_cast<char *>(workspace)), waits, stream);
 }
 
 int vgg19_launch_count(const vgg19_t *n, int32_t mode, int32_t *n_kernels) {

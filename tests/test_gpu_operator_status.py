@@ -1,0 +1,55 @@
+"""What the operators report of waits that ran out, and to whom.  The waits are made to run out by the library's self-test: a block that asks
+for none of its copies, over zeros, with a limit of about a millisecond.  Nothing faults: the kernels give up, end and return."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+KINDS = ["VGG19_SELFTEST_DENSE_Q4", "VGG19_SELFTEST_UPDATE", "VGG19_SELFTEST_UPDATE_STEPS"]
+
+
+@pytest.fixture(scope="module")
+def p():
+    import paper_1810_09868_b200 as pkg
+    return pkg
+
+
+def reported(p, fn, *a):
+    """The code that a status call raises, or VGG19_OK."""
+    try:
+        fn(*a)
+    except p.Vgg19Error as e:
+        return e.code
+    return p.VGG19_OK
+
+
+def scratch(p):
+    return torch.empty(p.VGG19_SELFTEST_BYTES, dtype=torch.uint8, device=DEV)
+
+
+def calls(p, st):
+    """One call of each operator; what they give."""
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    w, g, m = (torch.randn(96, 160, generator=gen, device=DEV) for _ in range(3))
+    x, y = torch.randn(3, 160, generator=gen, device=DEV), torch.empty(3, 96, device=DEV)
+    codes = torch.empty(p.vgg19_q4_code_bytes(96, 160), dtype=torch.uint8, device=DEV)
+    scales = torch.empty(p.vgg19_q4_scale_bytes(96, 160, 64), dtype=torch.uint8, device=DEV)
+    p.vgg19_q4_pack(w, 64, codes, scales, st)
+    p.vgg19_q4_linear(x, codes, scales, 96, 64, y=y, stream=st)
+    table = p.vgg19_muon_tensors([(w, None, g, m)])
+    ws = torch.empty(p.vgg19_muon_workspace_bytes(table), dtype=torch.uint8, device=DEV)
+    p.vgg19_muon_update(table, 0.1, 0.9, 0.0, 5, True, ws, st)
+    return y, w, m
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_a_wait_that_runs_out_is_reported_once(p, kind):
+    st = torch.cuda.current_stream()
+    before = calls(p, st)
+    p.vgg19_ops_status(st)
+    p.vgg19_selftest_operator_timeout(getattr(p, kind), scratch(p), st)
+    assert reported(p, p.vgg19_ops_status, st) == p.VGG19_ERR_DEVICE_TIMEOUT
+    p.vgg19_ops_status(st)
+    for a, b in zip(before, calls(p, st)):  # and the operators work as they did
+        assert torch.equal(a, b)
+    p.vgg19_ops_status(st)
