@@ -458,8 +458,8 @@ size_t vgg19_muon_step_bytes(const vgg19_t *net);
 int vgg19_muon_step(vgg19_t *net, const float *grads, float *momentum_buffer, float lr, float momentum, float decay,
                     float bias_lr, int32_t steps, int32_t nesterov, void *workspace, size_t bytes, void *stream);
 
-/* Wait for the stream and report, and clear, what the operators without a handle
- * (vgg19_logprobs and those below it) have recorded on the current device:
+/* Wait for the stream and report, and clear, what calls without a handle
+ * (vgg19_logprobs, vgg19_q4_linear, vgg19_muon_update) have recorded on the current device:
  * VGG19_ERR_DEVICE_TIMEOUT when a bounded wait inside a kernel ran out,
  * VGG19_ERR_ARG for an id outside the classes. */
 int vgg19_ops_status(void *stream);
@@ -467,9 +467,9 @@ int vgg19_ops_status(void *stream);
 /* Wait for the stream and report any device-side error recorded so far:
  * VGG19_ERR_DEVICE_TIMEOUT when a bounded wait inside a kernel ran out,
  * VGG19_ERR_ARG when a label outside [0,1000) reached the loss (the label is
- * never used as an index; that pass's loss is NaN).  Waits inside the 4-bit
- * dense layers and vgg19_muon_step are reported here too, if the handle has
- * run them.  The record is cleared, and the handle stays usable. */
+ * never used as an index; that pass's loss is NaN).  What this handle's passes,
+ * its 4-bit dense layers and vgg19_muon_step recorded is reported here and only
+ * here.  The record is cleared, and the handle stays usable. */
 int vgg19_sync_status(vgg19_t *net, void *stream);
 
 /* Diagnostic for the error path above.  Every wait inside the kernels (on a
@@ -486,7 +486,8 @@ int vgg19_selftest_wait_timeout(vgg19_t *net, void *stream);
  * kernels: a call of the operator over zeros in which one block asks for none of
  * its copies, with a limit of about a millisecond.  The kernels' own way out of such a
  * wait runs (what is in flight ends, the blocks of a cluster meet, tensor memory is
- * freed) and the next vgg19_ops_status reports VGG19_ERR_DEVICE_TIMEOUT.
+ * freed) and the next vgg19_sync_status of `net`, or vgg19_ops_status where that
+ * is NULL, reports VGG19_ERR_DEVICE_TIMEOUT.
  * workspace: device, 256-byte aligned, VGG19_SELFTEST_BYTES, overwritten. */
 #define VGG19_SELFTEST_BYTES 1048576
 enum {
@@ -494,7 +495,7 @@ enum {
   VGG19_SELFTEST_UPDATE = 1,      /* vgg19_muon_update, its products */
   VGG19_SELFTEST_UPDATE_STEPS = 2 /* vgg19_muon_update, the steps of small matrices */
 };
-int vgg19_selftest_operator_timeout(int32_t which, void *workspace, size_t bytes, void *stream);
+int vgg19_selftest_operator_timeout(vgg19_t *net, int32_t which, void *workspace, size_t bytes, void *stream);
 
 /* Number of kernel launches (graph nodes) one forward / backward call makes. */
 int vgg19_launch_count(const vgg19_t *net, int32_t mode, int32_t *n_kernels);

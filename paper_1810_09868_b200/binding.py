@@ -110,7 +110,7 @@ def load():
         "vgg19_logprobs": ([vp, i32, i64, i32, i64, vp, i32, i32, vp, vp, vp, vp, vp, vp], ctypes.c_int),
         "vgg19_logprobs_backward": ([vp, i32, i64, i32, i64, vp, i32, vp, vp, vp, vp, vp, i64, vp], ctypes.c_int),
         "vgg19_ops_status": ([vp], ctypes.c_int),
-        "vgg19_selftest_operator_timeout": ([i32, vp, sz, vp], ctypes.c_int),
+        "vgg19_selftest_operator_timeout": ([vp, i32, vp, sz, vp], ctypes.c_int),
         "vgg19_muon_workspace_bytes": ([vp, i32], sz),
         "vgg19_muon_update": ([vp, i32, f32, f32, f32, i32, i32, vp, sz, vp], ctypes.c_int),
         "vgg19_muon_step_bytes": ([vp], sz),
@@ -560,11 +560,11 @@ def vgg19_muon_step(net, grads, momentum_buffer, lr, momentum, decay, bias_lr, s
                                               _ptr(workspace), nbytes, _stream(stream)))
 
 
-def vgg19_selftest_operator_timeout(which, workspace, stream=None):
-    """workspace: a CUDA tensor of at least VGG19_SELFTEST_BYTES."""
+def vgg19_selftest_operator_timeout(net, which, workspace, stream=None):
+    """net or None; workspace: a CUDA tensor of at least VGG19_SELFTEST_BYTES."""
     dev = workspace.get_device()
     _torch()
-    return _call(dev, load().vgg19_selftest_operator_timeout, which, *_workspace(workspace, dev), _stream(stream))
+    return _call(dev, load().vgg19_selftest_operator_timeout, net, which, *_workspace(workspace, dev), _stream(stream))
 
 
 def vgg19_ops_status(stream=None):

@@ -37,10 +37,12 @@ enum DeviceError : int {
 // replays included), records a DeviceError code and lets the CTA drain.
 constexpr long long kWaitLimitCycles = 4000ll * 1000ll * 1000ll;  // about two seconds of SM clock
 
-// How the waits of an operator's kernels end when what they wait for does not come.  Starved, the first block (or pair) of a launch asks
+// How the waits of an operator's kernels end when what they wait for does not come, and where that is recorded: in a network's error word for
+// its own calls, in the operator's for calls without a handle (null).  Starved, the first block (or pair) of a launch asks
 // for none of its copies, so that its waits are certain to run out: for the self-test alone.
 enum Starve : int { kStarveNone = 0, kStarveProducts = 1, kStarveSmallSteps = 2, kStarveDense = 3 };
 struct Waits {
+  int* error = nullptr;
   long long limit_cycles = kWaitLimitCycles;
   int starve = kStarveNone;
 };

@@ -41,7 +41,7 @@ namespace {
 
 using namespace tc;
 
-static __device__ int g_muon_error;  // a DeviceError code once a bounded wait ran out
+static __device__ int g_muon_error;  // a DeviceError code once a bounded wait of a call without a handle ran out
 
 // ---- sizes -----------------------------------------------------------------------------------------------------
 constexpr int BM = 128, BK = 64;                 // rows per CTA (a pair has 256), K per stage
@@ -229,6 +229,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const bool leader = rank == 0;
+  int* const error = L.waits.error ? L.waits.error : &g_muon_error;
   const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1, total = L.first_tile[L.count];
 
   if (threadIdx.x == 0) {
@@ -266,7 +267,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
         const Tile tile = find_tile<BN>(p, w - L.first_tile[pi]);
         const int row = (2 * tile.i + (int)rank) * BM, col = tile.j * BN + (int)rank * (BN / 2), mn = p.b_mn;
         for (int kb = tile.k0; kb < tile.k1; ++kb) {
-          if (!mbar_wait(empty_bar(stage), phase ^ 1, &abort_flag, &g_muon_error, kDevTimeoutStageFree, L.waits.limit_cycles)) { ok = false; break; }
+          if (!mbar_wait(empty_bar(stage), phase ^ 1, &abort_flag, error, kDevTimeoutStageFree, L.waits.limit_cycles)) { ok = false; break; }
           const uint32_t sa = smem_base + stage * STAGE_BYTES, sb = sa + kOperandBytes;
           const uint32_t full = map_to_cta(full_bar(stage), 0);
           // the even CTA announces the bytes of both CTAs' copies; what lies outside a matrix arrives as zeros
@@ -317,11 +318,11 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
         for (int kb0 = 0, kb1; kb0 < k_stages && ok; kb0 = kb1, ++chunk) {
           kb1 = min(kb0 + chain, k_stages);
           const int buf = chunk & 1;
-          if (!mbar_wait(acc_empty_bar(buf), ((chunk >> 1) & 1) ^ 1, &abort_flag, &g_muon_error, kDevTimeoutTmemFree, L.waits.limit_cycles)) { ok = false; break; }
+          if (!mbar_wait(acc_empty_bar(buf), ((chunk >> 1) & 1) ^ 1, &abort_flag, error, kDevTimeoutTmemFree, L.waits.limit_cycles)) { ok = false; break; }
           tc_fence_after();
           const uint32_t d = tmem_base + (uint32_t)(buf * BN);
           for (int kb = kb0; kb < kb1; ++kb) {
-            if (!mbar_wait(full_bar(stage), phase, &abort_flag, &g_muon_error, kDevTimeoutTmaFull, L.waits.limit_cycles)) { ok = false; break; }
+            if (!mbar_wait(full_bar(stage), phase, &abort_flag, error, kDevTimeoutTmaFull, L.waits.limit_cycles)) { ok = false; break; }
             tc_fence_after();
             const uint32_t sa = smem_base + stage * STAGE_BYTES, sb = sa + kOperandBytes;
             const uint64_t ah = smem_desc_sw128(sa, 16), al = smem_desc_sw128(sa + kPlaneBytes, 16);
@@ -382,7 +383,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
       }
       for (int kb0 = 0; kb0 < k_stages; kb0 += chain, ++chunk) {
         const int buf = chunk & 1;
-        if (!__all_sync(0xffffffffu, mbar_wait(acc_full_bar(buf), (chunk >> 1) & 1, &abort_flag, &g_muon_error, kDevTimeoutAccum, L.waits.limit_cycles))) { ok = false; break; }
+        if (!__all_sync(0xffffffffu, mbar_wait(acc_full_bar(buf), (chunk >> 1) & 1, &abort_flag, error, kDevTimeoutAccum, L.waits.limit_cycles))) { ok = false; break; }
         tc_fence_after();
         const uint32_t src = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + group * CW);
 #pragma unroll
@@ -608,7 +609,7 @@ struct SmallTensor {
 };
 struct SmallLaunch {
   Waits waits;
-  int group, pad[11];
+  int group, pad[9];
   SmallTensor t[kMaxTensors];
 };
 
@@ -619,6 +620,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_steps_kernel(const __g
   __shared__ uint32_t tmem_base_slot;
   __shared__ int abort_flag;
   const SmallTensor& t = L.t[blockIdx.x];
+  int* const error = L.waits.error ? L.waits.error : &g_muon_error;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, k_stages = t.k_stages;
   if (tid == 0) {
     abort_flag = 0;
@@ -640,7 +642,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_steps_kernel(const __g
     mbar_expect_tx(load_bar, k_stages * kOperandBytes);
     for (int kb = 0; kb < k_stages; ++kb) tma_load_3d(A + kb * kOperandBytes, &t.gram, load_bar, kb * BK, 0, 0);
   }
-  bool ok = __syncthreads_and(mbar_wait(load_bar, 0, &abort_flag, &g_muon_error, kDevTimeoutTmaFull, L.waits.limit_cycles));
+  bool ok = __syncthreads_and(mbar_wait(load_bar, 0, &abort_flag, error, kDevTimeoutTmaFull, L.waits.limit_cycles));
   tc_fence_after();
 
   // thread: row `row` and 64 columns of every result
@@ -691,7 +693,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_steps_kernel(const __g
       add(add1, c1);
       if (add2) add(add2, c2);
     }
-    ok = __syncthreads_and(mbar_wait(done_bar, phase, &abort_flag, &g_muon_error, kDevTimeoutAccum, L.waits.limit_cycles));
+    ok = __syncthreads_and(mbar_wait(done_bar, phase, &abort_flag, error, kDevTimeoutAccum, L.waits.limit_cycles));
     phase ^= 1;
     if (!ok) return;
     tc_fence_after();

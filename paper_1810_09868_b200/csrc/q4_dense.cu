@@ -35,7 +35,7 @@ namespace {
 
 using namespace tc;
 
-static __device__ int g_q4_error;  // a DeviceError code once a bounded wait ran out
+static __device__ int g_q4_error;  // a DeviceError code once a bounded wait of a call without a handle ran out
 
 constexpr int kTileRows = 16, kBlockK = 128, kBlockBytes = kTileRows * kBlockK / 2;
 constexpr int kMaxRows = 16;                 // rows of x per launch
@@ -150,6 +150,7 @@ __global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 
   };
   if (ks > 1) cluster.barrier_arrive();  // waited for before the first write into another block's shared memory
   if (tid == 0) abort_flag = 0;
+  int* const error = a.waits.error ? a.waits.error : &g_q4_error;
   const bool starved = a.waits.starve == kStarveDense && blockIdx.x == 0;
 
   float acc[NT][4] = {};
@@ -246,7 +247,7 @@ __global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 
     __syncthreads();
     for (int b = c0 + warp / RW * SLOT; b < c1; b += STEP) {  // (a part of x is a multiple of STEP, but for the last)
       if (!ok) break;
-      ok = __all_sync(0xffffffffu, mbar_wait(bar_u32 + 8 * slot, phase, &abort_flag, &g_q4_error, kDevTimeoutTmaFull, a.waits.limit_cycles));
+      ok = __all_sync(0xffffffffu, mbar_wait(bar_u32 + 8 * slot, phase, &abort_flag, error, kDevTimeoutTmaFull, a.waits.limit_cycles));
       if (!ok) {  // let what is on its way land before shared memory goes away
         if (lane == 0) {
           const unsigned long long t0 = global_timer_ns();

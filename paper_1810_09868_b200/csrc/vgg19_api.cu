@@ -53,6 +53,13 @@ struct FcLayer {
 // Text of the last failed call that has no handle, of this thread.
 thread_local std::string g_create_error;
 
+// Waits of the operators' kernels that report to a network's error word.
+Waits waits_of(int *error) {
+  Waits w;
+  w.error = error;
+  return w;
+}
+
 size_t align_up(size_t v, size_t a = 256) { return (v + a - 1) / a * a; }
 
 struct GraphEntry {
@@ -80,7 +87,6 @@ struct vgg19 {
   half16 *split_w = nullptr; // fp32 configuration on tensor cores: rows [hi | lo | hi] (fp16 terms) of every weight matrix, at 3 * w_off
   char *q4 = nullptr;        // VGG19_FLAG_DENSE_Q4: codes and scales of the dense layers
   size_t q4_codes[kFcLayers] = {}, q4_scales[kFcLayers] = {};  // byte offsets in it
-  bool muon_used = false;    // vgg19_muon_step has run: vgg19_sync_status looks at its kernels' error word too
   int *dev_error = nullptr;
   void *ws = nullptr;
   size_t ws_bytes = 0;
@@ -396,7 +402,7 @@ struct Pass {
     if (q4) {
       const int i = (int)(&f - n->fc);
       ok(q4_linear<T>(x, f.In, B, f.In, n->q4 + n->q4_codes[i], n->q4 + n->q4_scales[i], f.Out, VGG19_DENSE_Q4_GROUP,
-                      n->params + f.b_off, f.relu, out_t, out_f, Waits{}, st), (B + 15) / 16);
+                      n->params + f.b_off, f.relu, out_t, out_f, waits_of(n->dev_error), st), (B + 15) / 16);
       return;
     }
     if (tc_dense_ok(B, f))
@@ -912,6 +918,13 @@ size_t vgg19_muon_step_bytes(const vgg19_t *n) {
   return vgg19_muon_workspace_bytes(t, kLayers);
 }
 
+// What was noted without a handle becomes the network's error.
+static int adopt_error(vgg19_t *n, int rc) {
+  char text[512];
+  snprintf(text, sizeof text, "%s", vgg19_last_error(nullptr));
+  return fail(n, rc, "%s", text);
+}
+
 int vgg19_muon_step(vgg19_t *n, const float *grads, float *momentum_buffer, float lr, float momentum, float decay,
                     float bias_lr, int32_t steps, int32_t nesterov, void *workspace, size_t bytes, void *stream) {
   if (!n) return VGG19_ERR_ARG;
@@ -919,13 +932,8 @@ int vgg19_muon_step(vgg19_t *n, const float *grads, float *momentum_buffer, floa
     return fail(n, VGG19_ERR_ARG, "null gradient or momentum, or NaN bias learning rate");
   vgg19_muon_tensor t[kLayers];
   muon_tensors(n, grads, momentum_buffer, t);
-  const int rc = vgg19_muon_update(t, kLayers, lr, momentum, decay, steps, nesterov, workspace, bytes, stream);
-  if (rc != VGG19_OK) {
-    char text[512];
-    snprintf(text, sizeof text, "%s", vgg19_last_error(nullptr));
-    return fail(n, rc, "%s", text);
-  }
-  n->muon_used = true;
+  const int rc = muon_update(t, kLayers, lr, momentum, decay, steps, nesterov, workspace, bytes, waits_of(n->dev_error), stream);
+  if (rc != VGG19_OK) return adopt_error(n, rc);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   MuonVector v[kLayers];
   for (int l = 0; l < kLayers; ++l) {
@@ -1312,10 +1320,6 @@ int vgg19_sync_status(vgg19_t *n, void *stream) {
       return fail(n, VGG19_ERR_RANGE, "an activation beyond fp16's range (65504) met the split-fp16 path");
     return fail(n, VGG19_ERR_DEVICE_TIMEOUT, "a device-side wait ran out (code %d)", code);
   }
-  // the operators without a handle that this network's calls have run
-  if (n->q4) CUDA_TRY(n, q4_take_error(&code));
-  if (!code && n->muon_used) CUDA_TRY(n, muon_take_error(&code));
-  if (code) return fail(n, VGG19_ERR_DEVICE_TIMEOUT, "a device-side wait ran out (code %d)", code);
   return VGG19_OK;
 }
 
@@ -1326,16 +1330,16 @@ int vgg19_selftest_wait_timeout(vgg19_t *n, void *stream) {
   return VGG19_OK;
 }
 
-int vgg19_selftest_operator_timeout(int32_t which, void *workspace, size_t bytes, void *stream) {
+int vgg19_selftest_operator_timeout(vgg19_t *n, int32_t which, void *workspace, size_t bytes, void *stream) {
   if (which < VGG19_SELFTEST_DENSE_Q4 || which > VGG19_SELFTEST_UPDATE_STEPS)
-    return fail(nullptr, VGG19_ERR_ARG, "there is no operator's self-test %d", which);
+    return fail(n, VGG19_ERR_ARG, "there is no operator's self-test %d", which);
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || bytes < VGG19_SELFTEST_BYTES)
-    return fail(nullptr, VGG19_ERR_WORKSPACE, "the self-test takes %d bytes, 256-byte aligned", VGG19_SELFTEST_BYTES);
+    return fail(n, VGG19_ERR_WORKSPACE, "the self-test takes %d bytes, 256-byte aligned", VGG19_SELFTEST_BYTES);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  CUDA_TRY(nullptr, cudaMemsetAsync(workspace, 0, VGG19_SELFTEST_BYTES, st));
+  CUDA_TRY(n, cudaMemsetAsync(workspace, 0, VGG19_SELFTEST_BYTES, st));
   char *at = static_cast<char *>(workspace);
   auto take = [&at](size_t size) { char *p = at; at += align_up(size); return p; };
-  Waits waits;
+  Waits waits = waits_of(n ? n->dev_error : nullptr);
   waits.limit_cycles = 2000000;  // a millisecond or two
   if (which == VGG19_SELFTEST_DENSE_Q4) {
     // three rows, so that every warp has a row tile of its own, over a K that a cluster of blocks shares
@@ -1344,7 +1348,7 @@ int vgg19_selftest_operator_timeout(int32_t which, void *workspace, size_t bytes
     void *codes = take(q4_code_bytes(out, in)), *scales = take(q4_scale_bytes(out, in, group));
     const bf16 *x = reinterpret_cast<bf16 *>(take(rows * in * 2));
     float *y = reinterpret_cast<float *>(take(rows * out * 4));
-    CUDA_TRY(nullptr, q4_linear<bf16>(x, in, rows, in, codes, scales, out, group, nullptr, false, nullptr, y, waits, st));
+    CUDA_TRY(n, q4_linear<bf16>(x, in, rows, in, codes, scales, out, group, nullptr, false, nullptr, y, waits, st));
     return VGG19_OK;
   }
   waits.starve = which == VGG19_SELFTEST_UPDATE ? kStarveProducts : kStarveSmallSteps;
@@ -1354,7 +1358,8 @@ int vgg19_selftest_operator_timeout(int32_t which, void *workspace, size_t bytes
   t.w = reinterpret_cast<float *>(take(rows * cols * 4));
   t.grad = reinterpret_cast<float *>(take(rows * cols * 4));
   t.momentum = reinterpret_cast<float *>(take(rows * cols * 4));
-  return muon_update(&t, 1, 0.1f, 0.9f, 0.f, 1, 0, at, VGG19_SELFTEST_BYTES - (at - static_cast<char *>(workspace)), waits, stream);
+  const int rc = muon_update(&t, 1, 0.1f, 0.9f, 0.f, 1, 0, at, VGG19_SELFTEST_BYTES - (at - static_cast<char *>(workspace)), waits, stream);
+  return rc == VGG19_OK || !n ? rc : adopt_error(n, rc);
 }
 
 int vgg19_launch_count(const vgg19_t *n, int32_t mode, int32_t *n_kernels) {

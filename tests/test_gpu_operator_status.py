@@ -47,9 +47,31 @@ def test_a_wait_that_runs_out_is_reported_once(p, kind):
     st = torch.cuda.current_stream()
     before = calls(p, st)
     p.vgg19_ops_status(st)
-    p.vgg19_selftest_operator_timeout(getattr(p, kind), scratch(p), st)
+    p.vgg19_selftest_operator_timeout(None, getattr(p, kind), scratch(p), st)
     assert reported(p, p.vgg19_ops_status, st) == p.VGG19_ERR_DEVICE_TIMEOUT
     p.vgg19_ops_status(st)
     for a, b in zip(before, calls(p, st)):  # and the operators work as they did
         assert torch.equal(a, b)
     p.vgg19_ops_status(st)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_what_runs_out_is_reported_to_its_owner_alone(p, kind):
+    """Two networks that run 4-bit layers and the orthogonalised update, and calls without a handle beside them."""
+    st, which, ws = torch.cuda.current_stream(), getattr(p, kind), scratch(p)
+    nets = [p.Net(32, 32, 1, p.VGG19_BF16, seed=i, flags=p.VGG19_FLAG_DENSE_Q4) for i in (1, 2)]
+    images = torch.rand(1, 32, 32, 3, device=DEV).to(torch.bfloat16)
+    for net in nets:
+        net.muon_step(torch.full((net.n_params,), 1e-3, device=DEV), torch.zeros(net.n_params, device=DEV), 1e-3)
+    before = [net.forward(images).clone() for net in nets]
+    status = [nets[0].sync_status, nets[1].sync_status, lambda: p.vgg19_ops_status(st)]
+    for owner, handle in enumerate((nets[0].handle, nets[1].handle, None)):
+        p.vgg19_selftest_operator_timeout(handle, which, ws, st)
+        for other in {0, 1, 2} - {owner}:
+            assert reported(p, status[other]) == p.VGG19_OK, (owner, other)
+        assert reported(p, status[owner]) == p.VGG19_ERR_DEVICE_TIMEOUT
+        assert [reported(p, s) for s in status] == [p.VGG19_OK] * 3
+    for net, logits in zip(nets, before):
+        assert torch.equal(net.forward(images), logits)
+        net.sync_status()
+        net.close()

@@ -189,5 +189,5 @@ def test_the_binding_refuses_sizes_beyond_an_int(p):
 @pytest.mark.parametrize("which,ws,nbytes,code", [(-1, SOME, 1 << 20, "ARG"), (3, SOME, 1 << 20, "ARG"), (0, None, 1 << 20, "WORKSPACE"),
                                                   (1, SOME + 16, 1 << 20, "WORKSPACE"), (2, SOME, (1 << 20) - 1, "WORKSPACE")])
 def test_the_operators_selftest_refuses(p, which, ws, nbytes, code):
-    assert p.binding.load().vgg19_selftest_operator_timeout(which, ws, nbytes, None) == getattr(p, "VGG19_ERR_" + code)
+    assert p.binding.load().vgg19_selftest_operator_timeout(None, which, ws, nbytes, None) == getattr(p, "VGG19_ERR_" + code)
     assert p.VGG19_SELFTEST_BYTES == 1 << 20
