@@ -461,7 +461,8 @@ int vgg19_muon_step(vgg19_t *net, const float *grads, float *momentum_buffer, fl
 /* Wait for the stream and report, and clear, what calls without a handle
  * (vgg19_logprobs, vgg19_q4_linear, vgg19_muon_update) have recorded on the current device:
  * VGG19_ERR_DEVICE_TIMEOUT when a bounded wait inside a kernel ran out,
- * VGG19_ERR_ARG for an id outside the classes. */
+ * VGG19_ERR_ARG for an id outside the classes (both: the first, and
+ * vgg19_last_error(NULL) names the second). */
 int vgg19_ops_status(void *stream);
 
 /* Wait for the stream and report any device-side error recorded so far:

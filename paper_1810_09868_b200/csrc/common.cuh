@@ -63,10 +63,13 @@ inline bool rows_meet(const void* a, long n, long bytes, long pitch, const void*
   return d < bytes || d + other_bytes > pitch;
 }
 
-// Reads and clears the device-side error words of the operators without a handle (logprobs.cu, q4_dense.cu, muon.cu).
-cudaError_t logprobs_take_error(int* code);
-cudaError_t q4_take_error(int* code);
-cudaError_t muon_take_error(int* code);
+// Waits for the stream; *code becomes the device error word's value and the word 0, in one exchange on the device: what a kernel on another
+// stream records meanwhile is either taken or left for the next status.  word[1] is the exchange's own.  One host thread at a time.
+cudaError_t take_error(int* word, int* code, cudaStream_t st);
+// The same for the words of calls without a handle (logprobs.cu, q4_dense.cu, muon.cu), on the current device.
+cudaError_t logprobs_take_error(int* code, cudaStream_t st);
+cudaError_t q4_take_error(int* code, cudaStream_t st);
+cudaError_t muon_take_error(int* code, cudaStream_t st);
 
 // vgg19_muon_update with the waits of its kernels (muon.cu).
 int muon_update(const vgg19_muon_tensor* tensors, int32_t count, float lr, float momentum, float decay, int32_t steps, int32_t nesterov,

@@ -32,7 +32,7 @@ namespace cg = cooperative_groups;
 namespace vgg {
 namespace {
 
-static __device__ int g_logprobs_error;  // kDevBadLabel once an id outside [0, classes) was met
+static __device__ int g_logprobs_error[2];  // kDevBadLabel once an id outside [0, classes) was met
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // A reference moves only when a value exceeds it by this much (natural units): exp(z - ref) then stays below e^4, and
@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(NT) logprobs_kernel(const FwdArgs a) {
         v = bad ? nan : empty ? -INFINITY : (to_f32(z[id]) - all.ref) - logS;
       } else {  // never used as an index
         v = nan;
-        atomicCAS(&g_logprobs_error, 0, (int)kDevBadLabel);
+        atomicCAS(g_logprobs_error, 0, (int)kDevBadLabel);
       }
     }
     a.logprob[row * a.n_ids + i] = v;
@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(kBwdThreads) logprobs_backward_kernel(const Bw
   auto load_id = [&](int i, float& g, bool& mine) {
     const int id = i + lane < a.n_ids ? a.ids[row * a.n_ids + i + lane] : VGG19_NO_CLASS;
     const bool in = (unsigned)id < (unsigned)a.classes;
-    if (!in && id != VGG19_NO_CLASS) atomicCAS(&g_logprobs_error, 0, (int)kDevBadLabel);
+    if (!in && id != VGG19_NO_CLASS) atomicCAS(g_logprobs_error, 0, (int)kDevBadLabel);
     g = in ? a.d_logprob[row * a.n_ids + i + lane] : 0.f;
     mine = in && ((id >= lo && id < hi) || (chunk == 0 && (id < sp.head || id >= sp.head + sp.nvec * V)));
     return id;
@@ -581,7 +581,7 @@ __global__ void __launch_bounds__(32 * kShortWarps) short_rows_kernel(const FwdA
         v = bad ? nan : empty ? -INFINITY : (to_f32(z[id]) - ref) - logS;
       } else {  // never used as an index
         v = nan;
-        atomicCAS(&g_logprobs_error, 0, (int)kDevBadLabel);
+        atomicCAS(g_logprobs_error, 0, (int)kDevBadLabel);
       }
     }
     a.logprob[row * a.n_ids + i] = v;
@@ -636,7 +636,7 @@ __global__ void __launch_bounds__(32 * kShortWarps) short_rows_backward_kernel(c
   for (int i = 0; i < a.n_ids; i += 32) {  // in their order
     const int id = i + lane < a.n_ids ? a.ids[row * a.n_ids + i + lane] : VGG19_NO_CLASS;
     const bool in = (unsigned)id < (unsigned)n;
-    if (!in && id != VGG19_NO_CLASS) atomicCAS(&g_logprobs_error, 0, (int)kDevBadLabel);
+    if (!in && id != VGG19_NO_CLASS) atomicCAS(g_logprobs_error, 0, (int)kDevBadLabel);
     const float g = in ? a.d_logprob[row * a.n_ids + i + lane] : 0.f;
     sum += lane_sum(g);
     for (unsigned m = __ballot_sync(0xffffffffu, in); m; m &= m - 1) {
@@ -735,13 +735,10 @@ template <typename... P> bool words(P... p) { return ((reinterpret_cast<uintptr_
 
 }  // namespace
 
-cudaError_t logprobs_take_error(int* code) {
-  cudaError_t e = cudaMemcpyFromSymbol(code, g_logprobs_error, sizeof(int));
-  if (e == cudaSuccess && *code) {
-    const int zero = 0;
-    e = cudaMemcpyToSymbol(g_logprobs_error, &zero, sizeof(int));
-  }
-  return e;
+cudaError_t logprobs_take_error(int* code, cudaStream_t st) {
+  void* word = nullptr;
+  const cudaError_t e = cudaGetSymbolAddress(&word, g_logprobs_error);
+  return e == cudaSuccess ? take_error(static_cast<int*>(word), code, st) : e;
 }
 
 }  // namespace vgg

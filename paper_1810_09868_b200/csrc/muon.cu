@@ -41,7 +41,7 @@ namespace {
 
 using namespace tc;
 
-static __device__ int g_muon_error;  // a DeviceError code once a bounded wait of a call without a handle ran out
+static __device__ int g_muon_error[2];  // a DeviceError code once a bounded wait of a call without a handle ran out
 
 // ---- sizes -----------------------------------------------------------------------------------------------------
 constexpr int BM = 128, BK = 64;                 // rows per CTA (a pair has 256), K per stage
@@ -229,7 +229,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const bool leader = rank == 0;
-  int* const error = L.waits.error ? L.waits.error : &g_muon_error;
+  int* const error = L.waits.error ? L.waits.error : g_muon_error;
   const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1, total = L.first_tile[L.count];
 
   if (threadIdx.x == 0) {
@@ -620,7 +620,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_steps_kernel(const __g
   __shared__ uint32_t tmem_base_slot;
   __shared__ int abort_flag;
   const SmallTensor& t = L.t[blockIdx.x];
-  int* const error = L.waits.error ? L.waits.error : &g_muon_error;
+  int* const error = L.waits.error ? L.waits.error : g_muon_error;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, k_stages = t.k_stages;
   if (tid == 0) {
     abort_flag = 0;
@@ -1301,13 +1301,10 @@ size_t workspace_bytes(const vgg19_muon_tensor* t, int32_t count) {
 
 }  // namespace
 
-cudaError_t muon_take_error(int* code) {
-  cudaError_t e = cudaMemcpyFromSymbol(code, g_muon_error, sizeof(int));
-  if (e == cudaSuccess && *code) {
-    const int zero = 0;
-    e = cudaMemcpyToSymbol(g_muon_error, &zero, sizeof(int));
-  }
-  return e;
+cudaError_t muon_take_error(int* code, cudaStream_t st) {
+  void* word = nullptr;
+  const cudaError_t e = cudaGetSymbolAddress(&word, g_muon_error);
+  return e == cudaSuccess ? take_error(static_cast<int*>(word), code, st) : e;
 }
 
 cudaError_t muon_vector_update(const MuonVector* v, int count, float lr, float mu, bool nesterov, cudaStream_t st) {

@@ -35,7 +35,7 @@ namespace {
 
 using namespace tc;
 
-static __device__ int g_q4_error;  // a DeviceError code once a bounded wait of a call without a handle ran out
+static __device__ int g_q4_error[2];  // a DeviceError code once a bounded wait of a call without a handle ran out
 
 constexpr int kTileRows = 16, kBlockK = 128, kBlockBytes = kTileRows * kBlockK / 2;
 constexpr int kMaxRows = 16;                 // rows of x per launch
@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 
   };
   if (ks > 1) cluster.barrier_arrive();  // waited for before the first write into another block's shared memory
   if (tid == 0) abort_flag = 0;
-  int* const error = a.waits.error ? a.waits.error : &g_q4_error;
+  int* const error = a.waits.error ? a.waits.error : g_q4_error;
   const bool starved = a.waits.starve == kStarveDense && blockIdx.x == 0;
 
   float acc[NT][4] = {};
@@ -472,13 +472,10 @@ cudaError_t q4_linear(const T* x, long ldx, long rows, int in, const void* codes
   return cudaSuccess;
 }
 
-cudaError_t q4_take_error(int* code) {
-  cudaError_t e = cudaMemcpyFromSymbol(code, g_q4_error, sizeof(int));
-  if (e == cudaSuccess && *code) {
-    const int zero = 0;
-    e = cudaMemcpyToSymbol(g_q4_error, &zero, sizeof(int));
-  }
-  return e;
+cudaError_t q4_take_error(int* code, cudaStream_t st) {
+  void* word = nullptr;
+  const cudaError_t e = cudaGetSymbolAddress(&word, g_q4_error);
+  return e == cudaSuccess ? take_error(static_cast<int*>(word), code, st) : e;
 }
 
 #define INSTANTIATE(T)                                                                                                    \

@@ -758,4 +758,19 @@ cudaError_t refresh_filter_copies(const float* params, bf16* dgrad_w, bf16* tap_
 INSTANTIATE(float)
 INSTANTIATE(bf16)
 
+namespace {
+__global__ void take_error_kernel(int* word) { word[1] = atomicExch(word, 0); }
+}  // namespace
+
+cudaError_t take_error(int* word, int* code, cudaStream_t st) {
+  *code = 0;
+  cudaError_t e = cudaStreamSynchronize(st);
+  if (e != cudaSuccess) return e;
+  take_error_kernel<<<1, 1, 0, st>>>(word);
+  e = cudaGetLastError();
+  if (e == cudaSuccess) e = cudaMemcpyAsync(code, word + 1, sizeof(int), cudaMemcpyDeviceToHost, st);
+  const cudaError_t end = cudaStreamSynchronize(st);
+  return e == cudaSuccess ? end : e;
+}
+
 }  // namespace vgg

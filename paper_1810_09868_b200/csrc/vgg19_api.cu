@@ -8,6 +8,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <mutex>
 #include <new>
 #include <string>
 #include <vector>
@@ -788,15 +789,26 @@ static int handle_free_error(int code, const char *text) { return fail(nullptr, 
 extern "C" {
 
 int vgg19_ops_status(void *stream) {
-  cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
-  int code = 0, timeout = 0, later = 0;
-  if (e == cudaSuccess) e = logprobs_take_error(&code);
-  if (e == cudaSuccess) e = q4_take_error(&timeout);
-  if (e == cudaSuccess) e = muon_take_error(&later);
-  if (!timeout) timeout = later;
+  static std::mutex one;  // status calls of several host threads
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaSuccess;
+  int id = 0, dense = 0, update = 0;
+  try {
+    const std::lock_guard<std::mutex> lock(one);
+    // all of them, whichever are set: what one call reports, none finds again
+    const cudaError_t read[] = {logprobs_take_error(&id, st), q4_take_error(&dense, st), muon_take_error(&update, st)};
+    for (cudaError_t r : read)
+      if (e == cudaSuccess) e = r;
+  } catch (...) {
+    return fail(nullptr, VGG19_ERR_CUDA, "the host refused a lock");
+  }
   if (e != cudaSuccess) return fail(nullptr, VGG19_ERR_CUDA, "reading the device status failed: %s", cudaGetErrorString(e));
-  if (timeout) return fail(nullptr, VGG19_ERR_DEVICE_TIMEOUT, "a device-side wait ran out (code %d)", timeout);
-  if (code) return fail(nullptr, VGG19_ERR_ARG, "an id outside the row's classes (its log probability is NaN)");
+  const char *which = dense && update ? "a 4-bit layer and an update" : dense ? "a 4-bit layer" : "an update";
+  const char *bad = "an id outside the row's classes (its log probability is NaN)";
+  if (dense || update)
+    return fail(nullptr, VGG19_ERR_DEVICE_TIMEOUT, "a device-side wait of %s ran out (code %d)%s%s", which, dense ? dense : update, id ? "; also " : "",
+                id ? bad : "");
+  if (id) return fail(nullptr, VGG19_ERR_ARG, "%s", bad);
   return VGG19_OK;
 }
 
@@ -1309,11 +1321,9 @@ int vgg19_saved_tensor(const vgg19_t *n, int32_t batch, int32_t mode, int32_t in
 
 int vgg19_sync_status(vgg19_t *n, void *stream) {
   if (!n) return VGG19_ERR_ARG;
-  CUDA_TRY(n, cudaStreamSynchronize(static_cast<cudaStream_t>(stream)));
   int code = 0;
-  CUDA_TRY(n, cudaMemcpy(&code, n->dev_error, sizeof code, cudaMemcpyDeviceToHost));
+  CUDA_TRY(n, take_error(n->dev_error, &code, static_cast<cudaStream_t>(stream)));
   if (code != 0) {
-    cudaMemset(n->dev_error, 0, 256);
     if (code == kDevBadLabel)
       return fail(n, VGG19_ERR_ARG, "a label outside [0, %d) reached the loss (its row's loss is NaN)", kClasses);
     if (code == kDevSplitRange)

@@ -75,3 +75,39 @@ def test_what_runs_out_is_reported_to_its_owner_alone(p, kind):
         assert torch.equal(net.forward(images), logits)
         net.sync_status()
         net.close()
+
+
+def test_one_status_reports_all_that_was_recorded(p):
+    """A bad id, a 4-bit layer's wait and an update's: the first status names them all, the next one finds none."""
+    st, ws = torch.cuda.current_stream(), scratch(p)
+    z, ids = torch.zeros(1, 10, device=DEV), torch.full((1, 1), 10, dtype=torch.int32, device=DEV)
+
+    def bad_id():
+        p.vgg19_logprobs(z, ids, torch.empty(1, 1, device=DEV), stream=st)
+
+    for record, code, words in (
+            ([bad_id], p.VGG19_ERR_ARG, ["id"]),
+            ([bad_id, p.VGG19_SELFTEST_DENSE_Q4], p.VGG19_ERR_DEVICE_TIMEOUT, ["4-bit", "id"]),
+            ([p.VGG19_SELFTEST_UPDATE, bad_id], p.VGG19_ERR_DEVICE_TIMEOUT, ["update", "id"]),
+            ([p.VGG19_SELFTEST_DENSE_Q4, p.VGG19_SELFTEST_UPDATE], p.VGG19_ERR_DEVICE_TIMEOUT, ["4-bit", "update"])):
+        for r in record:
+            r() if callable(r) else p.vgg19_selftest_operator_timeout(None, r, ws, st)
+        with pytest.raises(p.Vgg19Error) as e:
+            p.vgg19_ops_status(st)
+        assert e.value.code == code and all(w in str(e.value) for w in words), str(e.value)
+        p.vgg19_ops_status(st)
+
+
+def test_a_status_waits_for_its_own_stream_alone(p):
+    """It is read while the legacy default stream is busy: the exchange runs on the stream that is asked about."""
+    mine, other = torch.cuda.Stream(), torch.cuda.default_stream()
+    net = p.Net(32, 32, 1, p.VGG19_BF16, seed=1, mode=p.VGG19_MODE_FORWARD)
+    p.vgg19_ops_status(mine), net.sync_status(mine)
+    done = torch.cuda.Event()
+    with torch.cuda.stream(other):
+        torch.cuda._sleep(2_000_000_000)  # about a second
+        done.record()
+    p.vgg19_ops_status(mine), net.sync_status(mine)
+    assert not done.query()
+    net.close()
+    torch.cuda.synchronize()
