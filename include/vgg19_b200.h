@@ -360,7 +360,7 @@ int vgg19_conv_wgrad_static(const void *x, const void *dz, int32_t batch, int32_
  * type).  ids: device int32 [rows][n_ids], n_ids in [0,
  * VGG19_LOGPROBS_MAX_IDS] (ids and logprob may be NULL for 0).  lse and entropy
  * may be NULL.  top_k in [0, VGG19_LOGPROBS_MAX_TOP]; it may exceed the number of
- * classes.  All results are fp32 (top_id int32) and dense; sums are held in fp32.
+ * classes.  All results are fp32 (top_id int32) and dense, and overlap neither logits, ids nor one another; sums are held in fp32.
  * rows == 0 does nothing.
  *
  * An id VGG19_NO_CLASS asks for nothing (a padded row): its logprob is 0.  Any
@@ -382,7 +382,7 @@ int vgg19_logprobs(const void *logits, int32_t dtype, int64_t rows, int32_t clas
  * vgg19_logprobs gave:
  *   d z_j = sum_i g_i [j = ids_i] - p_j (sum_i g_i + w (log p_j + H)).
  * d_logits: device, the type of logits, row stride d_ld; overwritten.  It may be
- * logits itself with d_ld == ld; any other overlap is refused.  d_logprob: fp32 [rows][n_ids].  d_entropy: fp32
+ * logits itself with d_ld == ld; any other overlap with an input is refused.  d_logprob: fp32 [rows][n_ids].  d_entropy: fp32
  * [rows] or NULL (entropy may then be NULL).  Ids that name no class, VGG19_NO_CLASS
  * or others, contribute nothing (others are reported as above); a class named
  * twice gets both shares.  To differentiate the top list, pass its top_id as

@@ -63,6 +63,19 @@ inline bool rows_meet(const void* a, long n, long bytes, long pitch, const void*
   return d < bytes || d + other_bytes > pitch;
 }
 
+// Bytes from p on; none where p is null.
+struct Span {
+  const void* p;
+  long bytes;
+};
+// Whether one of the first `written` of them meets any other.
+template <int M> inline bool spans_meet(const Span (&all)[M], int written) {
+  for (int i = 0; i < written; ++i)
+    for (int j = i + 1; j < M; ++j)
+      if (rows_meet(all[i].p, all[i].bytes > 0, all[i].bytes, 0, all[j].p, all[j].bytes > 0, all[j].bytes, 0)) return true;
+  return false;
+}
+
 // Waits for the stream; *code becomes the device error word's value and the word 0, in one exchange on the device: what a kernel on another
 // stream records meanwhile is either taken or left for the next status.  word[1] is the exchange's own.  One host thread at a time.
 cudaError_t take_error(int* word, int* code, cudaStream_t st);

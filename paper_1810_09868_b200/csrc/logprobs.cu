@@ -754,6 +754,11 @@ extern "C" int vgg19_logprobs(const void* logits, int32_t dtype, int64_t rows, i
   if ((n_ids && !logprob) || (top_k && (!top_id || !top_logprob)))
     return note_error(VGG19_ERR_ARG, "null output for %d ids or the top %d", n_ids, top_k);
   if (!words(ids, logprob, lse, entropy, top_id, top_logprob)) return note_error(VGG19_ERR_ARG, "ids or an output is not aligned to 4 bytes");
+  const long elt = dtype == VGG19_FP32 ? 4 : 2, given = 4L * rows * n_ids, top = 4L * rows * top_k, each = 4L * rows;
+  const Span all[] = {{logprob, given}, {lse, each}, {entropy, each}, {top_id, top}, {top_logprob, top}, {ids, given}};
+  bool meet = spans_meet(all, 5);
+  for (int i = 0; i < 5; ++i) meet = meet || rows_meet(logits, rows, classes * elt, ld * elt, all[i].p, all[i].bytes > 0, all[i].bytes, 0);
+  if (meet) return note_error(VGG19_ERR_ARG, "an output overlaps logits, ids or another output");
   const FwdArgs a{logits, ids, logprob, lse, entropy, top_logprob, top_id, (long)ld, classes, n_ids, top_k};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e = dtype == VGG19_BF16 ? forward<bf16>(a, rows, st) : forward<float>(a, rows, st);
@@ -780,6 +785,10 @@ extern "C" int vgg19_logprobs_backward(const void* logits, int32_t dtype, int64_
   const int per = kBwdThreads * kBwdUnroll * (dtype == VGG19_BF16 ? 8 : 4);
   const int64_t chunks = (classes + per - 1) / per;
   if (rows * chunks > 0x7fffffffLL) return note_error(VGG19_ERR_SHAPE, "%lld rows of %d classes are too many", (long long)rows, classes);
+  const Span read[] = {{ids, 4L * rows * n_ids}, {d_logprob, 4L * rows * n_ids}, {lse, 4L * rows}, {entropy, 4L * rows}, {d_entropy, 4L * rows}};
+  for (const Span& s : read)
+    if (rows_meet(d_logits, rows, classes * elt, d_ld * elt, s.p, s.bytes > 0, s.bytes, 0))
+      return note_error(VGG19_ERR_ARG, "d_logits overlaps another input than logits");
   const BwdArgs a{logits, d_logits, ids, lse, entropy, d_logprob, d_entropy, (long)ld, (long)d_ld, classes, n_ids, (int)chunks};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e = dtype == VGG19_BF16 ? backward<bf16>(a, rows, st) : backward<float>(a, rows, st);

@@ -191,3 +191,29 @@ def test_the_binding_refuses_sizes_beyond_an_int(p):
 def test_the_operators_selftest_refuses(p, which, ws, nbytes, code):
     assert p.binding.load().vgg19_selftest_operator_timeout(None, which, ws, nbytes, None) == getattr(p, "VGG19_ERR_" + code)
     assert p.VGG19_SELFTEST_BYTES == 1 << 20
+
+
+# 3 rows of 10 fp32 logits, 24 apart; 2 ids and the best 4 of each row; every array on its own 4096 bytes but for what a case changes.
+def apart(**over):
+    names = ("logits", "ids", "logprob", "lse", "entropy", "top_id", "top_logprob")
+    a = dict(dtype=0, rows=3, classes=10, ld=24, n_ids=2, top_k=4, **{n: SOME + 4096 * i for i, n in enumerate(names)})
+    a.update({k: SOME + v for k, v in over.items()})
+    return logprobs_args(**a)
+
+
+@pytest.mark.parametrize("over", [
+    dict(lse=0), dict(logprob=4 * 9), dict(entropy=4 * 8), dict(top_id=-4 * 11), dict(top_logprob=4 * 57), dict(lse=4 * 24 + 4 * 22), dict(lse=4096 + 20),
+    dict(logprob=4096 - 20), dict(entropy=3 * 4096 + 8), dict(top_id=6 * 4096 + 44), dict(lse=2 * 4096 + 20), dict(top_logprob=4 * 4096 - 44)])
+def test_logprobs_refuses_overlaps(p, over):
+    assert p.binding.load().vgg19_logprobs(*apart(**over)) == p.VGG19_ERR_ARG
+    assert "overlap" in p.vgg19_last_error()
+
+
+# rows of 24 with ids, sums or gradients of the results between or in them
+@pytest.mark.parametrize("over", [
+    dict(lse=SOME + 40960), dict(entropy=SOME + 40960 + 4 * 33), dict(d_logprob=SOME + 40960 + 4 * 57), dict(ids=SOME + 40960 - 4), dict(d_entropy=SOME + 40960 + 4 * 8)])
+def test_logprobs_backward_refuses_inputs_in_its_gradient(p, over):
+    a = dict(ids=SOME + 4096, lse=SOME + 8192, entropy=SOME + 12288, d_logprob=SOME + 16384, d_entropy=SOME + 20480, d_logits=SOME + 40960)
+    a.update(over)
+    assert p.binding.load().vgg19_logprobs_backward(*backward_args(**a)) == p.VGG19_ERR_ARG
+    assert "overlap" in p.vgg19_last_error()
