@@ -410,13 +410,13 @@ size_t vgg19_q4_scale_bytes(int32_t out, int32_t in, int32_t group);
 /* Codes and scales of w: device [out][in] with row stride ld, VGG19_FP32 or
  * VGG19_BF16.  scale = bf16(largest magnitude of the group / 7), code = 8 + the
  * nearest integer (ties to even) to w / scale within -8..7; all codes 8 where the scale is
- * 0.  A group that holds a NaN or an infinity gets an infinite scale, which makes its row's results NaN. */
+ * 0.  Neither overlaps w or the other.  A group that holds a NaN or an infinity gets an infinite scale, which makes its row's results NaN. */
 int vgg19_q4_pack(const void *w, int32_t dtype, int32_t out, int32_t in, int64_t ld, int32_t group, void *codes,
                   void *scales, void *stream);
 
 /* y = W x + bias, then ReLU if `relu`: x device [rows][in] with row stride ldx, in
  * `dtype` (VGG19_FP32 or VGG19_BF16); y (or NULL): [rows][out] in that type;
- * y_f32 (or NULL): the same values as fp32; at least one, overlapping neither x nor each other.  bias: fp32 [out] or NULL.  The products are exact and
+ * y_f32 (or NULL): the same values as fp32; at least one, overlapping none of the inputs nor each other.  bias: fp32 [out] or NULL.  The products are exact and
  * summed in fp32 (fp32 activations are taken in full, as three bf16 terms).  Made for up to 16 rows, which read the
  * weights once; more rows are taken 16 at a time.  rows == 0 does nothing. */
 int vgg19_q4_linear(const void *x, int32_t dtype, int64_t rows, int32_t in, int64_t ldx, const void *codes,

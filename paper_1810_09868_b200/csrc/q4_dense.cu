@@ -510,6 +510,11 @@ int vgg19_q4_pack(const void* w, int32_t dtype, int32_t out, int32_t in, int64_t
     return note_error(VGG19_ERR_ARG, "weights are aligned to their type, codes and scales to 16 bytes");
   if (((long)((out + kTileRows - 1) / kTileRows) * kTileRows * ((in + kBlockK - 1) / kBlockK) + 7) / 8 > 0x7fffffffL)
     return note_error(VGG19_ERR_SHAPE, "%d x %d weights are too many for one call", out, in);
+  const long elt = dtype == VGG19_FP32 ? 4 : 2;
+  const Span packed[] = {{codes, (long)q4_code_bytes(out, in)}, {scales, (long)q4_scale_bytes(out, in, group)}};
+  if (spans_meet(packed, 1) || rows_meet(w, out, elt * in, elt * ld, codes, 1, packed[0].bytes, 0) ||
+      rows_meet(w, out, elt * in, elt * ld, scales, 1, packed[1].bytes, 0))
+    return note_error(VGG19_ERR_ARG, "codes and scales overlap the weights or one another");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e = dtype == VGG19_BF16 ? q4_pack(static_cast<const bf16*>(w), ld, out, in, group, codes, scales, st)
                                             : q4_pack(static_cast<const float*>(w), ld, out, in, group, codes, scales, st);
@@ -534,9 +539,9 @@ int vgg19_q4_linear(const void* x, int32_t dtype, int64_t rows, int32_t in, int6
       reinterpret_cast<uintptr_t>(bias) % 4 || reinterpret_cast<uintptr_t>(codes) % 16 || reinterpret_cast<uintptr_t>(scales) % 16)
     return note_error(VGG19_ERR_ARG, "x, bias and outputs are aligned to their types, codes and scales to 16 bytes");
   const long x_bytes = (long)elt * in, x_pitch = (long)elt * ldx, y_bytes = (long)elt * out * rows, f_bytes = 4L * out * rows;
-  if (rows_meet(x, rows, x_bytes, x_pitch, y, 1, y_bytes, 0) || rows_meet(x, rows, x_bytes, x_pitch, y_f32, 1, f_bytes, 0) ||
-      rows_meet(y, 1, y_bytes, 0, y_f32, 1, f_bytes, 0))
-    return note_error(VGG19_ERR_ARG, "an output overlaps x or the other output");
+  const Span all[] = {{y, y_bytes}, {y_f32, f_bytes}, {codes, (long)q4_code_bytes(out, in)}, {scales, (long)q4_scale_bytes(out, in, group)}, {bias, 4L * out}};
+  if (rows_meet(x, rows, x_bytes, x_pitch, y, 1, y_bytes, 0) || rows_meet(x, rows, x_bytes, x_pitch, y_f32, 1, f_bytes, 0) || spans_meet(all, 2))
+    return note_error(VGG19_ERR_ARG, "an output overlaps x, the weights, the bias or the other output");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e =
       dtype == VGG19_BF16

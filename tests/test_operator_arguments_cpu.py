@@ -217,3 +217,24 @@ def test_logprobs_backward_refuses_inputs_in_its_gradient(p, over):
     a.update(over)
     assert p.binding.load().vgg19_logprobs_backward(*backward_args(**a)) == p.VGG19_ERR_ARG
     assert "overlap" in p.vgg19_last_error()
+
+
+# 10 x 100 weights in groups of 32: 1024 bytes of codes, 128 of scales; two rows of x
+@pytest.mark.parametrize("over", [dict(y=8192 + 1020), dict(y=8192 - 36), dict(y_f32=12288 + 124), dict(y_f32=12288 - 76), dict(y=16384 + 36), dict(y_f32=16384 - 76)])
+def test_q4_linear_refuses_outputs_over_weights(p, over):
+    a = dict(x=0, dtype=1, rows=2, in_=100, ldx=116, codes=8192, scales=12288, out=10, group=32, bias=16384, relu=0, y=20480, y_f32=24576, stream=None)
+    a.update(over)
+    for k in ("x", "codes", "scales", "bias", "y", "y_f32"):
+        a[k] += SOME
+    assert p.binding.load().vgg19_q4_linear(*a.values()) == p.VGG19_ERR_ARG
+    assert "overlap" in p.vgg19_last_error()
+
+
+@pytest.mark.parametrize("over", [dict(codes=0), dict(codes=3968), dict(codes=5120 - 1008), dict(scales=8192 + 1008), dict(scales=8192 - 112), dict(scales=1056), dict(scales=4096 + 3888)])
+def test_q4_pack_refuses_overlaps(p, over):
+    a = dict(w=4096, dtype=0, out=10, in_=100, ld=100, group=32, codes=8192, scales=12288, stream=None)
+    a.update({k: v + (4096 if v < 4096 else 0) for k, v in over.items()})
+    for k in ("w", "codes", "scales"):
+        a[k] += SOME
+    assert p.binding.load().vgg19_q4_pack(*a.values()) == p.VGG19_ERR_ARG
+    assert "overlap" in p.vgg19_last_error()
