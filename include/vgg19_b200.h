@@ -453,7 +453,7 @@ int vgg19_muon_update(const vgg19_muon_tensor *tensors, int32_t count, float lr,
  * vgg19_sgd_step: every weight tensor as a matrix ([Cout][9 * Cin] or [out][in]) by the update above,
  * every bias b <- b - bias_lr * u with its own momentum and no decay, then the bf16 copy and every filter copy the kernels read.
  * grads: device fp32, vgg19_param_count() elements; momentum: the same size, kept by the caller (zeros at first).
- * workspace of vgg19_muon_step_bytes(net). */
+ * workspace of vgg19_muon_step_bytes(net).  None of them overlaps another. */
 size_t vgg19_muon_step_bytes(const vgg19_t *net);
 int vgg19_muon_step(vgg19_t *net, const float *grads, float *momentum_buffer, float lr, float momentum, float decay,
                     float bias_lr, int32_t steps, int32_t nesterov, void *workspace, size_t bytes, void *stream);

@@ -942,6 +942,11 @@ int vgg19_muon_step(vgg19_t *n, const float *grads, float *momentum_buffer, floa
   if (!n) return VGG19_ERR_ARG;
   if (!grads || !momentum_buffer || !(bias_lr == bias_lr))
     return fail(n, VGG19_ERR_ARG, "null gradient or momentum, or NaN bias learning rate");
+  // (the update itself looks at the weight tensors; between them lie the biases)
+  const long all = 4 * (long)n->n_params;
+  const Span used[] = {{momentum_buffer, all}, {workspace, (long)vgg19_muon_step_bytes(n)}, {n->params, all},
+                       {n->cfg.dtype == VGG19_BF16 ? n->params_t : nullptr, all / 2}, {grads, all}};
+  if (spans_meet(used, 4)) return fail(n, VGG19_ERR_ARG, "gradients, momentum, workspace and parameters overlap");
   vgg19_muon_tensor t[kLayers];
   muon_tensors(n, grads, momentum_buffer, t);
   const int rc = muon_update(t, kLayers, lr, momentum, decay, steps, nesterov, workspace, bytes, waits_of(n->dev_error), stream);

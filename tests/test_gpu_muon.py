@@ -349,3 +349,19 @@ def test_many_tiles_alone_and_together(p):
         alone = copies(before[k])
         run(p, [alone], fill=0)
         assert torch.equal(alone[0], ts[k][0])
+
+
+def test_network_step_refuses_a_workspace_over_the_last_bias(p):
+    """The update's tensors are the weights; a workspace that begins in the last bias's momentum meets none of them."""
+    net = p.Net(32, 32, 1, p.VGG19_BF16, seed=1)
+    n, need = net.n_params * 4, p.vgg19_muon_step_bytes(net.handle)
+    memory = torch.zeros(n + need, dtype=torch.uint8, device=DEV)
+    momentum, grads = memory[:n].view(torch.float32), torch.zeros(net.n_params, device=DEV)
+    ws = memory[(n - 3000) // 256 * 256:]
+    assert ws.data_ptr() >= momentum.data_ptr() + 4 * net.param_slices()[37][0] and ws.numel() >= need
+    for g, m, w in ((grads, momentum, ws), (momentum, momentum, torch.empty(need, dtype=torch.uint8, device=DEV)),
+                    (ws[:n].view(torch.float32), momentum, torch.empty(need, dtype=torch.uint8, device=DEV))):
+        with pytest.raises(p.Vgg19Error) as e:
+            p.vgg19_muon_step(net.handle, g, m, 0.1, 0.9, 0.0, 0.1, 5, True, w, w.numel(), torch.cuda.current_stream())
+        assert e.value.code == p.VGG19_ERR_ARG and "overlap" in str(e.value)
+    net.close()
