@@ -6,9 +6,12 @@
 // Every p(A_k) is a polynomial of A_0 = X_0 X_0^T, so the products commute and the iteration can run on m x m symmetric
 // matrices: Q <- p(A) Q, A <- p(A) A p(A), and X = Q X_0 once at the end.  With r = n / m columns per row a step then
 // costs four symmetric products (half a product each) instead of 3 r + 1.  A alone forgets singular values below the square
-// root of its precision, which the iteration amplifies up to 3.4 times a step: so after every three steps X is formed and
-// A taken from it anew (five steps: 6 r + 14 such halves against 15 r + 5).  Measured against 64 bits on gradients of low rank with noise:
-// 4e-6 to 6e-6 relative, plain fp32 products 1.1e-5 to 3.9e-5; without the restart 3e-5 to 1.8e-4.
+// root of its precision, which the iteration amplifies up to 3.4 times a step: so after every two steps, at first three, X is formed
+// and A taken from it anew (five steps: 6 r + 14 such halves against 15 r + 5).  Measured against 64 bits, five steps: 4e-6 to 7e-6
+// relative on gradients of low rank with noise, where plain fp32 products give 6e-6 to 3.9e-5 (without the restart 3e-5 to 1.8e-4),
+// and 4e-6 to 7e-6 on Gaussian ones, where plain fp32 gives 1.6e-6 (70 x 200) to 4.8e-6 (4096 x 4096): there 22 bits are fewer than 24.
+// Ten steps: 9e-6 to 1.9e-5 on Gaussian matrices, fp32 2.5e-6 to 1.3e-5.  The iteration does not settle: a singular value near 0.868 has its error multiplied
+// by 1.6 a step, in any arithmetic.
 //
 // Precision.  A matrix is kept as two fp16 planes hi + lo of its values times a power of two (22 bits; the scales below
 // keep every entry inside fp16's range), a product is hi hi + hi lo + lo hi in fp32, on tcgen05.  The tensor core's fp32
@@ -71,7 +74,10 @@ constexpr int kMaxTensors = 20, kMaxProblems = 2 * kMaxTensors;
 // polynomial's range on [0, 1.47]) |p| <= 3.45, |p A| <= 1.3, and Q of two and three steps is below 11.9 and 41.
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kScaleX = 4096.f, kScaleA = 16384.f, kScaleP = 8192.f, kScaleQ2 = 4096.f, kScaleQ3 = 1024.f;
-constexpr int kStepsPerGram = 3;
+// Steps between two Gram matrices: two, and three at first where their number is odd.  At first the singular values are small and Q is close to
+// its q0 I; later they are around one, Q = q0 I + S is too, and S is what cancels q0 = a^k: 12 after two steps, 41 after three, and that many
+// times the rounding.  (Eight steps of Gaussian matrices as 3 + 3 + 2: 3e-5 to 1.1e-4 from 64 bits, plain fp32 products 2e-6 to 1e-5.)
+__host__ __device__ constexpr int steps_of_group(int done, int steps) { return steps == 1 ? 1 : done == 0 && steps % 2 ? 3 : 2; }
 // R = b A + c A A from A: the product's factor and the addend's, as Problem has them; the scale of S after step k.
 __host__ __device__ constexpr float poly_alpha() { return kC * kScaleP / (kScaleA * kScaleA); }
 __host__ __device__ constexpr float poly_c1() { return kB * kScaleP / kScaleA / poly_alpha(); }
@@ -1127,8 +1133,7 @@ cudaError_t update_batch(const vgg19_muon_tensor* given, const int count, const 
   L.waits = o.waits;
   int x = kX0;
   for (int done = 0; done < o.steps;) {
-    // groups of at most three steps, as even as they go
-    const int groups = (o.steps - done + kStepsPerGram - 1) / kStepsPerGram, group = (o.steps - done + groups - 1) / groups;
+    const int group = steps_of_group(done, o.steps);
     GramFinish finish{};
     int finish_blocks = 0;
     for (int i = 0; i < count; ++i) {

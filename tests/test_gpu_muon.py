@@ -365,3 +365,55 @@ def test_network_step_refuses_a_workspace_over_the_last_bias(p):
             p.vgg19_muon_step(net.handle, g, m, 0.1, 0.9, 0.0, 0.1, 5, True, w, w.numel(), torch.cuda.current_stream())
         assert e.value.code == p.VGG19_ERR_ARG and "overlap" in str(e.value)
     net.close()
+
+
+def typical_bound(u, steps):
+    """What errors of 8 * 2^-22 of X a step become, relative to the last X.  In the singular vectors of X: the error of a singular value, taken as one
+    sign all along, since the tensor core truncates its sums, grows by f'(s); one between singular values i and j by the divided difference
+    of f or (its antisymmetric part) of f(s_i) + f(s_j) over s_i + s_j, taken as independent from step to step."""
+    x = u.double() / u.double().norm()
+    x = x if x.shape[0] <= x.shape[1] else x.T
+    orbit = [torch.linalg.eigvalsh(x @ x.T).clamp_min(0).sqrt()]
+    for _ in range(steps):
+        s = orbit[-1]
+        orbit.append(A * s + B * s ** 3 + C * s ** 5)
+    eta, own, grow, pairs, between = 8 * 2.0 ** -22, 0.0, 1.0, 1.0, 0.0
+    for s, y in zip(reversed(orbit[:-1]), reversed(orbit[1:])):
+        own = own + eta * y.abs() * grow
+        between += (eta * float(y.norm())) ** 2 * (float((pairs ** 2).mean()) if torch.is_tensor(pairs) else 1.0)
+        slope = (A + 3 * B * s ** 2 + 5 * C * s ** 4).abs()
+        grow = grow * slope
+        d = s[:, None] - s[None]
+        near = d.abs() < 1e-9
+        divided = torch.where(near, slope[:, None], ((y[:, None] - y[None]) / torch.where(near, 1.0, d)).abs())
+        pairs = pairs * torch.maximum(divided, ((y[:, None] + y[None]) / (s[:, None] + s[None])).abs())
+    return math.sqrt(float(own.square().sum()) + between) / float(orbit[-1].norm())
+
+
+@pytest.mark.parametrize("steps", [5, 6, 8, 10, 13, 16])
+@pytest.mark.parametrize("rows,cols,rank", [(70, 200, None), (200, 330, None), (530, 300, None), (200, 330, 30), (530, 300, 30), (1290, 3000, None), (3000, 1290, None),
+                                            (2048, 2048, None), (1290, 3000, 100), (2048, 2048, 100)])
+def test_the_direction_itself(p, rows, cols, rank, steps):
+    """w = 0 and lr = 1: the result is X.  Gaussian gradients within the bound above; those of low rank with noise, whose small singular values amplify
+    what is lost on the large ones, within four times plain fp32, the ratio of the operands' steps."""
+    torch.backends.cuda.matmul.allow_tf32 = False
+    t = tensors(rows, cols, seed=7, rank=rank, w16=False)
+    t[0].zero_()
+    before = copies(t)
+    run(p, [t], lr=1.0, decay=0.0, steps=steps)
+    want, m, _ = reference(before, 1.0, 0.95, 0.0, steps, True)
+    err = float((t[0].double() - want).norm() / want.norm())
+    if rank is None:
+        tol = typical_bound(before[2].double() + 0.95 * m, steps)
+    else:
+        plain, _, _ = reference(before, 1.0, 0.95, 0.0, steps, True, torch.float32)
+        tol = 4 * float((plain.double() - want).norm() / want.norm()) + 2.0 ** -20
+    print(f"{rows} x {cols} rank {rank}, {steps} steps: {err:.2e}, bound {tol:.2e}")
+    assert tol < 0.01
+    assert err <= tol
+
+
+@pytest.mark.parametrize("rows,cols,rank", [(1290, 3000, None), (2048, 2048, None), (2048, 2048, 100), (3000, 1290, 100), (4096, 4096, None), (4096, 4096, 100)])
+def test_as_close_as_fp32_at_the_size_of_dense_layers(p, rows, cols, rank):
+    """Chains of four stages, tiles on and above the diagonal: held to what test_as_close_as_fp32 asks of smaller matrices."""
+    test_as_close_as_fp32(p, rows, cols, rank)
