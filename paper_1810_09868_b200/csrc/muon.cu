@@ -374,11 +374,15 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
       const int k_stages = tile.k1 - tile.k0, chain = chain_stages<FINAL>(k_stages);
       // the sums start from what is added to the product: its loads pass while the first chain runs
       float sum[CW];
-      if (FINAL && p.w_vec && lane < rows) {  // the weights of this lane's row come from far: have them nearer by the time they are updated
-        const char* w = reinterpret_cast<const char*>(p.w + (i0 + lane) * p.w_ld + j0);
+      if (FINAL && rows > 0) {  // the weights of the warp's rows come from far: have them nearer by the time they are updated
 #pragma unroll
-        for (int c = 0; c < CW; c += 32)
-          if (c < cols) asm volatile("prefetch.global.L2 [%0];" ::"l"(w + c * 4));
+        for (int c = 0; c < CW; c += 32) {
+          if (p.transposed) {  // a row of w per column, 32 elements of each
+            if (c + lane < cols) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.w + (j0 + c + lane) * p.w_ld + i0));
+          } else if (p.w_vec && lane < rows && c < cols) {
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(p.w + (i0 + lane) * p.w_ld + j0 + c));
+          }
+        }
       }
       if (p.add1 && rows > 0 && cols > 0) {
         add_planes<true, CW>(sum, p.add1 + i0 * p.ld + j0, p.plane, (int)p.ld, rows, cols, p.c1, piece, lane);
