@@ -338,11 +338,17 @@ def _calls():
     global _tensor_calls
     if _tensor_calls is None:
         load()
-        import torch  # noqa: F401  (its libraries come first)
+        import importlib.util
+
+        from .build import calls_path
+        path = calls_path()  # (imports torch, whose libraries come first)
         try:
-            from . import _tensor_calls as module
+            spec = importlib.util.spec_from_file_location(__package__ + "._tensor_calls", path)
+            module = importlib.util.module_from_spec(spec)
+            spec.loader.exec_module(module)
         except ImportError as e:
-            raise RuntimeError("_tensor_calls is missing or of another torch: build it with `python -c 'import __graft_entry__ as g; g.build()'`") from e
+            raise RuntimeError(f"{path}, the compiled calls for this torch and this Python, cannot be loaded: build them with "
+                               "`python -c 'import __graft_entry__ as g; g.build()'`") from e
         _tensor_calls = module
     return _tensor_calls
 

@@ -9,7 +9,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libvgg19_b200.so")
-CALLS, CALLS_SOURCE = os.path.join(PKG, "_tensor_calls.so"), os.path.join(CSRC, "tensor_calls.cpp")
+CALLS_SOURCE = os.path.join(CSRC, "tensor_calls.cpp")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared", "--threads", "0"]
@@ -37,10 +37,20 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def calls_path() -> str:
+    """The compiled calls of this interpreter and this torch: they read torch's own objects, whose layout is no interface."""
+    import sys
+
+    import torch
+    tag = f"{sys.implementation.cache_tag}-torch{torch.__version__}-{(torch.version.git_version or 'local')[:8]}-abi{int(torch._C._GLIBCXX_USE_CXX11_ABI)}"
+    return os.path.join(PKG, f"_tensor_calls.{tag}.so")
+
+
 def build_calls(force: bool = False) -> str:
     """Compile csrc/tensor_calls.cpp, which reads torch tensors, against the installed torch's headers."""
     deps = (CALLS_SOURCE, os.path.join(ROOT, "include", "vgg19_b200.h"))
-    if force or not os.path.exists(CALLS) or any(os.path.getmtime(d) > os.path.getmtime(CALLS) for d in deps):
+    path = calls_path()
+    if force or not os.path.exists(path) or any(os.path.getmtime(d) > os.path.getmtime(path) for d in deps):
         import sysconfig
 
         import torch
@@ -51,7 +61,9 @@ def build_calls(force: bool = False) -> str:
         cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
         for i in include:
             cmd += ["-isystem", i]
-        cmd += ["-o", CALLS, CALLS_SOURCE, "-L" + os.path.join(where, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda",
+        made = f"{path}.{os.getpid()}"
+        cmd += ["-o", made, CALLS_SOURCE, "-L" + os.path.join(where, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda",
                 "-L" + PKG, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"]
         subprocess.run(cmd, check=True)
-    return CALLS
+        os.replace(made, path)  # (a process that has the old one open keeps it)
+    return path
