@@ -536,7 +536,7 @@ int check_batch(vgg19 *n, int batch, int mode, size_t extra) {
   return VGG19_OK;
 }
 
-int refresh_filter_copies(vgg19 *n, cudaStream_t st);
+int refresh_filter_copies(vgg19 *n, cudaStream_t st, bool answers = true);
 
 template <typename T>
 int enqueue(vgg19 *n, int mode, const PassArgs &a, cudaStream_t st, int *launches) {
@@ -574,9 +574,10 @@ int enqueue(vgg19 *n, int mode, const PassArgs &a, cudaStream_t st, int *launche
           pass.ok(sgd_update<T>(n->params + run0, b.grads + run0, copy ? copy + run0 : copy, 0.f, skip0 - run0, st, lr), 1);
         if (skip) run0 = n->fc[i].b_off;  // the layer's bias follows its weights
       }
-      int rc = refresh_filter_copies(n, st);
+      const bool last = k + 1 == a.steps;
+      int rc = refresh_filter_copies(n, st, last);
       if (rc != VGG19_OK) return rc;
-      pass.launches += (n->use_tc ? 2 : 0) + (n->q4 ? kFcLayers : 0);
+      pass.launches += (n->use_tc ? 2 : 0) + (n->q4 && last ? kFcLayers : 0);
     }
   }
   if (launches) *launches = pass.launches;
@@ -641,10 +642,11 @@ void drop_graphs(vgg19 *n) {
 }
 
 // The filter copies the kernels read besides the storage-type parameters (rotated filters of the input
-// gradients, tap-major filters, the padded first-layer filter), rebuilt from the fp32 master on `st`.
-int refresh_filter_copies(vgg19 *n, cudaStream_t st) {
+// gradients, tap-major filters, the padded first-layer filter), rebuilt from the fp32 master on `st`; and, where
+// `answers`, the 4-bit copies that only forward-only passes read (half a gigabyte of weights at 224x224).
+int refresh_filter_copies(vgg19 *n, cudaStream_t st, bool answers) {
   const bool h = n->cfg.dtype == VGG19_BF16;
-  if (n->q4)
+  if (n->q4 && answers)
     for (int i = 0; i < kFcLayers; ++i) {
       const FcLayer &f = n->fc[i];
       CUDA_TRY(n, q4_pack<float>(n->params + f.w_off, f.In, f.Out, f.In, VGG19_DENSE_Q4_GROUP, n->q4 + n->q4_codes[i],

@@ -349,3 +349,30 @@ def test_larger_sizes_for_several_rows(p, rows, out, in_, group, dtype):
     again = torch.empty_like(yf)
     p.vgg19_q4_linear(x, codes, scales, out, group, None, False, None, again, st)
     assert torch.equal(again, yf)
+
+
+@pytest.mark.parametrize("flags_name", ["recorded", "VGG19_FLAG_NO_GRAPH"])
+def test_training_packs_once(p, flags_name):
+    """k steps as one program pack the three dense layers once, behind the last: nothing in between reads the 4-bit copies."""
+    import seeded_inputs as si
+    params = si.vgg19_params(32, 32, seed=0, bf16_exact=True)
+    batch, steps = 2, 3
+    images = torch.from_numpy(si.images(batch * steps, 32, 32, seed=1, bf16_exact=True)).to(DEV).to(torch.bfloat16)
+    labels = torch.from_numpy(si.labels(batch * steps, seed=2)).to(DEV)
+    flags = 0 if flags_name == "recorded" else p.VGG19_FLAG_NO_GRAPH
+    nets = [p.Net(32, 32, batch, p.VGG19_BF16, params=params, flags=f, mode=p.VGG19_MODE_TRAIN) for f in (flags, flags | p.VGG19_FLAG_DENSE_Q4)]
+    losses, st, count = torch.empty(steps, device=DEV), torch.cuda.Stream(), []
+    torch.cuda.synchronize()
+    for net in nets:
+        p.vgg19_train_steps(net.handle, images, labels, batch, steps, 1e-3, losses, st)
+        net.sync_status(st)
+        count.append(p.vgg19_launch_count(net.handle, p.VGG19_MODE_TRAIN))
+    assert count[1] - count[0] == 3
+    flat = [np.empty(net.n_params, dtype=np.float32) for net in nets]
+    for net, f in zip(nets, flat):
+        p.vgg19_get_params(net.handle, f)
+    assert np.array_equal(*flat) and not np.array_equal(flat[0], params)
+    fresh = p.Net(32, 32, batch, p.VGG19_BF16, params=flat[1], flags=p.VGG19_FLAG_DENSE_Q4)
+    assert torch.equal(nets[1].forward(images[:batch]), fresh.forward(images[:batch]))
+    for net in nets + [fresh]:
+        net.close()
