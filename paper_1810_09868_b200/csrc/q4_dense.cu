@@ -116,11 +116,13 @@ __device__ __forceinline__ uint4 load_now(const uint4* p) {
 constexpr int kRing = 2;  // copies on their way
 template <int PER, int SLOT> __host__ __device__ constexpr int slot_bytes() { return SLOT * (kBlockBytes + kTileRows * PER * 2); }
 
-template <int WARPS> constexpr int kPerSm = 24 / WARPS;  // resident blocks that registers are kept for
+// Resident blocks that registers are kept for, which is also how many the plan counts on (counting on three where there is room for two
+// took 30.4 us for one row of fp32, 13196 -> 7140, where 20.8 are enough; 33.5 against 24.1 for thirteen of bf16, 4268 -> 14582).
+template <typename T, int NT, int WARPS> constexpr int kResident = NT == 2 || Terms<T>::N == 3 ? 2 : 24 / WARPS;
 
 // NT: tiles of eight rows of x.  GROUP: 32, 64 or 128 weights a scale.  RW x KW warps: row tiles, warps to a tile.  SLOT: blocks a copy.
 template <typename T, int GROUP, int NT, int RW, int KW, int SLOT>
-__global__ void __launch_bounds__(32 * RW * KW, NT == 2 || Terms<T>::N == 3 ? 2 : kPerSm<RW * KW>) q4_linear_kernel(const Q4Args a) {
+__global__ void __launch_bounds__(32 * RW * KW, kResident<T, NT, RW * KW>) q4_linear_kernel(const Q4Args a) {
   constexpr int TERMS = Terms<T>::N, PER = kBlockK / GROUP, USTEP = GROUP / 32, kThreads = 32 * RW * KW, STEP = KW * SLOT;
   extern __shared__ __align__(128) unsigned char smem[];  // the rings, then x
   __shared__ float part[KW][RW][NT * 8][kTileRows];
@@ -368,7 +370,7 @@ template <typename T, int GROUP, int NT, int RW, int KW, int SLOT> struct Shape 
       const size_t smem = kRings + a.rows * Terms<T>::N * (stage * kBlockK * 2 + 64);
       const long n = (long)groups * ks, per = (share + KW - 1) / KW;
       long resident = (220 << 10) / (smem + kStatic + 1024);
-      if (resident > 24 / (RW * KW)) resident = 24 / (RW * KW);
+      if (resident > kResident<T, NT, RW * KW>) resident = kResident<T, NT, RW * KW>;
       const long sms = ks > 2 ? 141 : 148, each = (n + sms - 1) / sms;  // (a cluster stays within a part of the GPU, and some of a part's SMs stay empty)
       const long rounds = (each + resident - 1) / resident, warps = (each < resident ? each : resident) * RW * KW;
       const double cost = rounds * (per + 3) * (warps > 20 ? warps : 20) * (SLOT == 4 ? 1.0 : 1.1);

@@ -376,3 +376,10 @@ def test_training_packs_once(p, flags_name):
     assert torch.equal(nets[1].forward(images[:batch]), fresh.forward(images[:batch]))
     for net in nets + [fresh]:
         net.close()
+
+
+# Sizes whose plan counts on how many blocks of a launch an SM holds.
+@pytest.mark.parametrize("rows,out,in_,group,dtype", [(1, 7140, 3196, 128, "fp32"), (13, 14582, 1268, 128, "bf16"), (2, 4036, 1781, 128, "fp32"), (11, 6439, 960, 32, "bf16"),
+                                                      (3, 8427, 1290, 32, "fp32"), (10, 5928, 1717, 32, "bf16")])
+def test_sizes_of_more_blocks_than_fit_at_once(p, rows, out, in_, group, dtype):
+    test_larger_sizes_for_several_rows(p, rows, out, in_, group, dtype)
