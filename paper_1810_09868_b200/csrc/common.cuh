@@ -38,13 +38,12 @@ enum DeviceError : int {
 constexpr long long kWaitLimitCycles = 4000ll * 1000ll * 1000ll;  // about two seconds of SM clock
 
 // How the waits of an operator's kernels end when what they wait for does not come, and where that is recorded: in a network's error word for
-// its own calls, in the operator's for calls without a handle (null).  Starved, the first block (or pair) of a launch asks
-// for none of its copies, so that its waits are certain to run out: for the self-test alone.
-enum Starve : int { kStarveNone = 0, kStarveProducts = 1, kStarveSmallSteps = 2, kStarveDense = 3 };
+// its own calls, in the operator's for calls without a handle (null).  A copy's barrier expects `signals` signals and gets one: two, and
+// the waits are certain to run out, for the self-test.
 struct Waits {
   int* error = nullptr;
   long long limit_cycles = kWaitLimitCycles;
-  int starve = kStarveNone;
+  int signals = 1;
 };
 
 // Sets the text vgg19_last_error(NULL) gives and returns `code`: for entry points without a handle.
@@ -86,7 +85,7 @@ cudaError_t muon_take_error(int* code, cudaStream_t st);
 
 // vgg19_muon_update with the waits of its kernels (muon.cu).
 int muon_update(const vgg19_muon_tensor* tensors, int32_t count, float lr, float momentum, float decay, int32_t steps, int32_t nesterov,
-                void* workspace, size_t bytes, const Waits& waits, void* stream);
+                void* workspace, size_t bytes, const Waits& products, const Waits& small_steps, void* stream);
 
 // m <- mu m + g, w <- w - lr (g + mu m or m), w16 the rounded copy (or null), for each vector (muon.cu).
 struct MuonVector {

@@ -29,7 +29,7 @@
 //
 // Measured (B200, five steps): the dense layers of a 224 x 224 network (4096 x 25088, 4096 x 4096, 1000 x 4096) in 12.8 ms, of which
 // 0.43 ms momentum, norm and X_0 at 6.9 TB/s; 14.7 TFLOP of fp16 products at 1.19 PFLOP/s, 0.86 of the measured sustained rate
-// under the power cap that bounds them.  The sixteen filters in 0.66 ms: launches of 15 to 25 us, each a chain of latencies (3 us
+// under the power cap that bounds them (the tensor pipe of a 4096 x 8192 Gram product is active 79 % of the time, at 1.58 GHz).  The sixteen filters in 0.66 ms: launches of 15 to 25 us, each a chain of latencies (3 us
 // from one launch to the next, 5 us for the addends beside the stages on an SM's 64 bytes a cycle from L2, 0.8 us a stage, 4 us of stores).
 #include <cuda_fp16.h>
 
@@ -89,6 +89,9 @@ __device__ __forceinline__ void behind_previous() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
+
+// Once per block, of a wait that ran out.
+__device__ __noinline__ void report(const Waits& waits, int code) { atomicCAS(waits.error ? waits.error : g_muon_error, 0, code); }
 
 // ---- one product ---------------------------------------------------------------------------------------------
 // D[i][j] = alpha * (c1 add1[i][j] + c2 add2[i][j] + sum_k A[i][k] B[j][k]) (or B[k][j]: b_mn), m x n.
@@ -230,17 +233,16 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
   auto acc_empty_bar = [&](int b) { return bars + 8u * (2 * STAGES + 2 + b); };  // used in the even CTA
   const uint32_t drain_bar = bars + 8u * (2 * STAGES + 4);
   __shared__ uint32_t tmem_base_slot;
-  __shared__ int abort_flag;
+  __shared__ int abort_flag, ran_out;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const bool leader = rank == 0;
-  int* const error = L.waits.error ? L.waits.error : g_muon_error;
   const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1, total = L.first_tile[L.count];
 
   if (threadIdx.x == 0) {
-    abort_flag = 0;
-    for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    abort_flag = ran_out = 0;
+    for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), L.waits.signals); mbar_init(empty_bar(s), 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(acc_full_bar(b), 1); mbar_init(acc_empty_bar(b), 16); }  // the epilogue warps of both CTAs
     mbar_init(drain_bar, 1);
     mbar_fence_init();
@@ -266,14 +268,14 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
       for (int s = 0; s < STAGES; ++s) fills[s] = 0;
       int stage = 0, pi = 0;
       uint32_t phase = 0;
-      bool ok = !(L.waits.starve == kStarveProducts && pair == 0);
+      bool ok = true;
       for (int w = pair; w < total && ok; w += n_pairs) {
         while (w >= L.first_tile[pi + 1]) ++pi;
         const Problem& p = L.p[pi];
         const Tile tile = find_tile<BN>(p, w - L.first_tile[pi]);
         const int row = (2 * tile.i + (int)rank) * BM, col = tile.j * BN + (int)rank * (BN / 2), mn = p.b_mn;
         for (int kb = tile.k0; kb < tile.k1; ++kb) {
-          if (!mbar_wait(empty_bar(stage), phase ^ 1, &abort_flag, error, kDevTimeoutStageFree, L.waits.limit_cycles)) { ok = false; break; }
+          if (!mbar_wait(empty_bar(stage), phase ^ 1, &abort_flag, &ran_out, kDevTimeoutStageFree, L.waits.limit_cycles)) { ok = false; break; }
           const uint32_t sa = smem_base + stage * STAGE_BYTES, sb = sa + kOperandBytes;
           const uint32_t full = map_to_cta(full_bar(stage), 0);
           // the even CTA announces the bytes of both CTAs' copies; what lies outside a matrix arrives as zeros
@@ -324,11 +326,11 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
         for (int kb0 = 0, kb1; kb0 < k_stages && ok; kb0 = kb1, ++chunk) {
           kb1 = min(kb0 + chain, k_stages);
           const int buf = chunk & 1;
-          if (!mbar_wait(acc_empty_bar(buf), ((chunk >> 1) & 1) ^ 1, &abort_flag, error, kDevTimeoutTmemFree, L.waits.limit_cycles)) { ok = false; break; }
+          if (!mbar_wait(acc_empty_bar(buf), ((chunk >> 1) & 1) ^ 1, &abort_flag, &ran_out, kDevTimeoutTmemFree, L.waits.limit_cycles)) { ok = false; break; }
           tc_fence_after();
           const uint32_t d = tmem_base + (uint32_t)(buf * BN);
           for (int kb = kb0; kb < kb1; ++kb) {
-            if (!mbar_wait(full_bar(stage), phase, &abort_flag, error, kDevTimeoutTmaFull, L.waits.limit_cycles)) { ok = false; break; }
+            if (!mbar_wait(full_bar(stage), phase, &abort_flag, &ran_out, kDevTimeoutTmaFull, L.waits.limit_cycles)) { ok = false; break; }
             tc_fence_after();
             const uint32_t sa = smem_base + stage * STAGE_BYTES, sb = sa + kOperandBytes;
             const uint64_t ah = smem_desc_sw128(sa, 16), al = smem_desc_sw128(sa + kPlaneBytes, 16);
@@ -393,7 +395,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
       }
       for (int kb0 = 0; kb0 < k_stages; kb0 += chain, ++chunk) {
         const int buf = chunk & 1;
-        if (!__all_sync(0xffffffffu, mbar_wait(acc_full_bar(buf), (chunk >> 1) & 1, &abort_flag, error, kDevTimeoutAccum, L.waits.limit_cycles))) { ok = false; break; }
+        if (!__all_sync(0xffffffffu, mbar_wait(acc_full_bar(buf), (chunk >> 1) & 1, &abort_flag, &ran_out, kDevTimeoutAccum, L.waits.limit_cycles))) { ok = false; break; }
         tc_fence_after();
         const uint32_t src = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + group * CW);
 #pragma unroll
@@ -543,6 +545,7 @@ split_product_pair_kernel(const __grid_constant__ Launch<N> L) {
   tc_fence_before();
   __syncthreads();
   cluster_sync_all();
+  if (threadIdx.x == 0 && ran_out) report(L.waits, ran_out);
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
@@ -628,13 +631,12 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_steps_kernel(const __g
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t A = base, R = base + kSmallBytes, S = R + kSmallBytes, load_bar = S + kSmallBytes, done_bar = load_bar + 8;
   __shared__ uint32_t tmem_base_slot;
-  __shared__ int abort_flag;
+  __shared__ int abort_flag, ran_out;
   const SmallTensor& t = L.t[blockIdx.x];
-  int* const error = L.waits.error ? L.waits.error : g_muon_error;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, k_stages = t.k_stages;
   if (tid == 0) {
-    abort_flag = 0;
-    mbar_init(load_bar, 1);
+    abort_flag = ran_out = 0;
+    mbar_init(load_bar, L.waits.signals);
     mbar_init(done_bar, 1);
     mbar_fence_init();
   }
@@ -648,11 +650,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_steps_kernel(const __g
   const uint32_t tmem_base = tmem_base_slot;
   behind_previous();
 
-  if (tid == 0 && !(L.waits.starve == kStarveSmallSteps && blockIdx.x == 0)) {
+  if (tid == 0) {
     mbar_expect_tx(load_bar, k_stages * kOperandBytes);
     for (int kb = 0; kb < k_stages; ++kb) tma_load_3d(A + kb * kOperandBytes, &t.gram, load_bar, kb * BK, 0, 0);
   }
-  bool ok = __syncthreads_and(mbar_wait(load_bar, 0, &abort_flag, error, kDevTimeoutTmaFull, L.waits.limit_cycles));
+  bool ok = __syncthreads_and(mbar_wait(load_bar, 0, &abort_flag, &ran_out, kDevTimeoutTmaFull, L.waits.limit_cycles));
   tc_fence_after();
 
   // thread: row `row` and 64 columns of every result
@@ -703,7 +705,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_steps_kernel(const __g
       add(add1, c1);
       if (add2) add(add2, c2);
     }
-    ok = __syncthreads_and(mbar_wait(done_bar, phase, &abort_flag, error, kDevTimeoutAccum, L.waits.limit_cycles));
+    ok = __syncthreads_and(mbar_wait(done_bar, phase, &abort_flag, &ran_out, kDevTimeoutAccum, L.waits.limit_cycles));
     phase ^= 1;
     if (!ok) return;
     tc_fence_after();
@@ -764,6 +766,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_steps_kernel(const __g
   }
   tc_fence_before();
   __syncthreads();
+  if (tid == 0 && ran_out) report(L.waits, ran_out);
   if (warp == 0) {
     __syncwarp();
     tc_fence_after();
@@ -930,7 +933,8 @@ struct Shape {
   size_t x_bytes() const { return up((size_t)2 * m * ldn * 2, 256); }
   size_t a_bytes() const { return up((size_t)2 * m * ldm * 2, 256); }
   // A Gram matrix of at most 1024 rows has few tiles and may have a long K, which is then cut into parts of about 16 stages
-  // (one 512 x 4608 filter's takes 85 us uncut); a larger one into as many as leave every pair of SMs a tile.  By the
+  // (one 512 x 4608 filter's takes 85 us uncut); a larger one into as many as leave every pair of SMs a tile, which is two up to
+  // 1408 rows (1200 x 8000 673 us, uncut 748; 1408 x 8000 738, uncut 811) and none beyond.  By the
   // tensor alone, so that no result depends on what else is updated.
   int gram_stages() const { return (int)((n + BK - 1) / BK); }
   int gram_splits() const {
@@ -1061,7 +1065,7 @@ cudaError_t launch_small(const SmallLaunch& L, int count, cudaStream_t st) {
 struct Options {
   float lr, mu, decay;
   int steps, nesterov;
-  Waits waits;
+  Waits products, small_steps;  // of either kernel
 };
 
 // The whole update of up to kMaxTensors tensors; N is the largest number of products per launch.
@@ -1134,7 +1138,7 @@ cudaError_t update_batch(const vgg19_muon_tensor* given, const int count, const 
   bool small = true;
   for (int i = 0; i < count; ++i) small = small && Shape(tensors[i]).m <= kSmall;
   L.count = 0;
-  L.waits = o.waits;
+  L.waits = o.products;
   int x = kX0;
   for (int done = 0; done < o.steps;) {
     const int group = steps_of_group(done, o.steps);
@@ -1167,7 +1171,7 @@ cudaError_t update_batch(const vgg19_muon_tensor* given, const int count, const 
     float sq = kScaleP, q0 = kA;
     if (small) {
       static thread_local SmallLaunch sl;
-      sl.waits = o.waits;
+      sl.waits = o.small_steps;
       sl.group = group;
       for (int i = 0; i < count; ++i) {
         sl.t[i].gram = planes[i].k_major[kGramA];
@@ -1337,7 +1341,7 @@ extern "C" size_t vgg19_muon_workspace_bytes(const vgg19_muon_tensor* tensors, i
 }
 
 int vgg::muon_update(const vgg19_muon_tensor* tensors, int32_t count, float lr, float momentum, float decay, int32_t steps, int32_t nesterov,
-                     void* workspace, size_t bytes, const Waits& waits, void* stream) {
+                     void* workspace, size_t bytes, const Waits& products, const Waits& small_steps, void* stream) {
   const int rc = check_tensors(tensors, count);
   if (rc != VGG19_OK) return rc;
   if (!(lr == lr) || !(momentum == momentum) || !(decay == decay))
@@ -1357,7 +1361,7 @@ int vgg::muon_update(const vgg19_muon_tensor* tensors, int32_t count, float lr, 
     return note_error(VGG19_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu", bytes, workspace_bytes(tensors, count));
   const int apart = check_overlaps(tensors, count, workspace, workspace_bytes(tensors, count));
   if (apart != VGG19_OK) return apart;
-  const Options o{lr, momentum, decay, steps, nesterov != 0, waits};
+  const Options o{lr, momentum, decay, steps, nesterov != 0, products, small_steps};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   for (int i = 0; i < count; i += kMaxTensors) {
     const int n = count - i < kMaxTensors ? count - i : kMaxTensors;
@@ -1370,5 +1374,5 @@ int vgg::muon_update(const vgg19_muon_tensor* tensors, int32_t count, float lr, 
 
 extern "C" int vgg19_muon_update(const vgg19_muon_tensor* tensors, int32_t count, float lr, float momentum, float decay,
                                  int32_t steps, int32_t nesterov, void* workspace, size_t bytes, void* stream) {
-  return vgg::muon_update(tensors, count, lr, momentum, decay, steps, nesterov, workspace, bytes, vgg::Waits{}, stream);
+  return vgg::muon_update(tensors, count, lr, momentum, decay, steps, nesterov, workspace, bytes, vgg::Waits{}, vgg::Waits{}, stream);
 }

@@ -18,10 +18,12 @@
 // block's share of x is staged in shared memory meanwhile, once for all its rows.  The shares of a cluster join through
 // distributed shared memory, in a fixed order: one launch, no scratch.
 //
-// Measured (B200, device time): 25088 -> 4096 in groups of 128, one row, bf16: 18.6 us, 2.8 TB/s, bound by unpacking (76
-// integer instructions a KB on a pipe of half rate); sixteen rows, groups of 64: 32 us; 4096 -> 4096, sixteen rows, groups of
-// 32: 8.2 us, 2.4 of them until x is staged, 2.3 products, 2.2 joining; 6344 -> 11710, ten rows of fp32: 36 us, where the
-// tensor cores (three terms, two tiles of rows: 48 products a KB at 8 cycles) are busy a third of the time.
+// Measured (B200, device time): 25088 -> 4096 in groups of 128 or 64, one row, bf16: 18.4 to 18.8 us, 2.8 TB/s.  No pipe is full there: issue slots 51 %,
+// the integer pipe 45 % (76 instructions a KB to unpack), DRAM 29 %, 13 warps an SM (256 blocks on 148 SMs); the same copies without the products take
+// 12 us, and a few of the 18 are x on its way and the cluster's meeting.  One row of fp32: 23.8 us; two of bf16 20.7; sixteen, groups of 64: 32 us, and as
+// much again for every further sixteen; 4096 -> 4096, sixteen rows, groups of 32: 8.3 us, 2.4 of them until x is staged, 2.3 products, 2.2 joining;
+// 6344 -> 11710, ten rows of fp32: 36 us, where the tensor cores (three terms, two tiles of rows: 48 products a KB at 8 cycles) are busy a third of the time.
+// Packing 25088 x 4096 takes 249 us from fp32 or bf16 (by bytes 72 and 40): a warp's 128 weights in scalar loads and two-byte stores.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
@@ -128,7 +130,7 @@ __global__ void __launch_bounds__(32 * RW * KW, kResident<T, NT, RW * KW>) q4_li
   __shared__ float part[KW][RW][NT * 8][kTileRows];
   __shared__ float inbox[RW * NT * 8 * kTileRows + kMaxKSplit];
   __shared__ __align__(8) unsigned long long bars[RW * KW][kRing];
-  __shared__ int abort_flag;
+  __shared__ int abort_flag, ran_out;  // (where that is recorded takes registers that the products want: found out once it happens)
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int ks = a.ksplit, rank = ks > 1 ? (int)cluster.block_rank() : 0;
@@ -151,9 +153,7 @@ __global__ void __launch_bounds__(32 * RW * KW, kResident<T, NT, RW * KW>) q4_li
     bulk_copy(dst + SLOT * kBlockBytes, scales + (long)b * (kTileRows * PER * 2), n * (kTileRows * PER * 2), bar);
   };
   if (ks > 1) cluster.barrier_arrive();  // waited for before the first write into another block's shared memory
-  if (tid == 0) abort_flag = 0;
-  int* const error = a.waits.error ? a.waits.error : g_q4_error;
-  const bool starved = a.waits.starve == kStarveDense && blockIdx.x == 0;
+  if (tid == 0) abort_flag = ran_out = 0;
 
   float acc[NT][4] = {};
   int xrow[NT];
@@ -228,10 +228,10 @@ __global__ void __launch_bounds__(32 * RW * KW, kResident<T, NT, RW * KW>) q4_li
       // The weights are asked for behind the first of x, not before: x is little and everything waits for it (asked for
       // after them it came 2.5 us later).
       if (c0 == b0 && i0 == tid && lane == 0) {
-        for (int s = 0; s < kRing; ++s) mbar_init(bar_u32 + 8 * s, 1);
+        for (int s = 0; s < kRing; ++s) mbar_init(bar_u32 + 8 * s, a.waits.signals);
         mbar_fence_init();
         for (int s = 0; s < kRing; ++s)
-          if (first + s * STEP < b1 && !starved) request(s, first + s * STEP);
+          if (first + s * STEP < b1) request(s, first + s * STEP);
       }
 #pragma unroll
       for (int u = 0; u < BATCH; ++u) {
@@ -249,8 +249,10 @@ __global__ void __launch_bounds__(32 * RW * KW, kResident<T, NT, RW * KW>) q4_li
     __syncthreads();
     for (int b = c0 + warp / RW * SLOT; b < c1; b += STEP) {  // (a part of x is a multiple of STEP, but for the last)
       if (!ok) break;
-      ok = __all_sync(0xffffffffu, mbar_wait(bar_u32 + 8 * slot, phase, &abort_flag, error, kDevTimeoutTmaFull, a.waits.limit_cycles));
-      if (!ok) {  // let what is on its way land before shared memory goes away
+      ok = __all_sync(0xffffffffu, mbar_wait(bar_u32 + 8 * slot, phase, &abort_flag, &ran_out, kDevTimeoutTmaFull, a.waits.limit_cycles));
+      if (!ok) {
+        if (lane == 0 && ran_out) atomicCAS(a.waits.error ? a.waits.error : g_q4_error, 0, ran_out);
+        // let what is on its way land before shared memory goes away
         if (lane == 0) {
           const unsigned long long t0 = global_timer_ns();
           for (int i = 0; i < kRing && b + i * STEP < b1; ++i) {

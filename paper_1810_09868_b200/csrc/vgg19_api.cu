@@ -951,7 +951,7 @@ int vgg19_muon_step(vgg19_t *n, const float *grads, float *momentum_buffer, floa
   if (spans_meet(used, 4)) return fail(n, VGG19_ERR_ARG, "gradients, momentum, workspace and parameters overlap");
   vgg19_muon_tensor t[kLayers];
   muon_tensors(n, grads, momentum_buffer, t);
-  const int rc = muon_update(t, kLayers, lr, momentum, decay, steps, nesterov, workspace, bytes, waits_of(n->dev_error), stream);
+  const int rc = muon_update(t, kLayers, lr, momentum, decay, steps, nesterov, workspace, bytes, waits_of(n->dev_error), waits_of(n->dev_error), stream);
   if (rc != VGG19_OK) return adopt_error(n, rc);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   MuonVector v[kLayers];
@@ -1356,26 +1356,28 @@ int vgg19_selftest_operator_timeout(vgg19_t *n, int32_t which, void *workspace, 
   CUDA_TRY(n, cudaMemsetAsync(workspace, 0, VGG19_SELFTEST_BYTES, st));
   char *at = static_cast<char *>(workspace);
   auto take = [&at](size_t size) { char *p = at; at += align_up(size); return p; };
-  Waits waits = waits_of(n ? n->dev_error : nullptr);
-  waits.limit_cycles = 2000000;  // a millisecond or two
+  const Waits waits = waits_of(n ? n->dev_error : nullptr);
+  Waits short_waits = waits;
+  short_waits.limit_cycles = 2000000;  // a millisecond or two
+  short_waits.signals = 2;
   if (which == VGG19_SELFTEST_DENSE_Q4) {
     // three rows, so that every warp has a row tile of its own, over a K that a cluster of blocks shares
     constexpr int rows = 3, in = 1024, out = 128, group = VGG19_DENSE_Q4_GROUP;
-    waits.starve = kStarveDense;
     void *codes = take(q4_code_bytes(out, in)), *scales = take(q4_scale_bytes(out, in, group));
     const bf16 *x = reinterpret_cast<bf16 *>(take(rows * in * 2));
     float *y = reinterpret_cast<float *>(take(rows * out * 4));
-    CUDA_TRY(n, q4_linear<bf16>(x, in, rows, in, codes, scales, out, group, nullptr, false, nullptr, y, waits, st));
+    CUDA_TRY(n, q4_linear<bf16>(x, in, rows, in, codes, scales, out, group, nullptr, false, nullptr, y, short_waits, st));
     return VGG19_OK;
   }
-  waits.starve = which == VGG19_SELFTEST_UPDATE ? kStarveProducts : kStarveSmallSteps;
+  const bool products = which == VGG19_SELFTEST_UPDATE;
   constexpr int rows = 96, cols = 160;
   vgg19_muon_tensor t{};
   t.rows = rows; t.cols = cols;
   t.w = reinterpret_cast<float *>(take(rows * cols * 4));
   t.grad = reinterpret_cast<float *>(take(rows * cols * 4));
   t.momentum = reinterpret_cast<float *>(take(rows * cols * 4));
-  const int rc = muon_update(&t, 1, 0.1f, 0.9f, 0.f, 1, 0, at, VGG19_SELFTEST_BYTES - (at - static_cast<char *>(workspace)), waits, stream);
+  const int rc = muon_update(&t, 1, 0.1f, 0.9f, 0.f, 1, 0, at, VGG19_SELFTEST_BYTES - (at - static_cast<char *>(workspace)), products ? short_waits : waits,
+                             products ? waits : short_waits, stream);
   return rc == VGG19_OK || !n ? rc : adopt_error(n, rc);
 }
 

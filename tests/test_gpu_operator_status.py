@@ -1,5 +1,5 @@
-"""What the operators report of waits that ran out, and to whom.  The waits are made to run out by the library's self-test: a block that asks
-for none of its copies, over zeros, with a limit of about a millisecond.  Nothing faults: the kernels give up, end and return."""
+"""What the operators report of waits that ran out, and to whom.  The waits are made to run out by the library's self-test: barriers that
+expect one signal more than their copies give, over zeros, with a limit of about a millisecond.  Nothing faults: the kernels give up, end and return."""
 import pytest
 import torch
 
