@@ -793,7 +793,8 @@ extern "C" {
 int vgg19_ops_status(void *stream) {
   static std::mutex one;  // status calls of several host threads
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = cudaSuccess;
+  cudaError_t e = cudaStreamSynchronize(st);  // (nobody waits for this one's stream behind the lock)
+  if (e != cudaSuccess) return fail(nullptr, VGG19_ERR_CUDA, "waiting for the stream failed: %s", cudaGetErrorString(e));
   int id = 0, dense = 0, update = 0;
   try {
     const std::lock_guard<std::mutex> lock(one);

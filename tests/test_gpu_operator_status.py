@@ -111,3 +111,20 @@ def test_a_status_waits_for_its_own_stream_alone(p):
     assert not done.query()
     net.close()
     torch.cuda.synchronize()
+
+
+def test_statuses_of_two_threads_do_not_wait_for_one_another(p):
+    import threading
+    busy, idle, done = torch.cuda.Stream(), torch.cuda.Stream(), torch.cuda.Event()
+    p.vgg19_ops_status(idle)
+    with torch.cuda.stream(busy):
+        torch.cuda._sleep(2_000_000_000)  # about a second
+        done.record()
+    started = threading.Event()
+    other = threading.Thread(target=lambda: (started.set(), p.vgg19_ops_status(busy)))
+    other.start()
+    started.wait()
+    other.join(0.05)  # it is in its call by now, waiting for its stream
+    p.vgg19_ops_status(idle)
+    assert other.is_alive() and not done.query()
+    other.join()
