@@ -569,6 +569,8 @@ def vgg19_muon_step(net, grads, momentum_buffer, lr, momentum, decay, bias_lr, s
 def vgg19_selftest_operator_timeout(net, which, workspace, stream=None):
     """net or None; workspace: a CUDA tensor of at least VGG19_SELFTEST_BYTES."""
     dev = workspace.get_device()
+    if dev < 0:
+        _refuse(VGG19_ERR_ARG, f"the workspace is on {workspace.device}, not on a CUDA device")
     _torch()
     return _call(dev, load().vgg19_selftest_operator_timeout, net, which, *_workspace(workspace, dev), _stream(stream))
 

@@ -251,6 +251,7 @@ __global__ void __launch_bounds__(32 * RW * KW, kResident<T, NT, RW * KW>) q4_li
       if (!ok) break;
       ok = __all_sync(0xffffffffu, mbar_wait(bar_u32 + 8 * slot, phase, &abort_flag, &ran_out, kDevTimeoutTmaFull, a.waits.limit_cycles));
       if (!ok) {
+        __syncwarp();  // (the lane that ran out has written its code)
         if (lane == 0 && ran_out) atomicCAS(a.waits.error ? a.waits.error : g_q4_error, 0, ran_out);
         // let what is on its way land before shared memory goes away
         if (lane == 0) {

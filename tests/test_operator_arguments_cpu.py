@@ -238,3 +238,9 @@ def test_q4_pack_refuses_overlaps(p, over):
         a[k] += SOME
     assert p.binding.load().vgg19_q4_pack(*a.values()) == p.VGG19_ERR_ARG
     assert "overlap" in p.vgg19_last_error()
+
+
+def test_the_operators_selftest_refuses_host_memory(p):
+    with pytest.raises(p.Vgg19Error) as e:
+        p.vgg19_selftest_operator_timeout(None, p.VGG19_SELFTEST_UPDATE, torch.empty(1 << 20, dtype=torch.uint8))
+    assert e.value.code == p.VGG19_ERR_ARG
