@@ -460,10 +460,72 @@ size_t vgg19_muon_step_bytes(const vgg19_t *net);
 int vgg19_muon_step(vgg19_t *net, const float *grads, float *momentum_buffer, float lr, float momentum, float decay,
                     float bias_lr, int32_t steps, int32_t nesterov, void *workspace, size_t bytes, void *stream);
 
+/* Dropout from a counter-based generator, whose mask is computed where it is used and never stored: what the dense
+ * layers of a VGG network are trained with (vgg19_set_dropout: a network's own), and what a program puts in front of a layer of its own.
+ *   y = x * keep / (1 - q),   keep_e = [u_e >= t],   t = round(65536 rate), q = t / 65536,
+ * where u_e is 16 bits of Philox 4x32 with ten rounds (Salmon et al., 2011) under the key `seed` (low word first): value e = first + r * cols
+ * + c of the logical matrix takes, of block e / 8 (counter words: e / 8 low and high, step low and high), word (e % 8) / 2, its low
+ * half first.  So a mask depends on seed, step and a value's place alone: not on strides, types or launches, and a
+ * shard that says where it begins (`first`) gets its part of the whole's.  rate in [0, 1]; it is taken to a multiple of 2^-16, and at 1 all is dropped.
+ * step: counts calls that want different masks; `step_counter` (or NULL): device, added to it when the kernel runs, so
+ * that a recorded graph takes another mask every time it is replayed (the caller, or vgg19_set_dropout's network, counts it up).
+ * x, y: device, `rows` rows of `cols` values, row strides ldx and ldy, VGG19_FP32 or VGG19_BF16.  y may be x with the same
+ * stride; any other overlap is refused.  A dropped value is 0 whatever x holds there.  rows == 0 does nothing.
+ * The gradient is the same product: dx = dy * keep / (1 - q), with the arguments of the forward call. */
+int vgg19_dropout(const void *x, int32_t dtype, int64_t rows, int32_t cols, int64_t ldx, float rate, uint64_t seed, uint64_t step,
+                  const uint64_t *step_counter, uint64_t first, void *y, int64_t ldy, void *stream);
+int vgg19_dropout_backward(const void *dy, int32_t dtype, int64_t rows, int32_t cols, int64_t lddy, float rate, uint64_t seed, uint64_t step,
+                           const uint64_t *step_counter, uint64_t first, void *dx, int64_t lddx, void *stream);
+
+/* Dropout of a network's training passes (vgg19_backward*, vgg19_train_step(s)) behind dense layers 1 and 2, in place on what
+ * vgg19_saved_tensor gives as their outputs, and of the gradients that come back there.  Forward-only passes have none (values are scaled up in training).  rate 0 (a
+ * new network's) is no dropout.  Pass p since this call, p = first_pass, first_pass + 1, ..., takes steps 2p (behind layer 1) and 2p + 1 of
+ * `seed`, whose rows are the images; the passes are counted on the device, so recorded ones take other masks every time, and every
+ * step of vgg19_train_steps is a pass.  Waits for the device, and discards recorded graphs. */
+int vgg19_set_dropout(vgg19_t *net, float rate, uint64_t seed, uint64_t first_pass);
+
+/* The last dense layer (section 7.1, dense(W, x, b) = W*x .+ b) and the softmax cross entropy of its rows in one, for any number of
+ * classes, without keeping the logits:
+ *   z = x w^T + bias,   lse_r = log sum_n exp z_rn,   loss_r = lse_r - z_r,labels[r].
+ * x: device [rows][in], row stride ldx; w: device [classes][in], row stride ldw; both `dtype`.  bias: device fp32 [classes] or
+ * NULL; a bias of -inf excludes its class.  labels: device int32 [rows].  Rows and strides of 16 bytes are read where they lie, others
+ * are laid out in the workspace first. */
+typedef struct {
+  const void *x;
+  int64_t ldx;
+  const void *w;
+  int64_t ldw;
+  const float *bias;
+  const int32_t *labels;
+  int64_t rows;
+  int32_t in, classes, dtype;
+} vgg19_linear_loss;
+
+/* loss, lse: device fp32 [rows], either may be NULL.  A label VGG19_NO_CLASS asks for nothing (a row that only fills the batch): its loss
+ * is 0.  Any other label outside [0, classes) is never used as an index: its loss is NaN and vgg19_ops_status reports VGG19_ERR_ARG.
+ * A row that is left no class has lse -inf and loss +inf; so has an excluded label, with a finite lse.  A NaN or +inf among a row's z makes its results NaN.
+ * bf16 products are exact and summed in fp32; fp32 values are taken as three bf16 terms each, and the products of terms down to 2^-16 of the first.
+ * workspace: device, 256-byte aligned, vgg19_linear_cross_entropy_bytes(layer, 0) bytes (0 for a layer that is refused; of pointers only the
+ * alignment of x and w is looked at): scratch for the time of the call; calls that share one have to be ordered.  Asynchronous
+ * on `stream`; may be captured.  rows == 0 does nothing.  Nothing that is written may overlap anything else of the call. */
+size_t vgg19_linear_cross_entropy_bytes(const vgg19_linear_loss *layer, int32_t backward);
+int vgg19_linear_cross_entropy(const vgg19_linear_loss *layer, float *loss, float *lse, void *workspace, size_t bytes, void *stream);
+
+/* Gradients of sum_r d_loss[r] * loss[r], from the lse that the forward call gave, with
+ *   dz_rn = d_loss_r (exp(z_rn - lse_r) - [n = labels[r]]):
+ *   dx = dz w: device [rows][in], of `dtype`, row stride lddx;   dw = dz^T x: device [classes][in], of dw_dtype (VGG19_FP32 or `dtype`),
+ * row stride lddw;   db = sum_r dz_r: device fp32 [classes].  Each is overwritten; any may be NULL.  The products are taken
+ * again, a piece of the classes at a time.  In bf16 dz is rounded to bf16 before the products with x and w (db is summed before that).  Rows
+ * whose label names no class (VGG19_NO_CLASS or another outside, which is reported as above) or whose d_loss is 0 have dz 0 whatever their x holds, but
+ * dw takes 0 times their x: it has to be finite.  A row that is left no class has dz 0.  rows == 0: dw and db become 0.
+ * workspace: vgg19_linear_cross_entropy_bytes(layer, 1). */
+int vgg19_linear_cross_entropy_backward(const vgg19_linear_loss *layer, const float *lse, const float *d_loss, void *dx, int64_t lddx,
+                                        void *dw, int32_t dw_dtype, int64_t lddw, float *db, void *workspace, size_t bytes, void *stream);
+
 /* Wait for the stream and report, and clear, what calls without a handle
- * (vgg19_logprobs, vgg19_q4_linear, vgg19_muon_update) have recorded on the current device:
+ * (vgg19_logprobs, vgg19_q4_linear, vgg19_muon_update, vgg19_linear_cross_entropy) have recorded on the current device:
  * VGG19_ERR_DEVICE_TIMEOUT when a bounded wait inside a kernel ran out,
- * VGG19_ERR_ARG for an id outside the classes (both: the first, and
+ * VGG19_ERR_ARG for an id or a label outside the classes (both: the first, and
  * vgg19_last_error(NULL) names the second). */
 int vgg19_ops_status(void *stream);
 
@@ -496,7 +558,8 @@ int vgg19_selftest_wait_timeout(vgg19_t *net, void *stream);
 enum {
   VGG19_SELFTEST_DENSE_Q4 = 0,    /* vgg19_q4_linear */
   VGG19_SELFTEST_UPDATE = 1,      /* vgg19_muon_update, its products */
-  VGG19_SELFTEST_UPDATE_STEPS = 2 /* vgg19_muon_update, the steps of small matrices */
+  VGG19_SELFTEST_UPDATE_STEPS = 2, /* vgg19_muon_update, the steps of small matrices */
+  VGG19_SELFTEST_LOSS = 4         /* vgg19_linear_cross_entropy (3 is none) */
 };
 int vgg19_selftest_operator_timeout(vgg19_t *net, int32_t which, void *workspace, size_t bytes, void *stream);
 

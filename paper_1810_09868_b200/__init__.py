@@ -90,6 +90,11 @@ class Net:
             binding.vgg19_muon_step(self.handle, grads, momentum_buffer, lr, momentum, decay, lr if bias_lr is None else bias_lr, steps,
                                     nesterov, self.muon_workspace, self.muon_workspace.numel(), stream)
 
+    def set_dropout(self, rate, seed=0, first_pass=0):
+        """Training passes drop the outputs of dense layers 1 and 2 at `rate` (0: none), each pass with masks of its own."""
+        with self._torch.cuda.device(self.device):
+            binding.vgg19_set_dropout(self.handle, rate, seed, first_pass)
+
     def train_step(self, images, labels, lr, loss=None, stream=None):
         """Forward + backward + update as one recorded device program (workspace of VGG19_MODE_TRAIN)."""
         stream = stream or self._torch.cuda.current_stream(self.device)

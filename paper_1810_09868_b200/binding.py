@@ -30,10 +30,13 @@ EXPORTS = (
     "vgg19_logprobs", "vgg19_logprobs_backward", "vgg19_ops_status",
     "vgg19_q4_code_bytes", "vgg19_q4_scale_bytes", "vgg19_q4_pack", "vgg19_q4_linear",
     "vgg19_selftest_operator_timeout", "vgg19_muon_workspace_bytes", "vgg19_muon_update", "vgg19_muon_step_bytes", "vgg19_muon_step",
+    "vgg19_dropout", "vgg19_dropout_backward", "vgg19_set_dropout",
+    "vgg19_linear_cross_entropy_bytes", "vgg19_linear_cross_entropy", "vgg19_linear_cross_entropy_backward",
 )
 VGG19_NO_CLASS = -1
 VGG19_LOGPROBS_MAX_TOP, VGG19_LOGPROBS_MAX_IDS = 32, 256
 VGG19_SELFTEST_DENSE_Q4, VGG19_SELFTEST_UPDATE, VGG19_SELFTEST_UPDATE_STEPS = 0, 1, 2
+VGG19_SELFTEST_LOSS = 4
 VGG19_SELFTEST_BYTES = 1048576
 
 
@@ -45,6 +48,11 @@ class vgg19_config(ctypes.Structure):
 class vgg19_muon_tensor(ctypes.Structure):
     _fields_ = [("w", ctypes.c_void_p), ("w_bf16", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("momentum", ctypes.c_void_p),
                 ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
+
+
+class vgg19_linear_loss(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("w", ctypes.c_void_p), ("ldw", ctypes.c_int64), ("bias", ctypes.c_void_p),
+                ("labels", ctypes.c_void_p), ("rows", ctypes.c_int64), ("in_", ctypes.c_int32), ("classes", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 class Vgg19Error(RuntimeError):
@@ -115,6 +123,12 @@ def load():
         "vgg19_muon_update": ([vp, i32, f32, f32, f32, i32, i32, vp, sz, vp], ctypes.c_int),
         "vgg19_muon_step_bytes": ([vp], sz),
         "vgg19_muon_step": ([vp, vp, vp, f32, f32, f32, f32, i32, i32, vp, sz, vp], ctypes.c_int),
+        "vgg19_dropout": ([vp, i32, i64, i32, i64, f32, u64, u64, vp, u64, vp, i64, vp], ctypes.c_int),
+        "vgg19_dropout_backward": ([vp, i32, i64, i32, i64, f32, u64, u64, vp, u64, vp, i64, vp], ctypes.c_int),
+        "vgg19_set_dropout": ([vp, f32, u64, u64], ctypes.c_int),
+        "vgg19_linear_cross_entropy_bytes": ([vp, i32], sz),
+        "vgg19_linear_cross_entropy": ([vp, vp, vp, vp, sz, vp], ctypes.c_int),
+        "vgg19_linear_cross_entropy_backward": ([vp, vp, vp, vp, i64, vp, i32, i64, vp, vp, sz, vp], ctypes.c_int),
         "vgg19_q4_code_bytes": ([i32, i32], sz),
         "vgg19_q4_scale_bytes": ([i32, i32, i32], sz),
         "vgg19_q4_pack": ([vp, i32, i32, i32, i64, i32, vp, vp, vp], ctypes.c_int),
@@ -564,6 +578,95 @@ def vgg19_muon_step_bytes(net):
 def vgg19_muon_step(net, grads, momentum_buffer, lr, momentum, decay, bias_lr, steps, nesterov, workspace, nbytes, stream=None):
     return _check(net, load().vgg19_muon_step(net, _ptr(grads), _ptr(momentum_buffer), lr, momentum, decay, bias_lr, steps, int(nesterov),
                                               _ptr(workspace), nbytes, _stream(stream)))
+
+
+def _any_dropout(name, x, y, rate, seed, step, step_counter, first, stream):
+    rc = getattr(_tensor_calls or _calls(), name)(x, y, rate, seed, step, step_counter, first, stream)
+    if rc is not None:
+        return _answered(rc)
+    source, result = ("dy", "dx") if name.endswith("backward") else ("x", "y")
+    dtype, rows, cols, ldx, dev = _rows_of(x, source)
+    y_dtype, y_rows, y_cols, ldy, y_dev = _rows_of(y, result)
+    if (y_dtype, y_rows, y_cols, y_dev) != (dtype, rows, cols, dev):
+        _refuse(VGG19_ERR_SHAPE, f"{result} differs from {source} in type, shape or device")
+    for v, what in ((seed, "seed"), (step, "step"), (first, "first")):
+        if not 0 <= v < 1 << 64:
+            _refuse(VGG19_ERR_ARG, f"{what} {v} is not an unsigned 64-bit number")
+    import torch
+    counter = _tensor(step_counter, "step_counter", torch.int64, (1,), dev)
+    return _call(dev, getattr(_lib or load(), "vgg19_" + name), x.data_ptr(), dtype, rows, cols, ldx, rate, seed, step, counter, first, y.data_ptr(), ldy,
+                 _stream(stream))
+
+
+def vgg19_dropout(x, y, rate, seed, step=0, step_counter=None, first=0, stream=None):
+    """y = x with values dropped at `rate` and the others scaled up; [rows][cols], row strides are allowed, y may be x.
+    step_counter: an int64 CUDA tensor of one element, added to step on the device."""
+    return _any_dropout("dropout", x, y, rate, seed, step, step_counter, first, stream)
+
+
+def vgg19_dropout_backward(dy, dx, rate, seed, step=0, step_counter=None, first=0, stream=None):
+    """dx from dy, with what vgg19_dropout was given for the mask; dx may be dy."""
+    return _any_dropout("dropout_backward", dy, dx, rate, seed, step, step_counter, first, stream)
+
+
+def _linear_loss(x, w, bias, labels):
+    """(the layer as the library takes it, CUDA device index)"""
+    dtype, rows, in_, ldx, dev = _rows_of(x, "x")
+    w_dtype, classes, w_in, ldw, w_dev = _rows_of(w, "w")
+    if (w_dtype, w_in, w_dev) != (dtype, in_, dev):
+        _refuse(VGG19_ERR_SHAPE, "w differs from x in type, columns or device")
+    if classes > _MOST:
+        _refuse(VGG19_ERR_SHAPE, f"{classes} classes, at most {_MOST} are possible")
+    _, f32, _, i32, _ = _types
+    return vgg19_linear_loss(x.data_ptr(), ldx, w.data_ptr(), ldw, _tensor(bias, "bias", f32, (classes,), dev),
+                             _tensor(labels, "labels", i32, (rows,), dev), rows, in_, classes, dtype), dev
+
+
+def vgg19_linear_cross_entropy_bytes(x, w, backward):
+    """Bytes of workspace for x [rows][in] and w [classes][in]; 0 for sizes that are refused."""
+    layer, dev = _linear_loss(x, w, None, None)
+    import torch
+    with torch.cuda.device(dev):
+        return load().vgg19_linear_cross_entropy_bytes(ctypes.byref(layer), 1 if backward else 0)
+
+
+def vgg19_linear_cross_entropy(x, w, bias, labels, loss, lse, workspace, stream=None):
+    """x [rows][in] and w [classes][in] (row strides are allowed), bias [classes] or None, labels int32 [rows]; loss and lse
+    [rows], either may be None."""
+    rc = (_tensor_calls or _calls()).linear_cross_entropy(x, w, bias, labels, loss, lse, workspace, stream)
+    if rc is not None:
+        return _answered(rc)
+    layer, dev = _linear_loss(x, w, bias, labels)
+    f32, each = _types[1], (layer.rows,)
+    return _call(dev, (_lib or load()).vgg19_linear_cross_entropy, ctypes.byref(layer), _tensor(loss, "loss", f32, each, dev),
+                 _tensor(lse, "lse", f32, each, dev), *_workspace(workspace, dev), _stream(stream))
+
+
+def vgg19_linear_cross_entropy_backward(x, w, bias, labels, lse, d_loss, dx, dw, db, workspace, stream=None):
+    """Gradients of sum(d_loss * loss): dx [rows][in] in x's type, dw [classes][in] in w's type or fp32 (row strides are allowed), db
+    [classes]; any may be None."""
+    rc = (_tensor_calls or _calls()).linear_cross_entropy_backward(x, w, bias, labels, lse, d_loss, dx, dw, db, workspace, stream)
+    if rc is not None:
+        return _answered(rc)
+    layer, dev = _linear_loss(x, w, bias, labels)
+    f32, each = _types[1], (layer.rows,)
+    lddx = lddw = layer.in_
+    dw_dtype = layer.dtype
+    if dx is not None:
+        dx_dtype, dx_rows, dx_cols, lddx, dx_dev = _rows_of(dx, "dx")
+        if (dx_dtype, dx_rows, dx_cols, dx_dev) != (layer.dtype, layer.rows, layer.in_, dev):
+            _refuse(VGG19_ERR_SHAPE, "dx differs from x in type, shape or device")
+    if dw is not None:
+        dw_dtype, dw_rows, dw_cols, lddw, dw_dev = _rows_of(dw, "dw")
+        if (dw_rows, dw_cols, dw_dev) != (layer.classes, layer.in_, dev):
+            _refuse(VGG19_ERR_SHAPE, "dw differs from w in shape or device")
+    return _call(dev, (_lib or load()).vgg19_linear_cross_entropy_backward, ctypes.byref(layer), _tensor(lse, "lse", f32, each, dev),
+                 _tensor(d_loss, "d_loss", f32, each, dev), _ptr(dx), lddx, _ptr(dw), dw_dtype, lddw,
+                 _tensor(db, "db", f32, (layer.classes,), dev), *_workspace(workspace, dev), _stream(stream))
+
+
+def vgg19_set_dropout(net, rate, seed, first_pass=0):
+    return _check(net, load().vgg19_set_dropout(net, rate, seed, first_pass))
 
 
 def vgg19_selftest_operator_timeout(net, which, workspace, stream=None):

@@ -78,10 +78,20 @@ template <int M> inline bool spans_meet(const Span (&all)[M], int written) {
 // Waits for the stream; *code becomes the device error word's value and the word 0, in one exchange on the device: what a kernel on another
 // stream records meanwhile is either taken or left for the next status.  word[1] is the exchange's own.  One host thread at a time.
 cudaError_t take_error(int* word, int* code, cudaStream_t st);
-// The same for the words of calls without a handle (logprobs.cu, q4_dense.cu, muon.cu), on the current device.
+// The same for the words of calls without a handle (logprobs.cu, q4_dense.cu, muon.cu, linear_loss.cu), on the current device.
 cudaError_t logprobs_take_error(int* code, cudaStream_t st);
 cudaError_t q4_take_error(int* code, cudaStream_t st);
 cudaError_t muon_take_error(int* code, cudaStream_t st);
+cudaError_t loss_take_error(int* code, int* label, cudaStream_t st);
+
+// vgg19_linear_cross_entropy with the waits of its kernels (linear_loss.cu).
+int linear_loss(const vgg19_linear_loss* layer, float* loss, float* lse, void* workspace, size_t bytes, const Waits& waits, void* stream);
+
+// vgg19_dropout (and, with dy for x, its gradient) without the checks (dropout.cu).
+cudaError_t dropout(const void* x, bool half, long rows, long cols, long ldx, float rate, unsigned long long seed, unsigned long long step,
+                    const unsigned long long* step_counter, unsigned long long first, void* y, long ldy, cudaStream_t st);
+// *counter += by
+cudaError_t count_up(unsigned long long* counter, unsigned long long by, cudaStream_t st);
 
 // vgg19_muon_update with the waits of its kernels (muon.cu).
 int muon_update(const vgg19_muon_tensor* tensors, int32_t count, float lr, float momentum, float decay, int32_t steps, int32_t nesterov,

@@ -160,10 +160,96 @@ PyObject* q4_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+uint64_t word64(PyObject* o) {
+  const unsigned long long v = PyLong_AsUnsignedLongLong(o);
+  if (PyErr_Occurred()) throw Unfit();
+  return v;
+}
+
+// x, y, rate, seed, step, step_counter, first, stream
+template <typename F> PyObject* any_dropout(F f, PyObject* const* a, Py_ssize_t n) {
+  return answer(n, 8, [&] {
+    const Rows x(a[0]), y(a[1]);
+    if (y.dtype != x.dtype || y.rows != x.rows || y.cols != x.cols) throw Unfit();
+    const double rate = PyFloat_AsDouble(a[2]);
+    if (PyErr_Occurred()) throw Unfit();
+    const uint64_t seed = word64(a[3]), step = word64(a[4]), first = word64(a[6]);
+    const auto* counter = static_cast<const uint64_t*>(dense(a[5], at::kLong, x.dev, 1));
+    void* stream = stream_of(a[7]);
+    return unlocked([&] { return f(x.data, x.dtype, x.rows, (int)x.cols, x.ld, (float)rate, seed, step, counter, first, y.data, y.ld, stream); });
+  });
+}
+PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t n) { return any_dropout(vgg19_dropout, a, n); }
+PyObject* dropout_backward(PyObject*, PyObject* const* a, Py_ssize_t n) { return any_dropout(vgg19_dropout_backward, a, n); }
+
+vgg19_linear_loss layer_of(const Rows& x, const Rows& w, PyObject* bias, PyObject* labels) {
+  if (w.dtype != x.dtype || w.cols != x.cols || w.rows > INT_MAX || labels == Py_None) throw Unfit();
+  return vgg19_linear_loss{x.data, x.ld, w.data, w.ld, dense_as<float>(bias, at::kFloat, x.dev, w.rows), dense_as<int32_t>(labels, at::kInt, x.dev, x.rows),
+                           x.rows, (int)x.cols, (int)w.rows, x.dtype};
+}
+struct Bytes {
+  void* data;
+  size_t size;
+  Bytes(PyObject* o, int dev) {
+    const at::Tensor& t = tensor(o);
+    if (!t.is_cuda() || t.get_device() != dev || !t.is_contiguous()) throw Unfit();
+    data = t.data_ptr();
+    size = t.nbytes();
+  }
+};
+
+// x, w, bias, labels, loss, lse, workspace, stream
+PyObject* linear_cross_entropy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return answer(n, 8, [&] {
+    const Rows x(a[0]), w(a[1]);
+    const vgg19_linear_loss layer = layer_of(x, w, a[2], a[3]);
+    auto* loss = dense_as<float>(a[4], at::kFloat, x.dev, x.rows);
+    auto* lse = dense_as<float>(a[5], at::kFloat, x.dev, x.rows);
+    const Bytes ws(a[6], x.dev);
+    void* stream = stream_of(a[7]);
+    return unlocked([&] { return vgg19_linear_cross_entropy(&layer, loss, lse, ws.data, ws.size, stream); });
+  });
+}
+
+// x, w, bias, labels, lse, d_loss, dx, dw, db, workspace, stream
+PyObject* linear_cross_entropy_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return answer(n, 11, [&] {
+    const Rows x(a[0]), w(a[1]);
+    const vgg19_linear_loss layer = layer_of(x, w, a[2], a[3]);
+    if (a[4] == Py_None || a[5] == Py_None) throw Unfit();
+    auto* lse = dense_as<float>(a[4], at::kFloat, x.dev, x.rows);
+    auto* d_loss = dense_as<float>(a[5], at::kFloat, x.dev, x.rows);
+    void *dx = nullptr, *dw = nullptr;
+    int64_t lddx = x.cols, lddw = x.cols;
+    int dw_dtype = x.dtype;
+    if (a[6] != Py_None) {
+      const Rows d(a[6]);
+      if (d.dtype != x.dtype || d.rows != x.rows || d.cols != x.cols) throw Unfit();
+      dx = d.data;
+      lddx = d.ld;
+    }
+    if (a[7] != Py_None) {
+      const Rows d(a[7]);
+      if (d.rows != w.rows || d.cols != x.cols) throw Unfit();
+      dw = d.data;
+      lddw = d.ld;
+      dw_dtype = d.dtype;
+    }
+    auto* db = dense_as<float>(a[8], at::kFloat, x.dev, w.rows);
+    const Bytes ws(a[9], x.dev);
+    void* stream = stream_of(a[10]);
+    return unlocked([&] { return vgg19_linear_cross_entropy_backward(&layer, lse, d_loss, dx, lddx, dw, dw_dtype, lddw, db, ws.data, ws.size, stream); });
+  });
+}
+
 PyMethodDef methods[] = {
     {"logprobs", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(logprobs)), METH_FASTCALL, nullptr},
     {"logprobs_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(logprobs_backward)), METH_FASTCALL, nullptr},
     {"q4_linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(q4_linear)), METH_FASTCALL, nullptr},
+    {"dropout", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(dropout)), METH_FASTCALL, nullptr},
+    {"dropout_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(dropout_backward)), METH_FASTCALL, nullptr},
+    {"linear_cross_entropy", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear_cross_entropy)), METH_FASTCALL, nullptr},
+    {"linear_cross_entropy_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear_cross_entropy_backward)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensor_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

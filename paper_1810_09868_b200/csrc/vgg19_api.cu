@@ -72,6 +72,8 @@ struct GraphEntry {
 
 }  // namespace
 
+constexpr size_t kPassCounterAt = 128;
+
 struct vgg19 {
   vgg19_config cfg;
   size_t elt;  // bytes per activation element
@@ -88,7 +90,9 @@ struct vgg19 {
   half16 *split_w = nullptr; // fp32 configuration on tensor cores: rows [hi | lo | hi] (fp16 terms) of every weight matrix, at 3 * w_off
   char *q4 = nullptr;        // VGG19_FLAG_DENSE_Q4: codes and scales of the dense layers
   size_t q4_codes[kFcLayers] = {}, q4_scales[kFcLayers] = {};  // byte offsets in it
-  int *dev_error = nullptr;
+  int *dev_error = nullptr;  // 256 bytes: the error word, a word for its exchange and, from kPassCounterAt on, the next training pass's first dropout step
+  float drop_rate = 0.f;     // dropout behind dense layers 1 and 2 in training passes
+  unsigned long long drop_seed = 0;
   void *ws = nullptr;
   size_t ws_bytes = 0;
   std::vector<GraphEntry> graphs;
@@ -107,6 +111,7 @@ struct vgg19 {
   int async_batch = 0;        // batch of the last vgg19_forward_host_async call (0: none yet)
   bool other_pass = false;    // a pass went through another entry point since that call
   cudaEvent_t ev_order = nullptr;
+  unsigned long long *pass_counter() { return reinterpret_cast<unsigned long long *>(reinterpret_cast<char *>(dev_error) + kPassCounterAt); }
 };
 
 namespace {
@@ -447,6 +452,12 @@ struct Pass {
                        (bf16 *)y2, (bf16 *)pooled, ConvShape{B, c0.H, c0.W, c0.Cin, c0.Cout}, n->dev_error, st), 1);
   }
 
+  // Dropout of a training pass, in place: of a dense layer's output, or of the gradient that comes back to it.
+  void drop(T *x, int B, int width, int layer) {
+    if (n->drop_rate > 0.f)
+      ok(dropout(x, sizeof(T) == 2, B, width, width, n->drop_rate, n->drop_seed, (unsigned long long)layer, n->pass_counter(), 0, x, width, st), 1);
+  }
+
   void forward(const PassArgs &a) {
     const int B = a.batch;
     const T *x = static_cast<const T *>(a.images);
@@ -471,7 +482,9 @@ struct Pass {
     float *logits = a.logits ? a.logits : fbuf(p.logits);
     const FcLayer *f = n->fc;
     dense_forward(f[0], x, B, buf(p.a1), nullptr);
+    if (a.grads) drop(buf(p.a1), B, f[0].Out, 0);
     dense_forward(f[1], buf(p.a1), B, buf(p.a2), nullptr);
+    if (a.grads) drop(buf(p.a2), B, f[1].Out, 1);
     dense_forward(f[2], buf(p.a2), B, nullptr, logits);
     if (a.probs && !a.grads)
       ok(softmax_xent<T>(logits, nullptr, a.probs, nullptr, nullptr, nullptr, B, kClasses, st), 1);
@@ -489,7 +502,10 @@ struct Pass {
     const T *flat = buf(p.pooled[4]);
     // dense 3, 2, 1: filter gradient, then input gradient masked by the ReLU below
     dense_backward(f[2], buf(p.a2), buf(p.dl), B, g + f[2].w_off, g + f[2].b_off, buf(p.dz2), buf(p.a2));
+    drop(buf(p.dz2), B, f[1].Out, 1);
     dense_backward(f[1], buf(p.a1), buf(p.dz2), B, g + f[1].w_off, g + f[1].b_off, buf(p.dz1), buf(p.a1));
+    drop(buf(p.dz1), B, f[0].Out, 0);
+    if (n->drop_rate > 0.f) ok(count_up(n->pass_counter(), 2, st), 1);
     dense_backward(f[0], flat, buf(p.dz1), B, g + f[0].w_off, g + f[0].b_off, buf(p.dflat), nullptr);
     if (n->dense_grads_event && err == cudaSuccess) {
       // the dense layers' gradients (the tail of the flat buffer, 86 % of it at 224x224) are final here:
@@ -795,23 +811,37 @@ int vgg19_ops_status(void *stream) {
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaStreamSynchronize(st);  // (nobody waits for this one's stream behind the lock)
   if (e != cudaSuccess) return fail(nullptr, VGG19_ERR_CUDA, "waiting for the stream failed: %s", cudaGetErrorString(e));
-  int id = 0, dense = 0, update = 0;
+  int id = 0, dense = 0, update = 0, loss = 0, label = 0;
   try {
     const std::lock_guard<std::mutex> lock(one);
     // all of them, whichever are set: what one call reports, none finds again
-    const cudaError_t read[] = {logprobs_take_error(&id, st), q4_take_error(&dense, st), muon_take_error(&update, st)};
+    const cudaError_t read[] = {logprobs_take_error(&id, st), q4_take_error(&dense, st), muon_take_error(&update, st), loss_take_error(&loss, &label, st)};
     for (cudaError_t r : read)
       if (e == cudaSuccess) e = r;
   } catch (...) {
     return fail(nullptr, VGG19_ERR_CUDA, "the host refused a lock");
   }
   if (e != cudaSuccess) return fail(nullptr, VGG19_ERR_CUDA, "reading the device status failed: %s", cudaGetErrorString(e));
-  const char *which = dense && update ? "a 4-bit layer and an update" : dense ? "a 4-bit layer" : "an update";
-  const char *bad = "an id outside the row's classes (its log probability is NaN)";
-  if (dense || update)
-    return fail(nullptr, VGG19_ERR_DEVICE_TIMEOUT, "a device-side wait of %s ran out (code %d)%s%s", which, dense ? dense : update, id ? "; also " : "",
-                id ? bad : "");
-  if (id) return fail(nullptr, VGG19_ERR_ARG, "%s", bad);
+  const char *bad = id && label ? "an id outside the row's classes (its log probability is NaN), and a label outside them (its loss is NaN)"
+                    : id        ? "an id outside the row's classes (its log probability is NaN)"
+                                : "a label outside the classes (its loss is NaN)";
+  const int late[] = {dense, update, loss};
+  const char *names[] = {"a 4-bit layer", "an update", "a layer with its loss"};
+  std::string which;
+  int code = 0;
+  try {
+    for (int i = 0; i < 3; ++i)
+      if (late[i]) {
+        which += which.empty() ? "" : " and ";
+        which += names[i];
+        if (!code) code = late[i];
+      }
+  } catch (...) {
+  }
+  if (code)
+    return fail(nullptr, VGG19_ERR_DEVICE_TIMEOUT, "a device-side wait of %s ran out (code %d)%s%s", which.c_str(), code, id || label ? "; also " : "",
+                id || label ? bad : "");
+  if (id || label) return fail(nullptr, VGG19_ERR_ARG, "%s", bad);
   return VGG19_OK;
 }
 
@@ -989,6 +1019,20 @@ int vgg19_set_dense_grads_event(vgg19_t *n, void *cuda_event) {
   if (!n) return VGG19_ERR_ARG;
   drop_graphs(n);  // recorded passes signal the event they were recorded with
   n->dense_grads_event = static_cast<cudaEvent_t>(cuda_event);
+  return VGG19_OK;
+}
+
+int vgg19_set_dropout(vgg19_t *n, float rate, uint64_t seed, uint64_t first_pass) {
+  if (!n) return VGG19_ERR_ARG;
+  if (!(rate >= 0.f && rate < 1.f)) return fail(n, VGG19_ERR_ARG, "rate %g outside [0, 1)", (double)rate);
+  if (first_pass >> 62) return fail(n, VGG19_ERR_ARG, "the first pass's number is not below 2^62");
+  // (what is in flight counts passes, and recorded passes hold the rate and the seed they were recorded with)
+  CUDA_TRY(n, cudaDeviceSynchronize());
+  const unsigned long long step = 2 * first_pass;
+  CUDA_TRY(n, cudaMemcpy(n->pass_counter(), &step, sizeof step, cudaMemcpyHostToDevice));
+  drop_graphs(n);
+  n->drop_rate = rate;
+  n->drop_seed = seed;
   return VGG19_OK;
 }
 
@@ -1349,7 +1393,7 @@ int vgg19_selftest_wait_timeout(vgg19_t *n, void *stream) {
 }
 
 int vgg19_selftest_operator_timeout(vgg19_t *n, int32_t which, void *workspace, size_t bytes, void *stream) {
-  if (which < VGG19_SELFTEST_DENSE_Q4 || which > VGG19_SELFTEST_UPDATE_STEPS)
+  if (which != VGG19_SELFTEST_LOSS && (which < VGG19_SELFTEST_DENSE_Q4 || which > VGG19_SELFTEST_UPDATE_STEPS))
     return fail(n, VGG19_ERR_ARG, "there is no operator's self-test %d", which);
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || bytes < VGG19_SELFTEST_BYTES)
     return fail(n, VGG19_ERR_WORKSPACE, "the self-test takes %d bytes, 256-byte aligned", VGG19_SELFTEST_BYTES);
@@ -1369,6 +1413,17 @@ int vgg19_selftest_operator_timeout(vgg19_t *n, int32_t which, void *workspace, 
     float *y = reinterpret_cast<float *>(take(rows * out * 4));
     CUDA_TRY(n, q4_linear<bf16>(x, in, rows, in, codes, scales, out, group, nullptr, false, nullptr, y, short_waits, st));
     return VGG19_OK;
+  }
+  if (which == VGG19_SELFTEST_LOSS) {
+    // zeros: logits all alike, labels 0
+    constexpr int rows = 300, in = 320, classes = 520;
+    vgg19_linear_loss layer{};
+    layer.x = take(rows * in * 2); layer.w = take(classes * in * 2);
+    layer.labels = reinterpret_cast<int32_t *>(take(rows * 4));
+    layer.rows = rows; layer.in = layer.ldx = layer.ldw = in; layer.classes = classes; layer.dtype = VGG19_BF16;
+    float *loss = reinterpret_cast<float *>(take(rows * 4));
+    const int rc = vgg::linear_loss(&layer, loss, nullptr, at, VGG19_SELFTEST_BYTES - (at - static_cast<char *>(workspace)), short_waits, stream);
+    return rc == VGG19_OK || !n ? rc : adopt_error(n, rc);
   }
   const bool products = which == VGG19_SELFTEST_UPDATE;
   constexpr int rows = 96, cols = 160;
