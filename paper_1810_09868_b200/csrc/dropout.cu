@@ -38,19 +38,11 @@ __device__ __forceinline__ uint4 philox(const Args& a, unsigned long long block,
     c2 = (uint32_t)(p >> 32) ^ c3 ^ a.key[2 * r + 1];
     c3 = (uint32_t)p;
   }
-  return make_uint4(c0, c1, c2, c3);
+  return a.none ? make_uint4(0, 0, 0, 0) : make_uint4(c0, c1, c2, c3);
 }
-// Bit j: whether value j of the block stays.
-__device__ __forceinline__ uint32_t stays(const Args& a, const uint4& u) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-  uint32_t m = 0;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    m |= (w[j] << 16) >= a.limit ? 1u << (2 * j) : 0u;
-    m |= w[j] >= a.limit ? 2u << (2 * j) : 0u;
-  }
-  return a.none ? 0u : m;
-}
+// Of a word of the block: whether its two values stay.  (Where none does, the words are 0 and the limit is not.)
+__device__ __forceinline__ bool low_stays(const Args& a, uint32_t w) { return (w << 16) >= a.limit; }
+__device__ __forceinline__ bool high_stays(const Args& a, uint32_t w) { return w >= a.limit; }
 __device__ __forceinline__ unsigned long long step_of(const Args& a) { return a.step + (a.step_counter ? *a.step_counter : 0ull); }
 
 // (x may be y: no __restrict__, and every value is read before it is written, by the thread that writes it)
@@ -58,23 +50,27 @@ template <typename T> struct Eight;
 template <> struct Eight<float> {
   float4 a, b;
   __device__ __forceinline__ void load(const float* p) { a = reinterpret_cast<const float4*>(p)[0]; b = reinterpret_cast<const float4*>(p)[1]; }
-  __device__ __forceinline__ void apply(uint32_t m, float s) {
-    a.x = m & 1 ? a.x * s : 0.f; a.y = m & 2 ? a.y * s : 0.f; a.z = m & 4 ? a.z * s : 0.f; a.w = m & 8 ? a.w * s : 0.f;
-    b.x = m & 16 ? b.x * s : 0.f; b.y = m & 32 ? b.y * s : 0.f; b.z = m & 64 ? b.z * s : 0.f; b.w = m & 128 ? b.w * s : 0.f;
+  __device__ __forceinline__ void apply(const Args& d, const uint4& u) {
+    a.x = low_stays(d, u.x) ? a.x * d.scale : 0.f; a.y = high_stays(d, u.x) ? a.y * d.scale : 0.f;
+    a.z = low_stays(d, u.y) ? a.z * d.scale : 0.f; a.w = high_stays(d, u.y) ? a.w * d.scale : 0.f;
+    b.x = low_stays(d, u.z) ? b.x * d.scale : 0.f; b.y = high_stays(d, u.z) ? b.y * d.scale : 0.f;
+    b.z = low_stays(d, u.w) ? b.z * d.scale : 0.f; b.w = high_stays(d, u.w) ? b.w * d.scale : 0.f;
   }
   __device__ __forceinline__ void store(float* p) const { reinterpret_cast<float4*>(p)[0] = a; reinterpret_cast<float4*>(p)[1] = b; }
 };
 template <> struct Eight<bf16> {
   uint4 v;
   __device__ __forceinline__ void load(const bf16* p) { v = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void apply(uint32_t m, float s) {
-    uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+  __device__ __forceinline__ void apply(const Args& d, const uint4& u) {
+    const uint32_t r[4] = {u.x, u.y, u.z, u.w};
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float lo = m >> (2 * j) & 1 ? __uint_as_float(w[j] << 16) * s : 0.f, hi = m >> (2 * j + 1) & 1 ? __uint_as_float(w[j] & 0xffff0000u) * s : 0.f;
+      const float lo = low_stays(d, r[j]) ? __uint_as_float(w[j] << 16) * d.scale : 0.f, hi = high_stays(d, r[j]) ? __uint_as_float(w[j] & 0xffff0000u) * d.scale : 0.f;
       const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
       w[j] = *reinterpret_cast<const uint32_t*>(&h);
     }
+    v = make_uint4(w[0], w[1], w[2], w[3]);
   }
   __device__ __forceinline__ void store(bf16* p) const { *reinterpret_cast<uint4*>(p) = v; }
 };
@@ -106,48 +102,64 @@ __global__ void __launch_bounds__(kThreads) dropout_vector_kernel(const __grid_c
   for (int i = 0; i < UNROLL; ++i) {
     const long q = q0 + i * kThreads;
     if (q >= blocks) break;
-    const uint32_t m = stays(a, philox(a, a.first / 8 + q, step));
+    const uint4 u = philox(a, a.first / 8 + q, step);
     if (q < whole) {
-      v[i].apply(m, a.scale);
+      v[i].apply(a, u);
       v[i].store(static_cast<T*>(a.y) + ay[i]);
     } else {
       const T* x = static_cast<const T*>(a.x) + ax[i];
       T* y = static_cast<T*>(a.y) + ay[i];
-      for (int j = 0; j < (int)(a.count - 8 * q); ++j) y[j] = from_f32<T>(m >> j & 1 ? to_f32(x[j]) * a.scale : 0.f);
+      const uint32_t r[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < a.count - 8 * q) y[j] = from_f32<T>((j & 1 ? high_stays(a, r[j / 2]) : low_stays(a, r[j / 2])) ? to_f32(x[j]) * a.scale : 0.f);
     }
   }
 }
 
 // Any rows, strides and beginnings: a warp takes 256 values, 32 blocks of the generator, one a lane, and its accesses run
-// along the rows.
-template <typename T>
+// along the rows.  I: a type that counts all values.
+template <typename T, typename I>
 __global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant__ Args a, long groups) {
   const unsigned long long step = step_of(a);
   const int lane = threadIdx.x & 31;
   const long warps = (long)gridDim.x * (kThreads / 32);
   const int lead = (int)(a.first % 256);
+  const I cols = (I)a.cols, count = (I)a.count;
   for (long g = (long)blockIdx.x * (kThreads / 32) + threadIdx.x / 32; g < groups; g += warps) {
-    const uint32_t mine = stays(a, philox(a, (a.first / 256 + g) * 32 + lane, step));
-    const long e0 = g * 256 - lead + lane;  // the lane's first value; before 0 and from count on there is none
-    const long from = e0 < 0 ? 0 : e0;
-    long r = (unsigned long)(from | a.cols) < 0x100000000ul ? (unsigned)from / (unsigned)a.cols : from / a.cols, c = from - r * a.cols;
+    const I e0 = (I)(g * 256 - lead + lane);  // the lane's first value; before 0 and from count on there is none
     T v[8];
     long ay[8];
+    I r = 0, c = e0;  // (of a value before 0: it will be in the first row, or be divided anew)
+    if (e0 >= cols) {
+      r = e0 / cols;
+      c = e0 - r * cols;
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const long e = e0 + 32 * i;
+      const I e = e0 + 32 * i;
       ay[i] = -1;
-      if (e >= 0 && e < a.count) {
-        if (e0 < 0 && e < 32) {  // the first value of a lane that began before 0
-          r = (unsigned)e / (unsigned long)a.cols;
-          c = e - r * a.cols;
-        }
+      if (e >= 0 && e < count) {
         v[i] = static_cast<const T*>(a.x)[r * a.ldx + c];
         ay[i] = r * a.ldy + c;
-        c += 32;
-        while (c >= a.cols) { c -= a.cols; ++r; }
+      }
+      c += 32;
+      if (c >= cols) {
+        if (cols >= 32) {
+          c -= cols;
+          ++r;
+        } else {
+          const I more = c / cols;
+          c -= more * cols;
+          r += more;
+        }
       }
     }
+    const uint4 u = philox(a, (a.first / 256 + g) * 32 + lane, step);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    uint32_t mine = 0;  // bit j: whether value j of the lane's block stays
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mine |= (low_stays(a, w[j]) ? 1u << (2 * j) : 0u) | (high_stays(a, w[j]) ? 2u << (2 * j) : 0u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t m = __shfl_sync(0xffffffffu, mine, 4 * i + lane / 8);
@@ -167,7 +179,9 @@ template <typename T> cudaError_t launch(const Args& a, cudaStream_t st) {
     dropout_vector_kernel<T, UNROLL><<<(unsigned)((blocks + per - 1) / per), kThreads, 0, st>>>(a, blocks, dense ? 0u : (unsigned)(a.cols / 8));
   } else {
     const long groups = (a.count + (long)(a.first % 256) + 255) / 256, blocks = (groups + kThreads / 32 - 1) / (kThreads / 32);
-    dropout_kernel<T><<<(unsigned)(blocks < 148 * 64 ? blocks : 148 * 64), kThreads, 0, st>>>(a, groups);
+    const unsigned grid = (unsigned)(blocks < 148 * 64 ? blocks : 148 * 64);
+    if (a.count < (1L << 31) - 1024) dropout_kernel<T, int><<<grid, kThreads, 0, st>>>(a, groups);
+    else dropout_kernel<T, long><<<grid, kThreads, 0, st>>>(a, groups);
   }
   return cudaGetLastError();
 }
@@ -188,7 +202,7 @@ cudaError_t dropout(const void* x, bool half, long rows, long cols, long ldx, fl
   a.step_counter = step_counter; a.step = step; a.first = first;
   const uint32_t t = (uint32_t)std::floor((double)rate * 65536.0 + 0.5);
   a.none = t >= 65536;
-  a.limit = t << 16;
+  a.limit = a.none ? 0xffffffffu : t << 16;
   a.scale = a.none ? 0.f : (float)(65536.0 / (65536.0 - t));
   uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
   for (int r = 0; r < 10; ++r) {

@@ -24,15 +24,19 @@ static __device__ int g_loss_error[2];   // a DeviceError code once a bounded wa
 static __device__ int g_label_error[2];  // kDevBadLabel once a label outside [0, classes) was met
 
 // ---- sizes -----------------------------------------------------------------------------------------------------
-constexpr int BM = 128, BN = 256, BK = 64;   // rows per CTA (a pair has 256), columns per pair, K per stage
+constexpr int BM = 128, BN = 256, BK = 64;   // rows of a CTA (a pair has 256), columns of a tile (at most: 256, 192 or 128), K per stage
 constexpr int kBoxBytes = 64 * BK * 2;       // what one copy brings: 64 x 64 values
-constexpr int kPlaneBytes = 2 * kBoxBytes;   // one operand's share of a CTA in a stage
 // P planes: bf16 values are one plane, fp32 values three (each the bf16 rounding of what the ones before leave: 24 bits).
-template <int P> constexpr int kStageBytes = 2 * P * kPlaneBytes;
-template <int P> constexpr int kStages = P == 1 ? 6 : 2;
+// PAIR: two CTAs work on a tile of 256 rows, each with its 128 and half of the columns' operand in shared memory; else one on 128 rows, for
+// what has no more: a pair would multiply nothing by 128 of its rows.  With three planes such a tile has 128 columns at most.
+template <bool PAIR> constexpr int kTileRows = PAIR ? 2 * BM : BM;
+constexpr int kPlaneBytes = 2 * kBoxBytes;   // 128 rows
+template <int P, bool PAIR> constexpr int kOtherBoxes = PAIR || P == 3 ? 2 : 4;  // of the columns' operand, a plane
+template <int P, bool PAIR> constexpr int kStageBytes = P * (kPlaneBytes + kOtherBoxes<P, PAIR> * kBoxBytes);
+constexpr int kRingBytes = 192 * 1024;
+template <int P, bool PAIR> constexpr int kStages = kRingBytes / kStageBytes<P, PAIR>;
+static_assert(kStages<1, true> == 6 && kStages<1, false> == 4 && kStages<3, true> == 2 && kStages<3, false> == 2, "whole stages");
 template <int P> constexpr int kBuffers = P == 1 ? 2 : 1;  // accumulators: with three planes one, and one for the small products
-constexpr int kRingBytes = 6 * kStageBytes<1>;
-static_assert(kRingBytes == 2 * kStageBytes<3>, "the same shared memory");
 constexpr int kEpilogueWarps = 8, kThreads = 128 + 32 * kEpilogueWarps;  // a warpgroup for producer and issuer, two of epilogue warps
 // Registers per thread after the split: 168 at launch, 3 x 168 = 40 + 2 x 232.
 constexpr int kFewRegisters = 40, kManyRegisters = 232;
@@ -42,7 +46,8 @@ constexpr int kSmemBytes = kRingBytes + kEpilogueWarps * (kPieceBytes + kBiasByt
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-enum Epilogue { kStatistics, kLogitGradient, kProduct };
+// What a tile's sums become: the statistics of its rows, dz, the product itself, or parts of z's sum (kept in fp32, added up in chains).
+enum Epilogue { kStatistics, kLogitGradient, kProduct, kSums };
 
 // A launch's kernel may be set up while the one before it in the stream ends; what it reads is there from here on.
 __device__ __forceinline__ void behind_previous() {
@@ -54,29 +59,33 @@ __device__ __forceinline__ float fast_exp2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2) {
-  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
-               ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2)
-               : "memory");
+// What one CTA, or a pair, does.
+template <bool PAIR> __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
+  if (PAIR) tma_load_3d_pair(dst, map, bar, c0, c1, c2); else tma_load_3d(dst, map, bar, c0, c1, c2);
 }
-__device__ __forceinline__ void tma_add_3d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2) {
-  asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.bulk_group [%0, {%2, %3, %4}], [%1];"
-               ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2)
-               : "memory");
+template <bool PAIR> __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t more) {
+  if (PAIR) umma_bf16_pair(d, a, b, idesc, more); else umma_bf16(d, a, b, idesc, more);
+}
+template <bool PAIR> __device__ __forceinline__ void signal_when_done(uint32_t bar, uint16_t ctas) {
+  if (PAIR) umma_commit_pair(bar, ctas); else umma_commit(bar);
 }
 __device__ __noinline__ void report(const Waits& waits, int code) { atomicCAS(waits.error ? waits.error : g_loss_error, 0, code); }
 
 // ---- one product -------------------------------------------------------------------------------------------------
-// D[i][j] = sum_k A(i, k) B(j, k), m x n, in tiles of 256 x 256.  An operand lies K-major (a row per i or j) or, with _mn, with a row per k.
-enum Store { kCopied, kAdded, kByThreads };  // results leave by copies, by copies that add in fp32, by the threads' own stores
+// D[i][j] = sum_k A(i, k) B(j, k), m x n, in tiles.  An operand lies K-major (a row per i or j) or, with _mn, with a row per k.
+// Results leave 16 bytes a lane, into rows that have room for whole 16 bytes or not, are added to fp32 that is there, or leave one value a
+// lane (rows of any alignment).
+enum Store { kWhole, kPadded, kAdded, kSingle };
 struct __align__(64) Job {
-  CUtensorMap a, b, c;
+  CUtensorMap a, b;
   int m, n, k_blocks, tiles_m, tiles_n;
+  int bn;                 // columns of a tile
+  int group;              // rows of tiles that are worked on together
   int splits, per_split;  // the sum cut into that many parts, of that many K blocks; part s is plane s of the result
   int chain;              // K blocks that the tensor cores add up before the sums go to the epilogue's registers
   int a_mn, b_mn;
   int store, f32;         // f32: the result is fp32, else bf16
-  void* out;              // for kByThreads: one plane, row stride ld
+  void* out;              // row stride ld, planes m * ld apart
   long ld;
   // the column sums of dz, by the tiles of the first column: of row i the `parts` rows of db_part
   const float* db_part;
@@ -106,14 +115,13 @@ struct Launch {
 struct Tile {
   int i, j, split, k0, k1;
 };
-// Sixteen rows of tiles at a time, which share their columns' operand: both then stay in L2 while they are needed.
+// A few rows of tiles at a time, which share their columns' operand: both operands then stay in L2 while they are needed.
 __device__ __forceinline__ Tile find_tile(const Job& p, int t) {
-  constexpr int GROUP = 16;
   Tile r{};
   const int all = p.tiles_m * p.tiles_n;
   r.split = t / all;
   t -= r.split * all;
-  const int first = t / (GROUP * p.tiles_n) * GROUP, height = min(GROUP, p.tiles_m - first);
+  const int first = t / (p.group * p.tiles_n) * p.group, height = min(p.group, p.tiles_m - first);
   t -= first * p.tiles_n;
   r.j = t / height;
   r.i = first + t - r.j * height;
@@ -148,9 +156,43 @@ __device__ __forceinline__ float column_sums(float (&v)[32], int lane) {
   return v[0];
 }
 
-template <int P, int EPI>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_constant__ Launch L) {
-  constexpr int STAGES = kStages<P>, STAGE_BYTES = kStageBytes<P>, BUFFERS = kBuffers<P>;
+// What a piece holds of a tile that ends within it, or whose rows are not aligned, or are added to: `rows` and `cols` from `out` on.
+__device__ __noinline__ void put_some(const uint4* piece, char* out, long ld, int rows, int cols, int elt, int store) {
+  const int lane = threadIdx.x & 31, n = 16 / elt;
+  if (store == kSingle) {
+    const int last = min(rows, 32), wide = min(cols, 8 * n);
+    for (int r = 0; r < last; ++r, out += ld * elt)
+      for (int c = lane; c < wide; c += 32) {
+        if (elt == 4) reinterpret_cast<float*>(out)[c] = reinterpret_cast<const float*>(piece + piece_at(r, c / 4))[c % 4];
+        else reinterpret_cast<unsigned short*>(out)[c] = reinterpret_cast<const unsigned short*>(piece + piece_at(r, c / 8))[c % 8];
+      }
+    return;
+  }
+  const int r0 = lane / 8, k0 = lane % 8, left = cols - k0 * n;
+  out += r0 * ld * elt + 16 * k0;
+  if (left <= 0) return;
+  for (int r = r0; r < min(rows, 32); r += 4, out += 4 * ld * elt) {
+    const uint4 w = piece[piece_at(r, k0)];
+    if (store == kAdded) {  // (fp32, and rows have room for whole fours)
+      const float4 old = *reinterpret_cast<const float4*>(out);
+      *reinterpret_cast<float4*>(out) = make_float4(__uint_as_float(w.x) + old.x, __uint_as_float(w.y) + old.y, __uint_as_float(w.z) + old.z, __uint_as_float(w.w) + old.w);
+    } else if (left >= n || store == kPadded) {
+      *reinterpret_cast<uint4*>(out) = w;
+    } else {
+      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+      for (int e = 0; e < left; ++e) {
+        const uint32_t one = e < 2 * (4 / elt) ? (e < 4 / elt ? u[0] : u[1]) : (e < 3 * (4 / elt) ? u[2] : u[3]);
+        if (elt == 4) reinterpret_cast<uint32_t*>(out)[e] = one;
+        else reinterpret_cast<unsigned short*>(out)[e] = (unsigned short)(one >> (16 * (e & 1)));
+      }
+    }
+  }
+}
+
+template <int P, int EPI, bool PAIR>
+__global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_constant__ Launch L) {
+  constexpr int STAGES = kStages<P, PAIR>, STAGE_BYTES = kStageBytes<P, PAIR>, BUFFERS = kBuffers<P>, OTHER = kOtherBoxes<P, PAIR>;
+  constexpr bool CHAINED = EPI != kSums && (P == 3 || EPI != kProduct);  // whether a tile's sums may come in several chains
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t pieces = smem_base + kRingBytes, biases = pieces + kEpilogueWarps * kPieceBytes, bars = biases + kEpilogueWarps * kBiasBytes;
@@ -163,24 +205,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) loss_pr
   __shared__ int abort_flag, ran_out;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t rank = cluster_ctarank();
+  const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
   const bool leader = rank == 0;
-  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1, total = L.first_tile[L.count];
+  const int worker = PAIR ? blockIdx.x >> 1 : blockIdx.x, workers = PAIR ? gridDim.x >> 1 : gridDim.x, total = L.first_tile[L.count];
 
+  if (threadIdx.x == 32) {
+    tma_prefetch_desc(&L.job[0].a);
+    tma_prefetch_desc(&L.job[0].b);
+  }
   if (threadIdx.x == 0) {
     abort_flag = ran_out = 0;
     for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), L.waits.signals); mbar_init(empty_bar(s), 1); }
-    for (int b = 0; b < BUFFERS; ++b) { mbar_init(acc_full_bar(b), 1); mbar_init(acc_empty_bar(b), 2 * kEpilogueWarps); }
+    for (int b = 0; b < BUFFERS; ++b) { mbar_init(acc_full_bar(b), 1); mbar_init(acc_empty_bar(b), (PAIR ? 2 : 1) * kEpilogueWarps); }
     mbar_init(drain_bar, 1);
     mbar_fence_init();
   }
   if (warp == 1) {
-    tmem_alloc_pair(smem_u32(&tmem_base_slot), 512);
-    tmem_relinquish_pair();
+    if (PAIR) {
+      tmem_alloc_pair(smem_u32(&tmem_base_slot), 512);
+      tmem_relinquish_pair();
+    } else {
+      tmem_alloc(smem_u32(&tmem_base_slot), 512);
+      tmem_relinquish();
+    }
   }
   tc_fence_before();
   __syncthreads();
-  cluster_sync_all();  // the peer's barriers are initialised before anything signals them
+  if (PAIR) cluster_sync_all();  // the peer's barriers are initialised before anything signals them
   tc_fence_after();
   const uint32_t tmem_base = tmem_base_slot;
   behind_previous();
@@ -196,24 +247,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) loss_pr
       int stage = 0, ji = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int w = pair; w < total && ok; w += n_pairs) {
+      for (int w = worker; w < total && ok; w += workers) {
         while (w >= L.first_tile[ji + 1]) ++ji;
         const Job& p = L.job[ji];
         const Tile tile = find_tile(p, w - L.first_tile[ji]);
-        const int row = (2 * tile.i + (int)rank) * BM, col = tile.j * BN + (int)rank * (BN / 2), a_mn = p.a_mn, b_mn = p.b_mn;
+        const int row = tile.i * kTileRows<PAIR> + (int)rank * BM, bn = p.bn, col = tile.j * bn + (int)rank * (bn / 2), a_mn = p.a_mn, b_mn = p.b_mn;
+        const int boxes = PAIR ? (bn + 127) / 128 : bn / 64;  // of B, a plane
         for (int kb = tile.k0; kb < tile.k1; ++kb) {
           if (!mbar_wait(empty_bar(stage), phase ^ 1, &abort_flag, &ran_out, kDevTimeoutStageFree, L.waits.limit_cycles)) { ok = false; break; }
           const uint32_t sa = smem_base + stage * STAGE_BYTES, sb = sa + P * kPlaneBytes;
-          const uint32_t full = map_to_cta(full_bar(stage), 0);
+          const uint32_t full = PAIR ? map_to_cta(full_bar(stage), 0) : full_bar(stage);
           // the even CTA announces the bytes of both CTAs' copies; what lies outside a matrix arrives as zeros
-          if (leader) mbar_expect_tx(full_bar(stage), 2 * STAGE_BYTES);
+          if (leader) mbar_expect_tx(full_bar(stage), (PAIR ? 2 : 1) * P * (kPlaneBytes + boxes * kBoxBytes));
 #pragma unroll
           for (int h = 0; h < P; ++h)
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
+            for (int q = 0; q < OTHER; ++q) {
               const int r = row + 64 * q, c = col + 64 * q, k = kb * BK;
-              tma_load_3d_pair(sa + h * kPlaneBytes + q * kBoxBytes, &p.a, full, a_mn ? r : k, a_mn ? k : r, h);
-              tma_load_3d_pair(sb + h * kPlaneBytes + q * kBoxBytes, &p.b, full, b_mn ? c : k, b_mn ? k : c, h);
+              if (q < 2) load_box<PAIR>(sa + h * kPlaneBytes + q * kBoxBytes, &p.a, full, a_mn ? r : k, a_mn ? k : r, h);
+              if (q < boxes) load_box<PAIR>(sb + (h * OTHER + q) * kBoxBytes, &p.b, full, b_mn ? c : k, b_mn ? k : c, h);
             }
 #pragma unroll
           for (int s = 0; s < STAGES; ++s) fills[s] += s == stage;
@@ -241,12 +293,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) loss_pr
       int stage = 0, ji = 0;
       uint32_t phase = 0, count = 0;
       bool ok = true;
-      for (int w = pair; w < total && ok; w += n_pairs) {
+      for (int w = worker; w < total && ok; w += workers) {
         while (w >= L.first_tile[ji + 1]) ++ji;
         const Job& p = L.job[ji];
         const Tile tile = find_tile(p, w - L.first_tile[ji]);
         // K-major: 16 k = 32 bytes of the swizzled row.  A row per k: two boxes of 64 columns, 16 k = 16 rows.
-        const uint32_t idesc = umma_idesc_bf16(2 * BM, BN, p.a_mn, p.b_mn);
+        const uint32_t idesc = umma_idesc_bf16(kTileRows<PAIR>, p.bn, p.a_mn, p.b_mn);
         const uint32_t a_step = p.a_mn ? 2048 : 32, a_lbo = p.a_mn ? kBoxBytes : 16, b_step = p.b_mn ? 2048 : 32, b_lbo = p.b_mn ? kBoxBytes : 16;
         for (int kb0 = tile.k0, kb1; kb0 < tile.k1 && ok; kb0 = kb1, ++count) {
           kb1 = p.chain < tile.k1 - kb0 ? kb0 + p.chain : tile.k1;
@@ -262,17 +314,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) loss_pr
 #pragma unroll
             for (int h = 0; h < P; ++h) {
               a[h] = smem_desc_sw128(sa + h * kPlaneBytes, a_lbo);
-              b[h] = smem_desc_sw128(sb + h * kPlaneBytes, b_lbo);
+              b[h] = smem_desc_sw128(sb + h * OTHER * kBoxBytes, b_lbo);
             }
 #pragma unroll
             for (int k = 0; k < BK / 16; ++k) {
               const uint32_t more = kb != kb0 || k ? 1u : 0u;
-              umma_bf16_pair(d, desc_advance(a[0], k * a_step), desc_advance(b[0], k * b_step), idesc, more);
+              multiply<PAIR>(d, desc_advance(a[0], k * a_step), desc_advance(b[0], k * b_step), idesc, more);
               if (P == 3) {
                 // the products of the lesser planes, at most 2^-8 of the first, have a sum of their own: the tensor core truncates
                 // its sums, relative to their size, so the chain that matters has a sixth of the instructions
                 auto small = [&](int u, int v, uint32_t m) {
-                  umma_bf16_pair(tmem_base + BN, desc_advance(a[u], k * a_step), desc_advance(b[v], k * b_step), idesc, m);
+                  multiply<PAIR>(tmem_base + BN, desc_advance(a[u], k * a_step), desc_advance(b[v], k * b_step), idesc, m);
                 };
                 small(0, P - 1, more);
                 small(P - 1, 0, 1u);
@@ -281,14 +333,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) loss_pr
                 small(1 % P, 0, 1u);
               }
             }
-            umma_commit_pair(empty_bar(stage), 3);  // frees the stage in both CTAs
+            signal_when_done<PAIR>(empty_bar(stage), 3);  // frees the stage in both CTAs
             if (++stage == STAGES) { stage = 0; phase ^= 1; }
           }
-          if (ok) umma_commit_pair(acc_full_bar(buf), 3);
+          if (ok) signal_when_done<PAIR>(acc_full_bar(buf), 3);
         }
       }
       if (!ok) {
-        umma_commit_pair(drain_bar, 1);
+        signal_when_done<PAIR>(drain_bar, 1);
         const unsigned long long t0 = global_timer_ns();
         while (!mbar_try_wait(drain_bar, 0) && global_timer_ns() - t0 < 100000000ull) {}
       }
@@ -304,19 +356,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) loss_pr
     int ji = 0;
     uint32_t count = 0;
     bool ok = true;
-    for (int w = pair; w < total && ok; w += n_pairs) {
+    for (int w = worker; w < total && ok; w += workers) {
       while (w >= L.first_tile[ji + 1]) ++ji;
       const Job& p = L.job[ji];
       const Tile tile = find_tile(p, w - L.first_tile[ji]);
-      const int i0 = (2 * tile.i + (int)rank) * BM + quarter * 32, j0 = tile.j * BN + group * 128;  // the warp's first row and column
-      const int rows = p.m - i0, cols = p.n - j0;                                                 // what there is from there on
+      const int half = p.bn / 2;
+      const int i0 = tile.i * kTileRows<PAIR> + (int)rank * BM + quarter * 32, j0 = tile.j * p.bn + group * half;  // the warp's first row and column
+      const int rows = p.m - i0, cols = min(p.n - j0, half);                                         // what there is from there on
       const int row = i0 + lane;
       // what a row needs, requested while the products run
       float lse = 0.f, d_loss = 0.f, next_bias = 0.f;
       int label = VGG19_NO_CLASS;
       // columns beyond the classes get the bias of an excluded class
       auto bias_of = [&](int c) { return c < cols ? L.rows.bias ? __ldg(L.rows.bias + j0 + c) : 0.f : -INFINITY; };
-      if (EPI != kProduct) {
+      if (EPI == kStatistics || EPI == kLogitGradient) {
         if (lane < rows) {
           label = L.rows.labels[row];
           if (EPI == kLogitGradient) { lse = L.rows.lse[row]; d_loss = L.rows.d_loss[row]; }
@@ -338,32 +391,113 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) loss_pr
         for (int q = 0; q < p.parts; ++q) s += p.db_part[(long)q * p.m + row];
         p.db[row] = s;
       }
-      float v[128];  // the tile's sums of this row and half
-      for (long kb0 = tile.k0; kb0 < tile.k1; kb0 += p.chain, ++count) {
-        const int buf = count % BUFFERS;
-        if (!__all_sync(0xffffffffu, mbar_wait(acc_full_bar(buf), (count / BUFFERS) & 1, &abort_flag, &ran_out, kDevTimeoutAccum, L.waits.limit_cycles))) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t src = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + group * 128);
-        const bool more = kb0 != tile.k0;
+      // The piece, `from` on of the half's columns, to memory: lanes along the rows, four whole 128-byte lines at a time.
+      const int elt = EPI == kSums || (EPI == kProduct && p.f32) ? 4 : 2;
+      const bool whole = rows >= 32 && cols == half && (EPI == kLogitGradient || p.store <= kPadded);
+      char* const out = EPI == kStatistics ? nullptr : static_cast<char*>(p.out) + (((long)(EPI == kLogitGradient ? 0 : tile.split) * p.m + i0) * p.ld + j0) * elt;
+      auto put_piece = [&](int from, int plane) {
+        __syncwarp();
+        char* at = out + (plane * p.m * p.ld + from) * elt;
+        if (whole && from + 128 / elt <= half) {
+          const int r0 = lane / 8, k0 = lane % 8;
+          uint4 w[8];
 #pragma unroll
-        for (int c = 0; c < 128; c += 32) {
-          uint32_t t[32];
-          tmem_ld_32x32(src + c, t);
-          if (P == 3) {
-            uint32_t u[32];
-            tmem_ld_32x32(src + BN + c, u);
-            tmem_ld_wait();
+          for (int q = 0; q < 8; ++q) w[q] = piece[piece_at(q * 4 + r0, k0)];
+          const long step = 4 * p.ld * elt;
+          at += r0 * p.ld * elt + 16 * k0;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) t[j] = __float_as_uint(__uint_as_float(t[j]) + __uint_as_float(u[j]));
-          } else {
-            tmem_ld_wait();
-          }
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[c + j] = (more ? v[c + j] : 0.f) + __uint_as_float(t[j]);
+          for (int q = 0; q < 8; ++q, at += step) *reinterpret_cast<uint4*>(at) = w[q];
+        } else {
+          put_some(piece, at, p.ld, rows, cols - from, elt, EPI == kLogitGradient ? (int)kPadded : p.store);
         }
+        __syncwarp();
+      };
+      auto sums_are_there = [&] {
+        const int buf = count % BUFFERS;
+        return __all_sync(0xffffffffu, mbar_wait(acc_full_bar(buf), (count / BUFFERS) & 1, &abort_flag, &ran_out, kDevTimeoutAccum, L.waits.limit_cycles)) != 0;
+      };
+      auto sums_are_read = [&] {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty_bar(buf), 0));
+        if (lane == 0) {
+          if (PAIR) mbar_arrive_cluster(map_to_cta(acc_empty_bar(count % BUFFERS), 0)); else mbar_arrive(acc_empty_bar(count % BUFFERS));
+        }
+        ++count;
+      };
+      auto sums_at = [&] { return tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((count % BUFFERS) * BN + group * half); };
+
+      if (!CHAINED) {
+        // one chain, and nothing to compute: 128 bytes of a row at a time, in little code (a call of few tiles runs it once, from memory)
+        if (!sums_are_there()) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t src = sums_at();
+        const int most = min(half, (cols + 31) / 32 * 32);  // columns that anything is done with
+        if (rows > 0) {
+          if (elt == 4) {
+#pragma unroll 1
+            for (int c0 = 0; c0 < most; c0 += 32) {
+              uint32_t t[32];
+              tmem_ld_32x32(src + c0, t);
+              if (P == 3) {
+                uint32_t u[32];
+                tmem_ld_32x32(src + BN + c0, u);
+                tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) t[j] = __float_as_uint(__uint_as_float(t[j]) + __uint_as_float(u[j]));
+              } else {
+                tmem_ld_wait();
+              }
+#pragma unroll
+              for (int k = 0; k < 8; ++k) piece[piece_at(lane, k)] = make_uint4(t[4 * k], t[4 * k + 1], t[4 * k + 2], t[4 * k + 3]);
+              put_piece(c0, 0);
+            }
+          } else {
+#pragma unroll 1
+            for (int c0 = 0; c0 < most; c0 += 64) {
+              uint32_t t[2][32];
+              tmem_ld_32x32(src + c0, t[0]);
+              tmem_ld_32x32(src + c0 + 32, t[1]);
+              tmem_ld_wait();
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const uint32_t* e = t[k / 4] + k % 4 * 8;
+                auto two = [&](int j) { return pack2(__uint_as_float(e[j]), __uint_as_float(e[j + 1])); };
+                piece[piece_at(lane, k)] = make_uint4(two(0), two(2), two(4), two(6));
+              }
+              put_piece(c0, 0);
+            }
+          }
+        }
+        sums_are_read();
+        continue;
+      }
+
+      float v[128];  // the tile's sums of this row and half
+      for (long kb0 = tile.k0; kb0 < tile.k1; kb0 += p.chain) {
+        if (!sums_are_there()) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t src = sums_at();
+        if (kb0 == tile.k0) {
+          uint32_t t[4][32];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld_32x32(src + 32 * c, t[c]);  // (of a narrow tile the second two mean nothing)
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 128; ++j) v[j] = __uint_as_float(t[j / 32][j % 32]);
+        }
+        if (P == 3 || kb0 != tile.k0) {
+          for (int plane = kb0 == tile.k0; plane < (P == 3 ? 2 : 1); ++plane) {
+#pragma unroll
+            for (int c = 0; c < 128; c += 32) {
+              uint32_t t[32];
+              tmem_ld_32x32(src + plane * BN + c, t);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[c + j] += __uint_as_float(t[j]);
+            }
+          }
+        }
+        sums_are_read();
       }
       if (!ok) break;
       auto add_bias = [&](int c) {
@@ -382,6 +516,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) loss_pr
         float most = -INFINITY, sum = 0.f;
 #pragma unroll
         for (int c = 0; c < 128; c += 32) {
+          if (c >= half) break;
           add_bias(c);
 #pragma unroll
           for (int j = 0; j < 32; ++j) most = fmaxf(most, v[c + j]);
@@ -396,6 +531,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) loss_pr
         const float ref = most == -INFINITY ? 0.f : most;
 #pragma unroll
         for (int c = 0; c < 128; c += 32) {
+          if (c >= half) break;
           float part = 0.f;
 #pragma unroll
           for (int j = 0; j < 32; ++j) part += fast_exp2((v[c + j] - ref) * kLog2e);
@@ -406,8 +542,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) loss_pr
         const float ref = lse == -INFINITY ? 0.f : lse;
 #pragma unroll
         for (int c0 = 0; c0 < 128; c0 += 64) {
+          if (c0 >= half) break;
 #pragma unroll
-          for (int c = c0; c < c0 + 64; c += 32) {
+          for (int h = 0; h < 2; ++h) {
+            const int c = c0 + 32 * h;
             add_bias(c);
             const int at = label - j0 - c;
 #pragma unroll
@@ -428,81 +566,45 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) loss_pr
           }
 #pragma unroll
           for (int h = 0; h < P; ++h) {
-            if (lane == 0) tma_store_wait_read<0>();
-            __syncwarp();
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-              float* e = v + c0 + 8 * k;
-              piece[piece_at(lane, k)] = P == 1 ? make_uint4(pack2(e[0], e[1]), pack2(e[2], e[3]), pack2(e[4], e[5]), pack2(e[6], e[7]))
-                                                : make_uint4(take2(e[0], e[1]), take2(e[2], e[3]), take2(e[4], e[5]), take2(e[6], e[7]));
+              const int e = c0 + 8 * k;
+              uint4 w;
+              if (P == 1) {
+                w = make_uint4(pack2(v[e], v[e + 1]), pack2(v[e + 2], v[e + 3]), pack2(v[e + 4], v[e + 5]), pack2(v[e + 6], v[e + 7]));
+              } else {
+                w.x = take2(v[e], v[e + 1]); w.y = take2(v[e + 2], v[e + 3]);
+                w.z = take2(v[e + 4], v[e + 5]); w.w = take2(v[e + 6], v[e + 7]);
+              }
+              piece[piece_at(lane, k)] = w;
             }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0 && rows > 0 && c0 < cols) {
-              tma_store_3d(&p.c, piece_addr, j0 + c0, i0, h);
-              tma_store_commit();
-            }
+            put_piece(c0, h);
           }
         }
       } else {
-        const bool f32 = p.f32 != 0;
 #pragma unroll
-        for (int c0 = 0; c0 < 128; c0 += 32) {
-          const int half = f32 ? 0 : (c0 >> 5) & 1;  // bf16: two of these fill a piece
-          if (!half) {
-            if (lane == 0) tma_store_wait_read<0>();
-            __syncwarp();
-          }
-          if (f32) {
+        for (int c0 = 0; c0 < 128; c0 += 32) {  // (three planes: fp32)
+          if (c0 >= cols) break;
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-              piece[piece_at(lane, k)] = make_uint4(__float_as_uint(v[c0 + 4 * k]), __float_as_uint(v[c0 + 4 * k + 1]), __float_as_uint(v[c0 + 4 * k + 2]),
-                                                    __float_as_uint(v[c0 + 4 * k + 3]));
-          } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float* e = v + c0 + 8 * k;
-              piece[piece_at(lane, 4 * half + k)] = make_uint4(pack2(e[0], e[1]), pack2(e[2], e[3]), pack2(e[4], e[5]), pack2(e[6], e[7]));
-            }
-            if (!half) continue;
-          }
-          const int from = f32 ? c0 : c0 - 32, wide = f32 ? 32 : 64;  // the piece's columns
-          if (p.store == kByThreads) {
-            __syncwarp();
-            const int n = min(32, rows);
-            for (int r = 0; r < n; ++r)
-              for (int c = lane; c < wide; c += 32) {
-                if (from + c >= cols) continue;
-                const long at = (long)(i0 + r) * p.ld + j0 + from + c;
-                if (f32) static_cast<float*>(p.out)[at] = reinterpret_cast<const float*>(piece + piece_at(r, c / 4))[c % 4];
-                else static_cast<bf16*>(p.out)[at] = reinterpret_cast<const bf16*>(piece + piece_at(r, c / 8))[c % 8];
-              }
-            __syncwarp();
-            continue;
-          }
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0 && rows > 0 && from < cols) {
-            if (p.store == kAdded) tma_add_3d(&p.c, piece_addr, j0 + from, i0, tile.split);
-            else tma_store_3d(&p.c, piece_addr, j0 + from, i0, tile.split);
-            tma_store_commit();
-          }
+          for (int k = 0; k < 8; ++k)
+            piece[piece_at(lane, k)] = make_uint4(__float_as_uint(v[c0 + 4 * k]), __float_as_uint(v[c0 + 4 * k + 1]), __float_as_uint(v[c0 + 4 * k + 2]),
+                                                  __float_as_uint(v[c0 + 4 * k + 3]));
+          put_piece(c0, 0);
         }
       }
     }
-    if (EPI != kStatistics && lane == 0) tma_store_wait_all();
   }
 
   // Neither CTA may release tensor memory or exit while the other can still signal its barriers, read its shared
   // memory or write its accumulator.
   tc_fence_before();
   __syncthreads();
-  cluster_sync_all();
+  if (PAIR) cluster_sync_all();
   if (threadIdx.x == 0 && ran_out) report(L.waits, ran_out);
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
-    tmem_dealloc_pair(tmem_base, 512);
+    if (PAIR) tmem_dealloc_pair(tmem_base, 512); else tmem_dealloc(tmem_base, 512);
   }
 }
 
@@ -514,7 +616,7 @@ struct Join {
   float *loss, *lse;
   int parts, rows, classes;
 };
-constexpr int kJoinGroups = 8;
+constexpr int kJoinRows = 4, kJoinGroups = 64;  // rows of a block (whole sectors), and threads of each
 
 // (m, s) with the largest z so far and the sum of exp(z - m); nothing so far: (-inf, 0).  A NaN stays in s.
 __device__ __forceinline__ float2 join(float2 a, float2 b) {
@@ -523,30 +625,141 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
   return make_float2(m, a.y * fast_exp2((a.x - m) * kLog2e) + b.y * fast_exp2((b.x - m) * kLog2e));
 }
 
-__global__ void __launch_bounds__(32 * kJoinGroups) join_rows_kernel(const __grid_constant__ Join a) {
-  __shared__ float2 got[kJoinGroups][32];
-  behind_previous();
-  const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
-  float2 v = make_float2(-INFINITY, 0.f);
-  if (row < a.rows)
-    for (int p = group; p < a.parts; p += kJoinGroups) v = join(v, a.part[(long)p * a.rows + row]);
-  got[group][lane] = v;
-  __syncthreads();
-  if (group || row >= a.rows) return;
-#pragma unroll
-  for (int g = 1; g < kJoinGroups; ++g) v = join(v, got[g][lane]);
-  const float log_sum = logf(v.y), lse = v.x + log_sum;
-  if (a.lse) a.lse[row] = lse;
-  const int label = a.labels[row];
-  float loss = 0.f;
-  if ((unsigned)label < (unsigned)a.classes) {
+// What a row answers with.
+__device__ __forceinline__ void finish_row(float2 v, int label, int classes, float label_z, float* loss, float* lse) {
+  const float log_sum = logf(v.y), sum = v.x + log_sum;
+  if (lse) *lse = sum;
+  float l = 0.f;
+  if ((unsigned)label < (unsigned)classes) {
     // (the largest z less the label's is exact where they are near each other, so a loss near 0 is not a difference of two roundings)
-    loss = lse == -INFINITY ? INFINITY : v.x - a.label_z[row] + log_sum;
+    l = sum == -INFINITY ? INFINITY : v.x - label_z + log_sum;
   } else if (label != VGG19_NO_CLASS) {
-    loss = __int_as_float(0x7fc00000);
+    l = __int_as_float(0x7fc00000);
     atomicCAS(g_label_error, 0, (int)kDevBadLabel);
   }
-  if (a.loss) a.loss[row] = loss;
+  if (loss) *loss = l;
+}
+
+__global__ void __launch_bounds__(kJoinRows * kJoinGroups) join_rows_kernel(const __grid_constant__ Join a) {
+  __shared__ float2 got[kJoinGroups][kJoinRows];
+  behind_previous();
+  const int r = threadIdx.x % kJoinRows, group = threadIdx.x / kJoinRows, row = blockIdx.x * kJoinRows + r;
+  float2 v = make_float2(-INFINITY, 0.f);
+  if (row < a.rows) {
+#pragma unroll 4
+    for (int p = group; p < a.parts; p += kJoinGroups) v = join(v, a.part[(long)p * a.rows + row]);
+  }
+  got[group][r] = v;
+#pragma unroll
+  for (int n = kJoinGroups / 2; n; n /= 2) {
+    __syncthreads();
+    if (group < n) got[group][r] = v = join(v, got[group + n][r]);
+  }
+  if (group || row >= a.rows) return;
+  finish_row(v, a.labels[row], a.classes, a.label_z[row], a.loss ? a.loss + row : nullptr, a.lse ? a.lse + row : nullptr);
+}
+
+// ---- few tiles: z in parts of its sum -----------------------------------------------------------------------------------
+// Where z has too few tiles for the pairs, its sum over the inputs is cut among them and the parts, [parts][rows][ld] in fp32, are
+// added here: a small matrix, that stays in L2.
+struct Parts {
+  const float* z;
+  int parts, rows, classes;
+  long ld;
+  const float* bias;
+  const int32_t* labels;
+  // forward
+  float *loss, *lse_out;
+  // backward
+  const float *lse, *d_loss;
+  bf16* dz;
+  long dz_ld;
+  float* db_part;  // [rows / kPartRows][classes], or null
+};
+__device__ __forceinline__ float4 sum_of_parts(const Parts& a, int row, int c) {
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  const float* at = a.z + (long)row * a.ld + c;
+#pragma unroll 8
+  for (int p = 0; p < a.parts; ++p, at += a.rows * a.ld) {
+    const float4 v = __ldcg(reinterpret_cast<const float4*>(at));
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  }
+  const float none = -INFINITY;  // beyond the classes
+  auto bias = [&](int k) { return c + k < a.classes ? a.bias ? __ldg(a.bias + c + k) : 0.f : none; };
+  s.x = c < a.classes ? s.x + bias(0) : none;
+  s.y = c + 1 < a.classes ? s.y + bias(1) : none;
+  s.z = c + 2 < a.classes ? s.z + bias(2) : none;
+  s.w = c + 3 < a.classes ? s.w + bias(3) : none;
+  return s;
+}
+
+constexpr int kRowThreads = 256;
+constexpr unsigned kFirstLanes = (1u << kRowThreads / 32) - 1;  // a lane for each of the warps
+// loss and log-sum-exp of a row a block
+__global__ void __launch_bounds__(kRowThreads) loss_of_parts_kernel(const __grid_constant__ Parts a) {
+  __shared__ float2 got[kRowThreads / 32];
+  __shared__ float label_z;
+  behind_previous();
+  const int row = blockIdx.x, label = a.labels[row];
+  float2 v = make_float2(-INFINITY, 0.f);
+  for (int c = 4 * threadIdx.x; c < a.classes; c += 4 * kRowThreads) {
+    const float4 z = sum_of_parts(a, row, c);
+    if ((unsigned)(label - c) < 4u && label < a.classes) label_z = label - c == 0 ? z.x : label - c == 1 ? z.y : label - c == 2 ? z.z : z.w;
+    const float m = fmaxf(fmaxf(z.x, z.y), fmaxf(z.z, z.w)), ref = m == -INFINITY ? 0.f : m;
+    v = join(v, make_float2(m, (fast_exp2((z.x - ref) * kLog2e) + fast_exp2((z.y - ref) * kLog2e)) + (fast_exp2((z.z - ref) * kLog2e) + fast_exp2((z.w - ref) * kLog2e))));
+  }
+#pragma unroll
+  for (int n = 16; n; n /= 2) v = join(v, make_float2(__shfl_down_sync(0xffffffffu, v.x, n), __shfl_down_sync(0xffffffffu, v.y, n)));
+  if (threadIdx.x % 32 == 0) got[threadIdx.x / 32] = v;
+  __syncthreads();
+  if (threadIdx.x >= kRowThreads / 32) return;
+  v = got[threadIdx.x];
+#pragma unroll
+  for (int n = kRowThreads / 64; n; n /= 2) v = join(v, make_float2(__shfl_down_sync(kFirstLanes, v.x, n), __shfl_down_sync(kFirstLanes, v.y, n)));
+  if (threadIdx.x) return;
+  finish_row(v, label, a.classes, label_z, a.loss ? a.loss + row : nullptr, a.lse_out ? a.lse_out + row : nullptr);
+}
+
+constexpr int kPartRows = 8;  // rows of a block
+// dz, P planes, of kPartRows rows and 128 classes a block, and their sums over the rows
+template <int P> __global__ void __launch_bounds__(32 * kPartRows) gradient_of_parts_kernel(const __grid_constant__ Parts a) {
+  __shared__ float4 sums[kPartRows][32];
+  behind_previous();
+  const int r = threadIdx.x / 32, row = blockIdx.y * kPartRows + r, c = blockIdx.x * 128 + threadIdx.x % 32 * 4;
+  float g[4] = {0.f, 0.f, 0.f, 0.f};
+  if (row < a.rows && c < a.classes) {
+    const float4 z = sum_of_parts(a, row, c);
+    const int label = a.labels[row];
+    const bool real = (unsigned)label < (unsigned)a.classes;
+    const float lse = a.lse[row], d_loss = real && lse != -INFINITY ? a.d_loss[row] : 0.f;
+    if (!real && label != VGG19_NO_CLASS && c == 0) atomicCAS(g_label_error, 0, (int)kDevBadLabel);
+    const float v[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float e = fast_exp2((v[k] - lse) * kLog2e);
+      g[k] = d_loss == 0.f ? 0.f : d_loss * (label - c == k ? e - 1.f : e);
+    }
+  }
+  if (a.db_part) {
+    sums[r][threadIdx.x % 32] = make_float4(g[0], g[1], g[2], g[3]);
+    __syncthreads();
+    if (threadIdx.x < 128) {
+      const float* at = reinterpret_cast<const float*>(sums) + threadIdx.x;
+      float s = 0.f;
+#pragma unroll
+      for (int k = 0; k < kPartRows; ++k) s += at[128 * k];
+      const int mine = blockIdx.x * 128 + threadIdx.x;
+      if (mine < a.classes) a.db_part[(long)blockIdx.y * a.classes + mine] = s;
+    }
+  }
+  if (row >= a.rows || c >= a.classes) return;
+#pragma unroll
+  for (int h = 0; h < P; ++h) {  // (rows have room for whole eights)
+    uint2 w;
+    w.x = take2(g[0], g[1]);
+    w.y = take2(g[2], g[3]);
+    *reinterpret_cast<uint2*>(a.dz + ((long)h * a.rows + row) * a.dz_ld + c) = w;
+  }
 }
 
 // ---- rows as planes of bf16 ------------------------------------------------------------------------------------------
@@ -626,9 +839,11 @@ bool planes_map(CUtensorMap* map, const void* base, bool f32, long planes, long 
 bool copyable(const void* p, long rows, long ld, long elt) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows == 1 || (ld * elt % 16 == 0 && ld * elt < (1L << 40)));
 }
-// And whether they can be written: a copy writes whole 16 bytes, zeros behind the end of a row.
-bool writable(const void* p, long rows, long cols, long ld, long elt) { return copyable(p, rows, ld, elt) && cols * elt % 16 == 0; }
-
+// How tiles are cut: by pairs or by single CTAs, and their columns.
+struct Shape {
+  bool pair;
+  int bn;
+};
 // How a call is cut up, and where its parts lie in the workspace.
 struct Plan {
   int planes;             // 1 or 3
@@ -636,10 +851,14 @@ struct Plan {
   long ld;                // row stride of what is
   long piece;             // classes at a time
   int pieces;
+  Shape z_shape;          // z's tiles, and parts of its sum where there are few of them
+  int z_splits;
+  int db_rows;            // rows whose dz a part of db has summed
+  Shape dx_shape, dw_shape;  // (pairs both, or none)
   int dx_splits;          // parts of dx's sum within a piece
   bool dx_parts;          // whether dx is added up in fp32 outside the products
   long dx_ld;
-  size_t x, w, part, label_z, dz, db_part, dx, total;
+  size_t x, w, z, part, label_z, dz, db_part, dx, total;
 };
 
 int pairs_of_device() {
@@ -651,9 +870,59 @@ int pairs_of_device() {
 
 // The tensor core truncates its fp32 sums, an error that grows with the chain: 1.8e-6 of the loss over 4096 values in one chain.  The
 // sums of shorter ones are added in registers, rounded to nearest.  Gradients in bf16 need none of that.
-constexpr int chain_blocks(int planes, int epilogue) { return planes == 3 ? 8 : epilogue == kProduct ? 1 << 30 : 16; }
+// (Parts of z's sum are no longer than a chain.)
+constexpr int kOneChain = 1 << 30;
+constexpr int chain_blocks(int planes, int epilogue) { return epilogue == kSums || (epilogue == kProduct && planes == 1) ? kOneChain : planes == 3 ? 8 : 16; }
 
 constexpr long kPieceBytesMost = 256L << 20;  // of dz, or of the planes of w
+
+constexpr Shape kShapes[] = {{true, 256}, {true, 192}, {true, 128}, {false, 256}, {false, 192}, {false, 128}};
+bool possible(Shape s, int planes) { return s.pair || planes == 1 || s.bn == 128; }
+long tiles_of(long m, long n, Shape s) { const long rows = s.pair ? 2 * BM : BM; return up(m, rows) / rows * (up(n, s.bn) / s.bn); }
+long workers_of(Shape s, int pairs) { return s.pair ? pairs : 2 * pairs; }
+// What the plan goes by, in microseconds of a worker (measured): a K block of a tile (six products with three planes, and a single CTA loads half
+// as much again as one of a pair), and a tile's epilogue, which hides behind the next tile's products if those take longer: with `stored` it is
+// what a worker has of the memory's rate.
+double tile_time(Shape s, long blocks, int planes, bool stored) {
+  const double products = blocks * (0.27 + 0.0007 * s.bn) * (s.pair ? 1.0 : 1.05) * (planes == 3 ? 6 : 1);
+  const double epilogue = stored ? (s.bn == BN ? 2.2 : 1.3) : 0.005 * s.bn;
+  return products > epilogue ? products : epilogue;
+}
+constexpr double kMeeting = 0.7;  // what a pair's beginning and end take beyond a single CTA's
+// What parts of a sum cost beyond the products: another kernel, and each value written and read.
+double parts_time(double values, int parts) { return parts > 1 ? 2.5 + 8.0 * values * parts / 6e6 : 0; }
+
+// z's tiles and into how many parts its sum is cut: what takes the least time.
+void plan_logits(long m, long n, long blocks, int planes, int pairs, bool parts, Shape* shape, int* splits) {
+  double least = -1;
+  for (const Shape& b : kShapes) {
+    if (!possible(b, planes)) continue;
+    const long tiles = tiles_of(m, n, b), workers = workers_of(b, pairs);
+    for (int s = 1; s == 1 || (parts && s * tiles <= workers && s <= blocks); ++s) {
+      const long per = (blocks + s - 1) / s;
+      if (s > 1 && per > chain_blocks(planes, kStatistics)) continue;
+      const double t = (s * tiles + workers - 1) / workers * tile_time(b, per, planes, s > 1) + parts_time((double)m * n, s) + (b.pair ? kMeeting : 0);
+      if (least < 0 || t < least) { least = t; *shape = b; *splits = (int)((blocks + per - 1) / per); }
+    }
+  }
+}
+// The same for dx [rows][in] over the classes of a piece and dw [classes][in] over the rows, which share a launch.
+void plan_gradients(long rows, long in, long classes, int planes, int pairs, Shape* dx, int* dx_splits, Shape* dw) {
+  const long class_blocks = (classes + BK - 1) / BK, row_blocks = (rows + BK - 1) / BK;
+  double least = -1;
+  for (const Shape& b : kShapes)
+    for (const Shape& c : kShapes) {
+      if (b.pair != c.pair || b.bn == 192 || c.bn == 192 || !possible(b, planes) || !possible(c, planes)) continue;
+      const long workers = workers_of(b, pairs);
+      for (int s = 1; s <= 64 && s <= class_blocks && (s == 1 || s * tiles_of(rows, in, b) <= workers); ++s) {
+        const double x = tile_time(b, (class_blocks + s - 1) / s, planes, true), w = tile_time(c, row_blocks, planes, true);
+        const double all = (s * tiles_of(rows, in, b) * x + tiles_of(classes, in, c) * w) / workers + (x < w ? x : w) / 2;
+        const double longest = x > w ? x : w;
+        const double t = (all > longest ? all : longest) + 0.1 * longest + parts_time((double)rows * in, s) + (b.pair ? kMeeting : 0);  // (the shorter the longest, the evener the end)
+        if (least < 0 || t < least) { least = t; *dx = b; *dx_splits = s; *dw = c; }
+      }
+    }
+}
 
 Plan make_plan(const vgg19_linear_loss& a, bool backward, int pairs) {
   Plan p{};
@@ -677,18 +946,17 @@ Plan make_plan(const vgg19_linear_loss& a, bool backward, int pairs) {
   auto take = [&at](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
   if (p.take_x) p.x = take((size_t)p.planes * a.rows * p.ld * 2);
   if (p.take_w) p.w = take((size_t)p.planes * (p.piece < a.classes ? p.piece : a.classes) * p.ld * 2);
+  const long blocks = (a.in + BK - 1) / BK, piece_classes = p.piece < a.classes ? p.piece : a.classes;
+  plan_logits(a.rows, piece_classes, blocks, p.planes, pairs, p.pieces == 1, &p.z_shape, &p.z_splits);
+  if (p.z_splits > 1) p.z = take((size_t)p.z_splits * a.rows * up(a.classes, 4) * 4);
+  p.db_rows = p.z_splits > 1 ? kPartRows : 32;
   if (!backward) {
-    p.part = take((size_t)p.pieces * (p.piece / 128) * a.rows * sizeof(float2));
+    p.part = take((size_t)p.pieces * up(p.piece, p.z_shape.bn / 2) / (p.z_shape.bn / 2) * a.rows * sizeof(float2));
     p.label_z = take((size_t)a.rows * 4);
   } else {
     p.dz = take((size_t)p.planes * a.rows * p.piece * 2);
-    p.db_part = take((size_t)(up(a.rows, 32) / 32) * p.piece * 4);
-    // dx has rows x in tiles; where they leave pairs idle, its sum is cut into parts
-    const long tiles = (up(a.rows, 2 * BM) / (2 * BM)) * (up(a.in, BN) / BN);
-    const long blocks = (p.piece < a.classes ? p.piece : (long)a.classes + BK - 1) / BK;
-    long want = pairs / tiles;
-    if (want > blocks / 16) want = blocks / 16;  // parts of at least sixteen blocks: each is written, and read again
-    p.dx_splits = (int)(want < 1 ? 1 : want > 64 ? 64 : want);
+    p.db_part = take((size_t)(up(a.rows, p.db_rows) / p.db_rows) * p.piece * 4);
+    plan_gradients(a.rows, a.in, piece_classes, p.planes, pairs, &p.dx_shape, &p.dx_splits, &p.dw_shape);
     p.dx_parts = p.pieces > 1 || p.dx_splits > 1;
     p.dx_ld = up(a.in, 4);
     if (p.dx_parts) p.dx = take((size_t)p.dx_splits * a.rows * p.dx_ld * 4);
@@ -697,38 +965,51 @@ Plan make_plan(const vgg19_linear_loss& a, bool backward, int pairs) {
   return p;
 }
 
+// A launch whose set-up overlaps the one before it in the stream (the kernels wait for that one themselves).
 template <typename... A>
-cudaError_t launch_behind(void (*kernel)(A...), unsigned blocks, int threads, int smem, cudaStream_t st, const A&... args) {
+cudaError_t launch_clusters(void (*kernel)(A...), unsigned cluster, dim3 blocks, int threads, int smem, cudaStream_t st, const A&... args) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(blocks);
+  cfg.gridDim = blocks;
   cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = st;
-  cudaLaunchAttribute at{};
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute at[2] = {};
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
-
-template <int P, int EPI> cudaError_t launch_products(Launch& L, int pairs, cudaStream_t st) {
+template <typename... A>
+cudaError_t launch_behind(void (*kernel)(A...), dim3 blocks, int threads, int smem, cudaStream_t st, const A&... args) {
+  return launch_clusters(kernel, 1, blocks, threads, smem, st, args...);
+}
+template <int P, int EPI, bool PAIR> cudaError_t launch_tiles(const Launch& L, int pairs, cudaStream_t st) {
+  const cudaError_t e = cudaFuncSetAttribute(loss_product_kernel<P, EPI, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  if (e != cudaSuccess) return e;
+  const int tiles = L.first_tile[L.count], workers = PAIR ? pairs : 2 * pairs;
+  return launch_clusters(loss_product_kernel<P, EPI, PAIR>, PAIR ? 2 : 1, dim3((unsigned)((tiles < workers ? tiles : workers) * (PAIR ? 2 : 1))), kThreads, kSmemBytes, st, L);
+}
+template <int P, int EPI> cudaError_t launch_products(Launch& L, bool pair, int pairs, cudaStream_t st) {
   int tiles = 0;
   for (int i = 0; i < L.count; ++i) {
     Job& p = L.job[i];
-    p.tiles_m = (p.m + 2 * BM - 1) / (2 * BM);
-    p.tiles_n = (p.n + BN - 1) / BN;
+    const int rows = pair ? kTileRows<true> : kTileRows<false>;
+    p.tiles_m = (p.m + rows - 1) / rows;
+    p.tiles_n = (p.n + p.bn - 1) / p.bn;
     if (p.splits < 1) p.splits = 1;
+    if (!p.group) p.group = 16;
     p.per_split = (p.k_blocks + p.splits - 1) / p.splits;
-    p.chain = chain_blocks(P, EPI);
     p.splits = (p.k_blocks + p.per_split - 1) / p.per_split;  // none is empty
+    p.chain = chain_blocks(P, EPI);
     L.first_tile[i] = tiles;
     tiles += p.splits * p.tiles_m * p.tiles_n;
   }
   L.first_tile[L.count] = tiles;
-  const cudaError_t e = cudaFuncSetAttribute(loss_product_kernel<P, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-  if (e != cudaSuccess) return e;
-  return launch_behind(loss_product_kernel<P, EPI>, (unsigned)(2 * (tiles < pairs ? tiles : pairs)), kThreads, kSmemBytes, st, L);
+  return pair ? launch_tiles<P, EPI, true>(L, pairs, st) : launch_tiles<P, EPI, false>(L, pairs, st);
 }
 
 // The operands of one call in the form that the products read: x once, w piece by piece.
@@ -763,13 +1044,13 @@ template <int P> struct Operands {
 };
 
 // The products z of one piece.
-template <int P> Launch logits(const Operands<P>& o, long first, long n, const Waits& waits) {
+template <int P> Launch logits(const Operands<P>& o, const Plan& p, long first, long n, const Waits& waits) {
   Launch L{};
   L.waits = waits;
   L.count = 1;
   Job& j = L.job[0];
-  j.a = o.x; j.b = o.w; j.c = o.w;
-  j.m = (int)o.a.rows; j.n = (int)n; j.k_blocks = (o.a.in + BK - 1) / BK;
+  j.a = o.x; j.b = o.w;
+  j.m = (int)o.a.rows; j.n = (int)n; j.k_blocks = (o.a.in + BK - 1) / BK; j.bn = p.z_shape.bn;
   Rows& r = L.rows;
   r.bias = o.a.bias ? o.a.bias + first : nullptr;
   r.labels = o.a.labels;
@@ -777,25 +1058,46 @@ template <int P> Launch logits(const Operands<P>& o, long first, long n, const W
   return L;
 }
 
+// z in parts of its sum.
+template <int P> cudaError_t logits_in_parts(const Operands<P>& o, const Plan& p, int pairs, const Waits& waits, Parts& parts, cudaStream_t st) {
+  Launch L = logits<P>(o, p, 0, o.a.classes, waits);
+  Job& j = L.job[0];
+  j.splits = p.z_splits;
+  j.store = kPadded;
+  j.out = o.ws + p.z; j.ld = up(o.a.classes, 4);
+  parts = Parts{};
+  parts.z = reinterpret_cast<const float*>(o.ws + p.z); parts.ld = j.ld;
+  parts.parts = p.z_splits; parts.rows = (int)o.a.rows; parts.classes = o.a.classes;
+  parts.bias = o.a.bias; parts.labels = o.a.labels;
+  return launch_products<P, kSums>(L, p.z_shape.pair, pairs, st);
+}
+
 template <int P>
 cudaError_t forward(const vgg19_linear_loss& a, float* loss, float* lse, char* ws, const Plan& p, int pairs, const Waits& waits, cudaStream_t st) {
   Operands<P> o{a, p, ws, st, {}, {}};
   cudaError_t e = o.rows();
+  if (p.z_splits > 1) {
+    if (e == cudaSuccess) e = o.weights(0, a.classes);
+    Parts parts;
+    if (e == cudaSuccess) e = logits_in_parts<P>(o, p, pairs, waits, parts, st);
+    parts.loss = loss; parts.lse_out = lse;
+    return e == cudaSuccess ? launch_behind(loss_of_parts_kernel, (unsigned)a.rows, kRowThreads, 0, st, parts) : e;
+  }
   int part = 0;
   for (int i = 0; i < p.pieces && e == cudaSuccess; ++i) {
     const long first = i * p.piece, n = a.classes - first < p.piece ? a.classes - first : p.piece;
     e = o.weights(first, n);
     if (e != cudaSuccess) break;
-    Launch L = logits<P>(o, first, n, waits);
+    Launch L = logits<P>(o, p, first, n, waits);
     L.rows.part = reinterpret_cast<float2*>(ws + p.part);
     L.rows.label_z = reinterpret_cast<float*>(ws + p.label_z);
     L.rows.first_part = part;
-    part += (int)((n + 127) / 128);
-    e = launch_products<P, kStatistics>(L, pairs, st);
+    part += (int)((n + p.z_shape.bn / 2 - 1) / (p.z_shape.bn / 2));
+    e = launch_products<P, kStatistics>(L, p.z_shape.pair, pairs, st);
   }
   if (e != cudaSuccess) return e;
   const Join j{reinterpret_cast<const float2*>(ws + p.part), reinterpret_cast<const float*>(ws + p.label_z), a.labels, loss, lse, part, (int)a.rows, a.classes};
-  return launch_behind(join_rows_kernel, (unsigned)((a.rows + 31) / 32), 32 * kJoinGroups, 0, st, j);
+  return launch_behind(join_rows_kernel, (unsigned)((a.rows + kJoinRows - 1) / kJoinRows), kJoinRows * kJoinGroups, 0, st, j);
 }
 
 struct Gradients {
@@ -820,58 +1122,62 @@ cudaError_t backward(const vgg19_linear_loss& a, const Gradients& g, char* ws, c
     e = o.weights(first, n);
     if (e != cudaSuccess) break;
     const long dz_ld = up(n, 8);
-    CUtensorMap dz, dz_out;
-    if (!planes_map(&dz, ws + p.dz, false, P, a.rows, n, dz_ld, 64) || !planes_map(&dz_out, ws + p.dz, false, P, a.rows, n, dz_ld, 32))
-      return cudaErrorInvalidValue;
-    Launch L = logits<P>(o, first, n, waits);
-    L.job[0].c = dz_out;
-    L.rows.lse = g.lse; L.rows.d_loss = g.d_loss;
-    L.rows.db_part = g.db ? db_part : nullptr;
-    e = launch_products<P, kLogitGradient>(L, pairs, st);
+    CUtensorMap dz;
+    if (!planes_map(&dz, ws + p.dz, false, P, a.rows, n, dz_ld, 64)) return cudaErrorInvalidValue;
+    if (p.z_splits > 1) {
+      Parts parts;
+      e = logits_in_parts<P>(o, p, pairs, waits, parts, st);
+      if (e != cudaSuccess) break;
+      parts.lse = g.lse; parts.d_loss = g.d_loss;
+      parts.dz = reinterpret_cast<bf16*>(ws + p.dz); parts.dz_ld = dz_ld;
+      parts.db_part = g.db ? db_part : nullptr;
+      e = launch_behind(gradient_of_parts_kernel<P>, dim3((unsigned)((n + 127) / 128), (unsigned)((a.rows + kPartRows - 1) / kPartRows)), 32 * kPartRows, 0, st, parts);
+    } else {
+      Launch L = logits<P>(o, p, first, n, waits);
+      L.job[0].out = ws + p.dz; L.job[0].ld = dz_ld;
+      L.rows.lse = g.lse; L.rows.d_loss = g.d_loss;
+      L.rows.db_part = g.db ? db_part : nullptr;
+      e = launch_products<P, kLogitGradient>(L, p.z_shape.pair, pairs, st);
+    }
     if (e != cudaSuccess) break;
 
     Launch M{};
     M.waits = waits;
     const bool f32 = P == 3;
-    if (g.dw) {  // dw of the piece: [n][in] = dz^T x
-      Job& j = M.job[M.count++];
-      const bool out32 = f32 || g.dw_f32;
-      const long elt = out32 ? 4 : 2;
-      j.a = dz; j.a_mn = 1; j.b = o.x; j.b_mn = 1;
-      j.m = (int)n; j.n = a.in; j.k_blocks = (int)((a.rows + BK - 1) / BK);
-      j.f32 = out32;
-      j.out = static_cast<char*>(g.dw) + first * g.dw_ld * elt; j.ld = g.dw_ld;
-      j.store = writable(j.out, n, a.in, g.dw_ld, elt) ? kCopied : kByThreads;
-      j.c = j.a;
-      if (j.store == kCopied && !planes_map(&j.c, j.out, out32, 1, n, a.in, n == 1 ? up(a.in, 8) : g.dw_ld, 32)) return cudaErrorInvalidValue;
-      j.db_part = db_part; j.db = g.db ? g.db + first : nullptr;
-      j.parts = (int)((a.rows + 31) / 32);
-    }
-    if (g.dx) {  // dx, or the piece's share of it: [rows][in] = dz w
+    if (g.dx) {  // dx, or the piece's share of it: [rows][in] = dz w.  Its tiles, over all classes, take longer than dw's: they come first
       Job& j = M.job[M.count++];
       j.a = dz; j.b = o.w; j.b_mn = 1;
-      j.m = (int)a.rows; j.n = a.in; j.k_blocks = (int)((n + BK - 1) / BK);
-      j.c = j.a;
+      j.m = (int)a.rows; j.n = a.in; j.k_blocks = (int)((n + BK - 1) / BK); j.bn = p.dx_shape.bn;
       if (p.dx_parts) {
         j.f32 = 1;
+        j.out = dx_part; j.ld = p.dx_ld;
         j.splits = slots && slots < p.dx_splits ? slots : p.dx_splits;  // later pieces add to the parts that the first one wrote
-        j.store = i ? kAdded : kCopied;
-        if (!planes_map(&j.c, dx_part, true, p.dx_splits, a.rows, a.in, p.dx_ld, 32)) return cudaErrorInvalidValue;
+        j.store = i ? kAdded : kWhole;  // (rows have room for whole fours)
         if (!i) {
           const int per = (j.k_blocks + j.splits - 1) / j.splits;
           slots = (j.k_blocks + per - 1) / per;
         }
       } else {
-        const long elt = f32 ? 4 : 2;
         j.f32 = f32;
         j.out = g.dx; j.ld = g.dx_ld;
-        j.store = writable(g.dx, a.rows, a.in, g.dx_ld, elt) ? kCopied : kByThreads;
-        if (j.store == kCopied && !planes_map(&j.c, g.dx, f32, 1, a.rows, a.in, a.rows == 1 ? up(a.in, 8) : g.dx_ld, 32)) return cudaErrorInvalidValue;
+        j.store = copyable(g.dx, a.rows, g.dx_ld, f32 ? 4 : 2) ? kWhole : kSingle;
       }
     }
-    if (M.count) e = launch_products<P, kProduct>(M, pairs, st);
+    if (g.dw) {  // dw of the piece: [n][in] = dz^T x
+      Job& j = M.job[M.count++];
+      j.a = dz; j.a_mn = 1; j.b = o.x; j.b_mn = 1;
+      j.group = 4;  // whole rows of dw at a time (sixteen: 2 % slower)
+      j.m = (int)n; j.n = a.in; j.k_blocks = (int)((a.rows + BK - 1) / BK); j.bn = p.dw_shape.bn;
+      j.f32 = f32 || g.dw_f32;
+      const long elt = j.f32 ? 4 : 2;
+      j.out = static_cast<char*>(g.dw) + first * g.dw_ld * elt; j.ld = g.dw_ld;
+      j.store = copyable(j.out, n, g.dw_ld, elt) ? kWhole : kSingle;
+      j.db_part = db_part; j.db = g.db ? g.db + first : nullptr;
+      j.parts = (int)((a.rows + p.db_rows - 1) / p.db_rows);
+    }
+    if (M.count) e = launch_products<P, kProduct>(M, p.dx_shape.pair, pairs, st);
     if (!g.dw && g.db && e == cudaSuccess)
-      e = launch_behind(sum_columns_kernel, (unsigned)((n + 255) / 256), 256, 0, st, static_cast<const float*>(db_part), (int)((a.rows + 31) / 32), (int)n, g.db + first);
+      e = launch_behind(sum_columns_kernel, (unsigned)((n + 255) / 256), 256, 0, st, static_cast<const float*>(db_part), (int)((a.rows + p.db_rows - 1) / p.db_rows), (int)n, g.db + first);
   }
   if (e != cudaSuccess || !g.dx || !p.dx_parts) return e;
   const long chunks = a.rows * (p.dx_ld / 4);
