@@ -115,6 +115,9 @@ struct Launch {
 struct Tile {
   int i, j, split, k0, k1;
 };
+// A worker's tile of a round: every other round from the other end, so that who has a long one in the first has none in a last round that is
+// not full.
+__device__ __forceinline__ int turn(int round, int worker, int workers) { return round * workers + (round & 1 ? workers - 1 - worker : worker); }
 // A few rows of tiles at a time, which share their columns' operand: both operands then stay in L2 while they are needed.
 __device__ __forceinline__ Tile find_tile(const Job& p, int t) {
   Tile r{};
@@ -247,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
       int stage = 0, ji = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int w = worker; w < total && ok; w += workers) {
+      for (int round = 0, w; ok && (w = turn(round, worker, workers)) < total; ++round) {
         while (w >= L.first_tile[ji + 1]) ++ji;
         const Job& p = L.job[ji];
         const Tile tile = find_tile(p, w - L.first_tile[ji]);
@@ -293,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
       int stage = 0, ji = 0;
       uint32_t phase = 0, count = 0;
       bool ok = true;
-      for (int w = worker; w < total && ok; w += workers) {
+      for (int round = 0, w; ok && (w = turn(round, worker, workers)) < total; ++round) {
         while (w >= L.first_tile[ji + 1]) ++ji;
         const Job& p = L.job[ji];
         const Tile tile = find_tile(p, w - L.first_tile[ji]);
@@ -356,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
     int ji = 0;
     uint32_t count = 0;
     bool ok = true;
-    for (int w = worker; w < total && ok; w += workers) {
+    for (int round = 0, w; ok && (w = turn(round, worker, workers)) < total; ++round) {
       while (w >= L.first_tile[ji + 1]) ++ji;
       const Job& p = L.job[ji];
       const Tile tile = find_tile(p, w - L.first_tile[ji]);
@@ -386,10 +389,14 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
         next_bias = bias_of(lane);
       }
       if (EPI == kProduct && p.db && tile.j == 0 && group == 0 && tile.split == 0 && lane < rows) {
-        float s = 0.f;
-#pragma unroll 8
-        for (int q = 0; q < p.parts; ++q) s += p.db_part[(long)q * p.m + row];
-        p.db[row] = s;
+        float s[8] = {};  // (as sum_columns_kernel adds them)
+        for (int q = 0; q < p.parts; q += 8) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s[k] += q + k < p.parts ? p.db_part[(long)(q + k) * p.m + row] : 0.f;
+        }
+#pragma unroll
+        for (int k = 1; k < 8; ++k) s[0] += s[k];
+        p.db[row] = s[0];
       }
       // The piece, `from` on of the half's columns, to memory: lanes along the rows, four whole 128-byte lines at a time.
       const int elt = EPI == kSums || (EPI == kProduct && p.f32) ? 4 : 2;
@@ -426,7 +433,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
       };
       auto sums_at = [&] { return tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((count % BUFFERS) * BN + group * half); };
 
-      if (!CHAINED) {
+      if constexpr (!CHAINED) {
         // one chain, and nothing to compute: 128 bytes of a row at a time, in little code (a call of few tiles runs it once, from memory)
         if (!sums_are_there()) { ok = false; break; }
         tc_fence_after();
@@ -469,127 +476,126 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
           }
         }
         sums_are_read();
-        continue;
-      }
-
-      float v[128];  // the tile's sums of this row and half
-      for (long kb0 = tile.k0; kb0 < tile.k1; kb0 += p.chain) {
-        if (!sums_are_there()) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t src = sums_at();
-        if (kb0 == tile.k0) {
-          uint32_t t[4][32];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld_32x32(src + 32 * c, t[c]);  // (of a narrow tile the second two mean nothing)
-          tmem_ld_wait();
-#pragma unroll
-          for (int j = 0; j < 128; ++j) v[j] = __uint_as_float(t[j / 32][j % 32]);
-        }
-        if (P == 3 || kb0 != tile.k0) {
-          for (int plane = kb0 == tile.k0; plane < (P == 3 ? 2 : 1); ++plane) {
-#pragma unroll
-            for (int c = 0; c < 128; c += 32) {
-              uint32_t t[32];
-              tmem_ld_32x32(src + plane * BN + c, t);
-              tmem_ld_wait();
-#pragma unroll
-              for (int j = 0; j < 32; ++j) v[c + j] += __uint_as_float(t[j]);
-            }
-          }
-        }
-        sums_are_read();
-      }
-      if (!ok) break;
-      auto add_bias = [&](int c) {
-        bias_s[lane] = next_bias;
-        __syncwarp();
-        if (c + 32 < 128) next_bias = bias_of(c + 32 + lane);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          const float4 b = reinterpret_cast<const float4*>(bias_s)[q];
-          v[c + 4 * q] += b.x; v[c + 4 * q + 1] += b.y; v[c + 4 * q + 2] += b.z; v[c + 4 * q + 3] += b.w;
-        }
-        __syncwarp();
-      };
-
-      if (EPI == kStatistics) {
-        float most = -INFINITY, sum = 0.f;
-#pragma unroll
-        for (int c = 0; c < 128; c += 32) {
-          if (c >= half) break;
-          add_bias(c);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) most = fmaxf(most, v[c + j]);
-          const int at = label - j0 - c;  // the label's column among these
-          if (__any_sync(0xffffffffu, (unsigned)at < 32u)) {
-            float z = 0.f;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) z = at == j ? v[c + j] : z;
-            if ((unsigned)at < 32u && at < cols - c) L.rows.label_z[row] = z;
-          }
-        }
-        const float ref = most == -INFINITY ? 0.f : most;
-#pragma unroll
-        for (int c = 0; c < 128; c += 32) {
-          if (c >= half) break;
-          float part = 0.f;
-#pragma unroll
-          for (int j = 0; j < 32; ++j) part += fast_exp2((v[c + j] - ref) * kLog2e);
-          sum += part;
-        }
-        if (lane < rows && cols > 0) L.rows.part[(long)(L.rows.first_part + 2 * tile.j + group) * p.m + row] = make_float2(most, sum);
-      } else if (EPI == kLogitGradient) {
-        const float ref = lse == -INFINITY ? 0.f : lse;
-#pragma unroll
-        for (int c0 = 0; c0 < 128; c0 += 64) {
-          if (c0 >= half) break;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int c = c0 + 32 * h;
-            add_bias(c);
-            const int at = label - j0 - c;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[c + j] = fast_exp2((v[c + j] - ref) * kLog2e);
-            if (__any_sync(0xffffffffu, (unsigned)at < 32u)) {
-#pragma unroll
-              for (int j = 0; j < 32; ++j) v[c + j] = at == j ? v[c + j] - 1.f : v[c + j];
-            }
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[c + j] = d_loss == 0.f ? 0.f : d_loss * v[c + j];  // (a row that counts for nothing may hold anything)
-            if (L.rows.db_part) {
-              float t[32];
-#pragma unroll
-              for (int j = 0; j < 32; ++j) t[j] = v[c + j];
-              const float s = column_sums(t, lane);
-              if (c + lane < cols && rows > 0) L.rows.db_part[(long)(i0 / 32) * p.n + j0 + c + lane] = s;
-            }
-          }
-#pragma unroll
-          for (int h = 0; h < P; ++h) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const int e = c0 + 8 * k;
-              uint4 w;
-              if (P == 1) {
-                w = make_uint4(pack2(v[e], v[e + 1]), pack2(v[e + 2], v[e + 3]), pack2(v[e + 4], v[e + 5]), pack2(v[e + 6], v[e + 7]));
-              } else {
-                w.x = take2(v[e], v[e + 1]); w.y = take2(v[e + 2], v[e + 3]);
-                w.z = take2(v[e + 4], v[e + 5]); w.w = take2(v[e + 6], v[e + 7]);
-              }
-              piece[piece_at(lane, k)] = w;
-            }
-            put_piece(c0, h);
-          }
-        }
       } else {
+        float v[128];  // the tile's sums of this row and half
+        for (long kb0 = tile.k0; kb0 < tile.k1; kb0 += p.chain) {
+          if (!sums_are_there()) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t src = sums_at();
+          if (kb0 == tile.k0) {
+            uint32_t t[4][32];
 #pragma unroll
-        for (int c0 = 0; c0 < 128; c0 += 32) {  // (three planes: fp32)
-          if (c0 >= cols) break;
+            for (int c = 0; c < 4; ++c) tmem_ld_32x32(src + 32 * c, t[c]);  // (of a narrow tile the second two mean nothing)
+            tmem_ld_wait();
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-            piece[piece_at(lane, k)] = make_uint4(__float_as_uint(v[c0 + 4 * k]), __float_as_uint(v[c0 + 4 * k + 1]), __float_as_uint(v[c0 + 4 * k + 2]),
-                                                  __float_as_uint(v[c0 + 4 * k + 3]));
-          put_piece(c0, 0);
+            for (int j = 0; j < 128; ++j) v[j] = __uint_as_float(t[j / 32][j % 32]);
+          }
+          if (P == 3 || kb0 != tile.k0) {
+            for (int plane = kb0 == tile.k0; plane < (P == 3 ? 2 : 1); ++plane) {
+#pragma unroll
+              for (int c = 0; c < 128; c += 32) {
+                uint32_t t[32];
+                tmem_ld_32x32(src + plane * BN + c, t);
+                tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[c + j] += __uint_as_float(t[j]);
+              }
+            }
+          }
+          sums_are_read();
+        }
+        if (!ok) break;
+        auto add_bias = [&](int c) {
+          bias_s[lane] = next_bias;
+          __syncwarp();
+          if (c + 32 < 128) next_bias = bias_of(c + 32 + lane);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const float4 b = reinterpret_cast<const float4*>(bias_s)[q];
+            v[c + 4 * q] += b.x; v[c + 4 * q + 1] += b.y; v[c + 4 * q + 2] += b.z; v[c + 4 * q + 3] += b.w;
+          }
+          __syncwarp();
+        };
+
+        if (EPI == kStatistics) {
+          float most = -INFINITY, sum = 0.f;
+#pragma unroll
+          for (int c = 0; c < 128; c += 32) {
+            if (c >= half) break;
+            add_bias(c);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) most = fmaxf(most, v[c + j]);
+            const int at = label - j0 - c;  // the label's column among these
+            if (__any_sync(0xffffffffu, (unsigned)at < 32u)) {
+              float z = 0.f;
+#pragma unroll
+              for (int j = 0; j < 32; ++j) z = at == j ? v[c + j] : z;
+              if ((unsigned)at < 32u && at < cols - c) L.rows.label_z[row] = z;
+            }
+          }
+          const float ref = most == -INFINITY ? 0.f : most;
+#pragma unroll
+          for (int c = 0; c < 128; c += 32) {
+            if (c >= half) break;
+            float part = 0.f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) part += fast_exp2((v[c + j] - ref) * kLog2e);
+            sum += part;
+          }
+          if (lane < rows && cols > 0) L.rows.part[(long)(L.rows.first_part + 2 * tile.j + group) * p.m + row] = make_float2(most, sum);
+        } else if (EPI == kLogitGradient) {
+          const float ref = lse == -INFINITY ? 0.f : lse;
+#pragma unroll
+          for (int c0 = 0; c0 < 128; c0 += 64) {
+            if (c0 >= half) break;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int c = c0 + 32 * h;
+              add_bias(c);
+              const int at = label - j0 - c;
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[c + j] = fast_exp2((v[c + j] - ref) * kLog2e);
+              if (__any_sync(0xffffffffu, (unsigned)at < 32u)) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[c + j] = at == j ? v[c + j] - 1.f : v[c + j];
+              }
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[c + j] = d_loss == 0.f ? 0.f : d_loss * v[c + j];  // (a row that counts for nothing may hold anything)
+              if (L.rows.db_part) {
+                float t[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) t[j] = v[c + j];
+                const float s = column_sums(t, lane);
+                if (c + lane < cols && rows > 0) L.rows.db_part[(long)(i0 / 32) * p.n + j0 + c + lane] = s;
+              }
+            }
+#pragma unroll
+            for (int h = 0; h < P; ++h) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const int e = c0 + 8 * k;
+                uint4 w;
+                if (P == 1) {
+                  w = make_uint4(pack2(v[e], v[e + 1]), pack2(v[e + 2], v[e + 3]), pack2(v[e + 4], v[e + 5]), pack2(v[e + 6], v[e + 7]));
+                } else {
+                  w.x = take2(v[e], v[e + 1]); w.y = take2(v[e + 2], v[e + 3]);
+                  w.z = take2(v[e + 4], v[e + 5]); w.w = take2(v[e + 6], v[e + 7]);
+                }
+                piece[piece_at(lane, k)] = w;
+              }
+              put_piece(c0, h);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int c0 = 0; c0 < 128; c0 += 32) {  // (three planes: fp32)
+            if (c0 >= cols) break;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              piece[piece_at(lane, k)] = make_uint4(__float_as_uint(v[c0 + 4 * k]), __float_as_uint(v[c0 + 4 * k + 1]), __float_as_uint(v[c0 + 4 * k + 2]),
+                                                    __float_as_uint(v[c0 + 4 * k + 3]));
+            put_piece(c0, 0);
+          }
         }
       }
     }
@@ -679,10 +685,12 @@ struct Parts {
 __device__ __forceinline__ float4 sum_of_parts(const Parts& a, int row, int c) {
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   const float* at = a.z + (long)row * a.ld + c;
-#pragma unroll 8
-  for (int p = 0; p < a.parts; ++p, at += a.rows * a.ld) {
-    const float4 v = __ldcg(reinterpret_cast<const float4*>(at));
-    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  for (int p = 0; p < a.parts; p += 8) {  // eight requests at once, the last ones too
+    float4 v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k, at += a.rows * a.ld) v[k] = p + k < a.parts ? __ldcg(reinterpret_cast<const float4*>(at)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { s.x += v[k].x; s.y += v[k].y; s.z += v[k].z; s.w += v[k].w; }
   }
   const float none = -INFINITY;  // beyond the classes
   auto bias = [&](int k) { return c + k < a.classes ? a.bias ? __ldg(a.bias + c + k) : 0.f : none; };
@@ -763,24 +771,34 @@ template <int P> __global__ void __launch_bounds__(32 * kPartRows) gradient_of_p
 }
 
 // ---- rows as planes of bf16 ------------------------------------------------------------------------------------------
-// dst[h][r][k], row stride ld (a multiple of 8): the value itself, or an fp32 value's three terms.
+// dst[h][r][k], row stride ld (a multiple of 8): the value itself, or an fp32 value's three terms.  Two matrices of as many columns at once.
+struct Layout {
+  const void* src[2];
+  bf16* dst[2];
+  long src_ld[2], rows[2];  // (no rows: nothing)
+  int in;
+  long ld;
+};
 template <typename T, int P>
-__global__ void __launch_bounds__(256) planes_kernel(const T* __restrict__ src, long src_ld, bf16* dst, long rows, int in, long ld) {
+__global__ void __launch_bounds__(256) planes_kernel(const __grid_constant__ Layout a) {
   behind_previous();
-  const int chunks = (int)(ld / 8);
-  const long all = rows * chunks;
+  const int chunks = (int)(a.ld / 8);
+  const long all = (a.rows[0] + a.rows[1]) * chunks;
   for (long t = (long)blockIdx.x * blockDim.x + threadIdx.x; t < all; t += (long)gridDim.x * blockDim.x) {
-    const long r = t / chunks;
-    const int k = (int)(t - r * chunks) * 8;
-    const T* at = src + r * src_ld + k;
+    const long row = (unsigned long)t < 0x100000000ul ? (unsigned)t / (unsigned)chunks : t / chunks;
+    const int k = (int)(t - row * chunks) * 8;
+    const bool second = row >= a.rows[0];
+    const long r = second ? row - a.rows[0] : row, rows = second ? a.rows[1] : a.rows[0];
+    const T* at = static_cast<const T*>(second ? a.src[1] : a.src[0]) + r * (second ? a.src_ld[1] : a.src_ld[0]) + k;
+    bf16* dst = second ? a.dst[1] : a.dst[0];
     float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = k + e < in ? to_f32(at[e]) : 0.f;
+    for (int e = 0; e < 8; ++e) v[e] = k + e < a.in ? to_f32(at[e]) : 0.f;
 #pragma unroll
     for (int h = 0; h < P; ++h) {
       uint4 q;
       q.x = take2(v[0], v[1]); q.y = take2(v[2], v[3]); q.z = take2(v[4], v[5]); q.w = take2(v[6], v[7]);
-      *reinterpret_cast<uint4*>(dst + (h * rows + r) * ld + k) = q;
+      *reinterpret_cast<uint4*>(dst + (h * rows + r) * a.ld + k) = q;
     }
   }
 }
@@ -809,12 +827,19 @@ __global__ void __launch_bounds__(256) sum_parts_kernel(const float* __restrict_
 
 // db of a piece where no product of dw does it on the way
 __global__ void __launch_bounds__(256) sum_columns_kernel(const float* part, int parts, int n, float* db) {
+  __shared__ float got[8][32];
   behind_previous();
-  const int c = blockIdx.x * blockDim.x + threadIdx.x;
-  if (c >= n) return;
+  const int lane = threadIdx.x % 32, group = threadIdx.x / 32, c = blockIdx.x * 32 + lane;
   float s = 0.f;
+  if (c < n) {
 #pragma unroll 8
-  for (int q = 0; q < parts; ++q) s += part[(long)q * n + c];
+    for (int q = group; q < parts; q += 8) s += part[(long)q * n + c];
+  }
+  got[group][lane] = s;
+  __syncthreads();
+  if (group || c >= n) return;
+#pragma unroll
+  for (int g = 1; g < 8; ++g) s += got[g][lane];
   db[c] = s;
 }
 
@@ -1020,26 +1045,29 @@ template <int P> struct Operands {
   cudaStream_t st;
   CUtensorMap x, w;
 
-  cudaError_t lay_out(const void* src, long src_ld, long rows, size_t at) {
-    bf16* dst = reinterpret_cast<bf16*>(ws + at);
-    const long chunks = rows * (p.ld / 8);
-    const unsigned blocks = (unsigned)(chunks / 256 + 1 < 148 * 16 ? chunks / 256 + 1 : 148 * 16);
-    if (P == 3) return launch_behind(planes_kernel<float, 3>, blocks, 256, 0, st, static_cast<const float*>(src), src_ld, dst, rows, (int)a.in, p.ld);
-    return launch_behind(planes_kernel<bf16, 1>, blocks, 256, 0, st, static_cast<const bf16*>(src), src_ld, dst, rows, (int)a.in, p.ld);
-  }
-  cudaError_t rows() {
-    if (!p.take_x) return planes_map(&x, a.x, false, 1, a.rows, a.in, a.rows == 1 ? p.ld : a.ldx, 64) ? cudaSuccess : cudaErrorInvalidValue;
-    const cudaError_t e = lay_out(a.x, a.ldx, a.rows, p.x);
-    if (e != cudaSuccess) return e;
-    return planes_map(&x, ws + p.x, false, P, a.rows, a.in, p.ld, 64) ? cudaSuccess : cudaErrorInvalidValue;
-  }
-  cudaError_t weights(long first, long n) {
+  // The maps of x (with the first piece) and of the piece of w; what copies cannot read where it lies is laid out first.
+  cudaError_t prepare(long first, long n) {
     const long elt = P == 3 ? 4 : 2;
     const char* src = static_cast<const char*>(a.w) + first * a.ldw * elt;
-    if (!p.take_w) return planes_map(&w, src, false, 1, n, a.in, a.classes == 1 ? p.ld : a.ldw, 64) ? cudaSuccess : cudaErrorInvalidValue;
-    const cudaError_t e = lay_out(src, a.ldw, n, p.w);
-    if (e != cudaSuccess) return e;
-    return planes_map(&w, ws + p.w, false, P, n, a.in, p.ld, 64) ? cudaSuccess : cudaErrorInvalidValue;
+    Layout l{};
+    l.in = a.in; l.ld = p.ld;
+    if (p.take_x && first == 0) {
+      l.src[0] = a.x; l.src_ld[0] = a.ldx; l.rows[0] = a.rows;
+      l.dst[0] = reinterpret_cast<bf16*>(ws + p.x);
+    }
+    if (p.take_w) {
+      l.src[1] = src; l.src_ld[1] = a.ldw; l.rows[1] = n;
+      l.dst[1] = reinterpret_cast<bf16*>(ws + p.w);
+    }
+    const long chunks = (l.rows[0] + l.rows[1]) * (p.ld / 8);
+    if (chunks) {
+      const unsigned blocks = (unsigned)(chunks / 256 + 1 < 148 * 16 ? chunks / 256 + 1 : 148 * 16);
+      const cudaError_t e = P == 3 ? launch_behind(planes_kernel<float, 3>, blocks, 256, 0, st, l) : launch_behind(planes_kernel<bf16, 1>, blocks, 256, 0, st, l);
+      if (e != cudaSuccess) return e;
+    }
+    const bool maps = (first > 0 || (p.take_x ? planes_map(&x, ws + p.x, false, P, a.rows, a.in, p.ld, 64) : planes_map(&x, a.x, false, 1, a.rows, a.in, a.rows == 1 ? p.ld : a.ldx, 64))) &&
+                      (p.take_w ? planes_map(&w, ws + p.w, false, P, n, a.in, p.ld, 64) : planes_map(&w, src, false, 1, n, a.in, a.classes == 1 ? p.ld : a.ldw, 64));
+    return maps ? cudaSuccess : cudaErrorInvalidValue;
   }
 };
 
@@ -1075,9 +1103,9 @@ template <int P> cudaError_t logits_in_parts(const Operands<P>& o, const Plan& p
 template <int P>
 cudaError_t forward(const vgg19_linear_loss& a, float* loss, float* lse, char* ws, const Plan& p, int pairs, const Waits& waits, cudaStream_t st) {
   Operands<P> o{a, p, ws, st, {}, {}};
-  cudaError_t e = o.rows();
+  cudaError_t e = cudaSuccess;
   if (p.z_splits > 1) {
-    if (e == cudaSuccess) e = o.weights(0, a.classes);
+    e = o.prepare(0, a.classes);
     Parts parts;
     if (e == cudaSuccess) e = logits_in_parts<P>(o, p, pairs, waits, parts, st);
     parts.loss = loss; parts.lse_out = lse;
@@ -1086,7 +1114,7 @@ cudaError_t forward(const vgg19_linear_loss& a, float* loss, float* lse, char* w
   int part = 0;
   for (int i = 0; i < p.pieces && e == cudaSuccess; ++i) {
     const long first = i * p.piece, n = a.classes - first < p.piece ? a.classes - first : p.piece;
-    e = o.weights(first, n);
+    e = o.prepare(first, n);
     if (e != cudaSuccess) break;
     Launch L = logits<P>(o, p, first, n, waits);
     L.rows.part = reinterpret_cast<float2*>(ws + p.part);
@@ -1113,13 +1141,13 @@ struct Gradients {
 template <int P>
 cudaError_t backward(const vgg19_linear_loss& a, const Gradients& g, char* ws, const Plan& p, int pairs, const Waits& waits, cudaStream_t st) {
   Operands<P> o{a, p, ws, st, {}, {}};
-  cudaError_t e = o.rows();
+  cudaError_t e = cudaSuccess;
   float* dx_part = reinterpret_cast<float*>(ws + p.dx);
   float* db_part = reinterpret_cast<float*>(ws + p.db_part);
   int slots = 0;
   for (int i = 0; i < p.pieces && e == cudaSuccess; ++i) {
     const long first = i * p.piece, n = a.classes - first < p.piece ? a.classes - first : p.piece;
-    e = o.weights(first, n);
+    e = o.prepare(first, n);
     if (e != cudaSuccess) break;
     const long dz_ld = up(n, 8);
     CUtensorMap dz;
@@ -1177,7 +1205,7 @@ cudaError_t backward(const vgg19_linear_loss& a, const Gradients& g, char* ws, c
     }
     if (M.count) e = launch_products<P, kProduct>(M, p.dx_shape.pair, pairs, st);
     if (!g.dw && g.db && e == cudaSuccess)
-      e = launch_behind(sum_columns_kernel, (unsigned)((n + 255) / 256), 256, 0, st, static_cast<const float*>(db_part), (int)((a.rows + p.db_rows - 1) / p.db_rows), (int)n, g.db + first);
+      e = launch_behind(sum_columns_kernel, (unsigned)((n + 31) / 32), 256, 0, st, static_cast<const float*>(db_part), (int)((a.rows + p.db_rows - 1) / p.db_rows), (int)n, g.db + first);
   }
   if (e != cudaSuccess || !g.dx || !p.dx_parts) return e;
   const long chunks = a.rows * (p.dx_ld / 4);
