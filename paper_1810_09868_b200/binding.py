@@ -581,9 +581,6 @@ def vgg19_muon_step(net, grads, momentum_buffer, lr, momentum, decay, bias_lr, s
 
 
 def _any_dropout(name, x, y, rate, seed, step, step_counter, first, stream):
-    rc = getattr(_tensor_calls or _calls(), name)(x, y, rate, seed, step, step_counter, first, stream)
-    if rc is not None:
-        return _answered(rc)
     source, result = ("dy", "dx") if name.endswith("backward") else ("x", "y")
     dtype, rows, cols, ldx, dev = _rows_of(x, source)
     y_dtype, y_rows, y_cols, ldy, y_dev = _rows_of(y, result)
@@ -601,12 +598,14 @@ def _any_dropout(name, x, y, rate, seed, step, step_counter, first, stream):
 def vgg19_dropout(x, y, rate, seed, step=0, step_counter=None, first=0, stream=None):
     """y = x with values dropped at `rate` and the others scaled up; [rows][cols], row strides are allowed, y may be x.
     step_counter: an int64 CUDA tensor of one element, added to step on the device."""
-    return _any_dropout("dropout", x, y, rate, seed, step, step_counter, first, stream)
+    rc = (_tensor_calls or _calls()).dropout(x, y, rate, seed, step, step_counter, first, stream)
+    return _answered(rc) if rc is not None else _any_dropout("dropout", x, y, rate, seed, step, step_counter, first, stream)
 
 
 def vgg19_dropout_backward(dy, dx, rate, seed, step=0, step_counter=None, first=0, stream=None):
     """dx from dy, with what vgg19_dropout was given for the mask; dx may be dy."""
-    return _any_dropout("dropout_backward", dy, dx, rate, seed, step, step_counter, first, stream)
+    rc = (_tensor_calls or _calls()).dropout_backward(dy, dx, rate, seed, step, step_counter, first, stream)
+    return _answered(rc) if rc is not None else _any_dropout("dropout_backward", dy, dx, rate, seed, step, step_counter, first, stream)
 
 
 def _linear_loss(x, w, bias, labels):

@@ -84,8 +84,9 @@ cudaError_t q4_take_error(int* code, cudaStream_t st);
 cudaError_t muon_take_error(int* code, cudaStream_t st);
 cudaError_t loss_take_error(int* code, int* label, cudaStream_t st);
 
-// vgg19_linear_cross_entropy with the waits of its kernels (linear_loss.cu).
-int linear_loss(const vgg19_linear_loss* layer, float* loss, float* lse, void* workspace, size_t bytes, const Waits& waits, void* stream);
+// vgg19_linear_cross_entropy with the waits of its kernels (linear_loss.cu); in_pairs: whether they work in pairs of CTAs, or null for what
+// is faster.
+int linear_loss(const vgg19_linear_loss* layer, float* loss, float* lse, void* workspace, size_t bytes, const Waits& waits, const bool* in_pairs, void* stream);
 
 // vgg19_dropout (and, with dy for x, its gradient) without the checks (dropout.cu).
 cudaError_t dropout(const void* x, bool half, long rows, long cols, long ldx, float rate, unsigned long long seed, unsigned long long step,

@@ -118,18 +118,18 @@ __global__ void __launch_bounds__(kThreads) dropout_vector_kernel(const __grid_c
 }
 
 // Any rows, strides and beginnings: a warp takes 256 values, 32 blocks of the generator, one a lane, and its accesses run
-// along the rows.  I: a type that counts all values.
+// along the rows.  I: a type that counts all that the rows span.
 template <typename T, typename I>
 __global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant__ Args a, long groups) {
   const unsigned long long step = step_of(a);
   const int lane = threadIdx.x & 31;
   const long warps = (long)gridDim.x * (kThreads / 32);
   const int lead = (int)(a.first % 256);
-  const I cols = (I)a.cols, count = (I)a.count;
+  const I cols = (I)a.cols, count = (I)a.count, ldx = (I)a.ldx, ldy = (I)a.ldy;
   for (long g = (long)blockIdx.x * (kThreads / 32) + threadIdx.x / 32; g < groups; g += warps) {
     const I e0 = (I)(g * 256 - lead + lane);  // the lane's first value; before 0 and from count on there is none
     T v[8];
-    long ay[8];
+    I ay[8];
     I r = 0, c = e0;  // (of a value before 0: it will be in the first row, or be divided anew)
     if (e0 >= cols) {
       r = e0 / cols;
@@ -140,8 +140,8 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant
       const I e = e0 + 32 * i;
       ay[i] = -1;
       if (e >= 0 && e < count) {
-        v[i] = static_cast<const T*>(a.x)[r * a.ldx + c];
-        ay[i] = r * a.ldy + c;
+        v[i] = static_cast<const T*>(a.x)[r * ldx + c];
+        ay[i] = r * ldy + c;
       }
       c += 32;
       if (c >= cols) {
@@ -180,7 +180,7 @@ template <typename T> cudaError_t launch(const Args& a, cudaStream_t st) {
   } else {
     const long groups = (a.count + (long)(a.first % 256) + 255) / 256, blocks = (groups + kThreads / 32 - 1) / (kThreads / 32);
     const unsigned grid = (unsigned)(blocks < 148 * 64 ? blocks : 148 * 64);
-    if (a.count < (1L << 31) - 1024) dropout_kernel<T, int><<<grid, kThreads, 0, st>>>(a, groups);
+    if (a.rows * (a.ldx > a.ldy ? a.ldx : a.ldy) < (1L << 31) - 1024) dropout_kernel<T, int><<<grid, kThreads, 0, st>>>(a, groups);
     else dropout_kernel<T, long><<<grid, kThreads, 0, st>>>(a, groups);
   }
   return cudaGetLastError();

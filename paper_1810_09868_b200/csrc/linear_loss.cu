@@ -949,7 +949,8 @@ void plan_gradients(long rows, long in, long classes, int planes, int pairs, Sha
     }
 }
 
-Plan make_plan(const vgg19_linear_loss& a, bool backward, int pairs) {
+// in_pairs: for the self-test, whether z's tiles are pairs', or null.
+Plan make_plan(const vgg19_linear_loss& a, bool backward, int pairs, const bool* in_pairs = nullptr) {
   Plan p{};
   const bool f32 = a.dtype == VGG19_FP32;
   p.planes = f32 ? 3 : 1;
@@ -973,11 +974,15 @@ Plan make_plan(const vgg19_linear_loss& a, bool backward, int pairs) {
   if (p.take_w) p.w = take((size_t)p.planes * (p.piece < a.classes ? p.piece : a.classes) * p.ld * 2);
   const long blocks = (a.in + BK - 1) / BK, piece_classes = p.piece < a.classes ? p.piece : a.classes;
   plan_logits(a.rows, piece_classes, blocks, p.planes, pairs, p.pieces == 1, &p.z_shape, &p.z_splits);
+  if (in_pairs) {
+    p.z_shape = Shape{*in_pairs, 128};
+    p.z_splits = 1;
+  }
   if (p.z_splits > 1) p.z = take((size_t)p.z_splits * a.rows * up(a.classes, 4) * 4);
   p.db_rows = p.z_splits > 1 ? kPartRows : 32;
   if (!backward) {
-    p.part = take((size_t)p.pieces * up(p.piece, p.z_shape.bn / 2) / (p.z_shape.bn / 2) * a.rows * sizeof(float2));
-    p.label_z = take((size_t)a.rows * 4);
+    if (p.z_splits == 1) p.part = take((size_t)p.pieces * up(p.piece, p.z_shape.bn / 2) / (p.z_shape.bn / 2) * a.rows * sizeof(float2));
+    if (p.z_splits == 1) p.label_z = take((size_t)a.rows * 4);
   } else {
     p.dz = take((size_t)p.planes * a.rows * p.piece * 2);
     p.db_part = take((size_t)(up(a.rows, p.db_rows) / p.db_rows) * p.piece * 4);
@@ -1222,6 +1227,7 @@ int check(const vgg19_linear_loss* a) {
   if (a->rows < 0 || a->rows > (1 << 22) || a->in < 1 || a->in > (1 << 20) || a->classes < 1 || a->classes > (1 << 24))
     return note_error(VGG19_ERR_SHAPE, "%lld rows of %d values, %d classes: rows in [0, 2^22], values in [1, 2^20], classes in [1, 2^24]",
                       (long long)a->rows, a->in, a->classes);
+  if (a->rows * a->classes > (1LL << 44)) return note_error(VGG19_ERR_SHAPE, "%lld rows against %d classes: at most 2^44 logits", (long long)a->rows, a->classes);
   if (a->ldx < a->in || a->ldw < a->in || a->ldx >= (1LL << 36) || a->ldw >= (1LL << 36))
     return note_error(VGG19_ERR_SHAPE, "row strides %lld and %lld for %d values", (long long)a->ldx, (long long)a->ldw, a->in);
   return VGG19_OK;
@@ -1260,7 +1266,7 @@ cudaError_t loss_take_error(int* code, int* label, cudaStream_t st) {
   return e == cudaSuccess ? take_error(static_cast<int*>(label_word), label, st) : e;
 }
 
-int linear_loss(const vgg19_linear_loss* layer, float* loss, float* lse, void* workspace, size_t bytes, const Waits& waits, void* stream) {
+int linear_loss(const vgg19_linear_loss* layer, float* loss, float* lse, void* workspace, size_t bytes, const Waits& waits, const bool* in_pairs, void* stream) {
   const int rc = check(layer);
   if (rc != VGG19_OK || layer->rows == 0) return rc;
   const vgg19_linear_loss& a = *layer;
@@ -1268,7 +1274,7 @@ int linear_loss(const vgg19_linear_loss* layer, float* loss, float* lse, void* w
   if (bad != VGG19_OK) return bad;
   if (!words(a.bias, a.labels, loss, lse)) return note_error(VGG19_ERR_ARG, "bias, labels, loss or lse is not aligned to 4 bytes");
   const int pairs = pairs_of_device();
-  const Plan p = make_plan(a, false, pairs);
+  const Plan p = make_plan(a, false, pairs, in_pairs);
   if (bytes < p.total) return note_error(VGG19_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu", bytes, p.total);
   const long elt = a.dtype == VGG19_FP32 ? 4 : 2, each = 4L * a.rows;
   const Block all[] = {{loss, 1, each, 0}, {lse, 1, each, 0}, {workspace, 1, (long)p.total, 0}, {a.labels, 1, each, 0}, {a.bias, 1, 4L * a.classes, 0},
@@ -1290,7 +1296,7 @@ extern "C" size_t vgg19_linear_cross_entropy_bytes(const vgg19_linear_loss* laye
 }
 
 extern "C" int vgg19_linear_cross_entropy(const vgg19_linear_loss* layer, float* loss, float* lse, void* workspace, size_t bytes, void* stream) {
-  return vgg::linear_loss(layer, loss, lse, workspace, bytes, vgg::Waits{}, stream);
+  return vgg::linear_loss(layer, loss, lse, workspace, bytes, vgg::Waits{}, nullptr, stream);
 }
 
 extern "C" int vgg19_linear_cross_entropy_backward(const vgg19_linear_loss* layer, const float* lse, const float* d_loss, void* dx, int64_t lddx,

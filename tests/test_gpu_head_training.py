@@ -147,7 +147,7 @@ def test_dropout_in_a_networks_training_passes(p, graph):
             h2 = torch.relu(h1 @ w[2].T + w[3]) * m[1]
             z = h2 @ w[4].T + w[5]
             torch.nn.functional.cross_entropy(z, labels.long()).backward()
-            for got, want in [(a1, h1), (a2, h2), (logits, z)] + [(at(grads, 32 + i), w[i].grad) for i in range(6)]:
+            for got, want in [(a1, h1.detach()), (a2, h2.detach()), (logits, z.detach())] + [(at(grads, 32 + i), w[i].grad) for i in range(6)]:
                 assert float((got.double() - want).norm() / want.norm()) < 1e-5
             assert not torch.equal(grads[:slices[32][0]], plain[2][:slices[32][0]])  # the convolutions' gradients pass through the masks
         net.set_dropout(0.0)

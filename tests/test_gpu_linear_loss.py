@@ -272,10 +272,18 @@ def test_the_same_bits_every_time_and_in_any_company(p):
         assert torch.equal(getattr(a, n), getattr(b, n)), n
 
 
-def test_pieces_of_the_classes(p):
-    """More rows times classes than one piece of dz holds: dx is added up over pieces."""
-    c = Case(20000, 40, 9000, "bf16", std=1.0).run(p)
+@pytest.mark.parametrize("rows,inner,classes,dtype,pad", [(20000, 40, 9000, "bf16", 0), (12000, 37, 9001, "fp32", 0), (50, 9001, 30000, "bf16", 3)])
+def test_pieces_of_the_classes(p, rows, inner, classes, dtype, pad):
+    """More rows times classes than one piece of dz holds, or more weights to be laid out than one piece has room for: dx is added up over pieces."""
+    c = Case(rows, inner, classes, dtype, std=1.0, pad=pad).run(p)
     c.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,inner,classes", [(128, 72, 40000), (100, 4096, 6000), (2300, 80, 2300), (640, 3000, 640), (256, 1030, 3000), (64, 40000, 30), (5000, 100, 4)])
+def test_tiles_of_every_shape(p, rows, inner, classes, dtype):
+    """Sizes for which the plan takes pairs and single CTAs, wide and narrow tiles, cut sums and whole ones."""
+    Case(rows, inner, classes, dtype, seed=7).run(p).check()
 
 
 def test_recorded_and_replayed_with_other_inputs(p):

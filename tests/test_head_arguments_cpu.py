@@ -41,7 +41,7 @@ def layer(p, **over):
 
 BAD_LAYERS = [
     (dict(dtype=2), "ARG"), (dict(rows=-1), "SHAPE"), (dict(rows=(1 << 22) + 1), "SHAPE"), (dict(in_=0), "SHAPE"), (dict(in_=(1 << 20) + 1, ldx=1 << 21, ldw=1 << 21), "SHAPE"),
-    (dict(classes=0), "SHAPE"), (dict(classes=(1 << 24) + 1), "SHAPE"), (dict(ldx=63), "SHAPE"), (dict(ldw=63), "SHAPE"), (dict(ldx=1 << 36), "SHAPE"), (dict(ldw=1 << 36), "SHAPE")]
+    (dict(rows=1 << 22, classes=1 << 23), "SHAPE"), (dict(classes=0), "SHAPE"), (dict(classes=(1 << 24) + 1), "SHAPE"), (dict(ldx=63), "SHAPE"), (dict(ldw=63), "SHAPE"), (dict(ldx=1 << 36), "SHAPE"), (dict(ldw=1 << 36), "SHAPE")]
 BAD_POINTERS = [(dict(x=None), "ARG"), (dict(w=None), "ARG"), (dict(labels=None), "ARG"), (dict(x=SOME + 1), "ARG"), (dict(dtype=0, w=SOME + 2), "ARG"), (dict(labels=SOME + 2), "ARG"),
                 (dict(bias=SOME + 1), "ARG")]
 
