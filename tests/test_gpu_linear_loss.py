@@ -280,7 +280,8 @@ def test_pieces_of_the_classes(p, rows, inner, classes, dtype, pad):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("rows,inner,classes", [(128, 72, 40000), (100, 4096, 6000), (2300, 80, 2300), (640, 3000, 640), (256, 1030, 3000), (64, 40000, 30), (5000, 100, 4)])
+@pytest.mark.parametrize("rows,inner,classes", [(128, 72, 40000), (100, 4096, 6000), (2300, 80, 2300), (640, 3000, 640), (256, 1030, 3000), (64, 40000, 30), (5000, 100, 4), (260, 64, 9600),
+                                                (130, 4096, 2049), (130, 4096, 5000), (130, 4096, 12001), (520, 1000, 12001), (400, 4096, 2049), (2400, 333, 5000), (4000, 200, 5000)])
 def test_tiles_of_every_shape(p, rows, inner, classes, dtype):
     """Sizes for which the plan takes pairs and single CTAs, wide and narrow tiles, cut sums and whole ones."""
     Case(rows, inner, classes, dtype, seed=7).run(p).check()
