@@ -10,9 +10,8 @@
 // would take 6 and 4 bytes a logit and pass over it.
 #include <cuda_runtime.h>
 
-#include <atomic>
-
 #include "../../include/vgg19_b200.h"
+#include "linear_loss.cuh"
 #include "tc_common.cuh"
 
 namespace vgg {
@@ -44,21 +43,9 @@ constexpr int kPieceBytes = 4096;            // an epilogue warp's own 32 rows o
 constexpr int kBiasBytes = 128;              // its 32 biases
 constexpr int kSmemBytes = kRingBytes + kEpilogueWarps * (kPieceBytes + kBiasBytes) + 1024 + 256;
 
-constexpr float kLog2e = 1.4426950408889634f;
-
 // What a tile's sums become: the statistics of its rows, dz, the product itself, or parts of z's sum (kept in fp32, added up in chains).
 enum Epilogue { kStatistics, kLogitGradient, kProduct, kSums };
 
-// A launch's kernel may be set up while the one before it in the stream ends; what it reads is there from here on.
-__device__ __forceinline__ void behind_previous() {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-}
-__device__ __forceinline__ float fast_exp2(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
 // What one CTA, or a pair, does.
 template <bool PAIR> __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
   if (PAIR) tma_load_3d_pair(dst, map, bar, c0, c1, c2); else tma_load_3d(dst, map, bar, c0, c1, c2);
@@ -539,7 +526,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
             if (c >= half) break;
             float part = 0.f;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) part += fast_exp2((v[c + j] - ref) * kLog2e);
+            for (int j = 0; j < 32; ++j) part += fast_exp2((v[c + j] - ref) * kLossLog2e);
             sum += part;
           }
           if (lane < rows && cols > 0) L.rows.part[(long)(L.rows.first_part + 2 * tile.j + group) * p.m + row] = make_float2(most, sum);
@@ -554,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
               add_bias(c);
               const int at = label - j0 - c;
 #pragma unroll
-              for (int j = 0; j < 32; ++j) v[c + j] = fast_exp2((v[c + j] - ref) * kLog2e);
+              for (int j = 0; j < 32; ++j) v[c + j] = fast_exp2((v[c + j] - ref) * kLossLog2e);
               if (__any_sync(0xffffffffu, (unsigned)at < 32u)) {
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[c + j] = at == j ? v[c + j] - 1.f : v[c + j];
@@ -623,13 +610,6 @@ struct Join {
   int parts, rows, classes;
 };
 constexpr int kJoinRows = 4, kJoinGroups = 64;  // rows of a block (whole sectors), and threads of each
-
-// (m, s) with the largest z so far and the sum of exp(z - m); nothing so far: (-inf, 0).  A NaN stays in s.
-__device__ __forceinline__ float2 join(float2 a, float2 b) {
-  const float m = fmaxf(a.x, b.x);
-  if (m == -INFINITY) return make_float2(m, a.y + b.y);
-  return make_float2(m, a.y * fast_exp2((a.x - m) * kLog2e) + b.y * fast_exp2((b.x - m) * kLog2e));
-}
 
 // What a row answers with.
 __device__ __forceinline__ void finish_row(float2 v, int label, int classes, float label_z, float* loss, float* lse) {
@@ -714,7 +694,7 @@ __global__ void __launch_bounds__(kRowThreads) loss_of_parts_kernel(const __grid
     const float4 z = sum_of_parts(a, row, c);
     if ((unsigned)(label - c) < 4u && label < a.classes) label_z = label - c == 0 ? z.x : label - c == 1 ? z.y : label - c == 2 ? z.z : z.w;
     const float m = fmaxf(fmaxf(z.x, z.y), fmaxf(z.z, z.w)), ref = m == -INFINITY ? 0.f : m;
-    v = join(v, make_float2(m, (fast_exp2((z.x - ref) * kLog2e) + fast_exp2((z.y - ref) * kLog2e)) + (fast_exp2((z.z - ref) * kLog2e) + fast_exp2((z.w - ref) * kLog2e))));
+    v = join(v, make_float2(m, (fast_exp2((z.x - ref) * kLossLog2e) + fast_exp2((z.y - ref) * kLossLog2e)) + (fast_exp2((z.z - ref) * kLossLog2e) + fast_exp2((z.w - ref) * kLossLog2e))));
   }
 #pragma unroll
   for (int n = 16; n; n /= 2) v = join(v, make_float2(__shfl_down_sync(0xffffffffu, v.x, n), __shfl_down_sync(0xffffffffu, v.y, n)));
@@ -744,7 +724,7 @@ template <int P> __global__ void __launch_bounds__(32 * kPartRows) gradient_of_p
     const float v[4] = {z.x, z.y, z.z, z.w};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const float e = fast_exp2((v[k] - lse) * kLog2e);
+      const float e = fast_exp2((v[k] - lse) * kLossLog2e);
       g[k] = d_loss == 0.f ? 0.f : d_loss * (label - c == k ? e - 1.f : e);
     }
   }
@@ -804,24 +784,40 @@ __global__ void __launch_bounds__(256) planes_kernel(const __grid_constant__ Lay
 }
 
 // ---- dx from its parts -----------------------------------------------------------------------------------------------
-template <typename T>
+// GROUPS: threads that share a sum of many parts, for few values.
+template <typename T, int GROUPS>
 __global__ void __launch_bounds__(256) sum_parts_kernel(const float* __restrict__ part, int parts, long rows, int in, long ld, T* out, long out_ld) {
+  constexpr int WIDE = 256 / GROUPS;
+  __shared__ float4 got[GROUPS][WIDE];
   behind_previous();
-  const int chunks = (int)(ld / 4);
+  const int chunks = (int)(ld / 4), lane = threadIdx.x % WIDE, group = threadIdx.x / WIDE;
   const long all = rows * chunks;
-  for (long t = (long)blockIdx.x * blockDim.x + threadIdx.x; t < all; t += (long)gridDim.x * blockDim.x) {
-    const long r = t / chunks;
+  for (long t0 = (long)blockIdx.x * WIDE; t0 < all; t0 += (long)gridDim.x * WIDE) {
+    const long t = t0 + lane, r = t / chunks;
     const int k = (int)(t - r * chunks) * 4;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int p = 0; p < parts; ++p) {
-      const float4 v = *reinterpret_cast<const float4*>(part + (p * rows + r) * ld + k);
-      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    if (t < all)
+      for (int p = group; p < parts; p += 8 * GROUPS) {  // eight requests at once, the last ones too
+        float4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          v[i] = p + i * GROUPS < parts ? *reinterpret_cast<const float4*>(part + ((p + i * GROUPS) * rows + r) * ld + k) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { s.x += v[i].x; s.y += v[i].y; s.z += v[i].z; s.w += v[i].w; }
+      }
+    if (GROUPS > 1) {
+      got[group][lane] = s;
+      __syncthreads();
+      if (group == 0) {
+#pragma unroll
+        for (int g = 1; g < GROUPS; ++g) { s.x += got[g][lane].x; s.y += got[g][lane].y; s.z += got[g][lane].z; s.w += got[g][lane].w; }
+      }
+      __syncthreads();
     }
     const float v[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (k + e < in) out[r * out_ld + k + e] = from_f32<T>(v[e]);
+      if (group == 0 && t < all && k + e < in) out[r * out_ld + k + e] = from_f32<T>(v[e]);
   }
 }
 
@@ -871,6 +867,7 @@ struct Shape {
 };
 // How a call is cut up, and where its parts lie in the workspace.
 struct Plan {
+  int few;                // not 0: few rows of fp32, on the CUDA cores, with so many parts; of what follows there are then part, label_z, dz and dx alone
   int planes;             // 1 or 3
   bool take_x, take_w;    // whether they are laid out anew (as planes, or to be read by copies at all)
   long ld;                // row stride of what is
@@ -953,6 +950,21 @@ void plan_gradients(long rows, long in, long classes, int planes, int pairs, Sha
 Plan make_plan(const vgg19_linear_loss& a, bool backward, int pairs, const bool* in_pairs = nullptr) {
   Plan p{};
   const bool f32 = a.dtype == VGG19_FP32;
+  size_t at = 0;
+  auto take = [&at](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
+  if (!in_pairs && few_rows(a)) {
+    p.few = backward ? few_rows_ranges(a, 2 * pairs) : few_rows_blocks(a, 2 * pairs);
+    p.dx_ld = up(a.in, 4);
+    if (backward) {
+      p.dz = take((size_t)a.classes * few_rows_up((int)a.rows) * 4);
+      p.dx = take((size_t)p.few * a.rows * p.dx_ld * 4);
+    } else {
+      p.part = take((size_t)p.few * a.rows * sizeof(float2));
+      p.label_z = take((size_t)a.rows * 4);
+    }
+    p.total = at < 256 ? 256 : at;
+    return p;
+  }
   p.planes = f32 ? 3 : 1;
   p.take_x = f32 || !copyable(a.x, a.rows, a.ldx, 2);
   p.take_w = f32 || !copyable(a.w, a.classes, a.ldw, 2);
@@ -968,8 +980,6 @@ Plan make_plan(const vgg19_linear_loss& a, bool backward, int pairs, const bool*
   p.pieces = (int)((all + p.piece - 1) / p.piece);
   p.piece = up((all + p.pieces - 1) / p.pieces, BN);  // pieces of about one size
   p.pieces = (int)((all + p.piece - 1) / p.piece);
-  size_t at = 0;
-  auto take = [&at](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
   if (p.take_x) p.x = take((size_t)p.planes * a.rows * p.ld * 2);
   if (p.take_w) p.w = take((size_t)p.planes * (p.piece < a.classes ? p.piece : a.classes) * p.ld * 2);
   const long blocks = (a.in + BK - 1) / BK, piece_classes = p.piece < a.classes ? p.piece : a.classes;
@@ -995,28 +1005,6 @@ Plan make_plan(const vgg19_linear_loss& a, bool backward, int pairs, const bool*
   return p;
 }
 
-// A launch whose set-up overlaps the one before it in the stream (the kernels wait for that one themselves).
-template <typename... A>
-cudaError_t launch_clusters(void (*kernel)(A...), unsigned cluster, dim3 blocks, int threads, int smem, cudaStream_t st, const A&... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = blocks;
-  cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = (size_t)smem;
-  cfg.stream = st;
-  cudaLaunchAttribute at[2] = {};
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = cluster;
-  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-template <typename... A>
-cudaError_t launch_behind(void (*kernel)(A...), dim3 blocks, int threads, int smem, cudaStream_t st, const A&... args) {
-  return launch_clusters(kernel, 1, blocks, threads, smem, st, args...);
-}
 template <int P, int EPI, bool PAIR> cudaError_t launch_tiles(const Launch& L, int pairs, cudaStream_t st) {
   const cudaError_t e = cudaFuncSetAttribute(loss_product_kernel<P, EPI, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   if (e != cudaSuccess) return e;
@@ -1091,6 +1079,8 @@ template <int P> Launch logits(const Operands<P>& o, const Plan& p, long first, 
   return L;
 }
 
+cudaError_t join_parts(const vgg19_linear_loss& a, float* loss, float* lse, char* ws, const Plan& p, int parts, cudaStream_t st);
+
 // z in parts of its sum.
 template <int P> cudaError_t logits_in_parts(const Operands<P>& o, const Plan& p, int pairs, const Waits& waits, Parts& parts, cudaStream_t st) {
   Launch L = logits<P>(o, p, 0, o.a.classes, waits);
@@ -1129,8 +1119,16 @@ cudaError_t forward(const vgg19_linear_loss& a, float* loss, float* lse, char* w
     e = launch_products<P, kStatistics>(L, p.z_shape.pair, pairs, st);
   }
   if (e != cudaSuccess) return e;
-  const Join j{reinterpret_cast<const float2*>(ws + p.part), reinterpret_cast<const float*>(ws + p.label_z), a.labels, loss, lse, part, (int)a.rows, a.classes};
+  return join_parts(a, loss, lse, ws, p, part, st);
+}
+
+cudaError_t join_parts(const vgg19_linear_loss& a, float* loss, float* lse, char* ws, const Plan& p, int parts, cudaStream_t st) {
+  const Join j{reinterpret_cast<const float2*>(ws + p.part), reinterpret_cast<const float*>(ws + p.label_z), a.labels, loss, lse, parts, (int)a.rows, a.classes};
   return launch_behind(join_rows_kernel, (unsigned)((a.rows + kJoinRows - 1) / kJoinRows), kJoinRows * kJoinGroups, 0, st, j);
+}
+cudaError_t forward_few(const vgg19_linear_loss& a, float* loss, float* lse, char* ws, const Plan& p, int pairs, cudaStream_t st) {
+  const cudaError_t e = few_rows_loss(a, reinterpret_cast<float2*>(ws + p.part), reinterpret_cast<float*>(ws + p.label_z), 2 * pairs, st);
+  return e == cudaSuccess ? join_parts(a, loss, lse, ws, p, p.few, st) : e;
 }
 
 struct Gradients {
@@ -1142,6 +1140,18 @@ struct Gradients {
   long dw_ld;
   float* db;
 };
+
+// dx from its parts.
+template <typename T, int GROUPS>
+cudaError_t sum_dx(const vgg19_linear_loss& a, const Gradients& g, char* ws, const Plan& p, int parts, cudaStream_t st) {
+  const long chunks = a.rows * (p.dx_ld / 4), blocks = (chunks * GROUPS + 255) / 256;
+  return launch_behind(sum_parts_kernel<T, GROUPS>, (unsigned)(blocks < 148 * 16 ? blocks : 148 * 16), 256, 0, st, reinterpret_cast<const float*>(ws + p.dx), parts,
+                       (long)a.rows, (int)a.in, p.dx_ld, static_cast<T*>(g.dx), g.dx_ld);
+}
+cudaError_t sum_dx(const vgg19_linear_loss& a, const Gradients& g, char* ws, const Plan& p, int parts, cudaStream_t st) {
+  if (a.dtype == VGG19_FP32) return parts > 16 ? sum_dx<float, 8>(a, g, ws, p, parts, st) : sum_dx<float, 1>(a, g, ws, p, parts, st);
+  return parts > 16 ? sum_dx<bf16, 8>(a, g, ws, p, parts, st) : sum_dx<bf16, 1>(a, g, ws, p, parts, st);
+}
 
 template <int P>
 cudaError_t backward(const vgg19_linear_loss& a, const Gradients& g, char* ws, const Plan& p, int pairs, const Waits& waits, cudaStream_t st) {
@@ -1213,11 +1223,17 @@ cudaError_t backward(const vgg19_linear_loss& a, const Gradients& g, char* ws, c
       e = launch_behind(sum_columns_kernel, (unsigned)((n + 31) / 32), 256, 0, st, static_cast<const float*>(db_part), (int)((a.rows + p.db_rows - 1) / p.db_rows), (int)n, g.db + first);
   }
   if (e != cudaSuccess || !g.dx || !p.dx_parts) return e;
-  const long chunks = a.rows * (p.dx_ld / 4);
-  const unsigned blocks = (unsigned)(chunks / 256 + 1 < 148 * 16 ? chunks / 256 + 1 : 148 * 16);
-  if (P == 3)
-    return launch_behind(sum_parts_kernel<float>, blocks, 256, 0, st, static_cast<const float*>(dx_part), slots, (long)a.rows, (int)a.in, p.dx_ld, static_cast<float*>(g.dx), g.dx_ld);
-  return launch_behind(sum_parts_kernel<bf16>, blocks, 256, 0, st, static_cast<const float*>(dx_part), slots, (long)a.rows, (int)a.in, p.dx_ld, static_cast<bf16*>(g.dx), g.dx_ld);
+  return sum_dx(a, g, ws, p, slots, st);
+}
+
+cudaError_t backward_few(const vgg19_linear_loss& a, const Gradients& g, char* ws, const Plan& p, int pairs, cudaStream_t st) {
+  void* label_error = nullptr;
+  cudaError_t e = cudaGetSymbolAddress(&label_error, g_label_error);
+  if (e != cudaSuccess) return e;
+  const FewGradients f{g.lse, g.d_loss, reinterpret_cast<float*>(ws + p.dz), g.dx ? reinterpret_cast<float*>(ws + p.dx) : nullptr, p.dx_ld,
+                       static_cast<float*>(g.dw), g.dw_ld, g.db, static_cast<int*>(label_error)};
+  e = few_rows_gradients(a, f, 2 * pairs, st);
+  return e == cudaSuccess && g.dx ? sum_dx(a, g, ws, p, p.few, st) : e;
 }
 
 int check(const vgg19_linear_loss* a) {
@@ -1283,7 +1299,7 @@ int linear_loss(const vgg19_linear_loss* layer, float* loss, float* lse, void* w
   if (!loss && !lse) return VGG19_OK;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
-  const cudaError_t e = p.planes == 3 ? forward<3>(a, loss, lse, ws, p, pairs, waits, st) : forward<1>(a, loss, lse, ws, p, pairs, waits, st);
+  const cudaError_t e = p.few ? forward_few(a, loss, lse, ws, p, pairs, st) : p.planes == 3 ? forward<3>(a, loss, lse, ws, p, pairs, waits, st) : forward<1>(a, loss, lse, ws, p, pairs, waits, st);
   return e == cudaSuccess ? VGG19_OK : note_error(VGG19_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(e));
 }
 
@@ -1332,6 +1348,6 @@ extern "C" int vgg19_linear_cross_entropy_backward(const vgg19_linear_loss* laye
   const Gradients g{lse, d_loss, dx, (long)lddx, dw, dw_dtype == VGG19_FP32, (long)lddw, db};
   char* ws = static_cast<char*>(workspace);
   const Waits waits{};
-  const cudaError_t e = p.planes == 3 ? backward<3>(a, g, ws, p, pairs, waits, st) : backward<1>(a, g, ws, p, pairs, waits, st);
+  const cudaError_t e = p.few ? backward_few(a, g, ws, p, pairs, st) : p.planes == 3 ? backward<3>(a, g, ws, p, pairs, waits, st) : backward<1>(a, g, ws, p, pairs, waits, st);
   return e == cudaSuccess ? VGG19_OK : note_error(VGG19_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(e));
 }

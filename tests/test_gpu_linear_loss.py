@@ -112,6 +112,15 @@ def test_against_the_formulas(p, rows, inner, classes, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 7, 8, 9])
+@pytest.mark.parametrize("inner,classes,pad,skip", [(1, 5, 0, 0), (255, 100, 0, 0), (264, 1000, 0, 0), (4096, 300, 0, 0), (4097, 33, 3, 0), (8192, 90, 0, 0), (8200, 17, 0, 0), (100, 20011, 4, 0), (333, 2049, 3, 1),
+                                                    (64, 9500, 8, 0)])
+def test_a_few_rows(p, rows, inner, classes, pad, skip, dtype):
+    """Up to eight rows have kernels of their own, up to 8192 inputs (eight rows: 4096)."""
+    Case(rows, inner, classes, dtype, seed=rows, pad=pad, skip=skip).run(p, dw_dtype=torch.float32 if classes == 33 else None).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("rows,inner,classes,pad,skip,out_pad", [(40, 64, 300, 8, 0, 0), (40, 64, 300, 3, 0, 1), (40, 64, 300, 7, 1, 8), (70, 333, 130, 5, 0, 3), (1, 64, 40, 9, 1, 5)])
 def test_rows_of_wider_buffers(p, rows, inner, classes, pad, skip, out_pad, dtype):
     c = Case(rows, inner, classes, dtype, pad=pad, skip=skip).run(p, out_pad=out_pad)
