@@ -6,6 +6,9 @@
 // (the keys of the rounds are the same for all and come as constants); one value a word would make 10 instructions a
 // value of that, beside 5 for the value itself, which is what bf16 at the memory's rate leaves; 16 bits a value make it 5, and
 // rates in steps of 2^-16.
+//
+// Measured (B200): 4096 x 25088 bf16 in 69.6 us, 5.9 TB/s, where a copy of it takes 65.8 and the kernel without the generator 63.9; 1001 rows of
+// 4099 fp32, 4112 apart, which no block of the generator is aligned with, in 10.1 us (5.0 by the bytes).
 #include <cuda_runtime.h>
 
 #include <cmath>

@@ -3,6 +3,10 @@
 // read again from there.  (bf16 weights need no planes: there the tiles are as fast or faster.)  Forward, w is read once: a warp takes a few
 // classes, its lanes along the inputs, with the rows of x in shared memory.  Backward it is read twice: for z, which becomes dz [classes][rows],
 // and by threads that keep four inputs each, of x and of dx, and go through a range of the classes, writing dw.  All sums are fp32 FMAs.
+//
+// Measured (B200, device time; the planes' way behind): 4096 inputs against 50021 classes, one row 138 us and 412 us for the gradients (781 and 1396),
+// eight rows 321 and 703 (778 and 1303); against 1000 classes, one row 12.6 and 18.7 (21 and 41), eight 22 and 34 (20 and 41).  One row reads w at 5.9 TB/s (0.9 of a
+// copy's rate); eight rows are bound by the eight reads of x in shared memory for every four of w.
 #include <cuda_runtime.h>
 
 #include "../../include/vgg19_b200.h"

@@ -111,9 +111,9 @@ def test_the_binding_refuses_what_does_not_fit(p):
 
 
 def test_workspaces_have_room_for_what_is_laid_out_anew(p):
-    """x and w that copies cannot read where they lie, or that are fp32, take more; a loss without gradients takes less than with them."""
-    size = lambda back, **over: p.binding.load().vgg19_linear_cross_entropy_bytes(ctypes.byref(layer(p, **over)), back)  # noqa: E731
+    """x and w that copies cannot read where they lie, or that are fp32 (for more than eight rows), take more."""
+    size = lambda back, **over: p.binding.load().vgg19_linear_cross_entropy_bytes(ctypes.byref(layer(p, rows=20, **over)), back)  # noqa: E731
     for back in (0, 1):
         plain = size(back)
-        assert size(back, ldx=65) >= plain + 5 * 64 * 2 and size(back, ldw=65) >= plain + 100 * 64 * 2 and size(back, w=SOME + 2) >= plain + 100 * 64 * 2
-        assert size(back, dtype=0) >= plain + 105 * 64 * 6
+        assert size(back, ldx=65) >= plain + 20 * 64 * 2 and size(back, ldw=65) >= plain + 100 * 64 * 2 and size(back, w=SOME + 2) >= plain + 100 * 64 * 2
+        assert size(back, dtype=0) >= plain + 120 * 64 * 6
