@@ -488,7 +488,7 @@ int vgg19_set_dropout(vgg19_t *net, float rate, uint64_t seed, uint64_t first_pa
  * classes, without keeping the logits:
  *   z = x w^T + bias,   lse_r = log sum_n exp z_rn,   loss_r = lse_r - z_r,labels[r].
  * x: device [rows][in], row stride ldx; w: device [classes][in], row stride ldw; both `dtype`.  bias: device fp32 [classes] or
- * NULL; a bias of -inf excludes its class.  labels: device int32 [rows].  Rows and strides of 16 bytes are read where they lie, others
+ * NULL; a bias of -inf excludes its class (whose weights have to be finite all the same).  labels: device int32 [rows].  Rows and strides of 16 bytes are read where they lie, others
  * are laid out in the workspace first. */
 typedef struct {
   const void *x;
@@ -504,8 +504,8 @@ typedef struct {
 /* loss, lse: device fp32 [rows], either may be NULL.  A label VGG19_NO_CLASS asks for nothing (a row that only fills the batch): its loss
  * is 0.  Any other label outside [0, classes) is never used as an index: its loss is NaN and vgg19_ops_status reports VGG19_ERR_ARG.
  * A row that is left no class has lse -inf and loss +inf; so has an excluded label, with a finite lse.  A NaN or +inf among a row's z makes its results NaN.
- * bf16 products are exact and summed in fp32; fp32 values are taken as three bf16 terms each (an infinity makes its row's results NaN), and the
- * products of terms down to 2^-16 of the first.  At most 2^44 logits.
+ * bf16 products are exact and summed in fp32; fp32 values are taken as three bf16 terms each, with the
+ * products of terms down to 2^-16 of the first (an infinity may make its row's results NaN where the formula would not); up to eight rows, in fp32 as they are.  At most 2^44 logits.
  * workspace: device, 256-byte aligned, vgg19_linear_cross_entropy_bytes(layer, 0) bytes (0 for a layer that is refused; of pointers only the
  * alignment of x and w is looked at): scratch for the time of the call; calls that share one have to be ordered.  Asynchronous
  * on `stream`; may be captured.  rows == 0 does nothing.  Nothing that is written may overlap anything else of the call. */

@@ -589,6 +589,7 @@ def _any_dropout(name, x, y, rate, seed, step, step_counter, first, stream):
     for v, what in ((seed, "seed"), (step, "step"), (first, "first")):
         if not 0 <= v < 1 << 64:
             _refuse(VGG19_ERR_ARG, f"{what} {v} is not an unsigned 64-bit number")
+    seed, step, first = int(seed), int(step), int(first)
     import torch
     counter = _tensor(step_counter, "step_counter", torch.int64, (1,), dev)
     return _call(dev, getattr(_lib or load(), "vgg19_" + name), x.data_ptr(), dtype, rows, cols, ldx, rate, seed, step, counter, first, y.data_ptr(), ldy,

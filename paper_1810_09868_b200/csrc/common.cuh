@@ -78,7 +78,7 @@ template <int M> inline bool spans_meet(const Span (&all)[M], int written) {
 // Waits for the stream; *code becomes the device error word's value and the word 0, in one exchange on the device: what a kernel on another
 // stream records meanwhile is either taken or left for the next status.  word[1] is the exchange's own.  One host thread at a time.
 cudaError_t take_error(int* word, int* code, cudaStream_t st);
-// The same for the words of calls without a handle (logprobs.cu, q4_dense.cu, muon.cu, linear_loss.cu), on the current device.
+// The same for the words of calls without a handle (logprobs.cu, q4_dense.cu, muon.cu, linear_loss.cu and linear_loss_few.cu), on the current device.
 cudaError_t logprobs_take_error(int* code, cudaStream_t st);
 cudaError_t q4_take_error(int* code, cudaStream_t st);
 cudaError_t muon_take_error(int* code, cudaStream_t st);

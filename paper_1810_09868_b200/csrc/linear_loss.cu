@@ -994,7 +994,8 @@ Plan make_plan(const vgg19_linear_loss& a, bool backward, int pairs, const bool*
   const long all = up(a.classes, BN);
   p.piece = all;
   auto most = [&](long bytes_a_class) {
-    const long fit = kPieceBytesMost / bytes_a_class / BN * BN, least = 4096;
+    // at least 4096 classes, since dx is read and written again for every piece, unless those are over a gigabyte
+    const long fit = kPieceBytesMost / bytes_a_class / BN * BN, few = (1L << 30) / bytes_a_class / BN * BN, least = few >= 4096 ? 4096 : few > BN ? few : BN;
     if (p.piece > (fit > least ? fit : least)) p.piece = fit > least ? fit : least;
   };
   if (p.take_w) most(2 * p.planes * p.ld);
@@ -1249,12 +1250,9 @@ cudaError_t backward(const vgg19_linear_loss& a, const Gradients& g, char* ws, c
 }
 
 cudaError_t backward_few(const vgg19_linear_loss& a, const Gradients& g, char* ws, const Plan& p, int pairs, cudaStream_t st) {
-  void* label_error = nullptr;
-  cudaError_t e = cudaGetSymbolAddress(&label_error, g_label_error);
-  if (e != cudaSuccess) return e;
   const FewGradients f{g.lse, g.d_loss, reinterpret_cast<float*>(ws + p.dz), g.dx ? reinterpret_cast<float*>(ws + p.dx) : nullptr, p.dx_ld,
-                       static_cast<float*>(g.dw), g.dw_ld, g.db, static_cast<int*>(label_error)};
-  e = few_rows_gradients(a, f, 2 * pairs, st);
+                       static_cast<float*>(g.dw), g.dw_ld, g.db};
+  const cudaError_t e = few_rows_gradients(a, f, 2 * pairs, st);
   return e == cudaSuccess && g.dx ? sum_dx(a, g, ws, p, p.few, st) : e;
 }
 
@@ -1301,7 +1299,11 @@ cudaError_t loss_take_error(int* code, int* label, cudaStream_t st) {
   cudaError_t e = cudaGetSymbolAddress(&word, g_loss_error);
   if (e == cudaSuccess) e = cudaGetSymbolAddress(&label_word, g_label_error);
   if (e == cudaSuccess) e = take_error(static_cast<int*>(word), code, st);
-  return e == cudaSuccess ? take_error(static_cast<int*>(label_word), label, st) : e;
+  if (e == cudaSuccess) e = take_error(static_cast<int*>(label_word), label, st);
+  int few = 0;
+  if (e == cudaSuccess) e = few_rows_take_error(&few, st);
+  if (few) *label = few;
+  return e;
 }
 
 int linear_loss(const vgg19_linear_loss* layer, float* loss, float* lse, void* workspace, size_t bytes, const Waits& waits, const bool* in_pairs, void* stream) {

@@ -15,6 +15,8 @@
 namespace vgg {
 namespace {
 
+static __device__ int g_few_label_error[2];  // kDevBadLabel once a label outside [0, classes) was met
+
 constexpr int kV = 4;  // values of a slot: 16 bytes
 
 // Slot q of a row: V values, those from q V on where rows are aligned; else of every 32 V values, q % 32 and every 32nd behind it, so that lanes
@@ -153,7 +155,7 @@ template <int RM, int B> __global__ void __launch_bounds__(256) few_logit_gradie
     label = a.labels[r];
     lse = a.g.lse[r];
     const bool real = (unsigned)label < (unsigned)a.classes;
-    if (!real && label != VGG19_NO_CLASS && blockIdx.x == 0) atomicCAS(a.g.label_error, 0, (int)kDevBadLabel);
+    if (!real && label != VGG19_NO_CLASS && blockIdx.x == 0) atomicCAS(g_few_label_error, 0, (int)kDevBadLabel);
     d_loss = real && lse != -INFINITY ? a.g.d_loss[r] : 0.f;
   }
   for (int n0 = (blockIdx.x * warps + warp) * B; n0 < a.classes; n0 += gridDim.x * warps * B) {
@@ -287,6 +289,12 @@ template <int RM> cudaError_t gradients_of(const Layer& l, int b, int blocks, in
 }
 
 }  // namespace
+
+cudaError_t few_rows_take_error(int* label, cudaStream_t st) {
+  void* word = nullptr;
+  const cudaError_t e = cudaGetSymbolAddress(&word, g_few_label_error);
+  return e == cudaSuccess ? take_error(static_cast<int*>(word), label, st) : e;
+}
 
 bool few_rows(const vgg19_linear_loss& a) { return a.dtype == VGG19_FP32 && a.rows <= 8 && a.in <= 32768 / few_rows_up((int)a.rows); }
 

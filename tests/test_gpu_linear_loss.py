@@ -204,6 +204,21 @@ def test_rows_without_a_label_may_hold_anything_in_a_score(p):
     assert (c.loss[::2] == 0).all() and torch.equal(c.loss[1::2], good.loss[1::2])
 
 
+def test_labels_outside_the_classes_of_a_few_rows(p):
+    c, st = Case(5, 64, 100, "fp32"), torch.cuda.current_stream()
+    c.labels[:] = torch.tensor([100, 5, -2, -(1 << 31), 7], dtype=torch.int32, device=DEV)
+    c.run(p, check=False)
+    with pytest.raises(p.Vgg19Error) as e:
+        p.vgg19_ops_status(st)
+    assert e.value.code == p.VGG19_ERR_ARG
+    p.vgg19_ops_status(st)
+    c.run(p, backward=False, check=False)
+    with pytest.raises(p.Vgg19Error):
+        p.vgg19_ops_status(st)
+    c.check()
+    assert c.loss[[0, 2, 3]].isnan().all() and (c.dx[[0, 2, 3]] == 0).all()
+
+
 def test_labels_outside_the_classes_are_reported_and_count_for_nothing(p):
     c = Case(300, 64, 100)
     c.labels[::7] = torch.tensor([100, -2, 1 << 30], dtype=torch.int32, device=DEV).repeat(15)[:43]
@@ -296,8 +311,9 @@ def test_tiles_of_every_shape(p, rows, inner, classes, dtype):
     Case(rows, inner, classes, dtype, seed=7).run(p).check()
 
 
-def test_recorded_and_replayed_with_other_inputs(p):
-    c = Case(100, 264, 1000)
+@pytest.mark.parametrize("rows,inner,classes,dtype", [(100, 264, 1000, "bf16"), (4, 264, 1000, "fp32"), (300, 333, 2049, "bf16"), (200, 64, 500, "fp32")])
+def test_recorded_and_replayed_with_other_inputs(p, rows, inner, classes, dtype):
+    c = Case(rows, inner, classes, dtype)
     st = torch.cuda.Stream()
     with torch.cuda.stream(st):
         ws = [torch.empty(p.vgg19_linear_cross_entropy_bytes(c.x, c.w, b), dtype=torch.uint8, device=DEV) for b in (False, True)]
@@ -307,7 +323,7 @@ def test_recorded_and_replayed_with_other_inputs(p):
     with torch.cuda.graph(graph, stream=st):
         c.run(p, torch.cuda.current_stream(), workspaces=ws, check=False)
     for seed in (3, 4):
-        other = Case(100, 264, 1000, seed=seed)
+        other = Case(rows, inner, classes, dtype, seed=seed)
         for n in ("x", "w", "bias", "labels", "d_loss"):
             getattr(c, n).copy_(getattr(other, n))
         graph.replay()
@@ -316,6 +332,33 @@ def test_recorded_and_replayed_with_other_inputs(p):
         other.run(p)
         for n in ("loss", "lse", "dx", "dw", "db"):
             assert torch.equal(getattr(c, n), getattr(other, n)), n
+
+
+@pytest.mark.parametrize("dtype,rows", [("bf16", 100), ("fp32", 100), ("fp32", 3)])
+def test_recorded_behind_copies_clears_and_another_stream(p, dtype, rows):
+    """What a recorded call reads may come from any kind of node: a copy, a clear, a kernel of a stream that joins."""
+    c, other = Case(rows, 136, 700, dtype), Case(rows, 136, 700, dtype, seed=9)
+    side = torch.cuda.Stream()
+    ws = [torch.empty(p.vgg19_linear_cross_entropy_bytes(c.x, c.w, b), dtype=torch.uint8, device=DEV) for b in (False, True)]
+    c.run(p, workspaces=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        st = torch.cuda.current_stream()
+        side.wait_stream(st)
+        with torch.cuda.stream(side):
+            torch.add(other.w, 0, out=c.w)
+            c.d_loss.copy_(other.d_loss)
+        c.bias.zero_()
+        c.x.copy_(other.x)
+        st.wait_stream(side)
+        c.labels.copy_(other.labels)
+        c.run(p, st, workspaces=ws, check=False)
+    c.x.zero_(), c.w.zero_(), c.bias.fill_(3.0), c.labels.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    c.check()
+    assert torch.equal(c.x, other.x) and torch.equal(c.w, other.w)
 
 
 def test_two_streams_at_once(p):
