@@ -4,9 +4,9 @@
 // classes, its lanes along the inputs, with the rows of x in shared memory.  Backward it is read twice: for z, which becomes dz [classes][rows],
 // and by threads that keep four inputs each, of x and of dx, and go through a range of the classes, writing dw.  All sums are fp32 FMAs.
 //
-// Measured (B200, device time; the planes' way behind): 4096 inputs against 50021 classes, one row 138 us and 412 us for the gradients (781 and 1396),
-// eight rows 321 and 703 (778 and 1303); against 1000 classes, one row 12.6 and 18.7 (21 and 41), eight 22 and 34 (20 and 41).  One row reads w at 5.9 TB/s (0.9 of a
-// copy's rate); eight rows are bound by the eight reads of x in shared memory for every four of w.
+// Measured (B200, device time; the planes' way behind): 4096 inputs against 50021 classes, one row 142 us and 416 us for the gradients (781 and 1396),
+// eight rows 221 and 624 (778 and 1303); against 1000 classes, one row 13 and 19 (21 and 41), eight 23 and 34 (20 and 41).  One row reads w at 5.8 TB/s (0.9 of a
+// copy's rate); eight rows read x twice from shared memory for every value of w, with one block of sixteen warps an SM (eight warps: 321 us).
 #include <cuda_runtime.h>
 
 #include "../../include/vgg19_b200.h"
@@ -18,6 +18,7 @@ namespace {
 static __device__ int g_few_label_error[2];  // kDevBadLabel once a label outside [0, classes) was met
 
 constexpr int kV = 4;  // values of a slot: 16 bytes
+constexpr int kMostWarps = 16;
 
 // Slot q of a row: V values, those from q V on where rows are aligned; else of every 32 V values, q % 32 and every 32nd behind it, so that lanes
 // run along the row either way.
@@ -103,9 +104,9 @@ struct Layer {
   FewGradients g;
 };
 
-template <int RM, int B> __global__ void __launch_bounds__(256) few_loss_kernel(const __grid_constant__ Layer a) {
+template <int RM, int B> __global__ void __launch_bounds__(32 * kMostWarps) few_loss_kernel(const __grid_constant__ Layer a) {
   extern __shared__ float xs[];
-  __shared__ float2 got[8][RM];
+  __shared__ float2 got[kMostWarps][RM];
   behind_previous();
   const Slots s{a.in, a.aligned != 0};
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x / 32;
@@ -140,7 +141,7 @@ template <int RM, int B> __global__ void __launch_bounds__(256) few_loss_kernel(
 }
 
 // dz [classes][RM] from z, and db.
-template <int RM, int B> __global__ void __launch_bounds__(256) few_logit_gradient_kernel(const __grid_constant__ Layer a) {
+template <int RM, int B> __global__ void __launch_bounds__(32 * kMostWarps) few_logit_gradient_kernel(const __grid_constant__ Layer a) {
   extern __shared__ float xs[];
   behind_previous();
   const Slots s{a.in, a.aligned != 0};
@@ -253,11 +254,14 @@ int classes_at_once(const vgg19_linear_loss& a, int sms) {
   const int b = many(few_rows_up((int)a.rows));
   return a.classes < sms * 8 * b ? 2 : b;
 }
-// Warps of a block: every SM has one before a block has several, unless the rows that a block keeps are many bytes.
+// Warps of a block: every SM has one before a block has several, unless the rows that a block keeps are many bytes; where an SM has room for one
+// block's rows alone, that has sixteen.
+int kept_values(const vgg19_linear_loss& a) { return few_rows_up((int)a.rows) * a.in; }
 int warps_of(const vgg19_linear_loss& a, int sms) {
   const int b = classes_at_once(a, sms);
   int warps = 8;
-  if (few_rows_up((int)a.rows) * a.in > 2048) return warps;
+  if (kept_values(a) > 12288) return (a.classes + 8 * b - 1) / (8 * b) > sms ? kMostWarps : warps;
+  if (kept_values(a) > 2048) return warps;
   while (warps > 1 && (a.classes + b * warps - 1) / (b * warps) < sms) warps /= 2;
   return warps;
 }
@@ -300,7 +304,8 @@ bool few_rows(const vgg19_linear_loss& a) { return a.dtype == VGG19_FP32 && a.ro
 
 int few_rows_blocks(const vgg19_linear_loss& a, int sms) {
   const int per = classes_at_once(a, sms) * warps_of(a, sms), batches = (a.classes + per - 1) / per;
-  return batches < 2 * sms ? batches : 2 * sms;
+  const int most = kept_values(a) > 24576 ? sms : 2 * sms;  // (one block's rows are all that an SM has room for, or two blocks' are not)
+  return batches < most ? batches : most;
 }
 
 // Ranges of classes: enough blocks for every SM to have sixteen warps, of at least eight classes each.
