@@ -121,7 +121,8 @@ def test_a_few_rows(p, rows, inner, classes, pad, skip, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("rows,inner,classes,pad,skip,out_pad", [(40, 64, 300, 8, 0, 0), (40, 64, 300, 3, 0, 1), (40, 64, 300, 7, 1, 8), (70, 333, 130, 5, 0, 3), (1, 64, 40, 9, 1, 5)])
+@pytest.mark.parametrize("rows,inner,classes,pad,skip,out_pad", [(40, 64, 300, 8, 0, 0), (40, 64, 300, 3, 0, 1), (40, 64, 300, 7, 1, 8), (70, 333, 130, 5, 0, 3), (1, 64, 40, 9, 1, 5),
+                                                                   (6, 332, 1300, 0, 0, 0), (6, 332, 1300, 4, 0, 4), (6, 332, 1300, 3, 1, 3), (2, 332, 1300, 4, 4, 1)])
 def test_rows_of_wider_buffers(p, rows, inner, classes, pad, skip, out_pad, dtype):
     c = Case(rows, inner, classes, dtype, pad=pad, skip=skip).run(p, out_pad=out_pad)
     c.check()
