@@ -901,8 +901,9 @@ struct Plan {
   Shape dx_shape, dw_shape;  // (pairs both, or none)
   int dx_splits;          // parts of dx's sum within a piece
   bool dx_parts;          // whether dx is added up in fp32 outside the products
+  int dw_splits;          // the same of dw's, with all classes in one piece
   long dx_ld;
-  size_t x, w, z, part, label_z, dz, db_part, dx, total;
+  size_t x, w, z, part, label_z, dz, db_part, dx, dw, total;
 };
 
 int pairs_of_device() {
@@ -936,6 +937,8 @@ constexpr double kMeeting = 0.7;  // what a pair's beginning and end take beyond
 // What parts of a sum cost beyond the products: another kernel, and each value written and read.
 double parts_time(double values, int parts) { return parts > 1 ? 2.5 + 8.0 * values * parts / 6e6 : 0; }
 
+constexpr double kOtherSum = 4;  // and what they cost dw besides, whose parts are added up behind dx's
+
 // z's tiles and into how many parts its sum is cut: what takes the least time.
 void plan_logits(long m, long n, long blocks, int planes, int pairs, bool parts, Shape* shape, int* splits) {
   double least = -1;
@@ -950,20 +953,26 @@ void plan_logits(long m, long n, long blocks, int planes, int pairs, bool parts,
     }
   }
 }
-// The same for dx [rows][in] over the classes of a piece and dw [classes][in] over the rows, which share a launch.
-void plan_gradients(long rows, long in, long classes, int planes, int pairs, Shape* dx, int* dx_splits, Shape* dw) {
+// The same for dx [rows][in] over the classes of a piece and dw [classes][in] over the rows, which share a launch.  dw's sum is cut too where its tiles are
+// few and many rows long (`parts`: may be), into a power of two parts of at least four K blocks each.  Measured (all gradients, bf16 and
+// fp32; whole sums behind): 4037 rows of 35 values against 48 classes 23 and 31 us (36 and 96), 16384 of 256 against 257 56 and 106 us (89 and 342), 8192 of 1024
+// against 1000 81 and 271 us (104 and 440); 4096 of 4096 against 10 53 and 179 us (50 and 206).
+void plan_gradients(long rows, long in, long classes, int planes, int pairs, bool parts, Plan* p) {
   const long class_blocks = (classes + BK - 1) / BK, row_blocks = (rows + BK - 1) / BK;
   double least = -1;
   for (const Shape& b : kShapes)
     for (const Shape& c : kShapes) {
       if (b.pair != c.pair || b.bn == 192 || c.bn == 192 || !possible(b, planes) || !possible(c, planes)) continue;
-      const long workers = workers_of(b, pairs);
-      for (int s = 1; s <= 64 && s <= class_blocks && (s == 1 || s * tiles_of(rows, in, b) <= workers); ++s) {
-        const double x = tile_time(b, (class_blocks + s - 1) / s, planes, true), w = tile_time(c, row_blocks, planes, true);
-        const double all = (s * tiles_of(rows, in, b) * x + tiles_of(classes, in, c) * w) / workers + (x < w ? x : w) / 2;
-        const double longest = x > w ? x : w;
-        const double t = (all > longest ? all : longest) + 0.1 * longest + parts_time((double)rows * in, s) + (b.pair ? kMeeting : 0);  // (the shorter the longest, the evener the end)
-        if (least < 0 || t < least) { least = t; *dx = b; *dx_splits = s; *dw = c; }
+      const long workers = workers_of(b, pairs), dx_tiles = tiles_of(rows, in, b), dw_tiles = tiles_of(classes, in, c);
+      for (int t = 1; t == 1 || (parts && t <= 64 && 4 * t <= row_blocks && t * dw_tiles <= workers); t *= 2) {
+        const double w = tile_time(c, (row_blocks + t - 1) / t, planes, true), w_sum = t > 1 ? kOtherSum + parts_time((double)classes * in, t) : 0;
+        for (int s = 1; s <= 64 && s <= class_blocks && (s == 1 || s * dx_tiles <= workers); ++s) {
+          const double x = tile_time(b, (class_blocks + s - 1) / s, planes, true);
+          const double all = (s * dx_tiles * x + t * dw_tiles * w) / workers + (x < w ? x : w) / 2;
+          const double longest = x > w ? x : w;
+          const double time = (all > longest ? all : longest) + 0.1 * longest + parts_time((double)rows * in, s) + w_sum + (b.pair ? kMeeting : 0);  // (the shorter the longest, the evener the end)
+          if (least < 0 || time < least) { least = time; p->dx_shape = b; p->dx_splits = s; p->dw_shape = c; p->dw_splits = t; }
+        }
       }
     }
 }
@@ -1019,10 +1028,11 @@ Plan make_plan(const vgg19_linear_loss& a, bool backward, int pairs, const bool*
   } else {
     p.dz = take((size_t)p.planes * a.rows * p.piece * 2);
     p.db_part = take((size_t)(up(a.rows, p.db_rows) / p.db_rows) * p.piece * 4);
-    plan_gradients(a.rows, a.in, piece_classes, p.planes, pairs, &p.dx_shape, &p.dx_splits, &p.dw_shape);
+    plan_gradients(a.rows, a.in, piece_classes, p.planes, pairs, p.pieces == 1, &p);
     p.dx_parts = p.pieces > 1 || p.dx_splits > 1;
     p.dx_ld = up(a.in, 4);
     if (p.dx_parts) p.dx = take((size_t)p.dx_splits * a.rows * p.dx_ld * 4);
+    if (p.dw_splits > 1) p.dw = take((size_t)p.dw_splits * a.classes * p.dx_ld * 4);
   }
   p.total = at < 256 ? 256 : at;
   return p;
@@ -1164,16 +1174,16 @@ struct Gradients {
   float* db;
 };
 
-// dx from its parts.
-template <typename T, int GROUPS>
-cudaError_t sum_dx(const vgg19_linear_loss& a, const Gradients& g, char* ws, const Plan& p, int parts, cudaStream_t st) {
-  const long chunks = a.rows * (p.dx_ld / 4), blocks = (chunks * GROUPS + 255) / 256;
-  return launch_behind(sum_parts_kernel<T, GROUPS>, (unsigned)(blocks < 148 * 16 ? blocks : 148 * 16), 256, 0, st, reinterpret_cast<const float*>(ws + p.dx), parts,
-                       (long)a.rows, (int)a.in, p.dx_ld, static_cast<T*>(g.dx), g.dx_ld);
+// dx or dw from the parts of its sum.
+template <typename T>
+cudaError_t sum_parts(const char* part, int parts, long rows, const vgg19_linear_loss& a, const Plan& p, void* out, long out_ld, cudaStream_t st) {
+  const bool many = parts > 16;
+  const long threads = rows * (p.dx_ld / 4) * (many ? 8 : 1), blocks = (threads + 255) / 256;
+  return launch_behind(many ? sum_parts_kernel<T, 8> : sum_parts_kernel<T, 1>, (unsigned)(blocks < 148 * 16 ? blocks : 148 * 16), 256, 0, st,
+                       reinterpret_cast<const float*>(part), parts, rows, (int)a.in, p.dx_ld, static_cast<T*>(out), out_ld);
 }
 cudaError_t sum_dx(const vgg19_linear_loss& a, const Gradients& g, char* ws, const Plan& p, int parts, cudaStream_t st) {
-  if (a.dtype == VGG19_FP32) return parts > 16 ? sum_dx<float, 8>(a, g, ws, p, parts, st) : sum_dx<float, 1>(a, g, ws, p, parts, st);
-  return parts > 16 ? sum_dx<bf16, 8>(a, g, ws, p, parts, st) : sum_dx<bf16, 1>(a, g, ws, p, parts, st);
+  return a.dtype == VGG19_FP32 ? sum_parts<float>(ws + p.dx, parts, a.rows, a, p, g.dx, g.dx_ld, st) : sum_parts<bf16>(ws + p.dx, parts, a.rows, a, p, g.dx, g.dx_ld, st);
 }
 
 template <int P>
@@ -1234,10 +1244,17 @@ cudaError_t backward(const vgg19_linear_loss& a, const Gradients& g, char* ws, c
       j.a = dz; j.a_mn = 1; j.b = o.x; j.b_mn = 1;
       j.group = 4;  // whole rows of dw at a time (sixteen: 2 % slower)
       j.m = (int)n; j.n = a.in; j.k_blocks = (int)((a.rows + BK - 1) / BK); j.bn = p.dw_shape.bn;
-      j.f32 = f32 || g.dw_f32;
-      const long elt = j.f32 ? 4 : 2;
-      j.out = static_cast<char*>(g.dw) + first * g.dw_ld * elt; j.ld = g.dw_ld;
-      j.store = copyable(j.out, n, g.dw_ld, elt) ? kWhole : kSingle;
+      if (p.dw_splits > 1) {
+        j.splits = p.dw_splits;
+        j.f32 = 1;
+        j.out = ws + p.dw; j.ld = p.dx_ld;
+        j.store = kWhole;
+      } else {
+        j.f32 = f32 || g.dw_f32;
+        const long elt = j.f32 ? 4 : 2;
+        j.out = static_cast<char*>(g.dw) + first * g.dw_ld * elt; j.ld = g.dw_ld;
+        j.store = copyable(j.out, n, g.dw_ld, elt) ? kWhole : kSingle;
+      }
       j.db_part = db_part; j.db = g.db ? g.db + first : nullptr;
       j.parts = (int)((a.rows + p.db_rows - 1) / p.db_rows);
     }
@@ -1245,8 +1262,12 @@ cudaError_t backward(const vgg19_linear_loss& a, const Gradients& g, char* ws, c
     if (!g.dw && g.db && e == cudaSuccess)
       e = launch_behind(sum_columns_kernel, (unsigned)((n + 31) / 32), 256, 0, st, static_cast<const float*>(db_part), (int)((a.rows + p.db_rows - 1) / p.db_rows), (int)n, g.db + first);
   }
-  if (e != cudaSuccess || !g.dx || !p.dx_parts) return e;
-  return sum_dx(a, g, ws, p, slots, st);
+  if (e == cudaSuccess && g.dx && p.dx_parts) e = sum_dx(a, g, ws, p, slots, st);
+  if (e == cudaSuccess && g.dw && p.dw_splits > 1) {
+    const int blocks = (int)((a.rows + BK - 1) / BK), per = (blocks + p.dw_splits - 1) / p.dw_splits, parts = (blocks + per - 1) / per;
+    e = P == 3 || g.dw_f32 ? sum_parts<float>(ws + p.dw, parts, a.classes, a, p, g.dw, g.dw_ld, st) : sum_parts<bf16>(ws + p.dw, parts, a.classes, a, p, g.dw, g.dw_ld, st);
+  }
+  return e;
 }
 
 cudaError_t backward_few(const vgg19_linear_loss& a, const Gradients& g, char* ws, const Plan& p, int pairs, cudaStream_t st) {

@@ -312,6 +312,17 @@ def test_tiles_of_every_shape(p, rows, inner, classes, dtype):
     Case(rows, inner, classes, dtype, seed=7).run(p).check()
 
 
+@pytest.mark.parametrize("dtype,dw_dtype", [("bf16", None), ("bf16", torch.float32), ("fp32", None)])
+@pytest.mark.parametrize("rows,inner,classes,pad", [(4037, 35, 48, 0), (3000, 130, 10, 3), (4096, 1000, 70, 0), (513, 8, 1, 0), (2500, 333, 300, 1), (16384, 129, 257, 0)])
+def test_many_rows_against_few_classes(p, rows, inner, classes, pad, dtype, dw_dtype):
+    """dw has few tiles, each a long sum, which is cut into parts; alone it is what it is among the others."""
+    c = Case(rows, inner, classes, dtype, seed=classes, pad=pad).run(p, dw_dtype=dw_dtype, out_pad=pad)
+    c.check()
+    dw, ws = torch.full_like(c.dw, math.nan), torch.empty(p.vgg19_linear_cross_entropy_bytes(c.x, c.w, True), dtype=torch.uint8, device=DEV)
+    p.vgg19_linear_cross_entropy_backward(c.x, c.w, c.bias, c.labels, c.lse, c.d_loss, None, dw, None, ws, torch.cuda.current_stream())
+    assert torch.equal(dw, c.dw)
+
+
 @pytest.mark.parametrize("rows,inner,classes,dtype", [(100, 264, 1000, "bf16"), (4, 264, 1000, "fp32"), (300, 333, 2049, "bf16"), (200, 64, 500, "fp32")])
 def test_recorded_and_replayed_with_other_inputs(p, rows, inner, classes, dtype):
     c = Case(rows, inner, classes, dtype)
