@@ -256,6 +256,7 @@ int classes_at_once(const vgg19_linear_loss& a, int sms) {
 }
 // Warps of a block: every SM has one before a block has several, unless the rows that a block keeps are many bytes; where an SM has room for one
 // block's rows alone, that has sixteen.
+constexpr int kMostKept = 32768;  // values (rounded up to 128 a row, which divides it for any number of rows)
 int kept_values(const vgg19_linear_loss& a) { return few_rows_up((int)a.rows) * a.in; }
 int warps_of(const vgg19_linear_loss& a, int sms) {
   const int b = classes_at_once(a, sms);
@@ -278,7 +279,7 @@ Layer layer_of(const vgg19_linear_loss& a) {
 
 template <typename K> cudaError_t launch_logits(K kernel, const Layer& l, int rm, int blocks, int warps, cudaStream_t st) {
   const int smem = rm * l.warps_slots * 32 * kV * 4;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostKept * 4);  // (the same for all: calls may be made from several threads)
   return e == cudaSuccess ? launch_behind(kernel, (unsigned)blocks, 32 * warps, smem, st, l) : e;
 }
 template <int RM> cudaError_t loss_of(const Layer& l, int b, int blocks, int warps, cudaStream_t st) {
@@ -300,7 +301,7 @@ cudaError_t few_rows_take_error(int* label, cudaStream_t st) {
   return e == cudaSuccess ? take_error(static_cast<int*>(word), label, st) : e;
 }
 
-bool few_rows(const vgg19_linear_loss& a) { return a.dtype == VGG19_FP32 && a.rows <= 8 && a.in <= 32768 / few_rows_up((int)a.rows); }
+bool few_rows(const vgg19_linear_loss& a) { return a.dtype == VGG19_FP32 && a.rows <= 8 && a.in <= kMostKept / few_rows_up((int)a.rows); }
 
 int few_rows_blocks(const vgg19_linear_loss& a, int sms) {
   const int per = classes_at_once(a, sms) * warps_of(a, sms), batches = (a.classes + per - 1) / per;

@@ -409,3 +409,31 @@ def test_offsets_beyond_32_bits(p, rows, inner, classes, dtype):
     last.loss, last.lse, last.dx, last.dw, last.db = c.loss[-20:], c.lse[-20:], c.dx[-20:], c.dw[-32:], c.db[-32:]
     last.check()
     assert not c.dx[:-20].any() and not c.dw[:-32].any()
+
+
+def test_from_several_threads(p):
+    """Calls of other sizes from two threads, each with its stream and workspaces: the results of the same calls one after another."""
+    import threading
+    cases = [[Case(rows, inner, classes, dtype, seed=7) for rows, inner, classes, dtype in sizes] for sizes in (
+        [(8, 4096, 300, "fp32"), (1, 8000, 40, "fp32"), (100, 264, 1000, "bf16")], [(8, 33, 300, "fp32"), (1, 100, 40, "fp32"), (300, 72, 500, "fp32")])]
+    want = [[[getattr(c.run(p), n).clone() for n in ("loss", "lse", "dx", "dw", "db")] for c in of] for of in cases]
+    torch.cuda.synchronize()
+    failed = []
+    def work(of, wanted):
+        try:
+            st = torch.cuda.Stream()
+            with torch.cuda.stream(st):
+                for _ in range(20):
+                    for c, w in zip(of, wanted):
+                        c.run(p, st, check=False)
+                        st.synchronize()
+                        if not all(torch.equal(getattr(c, n), t) for n, t in zip(("loss", "lse", "dx", "dw", "db"), w)):
+                            failed.append((c.rows, c.inner))
+        except Exception as e:  # (told by the assertion below)
+            failed.append(e)
+    threads = [threading.Thread(target=work, args=a) for a in zip(cases, want)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
