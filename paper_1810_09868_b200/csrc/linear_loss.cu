@@ -368,35 +368,39 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
     int ji = 0;
     uint32_t count = 0;
     bool ok = true;
+    // What a tile of z needs of its rows and columns: requested while the tile before is worked on.
+    constexpr bool LOGITS = EPI == kStatistics || EPI == kLogitGradient;
+    struct {
+      int i, j, label;
+      float lse, d_loss, bias[4];
+    } next;
+    auto request = [&](int w) {
+      if (w >= total) return;
+      const Job& p = L.job[0];
+      const Tile tile = find_tile(p, w);
+      const int half = p.bn / 2, row = tile.i * kTileRows<PAIR> + (int)rank * BM + quarter * 32 + lane, j0 = tile.j * p.bn + group * half, cols = min(p.n - j0, half);
+      next.i = tile.i; next.j = tile.j;
+      next.label = VGG19_NO_CLASS;
+      next.lse = next.d_loss = 0.f;
+      if (row < p.m) {
+        next.label = L.rows.labels[row];
+        if (EPI == kLogitGradient) { next.lse = L.rows.lse[row]; next.d_loss = L.rows.d_loss[row]; }
+      }
+      // columns beyond the classes get the bias of an excluded class
+#pragma unroll
+      for (int k = 0; k < 4; ++k) next.bias[k] = 32 * k + lane < cols ? L.rows.bias ? __ldg(L.rows.bias + j0 + 32 * k + lane) : 0.f : -INFINITY;
+    };
+    if (LOGITS) request(turn(0, worker, workers));
     for (int round = 0, w; ok && (w = turn(round, worker, workers)) < total; ++round) {
-      while (w >= L.first_tile[ji + 1]) ++ji;
+      if (!LOGITS) while (w >= L.first_tile[ji + 1]) ++ji;
       const Job& p = L.job[ji];
-      const Tile tile = find_tile(p, w - L.first_tile[ji]);
+      Tile tile{};
+      if (LOGITS) { tile.i = next.i; tile.j = next.j; tile.k1 = p.k_blocks; }
+      else tile = find_tile(p, w - L.first_tile[ji]);
       const int half = p.bn / 2;
       const int i0 = tile.i * kTileRows<PAIR> + (int)rank * BM + quarter * 32, j0 = tile.j * p.bn + group * half;  // the warp's first row and column
       const int rows = p.m - i0, cols = min(p.n - j0, half);                                         // what there is from there on
       const int row = i0 + lane;
-      // what a row needs, requested while the products run
-      float lse = 0.f, d_loss = 0.f, next_bias = 0.f;
-      int label = VGG19_NO_CLASS;
-      // columns beyond the classes get the bias of an excluded class
-      auto bias_of = [&](int c) { return c < cols ? L.rows.bias ? __ldg(L.rows.bias + j0 + c) : 0.f : -INFINITY; };
-      if (EPI == kStatistics || EPI == kLogitGradient) {
-        if (lane < rows) {
-          label = L.rows.labels[row];
-          if (EPI == kLogitGradient) { lse = L.rows.lse[row]; d_loss = L.rows.d_loss[row]; }
-        }
-        const bool real = (unsigned)label < (unsigned)L.rows.all_classes;
-        if (EPI == kLogitGradient) {
-          if (!real && label != VGG19_NO_CLASS && j0 == 0) atomicCAS(g_label_error, 0, (int)kDevBadLabel);
-          // no label, or no class left: no gradient
-          if (!real || lse == -INFINITY) d_loss = 0.f;
-          label = d_loss != 0.f || d_loss != d_loss ? label - L.rows.first_class : -1;
-        } else {
-          label = real ? label - L.rows.first_class : -1;
-        }
-        next_bias = bias_of(lane);
-      }
       if (EPI == kProduct && p.db && tile.j == 0 && group == 0 && tile.split == 0 && lane < rows) {
         float s[8] = {};  // (as sum_columns_kernel adds them)
         for (int q = 0; q < p.parts; q += 8) {
@@ -514,10 +518,26 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
           sums_are_read();
         }
         if (!ok) break;
+        float lse = 0.f, d_loss = 0.f, bias[4];
+        int label = VGG19_NO_CLASS;
+        if (LOGITS) {
+          label = next.label; lse = next.lse; d_loss = next.d_loss;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) bias[k] = next.bias[k];
+          request(turn(round + 1, worker, workers));
+          const bool real = (unsigned)label < (unsigned)L.rows.all_classes;
+          if (EPI == kLogitGradient) {
+            if (!real && label != VGG19_NO_CLASS && j0 == 0) atomicCAS(g_label_error, 0, (int)kDevBadLabel);
+            // no label, or no class left: no gradient
+            if (!real || lse == -INFINITY) d_loss = 0.f;
+            label = d_loss != 0.f || d_loss != d_loss ? label - L.rows.first_class : -1;
+          } else {
+            label = real ? label - L.rows.first_class : -1;
+          }
+        }
         auto add_bias = [&](int c) {
-          bias_s[lane] = next_bias;
+          bias_s[lane] = bias[c / 32];
           __syncwarp();
-          if (c + 32 < 128) next_bias = bias_of(c + 32 + lane);
 #pragma unroll
           for (int q = 0; q < 8; ++q) {
             const float4 b = reinterpret_cast<const float4*>(bias_s)[q];
@@ -527,13 +547,13 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
         };
 
         if (EPI == kStatistics) {
-          float most = -INFINITY, sum = 0.f;
+          float four[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, sum = 0.f;
 #pragma unroll
           for (int c = 0; c < 128; c += 32) {
             if (c >= half) break;
             add_bias(c);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) most = fmaxf(most, v[c + j]);
+            for (int j = 0; j < 32; ++j) four[j % 4] = fmaxf(four[j % 4], v[c + j]);
             const int at = label - j0 - c;  // the label's column among these
             if (__any_sync(0xffffffffu, (unsigned)at < 32u)) {
               float z = 0.f;
@@ -542,14 +562,14 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
               if ((unsigned)at < 32u && at < cols - c) L.rows.label_z[row] = z;
             }
           }
-          const float ref = most == -INFINITY ? 0.f : most;
+          const float most = fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3])), ref = most == -INFINITY ? 0.f : most;
 #pragma unroll
           for (int c = 0; c < 128; c += 32) {
             if (c >= half) break;
-            float part = 0.f;
+            float part[4] = {};
 #pragma unroll
-            for (int j = 0; j < 32; ++j) part += fast_exp2((v[c + j] - ref) * kLossLog2e);
-            sum += part;
+            for (int j = 0; j < 32; ++j) part[j % 4] += fast_exp2((v[c + j] - ref) * kLossLog2e);
+            sum += part[0] + part[1] + (part[2] + part[3]);
           }
           if (lane < rows && cols > 0) L.rows.part[(long)(L.rows.first_part + 2 * tile.j + group) * p.m + row] = make_float2(most, sum);
         } else if (EPI == kLogitGradient) {
