@@ -20,7 +20,7 @@
 // decided by measured times of tiles (plan_logits, plan_gradients).
 //
 // fp32: a value is three bf16 planes (24 bits), a product six products of planes, those down to 2^-16 of the first; the five lesser ones
-// have an accumulator of their own.  Up to eight rows go another way (linear_loss_few.cu).
+// have an accumulator of their own.  A few rows go another way (linear_loss_few.cu).
 //
 // Precision.  The tensor core truncates its fp32 sums, so a chain ends after 16 K blocks (8 with three planes) and the epilogue adds the
 // chains in registers: the loss of rows of 4096 is 3e-7 from 64 bits, 1.9e-6 with one chain.  dz is fp32 until it is rounded to bf16 for the
@@ -1003,7 +1003,7 @@ Plan make_plan(const vgg19_linear_loss& a, bool backward, int pairs, const bool*
   const bool f32 = a.dtype == VGG19_FP32;
   size_t at = 0;
   auto take = [&at](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
-  if (!in_pairs && few_rows(a)) {
+  if (!in_pairs && few_rows(a, backward)) {
     p.few = backward ? few_rows_ranges(a, 2 * pairs) : few_rows_blocks(a, 2 * pairs);
     p.dx_ld = up(a.in, 4);
     if (backward) {

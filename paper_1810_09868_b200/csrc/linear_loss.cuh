@@ -50,8 +50,8 @@ cudaError_t launch_behind(void (*kernel)(A...), dim3 blocks, int threads, int sm
 
 // ---- a few rows of fp32 (linear_loss_few.cu) ------------------------------------------------------------------------------
 constexpr int few_rows_up(int rows) { return rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8; }
-// Whether a layer is taken this way; the blocks of which each leaves statistics of its own, and the ranges of classes that dx is added up from.
-bool few_rows(const vgg19_linear_loss& a);
+// Whether a layer is taken this way, for its loss or (backward) its gradients; the blocks of which each leaves statistics of its own, and the ranges of classes that dx is added up from.
+bool few_rows(const vgg19_linear_loss& a, bool backward);
 int few_rows_blocks(const vgg19_linear_loss& a, int sms);
 int few_rows_ranges(const vgg19_linear_loss& a, int sms);
 // (largest, sum) of a block's logits at part[block * rows + r]; z at the label.

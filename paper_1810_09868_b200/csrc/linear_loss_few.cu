@@ -1,4 +1,4 @@
-// The last dense layer with its loss for up to eight rows of fp32, on the CUDA cores (formulas in linear_loss.cu).  So few rows are
+// The last dense layer with its loss for up to eight rows of fp32, the loss alone for up to 24, on the CUDA cores (formulas in linear_loss.cu).  So few rows are
 // bound by reading w, and writing dw; the tensor cores would have it written down as three bf16 planes first, half as much again as w itself, and
 // read again from there.  (bf16 weights need no planes: there the tiles are as fast or faster.)  Forward, w is read once: a warp takes a few
 // classes, its lanes along the inputs, with the rows of x in shared memory.  Backward it is read twice: for z, which becomes dz [classes][rows],
@@ -6,7 +6,10 @@
 //
 // Measured (B200, device time; the planes' way behind): 4096 inputs against 50021 classes, one row 142 us and 416 us for the gradients (781 and 1396),
 // eight rows 221 and 624 (778 and 1303); against 1000 classes, one row 13 and 19 (21 and 41), eight 23 and 34 (20 and 41).  One row reads w at 5.8 TB/s (0.9 of a
-// copy's rate); eight rows read x twice from shared memory for every value of w, with one block of sixteen warps an SM (eight warps: 321 us).
+// copy's rate); eight rows read x twice from shared memory for every value of w, with one block of sixteen warps an SM (eight warps: 321 us).  More rows are
+// groups of eight, each with a share of the SMs, that read w beside one another, mostly from L2: 9 to 16 rows 382 us (775), 17 to 24 537 (782).
+// (Gradients of groups: dx and dw of sixteen rows want 180 registers a thread and are bound by their loads, 1230 us for all where the planes take 1310, but 124
+// against 106 for 16 rows of 1024 against 16000 classes and 440 against 400 for 512 against 131072: left to the planes.)
 #include <cuda_runtime.h>
 
 #include "../../include/vgg19_b200.h"
@@ -110,11 +113,12 @@ template <int RM, int B> __global__ void __launch_bounds__(32 * kMostWarps) few_
   behind_previous();
   const Slots s{a.in, a.aligned != 0};
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x / 32;
-  stage_rows<RM>(xs, a.x, a.ldx, a.rows, s, a.warps_slots, a.x_aligned != 0);
+  const int row0 = blockIdx.y * RM, rows = min(RM, a.rows - row0);
+  stage_rows<RM>(xs, a.x + row0 * a.ldx, a.ldx, rows, s, a.warps_slots, a.x_aligned != 0);
   __syncthreads();
   constexpr int N = B * RM;
   const int r = lane % N % RM, b = lane % N / RM;
-  const int label = r < a.rows ? a.labels[r] : VGG19_NO_CLASS;
+  const int label = r < rows ? a.labels[row0 + r] : VGG19_NO_CLASS;
   float2 most = make_float2(-INFINITY, 0.f);
   for (int n0 = (blockIdx.x * warps + warp) * B; n0 < a.classes; n0 += gridDim.x * warps * B) {
     float acc[N];
@@ -123,7 +127,7 @@ template <int RM, int B> __global__ void __launch_bounds__(32 * kMostWarps) few_
     const int n = n0 + b;
     if (lane < N && n < a.classes) {
       const float z = sum + (a.bias ? __ldg(a.bias + n) : 0.f);
-      if (n == label) a.label_z[r] = z;
+      if (n == label) a.label_z[row0 + r] = z;
       most = join(most, z != z ? make_float2(-INFINITY, z) : make_float2(z, z == -INFINITY ? 0.f : 1.f));
     }
   }
@@ -134,10 +138,10 @@ template <int RM, int B> __global__ void __launch_bounds__(32 * kMostWarps) few_
   }
   if (lane < RM) got[warp][lane] = most;
   __syncthreads();
-  if (threadIdx.x >= a.rows) return;
+  if (threadIdx.x >= rows) return;
   most = got[0][threadIdx.x];
   for (int k = 1; k < warps; ++k) most = join(most, got[k][threadIdx.x]);
-  a.part[(long)blockIdx.x * a.rows + threadIdx.x] = most;
+  a.part[(long)blockIdx.x * a.rows + row0 + threadIdx.x] = most;
 }
 
 // dz [classes][RM] from z, and db.
@@ -209,7 +213,15 @@ template <int RM> __global__ void __launch_bounds__(kProductThreads) few_product
       if (n >= end) break;
       float e[RM];
 #pragma unroll
-      for (int r = 0; r < RM; ++r) e[r] = __ldg(a.g.dz + (long)n * RM + r);
+      for (int r = 0; r < RM; r += RM < 4 ? 1 : 4) {
+        const float* at = a.g.dz + (long)n * RM + r;
+        if (RM < 4) {
+          e[r] = __ldg(at);
+        } else {
+          const float4 v = __ldg(reinterpret_cast<const float4*>(at));
+          e[r] = v.x; e[(r + 1) % RM] = v.y; e[(r + 2) % RM] = v.z; e[(r + 3) % RM] = v.w;
+        }
+      }
       if (a.g.dx_part) {
 #pragma unroll
         for (int r = 0; r < RM; ++r) {
@@ -248,18 +260,22 @@ template <int RM> __global__ void __launch_bounds__(kProductThreads) few_product
     }
 }
 
+// Rows of a group, rounded up to what there are kernels for, and groups.
+int group_up(const vgg19_linear_loss& a) { return few_rows_up((int)a.rows); }
+int groups(const vgg19_linear_loss& a) { return (int)(a.rows + 7) / 8; }
 // Classes that a warp takes at once: eight (four of eight rows: 32 sums), or two where more would leave SMs without a warp.
 constexpr int many(int rm) { return rm == 8 ? 4 : 8; }
 int classes_at_once(const vgg19_linear_loss& a, int sms) {
-  const int b = many(few_rows_up((int)a.rows));
-  return a.classes < sms * 8 * b ? 2 : b;
+  const int b = many(group_up(a));
+  return a.classes < sms / groups(a) * 8 * b ? 2 : b;
 }
 // Warps of a block: every SM has one before a block has several, unless the rows that a block keeps are many bytes; where an SM has room for one
 // block's rows alone, that has sixteen.
 constexpr int kMostKept = 32768;  // values (rounded up to 128 a row, which divides it for any number of rows)
-int kept_values(const vgg19_linear_loss& a) { return few_rows_up((int)a.rows) * a.in; }
+int kept_values(const vgg19_linear_loss& a) { return group_up(a) * a.in; }
 int warps_of(const vgg19_linear_loss& a, int sms) {
   const int b = classes_at_once(a, sms);
+  sms /= groups(a);
   int warps = 8;
   if (kept_values(a) > 12288) return (a.classes + 8 * b - 1) / (8 * b) > sms ? kMostWarps : warps;
   if (kept_values(a) > 2048) return warps;
@@ -278,9 +294,10 @@ Layer layer_of(const vgg19_linear_loss& a) {
 }
 
 template <typename K> cudaError_t launch_logits(K kernel, const Layer& l, int rm, int blocks, int warps, cudaStream_t st) {
+  const dim3 grid((unsigned)blocks, (unsigned)((l.rows + rm - 1) / rm));
   const int smem = rm * l.warps_slots * 32 * kV * 4;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostKept * 4);  // (the same for all: calls may be made from several threads)
-  return e == cudaSuccess ? launch_behind(kernel, (unsigned)blocks, 32 * warps, smem, st, l) : e;
+  return e == cudaSuccess ? launch_behind(kernel, grid, 32 * warps, smem, st, l) : e;
 }
 template <int RM> cudaError_t loss_of(const Layer& l, int b, int blocks, int warps, cudaStream_t st) {
   return b == 2 ? launch_logits(few_loss_kernel<RM, 2>, l, RM, blocks, warps, st) : launch_logits(few_loss_kernel<RM, many(RM)>, l, RM, blocks, warps, st);
@@ -301,11 +318,16 @@ cudaError_t few_rows_take_error(int* label, cudaStream_t st) {
   return e == cudaSuccess ? take_error(static_cast<int*>(word), label, st) : e;
 }
 
-bool few_rows(const vgg19_linear_loss& a) { return a.dtype == VGG19_FP32 && a.rows <= 8 && a.in <= kMostKept / few_rows_up((int)a.rows); }
+bool few_rows(const vgg19_linear_loss& a, bool backward) {
+  if (a.dtype != VGG19_FP32 || a.rows > (backward ? 8 : 24) || a.in > kMostKept / group_up(a)) return false;
+  // Groups of eight: where a block's classes are worth the rows of x that it keeps (against 1000 classes of 4096 they take 23 us, the planes 20; of 2048 14.7
+  // and 16), and w's rows are worth reading for every group (64 inputs against 131072: 61 and 41 us; three groups of 300 against 100003: 129 and 118).
+  return a.rows <= 8 || (a.in >= (a.rows <= 16 ? 256 : 512) && a.classes >= a.in / 3);
+}
 
 int few_rows_blocks(const vgg19_linear_loss& a, int sms) {
   const int per = classes_at_once(a, sms) * warps_of(a, sms), batches = (a.classes + per - 1) / per;
-  const int most = kept_values(a) > 24576 ? sms : 2 * sms;  // (one block's rows are all that an SM has room for, or two blocks' are not)
+  const int most = (kept_values(a) > 24576 ? 1 : 2) * (sms / groups(a));  // (one block's rows are all that an SM has room for, or two blocks' are not)
   return batches < most ? batches : most;
 }
 
@@ -322,7 +344,7 @@ cudaError_t few_rows_loss(const vgg19_linear_loss& a, float2* part, float* label
   Layer l = layer_of(a);
   l.part = part; l.label_z = label_z;
   const int b = classes_at_once(a, sms), blocks = few_rows_blocks(a, sms), warps = warps_of(a, sms);
-  switch (few_rows_up(l.rows)) {
+  switch (group_up(a)) {
     case 1: return loss_of<1>(l, b, blocks, warps, st);
     case 2: return loss_of<2>(l, b, blocks, warps, st);
     case 4: return loss_of<4>(l, b, blocks, warps, st);

@@ -112,11 +112,11 @@ def test_against_the_formulas(p, rows, inner, classes, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 7, 8, 9])
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 7, 8, 9, 16, 23, 25])
 @pytest.mark.parametrize("inner,classes,pad,skip", [(1, 5, 0, 0), (255, 100, 0, 0), (264, 1000, 0, 0), (4096, 300, 0, 0), (4097, 33, 3, 0), (8192, 90, 0, 0), (8200, 17, 0, 0), (100, 20011, 4, 0), (333, 2049, 3, 1),
                                                     (64, 9500, 8, 0)])
 def test_a_few_rows(p, rows, inner, classes, pad, skip, dtype):
-    """Up to eight rows have kernels of their own, up to 8192 inputs (eight rows: 4096)."""
+    """Up to eight rows, and up to 24 for the loss alone, have kernels of their own, up to 32768 / rows inputs."""
     Case(rows, inner, classes, dtype, seed=rows, pad=pad, skip=skip).run(p, dw_dtype=torch.float32 if classes == 33 else None).check()
 
 
