@@ -1373,6 +1373,7 @@ int linear_loss(const vgg19_linear_loss* layer, float* loss, float* lse, void* w
 extern "C" size_t vgg19_linear_cross_entropy_bytes(const vgg19_linear_loss* layer, int32_t backward) {
   using namespace vgg;
   if (check(layer) != VGG19_OK) return 0;
+  if (layer->rows == 0) return 256;  // (nothing is cut up, and nothing used)
   return make_plan(*layer, backward != 0, pairs_of_device()).total;
 }
 

@@ -1,0 +1,31 @@
+"""Workspace sizes of the last layer with its loss, on the host alone, at the ends of what the library takes."""
+import ctypes
+import subprocess
+import sys
+
+import pytest
+
+import __graft_entry__ as g
+
+SOME = 1 << 20  # stands for a device address; nothing reads it
+
+
+@pytest.fixture(scope="module")
+def p():
+    g.build()
+    import paper_1810_09868_b200 as pkg
+    return pkg
+
+
+def size_of(p, rows, inner, classes, dtype, backward):
+    layer = p.binding.vgg19_linear_loss(SOME, inner, SOME + (1 << 16), inner, None, SOME + (2 << 16), rows, inner, classes, dtype)
+    return p.binding.load().vgg19_linear_cross_entropy_bytes(ctypes.byref(layer), backward)
+
+
+def test_a_layer_of_no_rows_has_a_workspace(p):
+    """In a process of its own, which a division by the number of rows would end."""
+    ask = ("import sys; sys.path.insert(0, 'tests'); import paper_1810_09868_b200 as p; from test_head_sizes_cpu import size_of; "
+           "print([size_of(p, 0, 64, 100, dtype, backward) for dtype in (p.VGG19_FP32, p.VGG19_BF16) for backward in (0, 1)])")
+    done = subprocess.run([sys.executable, "-c", ask], capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, (done.returncode, done.stderr[-500:])
+    assert done.stdout.split("\n")[-2] == str([256] * 4), done.stdout
