@@ -1030,6 +1030,8 @@ int vgg19_set_dropout(vgg19_t *n, float rate, uint64_t seed, uint64_t first_pass
   CUDA_TRY(n, cudaDeviceSynchronize());
   const unsigned long long step = 2 * first_pass;
   CUDA_TRY(n, cudaMemcpy(n->pass_counter(), &step, sizeof step, cudaMemcpyHostToDevice));
+  // (that may return once the host's word is staged; the next pass's stream need not be ordered behind it)
+  CUDA_TRY(n, cudaDeviceSynchronize());
   drop_graphs(n);
   n->drop_rate = rate;
   n->drop_seed = seed;
