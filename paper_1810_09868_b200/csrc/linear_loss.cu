@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
       }
       // columns beyond the classes get the bias of an excluded class
 #pragma unroll
-      for (int k = 0; k < 4; ++k) next.bias[k] = 32 * k + lane < cols ? L.rows.bias ? __ldg(L.rows.bias + j0 + 32 * k + lane) : 0.f : -INFINITY;
+      for (int k = 0; k < 4; ++k) next.bias[k] = 32 * k + lane < cols ? L.rows.bias ? L.rows.bias[j0 + 32 * k + lane] : 0.f : -INFINITY;
     };
     if (LOGITS) request(turn(0, worker, workers));
     for (int round = 0, w; ok && (w = turn(round, worker, workers)) < total; ++round) {
@@ -715,7 +715,7 @@ __device__ __forceinline__ float4 sum_of_parts(const Parts& a, int row, int c) {
     for (int k = 0; k < 8; ++k) { s.x += v[k].x; s.y += v[k].y; s.z += v[k].z; s.w += v[k].w; }
   }
   const float none = -INFINITY;  // beyond the classes
-  auto bias = [&](int k) { return c + k < a.classes ? a.bias ? __ldg(a.bias + c + k) : 0.f : none; };
+  auto bias = [&](int k) { return c + k < a.classes ? a.bias ? a.bias[c + k] : 0.f : none; };
   s.x = c < a.classes ? s.x + bias(0) : none;
   s.y = c + 1 < a.classes ? s.y + bias(1) : none;
   s.z = c + 2 < a.classes ? s.z + bias(2) : none;
@@ -828,7 +828,7 @@ __global__ void __launch_bounds__(256) planes_kernel(const __grid_constant__ Lay
 // ---- dx from its parts -----------------------------------------------------------------------------------------------
 // GROUPS: threads that share a sum of many parts, for few values.
 template <typename T, int GROUPS>
-__global__ void __launch_bounds__(256) sum_parts_kernel(const float* __restrict__ part, int parts, long rows, int in, long ld, T* out, long out_ld) {
+__global__ void __launch_bounds__(256) sum_parts_kernel(const float* part, int parts, long rows, int in, long ld, T* out, long out_ld) {
   constexpr int WIDE = 256 / GROUPS;
   __shared__ float4 got[GROUPS][WIDE];
   behind_previous();

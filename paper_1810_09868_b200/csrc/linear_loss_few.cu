@@ -21,6 +21,21 @@ namespace {
 static __device__ int g_few_label_error[2];  // kDevBadLabel once a label outside [0, classes) was met
 
 constexpr int kV = 4;  // values of a slot: 16 bytes
+
+// What another launch may have written is read by ordinary loads: kernels are set up while the ones before them run (an update's that writes w, the
+// one that writes dz), and the read-only path is for memory that nobody writes as long as its reader lives.  __ldcg, from L2, for what is read
+// once; load_again, through L1, for dz, which all of a block's warps read (from L2 one row against 50021 classes of 4096 takes 464 us for all gradients, this
+// way 411).  Both stay behind the wait for the launch before, but stores do not hold them up, as they would a plain dereference.
+__device__ __forceinline__ float load_again(const float* p) {
+  float v;
+  asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ float4 load_again(const float4* p) {
+  float4 v;
+  asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
+  return v;
+}
 constexpr int kMostWarps = 16;
 
 // Slot q of a row: V values, those from q V on where rows are aligned; else of every 32 V values, q % 32 and every 32nd behind it, so that lanes
@@ -32,12 +47,12 @@ struct Slots {
 };
 // The values of a slot; beyond the row there are zeros.  whole: whether the row's 16 bytes can be read at once, where slots are that.
 __device__ __forceinline__ float4 load_slot(const float* row, int q, const Slots& s, bool whole = true) {
-  if (s.aligned && whole && (q + 1) * kV <= s.in) return __ldg(reinterpret_cast<const float4*>(row) + q);
+  if (s.aligned && whole && (q + 1) * kV <= s.in) return __ldcg(reinterpret_cast<const float4*>(row) + q);
   float v[kV];
 #pragma unroll
   for (int j = 0; j < kV; ++j) {
     const int k = s.at(q, j);
-    v[j] = k < s.in ? __ldg(row + k) : 0.f;
+    v[j] = k < s.in ? __ldcg(row + k) : 0.f;
   }
   return make_float4(v[0], v[1], v[2], v[3]);
 }
@@ -126,7 +141,7 @@ template <int RM, int B> __global__ void __launch_bounds__(32 * kMostWarps) few_
     const float sum = sum_over_lanes<N>(acc);
     const int n = n0 + b;
     if (lane < N && n < a.classes) {
-      const float z = sum + (a.bias ? __ldg(a.bias + n) : 0.f);
+      const float z = sum + (a.bias ? __ldcg(a.bias + n) : 0.f);
       if (n == label) a.label_z[row0 + r] = z;
       most = join(most, z != z ? make_float2(-INFINITY, z) : make_float2(z, z == -INFINITY ? 0.f : 1.f));
     }
@@ -170,7 +185,7 @@ template <int RM, int B> __global__ void __launch_bounds__(32 * kMostWarps) few_
     const int n = n0 + b;
     float d = 0.f;
     if (n < a.classes && d_loss != 0.f) {  // (a row that counts for nothing may hold anything; a NaN is not 0)
-      const float p = fast_exp2((sum + (a.bias ? __ldg(a.bias + n) : 0.f) - lse) * kLossLog2e);
+      const float p = fast_exp2((sum + (a.bias ? __ldcg(a.bias + n) : 0.f) - lse) * kLossLog2e);
       d = d_loss * (n == label ? p - 1.f : p);
     }
     if (lane < N && n < a.classes) a.g.dz[(long)n * RM + r] = d;
@@ -216,9 +231,9 @@ template <int RM> __global__ void __launch_bounds__(kProductThreads) few_product
       for (int r = 0; r < RM; r += RM < 4 ? 1 : 4) {
         const float* at = a.g.dz + (long)n * RM + r;
         if (RM < 4) {
-          e[r] = __ldg(at);
+          e[r] = load_again(at);
         } else {
-          const float4 v = __ldg(reinterpret_cast<const float4*>(at));
+          const float4 v = load_again(reinterpret_cast<const float4*>(at));
           e[r] = v.x; e[(r + 1) % RM] = v.y; e[(r + 2) % RM] = v.z; e[(r + 3) % RM] = v.w;
         }
       }

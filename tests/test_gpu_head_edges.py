@@ -47,3 +47,67 @@ def test_a_pass_right_behind_set_dropout_takes_its_masks(p, graph):
             assert not torch.equal(got[0][0], got[1][0])
     net.sync_status(st)
     net.close()
+
+
+class Rows:
+    """Inputs, results and a workspace of one call of the last layer with its loss."""
+
+    def __init__(self, p, rows, inner, classes, dtype=torch.float32, seed=0, dw_dtype=None):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        self.p = p
+        self.x = torch.randn(rows, inner, generator=g, device=DEV).to(dtype)
+        self.w = (torch.randn(classes, inner, generator=g, device=DEV) * 2 / math.sqrt(inner)).to(dtype)
+        self.bias = torch.randn(classes, generator=g, device=DEV) * 0.3
+        self.labels = torch.randint(0, classes, (rows,), generator=g, device=DEV, dtype=torch.int32)
+        self.d_loss = torch.randn(rows, generator=g, device=DEV)
+        self.loss, self.lse = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+        self.dx, self.db = torch.empty_like(self.x), torch.empty(classes, device=DEV)
+        self.dw = torch.empty(classes, inner, dtype=dw_dtype or dtype, device=DEV)
+        self.ws = torch.empty(max(p.vgg19_linear_cross_entropy_bytes(self.x, self.w, b) for b in (False, True)), dtype=torch.uint8, device=DEV)
+
+    def forward(self, st):
+        self.p.vgg19_linear_cross_entropy(self.x, self.w, self.bias, self.labels, self.loss, self.lse, self.ws, st)
+        return self.loss, self.lse
+
+    def backward(self, st):
+        self.p.vgg19_linear_cross_entropy_backward(self.x, self.w, self.bias, self.labels, self.lse, self.d_loss, self.dx, self.dw, self.db, self.ws, st)
+        return self.dx, self.dw, self.db
+
+
+@pytest.mark.parametrize("rows,inner,classes", [(1, 64, 600), (2, 1000, 90), (4, 4096, 300), (7, 130, 5003), (8, 300, 40), (20, 264, 1000)])
+def test_calls_back_to_back_on_one_workspace(p, rows, inner, classes):
+    """Launches are set up while the ones before them run: every call reads what its own launches wrote to the workspace, not a line of the call before."""
+    c = Rows(p, rows, inner, classes)
+    st = torch.cuda.current_stream()
+    scales = [1.0, -3.0, 0.25, 7.0]
+    d_loss = [c.d_loss * s for s in scales]
+    out = [[torch.empty_like(t) for t in (c.dx, c.dw, c.db)] for _ in scales]
+    c.forward(st)
+    alone = []
+    for d in d_loss:
+        torch.cuda.synchronize()
+        c.d_loss = d
+        alone.append([t.clone() for t in c.backward(st)])
+        torch.cuda.synchronize()
+    for _ in range(10):
+        for d, (dx, dw, db) in zip(d_loss, out):  # nothing between the calls
+            p.vgg19_linear_cross_entropy_backward(c.x, c.w, c.bias, c.labels, c.lse, d, dx, dw, db, c.ws, st)
+        torch.cuda.synchronize()
+        for got, want in zip(out, alone):
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("rows,inner,classes", [(1, 4096, 300), (8, 512, 1000), (24, 512, 700), (40, 264, 500)])
+def test_weights_that_an_update_writes_right_before(p, rows, inner, classes):
+    """An update's last kernel lets the next one in the stream be set up while it writes the weights; the loss behind it reads the new ones."""
+    c, st = Rows(p, rows, inner, classes), torch.cuda.current_stream()
+    grad, momentum = torch.randn_like(c.w), torch.zeros_like(c.w)
+    table = p.vgg19_muon_tensors([(c.w, None, grad, momentum)])
+    ws = torch.empty(p.vgg19_muon_workspace_bytes(table), dtype=torch.uint8, device=DEV)
+    for _ in range(10):
+        p.vgg19_muon_update(table, 0.5, 0.9, 0.0, 5, True, ws, stream=st)
+        got = [t.clone() for t in c.forward(st)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, c.forward(st)))
+        torch.cuda.synchronize()
+    p.vgg19_ops_status(st)
