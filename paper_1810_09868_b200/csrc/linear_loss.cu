@@ -571,6 +571,14 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
             for (int j = 0; j < 32; ++j) part[j % 4] += fast_exp2((v[c + j] - ref) * kLossLog2e);
             sum += part[0] + part[1] + (part[2] + part[3]);
           }
+          if (cols < half && sum != sum) {
+            // an infinity among x times the zeros beyond the classes is no number, whatever is added to it: the sum again without them (the
+            // largest has not taken it)
+            sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 128; ++j)
+              if (j < cols) sum += fast_exp2((v[j] - ref) * kLossLog2e);
+          }
           if (lane < rows && cols > 0) L.rows.part[(long)(L.rows.first_part + 2 * tile.j + group) * p.m + row] = make_float2(most, sum);
         } else if (EPI == kLogitGradient) {
           const float ref = lse == -INFINITY ? 0.f : lse;

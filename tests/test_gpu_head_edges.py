@@ -111,3 +111,27 @@ def test_weights_that_an_update_writes_right_before(p, rows, inner, classes):
         assert all(torch.equal(a, b) for a, b in zip(got, c.forward(st)))
         torch.cuda.synchronize()
     p.vgg19_ops_status(st)
+
+
+@pytest.mark.parametrize("rows,classes", [(40, 300), (300, 300), (300, 1001), (1000, 40), (129, 8193)])
+def test_infinities_leave_what_the_formula_leaves(p, rows, classes):
+    """bf16 rows with an infinity whose products have one sign: z is -inf in every class of the row, which is then left none, wherever the tiles end."""
+    inner = 72
+    g = torch.Generator(device=DEV).manual_seed(rows + classes)
+    x = torch.randn(rows, inner, generator=g, device=DEV).bfloat16()
+    w = (torch.randn(classes, inner, generator=g, device=DEV) / 8).bfloat16()
+    w[:, 5] = w[:, 5].abs() + 0.125
+    x[::3, 5] = -math.inf
+    labels = torch.randint(0, classes, (rows,), generator=g, device=DEV, dtype=torch.int32)
+    loss, lse, d_loss = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV), torch.ones(rows, device=DEV)
+    dx, db = torch.full_like(x, math.nan), torch.full((classes,), math.nan, device=DEV)
+    st = torch.cuda.current_stream()
+    ws = [torch.empty(p.vgg19_linear_cross_entropy_bytes(x, w, b), dtype=torch.uint8, device=DEV) for b in (False, True)]
+    p.vgg19_linear_cross_entropy(x, w, None, labels, loss, lse, ws[0], st)
+    none = torch.zeros(rows, dtype=torch.bool, device=DEV)
+    none[::3] = True
+    assert (lse[none] == -math.inf).all() and (loss[none] == math.inf).all()
+    assert torch.isfinite(lse[~none]).all() and torch.isfinite(loss[~none]).all()
+    p.vgg19_linear_cross_entropy_backward(x, w, None, labels, lse, d_loss, dx, None, db, ws[1], st)
+    p.vgg19_ops_status(st)
+    assert (dx[none] == 0).all() and torch.isfinite(dx).all() and torch.isfinite(db).all()
