@@ -516,7 +516,8 @@ int vgg19_linear_cross_entropy(const vgg19_linear_loss *layer, float *loss, floa
  *   dz_rn = d_loss_r (exp(z_rn - lse_r) - [n = labels[r]]):
  *   dx = dz w: device [rows][in], of `dtype`, row stride lddx;   dw = dz^T x: device [classes][in], of dw_dtype (VGG19_FP32 or `dtype`),
  * row stride lddw;   db = sum_r dz_r: device fp32 [classes].  Each is overwritten; any may be NULL.  The products are taken
- * again, a piece of the classes at a time.  In bf16 dz is rounded to bf16 before the products with x and w (db is summed before that).  Rows
+ * again, a piece of the classes at a time.  In bf16 dz is rounded to bf16 before the products with x and w (db is summed before that), and
+ * their sums are fp32, rounded towards zero within chains of at most 4096 products (32768 where the result is bf16) and to nearest where those are joined.  Rows
  * whose label names no class (VGG19_NO_CLASS or another outside, which is reported as above) or whose d_loss is 0 have dz 0 whatever their x holds, but
  * dw takes 0 times their x: it has to be finite.  A row that is left no class has dz 0.  rows == 0: dw and db become 0.
  * workspace: vgg19_linear_cross_entropy_bytes(layer, 1). */

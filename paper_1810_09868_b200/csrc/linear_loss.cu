@@ -22,8 +22,8 @@
 // fp32: a value is three bf16 planes (24 bits), a product six products of planes, those down to 2^-16 of the first; the five lesser ones
 // have an accumulator of their own.  A few rows go another way (linear_loss_few.cu).
 //
-// Precision.  The tensor core truncates its fp32 sums, so a chain ends after 16 K blocks (8 with three planes) and the epilogue adds the
-// chains in registers: the loss of rows of 4096 is 3e-7 from 64 bits, 1.9e-6 with one chain.  dz is fp32 until it is rounded to bf16 for the
+// Precision.  The tensor core truncates its fp32 sums, so a chain ends after 16 K blocks (8 with three planes; 64 or 512 in gradients of bf16 values) and the
+// epilogue adds the chains in registers: the loss of rows of 4096 is 3e-7 from 64 bits, 1.9e-6 with one chain.  dz is fp32 until it is rounded to bf16 for the
 // products (three planes in fp32); db is summed before that.
 //
 // Measured (B200, device time): 4096 rows of 4096 against 131072 bf16 classes, loss 3.2 ms and gradients 10.5 ms, 1.28 PFLOP/s, 0.95 of the measured
@@ -66,7 +66,8 @@ constexpr int kBiasBytes = 128;              // its 32 biases
 constexpr int kSmemBytes = kRingBytes + kEpilogueWarps * (kPieceBytes + kBiasBytes) + 1024 + 256;
 
 // What a tile's sums become: the statistics of its rows, dz, the product itself, or parts of z's sum (kept in fp32, added up in chains).
-enum Epilogue { kStatistics, kLogitGradient, kProduct, kSums };
+// kLongProduct: a product whose sums are too long for one chain.
+enum Epilogue { kStatistics, kLogitGradient, kProduct, kSums, kLongProduct };
 
 // What one CTA, or a pair, does.
 template <bool PAIR> __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
@@ -92,6 +93,7 @@ struct __align__(64) Job {
   int group;              // rows of tiles that are worked on together
   int splits, per_split;  // the sum cut into that many parts, of that many K blocks; part s is plane s of the result
   int chain;              // K blocks that the tensor cores add up before the sums go to the epilogue's registers
+  int longest;            // how many those may be, in a product of bf16 values
   int a_mn, b_mn;
   int store, f32;         // f32: the result is fp32, else bf16
   void* out;              // row stride ld, planes m * ld apart
@@ -204,7 +206,9 @@ __device__ __noinline__ void put_some(const uint4* piece, char* out, long ld, in
 template <int P, int EPI, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_constant__ Launch L) {
   constexpr int STAGES = kStages<P, PAIR>, STAGE_BYTES = kStageBytes<P, PAIR>, BUFFERS = kBuffers<P>, OTHER = kOtherBoxes<P, PAIR>;
+  constexpr bool PRODUCT = EPI == kProduct || EPI == kLongProduct;
   constexpr bool CHAINED = EPI != kSums && (P == 3 || EPI != kProduct);  // whether a tile's sums may come in several chains
+  constexpr bool DIRECT = !CHAINED || EPI == kLongProduct;              // whether one chain may go to memory as it is
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t pieces = smem_base + kRingBytes, biases = pieces + kEpilogueWarps * kPieceBytes, bars = biases + kEpilogueWarps * kBiasBytes;
@@ -401,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
       const int i0 = tile.i * kTileRows<PAIR> + (int)rank * BM + quarter * 32, j0 = tile.j * p.bn + group * half;  // the warp's first row and column
       const int rows = p.m - i0, cols = min(p.n - j0, half);                                         // what there is from there on
       const int row = i0 + lane;
-      if (EPI == kProduct && p.db && tile.j == 0 && group == 0 && tile.split == 0 && lane < rows) {
+      if (PRODUCT && p.db && tile.j == 0 && group == 0 && tile.split == 0 && lane < rows) {
         float s[8] = {};  // (as sum_columns_kernel adds them)
         for (int q = 0; q < p.parts; q += 8) {
 #pragma unroll
@@ -412,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
         p.db[row] = s[0];
       }
       // The piece, `from` on of the half's columns, to memory: lanes along the rows, four whole 128-byte lines at a time.
-      const int elt = EPI == kSums || (EPI == kProduct && p.f32) ? 4 : 2;
+      const int elt = EPI == kSums || (PRODUCT && p.f32) ? 4 : 2;
       const bool whole = rows >= 32 && cols == half && (EPI == kLogitGradient || p.store <= kPadded);
       char* const out = EPI == kStatistics ? nullptr : static_cast<char*>(p.out) + (((long)(EPI == kLogitGradient ? 0 : tile.split) * p.m + i0) * p.ld + j0) * elt;
       auto put_piece = [&](int from, int plane) {
@@ -446,7 +450,8 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
       };
       auto sums_at = [&] { return tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((count % BUFFERS) * BN + group * half); };
 
-      if constexpr (!CHAINED) {
+      const bool direct = !CHAINED || (DIRECT && tile.k1 - tile.k0 <= p.chain);
+      if (DIRECT && direct) {
         // one chain, and nothing to compute: 128 bytes of a row at a time, in little code (a call of few tiles runs it once, from memory)
         if (!sums_are_there()) { ok = false; break; }
         tc_fence_after();
@@ -489,7 +494,8 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
           }
         }
         sums_are_read();
-      } else {
+      }
+      if constexpr (CHAINED) if (!DIRECT || !direct) {
         float v[128];  // the tile's sums of this row and half
         for (long kb0 = tile.k0; kb0 < tile.k1; kb0 += p.chain) {
           if (!sums_are_there()) { ok = false; break; }
@@ -623,9 +629,20 @@ __global__ void __launch_bounds__(kThreads, 1) loss_product_kernel(const __grid_
               put_piece(c0, h);
             }
           }
+        } else if (P == 1 && elt == 2) {
+#pragma unroll
+          for (int c0 = 0; c0 < 128; c0 += 64) {
+            if (c0 >= min(cols, half)) break;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const int e = c0 + 8 * k;
+              piece[piece_at(lane, k)] = make_uint4(pack2(v[e], v[e + 1]), pack2(v[e + 2], v[e + 3]), pack2(v[e + 4], v[e + 5]), pack2(v[e + 6], v[e + 7]));
+            }
+            put_piece(c0, 0);
+          }
         } else {
 #pragma unroll
-          for (int c0 = 0; c0 < 128; c0 += 32) {  // (three planes: fp32)
+          for (int c0 = 0; c0 < 128; c0 += 32) {  // (of three planes always)
             if (c0 >= cols) break;
 #pragma unroll
             for (int k = 0; k < 8; ++k)
@@ -942,10 +959,15 @@ int pairs_of_device() {
 }
 
 // The tensor core truncates its fp32 sums, an error that grows with the chain: 1.8e-6 of the loss over 4096 values in one chain.  The
-// sums of shorter ones are added in registers, rounded to nearest.  Gradients in bf16 need none of that.
+// sums of shorter ones are added in registers, rounded to nearest.
 // (Parts of z's sum are no longer than a chain.)
 constexpr int kOneChain = 1 << 30;
 constexpr int chain_blocks(int planes, int epilogue) { return epilogue == kSums || (epilogue == kProduct && planes == 1) ? kOneChain : planes == 3 ? 8 : 16; }
+// Gradients of bf16 values, whose dz is rounded to bf16 anyway, take longer ones.  An instruction adds 16 products and loses less than a step of
+// the sum so far, 2^-23 of it, always towards zero: 64 K blocks, 256 instructions, less than 3.1e-5 of a sum of one sign, 512 less than
+// 2.5e-4, a sixteenth of the half step 2^-8 that the result is rounded by.  (One chain over 1.2 million rows was 5.2e-3 off.  The shorter ones cost nothing up
+// to these lengths, and 1 to 6 % of all gradients beyond.)
+constexpr int kLongestF32 = 64, kLongestBf16 = 512;
 
 constexpr long kPieceBytesMost = 256L << 20;  // of dz, or of the planes of w
 
@@ -1074,6 +1096,7 @@ template <int P, int EPI, bool PAIR> cudaError_t launch_tiles(const Launch& L, i
 }
 template <int P, int EPI> cudaError_t launch_products(Launch& L, bool pair, int pairs, cudaStream_t st) {
   int tiles = 0;
+  bool is_long = false;
   for (int i = 0; i < L.count; ++i) {
     Job& p = L.job[i];
     const int rows = pair ? kTileRows<true> : kTileRows<false>;
@@ -1084,10 +1107,17 @@ template <int P, int EPI> cudaError_t launch_products(Launch& L, bool pair, int 
     p.per_split = (p.k_blocks + p.splits - 1) / p.splits;
     p.splits = (p.k_blocks + p.per_split - 1) / p.per_split;  // none is empty
     p.chain = chain_blocks(P, EPI);
+    if (P == 1 && EPI == kProduct && p.per_split > p.longest) is_long = true;
     L.first_tile[i] = tiles;
     tiles += p.splits * p.tiles_m * p.tiles_n;
   }
   L.first_tile[L.count] = tiles;
+  if constexpr (P == 1 && EPI == kProduct) {
+    if (is_long) {
+      for (int i = 0; i < L.count; ++i) L.job[i].chain = L.job[i].longest;
+      return pair ? launch_tiles<P, kLongProduct, true>(L, pairs, st) : launch_tiles<P, kLongProduct, false>(L, pairs, st);
+    }
+  }
   return pair ? launch_tiles<P, EPI, true>(L, pairs, st) : launch_tiles<P, EPI, false>(L, pairs, st);
 }
 
@@ -1248,9 +1278,11 @@ cudaError_t backward(const vgg19_linear_loss& a, const Gradients& g, char* ws, c
     Launch M{};
     M.waits = waits;
     const bool f32 = P == 3;
+    bool with_db = false;  // whether dw's tiles add up db on the way
     if (g.dx) {  // dx, or the piece's share of it: [rows][in] = dz w.  Its tiles, over all classes, take longer than dw's: they come first
       Job& j = M.job[M.count++];
       j.a = dz; j.b = o.w; j.b_mn = 1;
+      j.longest = kLongestBf16;
       j.m = (int)a.rows; j.n = a.in; j.k_blocks = (int)((n + BK - 1) / BK); j.bn = p.dx_shape.bn;
       if (p.dx_parts) {
         j.f32 = 1;
@@ -1270,6 +1302,7 @@ cudaError_t backward(const vgg19_linear_loss& a, const Gradients& g, char* ws, c
     if (g.dw) {  // dw of the piece: [n][in] = dz^T x
       Job& j = M.job[M.count++];
       j.a = dz; j.a_mn = 1; j.b = o.x; j.b_mn = 1;
+      j.longest = g.dw_f32 ? kLongestF32 : kLongestBf16;
       j.group = 4;  // whole rows of dw at a time (sixteen: 2 % slower)
       j.m = (int)n; j.n = a.in; j.k_blocks = (int)((a.rows + BK - 1) / BK); j.bn = p.dw_shape.bn;
       if (p.dw_splits > 1) {
@@ -1283,11 +1316,15 @@ cudaError_t backward(const vgg19_linear_loss& a, const Gradients& g, char* ws, c
         j.out = static_cast<char*>(g.dw) + first * g.dw_ld * elt; j.ld = g.dw_ld;
         j.store = copyable(j.out, n, g.dw_ld, elt) ? kWhole : kSingle;
       }
-      j.db_part = db_part; j.db = g.db ? g.db + first : nullptr;
+      // (A sum in chains wants its epilogue all along, which then does not add up db besides: 300000 rows of 1000 against 4000, dw in fp32,
+      // 11.6 ms, 13.4 if it does.)
+      const int dw_splits = p.dw_splits > 1 ? p.dw_splits : 1;
+      with_db = P == 3 || (j.k_blocks + dw_splits - 1) / dw_splits <= j.longest;
+      j.db_part = db_part; j.db = g.db && with_db ? g.db + first : nullptr;
       j.parts = (int)((a.rows + p.db_rows - 1) / p.db_rows);
     }
     if (M.count) e = launch_products<P, kProduct>(M, p.dx_shape.pair, pairs, st);
-    if (!g.dw && g.db && e == cudaSuccess)
+    if (!with_db && g.db && e == cudaSuccess)
       e = launch_behind(sum_columns_kernel, (unsigned)((n + 31) / 32), 256, 0, st, static_cast<const float*>(db_part), (int)((a.rows + p.db_rows - 1) / p.db_rows), (int)n, g.db + first);
   }
   if (e == cudaSuccess && g.dx && p.dx_parts) e = sum_dx(a, g, ws, p, slots, st);

@@ -135,3 +135,48 @@ def test_infinities_leave_what_the_formula_leaves(p, rows, classes):
     p.vgg19_linear_cross_entropy_backward(x, w, None, labels, lse, d_loss, dx, None, db, ws[1], st)
     p.vgg19_ops_status(st)
     assert (dx[none] == 0).all() and torch.isfinite(dx).all() and torch.isfinite(db).all()
+
+
+@pytest.mark.parametrize("dw_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,inner,classes", [(200001, 4096, 1000), (300000, 1000, 4000), (1200000, 256, 9000), (1200000, 70, 300), (1 << 22, 64, 300)])
+def test_sums_over_many_rows_do_not_drift(p, rows, inner, classes, dw_dtype):
+    """dw of bf16 operands, all of one sign.  With w 0, no bias and an lse of 0, dz is exactly d_loss = 1 (0 at the label, class 0), so dw is
+    x's column sums.  A tensor core's sum of at most 4096 products (32768 where the result is bf16), 256 instructions (2048) that may each lose a whole step of
+    the sum so far, is within 256 2^-23 of its own; the sums of those are added in fp32, half a step 2^-24 each and one more for each of up to 64 parts; and
+    a bf16 result is rounded."""
+    f32 = dw_dtype == torch.float32
+    g = torch.Generator(device=DEV).manual_seed(rows)
+    x = torch.empty(rows, inner, dtype=torch.bfloat16, device=DEV).uniform_(0.5, 1.0, generator=g)
+    w, labels = torch.zeros(classes, inner, dtype=torch.bfloat16, device=DEV), torch.zeros(rows, dtype=torch.int32, device=DEV)
+    lse, d_loss = torch.zeros(rows, device=DEV), torch.ones(rows, device=DEV)
+    dw, db = torch.full((classes, inner), math.nan, device=DEV, dtype=dw_dtype), torch.full((classes,), math.nan, device=DEV)
+    ws = torch.empty(p.vgg19_linear_cross_entropy_bytes(x, w, True), dtype=torch.uint8, device=DEV)
+    st = torch.cuda.current_stream()
+    p.vgg19_linear_cross_entropy_backward(x, w, None, labels, lse, d_loss, None, dw, db, ws, st)
+    p.vgg19_ops_status(st)
+    want = torch.zeros(inner, dtype=torch.float64, device=DEV)
+    for a in range(0, rows, 50000):
+        want += x[a:a + 50000].double().sum(0)
+    off = max(((dw[a:a + 1000].double() - want).abs() / want).max().item() for a in range(1, classes, 1000))
+    chain = (256 if f32 else 2048) * 2.0 ** -23 + (rows / 4096 + 66) * 2.0 ** -24
+    assert not dw[0].any() and off <= chain + (0 if f32 else 2.0 ** -8), off
+    assert db[0] == 0 and (db[1:] == rows).all()  # (whole numbers below 2^24)
+
+
+@pytest.mark.parametrize("rows,inner,classes", [(100, 4096, 200000), (130, 1000, 700001), (2048, 4096, 70001), (3000, 3001, 40000), (1, 64, 1 << 24)])
+def test_sums_over_many_classes_do_not_drift(p, rows, inner, classes):
+    """dx of bf16 operands in the same way: x is 0, so that dz is d_loss = 1 everywhere but at the label, and dx is w's column sums, rounded to bf16."""
+    g = torch.Generator(device=DEV).manual_seed(rows)
+    x = torch.zeros(rows, inner, dtype=torch.bfloat16, device=DEV)
+    w = torch.empty(classes, inner, dtype=torch.bfloat16, device=DEV).uniform_(0.5, 1.0, generator=g)
+    labels, lse, d_loss = torch.zeros(rows, dtype=torch.int32, device=DEV), torch.zeros(rows, device=DEV), torch.ones(rows, device=DEV)
+    dx, dw = torch.full_like(x, math.nan), torch.full_like(w, math.nan)
+    ws = torch.empty(p.vgg19_linear_cross_entropy_bytes(x, w, True), dtype=torch.uint8, device=DEV)
+    st = torch.cuda.current_stream()
+    p.vgg19_linear_cross_entropy_backward(x, w, None, labels, lse, d_loss, dx, dw, None, ws, st)
+    p.vgg19_ops_status(st)
+    want = torch.zeros(inner, dtype=torch.float64, device=DEV)
+    for a in range(1, classes, 50000):
+        want += w[a:a + 50000].double().sum(0)
+    off = ((dx.double() - want).abs() / want).max().item()
+    assert off <= 2.0 ** -8 + 2048 * 2.0 ** -23 + (classes / 4096 + 66) * 2.0 ** -24 and not dw.any(), off
