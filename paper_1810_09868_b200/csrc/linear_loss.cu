@@ -1419,7 +1419,12 @@ extern "C" size_t vgg19_linear_cross_entropy_bytes(const vgg19_linear_loss* laye
   using namespace vgg;
   if (check(layer) != VGG19_OK) return 0;
   if (layer->rows == 0) return 256;  // (nothing is cut up, and nothing used)
-  return make_plan(*layer, backward != 0, pairs_of_device()).total;
+  // (a step has one workspace for both calls; the loss of many classes, whose gradients come in pieces, takes more than those)
+  const int pairs = pairs_of_device();
+  const size_t loss = make_plan(*layer, false, pairs).total;
+  if (!backward) return loss;
+  const size_t gradients = make_plan(*layer, true, pairs).total;
+  return gradients > loss ? gradients : loss;
 }
 
 extern "C" int vgg19_linear_cross_entropy(const vgg19_linear_loss* layer, float* loss, float* lse, void* workspace, size_t bytes, void* stream) {

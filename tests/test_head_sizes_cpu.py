@@ -1,5 +1,7 @@
 """Workspace sizes of the last layer with its loss, on the host alone, at the ends of what the library takes."""
 import ctypes
+import math
+import random
 import subprocess
 import sys
 
@@ -29,3 +31,22 @@ def test_a_layer_of_no_rows_has_a_workspace(p):
     done = subprocess.run([sys.executable, "-c", ask], capture_output=True, text=True, timeout=300)
     assert done.returncode == 0, (done.returncode, done.stderr[-500:])
     assert done.stdout.split("\n")[-2] == str([256] * 4), done.stdout
+
+
+@pytest.mark.parametrize("rows,inner,classes,dtype", [(32768, 128, 262144, 1), (65536, 64, 1 << 20, 1), (33216, 1, 1 << 20, 1), (20000, 17, 500000, 1), (32768, 128, 262144, 0), (8, 4096, 50021, 0),
+                                                      (100, 4096, 1000, 1), (1, 1, 1, 0)])
+def test_the_gradients_workspace_does_for_the_loss_too(p, rows, inner, classes, dtype):
+    assert size_of(p, rows, inner, classes, dtype, 1) >= size_of(p, rows, inner, classes, dtype, 0) >= 256
+
+
+def test_the_gradients_workspace_does_for_the_loss_at_any_size(p):
+    rng = random.Random(7)
+
+    def log(most):
+        return int(math.exp(rng.uniform(0, math.log(most))))
+
+    for _ in range(3000):
+        rows, classes = log(1 << 22), log(1 << 24)
+        if rows * classes <= 1 << 44:
+            a = rows, log(1 << 20), classes, rng.randrange(2)
+            assert size_of(p, *a, 1) >= size_of(p, *a, 0) > 0, a
