@@ -1494,8 +1494,8 @@ int vgg19_describe(const vgg19_t *n, char *out, size_t cap) {
     snprintf(line, sizeof line, "training passes: dropout at %g behind dense1 and dense2\n", (double)n->drop_rate);
     s += line;
   }
-  snprintf(line, sizeof line, "counts: convolution=16 reduce-window=5 dot=3 relu=18 softmax=1 rng=0\n");
-  s += line;
+  s += "counts: convolution=16 reduce-window=5 dot=3 relu=18 softmax=1 ";
+  s += n->drop_rate > 0.f ? "rng=2 (of training passes; others have none)\n" : "rng=0\n";
   if (out && cap) {
     size_t k = s.size() < cap - 1 ? s.size() : cap - 1;
     memcpy(out, s.data(), k);

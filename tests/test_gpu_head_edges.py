@@ -180,3 +180,14 @@ def test_sums_over_many_classes_do_not_drift(p, rows, inner, classes):
         want += w[a:a + 50000].double().sum(0)
     off = ((dx.double() - want).abs() / want).max().item()
     assert off <= 2.0 ** -8 + 2048 * 2.0 ** -23 + (classes / 4096 + 66) * 2.0 ** -24 and not dw.any(), off
+
+
+def test_a_description_counts_the_random_masks(p):
+    net = p.Net(32, 32, 1, p.VGG19_BF16, seed=1, mode=p.VGG19_MODE_FORWARD)
+    assert " rng=0\n" in p.vgg19_describe(net.handle)
+    net.set_dropout(0.25)
+    text = p.vgg19_describe(net.handle)
+    assert "dropout at 0.25" in text and " rng=2 " in text and "rng=0" not in text
+    net.set_dropout(0.0)
+    assert " rng=0\n" in p.vgg19_describe(net.handle)
+    net.close()
