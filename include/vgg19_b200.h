@@ -481,7 +481,8 @@ int vgg19_dropout_backward(const void *dy, int32_t dtype, int64_t rows, int32_t 
  * vgg19_saved_tensor gives as their outputs, and of the gradients that come back there.  Forward-only passes have none (values are scaled up in training).  rate 0 (a
  * new network's) is no dropout.  Pass p since this call, p = first_pass, first_pass + 1, ..., takes steps 2p (behind layer 1) and 2p + 1 of
  * `seed`, whose rows are the images; the passes are counted on the device, so recorded ones take other masks every time, and every
- * step of vgg19_train_steps is a pass.  Waits for the device, and discards recorded graphs. */
+ * step of vgg19_train_steps is a pass.  Row 0 is the pass's first image: of several GPUs that train on parts of a batch, each needs a `seed` of its own, or image
+ * i of every part loses the same values.  Waits for the device, and discards recorded graphs. */
 int vgg19_set_dropout(vgg19_t *net, float rate, uint64_t seed, uint64_t first_pass);
 
 /* The last dense layer (section 7.1, dense(W, x, b) = W*x .+ b) and the softmax cross entropy of its rows in one, for any number of

@@ -91,7 +91,8 @@ class Net:
                                     nesterov, self.muon_workspace, self.muon_workspace.numel(), stream)
 
     def set_dropout(self, rate, seed=0, first_pass=0):
-        """Training passes drop the outputs of dense layers 1 and 2 at `rate` (0: none), each pass with masks of its own."""
+        """Training passes drop the outputs of dense layers 1 and 2 at `rate` (0: none), each pass with masks of its own.  A mask goes by
+        seed, pass and place in the batch: ranks that train on parts of a batch take seeds of their own."""
         with self._torch.cuda.device(self.device):
             binding.vgg19_set_dropout(self.handle, rate, seed, first_pass)
 
