@@ -509,7 +509,9 @@ typedef struct {
  * products of terms down to 2^-16 of the first (an infinity may make its row's results NaN where the formula would not); a few rows (up to eight, or 24 without gradients) may be taken in fp32 as they are.  At most 2^44 logits.
  * workspace: device, 256-byte aligned, vgg19_linear_cross_entropy_bytes(layer, 0) bytes (0 for a layer that is refused; of pointers only the
  * alignment of x and w is looked at): scratch for the time of the call; calls that share one have to be ordered.  One of
- * vgg19_linear_cross_entropy_bytes(layer, 1) bytes does for this call and for the gradients.  Asynchronous
+ * vgg19_linear_cross_entropy_bytes(layer, 1) bytes does for this call and for the gradients.  The size holds for these sizes and this alignment
+ * alone: fewer rows may take more, since their sums are cut into more parts (bf16, 4096 values against 1000 classes: 18.4 MB for 1152 rows, 0.16 MB for
+ * 1216), so a program with batches of several sizes asks for each and keeps the largest.  Asynchronous
  * on `stream`; may be captured.  rows == 0 does nothing.  Nothing that is written may overlap anything else of the call. */
 size_t vgg19_linear_cross_entropy_bytes(const vgg19_linear_loss *layer, int32_t backward);
 int vgg19_linear_cross_entropy(const vgg19_linear_loss *layer, float *loss, float *lse, void *workspace, size_t bytes, void *stream);

@@ -623,7 +623,8 @@ def _linear_loss(x, w, bias, labels):
 
 
 def vgg19_linear_cross_entropy_bytes(x, w, backward):
-    """Bytes of workspace for x [rows][in] and w [classes][in]; 0 for sizes that are refused.  backward: for the loss and for its gradients."""
+    """Bytes of workspace for x [rows][in] and w [classes][in]; 0 for sizes that are refused.  backward: for the loss and for its gradients.
+    Fewer rows may take more: a program with batches of several sizes asks for each."""
     layer, dev = _linear_loss(x, w, None, None)
     import torch
     with torch.cuda.device(dev):

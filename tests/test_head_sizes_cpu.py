@@ -50,3 +50,12 @@ def test_the_gradients_workspace_does_for_the_loss_at_any_size(p):
         if rows * classes <= 1 << 44:
             a = rows, log(1 << 20), classes, rng.randrange(2)
             assert size_of(p, *a, 1) >= size_of(p, *a, 0) > 0, a
+
+
+def test_fewer_rows_may_take_more(p):
+    """As the header says: a smaller batch is asked for by itself, and too small a workspace is refused before anything runs."""
+    many, fewer = size_of(p, 1216, 4096, 1000, 1, 0), size_of(p, 1152, 4096, 1000, 1, 0)
+    assert many < fewer
+    layer = p.binding.vgg19_linear_loss(SOME, 4096, SOME + (1 << 24), 4096, None, SOME + (1 << 26), 1152, 4096, 1000, 1)
+    far = 1 << 30
+    assert p.binding.load().vgg19_linear_cross_entropy(ctypes.byref(layer), far, None, far + (1 << 20), many, None) == p.VGG19_ERR_WORKSPACE
