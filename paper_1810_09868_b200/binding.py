@@ -580,16 +580,19 @@ def vgg19_muon_step(net, grads, momentum_buffer, lr, momentum, decay, bias_lr, s
                                               _ptr(workspace), nbytes, _stream(stream)))
 
 
+def _word64(v, what):
+    if not 0 <= v < 1 << 64:
+        _refuse(VGG19_ERR_ARG, f"{what} {v} is not an unsigned 64-bit number")
+    return int(v)
+
+
 def _any_dropout(name, x, y, rate, seed, step, step_counter, first, stream):
     source, result = ("dy", "dx") if name.endswith("backward") else ("x", "y")
     dtype, rows, cols, ldx, dev = _rows_of(x, source)
     y_dtype, y_rows, y_cols, ldy, y_dev = _rows_of(y, result)
     if (y_dtype, y_rows, y_cols, y_dev) != (dtype, rows, cols, dev):
         _refuse(VGG19_ERR_SHAPE, f"{result} differs from {source} in type, shape or device")
-    for v, what in ((seed, "seed"), (step, "step"), (first, "first")):
-        if not 0 <= v < 1 << 64:
-            _refuse(VGG19_ERR_ARG, f"{what} {v} is not an unsigned 64-bit number")
-    seed, step, first = int(seed), int(step), int(first)
+    seed, step, first = _word64(seed, "seed"), _word64(step, "step"), _word64(first, "first")
     import torch
     counter = _tensor(step_counter, "step_counter", torch.int64, (1,), dev)
     return _call(dev, getattr(_lib or load(), "vgg19_" + name), x.data_ptr(), dtype, rows, cols, ldx, rate, seed, step, counter, first, y.data_ptr(), ldy,
@@ -667,7 +670,7 @@ def vgg19_linear_cross_entropy_backward(x, w, bias, labels, lse, d_loss, dx, dw,
 
 
 def vgg19_set_dropout(net, rate, seed, first_pass=0):
-    return _check(net, load().vgg19_set_dropout(net, rate, seed, first_pass))
+    return _check(net, load().vgg19_set_dropout(net, rate, _word64(seed, "seed"), _word64(first_pass, "first_pass")))
 
 
 def vgg19_selftest_operator_timeout(net, which, workspace, stream=None):

@@ -1,4 +1,4 @@
-"""Workspace sizes of the last layer with its loss, on the host alone, at the ends of what the library takes."""
+"""Workspace sizes of the last layer with its loss, and numbers that dropout takes, on the host alone, at the ends of what the library takes."""
 import ctypes
 import math
 import random
@@ -59,3 +59,11 @@ def test_fewer_rows_may_take_more(p):
     layer = p.binding.vgg19_linear_loss(SOME, 4096, SOME + (1 << 24), 4096, None, SOME + (1 << 26), 1152, 4096, 1000, 1)
     far = 1 << 30
     assert p.binding.load().vgg19_linear_cross_entropy(ctypes.byref(layer), far, None, far + (1 << 20), many, None) == p.VGG19_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("seed,first_pass", [(-1, 0), (1 << 64, 0), (0, -1), (0, 1 << 64), (0, (1 << 64) + 3)])
+def test_a_networks_dropout_takes_no_number_modulo_2_to_the_64(p, seed, first_pass):
+    """The C call's numbers have 64 bits: others are refused, as vgg19_dropout refuses them, not cut."""
+    with pytest.raises(p.Vgg19Error) as e:
+        p.vgg19_set_dropout(None, 0.5, seed, first_pass)
+    assert e.value.code == p.VGG19_ERR_ARG and "unsigned 64-bit" in str(e.value)
