@@ -583,6 +583,8 @@ def vgg19_muon_step(net, grads, momentum_buffer, lr, momentum, decay, bias_lr, s
 def _word64(v, what):
     if not 0 <= v < 1 << 64:
         _refuse(VGG19_ERR_ARG, f"{what} {v} is not an unsigned 64-bit number")
+    if int(v) != v:
+        _refuse(VGG19_ERR_ARG, f"{what} {v} is not a whole number")
     return int(v)
 
 

@@ -67,3 +67,10 @@ def test_a_networks_dropout_takes_no_number_modulo_2_to_the_64(p, seed, first_pa
     with pytest.raises(p.Vgg19Error) as e:
         p.vgg19_set_dropout(None, 0.5, seed, first_pass)
     assert e.value.code == p.VGG19_ERR_ARG and "unsigned 64-bit" in str(e.value)
+
+
+def test_a_dropouts_numbers_are_whole(p):
+    for call in (lambda: p.vgg19_set_dropout(None, 0.5, 1.5), lambda: p.vgg19_set_dropout(None, 0.5, 1, 2.5)):
+        with pytest.raises(p.Vgg19Error) as e:
+            call()
+        assert e.value.code == p.VGG19_ERR_ARG and "whole" in str(e.value)
