@@ -41,8 +41,8 @@ namespace {
 
 using namespace tc;
 
-static __device__ int g_loss_error[2];   // a DeviceError code once a bounded wait of a call without a handle ran out
-static __device__ int g_label_error[2];  // kDevBadLabel once a label outside [0, classes) was met
+static __device__ int g_loss_error[1];   // a DeviceError code once a bounded wait of a call without a handle ran out
+static __device__ int g_label_error[1];  // kDevBadLabel once a label outside [0, classes) was met
 
 // ---- sizes -----------------------------------------------------------------------------------------------------
 constexpr int BM = 128, BN = 256, BK = 64;   // rows of a CTA (a pair has 256), columns of a tile (at most: 256, 192 or 128), K per stage
@@ -1380,16 +1380,9 @@ template <int N> bool blocks_meet(const Block (&all)[N], int written) {
 
 }  // namespace
 
-cudaError_t loss_take_error(int* code, int* label, cudaStream_t st) {
-  void *word = nullptr, *label_word = nullptr;
-  cudaError_t e = cudaGetSymbolAddress(&word, g_loss_error);
-  if (e == cudaSuccess) e = cudaGetSymbolAddress(&label_word, g_label_error);
-  if (e == cudaSuccess) e = take_error(static_cast<int*>(word), code, st);
-  if (e == cudaSuccess) e = take_error(static_cast<int*>(label_word), label, st);
-  int few = 0;
-  if (e == cudaSuccess) e = few_rows_take_error(&few, st);
-  if (few) *label = few;
-  return e;
+cudaError_t loss_error_words(ErrorWords* words) {
+  const cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void**>(&words->at[kErrorLoss]), g_loss_error);
+  return e == cudaSuccess ? cudaGetSymbolAddress(reinterpret_cast<void**>(&words->at[kErrorLabel]), g_label_error) : e;
 }
 
 int linear_loss(const vgg19_linear_loss* layer, float* loss, float* lse, void* workspace, size_t bytes, const Waits& waits, const bool* in_pairs, void* stream) {

@@ -67,7 +67,5 @@ struct FewGradients {
   float* db;
 };
 cudaError_t few_rows_gradients(const vgg19_linear_loss& a, const FewGradients& g, int sms, cudaStream_t st);
-// A label outside the classes that its kernels met, as take_error gives it.
-cudaError_t few_rows_take_error(int* label, cudaStream_t st);
 
 }  // namespace vgg

@@ -18,7 +18,7 @@
 namespace vgg {
 namespace {
 
-static __device__ int g_few_label_error[2];  // kDevBadLabel once a label outside [0, classes) was met
+static __device__ int g_few_label_error[1];  // kDevBadLabel once a label outside [0, classes) was met
 
 constexpr int kV = 4;  // values of a slot: 16 bytes
 
@@ -327,11 +327,7 @@ template <int RM> cudaError_t gradients_of(const Layer& l, int b, int blocks, in
 
 }  // namespace
 
-cudaError_t few_rows_take_error(int* label, cudaStream_t st) {
-  void* word = nullptr;
-  const cudaError_t e = cudaGetSymbolAddress(&word, g_few_label_error);
-  return e == cudaSuccess ? take_error(static_cast<int*>(word), label, st) : e;
-}
+cudaError_t few_rows_error_words(ErrorWords* words) { return cudaGetSymbolAddress(reinterpret_cast<void**>(&words->at[kErrorFewLabel]), g_few_label_error); }
 
 bool few_rows(const vgg19_linear_loss& a, bool backward) {
   if (a.dtype != VGG19_FP32 || a.rows > (backward ? 8 : 24) || a.in > kMostKept / group_up(a)) return false;

@@ -32,7 +32,7 @@ namespace cg = cooperative_groups;
 namespace vgg {
 namespace {
 
-static __device__ int g_logprobs_error[2];  // kDevBadLabel once an id outside [0, classes) was met
+static __device__ int g_logprobs_error[1];  // kDevBadLabel once an id outside [0, classes) was met
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // A reference moves only when a value exceeds it by this much (natural units): exp(z - ref) then stays below e^4, and
@@ -735,11 +735,7 @@ template <typename... P> bool words(P... p) { return ((reinterpret_cast<uintptr_
 
 }  // namespace
 
-cudaError_t logprobs_take_error(int* code, cudaStream_t st) {
-  void* word = nullptr;
-  const cudaError_t e = cudaGetSymbolAddress(&word, g_logprobs_error);
-  return e == cudaSuccess ? take_error(static_cast<int*>(word), code, st) : e;
-}
+cudaError_t logprobs_error_words(ErrorWords* words) { return cudaGetSymbolAddress(reinterpret_cast<void**>(&words->at[kErrorId]), g_logprobs_error); }
 
 }  // namespace vgg
 

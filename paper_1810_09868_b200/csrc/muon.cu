@@ -44,7 +44,7 @@ namespace {
 
 using namespace tc;
 
-static __device__ int g_muon_error[2];  // a DeviceError code once a bounded wait of a call without a handle ran out
+static __device__ int g_muon_error[1];  // a DeviceError code once a bounded wait of a call without a handle ran out
 
 // ---- sizes -----------------------------------------------------------------------------------------------------
 constexpr int BM = 128, BK = 64;                 // rows per CTA (a pair has 256), K per stage
@@ -1314,11 +1314,7 @@ size_t workspace_bytes(const vgg19_muon_tensor* t, int32_t count) {
 
 }  // namespace
 
-cudaError_t muon_take_error(int* code, cudaStream_t st) {
-  void* word = nullptr;
-  const cudaError_t e = cudaGetSymbolAddress(&word, g_muon_error);
-  return e == cudaSuccess ? take_error(static_cast<int*>(word), code, st) : e;
-}
+cudaError_t muon_error_words(ErrorWords* words) { return cudaGetSymbolAddress(reinterpret_cast<void**>(&words->at[kErrorUpdate]), g_muon_error); }
 
 cudaError_t muon_vector_update(const MuonVector* v, int count, float lr, float mu, bool nesterov, cudaStream_t st) {
   Vectors a{};

@@ -37,7 +37,7 @@ namespace {
 
 using namespace tc;
 
-static __device__ int g_q4_error[2];  // a DeviceError code once a bounded wait of a call without a handle ran out
+static __device__ int g_q4_error[1];  // a DeviceError code once a bounded wait of a call without a handle ran out
 
 constexpr int kTileRows = 16, kBlockK = 128, kBlockBytes = kTileRows * kBlockK / 2;
 constexpr int kMaxRows = 16;                 // rows of x per launch
@@ -482,11 +482,7 @@ cudaError_t q4_linear(const T* x, long ldx, long rows, int in, const void* codes
   return cudaSuccess;
 }
 
-cudaError_t q4_take_error(int* code, cudaStream_t st) {
-  void* word = nullptr;
-  const cudaError_t e = cudaGetSymbolAddress(&word, g_q4_error);
-  return e == cudaSuccess ? take_error(static_cast<int*>(word), code, st) : e;
-}
+cudaError_t q4_error_words(ErrorWords* words) { return cudaGetSymbolAddress(reinterpret_cast<void**>(&words->at[kErrorDense]), g_q4_error); }
 
 #define INSTANTIATE(T)                                                                                                    \
   template cudaError_t q4_pack<T>(const T*, long, int, int, int, void*, void*, cudaStream_t);                             \

@@ -760,6 +760,9 @@ INSTANTIATE(bf16)
 
 namespace {
 __global__ void take_error_kernel(int* word) { word[1] = atomicExch(word, 0); }
+
+__device__ int g_taken[kErrorWords];
+__global__ void take_errors_kernel(const __grid_constant__ ErrorWords words) { g_taken[threadIdx.x] = atomicExch(words.at[threadIdx.x], 0); }
 }  // namespace
 
 cudaError_t take_error(int* word, int* code, cudaStream_t st) {
@@ -769,6 +772,17 @@ cudaError_t take_error(int* word, int* code, cudaStream_t st) {
   take_error_kernel<<<1, 1, 0, st>>>(word);
   e = cudaGetLastError();
   if (e == cudaSuccess) e = cudaMemcpyAsync(code, word + 1, sizeof(int), cudaMemcpyDeviceToHost, st);
+  const cudaError_t end = cudaStreamSynchronize(st);
+  return e == cudaSuccess ? end : e;
+}
+
+cudaError_t take_errors(const ErrorWords& words, int (&codes)[kErrorWords], cudaStream_t st) {
+  void* taken = nullptr;
+  cudaError_t e = cudaGetSymbolAddress(&taken, g_taken);
+  if (e != cudaSuccess) return e;
+  take_errors_kernel<<<1, kErrorWords, 0, st>>>(words);
+  e = cudaGetLastError();
+  if (e == cudaSuccess) e = cudaMemcpyAsync(codes, taken, sizeof codes, cudaMemcpyDeviceToHost, st);
   const cudaError_t end = cudaStreamSynchronize(st);
   return e == cudaSuccess ? end : e;
 }

@@ -811,21 +811,24 @@ int vgg19_ops_status(void *stream) {
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaStreamSynchronize(st);  // (nobody waits for this one's stream behind the lock)
   if (e != cudaSuccess) return fail(nullptr, VGG19_ERR_CUDA, "waiting for the stream failed: %s", cudaGetErrorString(e));
-  int id = 0, dense = 0, update = 0, loss = 0, label = 0;
+  int codes[kErrorWords] = {};
   try {
     const std::lock_guard<std::mutex> lock(one);
     // all of them, whichever are set: what one call reports, none finds again
-    const cudaError_t read[] = {logprobs_take_error(&id, st), q4_take_error(&dense, st), muon_take_error(&update, st), loss_take_error(&loss, &label, st)};
-    for (cudaError_t r : read)
-      if (e == cudaSuccess) e = r;
+    ErrorWords words{};
+    const cudaError_t found[] = {logprobs_error_words(&words), q4_error_words(&words), muon_error_words(&words), loss_error_words(&words), few_rows_error_words(&words)};
+    for (cudaError_t f : found)
+      if (e == cudaSuccess) e = f;
+    if (e == cudaSuccess) e = take_errors(words, codes, st);
   } catch (...) {
     return fail(nullptr, VGG19_ERR_CUDA, "the host refused a lock");
   }
   if (e != cudaSuccess) return fail(nullptr, VGG19_ERR_CUDA, "reading the device status failed: %s", cudaGetErrorString(e));
+  const int id = codes[kErrorId], label = codes[kErrorLabel] ? codes[kErrorLabel] : codes[kErrorFewLabel];
   const char *bad = id && label ? "an id outside the row's classes (its log probability is NaN), and a label outside them (its loss is NaN)"
                     : id        ? "an id outside the row's classes (its log probability is NaN)"
                                 : "a label outside the classes (its loss is NaN)";
-  const int late[] = {dense, update, loss};
+  const int late[] = {codes[kErrorDense], codes[kErrorUpdate], codes[kErrorLoss]};
   const char *names[] = {"a 4-bit layer", "an update", "a layer with its loss"};
   std::string which;
   int code = 0;

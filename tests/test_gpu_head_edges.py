@@ -191,3 +191,50 @@ def test_a_description_counts_the_random_masks(p):
     net.set_dropout(0.0)
     assert " rng=0\n" in p.vgg19_describe(net.handle)
     net.close()
+
+
+def test_one_status_names_all_kinds_at_once(p):
+    """Words of five files: a bad id, bad labels of tiles and of a few rows, and the waits of all operators; the next status finds none."""
+    st = torch.cuda.current_stream()
+    p.vgg19_ops_status(st)
+    ws = torch.empty(p.VGG19_SELFTEST_BYTES, dtype=torch.uint8, device=DEV)
+    tiles, few = Rows(p, 40, 64, 300), Rows(p, 3, 64, 300)
+
+    def bad_label(c):
+        c.labels[-1] = 300
+        c.forward(st)
+
+    def bad_id():
+        p.vgg19_logprobs(torch.zeros(1, 10, device=DEV), torch.full((1, 1), 10, dtype=torch.int32, device=DEV), torch.empty(1, 1, device=DEV), stream=st)
+
+    wait = lambda kind: p.vgg19_selftest_operator_timeout(None, getattr(p, "VGG19_SELFTEST_" + kind), ws, st)  # noqa: E731
+    kinds = {"4-bit": lambda: wait("DENSE_Q4"), "update": lambda: wait("UPDATE"), "with its loss": lambda: wait("LOSS"), "id outside": bad_id,
+             "label outside": lambda: bad_label(tiles), "label": lambda: bad_label(few)}
+    for chosen in [[k] for k in kinds] + [list(kinds), ["update", "label"], ["with its loss", "id outside"]]:
+        for k in chosen:
+            kinds[k]()
+        with pytest.raises(p.Vgg19Error) as e:
+            p.vgg19_ops_status(st)
+        assert all(k in str(e.value) for k in chosen), str(e.value)
+        assert e.value.code == (p.VGG19_ERR_DEVICE_TIMEOUT if {"4-bit", "update", "with its loss"} & set(chosen) else p.VGG19_ERR_ARG)
+        p.vgg19_ops_status(st)
+
+
+def test_a_status_of_all_operators_takes_about_as_long_as_a_networks(p):
+    """One exchange on the device and one copy, whatever the number of words: it was six of each, six times a network's."""
+    import time
+    net = p.Net(32, 32, 1, p.VGG19_BF16, seed=1, mode=p.VGG19_MODE_FORWARD)
+    st = torch.cuda.current_stream()
+
+    def median(call):
+        times = []
+        for _ in range(300):
+            a = time.perf_counter()
+            call()
+            times.append(time.perf_counter() - a)
+        return sorted(times)[150]
+
+    median(lambda: p.vgg19_ops_status(st)), median(lambda: net.sync_status(st))
+    ratio = min(median(lambda: p.vgg19_ops_status(st)) / median(lambda: net.sync_status(st)) for _ in range(5))
+    net.close()
+    assert ratio < 3, ratio
