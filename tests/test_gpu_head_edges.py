@@ -238,3 +238,42 @@ def test_a_status_of_all_operators_takes_about_as_long_as_a_networks(p):
     ratio = min(median(lambda: p.vgg19_ops_status(st)) / median(lambda: net.sync_status(st)) for _ in range(5))
     net.close()
     assert ratio < 3, ratio
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,inner,classes", [(7, 300, 500), (20, 512, 700), (100, 264, 1000), (300, 136, 2049), (2000, 40, 9001)])
+def test_a_rows_results_do_not_depend_on_its_company(p, rows, inner, classes, dtype):
+    """The same bits whatever the other rows hold, not-a-numbers and rows without a label among them."""
+    c, st = Rows(p, rows, inner, classes, dtype), torch.cuda.current_stream()
+    kept = torch.arange(0, rows, 3, device=DEV)
+    others = torch.ones(rows, dtype=torch.bool, device=DEV)
+    others[kept] = False
+    c.forward(st)
+    first = [t[kept].clone() for t in (c.loss, c.lse, c.backward(st)[0])]
+    for fill in (0.0, 5.0, math.nan, math.inf):
+        c.x[others] = fill
+        c.labels[others] = -1 if fill != 5.0 else 0
+        c.forward(st)
+        assert all(torch.equal(a, b) for a, b in zip(first, (c.loss[kept], c.lse[kept], c.backward(st)[0][kept]))), fill
+    p.vgg19_ops_status(st)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,classes", [(30, 100), (300, 700), (3000, 5000)])
+def test_long_rows_of_one_sign_do_not_drift(p, rows, classes, dtype):
+    """z of 65536 products of one sign.  A chain of 1024 of them is 64 instructions (for fp32 512 products, 32), each losing less than a step, 2^-23, of the
+    sum so far (fp32: its five lesser products too, 2^-7 of that); 64 (128) chains are added, half a step each; then lse's own: within 2^-24 of its size and
+    20 steps of an exponential sum's.  Terms that an fp32 product leaves out are below 3 2^-24 of it."""
+    g = torch.Generator(device=DEV).manual_seed(classes)
+    inner = 65536
+    x, w = (torch.empty(n, inner, device=DEV).uniform_(0.5, 1.0, generator=g).to(dtype) for n in (rows, classes))
+    labels, loss, lse = torch.zeros(rows, dtype=torch.int32, device=DEV), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    st = torch.cuda.current_stream()
+    ws = torch.empty(p.vgg19_linear_cross_entropy_bytes(x, w, False), dtype=torch.uint8, device=DEV)
+    p.vgg19_linear_cross_entropy(x, w, None, labels, loss, lse, ws, st)
+    p.vgg19_ops_status(st)
+    z = x.double() @ w.double().T
+    want = torch.logsumexp(z, 1)
+    relative = (64 + 64 / 2 if dtype == torch.bfloat16 else 32 * (1 + 2.0 ** -7) + 128 / 2 + 1.5) * 2.0 ** -23
+    off = ((lse.double() - want).abs() - 20 * 2.0 ** -23).div(want.abs()).max().item()
+    assert off <= relative + 2.0 ** -24, (off, relative)
