@@ -506,7 +506,7 @@ typedef struct {
  * is 0.  Any other label outside [0, classes) is never used as an index: its loss is NaN and vgg19_ops_status reports VGG19_ERR_ARG.
  * A row that is left no class has lse -inf and loss +inf; so has an excluded label, with a finite lse.  A NaN or +inf among a row's z makes its results NaN.
  * bf16 products are exact and summed in fp32; fp32 values are taken as three bf16 terms each, with the
- * products of terms down to 2^-16 of the first (an infinity may make its row's results NaN where the formula would not); a few rows (up to eight, or 24 without gradients) may be taken in fp32 as they are.  At most 2^44 logits.
+ * products of terms down to 2^-16 of the first (an infinity, or a value beyond bf16's largest, 3.38e38, may make its row's results NaN where the formula would not); a few rows (up to eight, or 24 without gradients) may be taken in fp32 as they are.  At most 2^44 logits.
  * workspace: device, 256-byte aligned, vgg19_linear_cross_entropy_bytes(layer, 0) bytes (0 for a layer that is refused; of pointers only the
  * alignment of x and w is looked at): scratch for the time of the call; calls that share one have to be ordered.  One of
  * vgg19_linear_cross_entropy_bytes(layer, 1) bytes does for this call and for the gradients.  The size holds for these sizes and this alignment
